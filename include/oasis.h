@@ -362,6 +362,106 @@ int oasis_append_kv_layers(const oasis_dims_t *dims, int32_t n_layers, const voi
                            void *const *hbm_pools, void *const *host_kvs, void *stream);
 
 /*
+ * A tree of drafted tokens (no counterpart in the paper, whose step verifies a chain of drafts; Sec. 4.2.1 stacks the
+ * verified token and the drafts into one call, and these three operators take that call to drafts that branch).
+ * One step of a request has n_nodes[b] <= n_tree <= OASIS_MAX_TREE nodes, node 0 first:
+ *   node 0      the verified token: its key and value are not in the cache yet, it is kept in any case;
+ *   parent      [B][n_tree] int32: the node that a node continues, parent[b][t] < t; anything outside [0, t) makes
+ *               the node a root (it continues the history).  A chain is parent[b][t] = t - 1;
+ *   n_nodes     [B] int32: nodes t >= n_nodes[b] are padding (values outside [0, n_tree] are clamped).  A request with
+ *               no node is a padded place of the batch: it is read and written nowhere.
+ * The nodes' keys and values stay in tree_kv until oasis_commit_kv writes the kept ones into the cache:
+ *   tree_kv     [B][n_tree][Hkv][2][128] bf16, key row then value row (the layout of oasis_append_kv's new_kv)
+ */
+#define OASIS_MAX_TREE 64
+
+/*
+ * Tree attention: node t of request b attends to the history in the working set, i.e. the tokens i of every column c
+ * with blk_tbl[b][h][c] = j >= 0 and j * 16 + i < seq_len[b] (seq_len [B] int32: tokens in the cache), to its
+ * ancestors in the tree and to itself.
+ *   out = softmax(scale * q K^T) V, bf16 tensor-core products with fp32 accumulation and fp32 softmax statistics.
+ *   q, out      [B][n_tree][Hq][128] bf16
+ *   tree_kv, parent, n_nodes as above; hbm_pool, slot_tbl, blk_tbl, n_cols as in oasis_sparse_attn
+ *   scale       finite and above zero
+ *   lse         optional [B][n_tree][Hq] fp32: natural-log sum of exponentials
+ *   workspace   device scratch of at least oasis_tree_attn_workspace_bytes() bytes, 16-byte aligned; contents undefined
+ *               before and after; may be NULL when that function returns 0.  Calls that may run at the same time (other
+ *               streams, captured graphs that are replayed together) need a workspace each.
+ * Rows t >= n_nodes[b] of out and lse are left as they were.  Positions that no node sees (history rows at or past
+ * seq_len[b], padding nodes) may hold anything, infinities and NaN included; every visible row must be finite.
+ * n_tree may not exceed OASIS_MAX_TREE; any group size n_q_heads / n_kv_heads up to 128 is taken.
+ */
+int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t n_tree, const void *tree_kv,
+                    const int32_t *parent, const int32_t *n_nodes, const void *hbm_pool,
+                    const int32_t *slot_tbl, const int32_t *blk_tbl, int32_t n_cols, const int32_t *seq_len,
+                    float scale, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Scratch bytes oasis_tree_attn needs for these shapes on the current device. */
+size_t oasis_tree_attn_workspace_bytes(const oasis_dims_t *dims, int32_t n_tree, int32_t n_cols);
+
+typedef enum { OASIS_F32 = 0, OASIS_BF16 = 1, OASIS_F16 = 2 } oasis_dtype_t;
+
+/*
+ * Verification of a tree of drafted tokens against the target model's logits.  Per request the walk starts at node 0
+ * and, at node x with the target distribution p = softmax(logits[b][x] / temperature[b]), tries x's children in
+ * ascending order; the first one that is kept is the next node of the walk.
+ *   temperature <= 0 (or NaN)   greedy: the child whose token is the row's largest logit (equal ones: lowest index).
+ *   temperature > 0, child c with token v, the draft's distribution q (draft_probs[b][x] if given, else all of it on v):
+ *       kept if      uniforms[b][c] * q(v) < p(v)
+ *       rejected     p becomes max(p - q, 0), normalised (without draft_probs: v is left out); were nothing left, p stays.
+ * This is speculative sampling: the kept tokens and the next one are distributed as the target's own samples, if the
+ * children of a node were drawn independently from draft_probs[b][x], or (without draft_probs) chosen without chance.
+ * Where no child is kept, or the path has max_path nodes, the walk ends and the next token is drawn from what p is by
+ * then: the lowest index at which the running sum of p exceeds uniforms[b][0] (greedy: the largest logit's index).
+ *   logits      element (b, x, v) at logits[b * logits_batch_stride + x * logits_row_stride + v], of type logits_type
+ *               (oasis_dtype_t); strides in elements, row stride >= vocab; any alignment of its type.  -infinity leaves
+ *               a token out, and so does NaN; +infinity shares all of p among the tokens that have it.
+ *   tokens      [B][n_tree] int32: the nodes' tokens (node 0's is not read); one outside [0, vocab) is never kept
+ *   uniforms    [B][n_tree] fp32 random numbers, taken into [0, 1 - 2^-24]
+ *   temperature [B] fp32
+ *   draft_probs optional fp32, element (b, x, v) at draft_probs[b * draft_batch_stride + x * draft_row_stride + v]
+ *   path        [B][max_path] int32: the nodes of the walk, node 0 first, then -1
+ *   n_commit    [B] int32: how many they are; 0 for a request without nodes
+ *   next_token  [B] int32: -1 for a request without nodes, and where every logit of the last node's row is left out
+ * Comparisons and sums that decide are made in 64 bits; the result does not depend on the launch.
+ * 1 <= n_tree <= OASIS_MAX_TREE, 1 <= max_path <= n_tree, 1 <= vocab <= OASIS_MAX_VOCAB.
+ */
+#define OASIS_MAX_VOCAB 4194304
+int oasis_verify_tree(int32_t batch, int32_t n_tree, int32_t vocab, const void *logits, int32_t logits_type,
+                      int64_t logits_batch_stride, int64_t logits_row_stride, const int32_t *tokens,
+                      const int32_t *parent, const int32_t *n_nodes, const float *uniforms, const float *temperature,
+                      const float *draft_probs, int64_t draft_batch_stride, int64_t draft_row_stride,
+                      int32_t *path, int32_t max_path, int32_t *n_commit, int32_t *next_token, void *stream);
+
+/*
+ * Commit of a verified path: like oasis_append_kv, for a different number of tokens per request and from rows that are
+ * picked by the path.  With L = seq_len[b] and n = n_commit[b] (taken into [0, max_path]), for every KV head h and i < n:
+ *   1. row path[b][i] of tree_kv goes to row (L + i) % 16 of the K part and of the V part of entry
+ *      slot_tbl[b][h][local_col + (j & 1)] of hbm_pool, j = (L + i) / 16, and of entry (block_table[b][j], h) of host_kv
+ *      (if host_kv is not NULL);
+ *   2. if n > 0 the local columns of blk_tbl are set as by oasis_local_window for n tokens at L: the blocks that hold the
+ *      kept tokens stay local.  A selection that is made after this step has to leave them out (n_full_blocks = L / 16);
+ *      a caller that selects among them as well calls oasis_local_window for the new length first;
+ *   3. next_len[b] = L + n (if next_len is not NULL; it may not be seq_len).
+ * Everything else is left as it was: with n = 0 only next_len is written.  A path entry outside [0, n_tree), a position
+ * outside the max_blocks of the request and a negative slot are skipped.
+ *   path        [B][max_path] int32 (device), 1 <= max_path <= 16;  n_commit, seq_len, next_len [B] int32 (device)
+ *   block_table [B][max_blocks], slot_tbl, blk_tbl [B][Hkv][n_cols] int32 (device), local_col + 2 <= n_cols
+ *   host_kv     the CPU full-KV pool (mapped pinned memory, or device memory)
+ * oasis_commit_kv_layers does the same for n_layers <= OASIS_MAX_APPEND_LAYERS layers in one launch (host arrays of
+ * per-layer device pointers): the path is known only after the last layer, so a step commits all layers at once.
+ */
+int oasis_commit_kv(const oasis_dims_t *dims, const void *tree_kv, int32_t n_tree, const int32_t *path, int32_t max_path,
+                    const int32_t *n_commit, const int32_t *seq_len, const int32_t *block_table,
+                    const int32_t *slot_tbl, int32_t *blk_tbl, int32_t n_cols, int32_t local_col, void *hbm_pool,
+                    void *host_kv, int32_t *next_len, void *stream);
+int oasis_commit_kv_layers(const oasis_dims_t *dims, int32_t n_layers, const void *const *tree_kvs, int32_t n_tree,
+                           const int32_t *path, int32_t max_path, const int32_t *n_commit, const int32_t *seq_len,
+                           const int32_t *const *block_tables, const int32_t *const *slot_tbls,
+                           int32_t *const *blk_tbls, int32_t n_cols, int32_t local_col, void *const *hbm_pools,
+                           void *const *host_kvs, int32_t *next_len, void *stream);
+
+/*
  * Head-union block set (Sec. 4.4.1, partial transfer: per layer the per-head selected sets are
  * united at block granularity -- a block is included if at least one KV head selected it -- and
  * the index of every included block is sent with its data).

@@ -25,7 +25,8 @@ SYMBOLS = ("oasis_build_summaries", "oasis_score_blocks", "oasis_select_topk",
            "oasis_offload_blocks", "oasis_attn_and_score", "oasis_attn_and_score_supported",
            "oasis_build_summaries_layers", "oasis_selftest_wait_timeout",
            "oasis_local_window", "oasis_append_kv", "oasis_append_kv_layers", "oasis_stage_blocks_layers", "oasis_stage_blocks_bulk",
-           "oasis_set_extents", "oasis_bounds_checked")
+           "oasis_set_extents", "oasis_bounds_checked",
+           "oasis_tree_attn", "oasis_tree_attn_workspace_bytes", "oasis_verify_tree", "oasis_commit_kv", "oasis_commit_kv_layers")
 
 
 class OasisError(RuntimeError):
@@ -107,6 +108,16 @@ def lib():
         L.oasis_set_extents.restype = ctypes.c_int
         L.oasis_bounds_checked.argtypes = []
         L.oasis_bounds_checked.restype = ctypes.c_int
+        L.oasis_tree_attn.argtypes = [dp, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, f32, vp, vp, vp, sz, vp]
+        L.oasis_tree_attn.restype = ctypes.c_int
+        L.oasis_tree_attn_workspace_bytes.argtypes = [dp, i32, i32]
+        L.oasis_tree_attn_workspace_bytes.restype = sz
+        L.oasis_verify_tree.argtypes = [i32, i32, i32, vp, i32, i64, i64, vp, vp, vp, vp, vp, vp, i64, i64, vp, i32, vp, vp, vp]
+        L.oasis_verify_tree.restype = ctypes.c_int
+        L.oasis_commit_kv.argtypes = [dp, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+        L.oasis_commit_kv.restype = ctypes.c_int
+        L.oasis_commit_kv_layers.argtypes = [dp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+        L.oasis_commit_kv_layers.restype = ctypes.c_int
         L.oasis_set_error_word.argtypes = [vp]
         L.oasis_set_error_word.restype = ctypes.c_int
         L.oasis_last_error.restype = ctypes.c_char_p
@@ -400,3 +411,159 @@ def stage_blocks_bulk(host_kvs, idx, slots, n, hbm_pools, max_streams=0, stream=
     _check(lib().oasis_stage_blocks_bulk(
         nl, mk(host_kvs, torch.bfloat16, "host_kvs"), mk(idx, torch.int64, "idx"), mk(slots, torch.int32, "slots"), int(n),
         mk(hbm_pools, torch.bfloat16, "hbm_pools"), int(max_streams), _stream(stream)), "oasis_stage_blocks_bulk")
+
+
+# ---- a tree of drafted tokens: attention, verification, commit ------------------------------------------------------
+MAX_TREE = 64
+_LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _dev(t, dtype, shape, name, device):
+    """Address of a dense tensor of this type and shape on `device` (the current device's index)."""
+    if t.dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current CUDA device" % name)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+def _pool_ptr(t, dtype, name, device, host_ok=False):
+    """Address of a pool of entries [..][2][16][128] in device memory (or, `host_ok`, pinned host memory)."""
+    if t.dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if t.shape[-3:] != (2, 16, 128) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous pool of [2][16][128] entries" % name)
+    if t.get_device() != device and not (host_ok and not t.is_cuda and t.is_pinned()):
+        raise ValueError("%s must be on the current CUDA device%s" % (name, " or in pinned host memory" if host_ok else ""))
+    return t.data_ptr()
+
+
+def _stream_id(stream):
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def tree_attn_workspace_bytes(dims, n_tree, n_cols) -> int:
+    d = dims.c()
+    return int(lib().oasis_tree_attn_workspace_bytes(ctypes.byref(d), int(n_tree), int(n_cols)))
+
+
+def tree_attn(dims, q, tree_kv, parent, n_nodes, hbm_pool, slot_tbl, blk_tbl, seq_len, scale, out, lse=None,
+              workspace=None, stream=None):
+    """Attention of a tree of drafted tokens over the working set: node t of request b sees the history (positions
+    below seq_len[b] in the columns of blk_tbl), its ancestors and itself.  q, out [B][T][Hq][128]; tree_kv
+    [B][T][Hkv][2][128]; parent [B][T], n_nodes [B] int32; rows of padding nodes are left as they were.
+    `workspace`: tree_attn_workspace_bytes() bytes where that is not zero."""
+    B, T, Hq, Hkv = dims.batch, q.shape[1], dims.n_q_heads, dims.n_kv_heads
+    n_cols = blk_tbl.shape[-1]
+    dev = torch.cuda.current_device()
+    bf, i32 = torch.bfloat16, torch.int32
+    d = dims.c()
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        raise ValueError("workspace must be contiguous and on the current CUDA device")
+    _check(lib().oasis_tree_attn(
+        ctypes.byref(d), _dev(q, bf, (B, T, Hq, 128), "q", dev), T, _dev(tree_kv, bf, (B, T, Hkv, 2, 128), "tree_kv", dev),
+        _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, (B,), "n_nodes", dev),
+        _pool_ptr(hbm_pool, bf, "hbm_pool", dev), _dev(slot_tbl, i32, (B, Hkv, n_cols), "slot_tbl", dev),
+        _dev(blk_tbl, i32, (B, Hkv, n_cols), "blk_tbl", dev), n_cols, _dev(seq_len, i32, (B,), "seq_len", dev), scale,
+        _dev(out, bf, (B, T, Hq, 128), "out", dev),
+        None if lse is None else _dev(lse, torch.float32, (B, T, Hq), "lse", dev),
+        None if workspace is None else workspace.data_ptr(), ws_bytes, _stream_id(stream)), "oasis_tree_attn")
+
+
+def _rows(t, name, B, T, V, dev):
+    """Address, batch stride and row stride of a [B][T][V] tensor whose rows are dense."""
+    if t.shape != (B, T, V):
+        raise ValueError("%s: expected shape %s, got %s" % (name, (B, T, V), tuple(t.shape)))
+    if t.get_device() != dev:
+        raise ValueError("%s must be on the current CUDA device" % name)
+    sb, sr, s1 = t.stride()
+    if s1 != 1 and V > 1:
+        raise ValueError("%s: the rows must be dense" % name)
+    if T == 1 and sr < V:
+        sr = V                                   # (the stride of a single row means nothing)
+    if sr < V or (sb < 0 and B > 1):
+        raise ValueError("%s: rows must not overlap" % name)
+    return t.data_ptr(), max(sb, 0), sr
+
+
+def verify_tree(logits, tokens, parent, n_nodes, uniforms, temperature, path, n_commit, next_token, draft_probs=None,
+                stream=None):
+    """Walks each request's tree of drafted tokens against the target's logits [B][T][V] (fp32, bf16 or fp16; rows
+    dense, any row and batch stride) and writes the kept path [B][max_path] (node 0 first, then -1), its length
+    n_commit [B] and the token that follows it, next_token [B].  uniforms [B][T] fp32: element c decides on node c,
+    element 0 draws the next token.  temperature [B] fp32: 0 is greedy.  draft_probs [B][T][V] fp32: row x is the
+    distribution that node x's children were drawn from; without it the drafts count as chosen without chance."""
+    if logits.dtype not in _LOGIT_TYPES:
+        raise TypeError("logits: expected float32, bfloat16 or float16, got %s" % logits.dtype)
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B][T][V]")
+    B, T, V = logits.shape
+    dev = torch.cuda.current_device()
+    i32, f32 = torch.int32, torch.float32
+    lp, lb, lr = _rows(logits, "logits", B, T, V, dev)
+    dp, db, dr = None, 0, 0
+    if draft_probs is not None:
+        if draft_probs.dtype != f32:
+            raise TypeError("draft_probs: expected float32, got %s" % draft_probs.dtype)
+        dp, db, dr = _rows(draft_probs, "draft_probs", B, T, V, dev)
+    M = path.shape[-1]
+    _check(lib().oasis_verify_tree(
+        B, T, V, lp, _LOGIT_TYPES[logits.dtype], lb, lr, _dev(tokens, i32, (B, T), "tokens", dev),
+        _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, (B,), "n_nodes", dev),
+        _dev(uniforms, f32, (B, T), "uniforms", dev), _dev(temperature, f32, (B,), "temperature", dev), dp, db, dr,
+        _dev(path, i32, (B, M), "path", dev), M, _dev(n_commit, i32, (B,), "n_commit", dev),
+        _dev(next_token, i32, (B,), "next_token", dev), _stream_id(stream)), "oasis_verify_tree")
+
+
+class CommitPlan:
+    """The buffers of all layers that `commit_kv_layers` writes, checked once: lists with one tensor per layer
+    (host_kvs: None, or a list in which a layer may be None).  Holds the tensors."""
+
+    def __init__(self, dims, tree_kvs, block_tables, slot_tbls, blk_tbls, local_col, hbm_pools, host_kvs=None):
+        n = len(tree_kvs)
+        host_kvs = [None] * n if host_kvs is None else list(host_kvs)
+        if not all(len(x) == n for x in (block_tables, slot_tbls, blk_tbls, hbm_pools, host_kvs)):
+            raise ValueError("one tensor per layer is needed in every list")
+        if not 1 <= n <= MAX_APPEND_LAYERS:
+            raise ValueError("%d layers outside [1, %d]" % (n, MAX_APPEND_LAYERS))
+        self.device = torch.cuda.current_device()
+        B, Hkv, dev = dims.batch, dims.n_kv_heads, self.device
+        self.T, self.n_cols, self.n_layers, self.local_col, self.batch = tree_kvs[0].shape[1], blk_tbls[0].shape[-1], n, int(local_col), B
+        arr = ctypes.c_void_p * n
+        bf, i32 = torch.bfloat16, torch.int32
+        self.dims = dims.c()
+        self.tree_kvs = arr(*[_dev(t, bf, (B, self.T, Hkv, 2, 128), "tree_kvs", dev) for t in tree_kvs])
+        self.block_tables = arr(*[_dev(t, i32, (B, dims.max_blocks), "block_tables", dev) for t in block_tables])
+        self.slot_tbls = arr(*[_dev(t, i32, (B, Hkv, self.n_cols), "slot_tbls", dev) for t in slot_tbls])
+        self.blk_tbls = arr(*[_dev(t, i32, (B, Hkv, self.n_cols), "blk_tbls", dev) for t in blk_tbls])
+        self.pools = arr(*[_pool_ptr(t, bf, "hbm_pools", dev) for t in hbm_pools])
+        self.host_kvs = arr(*[None if t is None else _pool_ptr(t, bf, "host_kvs", dev, host_ok=True) for t in host_kvs])
+        self._held = (tree_kvs, block_tables, slot_tbls, blk_tbls, hbm_pools, host_kvs)
+
+
+def commit_kv_layers(plan, path, n_commit, seq_len, next_len=None, stream=None):
+    """Writes the kept path [B][max_path] of every request (its first n_commit[b] nodes) from the layers' tree buffers
+    into their local windows and full-KV pools, sets the local columns, and next_len = seq_len + n_commit."""
+    B, dev, i32 = plan.batch, torch.cuda.current_device(), torch.int32
+    if dev != plan.device:
+        raise ValueError("the plan's buffers are on another device")
+    M = path.shape[-1]
+    _check(lib().oasis_commit_kv_layers(
+        plan.dims, plan.n_layers, plan.tree_kvs, plan.T, _dev(path, i32, (B, M), "path", dev), M,
+        _dev(n_commit, i32, (B,), "n_commit", dev), _dev(seq_len, i32, (B,), "seq_len", dev), plan.block_tables, plan.slot_tbls,
+        plan.blk_tbls, plan.n_cols, plan.local_col, plan.pools, plan.host_kvs,
+        None if next_len is None else _dev(next_len, i32, (B,), "next_len", dev), _stream_id(stream)), "oasis_commit_kv_layers")
+
+
+def commit_kv(dims, tree_kv, path, n_commit, seq_len, block_table, slot_tbl, blk_tbl, local_col, hbm_pool, host_kv=None,
+              next_len=None, stream=None):
+    """commit_kv_layers for one layer."""
+    commit_kv_layers(CommitPlan(dims, [tree_kv], [block_table], [slot_tbl], [blk_tbl], local_col, [hbm_pool], [host_kv]),
+                     path, n_commit, seq_len, next_len=next_len, stream=stream)

@@ -1,0 +1,134 @@
+// Commit of a verified path of a draft tree: the kept nodes' keys and values go from the step's tree buffer into the
+// local window of the working set and into the CPU full-KV pool, for all layers in one launch.
+//
+// One warp per (request, path position, KV head) of a layer: lanes 0-15 carry the 256-byte key row, lanes 16-31 the
+// value row, 16 bytes each; the warp of path position 0 also sets the row's two local columns.  Positions past the
+// request's n_commit end at once.  Traffic per layer: 512 B read and 2 x 512 B written per (request, kept token, head).
+#include "common.cuh"
+
+namespace oasis {
+
+constexpr int kCommitWarps = 8;
+
+struct CommitLayers {
+    const uint8_t *tree_kv[OASIS_MAX_APPEND_LAYERS];
+    const int32_t *block_table[OASIS_MAX_APPEND_LAYERS];
+    const int32_t *slot_tbl[OASIS_MAX_APPEND_LAYERS];
+    int32_t *blk_tbl[OASIS_MAX_APPEND_LAYERS];
+    uint8_t *pool[OASIS_MAX_APPEND_LAYERS];
+    uint8_t *host_kv[OASIS_MAX_APPEND_LAYERS];
+};
+
+struct CommitParams {
+    const int32_t *path, *n_commit, *seq_len;
+    int32_t *next_len;
+    int B, T, M, Hkv, max_blocks, n_cols, local_col;
+};
+
+__global__ void __launch_bounds__(kCommitWarps * 32)
+commit_kv_kernel(const __grid_constant__ CommitLayers ly, const CommitParams p, const Bounds bd)
+{
+    const int l = blockIdx.y, lane = threadIdx.x & 31;
+    const int total = p.B * p.M * p.Hkv;
+    for (int w = blockIdx.x * kCommitWarps + (threadIdx.x >> 5); w < total; w += gridDim.x * kCommitWarps) {
+        const int h = w % p.Hkv;
+        const int i = (w / p.Hkv) % p.M;
+        const int b = w / (p.Hkv * p.M);
+        const int n = max(0, min(p.n_commit[b], p.M));
+        const int L = p.seq_len[b];
+        if (p.next_len && l == 0 && h == 0 && i == 0 && lane == 0) p.next_len[b] = L + n;
+        if (i >= n) continue;
+        const int t = p.path[b * p.M + i];
+        const int pos = L + i, j = pos / kBlock, r = pos % kBlock;
+        const long long row = (long long)b * p.Hkv + h;
+        if (i == 0 && lane == 0) {
+            const int lo = L / kBlock, hi = (L + n - 1) / kBlock;
+            int32_t *cols = ly.blk_tbl[l] + row * p.n_cols + p.local_col;
+            cols[lo & 1] = lo;
+            cols[(lo & 1) ^ 1] = hi > lo ? hi : -1;
+        }
+        if (t < 0 || t >= p.T || pos < 0 || j >= p.max_blocks) {
+            if (kBoundsCheck && lane == 0 && j >= p.max_blocks) in_range(j, p.max_blocks, bd, kErrBlockId);
+            continue;
+        }
+        const int part = lane >> 4, off = (lane & 15) * 16;              // 0: key row, 1: value row
+        const uint4 v = *reinterpret_cast<const uint4 *>(ly.tree_kv[l] + (((long long)b * p.T + t) * p.Hkv + h) * 2 * kRowBytes +
+                                                         part * kRowBytes + off);
+        const long long slot = ly.slot_tbl[l][row * p.n_cols + p.local_col + (j & 1)];
+        const long long in_entry = (long long)part * kPartBytes + (long long)r * kRowBytes + off;
+        if (slot >= 0 && in_range(slot, bd.n_slots, bd, kErrSlot))
+            *reinterpret_cast<uint4 *>(ly.pool[l] + slot * kEntryBytes + in_entry) = v;
+        if (ly.host_kv[l]) {
+            const long long phys = ly.block_table[l][(long long)b * p.max_blocks + j];
+            if (phys >= 0 && in_range(phys * p.Hkv + h, bd.n_entries, bd, kErrHostEntry))
+                *reinterpret_cast<uint4 *>(ly.host_kv[l] + (phys * p.Hkv + h) * kEntryBytes + in_entry) = v;
+        }
+    }
+}
+
+static int launch_commit(const oasis_dims_t *dims, int n_layers, const void *const *tree_kvs, int T, const int32_t *path,
+                         int M, const int32_t *n_commit, const int32_t *seq_len, const int32_t *const *block_tables,
+                         const int32_t *const *slot_tbls, int32_t *const *blk_tbls, int n_cols, int local_col,
+                         void *const *pools, void *const *host_kvs, int32_t *next_len, cudaStream_t st, const char *who)
+{
+    if (int rc = check_dims(dims)) return rc;
+    if (n_layers < 0 || n_layers > OASIS_MAX_APPEND_LAYERS)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: n_layers %d outside [0, %d]", who, n_layers, OASIS_MAX_APPEND_LAYERS);
+    if (T < 1 || T > OASIS_MAX_TREE)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: n_tree %d outside [1, %d]", who, T, OASIS_MAX_TREE);
+    if (M < 1 || M > kBlock) return fail(OASIS_ERR_INVALID_ARG, "%s: max_path %d outside [1, %d]", who, M, kBlock);
+    if (local_col < 0 || n_cols < 2 || local_col > n_cols - 2)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: local columns %d and the next one outside the %d columns", who, local_col, n_cols);
+    if (!tree_kvs || !path || !n_commit || !seq_len || !block_tables || !slot_tbls || !blk_tbls || !pools)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
+    if (next_len == seq_len || next_len == n_commit)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: next_len may not be seq_len or n_commit", who);
+    CommitLayers ly = {};
+    for (int l = 0; l < n_layers; ++l) {
+        void *host = host_kvs ? host_kvs[l] : nullptr;
+        if (!tree_kvs[l] || !slot_tbls[l] || !blk_tbls[l] || !pools[l] || (host && !block_tables[l]))
+            return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer for layer %d", who, l);
+        if (!aligned16(tree_kvs[l]) || !aligned16(pools[l]) || !aligned16(host))
+            return fail(OASIS_ERR_INVALID_ARG, "%s: tree_kv, hbm_pool and host_kv must be 16-byte aligned (layer %d)", who, l);
+        ly.tree_kv[l] = (const uint8_t *)tree_kvs[l];
+        ly.block_table[l] = block_tables[l];
+        ly.slot_tbl[l] = slot_tbls[l];
+        ly.blk_tbl[l] = blk_tbls[l];
+        ly.pool[l] = (uint8_t *)pools[l];
+        ly.host_kv[l] = (uint8_t *)host;
+    }
+    const long long total = (long long)dims->batch * M * dims->n_kv_heads;
+    if (total > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: too many (request, token, head) rows", who);
+    if (total == 0 || n_layers == 0) return OASIS_OK;
+    CommitParams p;
+    p.path = path; p.n_commit = n_commit; p.seq_len = seq_len; p.next_len = next_len;
+    p.B = dims->batch; p.T = T; p.M = M; p.Hkv = dims->n_kv_heads; p.max_blocks = dims->max_blocks;
+    p.n_cols = n_cols; p.local_col = local_col;
+    long long grid = (total + kCommitWarps - 1) / kCommitWarps;
+    if (grid > 4096) grid = 4096;
+    prefer_max_shared_carveout(commit_kv_kernel);
+    commit_kv_kernel<<<dim3((unsigned)grid, (unsigned)n_layers), kCommitWarps * 32, 0, st>>>(ly, p, bounds());
+    return check_launch(who);
+}
+
+}  // namespace oasis
+
+extern "C" int oasis_commit_kv(const oasis_dims_t *dims, const void *tree_kv, int32_t n_tree, const int32_t *path,
+                               int32_t max_path, const int32_t *n_commit, const int32_t *seq_len,
+                               const int32_t *block_table, const int32_t *slot_tbl, int32_t *blk_tbl, int32_t n_cols,
+                               int32_t local_col, void *hbm_pool, void *host_kv, int32_t *next_len, void *stream)
+{
+    return oasis::launch_commit(dims, 1, &tree_kv, n_tree, path, max_path, n_commit, seq_len, &block_table, &slot_tbl, &blk_tbl,
+                                n_cols, local_col, &hbm_pool, &host_kv, next_len, (cudaStream_t)stream, "oasis_commit_kv");
+}
+
+extern "C" int oasis_commit_kv_layers(const oasis_dims_t *dims, int32_t n_layers, const void *const *tree_kvs, int32_t n_tree,
+                                      const int32_t *path, int32_t max_path, const int32_t *n_commit, const int32_t *seq_len,
+                                      const int32_t *const *block_tables, const int32_t *const *slot_tbls,
+                                      int32_t *const *blk_tbls, int32_t n_cols, int32_t local_col, void *const *hbm_pools,
+                                      void *const *host_kvs, int32_t *next_len, void *stream)
+{
+    return oasis::launch_commit(dims, n_layers, tree_kvs, n_tree, path, max_path, n_commit, seq_len, block_tables, slot_tbls,
+                                blk_tbls, n_cols, local_col, hbm_pools, host_kvs, next_len, (cudaStream_t)stream,
+                                "oasis_commit_kv_layers");
+}

@@ -534,57 +534,15 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return d;
 }
 
-// ---- one 64-key tile of the online softmax, shared by the attention kernel and the fused layer kernel --------
-// The calling thread owns one MMA row (one tensor-memory lane).  It reads its row of S = Q K^T for the blocks of
-// its copy, masks positions past `limit` (only tiles that hold a block of the local window need it), raises the
-// reference maximum lazily -- only when a logit exceeds it by 2^8; the O row in tensor memory is then rescaled,
-// after `wait_prev()` has made sure that the previous tile's P V has completed -- and writes P = 2^(s - m_ref),
-// rounded to bf16, back over S; the columns of the other copies' blocks get P = 0.  Running maximum and sum stay
-// in the thread's registers; there is no cross-thread reduction.
-//   s_tmem      tensor-memory address of the tile's S buffer at this thread's lane
-//   o_tmem      tensor-memory address of the O rows at this thread's lane
-//   tile_blk    the four block ids of the tile (shared memory), -1 = missing
-//   copy        which copy of the query rows this thread belongs to (0 when COPIES == 1)
-//   have_o      O already holds earlier tiles of this row (else there is nothing to rescale)
-// Returns false if wait_prev() gave up.
+// ---- the online softmax of one 64-key tile from the row's masked logits `x` on (arguments as in softmax_tile below) ----
 template <int COPIES, class WaitPrev>
-__device__ __forceinline__ bool softmax_tile(const uint32_t s_tmem, const uint32_t o_tmem, const int32_t *tile_blk, const int copy_in,
-                                             const int limit, const bool has_row, const float scale_log2, float &m_ref, float &l_sum,
+__device__ __forceinline__ bool softmax_rest(const float (&x)[kAtTileKeys / COPIES], const uint32_t s_tmem, const uint32_t o_tmem,
+                                             const int copy, const bool has_row, const float scale_log2, float &m_ref, float &l_sum,
                                              const bool have_o, WaitPrev &&wait_prev)
 {
     constexpr int BPC = kAtTileCols / COPIES;               // blocks of a tile each copy handles
     constexpr int KPC = BPC * kBlock;                       // keys of a tile each copy handles
-    const int copy = COPIES == 1 ? 0 : copy_in;
     bool alive = true;
-    int nvis[BPC];                                          // visible keys of each of this copy's blocks
-    bool masked = false;
-#pragma unroll
-    for (int c = 0; c < BPC; ++c) {
-        const int blk = tile_blk[copy * BPC + c];
-        int n = blk < 0 ? 0 : limit - blk * kBlock + 1;
-        n = max(0, min(n, kBlock));
-        nvis[c] = n;
-        masked |= has_row && n < kBlock;                    // lanes without an MMA row are zeroed below instead
-    }
-    masked = __any_sync(0xffffffffu, masked);
-    float x[KPC];
-    {
-        uint32_t v[BPC][16];
-#pragma unroll
-        for (int c = 0; c < BPC; ++c) tc_ld16_nowait(s_tmem + (copy * BPC + c) * 16, v[c]);
-        tc_wait_ld();
-#pragma unroll
-        for (int c = 0; c < BPC; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[c * 16 + e] = __uint_as_float(v[c][e]);
-    }
-    if (masked) {
-#pragma unroll
-        for (int c = 0; c < BPC; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (e >= nvis[c]) x[c * 16 + e] = -CUDART_INF_F;
-    }
     float mx4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
     for (int e = 4; e < KPC; e += 8) {                      // three-input maxima: two elements per instruction
@@ -660,6 +618,59 @@ __device__ __forceinline__ bool softmax_tile(const uint32_t s_tmem, const uint32
     }
     tc_wait_st();
     return alive;
+}
+
+// ---- one 64-key tile of the online softmax, shared by the attention kernel and the fused layer kernel --------
+// The calling thread owns one MMA row (one tensor-memory lane).  It reads its row of S = Q K^T for the blocks of
+// its copy, masks positions past `limit` (only tiles that hold a block of the local window need it), raises the
+// reference maximum lazily -- only when a logit exceeds it by 2^8; the O row in tensor memory is then rescaled,
+// after `wait_prev()` has made sure that the previous tile's P V has completed -- and writes P = 2^(s - m_ref),
+// rounded to bf16, back over S; the columns of the other copies' blocks get P = 0.  Running maximum and sum stay
+// in the thread's registers; there is no cross-thread reduction.
+//   s_tmem      tensor-memory address of the tile's S buffer at this thread's lane
+//   o_tmem      tensor-memory address of the O rows at this thread's lane
+//   tile_blk    the four block ids of the tile (shared memory), -1 = missing
+//   copy        which copy of the query rows this thread belongs to (0 when COPIES == 1)
+//   have_o      O already holds earlier tiles of this row (else there is nothing to rescale)
+// Returns false if wait_prev() gave up.
+template <int COPIES, class WaitPrev>
+__device__ __forceinline__ bool softmax_tile(const uint32_t s_tmem, const uint32_t o_tmem, const int32_t *tile_blk, const int copy_in,
+                                             const int limit, const bool has_row, const float scale_log2, float &m_ref, float &l_sum,
+                                             const bool have_o, WaitPrev &&wait_prev)
+{
+    constexpr int BPC = kAtTileCols / COPIES;               // blocks of a tile each copy handles
+    constexpr int KPC = BPC * kBlock;                       // keys of a tile each copy handles
+    const int copy = COPIES == 1 ? 0 : copy_in;
+    int nvis[BPC];                                          // visible keys of each of this copy's blocks
+    bool masked = false;
+#pragma unroll
+    for (int c = 0; c < BPC; ++c) {
+        const int blk = tile_blk[copy * BPC + c];
+        int n = blk < 0 ? 0 : limit - blk * kBlock + 1;
+        n = max(0, min(n, kBlock));
+        nvis[c] = n;
+        masked |= has_row && n < kBlock;                    // lanes without an MMA row are zeroed below instead
+    }
+    masked = __any_sync(0xffffffffu, masked);
+    float x[KPC];
+    {
+        uint32_t v[BPC][16];
+#pragma unroll
+        for (int c = 0; c < BPC; ++c) tc_ld16_nowait(s_tmem + (copy * BPC + c) * 16, v[c]);
+        tc_wait_ld();
+#pragma unroll
+        for (int c = 0; c < BPC; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[c * 16 + e] = __uint_as_float(v[c][e]);
+    }
+    if (masked) {
+#pragma unroll
+        for (int c = 0; c < BPC; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (e >= nvis[c]) x[c * 16 + e] = -CUDART_INF_F;
+    }
+    return softmax_rest<COPIES>(x, s_tmem, o_tmem, copy, has_row, scale_log2, m_ref, l_sum, have_o, wait_prev);
 }
 
 }  // namespace oasis

@@ -1,0 +1,709 @@
+// Attention of a tree of drafted tokens over the working set, on the 5th-generation tensor cores.
+//
+// A query row is (node t, query head a).  It sees the history in the row's columns (positions below seq_len) and, in the
+// tree buffer, its ancestors and itself.  The structure is that of the chain attention (attn_tc.cu, whose pieces in
+// tc_common.cuh it shares): work item = (request, KV head, row group, split of the column list), one thread block, the
+// group's query rows as the M rows of every MMA, tiles of four 16-key blocks in a ring of seven 32 KiB stages, warp 0 the
+// TMA producer, warps 1 and 2 the issuers of Q K^T and P V, the others softmax with one thread per MMA row.  What differs:
+//   - The keys are a list of blocks: the row's visible history blocks, then the blocks of the tree buffer, which comes
+//     through a tensor map of its own ([token][head][K, V] -> the same 8 KiB block image, nodes past n_tree read as
+//     zero).  The producer compacts: columns that are empty or lie past seq_len take no place in a tile and move no
+//     bytes, so a mostly empty resident table costs nothing; the other warps count the same columns meanwhile, because
+//     every role needs the number of tiles.
+//   - A block's visible keys are a 16-bit mask per row: a prefix for history blocks (the same for all rows), the node's
+//     ancestor bits for tree blocks.  Ancestors come from the parents by pointer doubling (six rounds for 64 nodes).
+//   - Key rows that no query may see hold anything, NaN included, and 0 x NaN is NaN in P V: before P is handed to the
+//     tensor core, the softmax warps overwrite those V rows with zeros in shared memory (masked tiles only).
+//   - More than 128 query rows are cut into row groups of equal size; the groups of a row are neighbouring thread blocks,
+//     which read the same entries at the same time, so all but one come from L2.
+// Algorithmic traffic: 8 KiB per (request, KV head, visible column), 512 B per (node, KV head), plus Q, O and lse.
+#include <cuda.h>
+#include <math_constants.h>
+
+#include "common.cuh"
+#include "tc_common.cuh"
+
+namespace oasis {
+
+constexpr int kTrThreads = 224;                             // producer, Q K^T issuer, P V issuer, four softmax warps
+__host__ __device__ constexpr int tr_threads(int mma_m, int copies) { return kTrThreads + (at_softmax_sets(mma_m, copies) - 1) * 128; }
+constexpr int kTrStages = 7;
+constexpr int32_t kTreeTag = 0x40000000;                    // tile_blk: kTreeTag + i = block i of the tree buffer
+// Behind the ring: 512 B of barriers and tile ids, two table windows, the producer's block queue, ancestor masks.
+constexpr int kTrQueue = 64;
+constexpr int kTrUp = 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 4) + 16 * kAtMaxStages;   // parents: behind barriers and tile ids
+constexpr int kTrMisc = 512 + 2 * kWinBytes + kTrQueue * 8 + OASIS_MAX_TREE * 8;
+constexpr size_t kTrSmem = 1024 + (size_t)kTrStages * kAtStageBytes + kTrMisc;
+static_assert(kTrUp + OASIS_MAX_TREE <= 512 && kTrSmem <= 232448, "shared memory of a thread block");
+
+struct TreeAttnParams {
+    const uint8_t *q;
+    const int32_t *slot_tbl, *blk_tbl, *seq_len, *parent, *n_nodes;
+    uint8_t *out;
+    float *lse;
+    float *part_o;      // [items][rows per group][128] fp32 (split runs only)
+    float *part_lse;    // [items][rows per group]      log2 domain
+    int32_t *err;
+    float scale_log2;
+    int T, Hq, Hkv, G, n_cols, R, n_splits, cols_per_split, n_groups, group_rows;
+    long long n_slots;  // bounds-check build: slots of the working-set pool (else unused)
+};
+
+__device__ __forceinline__ bool block_seen(int blk, int len) { return blk >= 0 && (long long)blk * kBlock < len; }
+
+template <int MMA_M, int COPIES>
+__global__ void __launch_bounds__(tr_threads(MMA_M, COPIES), 1)
+tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ CUtensorMap tree_map, const TreeAttnParams p)
+{
+    constexpr int RPC = MMA_M / COPIES;                     // MMA rows per copy of the query rows
+    constexpr int LANES = MMA_M / 4;                        // lanes of each softmax warp that hold an MMA row
+    constexpr int BPC = kAtTileCols / COPIES;               // blocks of a tile each copy handles
+    constexpr int SETS = at_softmax_sets(MMA_M, COPIES);    // softmax warp sets, taking alternate tiles
+    constexpr int SBUFS = at_s_bufs(SETS);                  // S / P buffers in tensor memory
+    constexpr int THREADS = tr_threads(MMA_M, COPIES);
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t kv_u32 = base;                                    // [stages][32 KiB]
+    uint8_t *misc = base_ptr + (size_t)kTrStages * kAtStageBytes;
+    const uint32_t bar_u32 = smem_u32(misc);
+    auto bar_full = [&](int s) { return bar_u32 + 8u * s; };
+    auto bar_empty = [&](int s) { return bar_u32 + 8u * (kAtMaxStages + s); };
+    auto bar_s_full = [&](int a) { return bar_u32 + 8u * (2 * kAtMaxStages + a); };
+    auto bar_p_full = [&](int a) { return bar_u32 + 8u * (2 * kAtMaxStages + kAtSBufs + a); };
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc + 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 2));
+    int32_t *s_count = reinterpret_cast<int32_t *>(misc + 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 2) + 4);
+    int32_t *tile_blk = reinterpret_cast<int32_t *>(misc + 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 4));   // [stages][4]
+    int32_t *win = reinterpret_cast<int32_t *>(misc + 512);                                             // two table windows
+    int2 *queue = reinterpret_cast<int2 *>(misc + 512 + 2 * kWinBytes);                                  // (block, slot)
+    unsigned long long *anc = reinterpret_cast<unsigned long long *>(queue + kTrQueue);                   // [T] ancestor masks
+    int8_t *up = reinterpret_cast<int8_t *>(misc + kTrUp);                                                // [T]
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // the merge launch behind this one (split runs) may bring its thread blocks onto the SMs already; it waits for the partials
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int grp = blockIdx.x % p.n_groups;
+    const int split = (blockIdx.x / p.n_groups) % p.n_splits;
+    const int bh = blockIdx.x / (p.n_groups * p.n_splits);
+    const int b = bh / p.Hkv, h = bh % p.Hkv;
+    const int n_nodes = max(0, min(p.n_nodes[b], p.T));
+    const int row0 = grp * p.group_rows;                             // first query row (node * G + head) of the group
+    const int rows = min(min(p.group_rows, p.R - row0), n_nodes * p.G - row0);
+    if (rows <= 0) return;                                           // only padding nodes: nothing is read or written
+    const int c0 = split * p.cols_per_split;
+    const int c1 = min(c0 + p.cols_per_split, p.n_cols);
+    const int L = p.seq_len[b];
+    // blocks of the tree buffer that the group's rows may see (ancestors have lower indices), taken by the last split
+    const int n_tree_blk = split == p.n_splits - 1 ? (row0 + rows - 1) / p.G / kBlock + 1 : 0;
+    const int32_t *slot_row = p.slot_tbl + (long long)bh * p.n_cols;
+    const int32_t *blk_row = p.blk_tbl + (long long)bh * p.n_cols;
+
+    // ---- set-up: barriers, tensor memory, Q operand, ancestor masks, number of tiles -------------------
+    if (tid == 0) {
+        for (int s = 0; s < kAtMaxStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+        for (int a = 0; a < kAtSBufs; ++a) { mbar_init(bar_s_full(a), 1); mbar_init(bar_p_full(a), 4); }
+        *s_count = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();                             // the barriers exist; the producer starts copying right away
+    uint32_t tmem_base = 0, tmem_o = 0, tmem_q = 0;
+    int n_tiles = 0;
+    if (warp != 0) {
+        // Meanwhile: warp 1 allocates the tensor memory, warp 2 works out the ancestors, all count the visible columns,
+        // and every softmax thread of the first set, owner of one MMA row, loads that row of Q (rows are replicated
+        // across the copies, rows past the group's are zero) and then stores it to its tensor-memory lane.
+        if (warp == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                         ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)kAtTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+        int seen = 0;
+        for (int c = c0 + tid - 32; c < c1; c += THREADS - 32) seen += block_seen(blk_row[c], L);
+        seen = __reduce_add_sync(0xffffffffu, seen);
+        if (lane == 0 && seen) atomicAdd(s_count, seen);
+        if (warp == 2) {
+            unsigned long long m[2];
+            int u[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int t = lane + 32 * e;
+                const int par = t < n_nodes ? p.parent[(long long)b * p.T + t] : -1;
+                u[e] = par >= 0 && par < t ? par : -1;
+                m[e] = 1ull << t;
+            }
+#pragma unroll 1
+            for (int round = 0; round < 6; ++round) {
+                __syncwarp();
+#pragma unroll
+                for (int e = 0; e < 2; ++e) { anc[lane + 32 * e] = m[e]; up[lane + 32 * e] = (int8_t)u[e]; }
+                __syncwarp();
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (u[e] >= 0) { m[e] |= anc[u[e]]; u[e] = up[u[e]]; }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) anc[lane + 32 * e] = m[e];
+        }
+        uint4 v[16];
+        if (warp >= 3 && warp < 7) {
+            const int m_row = (warp & 3) * LANES + lane;
+            const int r = m_row % RPC;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) v[c] = make_uint4(0, 0, 0, 0);
+            if (lane < LANES && r < rows) {
+                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + ((((long long)b * p.T + tq) * p.Hq + a) * kHeadDim) * 2);
+#pragma unroll
+                for (int c = 0; c < 16; ++c) v[c] = src[c];
+            }
+        }
+        tc_fence_before();
+        asm volatile("bar.sync 2, %0;" ::"n"(THREADS - 32) : "memory");
+        tc_fence_after();
+        n_tiles = (*s_count + n_tree_blk + kAtTileCols - 1) / kAtTileCols;
+        tmem_base = *tmem_slot;
+        tmem_o = tmem_base + SBUFS * kAtTileKeys;
+        tmem_q = tmem_o + SETS * kHeadDim;                           // Q as the A operand: 128 rows x 64 packed columns
+        if (warp >= 3 && warp < 7) q_row_to_tmem(tmem_q + ((uint32_t)((warp & 3) * 32) << 16), v);
+        tc_fence_before();
+        asm volatile("bar.sync 2, %0;" ::"n"(THREADS - 32) : "memory");
+        tc_fence_after();
+    }
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- producer
+        // Table entries come 32 columns at a time through two window buffers, one window ahead; the visible ones go into
+        // a queue, and every four of them are a tile.
+        const uint32_t win_u32 = smem_u32(win);
+        bool alive = true;
+        int s = 0, head = 0, tail = 0;
+        uint32_t ph = 1;                                             // parity of the "empty" phase to wait for
+        auto emit = [&](int count) {                                 // the queue's next `count` <= 4 blocks as a tile
+            int blk = -1, slot = -1;
+            if (lane < count) {
+                const int2 e = queue[(head + lane) & (kTrQueue - 1)];
+                blk = e.x;
+                slot = e.y;
+                if (kBoundsCheck && blk < kTreeTag && !in_range(slot, p.n_slots, Bounds{0, 0, p.err}, kErrSlot)) blk = -1;
+            }
+            head += count;
+            if (lane == 0) alive = mbar_wait(bar_empty(s), ph, p.err, 41);
+            alive = __shfl_sync(0xffffffffu, (int)alive, 0) != 0;
+            if (!alive) return;
+            uint8_t *stage = base_ptr + (size_t)s * kAtStageBytes;
+            const uint32_t stage_u32 = kv_u32 + s * kAtStageBytes;
+            const unsigned valid = __ballot_sync(0xffffffffu, lane < kAtTileCols && blk >= 0);
+            if (lane < kAtTileCols) tile_blk[s * kAtTileCols + lane] = blk;
+            if ((valid & 0xfu) != 0xfu) {
+                // a missing block contributes P = 0, which must not meet stale NaN patterns: the warp zeroes its V image
+#pragma unroll
+                for (int c = 0; c < kAtTileCols; ++c) {
+                    if ((valid >> c) & 1u) continue;
+                    uint8_t *dst = stage + c * kEntryBytes + (lane >> 4) * kImgGroup + ((lane >> 3) & 1) * kImgHalf + kImgPart + (lane & 7) * 128;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4 *>(dst + j * 16) = make_uint4(0, 0, 0, 0);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive_expect_tx(bar_full(s), (uint32_t)__popc(valid) * kEntryBytes);
+            __syncwarp();
+            if (lane < kAtTileCols && blk >= 0) {
+                const uint32_t dst = stage_u32 + lane * kEntryBytes;
+                if (blk < kTreeTag) {
+                    tma_load_5d(dst, &pool_map, 0, 0, 2 * slot, 0, 0, bar_full(s));
+                } else {                                             // the two 8-node groups of a tree block
+                    const int t = (blk - kTreeTag) * kBlock;
+                    tma_load_5d(dst, &tree_map, 0, t, 2 * h, 0, b, bar_full(s));
+                    tma_load_5d(dst + kImgGroup, &tree_map, 0, t + 8, 2 * h, 0, b, bar_full(s));
+                }
+            }
+            ph ^= (s + 1 == kTrStages);
+            s = (s + 1 == kTrStages) ? 0 : s + 1;
+        };
+        if (c0 < c1) window_request(win_u32, lane, blk_row, slot_row, c0 + lane, c1);
+        for (int c = c0, w = 0; c < c1 && alive; c += kWinCols, w ^= 1) {
+            window_wait();
+            if (c + kWinCols < c1) window_request(win_u32 + (w ^ 1) * kWinBytes, lane, blk_row, slot_row, c + kWinCols + lane, c1);
+            const int blk = win[w * (2 * kWinCols) + lane], slot = win[w * (2 * kWinCols) + kWinCols + lane];
+            const bool ok = block_seen(blk, L);                      // (columns past c1 are -1)
+            const unsigned got = __ballot_sync(0xffffffffu, ok);
+            if (ok) queue[(tail + __popc(got & ((1u << lane) - 1u))) & (kTrQueue - 1)] = make_int2(blk, slot);
+            tail += __popc(got);
+            __syncwarp();
+            while (alive && tail - head >= kAtTileCols) emit(kAtTileCols);
+        }
+        if (n_tree_blk > 0) {                                        // at most 3 + 4 entries are in the queue then
+            if (lane < n_tree_blk) queue[(tail + lane) & (kTrQueue - 1)] = make_int2(kTreeTag + lane, 0);
+            tail += n_tree_blk;
+            __syncwarp();
+        }
+        while (alive && tail > head) emit(min(kAtTileCols, tail - head));
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- Q K^T issuer (the whole warp, converged)
+        const uint32_t idesc = idesc_qk(MMA_M);
+        const uint64_t k_desc0 = smem_desc_sw128_k(kv_u32, kImgGroup);
+        bool alive = true;
+        int s = 0, sb = 0, s_old = 0;                                // stage and S buffer of tile i; stage of tile i - SBUFS
+        uint32_t ph = 0, ph_old = 0;
+        for (int i = 0; i < n_tiles && alive; ++i) {
+            // the S buffer also held P of tile i - SBUFS: its P V must have completed
+            if (i >= SBUFS) {
+                alive = mbar_wait_warp(bar_empty(s_old), ph_old, p.err, 51);
+                ph_old ^= (s_old + 1 == kTrStages);
+                s_old = (s_old + 1 == kTrStages) ? 0 : s_old + 1;
+            }
+            alive = alive && mbar_wait_warp(bar_full(s), ph, p.err, 52);
+            if (!alive) break;
+            tc_fence_after();
+            const uint64_t k_desc = k_desc0 + (uint64_t)((s * kAtStageBytes) >> 4);
+            issue_qk_tile(tmem_base + (uint32_t)(sb * kAtTileKeys), tmem_q, k_desc, idesc);
+            tc_commit(bar_s_full(sb));
+            ph ^= (s + 1 == kTrStages);
+            s = (s + 1 == kTrStages) ? 0 : s + 1;
+            sb = (sb + 1 == SBUFS) ? 0 : sb + 1;
+        }
+    } else if (warp == 2) {
+        // ---------------------------------------------------------------- P V issuer (the whole warp, converged)
+        const uint32_t idesc = idesc_pv(MMA_M);
+        const uint64_t v_desc0 = smem_desc_sw128_mn(kv_u32 + kImgPart, kImgHalf, kImgGroup);
+        bool alive = true;
+        int s = 0, sb = 0;
+        uint32_t ph_p = 0;
+        for (int i = 0; i < n_tiles && alive; ++i) {
+            alive = mbar_wait_warp(bar_p_full(sb), ph_p, p.err, 53);
+            if (!alive) break;
+            tc_fence_after();
+            const uint64_t v_desc = v_desc0 + (uint64_t)((s * kAtStageBytes) >> 4);
+            issue_pv_tile(tmem_o + (uint32_t)((i % SETS) * kHeadDim), tmem_base + (uint32_t)(sb * kAtTileKeys), v_desc, idesc, i < SETS);
+            tc_commit(bar_empty(s));                                 // stage free, and O complete up to this tile
+            s = (s + 1 == kTrStages) ? 0 : s + 1;
+            sb = (sb + 1 == SBUFS) ? 0 : sb + 1;
+            ph_p ^= (sb == 0);
+        }
+    } else {
+        // ---------------------------------------------------------------- softmax, one thread per MMA row
+        const int set = SETS == 2 ? (warp - 3) >> 2 : 0;
+        const int quarter = warp & 3;
+        const int m_row = quarter * LANES + (lane % LANES);         // MMA row held by this tensor-memory lane
+        const int copy = m_row / RPC, row = m_row % RPC;            // which copy of the rows, which query row of the group
+        const bool has_row = lane < LANES;
+        const bool live_row = has_row && row < rows;
+        const bool live_warp = (quarter * LANES) % RPC < rows;      // some lane of this warp holds a query row
+        const unsigned long long sees = live_row ? anc[(row0 + row) / p.G] : 0ull;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const int worker = quarter * 32 + lane;                     // of the set's 128 threads
+        float m_ref = -CUDART_INF_F, l_sum = 0.f;
+        bool alive = true;
+        int s = 0, s_prev = 0;                                      // ring stage of tile i and of this set's previous tile
+        uint32_t ph = 0, ph_prev = 0;                               // parities of the "empty" phases that end those tiles
+        int sb = set;                                               // S buffer of tile i (SETS < SBUFS)
+        uint32_t ph_s = 0;
+        ring_advance(s, ph, set, kTrStages);
+        const uint32_t my_o = tmem_o + (uint32_t)(set * kHeadDim) + lane_base;   // this thread's O row
+        for (int i = set; i < n_tiles && alive; i += SETS) {
+            alive = mbar_wait(bar_s_full(sb), ph_s, p.err, 61);
+            if (!alive) break;
+            tc_fence_after();
+            const int32_t *ids = tile_blk + s * kAtTileCols;
+            // V rows that nobody may see: history positions from seq_len on, padding nodes.  Thread -> (block, key, half).
+            {
+                const int c = worker >> 5, key = (worker >> 1) & 15, half = worker & 1;
+                const int blk = ids[c];
+                const int valid = blk < kTreeTag ? L - blk * kBlock : n_nodes - (blk - kTreeTag) * kBlock;
+                if (blk >= 0 && key >= valid) {
+                    uint8_t *dst = base_ptr + (size_t)s * kAtStageBytes + c * kEntryBytes + (key >> 3) * kImgGroup + half * kImgHalf +
+                                   kImgPart + (key & 7) * 128;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4 *>(dst + j * 16) = make_uint4(0, 0, 0, 0);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+            }
+            const uint32_t s_tmem = tmem_base + lane_base + (uint32_t)(sb * kAtTileKeys);
+            if (live_warp) {
+                uint32_t bits[BPC];                                 // visible keys of each of this copy's blocks
+                bool masked = false;
+#pragma unroll
+                for (int c = 0; c < BPC; ++c) {
+                    const int blk = ids[copy * BPC + c];
+                    uint32_t m = 0xffffu;                           // lanes without a query row need no masking
+                    if (live_row) {
+                        if (blk < 0) m = 0;
+                        else if (blk < kTreeTag) m = L - blk * kBlock < kBlock ? (1u << (L - blk * kBlock)) - 1u : 0xffffu;
+                        else m = (uint32_t)(sees >> ((blk - kTreeTag) * kBlock)) & 0xffffu;
+                    }
+                    bits[c] = m;
+                    masked |= m != 0xffffu;
+                }
+                masked = __any_sync(0xffffffffu, masked);
+                float x[BPC * kBlock];
+                {
+                    uint32_t v[BPC][16];
+#pragma unroll
+                    for (int c = 0; c < BPC; ++c) tc_ld16_nowait(s_tmem + (copy * BPC + c) * 16, v[c]);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < BPC; ++c)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[c * 16 + e] = __uint_as_float(v[c][e]);
+                }
+                if (masked) {
+#pragma unroll
+                    for (int c = 0; c < BPC; ++c)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (!((bits[c] >> e) & 1u)) x[c * 16 + e] = -CUDART_INF_F;
+                }
+                alive = softmax_rest<COPIES>(x, s_tmem, my_o, copy, has_row, p.scale_log2, m_ref, l_sum, i >= SETS,
+                                             // (the stage of this set's previous tile is released by the commit that follows
+                                             // its P V; with at least four stages in the ring the parity is unambiguous)
+                                             [&] { return mbar_wait(bar_empty(s_prev), ph_prev, p.err, 62); });
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_p_full(sb));
+            s_prev = s;
+            ph_prev = ph;
+            ring_advance(s, ph, SETS, kTrStages);
+#pragma unroll
+            for (int k = 0; k < SETS; ++k) {
+                sb = (sb + 1 == SBUFS) ? 0 : sb + 1;
+                ph_s ^= (sb == 0);
+            }
+        }
+        // ---- epilogue: merge the copies or sets, normalise, write out ----------------------------------------
+        if (alive && n_tiles > 0)
+            alive = mbar_wait(bar_empty((n_tiles - 1) % kTrStages), ((n_tiles - 1) / kTrStages) & 1, p.err, 63);
+        tc_fence_after();
+        // the K/V ring is idle now: stage the O rows there.  [128 MMA rows][132 floats], then max and sum.
+        float *o_sm = reinterpret_cast<float *>(base_ptr);
+        float *m_sm = o_sm + 128 * 132;
+        float *l_sm = m_sm + 128 * SETS;
+        const bool run = n_tiles > 0 && live_warp && alive;
+        // d0 .. d0 + 16 n of one row: acc * inv as bf16, or as a partial
+        auto place = [&](int r, long long &orow, float *&part) {
+            const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+            orow = ((long long)b * p.T + tq) * p.Hq + a;
+            part = p.part_o + ((long long)blockIdx.x * p.group_rows + r) * kHeadDim;
+        };
+        if (SETS == 2) {
+            // the two threads of a row exchange maximum and sum; each then merges and writes one half of the output dims,
+            // reading both O accumulators at its own tensor-memory lane
+            m_sm[set * 128 + m_row] = m_ref;
+            l_sm[set * 128 + m_row] = l_sum;
+            asm volatile("bar.sync 1, 256;" ::: "memory");          // the eight softmax warps
+            const float m_o = m_sm[(set ^ 1) * 128 + m_row], l_o = l_sm[(set ^ 1) * 128 + m_row];
+            const float mx = fmaxf(m_ref, m_o);
+            const float w_me = mx == -CUDART_INF_F ? 0.f : fast_exp2(m_ref - mx), w_ot = mx == -CUDART_INF_F ? 0.f : fast_exp2(m_o - mx);
+            const float den = w_me * l_sum + w_ot * l_o;
+            const float inv = den > 0.f ? 1.f / den : 0.f;
+            const float lse2 = den > 0.f ? mx + log2f(den) : -CUDART_INF_F;
+            const float w_a = set == 0 ? w_me : w_ot, w_b = set == 0 ? w_ot : w_me;   // weights of the first and second accumulator
+            long long orow;
+            float *part;
+            place(row, orow, part);
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                const int d0 = set * 64 + c * 16;
+                uint32_t va[16], vb[16];
+                if (run) {
+                    tc_ld16(tmem_o + lane_base + d0, va);
+                    tc_ld16(tmem_o + kHeadDim + lane_base + d0, vb);
+                }
+                if (!(live_row && alive)) continue;
+                float acc[16];
+                // an accumulator whose set saw no key (weight 0) may never have been written: its contents do not enter
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    acc[e] = ((w_a != 0.f ? w_a * __uint_as_float(va[e]) : 0.f) + (w_b != 0.f ? w_b * __uint_as_float(vb[e]) : 0.f)) * inv;
+                if (p.n_splits == 1) {
+                    uint4 *dst = reinterpret_cast<uint4 *>(p.out + (orow * kHeadDim + d0) * 2);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        dst[e] = make_uint4(pack_bf16x2(acc[8 * e], acc[8 * e + 1]), pack_bf16x2(acc[8 * e + 2], acc[8 * e + 3]),
+                                            pack_bf16x2(acc[8 * e + 4], acc[8 * e + 5]), pack_bf16x2(acc[8 * e + 6], acc[8 * e + 7]));
+                } else {
+                    float4 *dst = reinterpret_cast<float4 *>(part + d0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dst[e] = make_float4(acc[4 * e], acc[4 * e + 1], acc[4 * e + 2], acc[4 * e + 3]);
+                }
+            }
+            if (live_row && alive && set == 0) {
+                if (p.n_splits == 1) { if (p.lse) p.lse[orow] = lse2 * kAtLn2; }
+                else p.part_lse[(long long)blockIdx.x * p.group_rows + row] = lse2;
+            }
+        } else {
+            // several copies: their O rows meet in shared memory; the MMA_M (row, slice of the output dims) tasks go to the
+            // first MMA_M softmax threads
+            if (run) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t v[16];
+                    tc_ld16(tmem_o + lane_base + c * 16, v);
+                    float4 *dst = reinterpret_cast<float4 *>(o_sm + m_row * 132 + c * 16);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (has_row) dst[e] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]),
+                                             __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+                }
+            }
+            if (has_row) {
+                m_sm[m_row] = m_ref;
+                l_sm[m_row] = l_sum;
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");          // the four softmax warps
+            const int r = worker % RPC, dpart = worker / RPC;
+            constexpr int DLEN = kHeadDim / COPIES;
+            const int d0 = dpart * DLEN;
+            if (worker < MMA_M && r < rows && alive) {
+                float acc[DLEN], mw[COPIES], wt[COPIES];
+                float mx = -CUDART_INF_F, den = 0.f;
+#pragma unroll
+                for (int c = 0; c < COPIES; ++c) {
+                    mw[c] = m_sm[c * RPC + r];
+                    mx = fmaxf(mx, mw[c]);
+                }
+#pragma unroll
+                for (int c = 0; c < COPIES; ++c) {
+                    wt[c] = mx == -CUDART_INF_F ? 0.f : fast_exp2(mw[c] - mx);
+                    den += wt[c] * l_sm[c * RPC + r];
+                }
+#pragma unroll
+                for (int e = 0; e < DLEN; ++e) acc[e] = 0.f;
+                if (n_tiles > 0) {
+#pragma unroll
+                    for (int c = 0; c < COPIES; ++c) {
+                        if (wt[c] == 0.f) continue;                  // a copy that saw no key
+                        const float4 *src = reinterpret_cast<const float4 *>(o_sm + (c * RPC + r) * 132 + d0);
+#pragma unroll
+                        for (int e = 0; e < DLEN / 4; ++e) {
+                            const float4 f = src[e];
+                            acc[4 * e] += wt[c] * f.x; acc[4 * e + 1] += wt[c] * f.y;
+                            acc[4 * e + 2] += wt[c] * f.z; acc[4 * e + 3] += wt[c] * f.w;
+                        }
+                    }
+                }
+                const float inv = den > 0.f ? 1.f / den : 0.f;
+                const float lse2 = den > 0.f ? mx + log2f(den) : -CUDART_INF_F;
+                long long orow;
+                float *part;
+                place(r, orow, part);
+                if (p.n_splits == 1) {
+                    uint4 *dst = reinterpret_cast<uint4 *>(p.out + (orow * kHeadDim + d0) * 2);
+#pragma unroll
+                    for (int e = 0; e < DLEN / 8; ++e)
+                        dst[e] = make_uint4(pack_bf16x2(acc[8 * e] * inv, acc[8 * e + 1] * inv),
+                                            pack_bf16x2(acc[8 * e + 2] * inv, acc[8 * e + 3] * inv),
+                                            pack_bf16x2(acc[8 * e + 4] * inv, acc[8 * e + 5] * inv),
+                                            pack_bf16x2(acc[8 * e + 6] * inv, acc[8 * e + 7] * inv));
+                    if (p.lse && dpart == 0) p.lse[orow] = lse2 * kAtLn2;
+                } else {
+                    float4 *dst = reinterpret_cast<float4 *>(part + d0);
+#pragma unroll
+                    for (int e = 0; e < DLEN / 4; ++e)
+                        dst[e] = make_float4(acc[4 * e] * inv, acc[4 * e + 1] * inv, acc[4 * e + 2] * inv, acc[4 * e + 3] * inv);
+                    if (dpart == 0) p.part_lse[(long long)blockIdx.x * p.group_rows + r] = lse2;
+                }
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)kAtTmemCols)
+                     : "memory");
+    }
+}
+
+// Merges the splits of one query row: out = sum_s w_s o_s / sum_s w_s with w_s = 2^(lse_s - max lse).  One warp per row,
+// four output dims per thread, the loads of four splits in flight at a time.
+__global__ void __launch_bounds__(256)
+tree_combine_kernel(const TreeAttnParams p, int total)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int wi = 8 * blockIdx.x + (threadIdx.x >> 5);
+    if (wi >= total) return;
+    const int row = wi % p.R, bh = wi / p.R;
+    const int b = bh / p.Hkv, h = bh % p.Hkv;
+    const int tq = row / p.G, a = h * p.G + row % p.G;
+    if (tq >= p.n_nodes[b]) return;
+    const int grp = row / p.group_rows, r = row % p.group_rows;
+    const long long prow0 = ((long long)bh * p.n_splits * p.n_groups + grp) * p.group_rows + r;    // partial row of split 0
+    const long long pstride = (long long)p.n_groups * p.group_rows;
+    float mx = -CUDART_INF_F;
+    for (int s = lane; s < p.n_splits; s += 32) mx = fmaxf(mx, p.part_lse[prow0 + s * pstride]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float den = 0.f;
+    if (mx > -CUDART_INF_F) {
+#pragma unroll 1
+        for (int s0 = 0; s0 < p.n_splits; s0 += 4) {
+            float w[4];
+            float4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const bool in = s0 + u < p.n_splits;
+                const long long prow = prow0 + (in ? s0 + u : s0) * pstride;
+                w[u] = in ? p.part_lse[prow] : -CUDART_INF_F;
+                v[u] = reinterpret_cast<const float4 *>(p.part_o + prow * kHeadDim)[lane];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float ws = fast_exp2(w[u] - mx);               // 0 for the splits past the last one
+                acc.x += ws * v[u].x; acc.y += ws * v[u].y; acc.z += ws * v[u].z; acc.w += ws * v[u].w;
+                den += ws;
+            }
+        }
+    }
+    const bool any = den > 0.f;                                      // some split saw a key
+    if (!any) den = 1.f;
+    const long long orow = ((long long)b * p.T + tq) * p.Hq + a;
+    reinterpret_cast<uint2 *>(p.out + orow * kHeadDim * 2)[lane] =
+        make_uint2(pack_bf16x2(acc.x / den, acc.y / den), pack_bf16x2(acc.z / den, acc.w / den));
+    if (p.lse && lane == 0) p.lse[orow] = any ? (mx + log2f(den)) * kAtLn2 : -CUDART_INF_F;
+}
+
+// ---- host side -----------------------------------------------------------------------------------------
+struct TreePlan {
+    int n_groups, group_rows, n_splits, cols_per_split;
+    long long items;
+    size_t workspace;
+};
+
+static TreePlan tree_plan(const oasis_dims_t *dims, int T, int n_cols)
+{
+    TreePlan pl;
+    const int R = T * (dims->n_q_heads / dims->n_kv_heads);
+    pl.n_groups = (R + 127) / 128;
+    pl.group_rows = (R + pl.n_groups - 1) / pl.n_groups;
+    // all thread blocks resident at once (one per SM) as far as the column list can be split, eight columns per split
+    const long long items = (long long)dims->batch * dims->n_kv_heads * pl.n_groups;
+    long long s = items > 0 ? sm_count() / items : 1;
+    const long long most = (n_cols + 7) / 8;
+    if (s > most) s = most;
+    if (s < 1) s = 1;
+    pl.cols_per_split = (int)((n_cols + s - 1) / s);
+    pl.n_splits = (n_cols + pl.cols_per_split - 1) / pl.cols_per_split;
+    pl.items = items * pl.n_splits;
+    pl.workspace = pl.n_splits > 1 ? (size_t)pl.items * pl.group_rows * (kHeadDim + 1) * sizeof(float) : 0;
+    return pl;
+}
+
+static int check_tree(const oasis_dims_t *dims, int T, int n_cols, const char *who)
+{
+    if (int rc = check_dims(dims)) return rc;
+    if (T < 1 || T > OASIS_MAX_TREE)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: n_tree %d outside [1, %d]", who, T, OASIS_MAX_TREE);
+    if (n_cols < 1 || n_cols > (1 << 26)) return fail(OASIS_ERR_INVALID_ARG, "%s: n_cols %d", who, n_cols);
+    const int G = dims->n_q_heads / dims->n_kv_heads;
+    if (G > 128) return fail(OASIS_ERR_UNSUPPORTED, "%s: %d query heads per KV head > 128", who, G);
+    if ((long long)dims->batch * dims->n_kv_heads * T * G > 0x7fffffffLL)
+        return fail(OASIS_ERR_UNSUPPORTED, "%s: more than 2^31 query rows", who);
+    return OASIS_OK;
+}
+
+}  // namespace oasis
+
+extern "C" size_t oasis_tree_attn_workspace_bytes(const oasis_dims_t *dims, int32_t n_tree, int32_t n_cols)
+{
+    using namespace oasis;
+    if (check_tree(dims, n_tree, n_cols, "oasis_tree_attn_workspace_bytes") != OASIS_OK) return 0;
+    return tree_plan(dims, n_tree, n_cols).workspace;
+}
+
+extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t n_tree, const void *tree_kv,
+                               const int32_t *parent, const int32_t *n_nodes, const void *hbm_pool,
+                               const int32_t *slot_tbl, const int32_t *blk_tbl, int32_t n_cols, const int32_t *seq_len,
+                               float scale, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace oasis;
+    const char *who = "oasis_tree_attn";
+    if (int rc = check_tree(dims, n_tree, n_cols, who)) return rc;
+    if (!q || !tree_kv || !parent || !n_nodes || !hbm_pool || !slot_tbl || !blk_tbl || !seq_len || !out)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
+    if (!aligned16(q) || !aligned16(tree_kv) || !aligned16(hbm_pool) || !aligned16(out))
+        return fail(OASIS_ERR_INVALID_ARG, "%s: q, tree_kv, hbm_pool and out must be 16-byte aligned", who);
+    if (!(scale > 0.f) || scale > 3.0e38f) return fail(OASIS_ERR_INVALID_ARG, "%s: scale %g", who, (double)scale);
+    if (dims->batch == 0) return OASIS_OK;
+    const TreePlan pl = tree_plan(dims, n_tree, n_cols);
+    if (pl.workspace > 0) {
+        if (!workspace || workspace_bytes < pl.workspace)
+            return fail(OASIS_ERR_WORKSPACE, "%s: workspace of %zu bytes required, %zu given", who, pl.workspace,
+                        workspace ? workspace_bytes : (size_t)0);
+        if (!aligned16(workspace)) return fail(OASIS_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+    }
+    if (pl.items > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: grid too large", who);
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available", who);
+
+    // The pool as attn_tc.cu sees it: one box = one 8 KiB entry, landing as [group][half][K, V][8 rows][128 B].
+    CUtensorMap pool_map, tree_map;
+    const cuuint64_t pool_parts = (kBoundsCheck && bounds().n_slots < (1ll << 30)) ? (cuuint64_t)(2 * bounds().n_slots) : (cuuint64_t)1 << 31;
+    const cuuint64_t pdim[5] = {64, 8, pool_parts, 2, 2}, pstride[4] = {256, 4096, 128, 2048};
+    const cuuint32_t pbox[5] = {64, 8, 2, 2, 2}, estr[5] = {1, 1, 1, 1, 1};
+    CUresult cr = encode(&pool_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(hbm_pool), pdim, pstride, pbox, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (cr != CUDA_SUCCESS) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed (%d)", who, (int)cr);
+    // The tree buffer [B][T][Hkv][K, V][2 x 64 dims], innermost first: 64 elements | nodes | (head, part) | dim half |
+    // request.  One box = 8 nodes of one head, landing as [half][K, V][8 rows][128 B] = one row group of a block image;
+    // nodes past T read as zero.
+    const cuuint64_t Hkv = (cuuint64_t)dims->n_kv_heads, T64 = (cuuint64_t)n_tree;
+    const cuuint64_t tdim[5] = {64, T64, 2 * Hkv, 2, (cuuint64_t)dims->batch}, tstride[4] = {Hkv * 512, 256, 128, T64 * Hkv * 512};
+    const cuuint32_t tbox[5] = {64, 8, 2, 2, 1};
+    cr = encode(&tree_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(tree_kv), tdim, tstride, tbox, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (cr != CUDA_SUCCESS) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed (%d)", who, (int)cr);
+
+    TreeAttnParams p = {};
+    p.q = (const uint8_t *)q; p.slot_tbl = slot_tbl; p.blk_tbl = blk_tbl; p.seq_len = seq_len; p.parent = parent;
+    p.n_nodes = n_nodes; p.out = (uint8_t *)out; p.lse = lse; p.err = error_word();
+    p.scale_log2 = scale * kAtLog2e;
+    p.T = n_tree; p.Hq = dims->n_q_heads; p.Hkv = dims->n_kv_heads; p.G = p.Hq / p.Hkv; p.n_cols = n_cols; p.R = n_tree * p.G;
+    p.n_splits = pl.n_splits; p.cols_per_split = pl.cols_per_split; p.n_groups = pl.n_groups; p.group_rows = pl.group_rows;
+    p.n_slots = bounds().n_slots;
+    if (pl.n_splits > 1) {
+        p.part_o = (float *)workspace;
+        p.part_lse = p.part_o + (size_t)pl.items * pl.group_rows * kHeadDim;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e;
+#define OASIS_TREE_LAUNCH(M, C)                                                                                               \
+    do {                                                                                                                      \
+        e = cudaFuncSetAttribute(tree_attn_tc_kernel<M, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTrSmem);        \
+        if (e == cudaSuccess) prefer_max_shared_carveout(tree_attn_tc_kernel<M, C>);                                          \
+        if (e == cudaSuccess) tree_attn_tc_kernel<M, C><<<(unsigned)pl.items, tr_threads(M, C), kTrSmem, st>>>(pool_map, tree_map, p); \
+    } while (0)
+    if (pl.group_rows <= 16) OASIS_TREE_LAUNCH(64, 4);          // four copies of <= 16 rows, one block of a tile each
+    else if (pl.group_rows <= 32) OASIS_TREE_LAUNCH(64, 2);     // two copies of <= 32 rows, two blocks each
+    else if (pl.group_rows <= 64) OASIS_TREE_LAUNCH(128, 2);    // two copies of <= 64 rows: half the softmax work per thread
+    else OASIS_TREE_LAUNCH(128, 1);                             // two softmax warp sets, alternate tiles
+#undef OASIS_TREE_LAUNCH
+    if (e != cudaSuccess) return fail(OASIS_ERR_CUDA, "%s: shared memory %zu B: %s", who, kTrSmem, cudaGetErrorString(e));
+    if (int rc = check_launch(who)) return rc;
+    if (pl.n_splits > 1) {
+        // programmatic stream serialization: the merge's thread blocks become resident while the attention still runs
+        const int total = dims->batch * p.Hkv * p.R;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)((total + 7) / 8));
+        cfg.blockDim = dim3(256);
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        prefer_max_shared_carveout(tree_combine_kernel);
+        e = cudaLaunchKernelEx(&cfg, tree_combine_kernel, p, total);
+        if (e != cudaSuccess) return fail(OASIS_ERR_CUDA, "%s: combine launch: %s", who, cudaGetErrorString(e));
+        return check_launch(who);
+    }
+    return OASIS_OK;
+}

@@ -22,7 +22,7 @@ class DecodeLayer:
     """
 
     def __init__(self, batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, device="cuda",
-                 want_lse=False, out=None):
+                 want_lse=False, out=None, tree=False):
         self.B, self.Hq, self.Hkv, self.mb = batch, n_q_heads, n_kv_heads, max_blocks
         self.k, self.T = k, n_q_tokens
         self.cols = k + 2
@@ -39,7 +39,7 @@ class DecodeLayer:
         self.slot_tbl = torch.arange(rows * self.cols, dtype=torch.int32, device=dev).view(batch, n_kv_heads, self.cols)
         self.out = torch.empty((batch, n_q_tokens, n_q_heads, 128), dtype=torch.bfloat16, device=dev) if out is None else out
         self.lse = torch.empty((batch, n_q_tokens, n_q_heads), dtype=torch.float32, device=dev) if want_lse else None
-        ws = oasis.attn_workspace_bytes(self.dims, n_q_tokens, self.cols)
+        ws = (oasis.tree_attn_workspace_bytes if tree else oasis.attn_workspace_bytes)(self.dims, n_q_tokens, self.cols)
         self.workspace = torch.empty((max(ws, 16),), dtype=torch.uint8, device=dev)
         self.scale = 1.0 / math.sqrt(128.0)
 
@@ -50,7 +50,7 @@ class DecodeLayer:
 
     # step 1: the draft tokens are rows 1..T-1 of the stacked verify-step queries
     def score(self, q, n_full, reduce_mode=oasis.REDUCE_MAX, stream=None):
-        n_draft = self.T - 1
+        n_draft = min(self.T - 1, 128 // (self.Hq // self.Hkv))      # a wide tree: its first drafts (at most 128 rows score)
         q_draft = q[:, 1:]
         oasis.score_blocks(self.dims, q_draft, n_draft, self.summaries, n_full, self.scores,
                            reduce_mode=reduce_mode, q_batch_stride=self.T * self.Hq * 128, stream=stream)
@@ -77,6 +77,13 @@ class DecodeLayer:
         oasis.sparse_attn(self.dims, q, self.T, self.pool, self.slot_tbl if slot_tbl is None else slot_tbl,
                           self.sel if blk_tbl is None else blk_tbl, self.cols, seq_len, self.scale,
                           self.out, lse=self.lse, workspace=self.workspace, stream=stream)
+        return self.out
+
+    # step 4 for a tree of drafted tokens (layers made with tree=True; n_q_tokens is the largest tree)
+    def attend_tree(self, q, tree_kv, parent, n_nodes, seq_len, blk_tbl=None, slot_tbl=None, stream=None):
+        oasis.tree_attn(self.dims, q, tree_kv, parent, n_nodes, self.pool, self.slot_tbl if slot_tbl is None else slot_tbl,
+                        self.sel if blk_tbl is None else blk_tbl, seq_len, self.scale, self.out, lse=self.lse,
+                        workspace=self.workspace, stream=stream)
         return self.out
 
     # steps 4 + 1 in one launch (shapes permitting)
@@ -133,9 +140,15 @@ class DecodeEngine:
 
     def __init__(self, batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, n_layers,
                  device="cuda", mode="fetch_all", cap=None, fused=None, transfer_streams=1, wait_group=8,
-                 append=False, transfer_group=1, plan_stream="own", n_commit=1, transfer_ctas=0, transfer_kind="warp"):
+                 append=False, transfer_group=1, plan_stream="own", n_commit=1, transfer_ctas=0, transfer_kind="warp",
+                 tree=False):
         assert mode in ("fetch_all", "delta")
         assert not append or mode == "delta", "the KV append goes with delta selection"
+        if tree and not (append and n_q_tokens >= 2):
+            raise ValueError("draft trees need the KV append (delta mode) and room for two nodes or more")
+        if tree and fused:
+            raise ValueError("the fused launch takes chains of drafts")
+        self.tree = bool(tree)
         self.append = bool(append)
         self.transfer_ctas = int(transfer_ctas)  # thread blocks per gather launch (0: the library's default)
         if transfer_kind not in ("warp", "bulk"):
@@ -146,7 +159,8 @@ class DecodeEngine:
         self.device = torch.device(device)
         # the layers' outputs are slices of one tensor, so that several layers' outputs can leave in one copy
         self.out_all = torch.empty((n_layers, batch, n_q_tokens, n_q_heads, 128), dtype=torch.bfloat16, device=self.device)
-        self.layers = [DecodeLayer(batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, device, out=self.out_all[l])
+        self.layers = [DecodeLayer(batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, device, out=self.out_all[l],
+                                   tree=self.tree)
                        for l in range(n_layers)]
         self.kv = [None] * n_layers
         self.table = [None] * n_layers
@@ -168,7 +182,7 @@ class DecodeEngine:
         self.cap = cap
         self.wait_group = max(1, int(wait_group))
         self.transfer_group = max(1, min(int(transfer_group), oasis.MAX_STAGE_LAYERS))
-        can_fuse = n_layers > 0 and n_q_tokens > 1 and oasis.attn_and_score_supported(self.layers[0].dims, n_q_tokens, self.layers[0].cols, n_q_tokens - 1)
+        can_fuse = not self.tree and n_layers > 0 and n_q_tokens > 1 and oasis.attn_and_score_supported(self.layers[0].dims, n_q_tokens, self.layers[0].cols, n_q_tokens - 1)
         self.fused = can_fuse if fused is None else (bool(fused) and can_fuse)
         self._reset_events()
         if mode == "delta":
@@ -179,7 +193,8 @@ class DecodeEngine:
             n_req = cap + (0 if append else 2)       # requests per row: the admitted pairs (and the local blocks)
             self.plan_idx = [torch.empty(rows + (n_req,), dtype=torch.int64, device=dev) for _ in range(n_layers)]
             self.plan_slots = [torch.empty(rows + (n_req,), dtype=torch.int32, device=dev) for _ in range(n_layers)]
-        self._splits = oasis.attn_workspace_bytes(self.layers[0].dims, n_q_tokens, k + 2) > 0 if n_layers else False
+        ws_bytes = oasis.tree_attn_workspace_bytes if self.tree else oasis.attn_workspace_bytes
+        self._splits = ws_bytes(self.layers[0].dims, n_q_tokens, k + 2) > 0 if n_layers else False
 
     def _reset_events(self):
         """Forgets the previous step's events (everything before has completed)."""
@@ -189,6 +204,7 @@ class DecodeEngine:
         self.attn_done = [None] * n          # the layer's latest attention (it reads q, the tables and the pool)
         self.score_done = [None] * n         # unfused: the layer's latest scoring (it reads q)
         self.out_done = [None] * n           # end to end: the download of the layer's latest output
+        self.commit_done = None              # trees: the latest commit (summaries read what it wrote to the full-KV pool)
 
     def attach(self, layer, kv_src, block_table):
         """kv_src: the layer's full-KV pool (pinned host memory, or device memory)."""
@@ -333,7 +349,7 @@ class DecodeEngine:
                     self.side.wait_event(self.stage_done[l])
                     idx = torch.empty((B, L.Hkv, 2), dtype=torch.int64, device=self.device)
                     slots = torch.empty((B, L.Hkv, 2), dtype=torch.int32, device=self.device)
-                    oasis.local_window(L.dims, seq_next, self.T, self.table[l], self.resident[l], self.k, L.cols, idx, slots)
+                    oasis.local_window(L.dims, seq_next, 1 if self.tree else self.T, self.table[l], self.resident[l], self.k, L.cols, idx, slots)
                     oasis.stage_blocks(self.kv[l], idx, slots, idx.numel(), L.pool)
                     self.launches += 2
             if plan is not None:
@@ -343,7 +359,7 @@ class DecodeEngine:
         self._reset_events()                         # everything has completed
 
     def step(self, q_list, seq_len, first_block, n_new, n_full_next, seq_next, step_stamp=0,
-             timers=None, q_host=None, out_host=None, new_kv=None, sel_log=None):
+             timers=None, q_host=None, out_host=None, new_kv=None, sel_log=None, tree=None):
         """One decode step over all layers.  seq_len: history tokens of this step; the
         prediction works on the next step's view (n_full_next, seq_next).  With q_host /
         out_host (pinned tensors per layer) the step's queries are copied in and its outputs
@@ -351,8 +367,12 @@ class DecodeEngine:
         over the layers ([n_layers][B][T][Hq][128]) the copies are made for `wait_group` layers at a time: a few
         large copies disturb the gathers on the host link less than many small ones.  new_kv (one [B][T][Hkv][2][128] tensor per
         layer; engines built with append=True): the step's new keys and values.  sel_log (one tensor like
-        `layers[l].sel` per layer): receives a copy of each layer's selection of this step."""
+        `layers[l].sel` per layer): receives a copy of each layer's selection of this step.  tree (engines built with
+        tree=True): (parent, n_nodes) of the step's draft trees; new_kv then holds the nodes' keys and values, and
+        `commit` follows the step."""
         ms, n = self.main, self.n_layers
+        if self.tree != (tree is not None):
+            raise ValueError("tree must be given exactly when the engine was built with tree=True")
         if self.append != (new_kv is not None):
             raise ValueError("new_kv must be given exactly when the engine was built with append=True")
         q_ready = [None] * n
@@ -379,7 +399,9 @@ class DecodeEngine:
         # launch, the summary updates (one newly completed block per request every 16 steps), which only depend on the
         # append.  Only the group's first launch on the foreground stream waits for them.
         head_ready = {}
-        if self.append or self.fused:
+        if self.tree and self.commit_done is not None:
+            self.pred.wait_event(self.commit_done)
+        if (self.append and not self.tree) or self.fused:
             with torch.cuda.stream(self.pred):
                 for l0 in range(0, n, self.wait_group):
                     l1 = min(l0 + self.wait_group, n)
@@ -418,7 +440,10 @@ class DecodeEngine:
                     self._tock(timers, "layer", t0, ms)
                 else:
                     t0 = self._tick(timers, "attn", ms)
-                    L.attend(q_list[l], seq_len, blk_tbl=self.blk_tbl(l))
+                    if self.tree:
+                        L.attend_tree(q_list[l], new_kv[l], tree[0], tree[1], seq_len, blk_tbl=self.blk_tbl(l))
+                    else:
+                        L.attend(q_list[l], seq_len, blk_tbl=self.blk_tbl(l))
                     self._tock(timers, "attn", t0, ms)
                 self.launches += 2 if self._splits else 1      # the launch (and the merge of split rows)
                 attn_done = self._event(ms)
@@ -445,6 +470,23 @@ class DecodeEngine:
             if len(pending) == self.transfer_group or l == n - 1:
                 self._transfer(pending, readies, timers)
                 pending, readies = [], []
+
+    def commit_plan(self, tree_kvs):
+        """The handle of `commit` for these per-layer tree buffers [B][T][Hkv][2][128] (the `new_kv` of the steps)."""
+        return oasis.CommitPlan(self.layers[0].dims, list(tree_kvs), self.table, [L.slot_tbl for L in self.layers], self.resident,
+                                self.k, [L.pool for L in self.layers], self.kv)
+
+    def commit(self, plan, path, n_commit, seq_len, next_len=None):
+        """After a step with draft trees: the kept path of every request goes into the local windows and full-KV pools of
+        all layers (on the foreground stream, after the current stream's work so far, which produced the path)."""
+        if not self.tree:
+            raise ValueError("commit goes with engines built with tree=True")
+        self.main.wait_event(self._event(torch.cuda.current_stream(self.device)))
+        with torch.cuda.stream(self.main):
+            oasis.commit_kv_layers(plan, path, n_commit, seq_len, next_len=next_len)
+            self.launches += 1
+            self.commit_done = self._event(self.main)
+        torch.cuda.current_stream(self.device).wait_event(self.commit_done)
 
     def join(self):
         """Makes the foreground stream wait for everything the other streams have in flight."""
