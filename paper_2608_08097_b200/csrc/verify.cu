@@ -15,6 +15,7 @@
 #include <math_constants.h>
 
 #include "common.cuh"
+#include "tc_common.cuh"
 
 namespace oasis {
 
@@ -30,23 +31,53 @@ struct VerifyParams {
     const void *logits;
     const int32_t *tokens, *parent, *n_nodes;
     const float *uniforms, *temperature, *draft;
-    int32_t *path, *n_commit, *next_token;
+    int32_t *path, *n_commit, *next_token, *err;
     long long lb, lr, db, dr;          // strides (elements) of logits and draft
     int T, V, M;
 };
 
-template <typename LT> struct VecOf { static constexpr int n = 16 / sizeof(LT); };
-
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+template <typename LT> struct Logit;                   // elements per 16-byte vector, the pattern of -infinity, unpacking
+template <> struct Logit<float> {
+    static constexpr int N = 4;
+    static constexpr uint32_t kNone = 0xff800000u;
+    static __device__ __forceinline__ float get(const uint4 &w, int k) { return __uint_as_float((&w.x)[k]); }
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+};
+template <> struct Logit<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static constexpr uint32_t kNone = 0xff80u;
+    static __device__ __forceinline__ float get(const uint4 &w, int k)
+    {
+        const uint32_t h = (&w.x)[k >> 1];
+        return __uint_as_float((k & 1) ? (h & 0xffff0000u) : (h << 16));
+    }
+    static __device__ __forceinline__ float one(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+};
+template <> struct Logit<__half> {
+    static constexpr int N = 8;
+    static constexpr uint32_t kNone = 0xfc00u;
+    static __device__ __forceinline__ float get(const uint4 &w, int k)
+    {
+        const uint32_t h = (&w.x)[k >> 1];
+        return __half2float(__ushort_as_half((unsigned short)((k & 1) ? (h >> 16) : (h & 0xffffu))));
+    }
+    static __device__ __forceinline__ float one(const __half *p) { return __half2float(*p); }
+};
 // NaN counts as -infinity (fmaxf returns the operand that is a number).
 __device__ __forceinline__ float clean(float v) { return fmaxf(v, -CUDART_INF_F); }
+
+// Sets element k of a vector in shared memory to -infinity.
+template <typename LT>
+__device__ __forceinline__ void leave_out(uint4 *w, int k)
+{
+    if (sizeof(LT) == 4) reinterpret_cast<uint32_t *>(w)[k] = Logit<LT>::kNone;
+    else reinterpret_cast<uint16_t *>(w)[k] = (uint16_t)Logit<LT>::kNone;
+}
 
 // One row of logits as aligned 16-byte vectors: the first `skip` elements of vector 0 belong to what lies before the row.
 template <typename LT>
 struct Row {
-    static constexpr int N = VecOf<LT>::n;
+    static constexpr int N = Logit<LT>::N;
     const LT *base;                    // 16-byte aligned; element e of vector v is row element v * N + e - skip
     int skip, V, n_vec;
     __device__ Row(const LT *row, int vocab)
@@ -57,21 +88,30 @@ struct Row {
         n_vec = (vocab + skip + N - 1) / N;
     }
     __device__ __forceinline__ int first(int v) const { return v * N - skip; }
-    // The vector's logits; elements outside the row come as -infinity.
-    __device__ __forceinline__ void load(int v, float (&x)[N]) const
+    // This lane's vectors v, v + 32, ... below v_end to dst, dst + 32, ... by asynchronous copies (complete after
+    // stage_wait); what lies outside the row comes as -infinity.
+    __device__ __forceinline__ void stage(int v, int v_end, uint4 *dst) const
     {
-        const int i0 = first(v);
-        if (i0 >= 0 && i0 + N <= V) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(base + (long long)v * N);
-            const LT *e = reinterpret_cast<const LT *>(&w);
-#pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = clean(to_f32(e[k]));
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = (i0 + k >= 0 && i0 + k < V) ? clean(to_f32(base[(long long)v * N + k])) : -CUDART_INF_F;
+        const int lo = skip ? 1 : 0, hi = (V + skip) / N;              // the vectors that lie inside the row
+        const LT *src = base + (long long)v * N;
+#pragma unroll 4
+        for (int i = v; i < v_end; i += 32, src += 32 * N)
+            if (i >= lo && i < hi)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst + (i - v))), "l"(src) : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (skip && v == 0 && v_end > 0) edge(base, -skip, V, dst);
+        if (hi < n_vec && hi >= lo && hi >= v && hi < v_end && ((hi - v) & 31) == 0) edge(base + (long long)hi * N, hi * N - skip, V, dst + (hi - v));
+    }
+    // The row's first or last vector, whose element 0 is row element i0.
+    static __device__ __noinline__ void edge(const LT *src, int i0, int V, uint4 *dst)
+    {
+        for (int k = 0; k < N; ++k) {
+            if (i0 + k >= 0 && i0 + k < V) reinterpret_cast<LT *>(dst)[k] = src[k];
+            else leave_out<LT>(dst, k);
         }
     }
 };
+__device__ __forceinline__ void stage_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -85,365 +125,621 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// 16 bytes (two 64-bit words) to the same shared-memory place of thread block `rank` of the cluster.
-__device__ __forceinline__ void st_cluster(const void *place, uint32_t rank, uint64_t a, uint64_t b)
+// 16 bytes (two 64-bit words) to the same shared-memory place of thread block `rank` of the cluster, counted by its mbarrier.
+__device__ __forceinline__ void send(const void *place, uint32_t bar, uint32_t rank, uint64_t a, uint64_t b)
 {
-    uint32_t addr;
+    uint32_t addr, rbar;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(place)), "r"(rank));
-    asm volatile("st.shared::cluster.v2.u64 [%0], {%1, %2};" ::"r"(addr), "l"(a), "l"(b) : "memory");
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rbar) : "r"(bar), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(addr), "l"(a), "l"(b), "r"(rbar)
+                 : "memory");
 }
 
 struct __align__(16) Pair { uint64_t a, b; };
 
 // What the target's distribution at the current node has become: a token's share is
-//   max(a * w - b * q, 0)   with w = exp((logit - m) / temperature), tokens of `tried` left out (their q is all theirs)
+//   max(a * w - b * q, 0)   with w = exp((logit - m) / temperature); rejected tokens without a draft row are left out
 struct Dist {
-    float m;
-    double inv_t, a, b;
+    float l_min;                       // logits up to here have weight 0: 250 temperatures below m, and everything but m at tiny ones
+    double m, c;                       // c = 1024 log2(e) / temperature
+    double a, b;
     const float *q;                    // the draft's row, or NULL
-    unsigned long long tried;          // rejected children (without a draft row)
 };
 
-__device__ __forceinline__ double weight(float l, const Dist &d)
+// 2^(j / 1024), made at compile time from square roots (Newton's iteration) of two: the binary digits of j pick the factors.
+constexpr int kExpTable = 1024;
+struct ExpTable {
+    double v[kExpTable];
+    constexpr ExpTable() : v()
+    {
+        double root[10] = {};
+        double x = 2.0;
+        for (int i = 9; i >= 0; --i) {                     // root[i] = 2^(2^i / 1024)
+            double y = 1.0 + (x - 1.0) / 2;
+            for (int k = 0; k < 8; ++k) y = (y + x / y) / 2;
+            x = root[i] = y;
+        }
+        for (int j = 0; j < kExpTable; ++j) {
+            double f = 1.0;
+            for (int i = 0; i < 10; ++i)
+                if ((j >> i) & 1) f *= root[i];
+            v[j] = f;
+        }
+    }
+};
+__device__ const ExpTable g_exp_table = ExpTable();
+
+// exp((l - m) / temperature) in fp64, to about 1e-14 of itself.  With y = (l - m) c and n = y rounded to a whole number,
+//   2^(y / 1024) = 2^floor(n / 1024) * T[n mod 1024] * exp(r ln 2 / 1024),  r = y - n,  |r| <= 1 / 2,
+// and the series' fourth term is below 6e-16.  Ten instructions for the fp64 units, one conversion and one table look-up:
+// exp() takes twice as long, and this is the pass over 152,000 logits that the last node of every walk needs.  l = m gives
+// exactly 1, so equal logits have equal weights and sums of them are exact.
+__device__ __forceinline__ double weight(float l, const Dist &d, const double *table)
 {
-    if (l == d.m) return 1.0;          // also where both are infinite
-    return exp(((double)l - (double)d.m) * d.inv_t);
+    constexpr double kStep = 0.69314718055994530942 / kExpTable, kRound = 6755399441055744.0;   // 1.5 * 2^52
+    const double y = ((double)l - d.m) * d.c;
+    const double t = y + kRound;
+    const int n = __double2loint(t);
+    const double r = y - (t - kRound);
+    const double f = table[n & (kExpTable - 1)];
+    const double e = fma(r, fma(r, kStep * kStep * kStep / 6, kStep * kStep / 2), kStep);
+    const double w = fma(f * r, e, f);
+    const double scaled = __hiloint2double(__double2hiint(w) + ((n & ~(kExpTable - 1)) << 10), __double2loint(w));
+    return l > d.l_min ? scaled : 0.0;                     // (also for NaN and -infinity)
 }
 
+__device__ __forceinline__ double shfl_d(double v, int lane) { return __shfl_sync(0xffffffffu, v, lane); }
+
+// What warp 0 decides and the other warps carry out.
+enum { kGo = 0, kMass = 1, kSearch = 2, kEnd = 3 };        // on to a child | a mass pass under (ma, mb) | find the next token | done
+struct Control {
+    int cmd, cur, ahead;               // ahead: the likeliest node after cur, or -1
+    int infinite;                      // some logit of the row is +infinity
+    unsigned long long tried;          // rejected children (without a draft row)
+    Dist d;
+    double ma, mb;
+    // kept by warp 0 from one decision about a node to the next
+    double z, away;                    // sum of all weights; weight of the tried tokens
+    unsigned long long left;           // children not tried yet
+    int exact, have_mass, need;        // z is the fp64 sum; s_mass fits the distribution; what the mass pass is for
+    // the search
+    double target, before;
+    int in_warp, take_last;            // (in_warp -1: another thread block has it)
+};
+
+// One chunk of a warp's vectors under (ma, mb): the mass of every vector goes to my_sum, the lane's sum is returned.  Tokens
+// that were tried leave the row by turning their logits into -infinity.
 template <typename LT>
-__global__ void __launch_bounds__(kVerThreads)
-verify_tree_kernel(const VerifyParams p, const int C)
+__device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row, int vc, int ve, int lane, bool reload, uint4 *my_row,
+                                          double *my_sum, const double *table, const int *s_tok)
 {
-    constexpr int N = VecOf<LT>::n;
+    constexpr int N = Logit<LT>::N;
+    if (reload) { row.stage(vc + lane, ve, my_row); stage_wait(); }
+#pragma unroll 1
+    for (unsigned long long t = ctl.tried; t; t &= t - 1) {
+        const int token = s_tok[__ffsll((long long)t) - 1], e = token + row.skip, v = e / N;
+        if (token >= 0 && token < row.V && v >= vc && v < ve && ((v - vc) & 31) == lane) leave_out<LT>(my_row + (v - vc - lane), e % N);
+    }
+    const Dist d = ctl.d;
+    const double ma = ctl.ma, mb = ctl.mb;
+    double sum = 0.0;
+    if (d.q && mb == 0.0)                                          // a pass under the draft's row may follow: on its way to L2
+        for (int i = max(row.first(vc), 0) + lane * 32; i < min(row.first(ve), row.V); i += 32 * 32)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(d.q + i));
+    if (mb == 0.0 && !ctl.infinite) {
+#pragma unroll 1
+        for (int v = vc + lane; v < ve; v += 32) {
+            const uint4 w = my_row[v - vc - lane];
+            double part = 0.0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) part += weight(Logit<LT>::get(w, k), d, table);
+            my_sum[v - vc - lane] = part;
+            sum += part;
+        }
+    } else {
+        float q[N], q_next[N];
+        auto fetch = [&](int v, float (&f)[N]) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int i = row.first(v) + k;
+                f[k] = mb != 0.0 && v < ve && i >= 0 && i < row.V ? d.q[i] : 0.f;
+            }
+        };
+        fetch(vc + lane, q);
+#pragma unroll 1
+        for (int v = vc + lane; v < ve; v += 32) {
+            fetch(v + 32, q_next);
+            const uint4 w = my_row[v - vc - lane];
+            double part = 0.0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {                          // (outside the row the logit is -infinity)
+                const float l = Logit<LT>::get(w, k);
+                const double f = weight(!ctl.infinite ? l : l == CUDART_INF_F ? 0.f : -CUDART_INF_F, d, table);
+                part += mb == 0.0 ? f : fmax(ma * f - mb * (double)q[k], 0.0);
+                q[k] = q_next[k];
+            }
+            my_sum[v - vc - lane] = part;
+            sum += part;
+        }
+    }
+    return sum;
+}
+
+// cap: vectors per warp that shared memory holds.  A part of the row that is not larger (n_chunks == 1) is read once per
+// visited node, whatever happens there; a larger one is read again for every pass.
+// Between the passes warp 0 alone talks to the other thread blocks of the cluster and decides; that every warp did it cost
+// more than the passes (four warps per scheduler running the same 200 serial instructions).
+template <typename LT>
+__global__ void __launch_bounds__(kVerThreads, 2)
+verify_tree_kernel(const VerifyParams p, const int C, const int cap)
+{
+    constexpr int N = Logit<LT>::N;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ Pair s_x[2][kVerMaxCluster];            // what the thread blocks of the cluster tell one another
+    __shared__ __align__(8) uint64_t s_bar[2];
     __shared__ Pair s_w[kVerWarps];
     __shared__ double s_mass[kVerWarps];
+    __shared__ __align__(16) double s_table[kExpTable];
     __shared__ int s_tok[OASIS_MAX_TREE], s_par[OASIS_MAX_TREE];
-    __shared__ float s_u[OASIS_MAX_TREE], s_kid[OASIS_MAX_TREE], s_kq[OASIS_MAX_TREE];
+    __shared__ float s_u[OASIS_MAX_TREE];
     __shared__ int s_path[OASIS_MAX_TREE];
+    __shared__ Control ctl;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint4 *const my_row = reinterpret_cast<uint4 *>(smem_raw) + warp * cap + lane;              // this lane's vectors, 32 apart
+    double *const my_sum = reinterpret_cast<double *>(smem_raw + (size_t)kVerWarps * cap * 16) + warp * cap + lane;   // their masses
     const uint32_t rank = C > 1 ? cluster_rank() : 0u;
     const int b = blockIdx.x / C;
+    const LT *const logits = reinterpret_cast<const LT *>(p.logits) + (long long)b * p.lb;
+    const int parts_of_row = C * kVerWarps, part = (int)rank * kVerWarps + warp;
+    // this warp's vectors of node x's row, and their way into shared memory
+    Row<LT> row(logits, p.V);
+    int v0 = 0, v1 = 0, n_chunks = 1;
+    auto enter = [&](int x) {
+        row = Row<LT>(logits + (long long)x * p.lr, p.V);
+        const int per_warp = (row.n_vec + parts_of_row - 1) / parts_of_row;
+        v0 = min(part * per_warp, row.n_vec);
+        v1 = min(v0 + per_warp, row.n_vec);
+        n_chunks = (per_warp + cap - 1) / cap;         // the same for all warps
+        row.stage(v0 + lane, min(v0 + cap, v1), my_row);
+    };
+    enter(0);                                          // node 0's row is needed in any case
     const int n = max(0, min(p.n_nodes[b], p.T));
+    const float temp = p.temperature[b];
+    int tok = 0, par = -1;
+    float un = 0.f;
+    if (tid < p.T) {
+        const long long at = (long long)b * p.T + tid;
+        tok = p.tokens[at];
+        par = p.parent[at];
+        un = p.uniforms[at];
+    }
     if (n == 0) {                                      // the whole cluster leaves: nothing is exchanged
+        stage_wait();
         if (rank == 0) {
             for (int i = tid; i < p.M; i += kVerThreads) p.path[(long long)b * p.M + i] = -1;
             if (tid == 0) { p.n_commit[b] = 0; p.next_token[b] = -1; }
         }
         return;
     }
-    for (int i = tid; i < p.T; i += kVerThreads) {
-        const long long at = (long long)b * p.T + i;
-        s_tok[i] = p.tokens[at];
-        s_par[i] = p.parent[at];
-        s_u[i] = fminf(fmaxf(p.uniforms[at], 0.f), 1.f - 5.9604645e-8f);
-    }
-    const float temp = p.temperature[b];
     const bool sampled = temp > 0.f;
-    Dist d;
-    d.inv_t = sampled ? 1.0 / (double)temp : 0.0;
-    const float c2 = sampled ? fminf(1.4426950408889634f / temp, 3.0e38f) : 0.f;
-    __syncthreads();
-    int turn = 0;
+    if (sampled) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(s_table + 2 * tid)), "l"(g_exp_table.v + 2 * tid) : "memory");
+        static_assert(kExpTable == 2 * kVerThreads, "one copy per thread");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    if (tid < OASIS_MAX_TREE) {
+        s_tok[tid] = tok;
+        s_par[tid] = par;
+        s_u[tid] = fminf(fmaxf(un, 0.f), 1.f - 5.9604645e-8f);
+    }
+    // (kept away from 0 and infinity: a logit of -infinity has weight 0 at any temperature)
+    const float c2 = fmaxf(fminf(1.4426950408889634f / temp, 3.0e38f), 1.2e-38f);
+    if (tid == 0) {
+        s_path[0] = 0;
+        ctl.ahead = n > 1 ? 1 : -1;
+        ctl.d.c = 1024.0 * 1.4426950408889634 * (sampled ? fmax(1.0 / (double)temp, 1e-300) : 0.0);
+        mbar_init(smem_u32(&s_bar[0]), 1);
+        mbar_init(smem_u32(&s_bar[1]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (C > 1) cluster_sync();                         // the barriers of all blocks are there
+    else __syncthreads();
 
-    // A value of every thread block (two words), told to all of the cluster.  All threads of all blocks take part.
-    auto exchange = [&](uint64_t x, uint64_t y) -> const Pair * {        // x, y: valid in thread 0 .. C - 1
-        const Pair *got = s_x[turn];
-        if (C > 1) {
-            if (tid < C) st_cluster(&s_x[turn][rank], (uint32_t)tid, x, y);
-            cluster_sync();
-        } else {
-            if (tid == 0) s_x[turn][0] = Pair{x, y};
-            __syncthreads();
-        }
-        turn ^= 1;
-        return got;
-    };
-
-    int cur = 0, n_path = 1, next = -1;
-    if (tid == 0) s_path[0] = 0;
+    int turn = 0;                                      // exchanges so far
+    int n_path = 1, next = -1;
     for (;;) {
-        const LT *row_ptr = reinterpret_cast<const LT *>(p.logits) + (long long)b * p.lb + (long long)cur * p.lr;
-        const Row<LT> row(row_ptr, p.V);
-        d.q = p.draft ? p.draft + (long long)b * p.db + (long long)cur * p.dr : nullptr;
-        const int per_warp = (row.n_vec + C * kVerWarps - 1) / (C * kVerWarps);
-        const int v0 = min(((int)rank * kVerWarps + warp) * per_warp, row.n_vec), v1 = min(v0 + per_warp, row.n_vec);
-        // the node's children (nodes of higher index whose parent it is) and, by thread c, child c's logit
-        unsigned long long kids = 0;
-        if (n_path < p.M) {
-            const unsigned k0 = __ballot_sync(0xffffffffu, lane > cur && lane < n && s_par[min(lane, p.T - 1)] == cur);
-            const unsigned k1 = __ballot_sync(0xffffffffu, lane + 32 > cur && lane + 32 < n && s_par[min(lane + 32, p.T - 1)] == cur);
-            kids = (unsigned long long)k1 << 32 | k0;
+        const int cur = n_path == 1 ? 0 : ctl.cur;
+        const LT *const row_ptr = logits + (long long)cur * p.lr;
+        const float *const q_row = p.draft ? p.draft + (long long)b * p.db + (long long)cur * p.dr : nullptr;
+        const int ahead = ctl.ahead;
+        if (ahead >= 0) {                              // the likeliest next row on its way to L2
+            const Row<LT> next_row(logits + (long long)ahead * p.lr, p.V);
+            for (int v = v0 + lane * 8; v < min(v1, next_row.n_vec); v += 32 * 8)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(next_row.base + (long long)v * N));
         }
-        if (sampled && tid < OASIS_MAX_TREE && ((kids >> tid) & 1ull)) {
-            const int t = s_tok[tid];
-            const bool in = t >= 0 && t < p.V;
-            s_kid[tid] = in ? clean(to_f32(row_ptr[t])) : -CUDART_INF_F;
-            s_kq[tid] = in && d.q ? d.q[t] : 1.f;
+        // warp 0: the node's children (nodes of higher index whose parent it is); lane c holds the logits of children c, c + 32
+        unsigned kids0 = 0, kids1 = 0;
+        float kid0 = -CUDART_INF_F, kid1 = -CUDART_INF_F, kq0 = 1.f, kq1 = 1.f;
+        if (warp == 0 && n_path < p.M) {
+            kids0 = __ballot_sync(0xffffffffu, lane > cur && lane < n && s_par[lane] == cur);
+            kids1 = __ballot_sync(0xffffffffu, lane + 32 > cur && lane + 32 < n && s_par[lane + 32] == cur);
+            if (sampled && ((kids0 >> lane) & 1u) && (unsigned)s_tok[lane] < (unsigned)p.V) {
+                kid0 = Logit<LT>::one(row_ptr + s_tok[lane]);
+                if (q_row) kq0 = q_row[s_tok[lane]];
+            }
+            if (sampled && ((kids1 >> lane) & 1u) && (unsigned)s_tok[lane + 32] < (unsigned)p.V) {
+                kid1 = Logit<LT>::one(row_ptr + s_tok[lane + 32]);
+                if (q_row) kq1 = q_row[s_tok[lane + 32]];
+            }
         }
+        stage_wait();
 
+        // ---- one pass over the row
         if (!sampled) {
-            // ---- greedy: the row's first maximum, as (value, index); equal values go to the lower index
-            float best = -CUDART_INF_F;
-            int at = 0x7fffffff;
-            for (int v = v0 + lane; v < v1; v += 32) {
-                float x[N];
-                row.load(v, x);
+            // greedy: the first maximum, as one key: value (order-preserving, -0 as +0), then the lower index
+            unsigned long long best = 0;
+            for (int ch = 0; ch < n_chunks; ++ch) {
+                const int vc = v0 + cap * ch, ve = min(vc + cap, v1);
+                if (ch > 0) { row.stage(vc + lane, ve, my_row); stage_wait(); }
+                float top = -CUDART_INF_F;
+                int at = 0;
+#pragma unroll 2
+                for (int v = vc + lane; v < ve; v += 32) {
+                    const uint4 w = my_row[v - vc - lane];
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    if (x[k] > best) { best = x[k]; at = row.first(v) + k; }
+                    for (int k = 0; k < N; ++k) {
+                        const float x = Logit<LT>::get(w, k);                    // (a NaN is not larger)
+                        if (x > top) { top = x; at = row.first(v) + k; }
+                    }
+                }
+                const uint32_t u = __float_as_uint(top + 0.f), key = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+                const unsigned long long full = (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)at);
+                if (top > -CUDART_INF_F && full > best) best = full;
             }
-            auto better = [](float f, int i, float g, int j) { return f > g || (f == g && i < j); };
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                const float f = __shfl_xor_sync(0xffffffffu, best, o);
-                const int i = __shfl_xor_sync(0xffffffffu, at, o);
-                if (better(f, i, best, at)) { best = f; at = i; }
-            }
-            if (lane == 0) s_w[warp] = Pair{__float_as_uint(best), (uint64_t)(uint32_t)at};
-            __syncthreads();
-            if (tid < kVerMaxCluster) {
-                for (int k = 0; k < kVerWarps; ++k) {
-                    const float f = __uint_as_float((uint32_t)s_w[k].a);
-                    const int i = (int)s_w[k].b;
-                    if (better(f, i, best, at)) { best = f; at = i; }
+            for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+            if (lane == 0) s_w[warp].a = best;
+        } else {
+            // sampled: maximum and sum of exponentials in fp32
+            float m = -CUDART_INF_F, s = 0.f;
+            for (int ch = 0; ch < n_chunks; ++ch) {
+                const int vc = v0 + cap * ch, ve = min(vc + cap, v1);
+                if (ch > 0) { row.stage(vc + lane, ve, my_row); stage_wait(); }
+                float top = -CUDART_INF_F;
+#pragma unroll 2
+                for (int v = vc + lane; v < ve; v += 32) {
+                    const uint4 w = my_row[v - vc - lane];
+#pragma unroll
+                    for (int k = 0; k < N; ++k) top = fmaxf(top, Logit<LT>::get(w, k));         // (a NaN loses)
+                }
+                if (top > m) {
+                    s *= m == -CUDART_INF_F ? 0.f : fast_exp2((m - top) * c2);
+                    m = top;
+                }
+                if (m == -CUDART_INF_F) continue;
+#pragma unroll 2
+                for (int v = vc + lane; v < ve; v += 32) {
+                    const uint4 w = my_row[v - vc - lane];
+                    float add = 0.f;
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const float x = clean(Logit<LT>::get(w, k));
+                        add += x == m ? 1.f : fast_exp2((x - m) * c2);
+                    }
+                    s += add;
                 }
             }
-            const Pair *got = exchange(__float_as_uint(best), (uint64_t)(uint32_t)at);
-            best = -CUDART_INF_F;
-            at = 0x7fffffff;
-            for (int r = 0; r < C; ++r) {
-                const float f = __uint_as_float((uint32_t)got[r].a);
-                const int i = (int)got[r].b;
-                if (better(f, i, best, at)) { best = f; at = i; }
-            }
-            next = best == -CUDART_INF_F ? -1 : at;
-            int child = -1;
-            for (unsigned long long k = kids; k && child < 0; k &= k - 1) {
-                const int c = __ffsll((long long)k) - 1;
-                if (next >= 0 && s_tok[c] == next) child = c;
-            }
-            if (child < 0) break;
-            cur = child;
-            if (tid == 0) s_path[n_path] = cur;
-            ++n_path;
-            continue;
-        }
-
-        // ---- sampled: maximum and sum of exponentials in fp32
-        float m = -CUDART_INF_F, s = 0.f;
-        for (int v = v0 + lane; v < v1; v += 32) {
-            float x[N];
-            row.load(v, x);
-            float vm = x[0];
+            float top = m;
 #pragma unroll
-            for (int k = 1; k < N; ++k) vm = fmaxf(vm, x[k]);
-            if (vm > m) {
-                s *= m == -CUDART_INF_F ? 0.f : fast_exp2((m - vm) * c2);
-                m = vm;
-            }
-            if (m == -CUDART_INF_F) continue;
-            float add = 0.f;
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            s = m == top ? s : s * fast_exp2((m - top) * c2);
 #pragma unroll
-            for (int k = 0; k < N; ++k) add += x[k] == m ? 1.f : fast_exp2((x[k] - m) * c2);
-            s += add;
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (lane == 0) s_w[warp] = Pair{__float_as_uint(top), __float_as_uint(s)};
         }
-        auto join = [&](float &m1, float &s1, float m2, float s2) {
-            const float top = fmaxf(m1, m2);
-            s1 = (m1 == top ? s1 : s1 * fast_exp2((m1 - top) * c2)) + (m2 == top ? s2 : s2 * fast_exp2((m2 - top) * c2));
-            m1 = top;
-        };
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-            join(m, s, m2, s2);
-        }
-        if (lane == 0) s_w[warp] = Pair{__float_as_uint(m), __float_as_uint(s)};
         __syncthreads();
-        if (tid < kVerMaxCluster) {
-            m = __uint_as_float((uint32_t)s_w[0].a);
-            s = __uint_as_float((uint32_t)s_w[0].b);
-            for (int k = 1; k < kVerWarps; ++k) join(m, s, __uint_as_float((uint32_t)s_w[k].a), __uint_as_float((uint32_t)s_w[k].b));
-        }
-        const Pair *got = exchange(__float_as_uint(m), __float_as_uint(s));
-        m = __uint_as_float((uint32_t)got[0].a);
-        s = __uint_as_float((uint32_t)got[0].b);
-        for (int r = 1; r < C; ++r) join(m, s, __uint_as_float((uint32_t)got[r].a), __uint_as_float((uint32_t)got[r].b));
-        if (m == -CUDART_INF_F) break;                         // every token is left out: next stays -1
-        d.m = m;
-        d.a = 1.0;
-        d.b = 0.0;
-        d.tried = 0;
 
-        // Mass of the row under (a, b, tried) in fp64: of every warp's part in s_mass, of the thread blocks in *parts.
-        const Pair *parts = nullptr;
-        auto share = [&](float x, int i, double a, double bq) -> double {      // token i's share, not normalised
-            double f = weight(x, d);                           // (0 outside the row, where x is -infinity)
-            if (d.q) {
-                if (bq != 0.0) f = (i >= 0 && i < p.V) ? fmax(a * f - bq * (double)d.q[i], 0.0) : 0.0;
-            } else {
-                for (unsigned long long t = d.tried; t; t &= t - 1)
-                    if (s_tok[__ffsll((long long)t) - 1] == i) f = 0.0;
-            }
-            return f;
-        };
-        auto mass = [&](double a, double bq) -> double {
-            double sum = 0.0;
-            for (int v = v0 + lane; v < v1; v += 32) {
-                float x[N];
-                row.load(v, x);
-                const int i0 = row.first(v);
+        // ---- decisions (warp 0), and mass passes between them
+        for (bool first = true;; first = false) {
+            if (warp == 0) {
+                // the block's value, then the cluster's
+                uint64_t x0, x1 = 0;
+                float m = 0.f, s = 0.f;
+                if (!first) {
+                    double all = s_mass[lane & (kVerWarps - 1)];
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum += share(x[k], i0 + k, a, bq);
+                    for (int o = kVerWarps / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+                    x0 = (uint64_t)__double_as_longlong(all);
+                } else {
+                    const Pair mine = s_w[lane & (kVerWarps - 1)];
+                    x0 = mine.a;
+                    if (!sampled) {
+#pragma unroll
+                        for (int o = kVerWarps / 2; o > 0; o >>= 1) x0 = max((unsigned long long)x0, __shfl_xor_sync(0xffffffffu, (unsigned long long)x0, o));
+                    } else {
+                        m = __uint_as_float((uint32_t)mine.a);
+                        s = __uint_as_float((uint32_t)mine.b);
+                        float top = m;
+#pragma unroll
+                        for (int o = kVerWarps / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        s = m == top ? s : s * fast_exp2((m - top) * c2);
+#pragma unroll
+                        for (int o = kVerWarps / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                        x0 = __float_as_uint(top);
+                        x1 = __float_as_uint(s);
+                    }
+                }
+                const Pair *got = s_x[turn & 1];
+                bool alive = true;
+                if (C > 1) {
+                    const uint32_t bar = smem_u32(&s_bar[turn & 1]);
+                    if (lane < C) send(&s_x[turn & 1][rank], bar, (uint32_t)lane, x0, x1);
+                    if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)C * 16u);
+                    __syncwarp();
+                    // (two lanes probe in a predicated instruction: a wait inside `if (lane == 0)` left the warp diverged)
+                    alive = mbar_wait_warp2(bar, (uint32_t)(turn >> 1) & 1u, bar, (uint32_t)(turn >> 1) & 1u, p.err, 81);
+                } else {
+                    if (lane == 0) s_x[turn & 1][0] = Pair{x0, x1};
+                    __syncwarp();
+                }
+                ++turn;
+                const Pair theirs = got[lane & (C - 1)];           // (C is a power of two)
+                int cmd = kMass, child = -1;
+                if (!alive) {
+                    cmd = kEnd;
+                } else if (!sampled) {
+                    unsigned long long best = theirs.a;
+                    for (int o = C / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+                    next = best == 0 ? -1 : (int)(0xffffffffu - (uint32_t)best);  // 0: every token is left out
+                    const unsigned e0 = __ballot_sync(0xffffffffu, ((kids0 >> lane) & 1u) && s_tok[lane] == next);
+                    const unsigned e1 = __ballot_sync(0xffffffffu, ((kids1 >> lane) & 1u) && s_tok[lane + 32] == next);
+                    if (next >= 0) child = e0 ? __ffs(e0) - 1 : e1 ? __ffs(e1) + 31 : -1;
+                    cmd = child >= 0 ? kGo : kEnd;
+                } else {
+                    Dist d = ctl.d;
+                    double z = ctl.z, away = ctl.away, total = 0.0;
+                    unsigned long long left = ctl.left, tried = ctl.tried;
+                    bool exact = ctl.exact, have_mass = ctl.have_mass;
+                    int need = ctl.need;
+                    enum { kNothing, kExact, kRest, kFinal };
+                    if (first) {
+                        m = __uint_as_float((uint32_t)theirs.a);
+                        s = __uint_as_float((uint32_t)theirs.b);
+                        float top = m;
+                        for (int o = C / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        s = m == top ? s : s * fast_exp2((m - top) * c2);
+                        for (int o = C / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                        // tokens with a logit of +infinity share everything: such a row reads as 0 at them and -infinity elsewhere
+                        const bool infinite = top == CUDART_INF_F;
+                        if (infinite) {
+                            kid0 = kid0 == CUDART_INF_F ? 0.f : -CUDART_INF_F;
+                            kid1 = kid1 == CUDART_INF_F ? 0.f : -CUDART_INF_F;
+                        }
+                        const float at = infinite ? 0.f : top;
+                        d.m = (double)at;
+                        d.l_min = fminf(at - 250.f * temp, nextafterf(at, -CUDART_INF_F));
+                        d.q = q_row;
+                        d.a = 1.0;
+                        d.b = 0.0;
+                        z = (double)s;
+                        away = 0.0;
+                        left = (unsigned long long)kids1 << 32 | kids0;
+                        tried = 0;
+                        exact = have_mass = false;
+                        if (lane == 0) ctl.infinite = infinite;
+                        if (top == -CUDART_INF_F) { cmd = kEnd; left = 0; }          // every token is left out: next stays -1
+                    } else {
+                        double mass = 0.0;
+                        for (int r = 0; r < C; ++r) mass += __longlong_as_double((long long)got[r].a);
+                        if (need == kExact) {
+                            z = mass + away;
+                            exact = true;
+                        } else {
+                            have_mass = need == kFinal || mass > 0.0;               // (else nothing is left: p stays as it was)
+                            if (have_mass) total = mass;
+                            if (need == kRest && have_mass) {
+                                d.a = ctl.ma / mass;
+                                d.b = ctl.mb / mass;
+                            }
+                        }
+                        if (have_mass && need == kExact) have_mass = false;         // (s_mass was used for something else)
+                    }
+                    // The children in order.  Whatever needs the row's mass in fp64 (a close decision, a rejection against
+                    // a draft row, the next token) asks for a pass and comes back.
+                    const double w0 = weight(kid0, d, s_table);
+                    const double w1 = left >> 32 ? weight(kid1, d, s_table) : 0.0;
+                    need = kNothing;
+#pragma unroll 1
+                    while (left) {
+                        const int i = __ffsll((long long)left) - 1;
+                        const double u = (double)s_u[i];
+                        double wc = shfl_d(i < 32 ? w0 : w1, i & 31);
+                        if (q_row) {
+                            const double q = (double)__shfl_sync(0xffffffffu, i < 32 ? kq0 : kq1, i & 31);
+                            const double uq = u * q;
+                            if (d.b == 0.0 && !exact && fabs(uq * z - wc) <= kFuzzy * (uq * z + wc)) { need = kExact; break; }
+                            const double share = d.b == 0.0 ? wc / z : fmax(d.a * wc - d.b * q, 0.0);
+                            if (uq < share) { child = i; break; }
+                            if (!exact) { need = kExact; break; }
+                            if (d.b == 0.0) d.a = 1.0 / z;
+                            left &= left - 1;
+                            need = kRest;
+                            break;
+                        }
+                        for (unsigned long long t = tried; t; t &= t - 1)
+                            if (s_tok[__ffsll((long long)t) - 1] == s_tok[i]) wc = 0.0;          // a sibling had the same token
+                        if (!exact && fabs(u * (z - away) - wc) <= kFuzzy * z) { need = kExact; break; }
+                        if (u * (z - away) < wc) { child = i; break; }
+                        away += wc;
+                        tried |= 1ull << i;
+                        left &= left - 1;
+                    }
+                    if (child >= 0) {
+                        cmd = kGo;
+                    } else if (cmd != kEnd && need == kNothing && have_mass) {
+                        // the next token: the place of uniforms[b][0] in the running sum of what is left.  (Rounding can leave
+                        // the target at the end of the last part that holds anything: then it is that part's last token.)
+                        cmd = kSearch;
+                        const double target = (double)s_u[0] * total;
+                        double before = 0.0;
+                        int owner = -1, last = 0;
+                        for (int r = 0; r < C && owner < 0; ++r) {
+                            const double mine = __longlong_as_double((long long)got[r].a);
+                            if (mine > 0.0) last = r;
+                            if (target < before + mine) owner = r;
+                            else before += mine;
+                        }
+                        const bool take_last = owner < 0;
+                        if (take_last) owner = last;
+                        int in_warp = -1;
+                        if (owner == (int)rank) {
+                            last = 0;
+                            for (int k = 0; k < kVerWarps && in_warp < 0; ++k) {
+                                if (s_mass[k] > 0.0) last = k;
+                                if (!take_last && target < before + s_mass[k]) in_warp = k;
+                                else before += s_mass[k];
+                            }
+                        }
+                        if (lane == 0) {
+                            ctl.target = target;
+                            ctl.before = before;
+                            ctl.take_last = take_last || (owner == (int)rank && in_warp < 0);
+                            ctl.in_warp = owner != (int)rank ? -1 : in_warp < 0 ? last : in_warp;
+                        }
+                    } else if (cmd != kEnd) {
+                        if (need == kNothing) need = kFinal;
+                    }
+                    if (lane == 0) {
+                        if (cmd == kMass) {
+                            ctl.ma = need == kExact ? 1.0 : d.a;
+                            ctl.mb = need == kExact ? 0.0 : need == kRest ? d.b + 1.0 : d.b;
+                        }
+                        ctl.d = d;
+                        ctl.z = z;
+                        ctl.away = away;
+                        ctl.left = left;
+                        ctl.tried = tried;
+                        ctl.exact = exact;
+                        ctl.have_mass = have_mass;
+                        ctl.need = need;
+                    }
+                }
+                if (child >= 0) {
+                    // the child's own first child (for the prefetch), its place in the path
+                    const unsigned f0 = __ballot_sync(0xffffffffu, lane > child && lane < n && s_par[lane] == child);
+                    const unsigned f1 = __ballot_sync(0xffffffffu, lane + 32 > child && lane + 32 < n && s_par[lane + 32] == child);
+                    if (lane == 0) {
+                        ctl.cur = child;
+                        ctl.ahead = n_path + 1 >= p.M ? -1 : f0 ? __ffs(f0) - 1 : f1 ? __ffs(f1) + 31 : -1;
+                        s_path[n_path] = child;
+                    }
+                }
+                if (lane == 0) ctl.cmd = cmd;
+            }
+            __syncthreads();
+            if (ctl.cmd != kMass) break;
+
+            // ---- a mass pass: the share of every vector under (ma, mb) to my_sum, of the warp's part to s_mass
+            double sum = 0.0;
+            for (int ch = 0; ch < n_chunks; ++ch) {
+                const int vc = v0 + cap * ch, ve = min(vc + cap, v1);
+                sum += chunk_mass<LT>(ctl, row, vc, ve, lane, n_chunks > 1, my_row, my_sum, s_table, s_tok);
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            __syncthreads();                                   // earlier readers of s_mass are done
             if (lane == 0) s_mass[warp] = sum;
             __syncthreads();
-            double all = 0.0;
-            if (tid < kVerMaxCluster)
-                for (int k = 0; k < kVerWarps; ++k) all += s_mass[k];
-            parts = exchange((uint64_t)__double_as_longlong(all), 0);
-            double total = 0.0;
-            for (int r = 0; r < C; ++r) total += __longlong_as_double((long long)parts[r].a);
-            return total;
-        };
-
-        double z = (double)s, away = 0.0;                      // sum of all weights; weight of the tried tokens
-        bool exact = false, have_mass = false;                 // z is the fp64 sum; s_mass and parts fit the distribution
-        double total = 0.0;
-        double ma = 1.0, mb = 0.0;                             // the (a, b) that s_mass was taken with
-        int child = -1;
-        for (unsigned long long k = kids; k && child < 0; k &= k - 1) {
-            const int c = __ffsll((long long)k) - 1;
-            const double u = (double)s_u[c];
-            double w = s_kid[c] == -CUDART_INF_F ? 0.0 : weight(s_kid[c], d);
-            if (d.q) {
-                const double q = (double)s_kq[c];
-                bool keep;
-                if (d.b == 0.0) {
-                    if (!exact && fabs(u * q * z - w) <= kFuzzy * (u * q * z + w)) { z = mass(1.0, 0.0); exact = true; }
-                    keep = u * q < w / z;
-                } else {
-                    keep = u * q < fmax(d.a * w - d.b * q, 0.0);
-                }
-                if (keep) { child = c; break; }
-                if (!exact) { z = mass(1.0, 0.0); exact = true; }
-                if (d.b == 0.0) d.a = 1.0 / z;
-                ma = d.a;
-                mb = d.b + 1.0;
-                const double rest = mass(ma, mb);
-                have_mass = rest > 0.0;
-                if (have_mass) {                               // (else nothing is left: p stays as it was)
-                    total = rest;
-                    d.a = ma / rest;
-                    d.b = mb / rest;
-                }
-            } else {
-                for (unsigned long long t = d.tried; t; t &= t - 1)
-                    if (s_tok[__ffsll((long long)t) - 1] == s_tok[c]) w = 0.0;      // a sibling had the same token
-                if (!exact && fabs(u * (z - away) - w) <= kFuzzy * z) { z = mass(1.0, 0.0) + away; exact = true; }
-                if (u * (z - away) < w) { child = c; break; }
-                away += w;
-                d.tried |= 1ull << c;
-            }
         }
-        if (child >= 0) {
-            cur = child;
-            if (tid == 0) s_path[n_path] = cur;
+        const int cmd = ctl.cmd;
+        if (cmd == kGo) {
             ++n_path;
-            __syncthreads();                                   // s_kid is rewritten for the next node
+            enter(ctl.cur);
             continue;
         }
-
-        // ---- the next token: the place of uniforms[b][0] in the running sum of what is left
-        if (!have_mass) {
-            ma = d.a;
-            mb = d.b;
-            total = mass(ma, mb);
-        }
-        const double target = (double)s_u[0] * total;
-        double before = 0.0;
-        // (rounding can leave the target at the end of the last part that holds anything: then it is that part's last token)
-        int owner = -1, last = 0;
-        for (int r = 0; r < C && owner < 0; ++r) {
-            const double part = __longlong_as_double((long long)parts[r].a);
-            if (part > 0.0) last = r;
-            if (target < before + part) owner = r;
-            else before += part;
-        }
-        bool take_last = owner < 0;
-        if (take_last) owner = last;
-        if (owner != (int)rank) { next = -2; break; }          // another thread block writes the token
-        int in_warp = -1;
-        last = 0;
-        for (int k = 0; k < kVerWarps && in_warp < 0; ++k) {
-            if (s_mass[k] > 0.0) last = k;
-            if (!take_last && target < before + s_mass[k]) in_warp = k;
-            else before += s_mass[k];
-        }
-        take_last = take_last || in_warp < 0;
-        if (in_warp < 0) in_warp = last;
-        if (in_warp != warp) { next = -2; break; }             // another warp writes it
-        int found = -1, last_pos = -1;
-        double run_sum = before;
-        for (int vb = v0; vb < v1 && found < 0; vb += 32) {
-            const int v = vb + lane;
-            double f[N], sum = 0.0;
-            int my_last = -1;
-            if (v < v1) {
-                float x[N];
-                row.load(v, x);
-                const int i0 = row.first(v);
+        if (cmd == kSearch) {
+            next = -2;                                             // (some warp of the cluster writes the token)
+            if (ctl.in_warp == warp) {
+                // in index order through the warp's vectors: the first one at whose end the running sum exceeds the target
+                // (or the last one that holds anything), then through its elements
+                const double target = ctl.target;
+                bool take_last = ctl.take_last;
+                double run_sum = ctl.before, upto = 0.0;           // upto: the running sum in front of the vector
+                int vec = -1;
+                bool done = false;
+                for (int ch = 0; ch < n_chunks && !done; ++ch) {
+                    const int vc = v0 + cap * ch, ve = min(vc + cap, v1);
+                    if (n_chunks > 1) chunk_mass<LT>(ctl, row, vc, ve, lane, true, my_row, my_sum, s_table, s_tok);
+                    for (int vb = vc; vb < ve && !done; vb += 32) {
+                        const double own = vb + lane < ve ? my_sum[vb - vc] : 0.0;
+                        double incl = own;
 #pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    f[k] = share(x[k], i0 + k, ma, mb);
-                    sum += f[k];
-                    if (f[k] > 0.0) my_last = i0 + k;
-                }
-            }
-            double incl = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double up = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += up;
-            }
-            const unsigned hit = __ballot_sync(0xffffffffu, !take_last && my_last >= 0 && run_sum + incl > target);
-            if (hit) {
-                int mine = my_last;
-                if (lane == __ffs(hit) - 1) {
-                    double acc = run_sum + (incl - sum);
-                    const int i0 = row.first(v);
-#pragma unroll
-                    for (int k = N - 1; k >= 0; --k) {         // from the back: the lowest index that exceeds the target
-                        double upto = acc;
-#pragma unroll
-                        for (int e = 0; e <= k; ++e) upto += f[e];
-                        if (f[k] > 0.0 && upto > target) mine = i0 + k;
+                        for (int o = 1; o < 32; o <<= 1) {
+                            const double up = __shfl_up_sync(0xffffffffu, incl, o);
+                            if (lane >= o) incl += up;
+                        }
+                        const unsigned any = __ballot_sync(0xffffffffu, own > 0.0);
+                        const unsigned hit = take_last ? 0u : __ballot_sync(0xffffffffu, own > 0.0 && run_sum + incl > target);
+                        if (hit | any) {
+                            const int at = hit ? __ffs(hit) - 1 : 31 - __clz(any);
+                            vec = vb + at;                         // (without a hit: the last one so far)
+                            upto = run_sum + shfl_d(incl - own, at);
+                        }
+                        done = hit != 0;
+                        run_sum += shfl_d(incl, 31);
                     }
                 }
-                found = __shfl_sync(0xffffffffu, mine, __ffs(hit) - 1);
+                take_last |= !done;                                // no vector ends beyond the target: the last one's last token
+                next = -1;
+                if (vec >= 0 && lane == 0) {
+                    const int i0 = row.first(vec);
+                    double acc = upto;
+#pragma unroll 1
+                    for (int k = 0; k < N; ++k) {
+                        const int i = i0 + k;
+                        if (i < 0 || i >= p.V) continue;
+                        bool out = false;
+                        for (unsigned long long t = ctl.tried; t; t &= t - 1) out |= s_tok[__ffsll((long long)t) - 1] == i;
+                        if (out) continue;
+                        const float l = Logit<LT>::one(row_ptr + i);
+                        double f = weight(!ctl.infinite ? l : l == CUDART_INF_F ? 0.f : -CUDART_INF_F, ctl.d, s_table);
+                        if (ctl.mb != 0.0) f = fmax(ctl.ma * f - ctl.mb * (double)q_row[i], 0.0);
+                        if (!(f > 0.0)) continue;
+                        next = i;                                  // (the last positive one so far)
+                        acc += f;
+                        if (!take_last && acc > target) break;
+                    }
+                }
+                if (lane == 0) p.next_token[b] = next;
             }
-            const unsigned any = __ballot_sync(0xffffffffu, my_last >= 0);
-            if (any) last_pos = __shfl_sync(0xffffffffu, my_last, 31 - __clz(any));
-            run_sum += __shfl_sync(0xffffffffu, incl, 31);
         }
-        next = found >= 0 ? found : last_pos;
         break;
     }
-    // greedy and empty rows: every thread knows the token, block 0 writes it; sampled: one warp does (the others have -2)
-    __syncthreads();
-    if (rank == 0) {
-        for (int i = tid; i < p.M; i += kVerThreads) p.path[(long long)b * p.M + i] = i < n_path ? s_path[i] : -1;
-        if (tid == 0) p.n_commit[b] = n_path;
+    // the path, and the token of greedy requests and of rows that leave nothing (-1)
+    if (rank == 0 && warp == 0) {
+        for (int i = lane; i < p.M; i += 32) p.path[(long long)b * p.M + i] = i < n_path ? s_path[i] : -1;
+        if (lane == 0) {
+            p.n_commit[b] = n_path;
+            if (ctl.cmd == kEnd) p.next_token[b] = next;
+        }
     }
-    if (next != -2 && lane == 0 && (next >= 0 && sampled ? true : rank == 0 && warp == 0)) p.next_token[b] = next;
 }
 
 template <typename LT>
-static cudaError_t launch_verify(const VerifyParams &p, int batch, int C, cudaStream_t st)
+static cudaError_t launch_verify(const VerifyParams &p, int batch, cudaStream_t st)
 {
+    // As many thread blocks per request as there are places for at two per SM (clusters of eight do not fit everywhere, so
+    // one place per SM is counted on for them), at least 2,048 tokens for each block.
+    int C = kVerMaxCluster;
+    while (C > 1 && ((long long)batch * C > (C == 8 ? 1 : 2) * sm_count() || p.V < C * 2048)) C >>= 1;
+    const int vecs = (p.V + 2 * (Logit<LT>::N - 1)) / Logit<LT>::N;               // of an unaligned row
+    const int per_warp = (vecs + C * kVerWarps - 1) / (C * kVerWarps);
+    int cap = (per_warp + 31) / 32 * 32;
+    constexpr int most = (int)((size_t)100 * 1024 / (kVerWarps * 24)) / 32 * 32;   // two thread blocks per SM
+    if (cap > most) cap = most;
+    const size_t smem = (size_t)kVerWarps * cap * 24;
+    cudaError_t e = cudaSuccess;
+    if (smem > 46 * 1024) e = cudaFuncSetAttribute(verify_tree_kernel<LT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
     prefer_max_shared_carveout(verify_tree_kernel<LT>);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -453,10 +749,11 @@ static cudaError_t launch_verify(const VerifyParams &p, int batch, int C, cudaSt
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(batch * C));
     cfg.blockDim = dim3(kVerThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, verify_tree_kernel<LT>, p, C);
+    return cudaLaunchKernelEx(&cfg, verify_tree_kernel<LT>, p, C, cap);
 }
 
 }  // namespace oasis
@@ -490,15 +787,13 @@ extern "C" int oasis_verify_tree(int32_t batch, int32_t n_tree, int32_t vocab, c
     VerifyParams p;
     p.logits = logits; p.tokens = tokens; p.parent = parent; p.n_nodes = n_nodes; p.uniforms = uniforms;
     p.temperature = temperature; p.draft = draft_probs; p.path = path; p.n_commit = n_commit; p.next_token = next_token;
+    p.err = error_word();
     p.lb = logits_batch_stride; p.lr = logits_row_stride; p.db = draft_batch_stride; p.dr = draft_row_stride;
     p.T = n_tree; p.V = vocab; p.M = max_path;
-    // as many thread blocks per request as the SMs take at two each, at least 2,048 tokens for each
-    int C = kVerMaxCluster;
-    while (C > 1 && ((long long)batch * C > 2ll * sm_count() || vocab < C * 2048)) C >>= 1;
     cudaError_t e;
-    if (logits_type == OASIS_F32) e = launch_verify<float>(p, batch, C, (cudaStream_t)stream);
-    else if (logits_type == OASIS_BF16) e = launch_verify<__nv_bfloat16>(p, batch, C, (cudaStream_t)stream);
-    else e = launch_verify<__half>(p, batch, C, (cudaStream_t)stream);
+    if (logits_type == OASIS_F32) e = launch_verify<float>(p, batch, (cudaStream_t)stream);
+    else if (logits_type == OASIS_BF16) e = launch_verify<__nv_bfloat16>(p, batch, (cudaStream_t)stream);
+    else e = launch_verify<__half>(p, batch, (cudaStream_t)stream);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(OASIS_ERR_CUDA, "%s: launch: %s", who, cudaGetErrorString(e));
