@@ -19,13 +19,14 @@
 
 namespace oasis {
 
-constexpr int kVerThreads = 512;
+constexpr int kVerThreads = 256;
 constexpr int kVerWarps = kVerThreads / 32;
 constexpr int kVerMaxCluster = 8;
-// The fp32 sum of exponentials is off by less than 1e-3 of itself: a term of weight 2^-x has a relative error below
-// (1.5 x + 4) 2^-23; a lane adds at most 2^22 / 512 / 4 = 2048 partial sums one after the other (2048 * 2^-24) and may
-// rescale as often (2048 * 2^-22) -- 7e-4 together at the largest vocabulary.
-constexpr double kFuzzy = 1e-3;
+// The fp32 sum of exponentials is off by less than 2e-3 of itself: m c2 is rounded (2^-12, a common factor), a term of
+// weight 2^-x has a relative error below (1.5 x + 4) 2^-23, and a lane adds at most 2^22 / 512 / 4 = 2048 pairs to an
+// accumulator one after the other (2048 * 2^-24) -- 4e-4 together at the largest vocabulary; the careful loop, one
+// accumulator for up to 8192 terms, is off by 5e-4.
+constexpr double kFuzzy = 2e-3;
 
 struct VerifyParams {
     const void *logits;
@@ -141,50 +142,52 @@ struct __align__(16) Pair { uint64_t a, b; };
 //   max(a * w - b * q, 0)   with w = exp((logit - m) / temperature); rejected tokens without a draft row are left out
 struct Dist {
     float l_min;                       // logits up to here have weight 0: 250 temperatures below m, and everything but m at tiny ones
-    double m, c;                       // c = 1024 log2(e) / temperature
+    double m, c;                       // c = 64 log2(e) / temperature
     double a, b;
     const float *q;                    // the draft's row, or NULL
 };
 
-// 2^(j / 1024), made at compile time from square roots (Newton's iteration) of two: the binary digits of j pick the factors.
-constexpr int kExpTable = 1024;
+// 2^(j / 64), made at compile time from square roots (Newton's iteration) of two: the binary digits of j pick the factors.
+// Sixteen copies of each, so that the 16 lanes of a shared-memory wavefront read 16 different banks whatever their j.
+constexpr int kExpSteps = 64, kExpCopies = 16, kExpTable = kExpSteps * kExpCopies;
 struct ExpTable {
     double v[kExpTable];
     constexpr ExpTable() : v()
     {
-        double root[10] = {};
+        double root[6] = {};
         double x = 2.0;
-        for (int i = 9; i >= 0; --i) {                     // root[i] = 2^(2^i / 1024)
+        for (int i = 5; i >= 0; --i) {                     // root[i] = 2^(2^i / 64)
             double y = 1.0 + (x - 1.0) / 2;
             for (int k = 0; k < 8; ++k) y = (y + x / y) / 2;
             x = root[i] = y;
         }
-        for (int j = 0; j < kExpTable; ++j) {
+        for (int j = 0; j < kExpSteps; ++j) {
             double f = 1.0;
-            for (int i = 0; i < 10; ++i)
+            for (int i = 0; i < 6; ++i)
                 if ((j >> i) & 1) f *= root[i];
-            v[j] = f;
+            for (int k = 0; k < kExpCopies; ++k) v[j * kExpCopies + k] = f;
         }
     }
 };
 __device__ const ExpTable g_exp_table = ExpTable();
 
-// exp((l - m) / temperature) in fp64, to about 1e-14 of itself.  With y = (l - m) c and n = y rounded to a whole number,
-//   2^(y / 1024) = 2^floor(n / 1024) * T[n mod 1024] * exp(r ln 2 / 1024),  r = y - n,  |r| <= 1 / 2,
-// and the series' fourth term is below 6e-16.  Ten instructions for the fp64 units, one conversion and one table look-up:
-// exp() takes twice as long, and this is the pass over 152,000 logits that the last node of every walk needs.  l = m gives
-// exactly 1, so equal logits have equal weights and sums of them are exact.
-__device__ __forceinline__ double weight(float l, const Dist &d, const double *table)
+// exp((l - m) / temperature) in fp64, to about 1e-13 of itself.  With y = (l - m) c and n = y rounded to a whole number,
+//   2^(y / 64) = 2^floor(n / 64) * T[n mod 64] * exp(z),  z = (y - n) ln 2 / 64,  |z| <= 0.0055,
+// and four terms of the series for exp(z) - 1 leave 4e-14.  Kept to 33 bits: sums of equal weights are then exact, so that
+// a random number that falls on a border between equal logits is decided as in exact arithmetic.  This is the pass over
+// 152,000 logits that the last node of every walk needs; exp() takes 2.5 times as long (19.7 against 7.8 cycles per 32
+// logits and SM, with a table of 1,024 steps that had bank conflicts).
+__device__ __forceinline__ double weight(float l, const Dist &d, const double *table)       // table: this lane's copy
 {
-    constexpr double kStep = 0.69314718055994530942 / kExpTable, kRound = 6755399441055744.0;   // 1.5 * 2^52
+    constexpr double kStep = 0.69314718055994530942 / kExpSteps, kRound = 6755399441055744.0;   // 1.5 * 2^52
     const double y = ((double)l - d.m) * d.c;
     const double t = y + kRound;
     const int n = __double2loint(t);
     const double r = y - (t - kRound);
-    const double f = table[n & (kExpTable - 1)];
-    const double e = fma(r, fma(r, kStep * kStep * kStep / 6, kStep * kStep / 2), kStep);
+    const double f = table[(n & (kExpSteps - 1)) * kExpCopies];
+    const double e = fma(r, fma(r, fma(r, kStep * kStep * kStep * kStep / 24, kStep * kStep * kStep / 6), kStep * kStep / 2), kStep);
     const double w = fma(f * r, e, f);
-    const double scaled = __hiloint2double(__double2hiint(w) + ((n & ~(kExpTable - 1)) << 10), __double2loint(w));
+    const double scaled = __hiloint2double(__double2hiint(w) + ((n & ~(kExpSteps - 1)) << 14), __double2loint(w) & 0xfff00000);
     return l > d.l_min ? scaled : 0.0;                     // (also for NaN and -infinity)
 }
 
@@ -222,6 +225,7 @@ __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row
     }
     const Dist d = ctl.d;
     const double ma = ctl.ma, mb = ctl.mb;
+    const double *const my_table = table + (lane & (kExpCopies - 1));
     double sum = 0.0;
     if (d.q && mb == 0.0)                                          // a pass under the draft's row may follow: on its way to L2
         for (int i = max(row.first(vc), 0) + lane * 32; i < min(row.first(ve), row.V); i += 32 * 32)
@@ -230,9 +234,14 @@ __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row
 #pragma unroll 1
         for (int v = vc + lane; v < ve; v += 32) {
             const uint4 w = my_row[v - vc - lane];
-            double part = 0.0;
+            double f[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) part += weight(Logit<LT>::get(w, k), d, table);
+            for (int k = 0; k < N; ++k) f[k] = weight(Logit<LT>::get(w, k), d, my_table);
+#pragma unroll
+            for (int o = 1; o < N; o <<= 1)
+#pragma unroll
+                for (int k = 0; k < N; k += 2 * o) f[k] += f[k + o];
+            const double part = f[0];
             my_sum[v - vc - lane] = part;
             sum += part;
         }
@@ -245,19 +254,28 @@ __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row
                 f[k] = mb != 0.0 && v < ve && i >= 0 && i < row.V ? d.q[i] : 0.f;
             }
         };
+        const bool plain = !ctl.infinite;
         fetch(vc + lane, q);
 #pragma unroll 1
         for (int v = vc + lane; v < ve; v += 32) {
             fetch(v + 32, q_next);
             const uint4 w = my_row[v - vc - lane];
             double part = 0.0;
+            if (plain) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) {                          // (outside the row the logit is -infinity)
-                const float l = Logit<LT>::get(w, k);
-                const double f = weight(!ctl.infinite ? l : l == CUDART_INF_F ? 0.f : -CUDART_INF_F, d, table);
-                part += mb == 0.0 ? f : fmax(ma * f - mb * (double)q[k], 0.0);
-                q[k] = q_next[k];
+                for (int k = 0; k < N; ++k)                        // (outside the row the logit is -infinity)
+                    part += fmax(ma * weight(Logit<LT>::get(w, k), d, my_table) - mb * (double)q[k], 0.0);
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < N; ++k) {
+                    const float l = Logit<LT>::one(reinterpret_cast<const LT *>(my_row + (v - vc - lane)) + k);
+                    const double f = weight(!ctl.infinite ? l : l == CUDART_INF_F ? 0.f : -CUDART_INF_F, d, my_table);
+                    const int i = row.first(v) + k;
+                    part += mb == 0.0 ? f : i >= 0 && i < row.V ? fmax(ma * f - mb * (double)d.q[i], 0.0) : 0.0;
+                }
             }
+#pragma unroll
+            for (int k = 0; k < N; ++k) q[k] = q_next[k];
             my_sum[v - vc - lane] = part;
             sum += part;
         }
@@ -323,8 +341,8 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
     }
     const bool sampled = temp > 0.f;
     if (sampled) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(s_table + 2 * tid)), "l"(g_exp_table.v + 2 * tid) : "memory");
-        static_assert(kExpTable == 2 * kVerThreads, "one copy per thread");
+        for (int i = 2 * tid; i < kExpTable; i += 2 * kVerThreads)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(s_table + i)), "l"(g_exp_table.v + i) : "memory");
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
     if (tid < OASIS_MAX_TREE) {
@@ -337,7 +355,7 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
     if (tid == 0) {
         s_path[0] = 0;
         ctl.ahead = n > 1 ? 1 : -1;
-        ctl.d.c = 1024.0 * 1.4426950408889634 * (sampled ? fmax(1.0 / (double)temp, 1e-300) : 0.0);
+        ctl.d.c = kExpSteps * 1.4426950408889634 * (sampled ? fmax(1.0 / (double)temp, 1e-300) : 0.0);
         mbar_init(smem_u32(&s_bar[0]), 1);
         mbar_init(smem_u32(&s_bar[1]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -406,28 +424,51 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                 const int vc = v0 + cap * ch, ve = min(vc + cap, v1);
                 if (ch > 0) { row.stage(vc + lane, ve, my_row); stage_wait(); }
                 float top = -CUDART_INF_F;
-#pragma unroll 2
+#pragma unroll 4
                 for (int v = vc + lane; v < ve; v += 32) {
                     const uint4 w = my_row[v - vc - lane];
 #pragma unroll
-                    for (int k = 0; k < N; ++k) top = fmaxf(top, Logit<LT>::get(w, k));         // (a NaN loses)
+                    for (int k = 0; k < N; k += 2) top = max3(top, Logit<LT>::get(w, k), Logit<LT>::get(w, k + 1));   // (a NaN loses)
                 }
                 if (top > m) {
                     s *= m == -CUDART_INF_F ? 0.f : fast_exp2((m - top) * c2);
                     m = top;
                 }
                 if (m == -CUDART_INF_F) continue;
-#pragma unroll 2
-                for (int v = vc + lane; v < ve; v += 32) {
-                    const uint4 w = my_row[v - vc - lane];
-                    float add = 0.f;
+                // x c2 - m c2 as one packed multiply-add for two logits; the rounding of m c2 is a common factor, off by less
+                // than 2^-12 as long as |m c2| < 4096.  Rows with larger ones, NaN or infinities take the careful loop.
+                const float mc = -m * c2;
+                float sum = CUDART_INF_F;
+                if (fabsf(mc) < 4096.f) {
+                    const uint64_t c22 = f32x2(c2, c2), mc2 = f32x2(mc, mc);
+                    uint64_t acc[2] = {0ull, 0ull};
+#pragma unroll 4
+                    for (int v = vc + lane; v < ve; v += 32) {
+                        const uint4 w = my_row[v - vc - lane];
 #pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        const float x = clean(Logit<LT>::get(w, k));
-                        add += x == m ? 1.f : fast_exp2((x - m) * c2);
+                        for (int k = 0; k < N; k += 2) {
+                            float e0, e1;
+                            f32x2_split(fma_f32x2(f32x2(Logit<LT>::get(w, k), Logit<LT>::get(w, k + 1)), c22, mc2), e0, e1);
+                            acc[(k >> 1) & 1] = add_f32x2(acc[(k >> 1) & 1], f32x2(fast_exp2(e0), fast_exp2(e1)));
+                        }
                     }
-                    s += add;
+                    float a0, a1;
+                    f32x2_split(add_f32x2(acc[0], acc[1]), a0, a1);
+                    sum = a0 + a1;
                 }
+                if (!(sum < 1e30f)) {
+                    sum = 0.f;
+#pragma unroll 1
+                    for (int v = vc + lane; v < ve; v += 32) {
+                        const uint4 w = my_row[v - vc - lane];
+#pragma unroll
+                        for (int k = 0; k < N; ++k) {
+                            const float x = clean(Logit<LT>::get(w, k));
+                            sum += x == m ? 1.f : fast_exp2((x - m) * c2);
+                        }
+                    }
+                }
+                s += sum;
             }
             float top = m;
 #pragma unroll
@@ -546,8 +587,8 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                     }
                     // The children in order.  Whatever needs the row's mass in fp64 (a close decision, a rejection against
                     // a draft row, the next token) asks for a pass and comes back.
-                    const double w0 = weight(kid0, d, s_table);
-                    const double w1 = left >> 32 ? weight(kid1, d, s_table) : 0.0;
+                    const double w0 = weight(kid0, d, s_table + (lane & (kExpCopies - 1)));
+                    const double w1 = left >> 32 ? weight(kid1, d, s_table + (lane & (kExpCopies - 1))) : 0.0;
                     need = kNothing;
 #pragma unroll 1
                     while (left) {
