@@ -418,8 +418,22 @@ MAX_TREE = 64
 _LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (torch.cuda.current_stream() takes 3 us)
+
+
+def _cdims(dims):
+    """Reference to the dims' C struct, made once per Dims object (it is immutable)."""
+    ref = dims.__dict__.get("_ref")
+    if ref is None:
+        ref = ctypes.byref(dims.c())
+        dims.__dict__["_ref"] = ref
+    return ref
+
+
 def _dev(t, dtype, shape, name, device):
     """Address of a dense tensor of this type and shape on `device` (the current device's index)."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
     if t.shape != shape:
@@ -442,9 +456,9 @@ def _pool_ptr(t, dtype, name, device, host_ok=False):
     return t.data_ptr()
 
 
-def _stream_id(stream):
+def _stream_id(stream, device):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -463,18 +477,17 @@ def tree_attn(dims, q, tree_kv, parent, n_nodes, hbm_pool, slot_tbl, blk_tbl, se
     n_cols = blk_tbl.shape[-1]
     dev = torch.cuda.current_device()
     bf, i32 = torch.bfloat16, torch.int32
-    d = dims.c()
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("workspace must be contiguous and on the current CUDA device")
     _check(lib().oasis_tree_attn(
-        ctypes.byref(d), _dev(q, bf, (B, T, Hq, 128), "q", dev), T, _dev(tree_kv, bf, (B, T, Hkv, 2, 128), "tree_kv", dev),
+        _cdims(dims), _dev(q, bf, (B, T, Hq, 128), "q", dev), T, _dev(tree_kv, bf, (B, T, Hkv, 2, 128), "tree_kv", dev),
         _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, (B,), "n_nodes", dev),
         _pool_ptr(hbm_pool, bf, "hbm_pool", dev), _dev(slot_tbl, i32, (B, Hkv, n_cols), "slot_tbl", dev),
         _dev(blk_tbl, i32, (B, Hkv, n_cols), "blk_tbl", dev), n_cols, _dev(seq_len, i32, (B,), "seq_len", dev), scale,
         _dev(out, bf, (B, T, Hq, 128), "out", dev),
         None if lse is None else _dev(lse, torch.float32, (B, T, Hq), "lse", dev),
-        None if workspace is None else workspace.data_ptr(), ws_bytes, _stream_id(stream)), "oasis_tree_attn")
+        None if workspace is None else workspace.data_ptr(), ws_bytes, _stream_id(stream, dev)), "oasis_tree_attn")
 
 
 def _rows(t, name, B, T, V, dev):
@@ -519,7 +532,7 @@ def verify_tree(logits, tokens, parent, n_nodes, uniforms, temperature, path, n_
         _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, (B,), "n_nodes", dev),
         _dev(uniforms, f32, (B, T), "uniforms", dev), _dev(temperature, f32, (B,), "temperature", dev), dp, db, dr,
         _dev(path, i32, (B, M), "path", dev), M, _dev(n_commit, i32, (B,), "n_commit", dev),
-        _dev(next_token, i32, (B,), "next_token", dev), _stream_id(stream)), "oasis_verify_tree")
+        _dev(next_token, i32, (B,), "next_token", dev), _stream_id(stream, dev)), "oasis_verify_tree")
 
 
 class CommitPlan:
@@ -538,7 +551,7 @@ class CommitPlan:
         self.T, self.n_cols, self.n_layers, self.local_col, self.batch = tree_kvs[0].shape[1], blk_tbls[0].shape[-1], n, int(local_col), B
         arr = ctypes.c_void_p * n
         bf, i32 = torch.bfloat16, torch.int32
-        self.dims = dims.c()
+        self.dims = _cdims(dims)
         self.tree_kvs = arr(*[_dev(t, bf, (B, self.T, Hkv, 2, 128), "tree_kvs", dev) for t in tree_kvs])
         self.block_tables = arr(*[_dev(t, i32, (B, dims.max_blocks), "block_tables", dev) for t in block_tables])
         self.slot_tbls = arr(*[_dev(t, i32, (B, Hkv, self.n_cols), "slot_tbls", dev) for t in slot_tbls])
@@ -559,7 +572,7 @@ def commit_kv_layers(plan, path, n_commit, seq_len, next_len=None, stream=None):
         plan.dims, plan.n_layers, plan.tree_kvs, plan.T, _dev(path, i32, (B, M), "path", dev), M,
         _dev(n_commit, i32, (B,), "n_commit", dev), _dev(seq_len, i32, (B,), "seq_len", dev), plan.block_tables, plan.slot_tbls,
         plan.blk_tbls, plan.n_cols, plan.local_col, plan.pools, plan.host_kvs,
-        None if next_len is None else _dev(next_len, i32, (B,), "next_len", dev), _stream_id(stream)), "oasis_commit_kv_layers")
+        None if next_len is None else _dev(next_len, i32, (B,), "next_len", dev), _stream_id(stream, dev)), "oasis_commit_kv_layers")
 
 
 def commit_kv(dims, tree_kv, path, n_commit, seq_len, block_table, slot_tbl, blk_tbl, local_col, hbm_pool, host_kv=None,

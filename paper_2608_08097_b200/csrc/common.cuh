@@ -111,6 +111,27 @@ inline void prefer_max_shared_carveout_of(const void *kernel)
     if (n_seen < 256) seen[n_seen++] = kernel;
 }
 
+// Allows a kernel `bytes` of dynamic shared memory on the current device; asks the runtime only for what it has not granted yet.
+inline cudaError_t allow_dynamic_shared(const void *kernel, int bytes)
+{
+    static std::mutex lock;
+    static struct { const void *kernel; int device, bytes; } seen[256];
+    static int n_seen = 0;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> guard(lock);
+    int i = 0;
+    while (i < n_seen && !(seen[i].kernel == kernel && seen[i].device == dev)) ++i;
+    if (i < n_seen && seen[i].bytes >= bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && i < 256) {
+        seen[i] = {kernel, dev, bytes};
+        if (i == n_seen) ++n_seen;
+    }
+    return e;
+}
+
 template <typename K>
 inline void prefer_max_shared_carveout(K kernel)
 {

@@ -14,8 +14,8 @@
 //     ancestor bits for tree blocks.  Ancestors come from the parents by pointer doubling (six rounds for 64 nodes).
 //   - Key rows that no query may see hold anything, NaN included, and 0 x NaN is NaN in P V: before P is handed to the
 //     tensor core, the softmax warps overwrite those V rows with zeros in shared memory (masked tiles only).
-//   - More than 128 query rows are cut into row groups of equal size; the groups of a row are neighbouring thread blocks,
-//     which read the same entries at the same time, so all but one come from L2.
+//   - Up to 256 query rows share a thread block (two MMAs of 128 rows per tile); more are cut into row groups of equal
+//     size, neighbouring thread blocks that read the same entries at the same time, so that all but one come from L2.
 // Algorithmic traffic: 8 KiB per (request, KV head, visible column), 512 B per (node, KV head), plus Q, O and lse.
 #include <cuda.h>
 #include <math_constants.h>
@@ -25,16 +25,26 @@
 
 namespace oasis {
 
-constexpr int kTrThreads = 224;                             // producer, Q K^T issuer, P V issuer, four softmax warps
-__host__ __device__ constexpr int tr_threads(int mma_m, int copies) { return kTrThreads + (at_softmax_sets(mma_m, copies) - 1) * 128; }
-constexpr int kTrStages = 7;
+// Warp sets of four softmax warps: one, or two that take alternate tiles (65 to 128 rows) or half the rows each (PAIR).
+__host__ __device__ constexpr int tr_sets(int mma_m, int copies, bool pair) { return pair ? 2 : at_softmax_sets(mma_m, copies); }
+__host__ __device__ constexpr int tr_threads(int mma_m, int copies, bool pair)    // producer, two MMA issuers, softmax warps
+{
+    return 96 + 128 * tr_sets(mma_m, copies, pair);
+}
+// The query rows in shared memory: [dim half][MMA rows][128 B], 128-byte swizzle.
+__host__ __device__ constexpr int tr_rows(int mma_m, bool pair) { return pair ? 256 : mma_m; }
+__host__ __device__ constexpr int tr_stages(bool pair) { return pair ? 5 : 6; }      // of 32 KiB; with the queries 224 KiB at most
 constexpr int32_t kTreeTag = 0x40000000;                    // tile_blk: kTreeTag + i = block i of the tree buffer
 // Behind the ring: 512 B of barriers and tile ids, two table windows, the producer's block queue, ancestor masks.
 constexpr int kTrQueue = 64;
 constexpr int kTrUp = 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 4) + 16 * kAtMaxStages;   // parents: behind barriers and tile ids
+constexpr int kTrPlain = kTrUp + OASIS_MAX_TREE;                                       // one word per stage
 constexpr int kTrMisc = 512 + 2 * kWinBytes + kTrQueue * 8 + OASIS_MAX_TREE * 8;
-constexpr size_t kTrSmem = 1024 + (size_t)kTrStages * kAtStageBytes + kTrMisc;
-static_assert(kTrUp + OASIS_MAX_TREE <= 512 && kTrSmem <= 232448, "shared memory of a thread block");
+__host__ __device__ constexpr int tr_smem(int mma_m, bool pair)
+{
+    return 1024 + tr_rows(mma_m, pair) * kRowBytes + tr_stages(pair) * kAtStageBytes + kTrMisc;
+}
+static_assert(kTrPlain + 4 * kAtMaxStages <= 512 && tr_smem(128, false) <= 232448 && tr_smem(128, true) <= 232448, "shared memory of a thread block");
 
 struct TreeAttnParams {
     const uint8_t *q;
@@ -45,81 +55,104 @@ struct TreeAttnParams {
     float *part_lse;    // [items][rows per group]      log2 domain
     int32_t *err;
     float scale_log2;
-    int T, Hq, Hkv, G, n_cols, R, n_splits, cols_per_split, n_groups, group_rows;
+    int T, Hq, Hkv, G, n_cols, R, n_splits, cols_per_split, n_groups, group_rows;      // group_rows: a multiple of G
     long long n_slots;  // bounds-check build: slots of the working-set pool (else unused)
 };
 
 __device__ __forceinline__ bool block_seen(int blk, int len) { return blk >= 0 && (long long)blk * kBlock < len; }
 
-template <int MMA_M, int COPIES>
-__global__ void __launch_bounds__(tr_threads(MMA_M, COPIES), 1)
-tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ CUtensorMap tree_map, const TreeAttnParams p)
+// PAIR: 129 to 256 query rows, two MMAs of 128 rows per tile.  Each set of softmax warps owns 128 rows and takes every tile;
+// both have two S buffers and an O accumulator, which fills the tensor memory.
+template <int MMA_M, int COPIES, bool PAIR>
+__global__ void __launch_bounds__(tr_threads(MMA_M, COPIES, PAIR), 1)
+tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ CUtensorMap tree_map,
+                    const __grid_constant__ CUtensorMap q_map, const TreeAttnParams p)
 {
     constexpr int RPC = MMA_M / COPIES;                     // MMA rows per copy of the query rows
     constexpr int LANES = MMA_M / 4;                        // lanes of each softmax warp that hold an MMA row
     constexpr int BPC = kAtTileCols / COPIES;               // blocks of a tile each copy handles
-    constexpr int SETS = at_softmax_sets(MMA_M, COPIES);    // softmax warp sets, taking alternate tiles
-    constexpr int SBUFS = at_s_bufs(SETS);                  // S / P buffers in tensor memory
-    constexpr int THREADS = tr_threads(MMA_M, COPIES);
+    static_assert(!PAIR || (MMA_M == 128 && COPIES == 1), "two tiles of 128 query rows");
+    constexpr int SETS = PAIR ? 1 : at_softmax_sets(MMA_M, COPIES);    // softmax warp sets that take alternate tiles
+    constexpr int HALVES = PAIR ? 2 : 1;                    // MMA tiles of query rows
+    constexpr int SBUFS = PAIR ? 2 : kAtSBufs;              // S / P buffers in tensor memory (of each half)
+    constexpr int QHALF = tr_rows(MMA_M, PAIR) * 128;       // bytes of the query rows' first 64 dims
+    constexpr int THREADS = tr_threads(MMA_M, COPIES, PAIR);
+    constexpr int STAGES = tr_stages(PAIR);
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t kv_u32 = base;                                    // [stages][32 KiB]
-    uint8_t *misc = base_ptr + (size_t)kTrStages * kAtStageBytes;
+    uint8_t *const kv_ptr = base_ptr + 2 * QHALF;                    // [stages][32 KiB]
+    const uint32_t kv_u32 = base + 2 * QHALF;
+    uint8_t *misc = kv_ptr + (size_t)STAGES * kAtStageBytes;
     const uint32_t bar_u32 = smem_u32(misc);
     auto bar_full = [&](int s) { return bar_u32 + 8u * s; };
     auto bar_empty = [&](int s) { return bar_u32 + 8u * (kAtMaxStages + s); };
     auto bar_s_full = [&](int a) { return bar_u32 + 8u * (2 * kAtMaxStages + a); };
     auto bar_p_full = [&](int a) { return bar_u32 + 8u * (2 * kAtMaxStages + kAtSBufs + a); };
+    const uint32_t bar_q = bar_u32 + 8u * (2 * kAtMaxStages + 2 * kAtSBufs);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc + 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 2));
     int32_t *s_count = reinterpret_cast<int32_t *>(misc + 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 2) + 4);
     int32_t *tile_blk = reinterpret_cast<int32_t *>(misc + 8 * (2 * kAtMaxStages + 2 * kAtSBufs + 4));   // [stages][4]
     int32_t *win = reinterpret_cast<int32_t *>(misc + 512);                                             // two table windows
     int2 *queue = reinterpret_cast<int2 *>(misc + 512 + 2 * kWinBytes);                                  // (block, slot)
     unsigned long long *anc = reinterpret_cast<unsigned long long *>(queue + kTrQueue);                   // [T] ancestor masks
+    int32_t *plain = reinterpret_cast<int32_t *>(misc + kTrPlain);                                        // [stages]: all keys visible
     int8_t *up = reinterpret_cast<int8_t *>(misc + kTrUp);                                                // [T]
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    // the merge launch behind this one (split runs) may bring its thread blocks onto the SMs already; it waits for the partials
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int grp = blockIdx.x % p.n_groups;
     const int split = (blockIdx.x / p.n_groups) % p.n_splits;
     const int bh = blockIdx.x / (p.n_groups * p.n_splits);
     const int b = bh / p.Hkv, h = bh % p.Hkv;
-    const int n_nodes = max(0, min(p.n_nodes[b], p.T));
     const int row0 = grp * p.group_rows;                             // first query row (node * G + head) of the group
-    const int rows = min(min(p.group_rows, p.R - row0), n_nodes * p.G - row0);
-    if (rows <= 0) return;                                           // only padding nodes: nothing is read or written
     const int c0 = split * p.cols_per_split;
     const int c1 = min(c0 + p.cols_per_split, p.n_cols);
-    const int L = p.seq_len[b];
-    // blocks of the tree buffer that the group's rows may see (ancestors have lower indices), taken by the last split
-    const int n_tree_blk = split == p.n_splits - 1 ? (row0 + rows - 1) / p.G / kBlock + 1 : 0;
     const int32_t *slot_row = p.slot_tbl + (long long)bh * p.n_cols;
     const int32_t *blk_row = p.blk_tbl + (long long)bh * p.n_cols;
-
-    // ---- set-up: barriers, tensor memory, Q operand, ancestor masks, number of tiles -------------------
+    // a launch behind this one (the merge of the splits, or the next attention) may bring its thread blocks onto the SMs
+    // already, and this one may have been brought so: what earlier launches wrote is read from here on
     if (tid == 0) {
         for (int s = 0; s < kAtMaxStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
         for (int a = 0; a < kAtSBufs; ++a) { mbar_init(bar_s_full(a), 1); mbar_init(bar_p_full(a), 4); }
+        mbar_init(bar_q, 1);
         *s_count = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 0 && c0 < c1) window_request(smem_u32(win), lane, blk_row, slot_row, c0 + lane, c1);     // (needs no length)
+    // every first load is on its way before the first is used: lengths, this thread's column, the parents (warp 2)
+    const int n_nodes_raw = p.n_nodes[b], L = p.seq_len[b];
+    const int my_col = c0 + tid - 32;
+    const int my_blk = warp > 0 && my_col < c1 ? blk_row[my_col] : -1;
+    int par[2] = {-1, -1};
+    if (warp == 2) {
+        if (lane < p.T) par[0] = p.parent[(long long)b * p.T + lane];
+        if (lane + 32 < p.T) par[1] = p.parent[(long long)b * p.T + lane + 32];
+    }
+    const int n_nodes = max(0, min(n_nodes_raw, p.T));
+    const int rows = min(min(p.group_rows, p.R - row0), n_nodes * p.G - row0);
+    if (rows <= 0) {                                                 // only padding nodes: nothing is read or written
+        window_wait();
+        return;
+    }
+    // blocks of the tree buffer that the group's rows may see (ancestors have lower indices), taken by the last split
+    const int n_tree_blk = split == p.n_splits - 1 ? (row0 + rows - 1) / p.G / kBlock + 1 : 0;
+
+    // ---- set-up: tensor memory, ancestor masks, number of tiles --------------------------------------------
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();                             // the barriers exist; the producer starts copying right away
-    uint32_t tmem_base = 0, tmem_o = 0, tmem_q = 0;
+    uint32_t tmem_base = 0, tmem_o = 0;
     int n_tiles = 0;
     if (warp != 0) {
-        // Meanwhile: warp 1 allocates the tensor memory, warp 2 works out the ancestors, all count the visible columns,
-        // and every softmax thread of the first set, owner of one MMA row, loads that row of Q (rows are replicated
-        // across the copies, rows past the group's are zero) and then stores it to its tensor-memory lane.
+        // Meanwhile: warp 1 allocates the tensor memory, warp 2 works out the ancestors, all count the visible columns.
         if (warp == 1) {
             asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                          ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)kAtTmemCols) : "memory");
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
-        int seen = 0;
-        for (int c = c0 + tid - 32; c < c1; c += THREADS - 32) seen += block_seen(blk_row[c], L);
+        int seen = block_seen(my_blk, L);
+        for (int c = my_col + THREADS - 32; c < c1; c += THREADS - 32) seen += block_seen(blk_row[c], L);
         seen = __reduce_add_sync(0xffffffffu, seen);
         if (lane == 0 && seen) atomicAdd(s_count, seen);
         if (warp == 2) {
@@ -128,8 +161,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int t = lane + 32 * e;
-                const int par = t < n_nodes ? p.parent[(long long)b * p.T + t] : -1;
-                u[e] = par >= 0 && par < t ? par : -1;
+                u[e] = t < n_nodes && par[e] >= 0 && par[e] < t ? par[e] : -1;
                 m[e] = 1ull << t;
             }
 #pragma unroll 1
@@ -146,30 +178,12 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
 #pragma unroll
             for (int e = 0; e < 2; ++e) anc[lane + 32 * e] = m[e];
         }
-        uint4 v[16];
-        if (warp >= 3 && warp < 7) {
-            const int m_row = (warp & 3) * LANES + lane;
-            const int r = m_row % RPC;
-#pragma unroll
-            for (int c = 0; c < 16; ++c) v[c] = make_uint4(0, 0, 0, 0);
-            if (lane < LANES && r < rows) {
-                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
-                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + ((((long long)b * p.T + tq) * p.Hq + a) * kHeadDim) * 2);
-#pragma unroll
-                for (int c = 0; c < 16; ++c) v[c] = src[c];
-            }
-        }
         tc_fence_before();
         asm volatile("bar.sync 2, %0;" ::"n"(THREADS - 32) : "memory");
         tc_fence_after();
         n_tiles = (*s_count + n_tree_blk + kAtTileCols - 1) / kAtTileCols;
         tmem_base = *tmem_slot;
-        tmem_o = tmem_base + SBUFS * kAtTileKeys;
-        tmem_q = tmem_o + SETS * kHeadDim;                           // Q as the A operand: 128 rows x 64 packed columns
-        if (warp >= 3 && warp < 7) q_row_to_tmem(tmem_q + ((uint32_t)((warp & 3) * 32) << 16), v);
-        tc_fence_before();
-        asm volatile("bar.sync 2, %0;" ::"n"(THREADS - 32) : "memory");
-        tc_fence_after();
+        tmem_o = tmem_base + HALVES * SBUFS * kAtTileKeys;
     }
 
     if (warp == 0) {
@@ -192,10 +206,12 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
             if (lane == 0) alive = mbar_wait(bar_empty(s), ph, p.err, 41);
             alive = __shfl_sync(0xffffffffu, (int)alive, 0) != 0;
             if (!alive) return;
-            uint8_t *stage = base_ptr + (size_t)s * kAtStageBytes;
+            uint8_t *stage = kv_ptr + (size_t)s * kAtStageBytes;
             const uint32_t stage_u32 = kv_u32 + s * kAtStageBytes;
             const unsigned valid = __ballot_sync(0xffffffffu, lane < kAtTileCols && blk >= 0);
+            const unsigned full = __ballot_sync(0xffffffffu, lane < kAtTileCols && blk >= 0 && blk < kTreeTag && L - blk * kBlock >= kBlock);
             if (lane < kAtTileCols) tile_blk[s * kAtTileCols + lane] = blk;
+            if (lane == 0) plain[s] = full == 0xfu;
             if ((valid & 0xfu) != 0xfu) {
                 // a missing block contributes P = 0, which must not meet stale NaN patterns: the warp zeroes its V image
 #pragma unroll
@@ -220,10 +236,19 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
                     tma_load_5d(dst + kImgGroup, &tree_map, 0, t + 8, 2 * h, 0, b, bar_full(s));
                 }
             }
-            ph ^= (s + 1 == kTrStages);
-            s = (s + 1 == kTrStages) ? 0 : s + 1;
+            ph ^= (s + 1 == STAGES);
+            s = (s + 1 == STAGES) ? 0 : s + 1;
         };
-        if (c0 < c1) window_request(win_u32, lane, blk_row, slot_row, c0 + lane, c1);
+        if (lane == 0) {
+            // the group's query rows, once per copy: box = the tokens' rows of this KV head, one dim half
+            mbar_arrive_expect_tx(bar_q, (uint32_t)(COPIES * 2 * p.group_rows * 128));
+#pragma unroll
+            for (int c = 0; c < COPIES; ++c)
+#pragma unroll
+                for (int d = 0; d < 2; ++d)
+                    tma_load_5d(base + d * QHALF + c * RPC * 128, &q_map, 0, 0, h, b * p.T + row0 / p.G, d, bar_q);
+        }
+        __syncwarp();
         for (int c = c0, w = 0; c < c1 && alive; c += kWinCols, w ^= 1) {
             window_wait();
             if (c + kWinCols < c1) window_request(win_u32 + (w ^ 1) * kWinBytes, lane, blk_row, slot_row, c + kWinCols + lane, c1);
@@ -245,24 +270,32 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         // ---------------------------------------------------------------- Q K^T issuer (the whole warp, converged)
         const uint32_t idesc = idesc_qk(MMA_M);
         const uint64_t k_desc0 = smem_desc_sw128_k(kv_u32, kImgGroup);
-        bool alive = true;
+        bool alive = mbar_wait_warp(bar_q, 0, p.err, 50);
         int s = 0, sb = 0, s_old = 0;                                // stage and S buffer of tile i; stage of tile i - SBUFS
         uint32_t ph = 0, ph_old = 0;
         for (int i = 0; i < n_tiles && alive; ++i) {
             // the S buffer also held P of tile i - SBUFS: its P V must have completed
             if (i >= SBUFS) {
                 alive = mbar_wait_warp(bar_empty(s_old), ph_old, p.err, 51);
-                ph_old ^= (s_old + 1 == kTrStages);
-                s_old = (s_old + 1 == kTrStages) ? 0 : s_old + 1;
+                ph_old ^= (s_old + 1 == STAGES);
+                s_old = (s_old + 1 == STAGES) ? 0 : s_old + 1;
             }
             alive = alive && mbar_wait_warp(bar_full(s), ph, p.err, 52);
             if (!alive) break;
             tc_fence_after();
             const uint64_t k_desc = k_desc0 + (uint64_t)((s * kAtStageBytes) >> 4);
-            issue_qk_tile(tmem_base + (uint32_t)(sb * kAtTileKeys), tmem_q, k_desc, idesc);
-            tc_commit(bar_s_full(sb));
-            ph ^= (s + 1 == kTrStages);
-            s = (s + 1 == kTrStages) ? 0 : s + 1;
+#pragma unroll
+            for (int g = 0; g < HALVES; ++g) {
+                const uint64_t q_desc = smem_desc_sw128(base + g * 128 * 128);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    tc_mma_bf16(tmem_base + (uint32_t)((g * SBUFS + sb) * kAtTileKeys),
+                                q_desc + (uint64_t)(((k >> 2) * QHALF + (k & 3) * 32) >> 4),
+                                k_desc + (uint64_t)(((k >> 2) * kImgHalf + (k & 3) * 32) >> 4), idesc, k ? 1u : 0u);
+                tc_commit(bar_s_full(g * SBUFS + sb));
+            }
+            ph ^= (s + 1 == STAGES);
+            s = (s + 1 == STAGES) ? 0 : s + 1;
             sb = (sb + 1 == SBUFS) ? 0 : sb + 1;
         }
     } else if (warp == 2) {
@@ -273,25 +306,31 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         int s = 0, sb = 0;
         uint32_t ph_p = 0;
         for (int i = 0; i < n_tiles && alive; ++i) {
-            alive = mbar_wait_warp(bar_p_full(sb), ph_p, p.err, 53);
-            if (!alive) break;
-            tc_fence_after();
             const uint64_t v_desc = v_desc0 + (uint64_t)((s * kAtStageBytes) >> 4);
-            issue_pv_tile(tmem_o + (uint32_t)((i % SETS) * kHeadDim), tmem_base + (uint32_t)(sb * kAtTileKeys), v_desc, idesc, i < SETS);
+#pragma unroll
+            for (int g = 0; g < HALVES && alive; ++g) {              // (set 0 has also zeroed the V rows that nobody may see)
+                alive = mbar_wait_warp(bar_p_full(g * SBUFS + sb), ph_p, p.err, 53);
+                if (!alive) break;
+                tc_fence_after();
+                issue_pv_tile(tmem_o + (uint32_t)((PAIR ? g : i % SETS) * kHeadDim),
+                              tmem_base + (uint32_t)((g * SBUFS + sb) * kAtTileKeys), v_desc, idesc, i < SETS);
+            }
+            if (!alive) break;
             tc_commit(bar_empty(s));                                 // stage free, and O complete up to this tile
-            s = (s + 1 == kTrStages) ? 0 : s + 1;
+            s = (s + 1 == STAGES) ? 0 : s + 1;
             sb = (sb + 1 == SBUFS) ? 0 : sb + 1;
             ph_p ^= (sb == 0);
         }
     } else {
         // ---------------------------------------------------------------- softmax, one thread per MMA row
         const int set = SETS == 2 ? (warp - 3) >> 2 : 0;
+        const int half = PAIR ? (warp - 3) >> 2 : 0;
         const int quarter = warp & 3;
         const int m_row = quarter * LANES + (lane % LANES);         // MMA row held by this tensor-memory lane
-        const int copy = m_row / RPC, row = m_row % RPC;            // which copy of the rows, which query row of the group
+        const int copy = m_row / RPC, row = m_row % RPC + half * 128;       // which copy of the rows, which query row of the group
         const bool has_row = lane < LANES;
         const bool live_row = has_row && row < rows;
-        const bool live_warp = (quarter * LANES) % RPC < rows;      // some lane of this warp holds a query row
+        const bool live_warp = (quarter * LANES) % RPC + half * 128 < rows;     // some lane of this warp holds a query row
         const unsigned long long sees = live_row ? anc[(row0 + row) / p.G] : 0ull;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const int worker = quarter * 32 + lane;                     // of the set's 128 threads
@@ -301,43 +340,29 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         uint32_t ph = 0, ph_prev = 0;                               // parities of the "empty" phases that end those tiles
         int sb = set;                                               // S buffer of tile i (SETS < SBUFS)
         uint32_t ph_s = 0;
-        ring_advance(s, ph, set, kTrStages);
-        const uint32_t my_o = tmem_o + (uint32_t)(set * kHeadDim) + lane_base;   // this thread's O row
+        ring_advance(s, ph, set, STAGES);
+        const uint32_t my_o = tmem_o + (uint32_t)((set + half) * kHeadDim) + lane_base;   // this thread's O row
         for (int i = set; i < n_tiles && alive; i += SETS) {
-            alive = mbar_wait(bar_s_full(sb), ph_s, p.err, 61);
+            alive = mbar_wait(bar_s_full(half * SBUFS + sb), ph_s, p.err, 61);
             if (!alive) break;
             tc_fence_after();
             const int32_t *ids = tile_blk + s * kAtTileCols;
+            const bool all_seen = plain[s] != 0;                    // four full history blocks: nothing to mask
             // V rows that nobody may see: history positions from seq_len on, padding nodes.  Thread -> (block, key, half).
-            {
-                const int c = worker >> 5, key = (worker >> 1) & 15, half = worker & 1;
+            if (half == 0 && !all_seen) {
+                const int c = worker >> 5, key = (worker >> 1) & 15, dims = worker & 1;
                 const int blk = ids[c];
                 const int valid = blk < kTreeTag ? L - blk * kBlock : n_nodes - (blk - kTreeTag) * kBlock;
                 if (blk >= 0 && key >= valid) {
-                    uint8_t *dst = base_ptr + (size_t)s * kAtStageBytes + c * kEntryBytes + (key >> 3) * kImgGroup + half * kImgHalf +
+                    uint8_t *dst = kv_ptr + (size_t)s * kAtStageBytes + c * kEntryBytes + (key >> 3) * kImgGroup + dims * kImgHalf +
                                    kImgPart + (key & 7) * 128;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4 *>(dst + j * 16) = make_uint4(0, 0, 0, 0);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
             }
-            const uint32_t s_tmem = tmem_base + lane_base + (uint32_t)(sb * kAtTileKeys);
+            const uint32_t s_tmem = tmem_base + lane_base + (uint32_t)((half * SBUFS + sb) * kAtTileKeys);
             if (live_warp) {
-                uint32_t bits[BPC];                                 // visible keys of each of this copy's blocks
-                bool masked = false;
-#pragma unroll
-                for (int c = 0; c < BPC; ++c) {
-                    const int blk = ids[copy * BPC + c];
-                    uint32_t m = 0xffffu;                           // lanes without a query row need no masking
-                    if (live_row) {
-                        if (blk < 0) m = 0;
-                        else if (blk < kTreeTag) m = L - blk * kBlock < kBlock ? (1u << (L - blk * kBlock)) - 1u : 0xffffu;
-                        else m = (uint32_t)(sees >> ((blk - kTreeTag) * kBlock)) & 0xffffu;
-                    }
-                    bits[c] = m;
-                    masked |= m != 0xffffu;
-                }
-                masked = __any_sync(0xffffffffu, masked);
                 float x[BPC * kBlock];
                 {
                     uint32_t v[BPC][16];
@@ -349,12 +374,20 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
 #pragma unroll
                         for (int e = 0; e < 16; ++e) x[c * 16 + e] = __uint_as_float(v[c][e]);
                 }
-                if (masked) {
+                if (!all_seen) {
 #pragma unroll
-                    for (int c = 0; c < BPC; ++c)
+                    for (int c = 0; c < BPC; ++c) {                 // visible keys of each of this copy's blocks
+                        const int blk = ids[copy * BPC + c];
+                        uint32_t bits = 0xffffu;                    // lanes without a query row need no masking
+                        if (live_row) {
+                            if (blk < 0) bits = 0;
+                            else if (blk < kTreeTag) bits = L - blk * kBlock < kBlock ? (1u << (L - blk * kBlock)) - 1u : 0xffffu;
+                            else bits = (uint32_t)(sees >> ((blk - kTreeTag) * kBlock)) & 0xffffu;
+                        }
 #pragma unroll
                         for (int e = 0; e < 16; ++e)
-                            if (!((bits[c] >> e) & 1u)) x[c * 16 + e] = -CUDART_INF_F;
+                            if (!((bits >> e) & 1u)) x[c * 16 + e] = -CUDART_INF_F;
+                    }
                 }
                 alive = softmax_rest<COPIES>(x, s_tmem, my_o, copy, has_row, p.scale_log2, m_ref, l_sum, i >= SETS,
                                              // (the stage of this set's previous tile is released by the commit that follows
@@ -363,10 +396,10 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar_p_full(sb));
+            if (lane == 0) mbar_arrive(bar_p_full(half * SBUFS + sb));
             s_prev = s;
             ph_prev = ph;
-            ring_advance(s, ph, SETS, kTrStages);
+            ring_advance(s, ph, SETS, STAGES);
 #pragma unroll
             for (int k = 0; k < SETS; ++k) {
                 sb = (sb + 1 == SBUFS) ? 0 : sb + 1;
@@ -375,138 +408,84 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         }
         // ---- epilogue: merge the copies or sets, normalise, write out ----------------------------------------
         if (alive && n_tiles > 0)
-            alive = mbar_wait(bar_empty((n_tiles - 1) % kTrStages), ((n_tiles - 1) / kTrStages) & 1, p.err, 63);
+            alive = mbar_wait(bar_empty((n_tiles - 1) % STAGES), ((n_tiles - 1) / STAGES) & 1, p.err, 63);
         tc_fence_after();
-        // the K/V ring is idle now: stage the O rows there.  [128 MMA rows][132 floats], then max and sum.
-        float *o_sm = reinterpret_cast<float *>(base_ptr);
-        float *m_sm = o_sm + 128 * 132;
-        float *l_sm = m_sm + 128 * SETS;
-        const bool run = n_tiles > 0 && live_warp && alive;
-        // d0 .. d0 + 16 n of one row: acc * inv as bf16, or as a partial
-        auto place = [&](int r, long long &orow, float *&part) {
-            const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
-            orow = ((long long)b * p.T + tq) * p.Hq + a;
-            part = p.part_o + ((long long)blockIdx.x * p.group_rows + r) * kHeadDim;
-        };
-        if (SETS == 2) {
-            // the two threads of a row exchange maximum and sum; each then merges and writes one half of the output dims,
-            // reading both O accumulators at its own tensor-memory lane
-            m_sm[set * 128 + m_row] = m_ref;
-            l_sm[set * 128 + m_row] = l_sum;
-            asm volatile("bar.sync 1, 256;" ::: "memory");          // the eight softmax warps
-            const float m_o = m_sm[(set ^ 1) * 128 + m_row], l_o = l_sm[(set ^ 1) * 128 + m_row];
-            const float mx = fmaxf(m_ref, m_o);
-            const float w_me = mx == -CUDART_INF_F ? 0.f : fast_exp2(m_ref - mx), w_ot = mx == -CUDART_INF_F ? 0.f : fast_exp2(m_o - mx);
-            const float den = w_me * l_sum + w_ot * l_o;
-            const float inv = den > 0.f ? 1.f / den : 0.f;
-            const float lse2 = den > 0.f ? mx + log2f(den) : -CUDART_INF_F;
-            const float w_a = set == 0 ? w_me : w_ot, w_b = set == 0 ? w_ot : w_me;   // weights of the first and second accumulator
-            long long orow;
-            float *part;
-            place(row, orow, part);
-#pragma unroll 1
+        // The K/V ring is idle now.  Every accumulator row goes there with its maximum and sum (part = copy or set of the
+        // query row), then the warps write whole rows, four dims per lane: merged, normalised, coalesced.
+        constexpr int PARTS = COPIES * SETS, PITCH = kHeadDim + 4;
+        float *o_sm = reinterpret_cast<float *>(kv_ptr);            // [PARTS * RPC or 256][PITCH], then maxima and sums
+        float *m_sm = o_sm + 256 * PITCH;
+        float *l_sm = m_sm + 256;
+        const int mine = set * 128 + half * 128 + m_row;
+        if (n_tiles > 0 && live_warp && alive) {
+            float *dst = o_sm + mine * PITCH;
+#pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const int d0 = set * 64 + c * 16;
-                uint32_t va[16], vb[16];
-                if (run) {
-                    tc_ld16(tmem_o + lane_base + d0, va);
-                    tc_ld16(tmem_o + kHeadDim + lane_base + d0, vb);
-                }
-                if (!(live_row && alive)) continue;
-                float acc[16];
-                // an accumulator whose set saw no key (weight 0) may never have been written: its contents do not enter
+                uint32_t v[2][16];
+                tc_ld16_nowait(my_o + c * 32, v[0]);
+                tc_ld16_nowait(my_o + c * 32 + 16, v[1]);
+                tc_wait_ld();
+                if (has_row) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    acc[e] = ((w_a != 0.f ? w_a * __uint_as_float(va[e]) : 0.f) + (w_b != 0.f ? w_b * __uint_as_float(vb[e]) : 0.f)) * inv;
-                if (p.n_splits == 1) {
-                    uint4 *dst = reinterpret_cast<uint4 *>(p.out + (orow * kHeadDim + d0) * 2);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        dst[e] = make_uint4(pack_bf16x2(acc[8 * e], acc[8 * e + 1]), pack_bf16x2(acc[8 * e + 2], acc[8 * e + 3]),
-                                            pack_bf16x2(acc[8 * e + 4], acc[8 * e + 5]), pack_bf16x2(acc[8 * e + 6], acc[8 * e + 7]));
-                } else {
-                    float4 *dst = reinterpret_cast<float4 *>(part + d0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) dst[e] = make_float4(acc[4 * e], acc[4 * e + 1], acc[4 * e + 2], acc[4 * e + 3]);
+                    for (int e = 0; e < 8; ++e)
+                        reinterpret_cast<uint4 *>(dst + c * 32)[e] = make_uint4(v[e >> 2][(e & 3) * 4], v[e >> 2][(e & 3) * 4 + 1],
+                                                                                v[e >> 2][(e & 3) * 4 + 2], v[e >> 2][(e & 3) * 4 + 3]);
                 }
             }
-            if (live_row && alive && set == 0) {
-                if (p.n_splits == 1) { if (p.lse) p.lse[orow] = lse2 * kAtLn2; }
-                else p.part_lse[(long long)blockIdx.x * p.group_rows + row] = lse2;
-            }
-        } else {
-            // several copies: their O rows meet in shared memory; the MMA_M (row, slice of the output dims) tasks go to the
-            // first MMA_M softmax threads
-            if (run) {
+        }
+        if (has_row) {
+            m_sm[mine] = m_ref;
+            l_sm[mine] = l_sum;
+        }
+        alive = softmax_warps_all<THREADS - 96>(alive);
+        // one thread per row: the parts' weights, normalised, in place of their maxima; the row's place; its log-sum-exp
+        int32_t *row_sm = reinterpret_cast<int32_t *>(l_sm + 256);
+        {
+            const int r = tid - 96;
+            if (r < rows && alive) {
+                float mx = -CUDART_INF_F, den = 0.f, w[PARTS];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    uint32_t v[16];
-                    tc_ld16(tmem_o + lane_base + c * 16, v);
-                    float4 *dst = reinterpret_cast<float4 *>(o_sm + m_row * 132 + c * 16);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (has_row) dst[e] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]),
-                                             __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
-                }
-            }
-            if (has_row) {
-                m_sm[m_row] = m_ref;
-                l_sm[m_row] = l_sum;
-            }
-            asm volatile("bar.sync 1, 128;" ::: "memory");          // the four softmax warps
-            const int r = worker % RPC, dpart = worker / RPC;
-            constexpr int DLEN = kHeadDim / COPIES;
-            const int d0 = dpart * DLEN;
-            if (worker < MMA_M && r < rows && alive) {
-                float acc[DLEN], mw[COPIES], wt[COPIES];
-                float mx = -CUDART_INF_F, den = 0.f;
-#pragma unroll
-                for (int c = 0; c < COPIES; ++c) {
-                    mw[c] = m_sm[c * RPC + r];
-                    mx = fmaxf(mx, mw[c]);
+                for (int c = 0; c < PARTS; ++c) {
+                    w[c] = m_sm[c * RPC + r];
+                    mx = fmaxf(mx, w[c]);
                 }
 #pragma unroll
-                for (int c = 0; c < COPIES; ++c) {
-                    wt[c] = mx == -CUDART_INF_F ? 0.f : fast_exp2(mw[c] - mx);
-                    den += wt[c] * l_sm[c * RPC + r];
-                }
-#pragma unroll
-                for (int e = 0; e < DLEN; ++e) acc[e] = 0.f;
-                if (n_tiles > 0) {
-#pragma unroll
-                    for (int c = 0; c < COPIES; ++c) {
-                        if (wt[c] == 0.f) continue;                  // a copy that saw no key
-                        const float4 *src = reinterpret_cast<const float4 *>(o_sm + (c * RPC + r) * 132 + d0);
-#pragma unroll
-                        for (int e = 0; e < DLEN / 4; ++e) {
-                            const float4 f = src[e];
-                            acc[4 * e] += wt[c] * f.x; acc[4 * e + 1] += wt[c] * f.y;
-                            acc[4 * e + 2] += wt[c] * f.z; acc[4 * e + 3] += wt[c] * f.w;
-                        }
-                    }
+                for (int c = 0; c < PARTS; ++c) {
+                    w[c] = mx == -CUDART_INF_F ? 0.f : fast_exp2(w[c] - mx);
+                    den += w[c] * l_sm[c * RPC + r];
                 }
                 const float inv = den > 0.f ? 1.f / den : 0.f;
                 const float lse2 = den > 0.f ? mx + log2f(den) : -CUDART_INF_F;
-                long long orow;
-                float *part;
-                place(r, orow, part);
-                if (p.n_splits == 1) {
-                    uint4 *dst = reinterpret_cast<uint4 *>(p.out + (orow * kHeadDim + d0) * 2);
 #pragma unroll
-                    for (int e = 0; e < DLEN / 8; ++e)
-                        dst[e] = make_uint4(pack_bf16x2(acc[8 * e] * inv, acc[8 * e + 1] * inv),
-                                            pack_bf16x2(acc[8 * e + 2] * inv, acc[8 * e + 3] * inv),
-                                            pack_bf16x2(acc[8 * e + 4] * inv, acc[8 * e + 5] * inv),
-                                            pack_bf16x2(acc[8 * e + 6] * inv, acc[8 * e + 7] * inv));
-                    if (p.lse && dpart == 0) p.lse[orow] = lse2 * kAtLn2;
-                } else {
-                    float4 *dst = reinterpret_cast<float4 *>(part + d0);
-#pragma unroll
-                    for (int e = 0; e < DLEN / 4; ++e)
-                        dst[e] = make_float4(acc[4 * e] * inv, acc[4 * e + 1] * inv, acc[4 * e + 2] * inv, acc[4 * e + 3] * inv);
-                    if (dpart == 0) p.part_lse[(long long)blockIdx.x * p.group_rows + r] = lse2;
-                }
+                for (int c = 0; c < PARTS; ++c) m_sm[c * RPC + r] = w[c] * inv;
+                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+                const int orow = (b * p.T + tq) * p.Hq + a;
+                row_sm[r] = orow;
+                if (p.n_splits > 1) p.part_lse[(long long)blockIdx.x * p.group_rows + r] = lse2;
+                else if (p.lse) p.lse[orow] = lse2 * kAtLn2;
             }
+        }
+        softmax_warps_all<THREADS - 96>(true);
+        constexpr int WRITERS = (THREADS - 96) / 32;
+        const bool whole = p.n_splits == 1;
+        float *part_rows = p.part_o + (long long)blockIdx.x * p.group_rows * kHeadDim;
+#pragma unroll 4
+        for (int r = alive ? warp - 3 : rows; r < rows; r += WRITERS) {
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c) {
+                const float w = m_sm[c * RPC + r];
+                const float4 f = reinterpret_cast<const float4 *>(o_sm + (c * RPC + r) * PITCH)[lane];
+                // (a part that saw no key, weight 0, may never have been written: its contents do not enter)
+                acc.x = w != 0.f ? fmaf(w, f.x, acc.x) : acc.x;
+                acc.y = w != 0.f ? fmaf(w, f.y, acc.y) : acc.y;
+                acc.z = w != 0.f ? fmaf(w, f.z, acc.z) : acc.z;
+                acc.w = w != 0.f ? fmaf(w, f.w, acc.w) : acc.w;
+            }
+            if (whole)
+                reinterpret_cast<uint2 *>(p.out + (long long)row_sm[r] * kHeadDim * 2)[lane] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+            else
+                reinterpret_cast<float4 *>(part_rows + (long long)r * kHeadDim)[lane] = acc;
         }
     }
 
@@ -524,6 +503,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
 __global__ void __launch_bounds__(256)
 tree_combine_kernel(const TreeAttnParams p, int total)
 {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int wi = 8 * blockIdx.x + (threadIdx.x >> 5);
@@ -579,9 +559,9 @@ struct TreePlan {
 static TreePlan tree_plan(const oasis_dims_t *dims, int T, int n_cols)
 {
     TreePlan pl;
-    const int R = T * (dims->n_q_heads / dims->n_kv_heads);
-    pl.n_groups = (R + 127) / 128;
-    pl.group_rows = (R + pl.n_groups - 1) / pl.n_groups;
+    const int G = dims->n_q_heads / dims->n_kv_heads, most_tokens = 256 / G;
+    pl.n_groups = (T + most_tokens - 1) / most_tokens;
+    pl.group_rows = (T + pl.n_groups - 1) / pl.n_groups * G;         // whole nodes, as evenly as they go
     // all thread blocks resident at once (one per SM) as far as the column list can be split, eight columns per split
     const long long items = (long long)dims->batch * dims->n_kv_heads * pl.n_groups;
     long long s = items > 0 ? sm_count() / items : 1;
@@ -643,7 +623,7 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
     if (!encode) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available", who);
 
     // The pool as attn_tc.cu sees it: one box = one 8 KiB entry, landing as [group][half][K, V][8 rows][128 B].
-    CUtensorMap pool_map, tree_map;
+    CUtensorMap pool_map, tree_map, q_map;
     const cuuint64_t pool_parts = (kBoundsCheck && bounds().n_slots < (1ll << 30)) ? (cuuint64_t)(2 * bounds().n_slots) : (cuuint64_t)1 << 31;
     const cuuint64_t pdim[5] = {64, 8, pool_parts, 2, 2}, pstride[4] = {256, 4096, 128, 2048};
     const cuuint32_t pbox[5] = {64, 8, 2, 2, 2}, estr[5] = {1, 1, 1, 1, 1};
@@ -661,6 +641,15 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (cr != CUDA_SUCCESS) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed (%d)", who, (int)cr);
+    // The queries [B * T][Hkv][G][2 x 64 dims], innermost first: 64 elements | head of the group | KV head | token | dim half.
+    // One box = the query rows of one row group, one dim half, 128 bytes per row in the order (token, head of the group).
+    const cuuint64_t G64 = (cuuint64_t)(dims->n_q_heads / dims->n_kv_heads), Hq64 = (cuuint64_t)dims->n_q_heads;
+    const cuuint64_t qdim[5] = {64, G64, Hkv, (cuuint64_t)dims->batch * T64, 2}, qstride[4] = {256, G64 * 256, Hq64 * 256, 128};
+    const cuuint32_t qbox[5] = {64, (cuuint32_t)G64, 1, (cuuint32_t)(pl.group_rows / (int)G64), 1};
+    cr = encode(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(q), qdim, qstride, qbox, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (cr != CUDA_SUCCESS) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed (%d)", who, (int)cr);
 
     TreeAttnParams p = {};
     p.q = (const uint8_t *)q; p.slot_tbl = slot_tbl; p.blk_tbl = blk_tbl; p.seq_len = seq_len; p.parent = parent;
@@ -675,31 +664,38 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
     }
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
-#define OASIS_TREE_LAUNCH(M, C)                                                                                               \
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)pl.items);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+#define OASIS_TREE_LAUNCH(M, C, P)                                                                                            \
     do {                                                                                                                      \
-        e = cudaFuncSetAttribute(tree_attn_tc_kernel<M, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTrSmem);        \
-        if (e == cudaSuccess) prefer_max_shared_carveout(tree_attn_tc_kernel<M, C>);                                          \
-        if (e == cudaSuccess) tree_attn_tc_kernel<M, C><<<(unsigned)pl.items, tr_threads(M, C), kTrSmem, st>>>(pool_map, tree_map, p); \
+        cfg.blockDim = dim3(tr_threads(M, C, P));                                                                             \
+        cfg.dynamicSmemBytes = tr_smem(M, P);                                                                                 \
+        e = allow_dynamic_shared(reinterpret_cast<const void *>(tree_attn_tc_kernel<M, C, P>), tr_smem(M, P));                 \
+        if (e == cudaSuccess) prefer_max_shared_carveout(tree_attn_tc_kernel<M, C, P>);                                       \
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, tree_attn_tc_kernel<M, C, P>, pool_map, tree_map, q_map, p);       \
     } while (0)
-    if (pl.group_rows <= 16) OASIS_TREE_LAUNCH(64, 4);          // four copies of <= 16 rows, one block of a tile each
-    else if (pl.group_rows <= 32) OASIS_TREE_LAUNCH(64, 2);     // two copies of <= 32 rows, two blocks each
-    else if (pl.group_rows <= 64) OASIS_TREE_LAUNCH(128, 2);    // two copies of <= 64 rows: half the softmax work per thread
-    else OASIS_TREE_LAUNCH(128, 1);                             // two softmax warp sets, alternate tiles
+    if (pl.group_rows <= 16) OASIS_TREE_LAUNCH(64, 4, false);       // four copies of <= 16 rows, one block of a tile each
+    else if (pl.group_rows <= 32) OASIS_TREE_LAUNCH(64, 2, false);  // two copies of <= 32 rows, two blocks each
+    else if (pl.group_rows <= 64) OASIS_TREE_LAUNCH(128, 2, false); // two copies of <= 64 rows: half the softmax work per thread
+    else if (pl.group_rows <= 128) OASIS_TREE_LAUNCH(128, 1, false);   // two softmax warp sets, alternate tiles
+    else OASIS_TREE_LAUNCH(128, 1, true);                           // two softmax warp sets, 128 rows each
 #undef OASIS_TREE_LAUNCH
-    if (e != cudaSuccess) return fail(OASIS_ERR_CUDA, "%s: shared memory %zu B: %s", who, kTrSmem, cudaGetErrorString(e));
-    if (int rc = check_launch(who)) return rc;
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return fail(OASIS_ERR_CUDA, "%s: launch: %s", who, cudaGetErrorString(e));
+    }
     if (pl.n_splits > 1) {
-        // programmatic stream serialization: the merge's thread blocks become resident while the attention still runs
+        // (the merge's thread blocks become resident while the attention still runs and wait there for the partials)
         const int total = dims->batch * p.Hkv * p.R;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)((total + 7) / 8));
         cfg.blockDim = dim3(256);
-        cfg.stream = st;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
+        cfg.dynamicSmemBytes = 0;
         prefer_max_shared_carveout(tree_combine_kernel);
         e = cudaLaunchKernelEx(&cfg, tree_combine_kernel, p, total);
         if (e != cudaSuccess) return fail(OASIS_ERR_CUDA, "%s: combine launch: %s", who, cudaGetErrorString(e));

@@ -778,9 +778,7 @@ static cudaError_t launch_verify(const VerifyParams &p, int batch, cudaStream_t 
     constexpr int most = (int)((size_t)100 * 1024 / (kVerWarps * 24)) / 32 * 32;   // two thread blocks per SM
     if (cap > most) cap = most;
     const size_t smem = (size_t)kVerWarps * cap * 24;
-    cudaError_t e = cudaSuccess;
-    if (smem > 46 * 1024) e = cudaFuncSetAttribute(verify_tree_kernel<LT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+    if (cudaError_t e = allow_dynamic_shared(reinterpret_cast<const void *>(verify_tree_kernel<LT>), (int)smem)) return e;
     prefer_max_shared_carveout(verify_tree_kernel<LT>);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
