@@ -19,8 +19,6 @@
 
 namespace oasis {
 
-constexpr int kVerThreads = 256;
-constexpr int kVerWarps = kVerThreads / 32;
 constexpr int kVerMaxCluster = 8;
 // The fp32 sum of exponentials is off by less than 2e-3 of itself: m c2 is rounded (2^-12, a common factor), a term of
 // weight 2^-x has a relative error below (1.5 x + 4) 2^-23, and a lane adds at most 2^22 / 512 / 4 = 2048 pairs to an
@@ -287,16 +285,16 @@ __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row
 // visited node, whatever happens there; a larger one is read again for every pass.
 // Between the passes warp 0 alone talks to the other thread blocks of the cluster and decides; that every warp did it cost
 // more than the passes (four warps per scheduler running the same 200 serial instructions).
-template <typename LT>
-__global__ void __launch_bounds__(kVerThreads, 2)
+template <typename LT, int THREADS>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS)
 verify_tree_kernel(const VerifyParams p, const int C, const int cap)
 {
-    constexpr int N = Logit<LT>::N;
+    constexpr int N = Logit<LT>::N, WARPS = THREADS / 32;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ Pair s_x[2][kVerMaxCluster];            // what the thread blocks of the cluster tell one another
     __shared__ __align__(8) uint64_t s_bar[2];
-    __shared__ Pair s_w[kVerWarps];
-    __shared__ double s_mass[kVerWarps];
+    __shared__ Pair s_w[WARPS];
+    __shared__ double s_mass[WARPS];
     __shared__ __align__(16) double s_table[kExpTable];
     __shared__ int s_tok[OASIS_MAX_TREE], s_par[OASIS_MAX_TREE];
     __shared__ float s_u[OASIS_MAX_TREE];
@@ -304,11 +302,11 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
     __shared__ Control ctl;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint4 *const my_row = reinterpret_cast<uint4 *>(smem_raw) + warp * cap + lane;              // this lane's vectors, 32 apart
-    double *const my_sum = reinterpret_cast<double *>(smem_raw + (size_t)kVerWarps * cap * 16) + warp * cap + lane;   // their masses
+    double *const my_sum = reinterpret_cast<double *>(smem_raw + (size_t)WARPS * cap * 16) + warp * cap + lane;   // their masses
     const uint32_t rank = C > 1 ? cluster_rank() : 0u;
     const int b = blockIdx.x / C;
     const LT *const logits = reinterpret_cast<const LT *>(p.logits) + (long long)b * p.lb;
-    const int parts_of_row = C * kVerWarps, part = (int)rank * kVerWarps + warp;
+    const int parts_of_row = C * WARPS, part = (int)rank * WARPS + warp;
     // this warp's vectors of node x's row, and their way into shared memory
     Row<LT> row(logits, p.V);
     int v0 = 0, v1 = 0, n_chunks = 1;
@@ -334,14 +332,14 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
     if (n == 0) {                                      // the whole cluster leaves: nothing is exchanged
         stage_wait();
         if (rank == 0) {
-            for (int i = tid; i < p.M; i += kVerThreads) p.path[(long long)b * p.M + i] = -1;
+            for (int i = tid; i < p.M; i += THREADS) p.path[(long long)b * p.M + i] = -1;
             if (tid == 0) { p.n_commit[b] = 0; p.next_token[b] = -1; }
         }
         return;
     }
     const bool sampled = temp > 0.f;
     if (sampled) {
-        for (int i = 2 * tid; i < kExpTable; i += 2 * kVerThreads)
+        for (int i = 2 * tid; i < kExpTable; i += 2 * THREADS)
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(s_table + i)), "l"(g_exp_table.v + i) : "memory");
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
@@ -487,25 +485,25 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                 uint64_t x0, x1 = 0;
                 float m = 0.f, s = 0.f;
                 if (!first) {
-                    double all = s_mass[lane & (kVerWarps - 1)];
+                    double all = s_mass[lane & (WARPS - 1)];
 #pragma unroll
-                    for (int o = kVerWarps / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+                    for (int o = WARPS / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
                     x0 = (uint64_t)__double_as_longlong(all);
                 } else {
-                    const Pair mine = s_w[lane & (kVerWarps - 1)];
+                    const Pair mine = s_w[lane & (WARPS - 1)];
                     x0 = mine.a;
                     if (!sampled) {
 #pragma unroll
-                        for (int o = kVerWarps / 2; o > 0; o >>= 1) x0 = max((unsigned long long)x0, __shfl_xor_sync(0xffffffffu, (unsigned long long)x0, o));
+                        for (int o = WARPS / 2; o > 0; o >>= 1) x0 = max((unsigned long long)x0, __shfl_xor_sync(0xffffffffu, (unsigned long long)x0, o));
                     } else {
                         m = __uint_as_float((uint32_t)mine.a);
                         s = __uint_as_float((uint32_t)mine.b);
                         float top = m;
 #pragma unroll
-                        for (int o = kVerWarps / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        for (int o = WARPS / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                         s = m == top ? s : s * fast_exp2((m - top) * c2);
 #pragma unroll
-                        for (int o = kVerWarps / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                        for (int o = WARPS / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                         x0 = __float_as_uint(top);
                         x1 = __float_as_uint(s);
                     }
@@ -524,13 +522,16 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                     __syncwarp();
                 }
                 ++turn;
-                const Pair theirs = got[lane & (C - 1)];           // (C is a power of two)
+                const bool from = lane < C;                       // lane r holds what block r told, the others nothing
+                const Pair theirs = got[from ? lane : 0];
                 int cmd = kMass, child = -1;
                 if (!alive) {
                     cmd = kEnd;
                 } else if (!sampled) {
-                    unsigned long long best = theirs.a;
-                    for (int o = C / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+                    unsigned long long best = from ? theirs.a : 0;
+#pragma unroll
+                    for (int o = kVerMaxCluster / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+                    best = __shfl_sync(0xffffffffu, best, 0);
                     next = best == 0 ? -1 : (int)(0xffffffffu - (uint32_t)best);  // 0: every token is left out
                     const unsigned e0 = __ballot_sync(0xffffffffu, ((kids0 >> lane) & 1u) && s_tok[lane] == next);
                     const unsigned e1 = __ballot_sync(0xffffffffu, ((kids1 >> lane) & 1u) && s_tok[lane + 32] == next);
@@ -544,12 +545,16 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                     int need = ctl.need;
                     enum { kNothing, kExact, kRest, kFinal };
                     if (first) {
-                        m = __uint_as_float((uint32_t)theirs.a);
-                        s = __uint_as_float((uint32_t)theirs.b);
+                        m = from ? __uint_as_float((uint32_t)theirs.a) : -CUDART_INF_F;
+                        s = from ? __uint_as_float((uint32_t)theirs.b) : 0.f;
                         float top = m;
-                        for (int o = C / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll
+                        for (int o = kVerMaxCluster / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                         s = m == top ? s : s * fast_exp2((m - top) * c2);
-                        for (int o = C / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+#pragma unroll
+                        for (int o = kVerMaxCluster / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                        top = __shfl_sync(0xffffffffu, top, 0);
+                        s = __shfl_sync(0xffffffffu, s, 0);
                         // tokens with a logit of +infinity share everything: such a row reads as 0 at them and -infinity elsewhere
                         const bool infinite = top == CUDART_INF_F;
                         if (infinite) {
@@ -635,7 +640,7 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                         int in_warp = -1;
                         if (owner == (int)rank) {
                             last = 0;
-                            for (int k = 0; k < kVerWarps && in_warp < 0; ++k) {
+                            for (int k = 0; k < WARPS && in_warp < 0; ++k) {
                                 if (s_mass[k] > 0.0) last = k;
                                 if (!take_last && target < before + s_mass[k]) in_warp = k;
                                 else before += s_mass[k];
@@ -765,21 +770,18 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
     }
 }
 
-template <typename LT>
-static cudaError_t launch_verify(const VerifyParams &p, int batch, cudaStream_t st)
+template <typename LT, int THREADS>
+static cudaError_t launch_verify_as(const VerifyParams &p, int batch, int C, cudaStream_t st)
 {
-    // As many thread blocks per request as there are places for at two per SM (clusters of eight do not fit everywhere, so
-    // one place per SM is counted on for them), at least 2,048 tokens for each block.
-    int C = kVerMaxCluster;
-    while (C > 1 && ((long long)batch * C > (C == 8 ? 1 : 2) * sm_count() || p.V < C * 2048)) C >>= 1;
+    constexpr int WARPS = THREADS / 32;
     const int vecs = (p.V + 2 * (Logit<LT>::N - 1)) / Logit<LT>::N;               // of an unaligned row
-    const int per_warp = (vecs + C * kVerWarps - 1) / (C * kVerWarps);
+    const int per_warp = (vecs + C * WARPS - 1) / (C * WARPS);
     int cap = (per_warp + 31) / 32 * 32;
-    constexpr int most = (int)((size_t)100 * 1024 / (kVerWarps * 24)) / 32 * 32;   // two thread blocks per SM
+    constexpr int most = (int)((size_t)(THREADS == 512 ? 208 : 100) * 1024 / (WARPS * 24)) / 32 * 32;   // one or two thread blocks per SM
     if (cap > most) cap = most;
-    const size_t smem = (size_t)kVerWarps * cap * 24;
-    if (cudaError_t e = allow_dynamic_shared(reinterpret_cast<const void *>(verify_tree_kernel<LT>), (int)smem)) return e;
-    prefer_max_shared_carveout(verify_tree_kernel<LT>);
+    const size_t smem = (size_t)WARPS * cap * 24;
+    if (cudaError_t e = allow_dynamic_shared(reinterpret_cast<const void *>(verify_tree_kernel<LT, THREADS>), (int)smem)) return e;
+    prefer_max_shared_carveout(verify_tree_kernel<LT, THREADS>);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)C;
@@ -787,12 +789,65 @@ static cudaError_t launch_verify(const VerifyParams &p, int batch, cudaStream_t 
     attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(batch * C));
-    cfg.blockDim = dim3(kVerThreads);
+    cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, verify_tree_kernel<LT>, p, C, cap);
+    return cudaLaunchKernelEx(&cfg, verify_tree_kernel<LT, THREADS>, p, C, cap);
+}
+
+// Clusters of `size` thread blocks that run at the same time with one block per SM (a cluster stays within one of the GPU's
+// processing clusters, whose SM counts need not be a multiple of its size).  Asked once per device and size.
+static int clusters_at_once(int size)
+{
+    constexpr int kDevices = 64;
+    static std::mutex lock;
+    static int known[kDevices][kVerMaxCluster + 1] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) {
+        cudaGetLastError();
+        return sm_count() / (size + 1);
+    }
+    std::lock_guard<std::mutex> guard(lock);
+    if (known[dev][size] == 0) {
+        const auto kernel = verify_tree_kernel<float, 512>;
+        const int smem = 200 * 1024;                           // one block per SM
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)size;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(size * 1024));
+        cfg.blockDim = dim3(512);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (allow_dynamic_shared(reinterpret_cast<const void *>(kernel), smem) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
+            cudaGetLastError();
+            n = sm_count() / (size + 1);
+        }
+        known[dev][size] = n < 1 ? 1 : n;
+    }
+    return known[dev][size];
+}
+
+// The thread blocks of a request: as many as let all requests run at once, at most eight, with 2,048 tokens or more each.
+// Where all requests' clusters fit with one block per SM, blocks have 512 threads, else 256 with two blocks per SM.
+// (One request, 64-node tree, 151,936 tokens: 512 threads 21 us, 256 threads 28 us.  16 requests, whose clusters of eight do
+// not all fit alone: 8 blocks of 256 threads 29 us, 8 of 512 threads 33 us, 7 of 512 threads 30 us.  128 requests, 50,257
+// tokens: 2 blocks of 256 threads 31 us, 1 of 512 threads 43 us.)
+template <typename LT>
+static cudaError_t launch_verify(const VerifyParams &p, int batch, cudaStream_t st)
+{
+    int C = kVerMaxCluster;
+    while (C > 1 && p.V < C * 2048) C >>= 1;
+    if (batch <= clusters_at_once(C)) return launch_verify_as<LT, 512>(p, batch, C, st);
+    while (C > 1 && (long long)batch * C > 2ll * sm_count()) C >>= 1;
+    return launch_verify_as<LT, 256>(p, batch, C, st);
 }
 
 }  // namespace oasis
