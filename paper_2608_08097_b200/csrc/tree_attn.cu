@@ -438,54 +438,62 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
             l_sm[mine] = l_sum;
         }
         alive = softmax_warps_all<THREADS - 96>(alive);
-        // one thread per row: the parts' weights, normalised, in place of their maxima; the row's place; its log-sum-exp
-        int32_t *row_sm = reinterpret_cast<int32_t *>(l_sm + 256);
-        {
-            const int r = tid - 96;
-            if (r < rows && alive) {
-                float mx = -CUDART_INF_F, den = 0.f, w[PARTS];
-#pragma unroll
-                for (int c = 0; c < PARTS; ++c) {
-                    w[c] = m_sm[c * RPC + r];
-                    mx = fmaxf(mx, w[c]);
-                }
-#pragma unroll
-                for (int c = 0; c < PARTS; ++c) {
-                    w[c] = mx == -CUDART_INF_F ? 0.f : fast_exp2(w[c] - mx);
-                    den += w[c] * l_sm[c * RPC + r];
-                }
-                const float inv = den > 0.f ? 1.f / den : 0.f;
-                const float lse2 = den > 0.f ? mx + log2f(den) : -CUDART_INF_F;
-#pragma unroll
-                for (int c = 0; c < PARTS; ++c) m_sm[c * RPC + r] = w[c] * inv;
-                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
-                const int orow = (b * p.T + tq) * p.Hq + a;
-                row_sm[r] = orow;
-                if (p.n_splits > 1) p.part_lse[(long long)blockIdx.x * p.group_rows + r] = lse2;
-                else if (p.lse) p.lse[orow] = lse2 * kAtLn2;
-            }
-        }
-        softmax_warps_all<THREADS - 96>(true);
+        // A warp writes rows r0, r0 + WRITERS, ..: lane k works out row k's weights (the parts', normalised), place and
+        // log-sum-exp, then the half-warps copy two rows at a time.
         constexpr int WRITERS = (THREADS - 96) / 32;
-        const bool whole = p.n_splits == 1;
-        float *part_rows = p.part_o + (long long)blockIdx.x * p.group_rows * kHeadDim;
-#pragma unroll 4
-        for (int r = alive ? warp - 3 : rows; r < rows; r += WRITERS) {
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int r0 = warp - 3, n_mine = alive && rows > r0 ? (rows - r0 + WRITERS - 1) / WRITERS : 0;    // at most 32
+        float w[PARTS];
+        int orow = 0;
+        if (lane < n_mine) {
+            const int r = r0 + lane * WRITERS;
+            float mx = -CUDART_INF_F, den = 0.f;
 #pragma unroll
             for (int c = 0; c < PARTS; ++c) {
-                const float w = m_sm[c * RPC + r];
-                const float4 f = reinterpret_cast<const float4 *>(o_sm + (c * RPC + r) * PITCH)[lane];
-                // (a part that saw no key, weight 0, may never have been written: its contents do not enter)
-                acc.x = w != 0.f ? fmaf(w, f.x, acc.x) : acc.x;
-                acc.y = w != 0.f ? fmaf(w, f.y, acc.y) : acc.y;
-                acc.z = w != 0.f ? fmaf(w, f.z, acc.z) : acc.z;
-                acc.w = w != 0.f ? fmaf(w, f.w, acc.w) : acc.w;
+                w[c] = m_sm[c * RPC + r];
+                mx = fmaxf(mx, w[c]);
             }
-            if (whole)
-                reinterpret_cast<uint2 *>(p.out + (long long)row_sm[r] * kHeadDim * 2)[lane] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-            else
-                reinterpret_cast<float4 *>(part_rows + (long long)r * kHeadDim)[lane] = acc;
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c) {
+                w[c] = mx == -CUDART_INF_F ? 0.f : fast_exp2(w[c] - mx);
+                den += w[c] * l_sm[c * RPC + r];
+            }
+            const float inv = den > 0.f ? 1.f / den : 0.f;
+            const float lse2 = den > 0.f ? mx + log2f(den) : -CUDART_INF_F;
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c) w[c] *= inv;
+            const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+            orow = p.n_splits == 1 ? (b * p.T + tq) * p.Hq + a : blockIdx.x * p.group_rows + r;
+            if (p.n_splits > 1) p.part_lse[orow] = lse2;
+            else if (p.lse) p.lse[orow] = lse2 * kAtLn2;
+        }
+        const int side = lane >> 4, col = (lane & 15) * 4;          // four dims in either half of the row
+#pragma unroll 4
+        for (int k0 = 0; k0 < n_mine; k0 += 2) {
+            const int k = min(k0 + side, n_mine - 1), r = r0 + k * WRITERS;          // (an odd last row is written twice)
+            const long long o = __shfl_sync(0xffffffffu, orow, k);
+            float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c) {
+                const float wc = __shfl_sync(0xffffffffu, w[c], k);
+                const float *src = o_sm + (c * RPC + r) * PITCH + col;
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                    const float4 f = *reinterpret_cast<const float4 *>(src + 64 * d);
+                    // (a part that saw no key, weight 0, may never have been written: its contents do not enter)
+                    acc[d].x = wc != 0.f ? fmaf(wc, f.x, acc[d].x) : acc[d].x;
+                    acc[d].y = wc != 0.f ? fmaf(wc, f.y, acc[d].y) : acc[d].y;
+                    acc[d].z = wc != 0.f ? fmaf(wc, f.z, acc[d].z) : acc[d].z;
+                    acc[d].w = wc != 0.f ? fmaf(wc, f.w, acc[d].w) : acc[d].w;
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                if (p.n_splits == 1)
+                    *reinterpret_cast<uint2 *>(p.out + (o * kHeadDim + col + 64 * d) * 2) =
+                        make_uint2(pack_bf16x2(acc[d].x, acc[d].y), pack_bf16x2(acc[d].z, acc[d].w));
+                else
+                    *reinterpret_cast<float4 *>(p.part_o + o * kHeadDim + col + 64 * d) = acc[d];
+            }
         }
     }
 
@@ -605,12 +613,12 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
     using namespace oasis;
     const char *who = "oasis_tree_attn";
     if (int rc = check_tree(dims, n_tree, n_cols, who)) return rc;
+    if (!(scale > 0.f) || scale > 3.0e38f) return fail(OASIS_ERR_INVALID_ARG, "%s: scale %g", who, (double)scale);
+    if (dims->batch == 0) return OASIS_OK;
     if (!q || !tree_kv || !parent || !n_nodes || !hbm_pool || !slot_tbl || !blk_tbl || !seq_len || !out)
         return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
     if (!aligned16(q) || !aligned16(tree_kv) || !aligned16(hbm_pool) || !aligned16(out))
         return fail(OASIS_ERR_INVALID_ARG, "%s: q, tree_kv, hbm_pool and out must be 16-byte aligned", who);
-    if (!(scale > 0.f) || scale > 3.0e38f) return fail(OASIS_ERR_INVALID_ARG, "%s: scale %g", who, (double)scale);
-    if (dims->batch == 0) return OASIS_OK;
     const TreePlan pl = tree_plan(dims, n_tree, n_cols);
     if (pl.workspace > 0) {
         if (!workspace || workspace_bytes < pl.workspace)
@@ -618,7 +626,7 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
                         workspace ? workspace_bytes : (size_t)0);
         if (!aligned16(workspace)) return fail(OASIS_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
     }
-    if (pl.items > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: grid too large", who);
+    if (pl.items * pl.group_rows > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: grid too large", who);
     EncodeTiledFn encode = encode_tiled_fn();
     if (!encode) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available", who);
 

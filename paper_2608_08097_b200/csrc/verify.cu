@@ -867,6 +867,7 @@ extern "C" int oasis_verify_tree(int32_t batch, int32_t n_tree, int32_t vocab, c
         return fail(OASIS_ERR_INVALID_ARG, "%s: vocab %d outside [1, %d]", who, vocab, OASIS_MAX_VOCAB);
     if (max_path < 1 || max_path > n_tree)
         return fail(OASIS_ERR_INVALID_ARG, "%s: max_path %d outside [1, n_tree]", who, max_path);
+    if (batch == 0) return OASIS_OK;
     if (!logits || !tokens || !parent || !n_nodes || !uniforms || !temperature || !path || !n_commit || !next_token)
         return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
     if (logits_type != OASIS_F32 && logits_type != OASIS_BF16 && logits_type != OASIS_F16)
@@ -877,7 +878,6 @@ extern "C" int oasis_verify_tree(int32_t batch, int32_t n_tree, int32_t vocab, c
     if (logits_row_stride < vocab || logits_batch_stride < 0 || (draft_probs && (draft_row_stride < vocab || draft_batch_stride < 0)))
         return fail(OASIS_ERR_INVALID_ARG, "%s: row strides %lld, %lld of %d logits", who, (long long)logits_row_stride,
                     (long long)draft_row_stride, vocab);
-    if (batch == 0) return OASIS_OK;
     VerifyParams p;
     p.logits = logits; p.tokens = tokens; p.parent = parent; p.n_nodes = n_nodes; p.uniforms = uniforms;
     p.temperature = temperature; p.draft = draft_probs; p.path = path; p.n_commit = n_commit; p.next_token = next_token;

@@ -392,6 +392,14 @@ def test_verification_in_a_graph_and_on_a_stream(L):
     assert all(np.array_equal(w.cpu().numpy(), r) for w, r in zip(want, ref))
 
 
+@pytest.mark.parametrize("draft", [False, True], ids=["fixed", "drawn"])
+def test_rows_larger_than_shared_memory(L, draft):
+    """300 requests leave one thread block for each: its part of 70,001 tokens is read again for every pass."""
+    rng = np.random.default_rng(19 + draft)
+    logits, q, parent, tokens, u = make_verify(rng, 300, 3, 70001, torch.bfloat16, draft)
+    verify(L, logits, tokens, parent, [3] * 300, u, rng.choice([0.0, 0.7, 1.0], 300), 3, q)
+
+
 # ---- commit --------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("layers,B,Hkv,T,M,host", [(1, 1, 8, 1, 1, "device"), (1, 2, 1, 5, 5, "none"), (3, 5, 4, 64, 16, "pinned"),
                                                    (64, 2, 2, 7, 3, "device"), (2, 33, 3, 16, 11, "some")])
@@ -468,6 +476,29 @@ def test_wrong_tensors_are_refused(L):
             L.verify_tree(**{**good, name: bad})
     with pytest.raises(TypeError):
         L.verify_tree(**good, draft_probs=x.half())
+
+
+def test_empty_batches_do_nothing(L):
+    e = lambda *shape, dt=torch.int32: torch.zeros(shape, dtype=dt, device="cuda")  # noqa: E731
+    bf = torch.bfloat16
+    L.tree_attn(L.Dims(0, 8, 2, 4), e(0, 3, 8, 128, dt=bf), e(0, 3, 2, 2, 128, dt=bf), e(0, 3), e(0), e(1, 2, 16, 128, dt=bf), e(0, 2, 4), e(0, 2, 4),
+                e(0), SCALE, e(0, 3, 8, 128, dt=bf))
+    L.verify_tree(e(0, 3, 9, dt=torch.float32), e(0, 3), e(0, 3), e(0), e(0, 3, dt=torch.float32), e(0, dt=torch.float32), e(0, 2), e(0), e(0))
+    L.commit_kv(L.Dims(0, 8, 2, 4), e(0, 3, 2, 2, 128, dt=bf), e(0, 3), e(0), e(0), e(0, 4), e(0, 2, 4), e(0, 2, 4), 2, e(1, 2, 16, 128, dt=bf))
+
+
+def test_bounds_check_build(L):
+    """In a process of its own, because a process loads one build of the library."""
+    import json
+    import os
+    import subprocess
+    import sys
+    from paper_2608_08097_b200 import build
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "tests", "tree_checked_worker.py")], capture_output=True, text=True, timeout=600,
+                       env=dict(os.environ, OASIS_LIB=build.build(checked=True)))
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
+    assert json.loads(r.stdout.strip().splitlines()[-1])["ok"]
 
 
 # ---- together ------------------------------------------------------------------------------------------------------
