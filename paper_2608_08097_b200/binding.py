@@ -419,6 +419,7 @@ _LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (torch.cuda.current_stream() takes 3 us)
+_device = torch.cuda.current_device
 
 
 def _cdims(dims):
@@ -449,7 +450,7 @@ def _pool_ptr(t, dtype, name, device, host_ok=False):
     """Address of a pool of entries [..][2][16][128] in device memory (or, `host_ok`, pinned host memory)."""
     if t.dtype != dtype:
         raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
-    if t.shape[-3:] != (2, 16, 128) or not t.is_contiguous():
+    if t.shape[-3:] != (2, 16, 128) or not t.is_contiguous():        # (entries in any number of leading dimensions)
         raise ValueError("%s must be a contiguous pool of [2][16][128] entries" % name)
     if t.get_device() != device and not (host_ok and not t.is_cuda and t.is_pinned()):
         raise ValueError("%s must be on the current CUDA device%s" % (name, " or in pinned host memory" if host_ok else ""))
@@ -473,21 +474,21 @@ def tree_attn(dims, q, tree_kv, parent, n_nodes, hbm_pool, slot_tbl, blk_tbl, se
     below seq_len[b] in the columns of blk_tbl), its ancestors and itself.  q, out [B][T][Hq][128]; tree_kv
     [B][T][Hkv][2][128]; parent [B][T], n_nodes [B] int32; rows of padding nodes are left as they were.
     `workspace`: tree_attn_workspace_bytes() bytes where that is not zero."""
-    B, T, Hq, Hkv = dims.batch, q.shape[1], dims.n_q_heads, dims.n_kv_heads
-    n_cols = blk_tbl.shape[-1]
-    dev = torch.cuda.current_device()
-    bf, i32 = torch.bfloat16, torch.int32
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    B, Hq, Hkv = dims.batch, dims.n_q_heads, dims.n_kv_heads
+    T, n_cols = q.shape[1], blk_tbl.shape[-1]
+    dev, bf, i32 = _device(), torch.bfloat16, torch.int32
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("workspace must be contiguous and on the current CUDA device")
-    _check(lib().oasis_tree_attn(
-        _cdims(dims), _dev(q, bf, (B, T, Hq, 128), "q", dev), T, _dev(tree_kv, bf, (B, T, Hkv, 2, 128), "tree_kv", dev),
-        _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, (B,), "n_nodes", dev),
-        _pool_ptr(hbm_pool, bf, "hbm_pool", dev), _dev(slot_tbl, i32, (B, Hkv, n_cols), "slot_tbl", dev),
-        _dev(blk_tbl, i32, (B, Hkv, n_cols), "blk_tbl", dev), n_cols, _dev(seq_len, i32, (B,), "seq_len", dev), scale,
-        _dev(out, bf, (B, T, Hq, 128), "out", dev),
-        None if lse is None else _dev(lse, torch.float32, (B, T, Hq), "lse", dev),
-        None if workspace is None else workspace.data_ptr(), ws_bytes, _stream_id(stream, dev)), "oasis_tree_attn")
+    rows, table, per_request = (B, T, Hq, 128), (B, Hkv, n_cols), (B,)
+    rc = lib().oasis_tree_attn(
+        _cdims(dims), _dev(q, bf, rows, "q", dev), T, _dev(tree_kv, bf, (B, T, Hkv, 2, 128), "tree_kv", dev),
+        _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, per_request, "n_nodes", dev),
+        _pool_ptr(hbm_pool, bf, "hbm_pool", dev), _dev(slot_tbl, i32, table, "slot_tbl", dev),
+        _dev(blk_tbl, i32, table, "blk_tbl", dev), n_cols, _dev(seq_len, i32, per_request, "seq_len", dev), scale,
+        _dev(out, bf, rows, "out", dev), None if lse is None else _dev(lse, torch.float32, (B, T, Hq), "lse", dev),
+        None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream_id(stream, dev))
+    if rc:
+        _check(rc, "oasis_tree_attn")
 
 
 def _rows(t, name, B, T, V, dev):
@@ -518,8 +519,7 @@ def verify_tree(logits, tokens, parent, n_nodes, uniforms, temperature, path, n_
     if logits.dim() != 3:
         raise ValueError("logits must be [B][T][V]")
     B, T, V = logits.shape
-    dev = torch.cuda.current_device()
-    i32, f32 = torch.int32, torch.float32
+    dev, i32, f32 = _device(), torch.int32, torch.float32
     lp, lb, lr = _rows(logits, "logits", B, T, V, dev)
     dp, db, dr = None, 0, 0
     if draft_probs is not None:
