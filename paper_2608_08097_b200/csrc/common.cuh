@@ -22,6 +22,7 @@ int fail(int code, const char *fmt, ...);
 int check_dims(const oasis_dims_t *dims);
 int check_launch(const char *what);   // cudaGetLastError() -> status
 int sm_count();                       // multiprocessors of the current device (148 if unknown)
+int clusters_at_once(int size);       // thread-block clusters of this size (<= 8) that run together with one block per SM
 int32_t *error_word();                // device word registered with oasis_set_error_word (or NULL)
 
 // ---- bounds-check build (-DOASIS_BOUNDS_CHECK) ---------------------------------------------------------

@@ -3,8 +3,8 @@
 // A query row is (node t, query head a).  It sees the history in the row's columns (positions below seq_len) and, in the
 // tree buffer, its ancestors and itself.  The structure is that of the chain attention (attn_tc.cu, whose pieces in
 // tc_common.cuh it shares): work item = (request, KV head, row group, split of the column list), one thread block, the
-// group's query rows as the M rows of every MMA, tiles of four 16-key blocks in a ring of seven 32 KiB stages, warp 0 the
-// TMA producer, warps 1 and 2 the issuers of Q K^T and P V, the others softmax with one thread per MMA row.  What differs:
+// group's query rows as the M rows of every MMA, tiles of four 16-key blocks in a ring of six 32 KiB stages, the queries
+// in shared memory too (by TMA, read by every Q K^T from there), warp 0 the TMA producer, warps 1 and 2 the issuers of Q K^T and P V, the others softmax with one thread per MMA row.  What differs:
 //   - The keys are a list of blocks: the row's visible history blocks, then the blocks of the tree buffer, which comes
 //     through a tensor map of its own ([token][head][K, V] -> the same 8 KiB block image, nodes past n_tree read as
 //     zero).  The producer compacts: columns that are empty or lie past seq_len take no place in a tile and move no
@@ -16,7 +16,13 @@
 //     tensor core, the softmax warps overwrite those V rows with zeros in shared memory (masked tiles only).
 //   - Up to 256 query rows share a thread block (two MMAs of 128 rows per tile); more are cut into row groups of equal
 //     size, neighbouring thread blocks that read the same entries at the same time, so that all but one come from L2.
+//   - Splits of a row merge inside a thread-block cluster where a cluster reaches far enough, else in a second launch.
 // Algorithmic traffic: 8 KiB per (request, KV head, visible column), 512 B per (node, KV head), plus Q, O and lse.
+// What bounds it (32 query and 8 KV heads, per call in a replayed graph): HBM for long lists, 86.4 us at 6.2 TB/s for 2
+// requests x 4,098 columns; HBM and some 7 us of launch, first loads, epilogue and merge for 16 requests x 130 columns
+// under 16 nodes, 28.2 us (4.9 TB/s); the tensor pipe and the softmax between its MMAs under 64 nodes, 42.8 us: an MMA of
+// 64 key columns takes as long as one of 128, and tiles of 128 keys, whose logits fit into the tensor memory only once
+// beside the accumulators, take 47.4 us.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -34,6 +40,7 @@ __host__ __device__ constexpr int tr_threads(int mma_m, int copies, bool pair)  
 // The query rows in shared memory: [dim half][MMA rows][128 B], 128-byte swizzle.
 __host__ __device__ constexpr int tr_rows(int mma_m, bool pair) { return pair ? 256 : mma_m; }
 __host__ __device__ constexpr int tr_stages(bool pair) { return pair ? 5 : 6; }      // of 32 KiB; with the queries 224 KiB at most
+constexpr int kTrMaxCluster = 8;
 constexpr int32_t kTreeTag = 0x40000000;                    // tile_blk: kTreeTag + i = block i of the tree buffer
 // Behind the ring: 512 B of barriers and tile ids, two table windows, the producer's block queue, ancestor masks.
 constexpr int kTrQueue = 64;
@@ -59,11 +66,37 @@ struct TreeAttnParams {
     long long n_slots;  // bounds-check build: slots of the working-set pool (else unused)
 };
 
+// Values from the same shared-memory place of thread block `rank` of the cluster.
+__device__ __forceinline__ uint32_t at_rank(const void *place, uint32_t rank)
+{
+    uint32_t addr;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(place)), "r"(rank));
+    return addr;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_barrier()       // every thread of every block of the cluster
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 __device__ __forceinline__ bool block_seen(int blk, int len) { return blk >= 0 && (long long)blk * kBlock < len; }
 
 // PAIR: 129 to 256 query rows, two MMAs of 128 rows per tile.  Each set of softmax warps owns 128 rows and takes every tile;
 // both have two S buffers and an O accumulator, which fills the tensor memory.
-template <int MMA_M, int COPIES, bool PAIR>
+template <int MMA_M, int COPIES, bool PAIR, bool CLUSTER>
 __global__ void __launch_bounds__(tr_threads(MMA_M, COPIES, PAIR), 1)
 tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ CUtensorMap tree_map,
                     const __grid_constant__ CUtensorMap q_map, const TreeAttnParams p)
@@ -100,8 +133,9 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
     int8_t *up = reinterpret_cast<int8_t *>(misc + kTrUp);                                                // [T]
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int grp = blockIdx.x % p.n_groups;
-    const int split = (blockIdx.x / p.n_groups) % p.n_splits;
+    // (row groups of the same entries side by side; a row's splits, where they are a cluster)
+    const int grp = CLUSTER ? (blockIdx.x / p.n_splits) % p.n_groups : blockIdx.x % p.n_groups;
+    const int split = CLUSTER ? blockIdx.x % p.n_splits : (blockIdx.x / p.n_groups) % p.n_splits;
     const int bh = blockIdx.x / (p.n_groups * p.n_splits);
     const int b = bh / p.Hkv, h = bh % p.Hkv;
     const int row0 = grp * p.group_rows;                             // first query row (node * G + head) of the group
@@ -185,6 +219,13 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         tmem_base = *tmem_slot;
         tmem_o = tmem_base + HALVES * SBUFS * kAtTileKeys;
     }
+
+    // After the last tile the K/V ring is idle.  Every accumulator row goes there with its maximum and sum (part = copy or set
+    // of the query row), then the warps write whole rows: merged, normalised, coalesced.
+    constexpr int PARTS = COPIES * SETS, PITCH = kHeadDim + 4, WRITERS = (THREADS - 96) / 32;
+    float *const o_sm = reinterpret_cast<float *>(kv_ptr);           // [PARTS * RPC or 256][PITCH], then maxima and sums
+    float *const m_sm = o_sm + 256 * PITCH, *const l_sm = m_sm + 256;
+    float *const row_lse = l_sm + 256;                               // clusters: of the block's parts together
 
     if (warp == 0) {
         // ---------------------------------------------------------------- producer
@@ -410,12 +451,6 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         if (alive && n_tiles > 0)
             alive = mbar_wait(bar_empty((n_tiles - 1) % STAGES), ((n_tiles - 1) / STAGES) & 1, p.err, 63);
         tc_fence_after();
-        // The K/V ring is idle now.  Every accumulator row goes there with its maximum and sum (part = copy or set of the
-        // query row), then the warps write whole rows, four dims per lane: merged, normalised, coalesced.
-        constexpr int PARTS = COPIES * SETS, PITCH = kHeadDim + 4;
-        float *o_sm = reinterpret_cast<float *>(kv_ptr);            // [PARTS * RPC or 256][PITCH], then maxima and sums
-        float *m_sm = o_sm + 256 * PITCH;
-        float *l_sm = m_sm + 256;
         const int mine = set * 128 + half * 128 + m_row;
         if (n_tiles > 0 && live_warp && alive) {
             float *dst = o_sm + mine * PITCH;
@@ -440,7 +475,6 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         alive = softmax_warps_all<THREADS - 96>(alive);
         // A warp writes rows r0, r0 + WRITERS, ..: lane k works out row k's weights (the parts', normalised), place and
         // log-sum-exp, then the half-warps copy two rows at a time.
-        constexpr int WRITERS = (THREADS - 96) / 32;
         const int r0 = warp - 3, n_mine = alive && rows > r0 ? (rows - r0 + WRITERS - 1) / WRITERS : 0;    // at most 32
         float w[PARTS];
         int orow = 0;
@@ -462,8 +496,9 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
 #pragma unroll
             for (int c = 0; c < PARTS; ++c) w[c] *= inv;
             const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
-            orow = p.n_splits == 1 ? (b * p.T + tq) * p.Hq + a : blockIdx.x * p.group_rows + r;
-            if (p.n_splits > 1) p.part_lse[orow] = lse2;
+            orow = CLUSTER || p.n_splits == 1 ? (b * p.T + tq) * p.Hq + a : blockIdx.x * p.group_rows + r;
+            if (CLUSTER) row_lse[r] = lse2;
+            else if (p.n_splits > 1) p.part_lse[orow] = lse2;
             else if (p.lse) p.lse[orow] = lse2 * kAtLn2;
         }
         const int side = lane >> 4, col = (lane & 15) * 4;          // four dims in either half of the row
@@ -488,13 +523,54 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
             }
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
-                if (p.n_splits == 1)
+                if (CLUSTER) {                                       // in place of the row's first part, for the cluster's merge
+                    if (k0 + side < n_mine) *reinterpret_cast<float4 *>(o_sm + r * PITCH + col + 64 * d) = acc[d];
+                } else if (p.n_splits == 1)
                     *reinterpret_cast<uint2 *>(p.out + (o * kHeadDim + col + 64 * d) * 2) =
                         make_uint2(pack_bf16x2(acc[d].x, acc[d].y), pack_bf16x2(acc[d].z, acc[d].w));
                 else
                     *reinterpret_cast<float4 *>(p.part_o + o * kHeadDim + col + 64 * d) = acc[d];
             }
         }
+    }
+
+    if constexpr (CLUSTER) {
+        // ---- the cluster's merge: block `split` writes rows split, split + n_splits, ..; lane q holds block q's weight.  All
+        // of a row's reads are in flight together (one at a time they would cost more than the second launch they save).
+        cluster_barrier();
+        if (warp >= 3) {
+#pragma unroll 1
+            for (int r = split + p.n_splits * (warp - 3); r < rows; r += p.n_splits * WRITERS) {
+                const float lse2 = lane < p.n_splits ? ld_cluster(at_rank(row_lse + r, (uint32_t)lane)) : -CUDART_INF_F;
+                float4 f[kTrMaxCluster];
+#pragma unroll
+                for (int q = 0; q < kTrMaxCluster; ++q)
+                    f[q] = ld_cluster4(at_rank(o_sm + r * PITCH + lane * 4, (uint32_t)min(q, p.n_splits - 1)));
+                float mx = lse2;
+#pragma unroll
+                for (int o = 4; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                float w = lse2 == -CUDART_INF_F ? 0.f : fast_exp2(lse2 - mx), den = w;
+#pragma unroll
+                for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+                mx = __shfl_sync(0xffffffffu, mx, 0);
+                den = __shfl_sync(0xffffffffu, den, 0);
+                w *= den > 0.f ? 1.f / den : 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int q = 0; q < kTrMaxCluster; ++q) {            // (lanes past the last block have no weight)
+                    const float wq = __shfl_sync(0xffffffffu, w, q);
+                    acc.x = wq != 0.f ? fmaf(wq, f[q].x, acc.x) : acc.x;
+                    acc.y = wq != 0.f ? fmaf(wq, f[q].y, acc.y) : acc.y;
+                    acc.z = wq != 0.f ? fmaf(wq, f[q].z, acc.z) : acc.z;
+                    acc.w = wq != 0.f ? fmaf(wq, f[q].w, acc.w) : acc.w;
+                }
+                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+                const long long orow = ((long long)b * p.T + tq) * p.Hq + a;
+                reinterpret_cast<uint2 *>(p.out + orow * kHeadDim * 2)[lane] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+                if (p.lse && lane == 0) p.lse[orow] = den > 0.f ? (mx + log2f(den)) * kAtLn2 : -CUDART_INF_F;
+            }
+        }
+        cluster_barrier();                                           // nobody leaves while its shared memory is read
     }
 
     tc_fence_before();
@@ -560,6 +636,7 @@ tree_combine_kernel(const TreeAttnParams p, int total)
 // ---- host side -----------------------------------------------------------------------------------------
 struct TreePlan {
     int n_groups, group_rows, n_splits, cols_per_split;
+    bool in_cluster;
     long long items;
     size_t workspace;
 };
@@ -576,10 +653,22 @@ static TreePlan tree_plan(const oasis_dims_t *dims, int T, int n_cols)
     const long long most = (n_cols + 7) / 8;
     if (s > most) s = most;
     if (s < 1) s = 1;
+    // The splits of a row are a cluster, which merges them through distributed shared memory, where a cluster of at most
+    // eight (and of as many as all fit) costs no more than kMergeTiles tiles of four columns against the finest split; else
+    // the partials go through the workspace and a second launch.  In a graph the two take as long (8.9 and 9.0 us for one
+    // request of five nodes and 18 columns: a cluster's two barriers against a launch that is waiting already); launched one
+    // by one the cluster saves the host 2.2 us.  Three tiles more cost 2.5 us (24.7 against 22.2:
+    // seven requests of 302 columns, four KV heads; clusters of four instead of five splits).
+    long long c = s < kTrMaxCluster ? s : kTrMaxCluster;
+    while (c > 1 && clusters_at_once((int)c) < items) --c;
+    constexpr long long kMergeTiles = 1;
+    pl.in_cluster = c > 1 && n_cols / (4 * c) <= n_cols / (4 * s) + kMergeTiles;
+    if (pl.in_cluster) s = c;
     pl.cols_per_split = (int)((n_cols + s - 1) / s);
     pl.n_splits = (n_cols + pl.cols_per_split - 1) / pl.cols_per_split;
+    if (pl.n_splits == 1) pl.in_cluster = false;
     pl.items = items * pl.n_splits;
-    pl.workspace = pl.n_splits > 1 ? (size_t)pl.items * pl.group_rows * (kHeadDim + 1) * sizeof(float) : 0;
+    pl.workspace = pl.n_splits > 1 && !pl.in_cluster ? (size_t)pl.items * pl.group_rows * (kHeadDim + 1) * sizeof(float) : 0;
     return pl;
 }
 
@@ -666,27 +755,36 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
     p.T = n_tree; p.Hq = dims->n_q_heads; p.Hkv = dims->n_kv_heads; p.G = p.Hq / p.Hkv; p.n_cols = n_cols; p.R = n_tree * p.G;
     p.n_splits = pl.n_splits; p.cols_per_split = pl.cols_per_split; p.n_groups = pl.n_groups; p.group_rows = pl.group_rows;
     p.n_slots = bounds().n_slots;
-    if (pl.n_splits > 1) {
+    if (pl.n_splits > 1 && !pl.in_cluster) {
         p.part_o = (float *)workspace;
         p.part_lse = p.part_o + (size_t)pl.items * pl.group_rows * kHeadDim;
     }
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)pl.n_splits;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)pl.items);
     cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = pl.in_cluster ? 2 : 1;
+#define OASIS_TREE_LAUNCH_AS(M, C, P, X)                                                                                      \
+    do {                                                                                                                      \
+        e = allow_dynamic_shared(reinterpret_cast<const void *>(tree_attn_tc_kernel<M, C, P, X>), tr_smem(M, P));              \
+        if (e == cudaSuccess) prefer_max_shared_carveout(tree_attn_tc_kernel<M, C, P, X>);                                    \
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, tree_attn_tc_kernel<M, C, P, X>, pool_map, tree_map, q_map, p);    \
+    } while (0)
 #define OASIS_TREE_LAUNCH(M, C, P)                                                                                            \
     do {                                                                                                                      \
         cfg.blockDim = dim3(tr_threads(M, C, P));                                                                             \
         cfg.dynamicSmemBytes = tr_smem(M, P);                                                                                 \
-        e = allow_dynamic_shared(reinterpret_cast<const void *>(tree_attn_tc_kernel<M, C, P>), tr_smem(M, P));                 \
-        if (e == cudaSuccess) prefer_max_shared_carveout(tree_attn_tc_kernel<M, C, P>);                                       \
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, tree_attn_tc_kernel<M, C, P>, pool_map, tree_map, q_map, p);       \
+        if (pl.in_cluster) OASIS_TREE_LAUNCH_AS(M, C, P, true);                                                               \
+        else OASIS_TREE_LAUNCH_AS(M, C, P, false);                                                                            \
     } while (0)
     if (pl.group_rows <= 16) OASIS_TREE_LAUNCH(64, 4, false);       // four copies of <= 16 rows, one block of a tile each
     else if (pl.group_rows <= 32) OASIS_TREE_LAUNCH(64, 2, false);  // two copies of <= 32 rows, two blocks each
@@ -694,16 +792,18 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
     else if (pl.group_rows <= 128) OASIS_TREE_LAUNCH(128, 1, false);   // two softmax warp sets, alternate tiles
     else OASIS_TREE_LAUNCH(128, 1, true);                           // two softmax warp sets, 128 rows each
 #undef OASIS_TREE_LAUNCH
+#undef OASIS_TREE_LAUNCH_AS
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(OASIS_ERR_CUDA, "%s: launch: %s", who, cudaGetErrorString(e));
     }
-    if (pl.n_splits > 1) {
+    if (pl.n_splits > 1 && !pl.in_cluster) {
         // (the merge's thread blocks become resident while the attention still runs and wait there for the partials)
         const int total = dims->batch * p.Hkv * p.R;
         cfg.gridDim = dim3((unsigned)((total + 7) / 8));
         cfg.blockDim = dim3(256);
         cfg.dynamicSmemBytes = 0;
+        cfg.numAttrs = 1;
         prefer_max_shared_carveout(tree_combine_kernel);
         e = cudaLaunchKernelEx(&cfg, tree_combine_kernel, p, total);
         if (e != cudaSuccess) return fail(OASIS_ERR_CUDA, "%s: combine launch: %s", who, cudaGetErrorString(e));

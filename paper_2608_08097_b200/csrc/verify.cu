@@ -3,15 +3,21 @@
 //
 // The walk is serial: only after a node's distribution is known is it decided which child is next, and only the rows of
 // the visited nodes are needed (2 to 5 rows of a 64-node tree).  So a request is one cluster of 1 to 8 thread blocks that
-// share the vocabulary, and a visited row costs one pass and one exchange through distributed shared memory:
-//   1. per node, one pass in fp32 over the row: maximum and sum of exponentials (sampling) or the first maximum (greedy).
-//      The children's own logits are picked up meanwhile.
-//   2. the children are tried in order, by every thread alike.  A test that the fp32 sum (off by less than kFuzzy, see
-//      there) cannot decide is made with a sum in fp64: what decides is always the fp64 value.
-//   3. where the walk ends, one fp64 pass gives the mass of every warp's part of the row; the part that holds the random
+// share the vocabulary, and a visited row costs one pass and one exchange:
+//   1. per node, every warp copies its part of the row into shared memory (cp.async) and makes one pass in fp32 over it:
+//      maximum and sum of exponentials (sampling) or the first maximum (greedy).  The warps' results go to every block of
+//      the cluster by asynchronous stores into shared memory, which an mbarrier counts.
+//   2. warp 0 of each block then tries the children in order, all blocks alike, while the other warps wait: serial code
+//      that every warp ran would take the issue slots of the one that matters.  A test that the fp32 sum (off by less than
+//      kFuzzy, see there) cannot decide is made with a sum in fp64: what decides is always the fp64 value.
+//   3. where the walk ends, one fp64 pass over the staged part gives every warp's mass; the part that holds the random
 //      number's place in the running sum is scanned once more, in index order.  fp64, because a vocabulary of 150,000 has
 //      as many borders between tokens: sums in fp32 would put a noticeable share of the draws into the neighbour's interval.
-// All sums have a fixed order, so a result does not depend on timing.  The rows are re-read from L2, nothing is staged.
+// All sums have a fixed order, so a result does not depend on timing.
+// What bounds it: the latency of the serial steps, not bytes.  16 requests, 64-node trees, 151,936 bf16 logits: 28.7 us, of
+// which (cycles) start 4,500, each node 9,000 (copy 2,000, fp32 pass 2,900, exchange 1,300, decision 2,700), the fp64 pass
+// 9,800, the search 1,700.  One request, greedy, 32,000 logits: 8.1 us.  16 requests, chains of 5 with draft distributions,
+// 128,256 fp32 logits: 40.5 us.  128 requests, 6 nodes, 50,257 fp16 logits: 31.7 us.
 #include <math_constants.h>
 
 #include "common.cuh"
@@ -799,7 +805,7 @@ static cudaError_t launch_verify_as(const VerifyParams &p, int batch, int C, cud
 
 // Clusters of `size` thread blocks that run at the same time with one block per SM (a cluster stays within one of the GPU's
 // processing clusters, whose SM counts need not be a multiple of its size).  Asked once per device and size.
-static int clusters_at_once(int size)
+int clusters_at_once(int size)
 {
     constexpr int kDevices = 64;
     static std::mutex lock;

@@ -130,6 +130,12 @@ ATTN = [
     (5, 16, 2, 7, [1000, 999, 16, 31, 512], [7, 1, 7, 4, 9], 70),     # a count beyond n_tree is clamped
     (1, 8, 1, 4, [3000], [4], 190),                   # one row: split over many thread blocks
     (20, 16, 8, 4, [100 + 13 * i for i in range(20)], [4] * 20, 30),  # 160 rows: not split, more than the SMs
+    (2, 8, 2, 20, [700, 650], [20, 13], 40),          # 80 rows, splits that merge as a cluster
+    (1, 8, 2, 8, [500], [8], 31),                     # 32 rows, a cluster of five
+    (2, 24, 2, 5, [600, 20], [5, 4], 36),             # 60 rows, a cluster in which blocks of one request see no key
+    (1, 4, 1, 2, [4100], [2], 255),                   # 8 rows, splits that merge through the workspace
+    (1, 16, 2, 16, [3300], [15], 200),                # 128 rows, the same
+    (1, 8, 2, 64, [3400], [63], 210),                 # 256 rows, the same
 ]
 
 

@@ -121,14 +121,14 @@ def test_refusals_of_tree_attention(L):
     for name in ("q", "tree", "parent", "nodes", "pool", "slot", "blk", "lens", "out"):
         assert call(**{name: None}) == 1, name
     for name in ("q", "tree", "pool", "out", "ws"):
-        assert call(**{name: ODD}) == 1, name
+        assert call(**{"cols": 4000, name: ODD}) == 1, name
     for bad in (dict(T=0), dict(T=65), dict(cols=0), dict(cols=-3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
                 dict(scale=float("inf")), dict(dims=L.Dims(2, 30, 8, 64)), dict(dims=L.Dims(-1, 32, 8, 64))):
         assert call(**bad) == 1, bad
     for bad in (dict(dims=L.Dims(2, 32, 8, 64, head_dim=64)), dict(dims=L.Dims(2, 32, 8, 64, block_size=32)), dict(dims=L.Dims(2, 258, 2, 64))):
         assert call(**bad) == 2, bad
-    need = L.tree_attn_workspace_bytes(L.Dims(2, 32, 8, 64), 5, 10)
-    assert need > 0 and call(ws=None) == 4 and call(ws_bytes=need - 1) == 4 and "workspace" in L.last_error()
+    need = L.tree_attn_workspace_bytes(L.Dims(2, 32, 8, 64), 5, 4000)      # split over more SMs than a cluster has
+    assert need > 0 and call(cols=4000, ws=None) == 4 and call(cols=4000, ws_bytes=need - 1) == 4 and "workspace" in L.last_error()
     assert call(dims=L.Dims(0, 32, 8, 64), ws=None) == 0
     assert L.tree_attn_workspace_bytes(L.Dims(64, 32, 8, 64), 64, 130) == 0 == L.tree_attn_workspace_bytes(L.Dims(1, 32, 8, 64), 65, 130)
 
