@@ -442,7 +442,7 @@ int oasis_verify_tree(int32_t batch, int32_t n_tree, int32_t vocab, const void *
  *   2. if n > 0 the local columns of blk_tbl are set as by oasis_local_window for n tokens at L: the blocks that hold the
  *      kept tokens stay local.  A selection that is made after this step has to leave them out (n_full_blocks = L / 16);
  *      a caller that selects among them as well calls oasis_local_window for the new length first;
- *   3. next_len[b] = L + n (if next_len is not NULL; it may not be seq_len).
+ *   3. next_len[b] = L + n (if next_len is not NULL; it may not share memory with seq_len, n_commit or path).
  * Everything else is left as it was: with n = 0 only next_len is written.  A path entry outside [0, n_tree), a position
  * outside the max_blocks of the request and a negative slot are skipped.
  *   path        [B][max_path] int32 (device), 1 <= max_path <= 16;  n_commit, seq_len, next_len [B] int32 (device)

@@ -51,6 +51,9 @@ class Dims:
         return _Dims(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.block_size,
                      self.max_blocks)
 
+    def __getstate__(self):                          # copies and pickles: without the C struct that _cdims leaves here
+        return {k: v for k, v in self.__dict__.items() if k != "_ref"}
+
 
 _lib = None
 

@@ -97,8 +97,12 @@ static int launch_commit(const oasis_dims_t *dims, int n_layers, const void *con
     if (dims->batch == 0 || n_layers == 0) return OASIS_OK;
     if (!tree_kvs || !path || !n_commit || !seq_len || !block_tables || !slot_tbls || !blk_tbls || !pools)
         return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
-    if (next_len == seq_len || next_len == n_commit)
-        return fail(OASIS_ERR_INVALID_ARG, "%s: next_len may not be seq_len or n_commit", who);
+    const auto overlaps = [&](const int32_t *in, long long n) {        // (all layers and heads read them, in no order)
+        const uintptr_t a = reinterpret_cast<uintptr_t>(next_len), c = reinterpret_cast<uintptr_t>(in);
+        return a < c + 4 * (uintptr_t)n && c < a + 4 * (uintptr_t)dims->batch;
+    };
+    if (next_len && (overlaps(seq_len, dims->batch) || overlaps(n_commit, dims->batch) || overlaps(path, (long long)dims->batch * M)))
+        return fail(OASIS_ERR_INVALID_ARG, "%s: next_len may not share memory with seq_len, n_commit or path", who);
     CommitLayers ly = {};
     for (int l = 0; l < n_layers; ++l) {
         void *host = host_kvs ? host_kvs[l] : nullptr;

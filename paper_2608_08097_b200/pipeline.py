@@ -26,6 +26,7 @@ class DecodeLayer:
         self.B, self.Hq, self.Hkv, self.mb = batch, n_q_heads, n_kv_heads, max_blocks
         self.k, self.T = k, n_q_tokens
         self.cols = k + 2
+        self.tree = bool(tree)
         self.dims = oasis.Dims(batch, n_q_heads, n_kv_heads, max_blocks)
         self.device = torch.device(device)
         dev = self.device
@@ -50,7 +51,9 @@ class DecodeLayer:
 
     # step 1: the draft tokens are rows 1..T-1 of the stacked verify-step queries
     def score(self, q, n_full, reduce_mode=oasis.REDUCE_MAX, stream=None):
-        n_draft = min(self.T - 1, 128 // (self.Hq // self.Hkv))      # a wide tree: its first drafts (at most 128 rows score)
+        n_draft = self.T - 1
+        if self.tree:
+            n_draft = min(n_draft, 128 // (self.Hq // self.Hkv))     # a wide tree: its first drafts (at most 128 rows score)
         q_draft = q[:, 1:]
         oasis.score_blocks(self.dims, q_draft, n_draft, self.summaries, n_full, self.scores,
                            reduce_mode=reduce_mode, q_batch_stride=self.T * self.Hq * 128, stream=stream)

@@ -166,6 +166,10 @@ def test_refusals_of_the_commit(L):
     for bad in (dict(T=0), dict(T=65), dict(M=0), dict(M=17), dict(col=-1), dict(col=9), dict(cols=1, col=0), dict(layers=65), dict(layers=-1),
                 dict(nxt=ONE)):                                      # next_len is seq_len here
         assert call(**bad) == 1, bad
+    far, off = 1 << 20, ONE + 4                                      # next_len overlaps one of its inputs by an element
+    for inputs in (dict(path=far, n=far), dict(path=far, lens=far), dict(n=far, lens=far), dict(path=ONE - 36, n=far, lens=far)):
+        assert call(nxt=off if "path" not in inputs or inputs["path"] == far else ONE, **inputs) == 1, inputs
+        assert "share memory" in L.last_error()
     assert call(layers=0) == 0 and call(dims=L.Dims(0, 32, 8, 64)) == 0
 
 
@@ -175,6 +179,14 @@ def test_commit_plan_needs_one_tensor_per_layer(L):
         L.CommitPlan(L.Dims(1, 8, 8, 8), [t, t], [t], [t, t], [t, t], 0, [t, t])
     with pytest.raises(ValueError, match="layers outside"):
         L.CommitPlan(L.Dims(1, 8, 8, 8), [], [], [], [], 0, [])
+
+
+def test_dims_can_be_copied_after_a_call(L):
+    import copy
+    import pickle
+    d = L.Dims(2, 32, 8, 64)
+    L._cdims(d)
+    assert pickle.loads(pickle.dumps(d)) == d == copy.deepcopy(d) and L._cdims(copy.copy(d)) is not L._cdims(d)
 
 
 def test_an_engine_refuses_trees_it_cannot_run():
