@@ -52,7 +52,7 @@ class Dims:
                      self.max_blocks)
 
     def __getstate__(self):                          # copies and pickles: without the C struct that _cdims leaves here
-        return {k: v for k, v in self.__dict__.items() if k != "_ref"}
+        return {k: v for k, v in self.__dict__.items() if k != "_c"}
 
 
 _lib = None
@@ -418,26 +418,35 @@ def stage_blocks_bulk(host_kvs, idx, slots, n, hbm_pools, max_streams=0, stream=
 
 # ---- a tree of drafted tokens: attention, verification, commit ------------------------------------------------------
 MAX_TREE = 64
-_LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (torch.cuda.current_stream() takes 3 us)
-_device = torch.cuda.current_device
+_call = None
+
+
+def _calls():
+    """The native calls of the draft-tree operators (tensor checks and the call of the C ABI), bound to the loaded library."""
+    global _call
+    if _call is None:
+        L = lib()
+        try:
+            from . import _call as native
+        except ImportError as e:
+            raise OasisError("_call.so cannot be loaded: build it with `python -m paper_2608_08097_b200.build` (%s)" % e) from e
+        native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.oasis_tree_attn, L.oasis_verify_tree, L.oasis_commit_kv_layers)))
+        _call = native
+    return _call
 
 
 def _cdims(dims):
-    """Reference to the dims' C struct, made once per Dims object (it is immutable)."""
-    ref = dims.__dict__.get("_ref")
-    if ref is None:
-        ref = ctypes.byref(dims.c())
-        dims.__dict__["_ref"] = ref
-    return ref
+    """Address of the dims' C struct, which is made once per Dims object (it is immutable) and lives as long."""
+    c = dims.__dict__.get("_c")
+    if c is None:
+        c = dims.__dict__["_c"] = dims.c()
+    return ctypes.addressof(c)
 
 
 def _dev(t, dtype, shape, name, device):
     """Address of a dense tensor of this type and shape on `device` (the current device's index)."""
-    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
-        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
     if t.shape != shape:
@@ -460,10 +469,9 @@ def _pool_ptr(t, dtype, name, device, host_ok=False):
     return t.data_ptr()
 
 
-def _stream_id(stream, device):
-    if stream is None:
-        return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+def _handle(stream):
+    """A stream's raw handle; None (the current stream) stays None."""
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else None if stream is None else int(stream)
 
 
 def tree_attn_workspace_bytes(dims, n_tree, n_cols) -> int:
@@ -477,37 +485,10 @@ def tree_attn(dims, q, tree_kv, parent, n_nodes, hbm_pool, slot_tbl, blk_tbl, se
     below seq_len[b] in the columns of blk_tbl), its ancestors and itself.  q, out [B][T][Hq][128]; tree_kv
     [B][T][Hkv][2][128]; parent [B][T], n_nodes [B] int32; rows of padding nodes are left as they were.
     `workspace`: tree_attn_workspace_bytes() bytes where that is not zero."""
-    B, Hq, Hkv = dims.batch, dims.n_q_heads, dims.n_kv_heads
-    T, n_cols = q.shape[1], blk_tbl.shape[-1]
-    dev, bf, i32 = _device(), torch.bfloat16, torch.int32
-    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
-        raise ValueError("workspace must be contiguous and on the current CUDA device")
-    rows, table, per_request = (B, T, Hq, 128), (B, Hkv, n_cols), (B,)
-    rc = lib().oasis_tree_attn(
-        _cdims(dims), _dev(q, bf, rows, "q", dev), T, _dev(tree_kv, bf, (B, T, Hkv, 2, 128), "tree_kv", dev),
-        _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, per_request, "n_nodes", dev),
-        _pool_ptr(hbm_pool, bf, "hbm_pool", dev), _dev(slot_tbl, i32, table, "slot_tbl", dev),
-        _dev(blk_tbl, i32, table, "blk_tbl", dev), n_cols, _dev(seq_len, i32, per_request, "seq_len", dev), scale,
-        _dev(out, bf, rows, "out", dev), None if lse is None else _dev(lse, torch.float32, (B, T, Hq), "lse", dev),
-        None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream_id(stream, dev))
+    rc = (_call or _calls()).tree_attn(_cdims(dims), q, tree_kv, parent, n_nodes, hbm_pool, slot_tbl, blk_tbl, seq_len, scale,
+                                       out, lse, workspace, None if stream is None else _handle(stream))
     if rc:
         _check(rc, "oasis_tree_attn")
-
-
-def _rows(t, name, B, T, V, dev):
-    """Address, batch stride and row stride of a [B][T][V] tensor whose rows are dense."""
-    if t.shape != (B, T, V):
-        raise ValueError("%s: expected shape %s, got %s" % (name, (B, T, V), tuple(t.shape)))
-    if t.get_device() != dev:
-        raise ValueError("%s must be on the current CUDA device" % name)
-    sb, sr, s1 = t.stride()
-    if s1 != 1 and V > 1:
-        raise ValueError("%s: the rows must be dense" % name)
-    if T == 1 and sr < V:
-        sr = V                                   # (the stride of a single row means nothing)
-    if sr < V or (sb < 0 and B > 1):
-        raise ValueError("%s: rows must not overlap" % name)
-    return t.data_ptr(), max(sb, 0), sr
 
 
 def verify_tree(logits, tokens, parent, n_nodes, uniforms, temperature, path, n_commit, next_token, draft_probs=None,
@@ -517,25 +498,10 @@ def verify_tree(logits, tokens, parent, n_nodes, uniforms, temperature, path, n_
     n_commit [B] and the token that follows it, next_token [B].  uniforms [B][T] fp32: element c decides on node c,
     element 0 draws the next token.  temperature [B] fp32: 0 is greedy.  draft_probs [B][T][V] fp32: row x is the
     distribution that node x's children were drawn from; without it the drafts count as chosen without chance."""
-    if logits.dtype not in _LOGIT_TYPES:
-        raise TypeError("logits: expected float32, bfloat16 or float16, got %s" % logits.dtype)
-    if logits.dim() != 3:
-        raise ValueError("logits must be [B][T][V]")
-    B, T, V = logits.shape
-    dev, i32, f32 = _device(), torch.int32, torch.float32
-    lp, lb, lr = _rows(logits, "logits", B, T, V, dev)
-    dp, db, dr = None, 0, 0
-    if draft_probs is not None:
-        if draft_probs.dtype != f32:
-            raise TypeError("draft_probs: expected float32, got %s" % draft_probs.dtype)
-        dp, db, dr = _rows(draft_probs, "draft_probs", B, T, V, dev)
-    M = path.shape[-1]
-    _check(lib().oasis_verify_tree(
-        B, T, V, lp, _LOGIT_TYPES[logits.dtype], lb, lr, _dev(tokens, i32, (B, T), "tokens", dev),
-        _dev(parent, i32, (B, T), "parent", dev), _dev(n_nodes, i32, (B,), "n_nodes", dev),
-        _dev(uniforms, f32, (B, T), "uniforms", dev), _dev(temperature, f32, (B,), "temperature", dev), dp, db, dr,
-        _dev(path, i32, (B, M), "path", dev), M, _dev(n_commit, i32, (B,), "n_commit", dev),
-        _dev(next_token, i32, (B,), "next_token", dev), _stream_id(stream, dev)), "oasis_verify_tree")
+    rc = (_call or _calls()).verify_tree(logits, tokens, parent, n_nodes, uniforms, temperature, path, n_commit, next_token,
+                                         draft_probs, None if stream is None else _handle(stream))
+    if rc:
+        _check(rc, "oasis_verify_tree")
 
 
 class CommitPlan:
@@ -549,33 +515,31 @@ class CommitPlan:
             raise ValueError("one tensor per layer is needed in every list")
         if not 1 <= n <= MAX_APPEND_LAYERS:
             raise ValueError("%d layers outside [1, %d]" % (n, MAX_APPEND_LAYERS))
-        self.device = torch.cuda.current_device()
-        B, Hkv, dev = dims.batch, dims.n_kv_heads, self.device
-        self.T, self.n_cols, self.n_layers, self.local_col, self.batch = tree_kvs[0].shape[1], blk_tbls[0].shape[-1], n, int(local_col), B
-        arr = ctypes.c_void_p * n
+        B, Hkv, dev = dims.batch, dims.n_kv_heads, torch.cuda.current_device()
+        T, n_cols = tree_kvs[0].shape[1], blk_tbls[0].shape[-1]
         bf, i32 = torch.bfloat16, torch.int32
-        self.dims = _cdims(dims)
-        self.tree_kvs = arr(*[_dev(t, bf, (B, self.T, Hkv, 2, 128), "tree_kvs", dev) for t in tree_kvs])
-        self.block_tables = arr(*[_dev(t, i32, (B, dims.max_blocks), "block_tables", dev) for t in block_tables])
-        self.slot_tbls = arr(*[_dev(t, i32, (B, Hkv, self.n_cols), "slot_tbls", dev) for t in slot_tbls])
-        self.blk_tbls = arr(*[_dev(t, i32, (B, Hkv, self.n_cols), "blk_tbls", dev) for t in blk_tbls])
-        self.pools = arr(*[_pool_ptr(t, bf, "hbm_pools", dev) for t in hbm_pools])
-        self.host_kvs = arr(*[None if t is None else _pool_ptr(t, bf, "host_kvs", dev, host_ok=True) for t in host_kvs])
+
+        def arr(tensors, address):
+            return (ctypes.c_void_p * n)(*[None if t is None else address(t) for t in tensors])
+
+        lists = (arr(tree_kvs, lambda t: _dev(t, bf, (B, T, Hkv, 2, 128), "tree_kvs", dev)),
+                 arr(block_tables, lambda t: _dev(t, i32, (B, dims.max_blocks), "block_tables", dev)),
+                 arr(slot_tbls, lambda t: _dev(t, i32, (B, Hkv, n_cols), "slot_tbls", dev)),
+                 arr(blk_tbls, lambda t: _dev(t, i32, (B, Hkv, n_cols), "blk_tbls", dev)),
+                 arr(hbm_pools, lambda t: _pool_ptr(t, bf, "hbm_pools", dev)),
+                 arr(host_kvs, lambda t: _pool_ptr(t, bf, "host_kvs", dev, host_ok=True)))
+        kv, tables, slots, blks, pools, hosts = (ctypes.addressof(a) for a in lists)
+        self.args = (dev, _cdims(dims), n, kv, T, tables, slots, blks, n_cols, int(local_col), pools, hosts)
+        self._lists, self._dims = lists, dims                        # (what `args` holds the addresses of)
         self._held = (tree_kvs, block_tables, slot_tbls, blk_tbls, hbm_pools, host_kvs)
 
 
 def commit_kv_layers(plan, path, n_commit, seq_len, next_len=None, stream=None):
     """Writes the kept path [B][max_path] of every request (its first n_commit[b] nodes) from the layers' tree buffers
     into their local windows and full-KV pools, sets the local columns, and next_len = seq_len + n_commit."""
-    B, dev, i32 = plan.batch, torch.cuda.current_device(), torch.int32
-    if dev != plan.device:
-        raise ValueError("the plan's buffers are on another device")
-    M = path.shape[-1]
-    _check(lib().oasis_commit_kv_layers(
-        plan.dims, plan.n_layers, plan.tree_kvs, plan.T, _dev(path, i32, (B, M), "path", dev), M,
-        _dev(n_commit, i32, (B,), "n_commit", dev), _dev(seq_len, i32, (B,), "seq_len", dev), plan.block_tables, plan.slot_tbls,
-        plan.blk_tbls, plan.n_cols, plan.local_col, plan.pools, plan.host_kvs,
-        None if next_len is None else _dev(next_len, i32, (B,), "next_len", dev), _stream_id(stream, dev)), "oasis_commit_kv_layers")
+    rc = (_call or _calls()).commit_kv_layers(plan.args, path, n_commit, seq_len, next_len, None if stream is None else _handle(stream))
+    if rc:
+        _check(rc, "oasis_commit_kv_layers")
 
 
 def commit_kv(dims, tree_kv, path, n_commit, seq_len, block_table, slot_tbl, blk_tbl, local_col, hbm_pool, host_kv=None,

@@ -1,4 +1,5 @@
-"""Builds the CUDA library (csrc/*.cu -> liboasis.so, in-tree) for sm_100a.
+"""Builds the CUDA library (csrc/*.cu -> liboasis.so, in-tree) for sm_100a, and the Python calls of the draft-tree
+operators (csrc/py_call.cpp -> _call.so, host code only).
 
 nvcc cross-compiles without a GPU.  Objects are rebuilt only when their source (or a
 header) is newer; `python -m paper_2608_08097_b200.build --force` rebuilds everything,
@@ -8,9 +9,11 @@ device array is range-checked on the device; see include/oasis.h).
 """
 import concurrent.futures
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -18,6 +21,7 @@ OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "liboasis.so")
 OBJ_CHECKED = os.path.join(HERE, "build_checked")
 LIB_CHECKED = os.path.join(HERE, "liboasis_checked.so")
+CALL = os.path.join(HERE, "_call.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC"]
@@ -39,7 +43,22 @@ def _compile(src, verbose, obj_dir=OBJ, defines=()):
     return obj, r.stderr
 
 
+def _build_call(force=False):
+    src = os.path.join(CSRC, "py_call.cpp")
+    if not force and os.path.exists(CALL) and os.path.getmtime(CALL) >= max(os.path.getmtime(src), os.path.getmtime(os.path.join(HERE, "..", "include", "oasis.h"))):
+        return
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-I" + sysconfig.get_paths()["include"]]
+    cmd += ["-I" + os.path.join(d, "include") for d in (torch, cuda)] + ["-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include")]
+    cmd += [src, "-o", CALL, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for %s:\n%s\n%s" % (src, r.stdout, r.stderr))
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
+    _build_call(force)
     obj_dir, lib = (OBJ_CHECKED, LIB_CHECKED) if checked else (OBJ, LIB)
     defines = ("-DOASIS_BOUNDS_CHECK",) if checked else ()
     os.makedirs(obj_dir, exist_ok=True)

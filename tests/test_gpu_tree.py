@@ -482,6 +482,26 @@ def test_wrong_tensors_are_refused(L):
             L.verify_tree(**{**good, name: bad})
     with pytest.raises(TypeError):
         L.verify_tree(**good, draft_probs=x.half())
+    for name, bad, err in (("path", z[0], ValueError), ("path", z.long(), TypeError), ("n_commit", n[:1], ValueError), ("next_token", [1, 2], TypeError),
+                           ("n_nodes", n.cpu(), ValueError), ("draft_probs", x[:, :, :5], ValueError), ("draft_probs", x.cpu(), ValueError)):
+        with pytest.raises(err):
+            L.verify_tree(**{**good, name: bad})
+    dims, bf = L.Dims(2, 4, 2, 4), dict(dtype=torch.bfloat16, device="cuda")
+    kv, pool, host = torch.zeros((2, 3, 2, 2, 128), **bf), torch.zeros((20, 2, 16, 128), **bf), torch.zeros((8, 2, 2, 16, 128), dtype=torch.bfloat16)
+    table, cols = torch.zeros((2, 4), dtype=torch.int32, device="cuda"), torch.zeros((2, 2, 4), dtype=torch.int32, device="cuda")
+    plan = dict(dims=dims, tree_kvs=[kv], block_tables=[table], slot_tbls=[cols], blk_tbls=[cols.clone()], local_col=2, hbm_pools=[pool])
+    for name, bad, err in (("tree_kvs", kv.float(), TypeError), ("tree_kvs", kv.cpu(), ValueError), ("block_tables", table[:, :2], ValueError),
+                           ("slot_tbls", cols.long(), TypeError), ("hbm_pools", pool[:, :, :8], ValueError), ("host_kvs", host, ValueError)):
+        with pytest.raises(err):
+            L.CommitPlan(**{**plan, name: [bad]})
+    plan = L.CommitPlan(**plan)
+    good = dict(path=z, n_commit=n, seq_len=n.clone(), next_len=n.clone())
+    for name, bad, err in (("path", z[0], ValueError), ("path", z.float(), TypeError), ("n_commit", n.cpu(), ValueError), ("seq_len", n.repeat(2), ValueError),
+                           ("next_len", n.long(), TypeError)):
+        with pytest.raises(err):
+            L.commit_kv_layers(plan, **{**good, name: bad})
+    with pytest.raises(L.OasisError, match="share memory"):
+        L.commit_kv_layers(plan, z, n, good["seq_len"], next_len=good["seq_len"])
 
 
 def test_empty_batches_do_nothing(L):

@@ -186,7 +186,7 @@ def test_dims_can_be_copied_after_a_call(L):
     import pickle
     d = L.Dims(2, 32, 8, 64)
     L._cdims(d)
-    assert pickle.loads(pickle.dumps(d)) == d == copy.deepcopy(d) and L._cdims(copy.copy(d)) is not L._cdims(d)
+    assert pickle.loads(pickle.dumps(d)) == d == copy.deepcopy(d) and L._cdims(copy.copy(d)) != L._cdims(d)
 
 
 def test_an_engine_refuses_trees_it_cannot_run():
