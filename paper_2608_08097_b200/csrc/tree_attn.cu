@@ -535,39 +535,48 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
     }
 
     if constexpr (CLUSTER) {
-        // ---- the cluster's merge: block `split` writes rows split, split + n_splits, ..; lane q holds block q's weight.  All
-        // of a row's reads are in flight together (one at a time they would cost more than the second launch they save).
+        // ---- the cluster's merge: block `split` writes rows split, split + n_splits, ..  A warp takes four, two or one row at a
+        // time, so that eight reads are in flight whatever the size of the cluster: read e belongs to row e >> lg and block
+        // e & (per - 1), and lane e holds its weight.
         cluster_barrier();
         if (warp >= 3) {
+            const int lg = p.n_splits <= 2 ? 1 : p.n_splits <= 4 ? 2 : 3, per = 1 << lg, step = p.n_splits * WRITERS;
 #pragma unroll 1
-            for (int r = split + p.n_splits * (warp - 3); r < rows; r += p.n_splits * WRITERS) {
-                const float lse2 = lane < p.n_splits ? ld_cluster(at_rank(row_lse + r, (uint32_t)lane)) : -CUDART_INF_F;
+            for (int r0 = split + p.n_splits * (warp - 3); r0 < rows; r0 += step * (kTrMaxCluster >> lg)) {
+                const int my_r = r0 + (lane >> lg) * step, my_q = lane & (per - 1);
+                const bool mine = lane < kTrMaxCluster && my_r < rows && my_q < p.n_splits;
+                const float lse2 = mine ? ld_cluster(at_rank(row_lse + my_r, (uint32_t)my_q)) : -CUDART_INF_F;
                 float4 f[kTrMaxCluster];
 #pragma unroll
-                for (int q = 0; q < kTrMaxCluster; ++q)
-                    f[q] = ld_cluster4(at_rank(o_sm + r * PITCH + lane * 4, (uint32_t)min(q, p.n_splits - 1)));
+                for (int e = 0; e < kTrMaxCluster; ++e) {
+                    const int r = r0 + (e >> lg) * step, q = e & (per - 1);
+                    f[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (r < rows && q < p.n_splits) f[e] = ld_cluster4(at_rank(o_sm + r * PITCH + lane * 4, (uint32_t)q));
+                }
                 float mx = lse2;
-#pragma unroll
-                for (int o = 4; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                for (int o = per >> 1; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
                 float w = lse2 == -CUDART_INF_F ? 0.f : fast_exp2(lse2 - mx), den = w;
-#pragma unroll
-                for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-                mx = __shfl_sync(0xffffffffu, mx, 0);
-                den = __shfl_sync(0xffffffffu, den, 0);
+                for (int o = per >> 1; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
                 w *= den > 0.f ? 1.f / den : 0.f;
+                const int tq = (row0 + my_r) / p.G, a = h * p.G + (row0 + my_r) % p.G;
+                const long long my_row = ((long long)b * p.T + tq) * p.Hq + a;
+                if (p.lse && mine && my_q == 0) p.lse[my_row] = den > 0.f ? (mx + log2f(den)) * kAtLn2 : -CUDART_INF_F;
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int q = 0; q < kTrMaxCluster; ++q) {            // (lanes past the last block have no weight)
-                    const float wq = __shfl_sync(0xffffffffu, w, q);
-                    acc.x = wq != 0.f ? fmaf(wq, f[q].x, acc.x) : acc.x;
-                    acc.y = wq != 0.f ? fmaf(wq, f[q].y, acc.y) : acc.y;
-                    acc.z = wq != 0.f ? fmaf(wq, f[q].z, acc.z) : acc.z;
-                    acc.w = wq != 0.f ? fmaf(wq, f[q].w, acc.w) : acc.w;
+                for (int e = 0; e < kTrMaxCluster; ++e) {            // (places of no row or block have no weight)
+                    const float we = __shfl_sync(0xffffffffu, w, e);
+                    acc.x = we != 0.f ? fmaf(we, f[e].x, acc.x) : acc.x;
+                    acc.y = we != 0.f ? fmaf(we, f[e].y, acc.y) : acc.y;
+                    acc.z = we != 0.f ? fmaf(we, f[e].z, acc.z) : acc.z;
+                    acc.w = we != 0.f ? fmaf(we, f[e].w, acc.w) : acc.w;
+                    if ((e & (per - 1)) == per - 1) {                // the row's last
+                        const long long orow = __shfl_sync(0xffffffffu, my_row, e);
+                        if (r0 + (e >> lg) * step < rows)
+                            reinterpret_cast<uint2 *>(p.out + orow * kHeadDim * 2)[lane] =
+                                make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+                        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
                 }
-                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
-                const long long orow = ((long long)b * p.T + tq) * p.Hq + a;
-                reinterpret_cast<uint2 *>(p.out + orow * kHeadDim * 2)[lane] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-                if (p.lse && lane == 0) p.lse[orow] = den > 0.f ? (mx + log2f(den)) * kAtLn2 : -CUDART_INF_F;
             }
         }
         cluster_barrier();                                           // nobody leaves while its shared memory is read
@@ -653,16 +662,20 @@ static TreePlan tree_plan(const oasis_dims_t *dims, int T, int n_cols)
     const long long most = (n_cols + 7) / 8;
     if (s > most) s = most;
     if (s < 1) s = 1;
-    // The splits of a row are a cluster, which merges them through distributed shared memory, where a cluster of at most
-    // eight (and of as many as all fit) costs no more than kMergeTiles tiles of four columns against the finest split; else
-    // the partials go through the workspace and a second launch.  In a graph the two take as long (8.9 and 9.0 us for one
-    // request of five nodes and 18 columns: a cluster's two barriers against a launch that is waiting already); launched one
-    // by one the cluster saves the host 2.2 us.  Three tiles more cost 2.5 us (24.7 against 22.2:
-    // seven requests of 302 columns, four KV heads; clusters of four instead of five splits).
-    long long c = s < kTrMaxCluster ? s : kTrMaxCluster;
-    while (c > 1 && clusters_at_once((int)c) < items) --c;
+    // The splits of a row are a cluster of two, three, four or eight thread blocks, which merges them through distributed shared
+    // memory, where as many clusters as are needed run at once, a coarser split costs no more than kMergeTiles tiles of four
+    // columns against the finest one, and the rows are few or the blocks many; else the partials go through the workspace and a
+    // second launch.  In a graph, 32 query and 8 KV heads, 5 / 16 / 64 nodes, cluster against workspace:
+    //   1 request  x  18 columns   8.4 / 10.7 / 16.5   9.4 /  9.6 / 12.9 us   (the second launch spreads over idle SMs)
+    //   4 requests x 130 columns  13.8 / 15.2 / 24.4  16.7 / 17.0 / 25.4 us
+    //   5 requests x  62 columns  12.2 / 13.2 / 21.7  13.4 / 13.4 / 23.5 us
+    //   8 requests x 130 columns, 32 nodes      22.1                25.9 us
+    // Launched one by one, the cluster also saves the host 2 us a call.  Clusters of five (2 x 35 columns, 64 nodes) take 20 us
+    // against 15.6; three tiles more cost 2.5 us (24.7 against 22.2: seven requests of 302 columns, four instead of five splits).
     constexpr long long kMergeTiles = 1;
-    pl.in_cluster = c > 1 && n_cols / (4 * c) <= n_cols / (4 * s) + kMergeTiles;
+    long long c = s >= kTrMaxCluster ? kTrMaxCluster : s < 4 ? s : 4;
+    while (c > 1 && clusters_at_once((int)c) < items) c = c == kTrMaxCluster ? 4 : c - 1;
+    pl.in_cluster = c > 1 && n_cols / (4 * c) <= n_cols / (4 * s) + kMergeTiles && (pl.group_rows <= 32 || 2 * items * c >= sm_count());
     if (pl.in_cluster) s = c;
     pl.cols_per_split = (int)((n_cols + s - 1) / s);
     pl.n_splits = (n_cols + pl.cols_per_split - 1) / pl.cols_per_split;
