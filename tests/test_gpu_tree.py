@@ -130,9 +130,13 @@ ATTN = [
     (5, 16, 2, 7, [1000, 999, 16, 31, 512], [7, 1, 7, 4, 9], 70),     # a count beyond n_tree is clamped
     (1, 8, 1, 4, [3000], [4], 190),                   # one row: split over many thread blocks
     (20, 16, 8, 4, [100 + 13 * i for i in range(20)], [4] * 20, 30),  # 160 rows: not split, more than the SMs
-    (2, 8, 2, 20, [700, 650], [20, 13], 40),          # 80 rows, splits that merge as a cluster
-    (1, 8, 2, 8, [500], [8], 31),                     # 32 rows, a cluster of five
-    (2, 24, 2, 5, [600, 20], [5, 4], 36),             # 60 rows, a cluster in which blocks of one request see no key
+    (2, 8, 2, 20, [700, 650], [20, 13], 40),          # 80 rows
+    (1, 8, 2, 8, [500], [8], 31),                     # 32 rows, splits that merge as a cluster of four
+    (2, 24, 2, 5, [600, 20], [5, 4], 36),             # 60 rows
+    (11, 16, 4, 16, [350, 20, 0, 16, 90, 333, 17, 15, 111, 400, 5], [16, 9, 16, 1, 0, 16, 16, 3, 16, 16, 7], 24),     # 64 rows, clusters of three
+    (10, 16, 4, 20, [350, 20, 0, 16, 90, 333, 17, 15, 111, 400], [20, 9, 20, 1, 0, 20, 20, 3, 20, 19], 24),            # 80 rows, the same
+    (10, 16, 4, 41, [350, 20, 0, 16, 90, 333, 17, 15, 111, 400], [41, 9, 33, 1, 0, 40, 41, 3, 41, 41], 24),            # 164 rows, the same
+    (9, 16, 4, 64, [270, 20, 0, 16, 90, 260, 17, 15, 111], [64, 9, 33, 1, 0, 40, 64, 3, 64], 16),                      # 256 rows, clusters of two
     (1, 4, 1, 2, [4100], [2], 255),                   # 8 rows, splits that merge through the workspace
     (1, 16, 2, 16, [3300], [15], 200),                # 128 rows, the same
     (1, 8, 2, 64, [3400], [63], 210),                 # 256 rows, the same
