@@ -445,30 +445,6 @@ def _cdims(dims):
     return ctypes.addressof(c)
 
 
-def _dev(t, dtype, shape, name, device):
-    """Address of a dense tensor of this type and shape on `device` (the current device's index)."""
-    if t.dtype != dtype:
-        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
-    if t.shape != shape:
-        raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if t.get_device() != device:
-        raise ValueError("%s must be on the current CUDA device" % name)
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
-    return t.data_ptr()
-
-
-def _pool_ptr(t, dtype, name, device, host_ok=False):
-    """Address of a pool of entries [..][2][16][128] in device memory (or, `host_ok`, pinned host memory)."""
-    if t.dtype != dtype:
-        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
-    if t.shape[-3:] != (2, 16, 128) or not t.is_contiguous():        # (entries in any number of leading dimensions)
-        raise ValueError("%s must be a contiguous pool of [2][16][128] entries" % name)
-    if t.get_device() != device and not (host_ok and not t.is_cuda and t.is_pinned()):
-        raise ValueError("%s must be on the current CUDA device%s" % (name, " or in pinned host memory" if host_ok else ""))
-    return t.data_ptr()
-
-
 def _handle(stream):
     """A stream's raw handle; None (the current stream) stays None."""
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else None if stream is None else int(stream)
@@ -515,23 +491,16 @@ class CommitPlan:
             raise ValueError("one tensor per layer is needed in every list")
         if not 1 <= n <= MAX_APPEND_LAYERS:
             raise ValueError("%d layers outside [1, %d]" % (n, MAX_APPEND_LAYERS))
-        B, Hkv, dev = dims.batch, dims.n_kv_heads, torch.cuda.current_device()
+        B, Hkv, get = dims.batch, dims.n_kv_heads, _calls().addresses
         T, n_cols = tree_kvs[0].shape[1], blk_tbls[0].shape[-1]
-        bf, i32 = torch.bfloat16, torch.int32
-
-        def arr(tensors, address):
-            return (ctypes.c_void_p * n)(*[None if t is None else address(t) for t in tensors])
-
-        lists = (arr(tree_kvs, lambda t: _dev(t, bf, (B, T, Hkv, 2, 128), "tree_kvs", dev)),
-                 arr(block_tables, lambda t: _dev(t, i32, (B, dims.max_blocks), "block_tables", dev)),
-                 arr(slot_tbls, lambda t: _dev(t, i32, (B, Hkv, n_cols), "slot_tbls", dev)),
-                 arr(blk_tbls, lambda t: _dev(t, i32, (B, Hkv, n_cols), "blk_tbls", dev)),
-                 arr(hbm_pools, lambda t: _pool_ptr(t, bf, "hbm_pools", dev)),
-                 arr(host_kvs, lambda t: _pool_ptr(t, bf, "host_kvs", dev, host_ok=True)))
+        pointers = (get(list(tree_kvs), 0, (B, T, Hkv, 2, 128), "tree_kvs"), get(list(block_tables), 1, (B, dims.max_blocks), "block_tables"),
+                    get(list(slot_tbls), 1, (B, Hkv, n_cols), "slot_tbls"), get(list(blk_tbls), 1, (B, Hkv, n_cols), "blk_tbls"),
+                    get(list(hbm_pools), 2, (), "hbm_pools"), get(host_kvs, 3, (), "host_kvs"))
+        lists = tuple((ctypes.c_void_p * n).from_buffer_copy(p) for p in pointers)
         kv, tables, slots, blks, pools, hosts = (ctypes.addressof(a) for a in lists)
-        self.args = (dev, _cdims(dims), n, kv, T, tables, slots, blks, n_cols, int(local_col), pools, hosts)
+        self.args = (torch.cuda.current_device(), _cdims(dims), n, kv, T, tables, slots, blks, n_cols, int(local_col), pools, hosts)
         self._lists, self._dims = lists, dims                        # (what `args` holds the addresses of)
-        self._held = (tree_kvs, block_tables, slot_tbls, blk_tbls, hbm_pools, host_kvs)
+        self._held = tuple(tuple(x) for x in (tree_kvs, block_tables, slot_tbls, blk_tbls, hbm_pools, host_kvs))
 
 
 def commit_kv_layers(plan, path, n_commit, seq_len, next_len=None, stream=None):

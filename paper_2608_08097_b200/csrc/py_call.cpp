@@ -9,6 +9,7 @@
 #include <climits>
 #include <initializer_list>
 #include <string>
+#include <vector>
 
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -73,30 +74,33 @@ void of_type(const at::Tensor &t, at::ScalarType type, const char *name)
 }
 
 // Address of a dense tensor of this type and shape on `device`.
-void *dense(PyObject *o, at::ScalarType type, std::initializer_list<int64_t> shape, const char *name, int device)
+void *dense(PyObject *o, at::ScalarType type, at::IntArrayRef want, const char *name, int device)
 {
     const at::Tensor &t = tensor(o, name);
-    const at::IntArrayRef want(shape.begin(), shape.size());
     of_type(t, type, name);
     if (t.sizes() != want) refuse(PyExc_ValueError, std::string(name) + ": expected shape " + text_of(want) + ", got " + text_of(t.sizes()));
     on_device(t, name, device);
     if (!t.is_contiguous()) refuse(PyExc_ValueError, std::string(name) + " must be contiguous");
     return t.data_ptr();
 }
+void *dense(PyObject *o, at::ScalarType type, std::initializer_list<int64_t> shape, const char *name, int device)
+{
+    return dense(o, type, at::IntArrayRef(shape.begin(), shape.size()), name, device);
+}
 void *dense_or_null(PyObject *o, at::ScalarType type, std::initializer_list<int64_t> shape, const char *name, int device)
 {
     return o == Py_None ? nullptr : dense(o, type, shape, name, device);
 }
 
-// Address of a pool of entries [..][2][16][128] in device memory.
-void *pool(PyObject *o, const char *name, int device)
+// Address of a pool of entries [..][2][16][128] in device memory (or, `host_ok`, in pinned host memory).
+void *pool(PyObject *o, const char *name, int device, bool host_ok = false)
 {
     const at::Tensor &t = tensor(o, name);
     of_type(t, at::kBFloat16, name);
     const int64_t n = t.dim();
     if (n < 3 || t.size(n - 3) != 2 || t.size(n - 2) != 16 || t.size(n - 1) != 128 || !t.is_contiguous())
         refuse(PyExc_ValueError, std::string(name) + " must be a contiguous pool of [2][16][128] entries");
-    on_device(t, name, device);
+    if (!(host_ok && t.is_cpu() && t.is_pinned())) on_device(t, name, device, host_ok ? " or in pinned host memory" : "");
     return t.data_ptr();
 }
 
@@ -167,6 +171,30 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         g_verify_tree = address<decltype(g_verify_tree)>(a[1]);
         g_commit_kv_layers = address<decltype(g_commit_kv_layers)>(a[2]);
         Py_RETURN_NONE;
+    });
+}
+
+// addresses(tensors, kind, shape, name): the addresses of a list of tensors, one pointer after the other.  Kind 0: dense bf16 of
+// this shape, 1: dense int32 of this shape, 2: pools of entries in device memory, 3: the same or in pinned host memory, or None.
+PyObject *addresses(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        takes(n, 4);
+        if (!PyList_Check(a[0]) || !PyTuple_Check(a[2])) refuse(PyExc_TypeError, "addresses: expected a list and a tuple");
+        const int64_t kind = integer(a[1]);
+        std::vector<int64_t> shape;
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[2]); ++i) shape.push_back(integer(PyTuple_GET_ITEM(a[2], i)));
+        const char *name = PyUnicode_AsUTF8(a[3]);
+        if (!name) throw Raised{};
+        const int device = c10::cuda::current_device();
+        std::vector<const void *> got;
+        for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[0]); ++i) {
+            PyObject *t = PyList_GET_ITEM(a[0], i);
+            if (kind == 3 && t == Py_None) got.push_back(nullptr);
+            else if (kind >= 2) got.push_back(pool(t, name, device, kind == 3));
+            else got.push_back(dense(t, kind == 0 ? at::kBFloat16 : at::kInt, at::IntArrayRef(shape), name, device));
+        }
+        return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(got.data()), (Py_ssize_t)(got.size() * sizeof(void *)));
     });
 }
 
@@ -288,6 +316,7 @@ PyObject *commit_kv_layers(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
+    {"addresses", (PyCFunction)(void (*)(void))addresses, METH_FASTCALL, nullptr},
     {"tree_attn", (PyCFunction)(void (*)(void))tree_attn, METH_FASTCALL, nullptr},
     {"verify_tree", (PyCFunction)(void (*)(void))verify_tree, METH_FASTCALL, nullptr},
     {"commit_kv_layers", (PyCFunction)(void (*)(void))commit_kv_layers, METH_FASTCALL, nullptr},

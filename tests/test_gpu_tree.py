@@ -498,7 +498,10 @@ def test_wrong_tensors_are_refused(L):
                            ("slot_tbls", cols.long(), TypeError), ("hbm_pools", pool[:, :, :8], ValueError), ("host_kvs", host, ValueError)):
         with pytest.raises(err):
             L.CommitPlan(**{**plan, name: [bad]})
-    plan = L.CommitPlan(**plan)
+    layers = [kv]
+    plan = L.CommitPlan(**{**plan, "tree_kvs": layers})
+    layers.clear()                                                    # (the plan holds the tensors, not the list)
+    assert plan._held[0][0] is kv
     good = dict(path=z, n_commit=n, seq_len=n.clone(), next_len=n.clone())
     for name, bad, err in (("path", z[0], ValueError), ("path", z.float(), TypeError), ("n_commit", n.cpu(), ValueError), ("seq_len", n.repeat(2), ValueError),
                            ("next_len", n.long(), TypeError)):
