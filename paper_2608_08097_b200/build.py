@@ -51,10 +51,12 @@ def _build_call(force=False):
     cuda = os.path.dirname(os.path.dirname(NVCC))
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-I" + sysconfig.get_paths()["include"]]
     cmd += ["-I" + os.path.join(d, "include") for d in (torch, cuda)] + ["-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include")]
-    cmd += [src, "-o", CALL, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    part = "%s.%d" % (CALL, os.getpid())                             # (another process may be loading the old one)
+    cmd += [src, "-o", part, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("g++ failed for %s:\n%s\n%s" % (src, r.stdout, r.stderr))
+    os.replace(part, CALL)
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
