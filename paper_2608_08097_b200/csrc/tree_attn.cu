@@ -663,7 +663,7 @@ static TreePlan tree_plan(const oasis_dims_t *dims, int T, int n_cols)
     if (s > most) s = most;
     if (s < 1) s = 1;
     // The splits of a row are a cluster of two, three, four or eight thread blocks, which merges them through distributed shared
-    // memory, where as many clusters as are needed run at once, a coarser split costs no more than kMergeTiles tiles of four
+    // memory, where as many clusters as are needed run at once, a coarser split costs no more than a few tiles of four
     // columns against the finest one, and the rows are few or the blocks many; else the partials go through the workspace and a
     // second launch.  In a graph, 32 query and 8 KV heads, 5 / 16 / 64 nodes, cluster against workspace:
     //   1 request  x  18 columns   8.4 / 10.7 / 16.5   9.4 /  9.6 / 12.9 us   (the second launch spreads over idle SMs)
@@ -671,11 +671,13 @@ static TreePlan tree_plan(const oasis_dims_t *dims, int T, int n_cols)
     //   5 requests x  62 columns  12.2 / 13.2 / 21.7  13.4 / 13.4 / 23.5 us
     //   8 requests x 130 columns, 32 nodes      22.1                25.9 us
     // Launched one by one, the cluster also saves the host 2 us a call.  Clusters of five (2 x 35 columns, 64 nodes) take 20 us
-    // against 15.6; three tiles more cost 2.5 us (24.7 against 22.2: seven requests of 302 columns, four instead of five splits).
-    constexpr long long kMergeTiles = 1;
+    // against 15.6.  A tile more takes 0.5 us, with two MMAs per tile 1 us, and the second launch 2 to 3: seven ragged requests
+    // of 302 columns in fours instead of five splits (three tiles more) 21.3 against 22.3, 3 x 130 columns in fours instead of six
+    // (three more) 12.7 / 14.2 / 23.4 against 13.7 / 14.7 / 23.1.
+    const long long more_tiles = pl.group_rows <= 128 ? 4 : 2;
     long long c = s >= kTrMaxCluster ? kTrMaxCluster : s < 4 ? s : 4;
     while (c > 1 && clusters_at_once((int)c) < items) c = c == kTrMaxCluster ? 4 : c - 1;
-    pl.in_cluster = c > 1 && n_cols / (4 * c) <= n_cols / (4 * s) + kMergeTiles && (pl.group_rows <= 32 || 2 * items * c >= sm_count());
+    pl.in_cluster = c > 1 && n_cols / (4 * c) <= n_cols / (4 * s) + more_tiles && (pl.group_rows <= 32 || 2 * items * c >= sm_count());
     if (pl.in_cluster) s = c;
     pl.cols_per_split = (int)((n_cols + s - 1) / s);
     pl.n_splits = (n_cols + pl.cols_per_split - 1) / pl.cols_per_split;
