@@ -14,13 +14,13 @@
 //      number's place in the running sum is scanned once more, in index order.  fp64, because a vocabulary of 150,000 has
 //      as many borders between tokens: sums in fp32 would put a noticeable share of the draws into the neighbour's interval.
 // All sums have a fixed order, so a result does not depend on timing.
-// What bounds it: the latency of the serial steps, not bytes.  16 requests, 64-node trees, 151,936 bf16 logits: 28.6 us, of
+// What bounds it: the latency of the serial steps, not bytes.  16 requests, 64-node trees, 151,936 bf16 logits: 28.1 us, of
 // which (cycles) start 4,500, each node 9,000 (copy 2,000, fp32 pass 2,900, exchange 1,300, decision 2,700), the fp64 pass
 // 9,800, the search 1,700.  One request, greedy, 32,000 logits: 7.9 us.  16 requests, chains of 5 with draft distributions,
-// 128,256 fp32 logits: 41.9 us.  128 requests, 6 nodes, 50,257 fp16 logits: 31.1 us.  (In a graph.  The launch may overlap the
-// end of the previous kernel, which it waits for before it reads any input: that saves 1.3 to 2.1 us a call where calls are
-// launched one by one, and costs the chains 1.4 us in a graph.)  No launch_dependents here: a successor that starts early
-// could then overtake the kernel in front.
+// 128,256 fp32 logits: 39.7 us.  128 requests, 6 nodes, 50,257 fp16 logits: 31.2 us.  (In a graph.  The launch may overlap the
+// end of the previous kernel, which it waits for before it reads any input: that saves 1.5 to 2.4 us a call where calls are
+// launched one by one.)  No launch_dependents here: it gains 0.5 to 1 us for one request and for 128 and costs the chains 3 us,
+// whose successors' thread blocks then take the places beside theirs.
 #include <math_constants.h>
 
 #include "common.cuh"
@@ -327,7 +327,8 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
         n_chunks = (per_warp + cap - 1) / cap;         // the same for all warps
         row.stage(v0 + lane, min(v0 + cap, v1), my_row);
     };
-    // What needs no input may run before the previous kernel in the stream has ended: the table of the weights, the barriers.
+    // What needs no input may run before the previous kernel in the stream has ended: the table of the weights, the barriers
+    // (the cluster's own barrier comes later, beside the first row's copy: in front of it it would cost the chains 2.2 us).
     for (int i = 2 * tid; i < kExpTable; i += 2 * THREADS)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(s_table + i)), "l"(g_exp_table.v + i) : "memory");
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -336,7 +337,6 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
         mbar_init(smem_u32(&s_bar[1]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (C > 1) cluster_sync();                         // the barriers of all blocks are there
     asm volatile("griddepcontrol.wait;" ::: "memory");
     enter(0);                                          // node 0's row is needed in any case
     const int n = max(0, min(p.n_nodes[b], p.T));
@@ -370,7 +370,8 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
         ctl.ahead = n > 1 ? 1 : -1;
         ctl.d.c = kExpSteps * 1.4426950408889634 * (sampled ? fmax(1.0 / (double)temp, 1e-300) : 0.0);
     }
-    __syncthreads();
+    if (C > 1) cluster_sync();                         // the barriers of all blocks are there
+    else __syncthreads();
 
     int turn = 0;                                      // exchanges so far
     int n_path = 1, next = -1;
