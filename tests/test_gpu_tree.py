@@ -462,6 +462,70 @@ def test_a_commit_past_the_last_block_is_skipped(L):
     assert torch.equal(pool[[3, 7]][:, :, 12:], tree[0, :4].permute(1, 2, 0, 3))
 
 
+def test_attention_verification_and_commit_in_one_graph(L):
+    """Three steps of a loop whose lengths move on the device, replayed from one graph, against the same calls made one by one:
+    the kernels overlap each other's ends in either case, and every one has to see what those before it wrote."""
+    B, Hq, Hkv, T, V, M, layers, mb, cols = 4, 16, 2, 9, 700, 6, 2, 16, 10
+    g, rng = gen(50), np.random.default_rng(50)
+    dims, lens = L.Dims(B, Hq, Hkv, mb), [30, 16, 0, 47]
+    slot = i32(np.arange(B * Hkv * cols).reshape(B, Hkv, cols).tolist())
+    table = i32(rng.permutation(B * mb).reshape(B, mb).tolist())
+    q, tree_kv = [randn(g, B, T, Hq, 128) for _ in range(3)], [[randn(g, B, T, Hkv, 2, 128) for _ in range(layers)] for _ in range(3)]
+    logits, uniforms = torch.randn((3, B, T, V), generator=g, device="cuda"), torch.rand((3, B, T), generator=g, device="cuda") * 0.02
+    temperature, parent, nodes = torch.tensor([0.0, 0.4, 0.7, 1.0], device="cuda"), i32(random_tree(rng, B, T).tolist()), i32([T, 1, T, 5])
+    tokens = torch.gather(logits.argmax(-1), 2, parent.long().clamp(min=0).expand(3, B, T)).to(torch.int32)
+    init = [(randn(gen(60 + l), B * Hkv * cols, 2, 16, 128), randn(gen(70 + l), B * mb * Hkv, 2, 16, 128)) for l in range(layers)]
+    blk0 = torch.full((B, Hkv, cols), -1, dtype=torch.int32, device="cuda")
+    for b, n in enumerate(lens):
+        for j in range((n + 15) // 16):
+            blk0[b, :, 8 + (j & 1) if j >= n // 16 - 1 else j] = j
+
+    class State:
+        def __init__(self):
+            self.blk = [blk0.clone() for _ in range(layers)]
+            self.pools, self.kvs = [p.clone() for p, _ in init], [k.clone() for _, k in init]
+            self.len, self.next = i32(lens), i32([0] * B)
+            self.q, self.kv = q[0].clone(), [t.clone() for t in tree_kv[0]]
+            self.x, self.u, self.tok = logits[0].clone(), uniforms[0].clone(), tokens[0].clone()
+            self.out = [torch.zeros((B, T, Hq, 128), dtype=torch.bfloat16, device="cuda") for _ in range(layers)]
+            self.path, self.n, self.token = i32([[0] * M] * B), i32([0] * B), i32([0] * B)
+            self.ws = torch.empty(max(16, L.tree_attn_workspace_bytes(dims, T, cols)), dtype=torch.uint8, device="cuda")
+            self.plan = L.CommitPlan(dims, self.kv, [table] * layers, [slot] * layers, self.blk, 8, self.pools, self.kvs)
+
+        def load(self, k):
+            for mine, new in zip((self.q, self.x, self.u, self.tok, *self.kv), (q[k], logits[k], uniforms[k], tokens[k], *tree_kv[k])):
+                mine.copy_(new)
+
+        def step(self):
+            for l in range(layers):
+                L.tree_attn(dims, self.q, self.kv[l], parent, nodes, self.pools[l], slot, self.blk[l], self.len, SCALE, self.out[l], workspace=self.ws)
+            L.verify_tree(self.x, self.tok, parent, nodes, self.u, temperature, self.path, self.n, self.token)
+            L.commit_kv_layers(self.plan, self.path, self.n, self.len, next_len=self.next)
+            self.len.copy_(self.next)
+
+        def all(self):
+            return [*self.out, *self.pools, *self.kvs, *self.blk, self.len, self.path, self.n, self.token]
+
+    eager, other = State(), State()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other.step()
+    moved = 0
+    for k in range(3):
+        eager.load(k)
+        other.load(k)
+        torch.cuda.synchronize()
+        eager.step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager.all(), other.all())), k
+        ref = ot.verify_tree(f64(logits[k]), tokens[k].cpu().numpy(), parent.cpu().numpy(), nodes.tolist(), uniforms[k].cpu().numpy(), temperature.cpu().numpy(), M)
+        assert all(np.array_equal(a.cpu().numpy(), r) for a, r in zip((eager.path, eager.n, eager.token), ref))
+        moved += int(eager.n.sum())
+    assert eager.len.tolist() != lens and moved == sum(eager.len.tolist()) - sum(lens)
+
+
 # ---- what the Python layer refuses ---------------------------------------------------------------------------------
 def test_wrong_tensors_are_refused(L):
     c = AttnCase(L, 1, 4, 2, 3, [20], [3], 4, seed=30)
