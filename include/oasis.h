@@ -399,6 +399,20 @@ int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t n_tree, con
 /* Scratch bytes oasis_tree_attn needs for these shapes on the current device. */
 size_t oasis_tree_attn_workspace_bytes(const oasis_dims_t *dims, int32_t n_tree, int32_t n_cols);
 
+/*
+ * Step 1 for draft trees: oasis_score_blocks with the queries of each request's own drafts.  With n = n_nodes[b] (taken into
+ * [0, n_tree]) the scores of request b come from the rows of nodes 1 .. n - 1, of node 0 if n is 1; at most the first
+ * 128 / (Hq/Hkv) drafts take part, the columns of one contraction.  Rows of padding nodes are not read.  A request without
+ * nodes has no candidates: its scores are -inf.
+ *   q             [B][n_tree][Hq][128] bf16, the tree's queries (as for oasis_tree_attn)
+ *   n_full_blocks, reduce_mode, scores, summaries as in oasis_score_blocks
+ *   n_candidates  optional [B] int32 out: n_full_blocks[b], or 0 for a request without nodes -- what oasis_select_topk takes as
+ *                 n_full_blocks so that such a request selects nothing
+ */
+int oasis_score_tree(const oasis_dims_t *dims, const void *q, int32_t n_tree, const int32_t *n_nodes,
+                     const void *summaries, const int32_t *n_full_blocks, int32_t reduce_mode, float *scores,
+                     int32_t *n_candidates, void *stream);
+
 typedef enum { OASIS_F32 = 0, OASIS_BF16 = 1, OASIS_F16 = 2 } oasis_dtype_t;
 
 /*

@@ -26,7 +26,7 @@ SYMBOLS = ("oasis_build_summaries", "oasis_score_blocks", "oasis_select_topk",
            "oasis_build_summaries_layers", "oasis_selftest_wait_timeout",
            "oasis_local_window", "oasis_append_kv", "oasis_append_kv_layers", "oasis_stage_blocks_layers", "oasis_stage_blocks_bulk",
            "oasis_set_extents", "oasis_bounds_checked",
-           "oasis_tree_attn", "oasis_tree_attn_workspace_bytes", "oasis_verify_tree", "oasis_commit_kv", "oasis_commit_kv_layers")
+           "oasis_score_tree", "oasis_tree_attn", "oasis_tree_attn_workspace_bytes", "oasis_verify_tree", "oasis_commit_kv", "oasis_commit_kv_layers")
 
 
 class OasisError(RuntimeError):
@@ -111,6 +111,8 @@ def lib():
         L.oasis_set_extents.restype = ctypes.c_int
         L.oasis_bounds_checked.argtypes = []
         L.oasis_bounds_checked.restype = ctypes.c_int
+        L.oasis_score_tree.argtypes = [dp, vp, i32, vp, vp, vp, i32, vp, vp, vp]
+        L.oasis_score_tree.restype = ctypes.c_int
         L.oasis_tree_attn.argtypes = [dp, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, f32, vp, vp, vp, sz, vp]
         L.oasis_tree_attn.restype = ctypes.c_int
         L.oasis_tree_attn_workspace_bytes.argtypes = [dp, i32, i32]
@@ -465,6 +467,28 @@ def tree_attn(dims, q, tree_kv, parent, n_nodes, hbm_pool, slot_tbl, blk_tbl, se
                                        out, lse, workspace, None if stream is None else _handle(stream))
     if rc:
         _check(rc, "oasis_tree_attn")
+
+
+def score_tree(dims, q, n_nodes, summaries, n_full_blocks, scores, reduce_mode=REDUCE_MAX, n_candidates=None, stream=None):
+    """Block scores from the drafts of each request's tree (nodes 1 .. n_nodes[b] - 1, or node 0 where there is no other; at most
+    the first 128 // group of them).  q [B][T][Hq][128]: rows of padding nodes are not read.  n_candidates [B] int32 receives
+    n_full_blocks, or 0 for requests without nodes."""
+    if q.dim() != 4:
+        raise ValueError("q: expected shape [B][T][Hq][128], got %s" % (tuple(q.shape),))
+    B, Hkv, mb, device = dims.batch, dims.n_kv_heads, dims.max_blocks, torch.cuda.current_device()
+    for name, t, shape in (("q", q, (B, q.shape[1], dims.n_q_heads, 128)), ("n_nodes", n_nodes, (B,)), ("n_full_blocks", n_full_blocks, (B,)),
+                           ("summaries", summaries, (B, Hkv, mb, 2, 128)), ("scores", scores, (B, Hkv, mb)), ("n_candidates", n_candidates, (B,))):
+        if t is None and name == "n_candidates":
+            continue
+        if tuple(t.shape) != shape:
+            raise ValueError("%s: expected shape %s, got %s" % (name, shape, tuple(t.shape)))
+        if not t.is_cuda or t.get_device() != device:
+            raise ValueError("%s must be on the current CUDA device" % name)
+    d = dims.c()
+    _check(lib().oasis_score_tree(
+        ctypes.byref(d), _ptr(q, torch.bfloat16, "q"), int(q.shape[1]), _ptr(n_nodes, torch.int32, "n_nodes"),
+        _ptr(summaries, torch.bfloat16, "summaries"), _ptr(n_full_blocks, torch.int32, "n_full_blocks"), int(reduce_mode),
+        _ptr(scores, torch.float32, "scores"), _ptr(n_candidates, torch.int32, "n_candidates"), _stream(stream)), "oasis_score_tree")
 
 
 def verify_tree(logits, tokens, parent, n_nodes, uniforms, temperature, path, n_commit, next_token, draft_probs=None,

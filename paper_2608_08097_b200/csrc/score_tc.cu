@@ -47,8 +47,14 @@ struct ScoreTcParams {
     int32_t *err;
     int Hq, Hkv, G, R, N, max_blocks, tiles_per_bh, reduce_sum, stages, tmem_cols, n_bbuf;
     long long total_tiles;
+    const int32_t *n_nodes;       // draft trees: live nodes of each request's q, which starts at node 0
+    int32_t *n_candidates;        // draft trees, optional: n_full of the requests that have nodes, else 0
+    int B, T;
 };
 
+// TREE: the query rows are those of a request's live drafts, nodes 1 to n_nodes - 1 (of a request with one node: that node's), as
+// far as R goes; padding nodes are not read, and a request without nodes has no candidates.
+template <bool TREE>
 __global__ void __launch_bounds__(kTcThreads, 1)
 score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreTcParams p)
 {
@@ -72,6 +78,9 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreTcParams p)
 
     const long long t0 = p.total_tiles * blockIdx.x / gridDim.x;
     const long long t1 = p.total_tiles * (blockIdx.x + 1) / gridDim.x;
+    auto n_full = [&](int b) { return TREE && p.n_nodes[b] <= 0 ? 0 : p.n_full[b]; };
+    if (TREE && p.n_candidates && blockIdx.x == 0)
+        for (int b = tid; b < p.B; b += kTcThreads) p.n_candidates[b] = n_full(b);
 
     // First tile at or after t (and before t1) that has candidate blocks; t1 if there is none.
     auto next_active = [&](long long t) {
@@ -79,7 +88,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreTcParams p)
         for (; t < t1; ++t) {
             const long long bh = t / p.tiles_per_bh;
             const int j0 = (int)(t % p.tiles_per_bh) * kTileBlocks;
-            if (j0 < p.n_full[(int)(bh / p.Hkv)]) break;
+            if (j0 < n_full((int)(bh / p.Hkv))) break;
         }
         return t;
     };
@@ -87,8 +96,10 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreTcParams p)
     // lives in sub-tile k / 64.  `nthr` threads (index `me`) share the work; loads are issued
     // eight at a time so their latencies overlap.
     auto build_b = [&](long long bh, int buf, int me, int nthr) {
-        build_qpm_operand(b_ptr + (size_t)buf * b_bytes, p.q, p.q_batch_stride, (int)(bh / p.Hkv), (int)(bh % p.Hkv), p.R, p.G, p.Hq,
-                          p.N, p.reduce_sum, me, nthr);
+        const int b = (int)(bh / p.Hkv), live = TREE ? min(p.n_nodes[b], p.T) : 0;
+        const int R = TREE ? min(max(live - 1, 1) * p.G, p.R) : p.R;
+        const uint8_t *q = TREE && live > 1 ? p.q + (size_t)p.Hq * kRowBytes : p.q;
+        build_qpm_operand(b_ptr + (size_t)buf * b_bytes, q, p.q_batch_stride, b, (int)(bh % p.Hkv), R, p.G, p.Hq, p.N, p.reduce_sum, me, nthr);
     };
 
     if (tid == 0) {
@@ -155,7 +166,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreTcParams p)
                 const long long bh = t / p.tiles_per_bh;
                 const int j0 = (int)(t % p.tiles_per_bh) * kTileBlocks;
                 const int b = (int)(bh / p.Hkv);
-                if (j0 >= p.n_full[b]) continue;
+                if (j0 >= n_full(b)) continue;
                 if (bh != cur_bh) {
                     if (bo >= 0) tc_commit(bar_b_empty(bo % p.n_bbuf));   // earlier MMAs no longer read that operand
                     cur_bh = bh;
@@ -164,7 +175,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreTcParams p)
                     if (!alive) break;
                 }
                 const int acc = it & 1, s = it % p.stages;
-alive = mbar_wait_warp2(bar_acc_empty(acc), ((it >> 1) & 1) ^ 1, bar_full(s), (it / p.stages) & 1, p.err, 23);
+                alive = mbar_wait_warp2(bar_acc_empty(acc), ((it >> 1) & 1) ^ 1, bar_full(s), (it / p.stages) & 1, p.err, 23);
                 if (!alive) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + (uint32_t)(acc * p.N);
@@ -207,7 +218,7 @@ alive = mbar_wait_warp2(bar_acc_empty(acc), ((it >> 1) & 1) ^ 1, bar_full(s), (i
             const long long bh = t / p.tiles_per_bh;
             const int j0 = (int)(t % p.tiles_per_bh) * kTileBlocks;
             const int b = (int)(bh / p.Hkv);
-            const int nf = p.n_full[b];
+            const int nf = n_full(b);
             if (kBoundsCheck && lane == 0 && nf > p.max_blocks) in_range(nf, p.max_blocks + 1, Bounds{0, 0, p.err}, kErrBlockCount);
             const int j = j0 + quarter * 32 + lane;
             float *out = p.scores + bh * p.max_blocks;
@@ -242,10 +253,11 @@ alive = mbar_wait_warp2(bar_acc_empty(acc), ((it >> 1) & 1) ^ 1, bar_full(s), (i
 
 int score_blocks_tc(const oasis_dims_t *dims, const void *q_draft, int64_t q_batch_stride, int32_t n_draft,
                     const void *summaries, const int32_t *n_full_blocks, int32_t reduce_mode, float *scores,
-                    int32_t *err_word, cudaStream_t st)
+                    int32_t *err_word, cudaStream_t st, const int32_t *n_nodes, int32_t *n_candidates)
 {
+    const char *who = n_nodes ? "oasis_score_tree" : "oasis_score_blocks";
     EncodeTiledFn encode = encode_tiled_fn();
-    if (!encode) return fail(OASIS_ERR_CUDA, "oasis_score_blocks: cuTensorMapEncodeTiled is not available");
+    if (!encode) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available", who);
     const int G = dims->n_q_heads / dims->n_kv_heads;
     const int R = n_draft * G;
     const int N = (R + 15) / 16 * 16;
@@ -259,12 +271,14 @@ int score_blocks_tc(const oasis_dims_t *dims, const void *q_draft, int64_t q_bat
     CUresult cr = encode(&tmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(summaries), gdim, gstride, box,
                          estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (cr != CUDA_SUCCESS) return fail(OASIS_ERR_CUDA, "oasis_score_blocks: cuTensorMapEncodeTiled failed (%d)", (int)cr);
+    if (cr != CUDA_SUCCESS) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed (%d)", who, (int)cr);
 
     ScoreTcParams p;
     p.q = (const uint8_t *)q_draft;
     p.q_batch_stride = q_batch_stride;
     p.n_full = n_full_blocks;
+    p.n_nodes = n_nodes; p.n_candidates = n_candidates; p.B = dims->batch;
+    p.T = n_nodes ? (int)(q_batch_stride / ((int64_t)dims->n_q_heads * kHeadDim)) : 0;
     p.scores = scores;
     p.err = err_word;
     p.Hq = dims->n_q_heads; p.Hkv = dims->n_kv_heads; p.G = G; p.R = R; p.N = N;
@@ -278,12 +292,13 @@ int score_blocks_tc(const oasis_dims_t *dims, const void *q_draft, int64_t q_bat
     p.tmem_cols = cols;
     p.total_tiles = (long long)dims->batch * dims->n_kv_heads * p.tiles_per_bh;
     const size_t smem = 1024 + (size_t)p.stages * kATileBytes + (size_t)p.n_bbuf * N * kSummaryBytes + 256;
-    cudaError_t e = cudaFuncSetAttribute(score_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return fail(OASIS_ERR_CUDA, "oasis_score_blocks: shared memory %zu B: %s", smem, cudaGetErrorString(e));
-    prefer_max_shared_carveout(score_tc_kernel);
+    const auto kernel = n_nodes ? score_tc_kernel<true> : score_tc_kernel<false>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return fail(OASIS_ERR_CUDA, "%s: shared memory %zu B: %s", who, smem, cudaGetErrorString(e));
+    prefer_max_shared_carveout(kernel);
     long long grid = p.total_tiles < sm_count() ? p.total_tiles : sm_count();
-    score_tc_kernel<<<(unsigned)grid, kTcThreads, smem, st>>>(tmap, p);
-    return check_launch("oasis_score_blocks");
+    kernel<<<(unsigned)grid, kTcThreads, smem, st>>>(tmap, p);
+    return check_launch(who);
 }
 
 }  // namespace oasis

@@ -43,19 +43,25 @@ class DecodeLayer:
         ws = (oasis.tree_attn_workspace_bytes if tree else oasis.attn_workspace_bytes)(self.dims, n_q_tokens, self.cols)
         self.workspace = torch.empty((max(ws, 16),), dtype=torch.uint8, device=dev)
         self.scale = 1.0 / math.sqrt(128.0)
+        if self.tree:
+            self.all_nodes = torch.full((batch,), n_q_tokens, dtype=torch.int32, device=dev)
+            self.n_cand = torch.zeros((batch,), dtype=torch.int32, device=dev)     # blocks that the latest selection was made among
 
     # step 0
     def build_summaries(self, kv_pool, block_table, first_block, n_blocks, max_new_blocks, stream=None):
         oasis.build_summaries(self.dims, kv_pool, block_table, first_block, n_blocks, max_new_blocks,
                               self.summaries, stream=stream)
 
-    # step 1: the draft tokens are rows 1..T-1 of the stacked verify-step queries
-    def score(self, q, n_full, reduce_mode=oasis.REDUCE_MAX, stream=None):
-        n_draft = self.T - 1
+    # step 1: the draft tokens are rows 1..T-1 of the stacked verify-step queries; of a tree, those of them that are nodes
+    def score(self, q, n_full, reduce_mode=oasis.REDUCE_MAX, stream=None, n_nodes=None):
+        """Layers made with tree=True: n_nodes [B] int32 (None: n_q_tokens nodes each) tells which rows are drafts; at most
+        the first 128 // (Hq // Hkv) of them score, and `n_cand` receives the number of candidates (none without nodes)."""
         if self.tree:
-            n_draft = min(n_draft, 128 // (self.Hq // self.Hkv))     # a wide tree: its first drafts (at most 128 rows score)
+            oasis.score_tree(self.dims, q, self.all_nodes if n_nodes is None else n_nodes, self.summaries, n_full, self.scores,
+                             reduce_mode=reduce_mode, n_candidates=self.n_cand, stream=stream)
+            return
         q_draft = q[:, 1:]
-        oasis.score_blocks(self.dims, q_draft, n_draft, self.summaries, n_full, self.scores,
+        oasis.score_blocks(self.dims, q_draft, self.T - 1, self.summaries, n_full, self.scores,
                            reduce_mode=reduce_mode, q_batch_stride=self.T * self.Hq * 128, stream=stream)
 
     def score_queries(self, q_rows, n_full, reduce_mode=oasis.REDUCE_MAX, stream=None):
@@ -239,7 +245,7 @@ class DecodeEngine:
         return ev
 
     def _predict(self, l, q, first_block, n_new, max_new, n_full_next, seq_next, stamp, timers,
-                 attn_done=None, plan=None, scored=None, n_local=2, sel_log=None):
+                 attn_done=None, plan=None, scored=None, n_local=2, sel_log=None, n_nodes=None):
         """Prediction chain of one layer; returns the event after which the layer's gather may start.
         `scored`: the scores were already produced (by the fused launch) and this event marks them."""
         L, ps, qs = self.layers[l], self.pred, self.selq
@@ -251,7 +257,7 @@ class DecodeEngine:
                     ps.wait_event(self.sel_done[l])
                 L.build_summaries(self.kv[l], self.table[l], first_block, n_new, max_new)
                 t0 = self._tick(timers, "score", ps)
-                L.score(q, n_full_next)
+                L.score(q, n_full_next, n_nodes=n_nodes)
                 self._tock(timers, "score", t0, ps)
                 scored = self._event(ps)
                 self.score_done[l] = scored
@@ -262,7 +268,7 @@ class DecodeEngine:
             if attn_done is not None:
                 qs.wait_event(attn_done)            # sel / resident are read by this step's attention
             t0 = self._tick(timers, "select", qs)
-            L.select(n_full_next, seq_next, self.table[l])
+            L.select(L.n_cand if self.tree else n_full_next, seq_next, self.table[l])
             self._tock(timers, "select", t0, qs)
             if sel_log is not None:
                 sel_log.copy_(L.sel, non_blocking=True)  # a record of this step's selection (tests, analysis)
@@ -327,11 +333,11 @@ class DecodeEngine:
                                  self.kv[layer], None)
         self.launches += 2
 
-    def prime(self, q_list, n_full_next, seq_next, step_stamp=0, summaries_ready=False):
+    def prime(self, q_list, n_full_next, seq_next, step_stamp=0, summaries_ready=False, n_nodes=None):
         """Before the first step: build every summary (unless the hand-over already did) and run one
         prediction + transfer per layer, as the step before the first one would have done.  With the KV
         append the (partially filled) local block is loaded from the full-KV pool into the local window
-        once, here."""
+        once, here.  n_nodes (engines built with tree=True): the rows of q_list that are nodes, as in `step`; None: all."""
         B = self.layers[0].B
         zeros = torch.zeros(B, dtype=torch.int32, device=self.device)
         n_build = zeros if summaries_ready else n_full_next
@@ -345,7 +351,7 @@ class DecodeEngine:
         for l in range(self.n_layers):
             L = self.layers[l]
             ready = self._predict(l, q_list[l], zeros, n_build, L.mb, n_full_next, seq_next,
-                                  step_stamp, None, plan=plan, n_local=n_local)
+                                  step_stamp, None, plan=plan, n_local=n_local, n_nodes=n_nodes)
             self._transfer([l], [ready], None, plan=plan)
             if self.append:
                 with torch.cuda.stream(self.side):
@@ -372,7 +378,9 @@ class DecodeEngine:
         layer; engines built with append=True): the step's new keys and values.  sel_log (one tensor like
         `layers[l].sel` per layer): receives a copy of each layer's selection of this step.  tree (engines built with
         tree=True): (parent, n_nodes) of the step's draft trees; new_kv then holds the nodes' keys and values, and
-        `commit` follows the step."""
+        `commit` follows the step.  The next working set is predicted from a request's drafts (its first 128 // group of
+        them; node 0 where it has none); rows of padding nodes take no part, and a request without nodes selects nothing: its
+        working set stays."""
         ms, n = self.main, self.n_layers
         if self.tree != (tree is not None):
             raise ValueError("tree must be given exactly when the engine was built with tree=True")
@@ -467,7 +475,8 @@ class DecodeEngine:
                 self.pred.wait_event(q_ready[l])
             ready = self._predict(l, q_list[l], first_block, n_new, 1, n_full_next, seq_next, step_stamp, timers,
                                   attn_done=attn_done, scored=attn_done if self.fused else None,
-                                  n_local=0 if self.append else 2, sel_log=None if sel_log is None else sel_log[l])
+                                  n_local=0 if self.append else 2, sel_log=None if sel_log is None else sel_log[l],
+                                  n_nodes=tree[1] if self.tree else None)
             pending.append(l)
             readies.append(ready)
             if len(pending) == self.transfer_group or l == n - 1:

@@ -1,0 +1,30 @@
+"""CPU checks of the draft-tree calls: refusals made on the host, lifetimes and the build."""
+import ctypes
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2608_08097_b200 import binding, build
+    build.build()
+    return binding
+
+
+ONE, ODD = 4096, 4104          # never dereferenced on the host; the second one is not 16-byte aligned
+
+
+def test_refusals_of_the_tree_scoring(L):
+    lib = L.lib()
+
+    def call(dims=L.Dims(2, 32, 8, 64), q=ONE, T=5, nodes=ONE, summ=ONE, n_full=ONE, mode=0, scores=ONE, cand=None):
+        d = dims.c()
+        return lib.oasis_score_tree(ctypes.byref(d), q, T, nodes, summ, n_full, mode, scores, cand, None)
+
+    for name in ("q", "nodes", "summ", "n_full", "scores"):
+        assert call(**{name: None}) == 1, name
+    for bad in (dict(q=ODD), dict(summ=ODD), dict(T=0), dict(T=65), dict(mode=2), dict(mode=-1), dict(dims=L.Dims(2, 30, 8, 64))):
+        assert call(**bad) == 1, bad
+    for bad in (dict(dims=L.Dims(2, 258, 2, 64)), dict(dims=L.Dims(1 << 12, 32, 8, 1 << 17)), dict(dims=L.Dims(2, 32, 8, 64, head_dim=64))):
+        assert call(**bad) == 2, bad
+    assert call(dims=L.Dims(0, 32, 8, 64), q=None) == 0
