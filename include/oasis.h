@@ -457,13 +457,18 @@ int oasis_verify_tree(int32_t batch, int32_t n_tree, int32_t vocab, const void *
  *      kept tokens stay local.  A selection that is made after this step has to leave them out (n_full_blocks = L / 16);
  *      a caller that selects among them as well calls oasis_local_window for the new length first;
  *   3. next_len[b] = L + n (if next_len is not NULL; it may not share memory with seq_len, n_commit or path).
- * Everything else is left as it was: with n = 0 only next_len is written.  A path entry outside [0, n_tree), a position
- * outside the max_blocks of the request and a negative slot are skipped.
+ * Everything else is left as it was: with n = 0 only next_len is written (but see the last entry point).  A path
+ * entry outside [0, n_tree), a position outside the max_blocks of the request and a negative slot are skipped.
  *   path        [B][max_path] int32 (device), 1 <= max_path <= 16;  n_commit, seq_len, next_len [B] int32 (device)
  *   block_table [B][max_blocks], slot_tbl, blk_tbl [B][Hkv][n_cols] int32 (device), local_col + 2 <= n_cols
  *   host_kv     the CPU full-KV pool (mapped pinned memory, or device memory)
  * oasis_commit_kv_layers does the same for n_layers <= OASIS_MAX_APPEND_LAYERS layers in one launch (host arrays of
  * per-layer device pointers): the path is known only after the last layer, so a step commits all layers at once.
+ * oasis_commit_kv_layers_after_select is the commit of a loop that has selected blocks since the last one: n_candidates ([B] int32,
+ * device, or NULL) holds the n_full_blocks of that selection, 0 for a request that none was made for (the n_candidates of
+ * oasis_score_tree).  Where n = 0, i.e. a request's step is thrown away, a local column with a block below n_candidates[b] becomes
+ * -1: the selection may have brought that block in as well, and a block that two columns hold would be attended twice.
+ * (Where n > 0 rule 2 sets both columns anyway.)  next_len may not share memory with n_candidates either.
  */
 int oasis_commit_kv(const oasis_dims_t *dims, const void *tree_kv, int32_t n_tree, const int32_t *path, int32_t max_path,
                     const int32_t *n_commit, const int32_t *seq_len, const int32_t *block_table,
@@ -474,6 +479,12 @@ int oasis_commit_kv_layers(const oasis_dims_t *dims, int32_t n_layers, const voi
                            const int32_t *const *block_tables, const int32_t *const *slot_tbls,
                            int32_t *const *blk_tbls, int32_t n_cols, int32_t local_col, void *const *hbm_pools,
                            void *const *host_kvs, int32_t *next_len, void *stream);
+int oasis_commit_kv_layers_after_select(const oasis_dims_t *dims, int32_t n_layers, const void *const *tree_kvs,
+                                        int32_t n_tree, const int32_t *path, int32_t max_path, const int32_t *n_commit,
+                                        const int32_t *seq_len, const int32_t *const *block_tables,
+                                        const int32_t *const *slot_tbls, int32_t *const *blk_tbls, int32_t n_cols,
+                                        int32_t local_col, void *const *hbm_pools, void *const *host_kvs,
+                                        const int32_t *n_candidates, int32_t *next_len, void *stream);
 
 /*
  * Head-union block set (Sec. 4.4.1, partial transfer: per layer the per-head selected sets are

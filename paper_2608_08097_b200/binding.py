@@ -26,7 +26,8 @@ SYMBOLS = ("oasis_build_summaries", "oasis_score_blocks", "oasis_select_topk",
            "oasis_build_summaries_layers", "oasis_selftest_wait_timeout",
            "oasis_local_window", "oasis_append_kv", "oasis_append_kv_layers", "oasis_stage_blocks_layers", "oasis_stage_blocks_bulk",
            "oasis_set_extents", "oasis_bounds_checked",
-           "oasis_score_tree", "oasis_tree_attn", "oasis_tree_attn_workspace_bytes", "oasis_verify_tree", "oasis_commit_kv", "oasis_commit_kv_layers")
+           "oasis_score_tree", "oasis_tree_attn", "oasis_tree_attn_workspace_bytes", "oasis_verify_tree", "oasis_commit_kv", "oasis_commit_kv_layers",
+           "oasis_commit_kv_layers_after_select")
 
 
 class OasisError(RuntimeError):
@@ -123,6 +124,8 @@ def lib():
         L.oasis_commit_kv.restype = ctypes.c_int
         L.oasis_commit_kv_layers.argtypes = [dp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
         L.oasis_commit_kv_layers.restype = ctypes.c_int
+        L.oasis_commit_kv_layers_after_select.argtypes = [dp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+        L.oasis_commit_kv_layers_after_select.restype = ctypes.c_int
         L.oasis_set_error_word.argtypes = [vp]
         L.oasis_set_error_word.restype = ctypes.c_int
         L.oasis_last_error.restype = ctypes.c_char_p
@@ -434,7 +437,7 @@ def _calls():
             from . import _call as native
         except ImportError as e:
             raise OasisError("_call.so cannot be loaded: build it with `python -m paper_2608_08097_b200.build` (%s)" % e) from e
-        native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.oasis_tree_attn, L.oasis_verify_tree, L.oasis_commit_kv_layers)))
+        native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.oasis_tree_attn, L.oasis_verify_tree, L.oasis_commit_kv_layers_after_select)))
         _call = native
     return _call
 
@@ -527,12 +530,15 @@ class CommitPlan:
         self._held = tuple(tuple(x) for x in (tree_kvs, block_tables, slot_tbls, blk_tbls, hbm_pools, host_kvs))
 
 
-def commit_kv_layers(plan, path, n_commit, seq_len, next_len=None, stream=None):
+def commit_kv_layers(plan, path, n_commit, seq_len, next_len=None, stream=None, n_candidates=None):
     """Writes the kept path [B][max_path] of every request (its first n_commit[b] nodes) from the layers' tree buffers
-    into their local windows and full-KV pools, sets the local columns, and next_len = seq_len + n_commit."""
-    rc = (_call or _calls()).commit_kv_layers(plan.args, path, n_commit, seq_len, next_len, None if stream is None else _handle(stream))
+    into their local windows and full-KV pools, sets the local columns, and next_len = seq_len + n_commit.  n_candidates [B] int32
+    (score_tree's; None: no selection was made since the last commit): where n_commit is 0, local blocks below it, which the
+    selection may have brought in, leave the local columns."""
+    rc = (_call or _calls()).commit_kv_layers(plan.args, path, n_commit, seq_len, next_len, None if stream is None else _handle(stream),
+                                              n_candidates)
     if rc:
-        _check(rc, "oasis_commit_kv_layers")
+        _check(rc, "oasis_commit_kv_layers_after_select")
 
 
 def commit_kv(dims, tree_kv, path, n_commit, seq_len, block_table, slot_tbl, blk_tbl, local_col, hbm_pool, host_kv=None,

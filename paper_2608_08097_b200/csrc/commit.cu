@@ -24,7 +24,7 @@ struct CommitLayers {
 };
 
 struct CommitParams {
-    const int32_t *path, *n_commit, *seq_len;
+    const int32_t *path, *n_commit, *seq_len, *n_candidates;
     int32_t *next_len;
     int B, T, M, Hkv, max_blocks, n_cols, local_col;
 };
@@ -37,10 +37,14 @@ commit_kv_kernel(const __grid_constant__ CommitLayers ly, const CommitParams p, 
     if (row >= (long long)p.B * p.Hkv) return;
     const int b = (int)(row / p.Hkv), h = (int)(row % p.Hkv);
     asm volatile("griddepcontrol.wait;" ::: "memory");              // (the launch may overlap the end of the previous kernel)
-    const int n_raw = p.n_commit[b], L = p.seq_len[b];
+    const int n_raw = p.n_commit[b], L = p.seq_len[b], n_cand = p.n_candidates ? p.n_candidates[b] : 0;
     const int t_mine = lane < p.M ? p.path[b * p.M + lane] : -1;
     const int n = max(0, min(n_raw, p.M));
     if (p.next_len && l == 0 && h == 0 && lane == 0) p.next_len[b] = L + n;
+    if (n == 0 && lane < 2) {                                        // a local block that may have been selected leaves its column
+        int32_t *const col = ly.blk_tbl[l] + row * p.n_cols + p.local_col + lane;
+        if (n_cand > 0 && *col >= 0 && *col < n_cand) *col = -1;
+    }
     if (n == 0 || L < 0) return;
     const int lo = L / kBlock, hi = (L + n - 1) / kBlock;
     // lane 0: block lo, lane 1: the next one; their slot and their entry of the full-KV pool, -1 where there is none
@@ -87,7 +91,8 @@ commit_kv_kernel(const __grid_constant__ CommitLayers ly, const CommitParams p, 
 static int launch_commit(const oasis_dims_t *dims, int n_layers, const void *const *tree_kvs, int T, const int32_t *path,
                          int M, const int32_t *n_commit, const int32_t *seq_len, const int32_t *const *block_tables,
                          const int32_t *const *slot_tbls, int32_t *const *blk_tbls, int n_cols, int local_col,
-                         void *const *pools, void *const *host_kvs, int32_t *next_len, cudaStream_t st, const char *who)
+                         void *const *pools, void *const *host_kvs, const int32_t *n_candidates, int32_t *next_len, cudaStream_t st,
+                         const char *who)
 {
     if (int rc = check_dims(dims)) return rc;
     if (n_layers < 0 || n_layers > OASIS_MAX_APPEND_LAYERS)
@@ -104,8 +109,9 @@ static int launch_commit(const oasis_dims_t *dims, int n_layers, const void *con
         const uintptr_t a = reinterpret_cast<uintptr_t>(next_len), c = reinterpret_cast<uintptr_t>(in);
         return a < c + 4 * (uintptr_t)n && c < a + 4 * (uintptr_t)dims->batch;
     };
-    if (next_len && (overlaps(seq_len, dims->batch) || overlaps(n_commit, dims->batch) || overlaps(path, (long long)dims->batch * M)))
-        return fail(OASIS_ERR_INVALID_ARG, "%s: next_len may not share memory with seq_len, n_commit or path", who);
+    if (next_len && (overlaps(seq_len, dims->batch) || overlaps(n_commit, dims->batch) || overlaps(path, (long long)dims->batch * M) ||
+                     (n_candidates && overlaps(n_candidates, dims->batch))))
+        return fail(OASIS_ERR_INVALID_ARG, "%s: next_len may not share memory with seq_len, n_commit, path or n_candidates", who);
     CommitLayers ly = {};
     for (int l = 0; l < n_layers; ++l) {
         void *host = host_kvs ? host_kvs[l] : nullptr;
@@ -122,7 +128,7 @@ static int launch_commit(const oasis_dims_t *dims, int n_layers, const void *con
     }
     const long long total = (long long)dims->batch * dims->n_kv_heads;
     CommitParams p;
-    p.path = path; p.n_commit = n_commit; p.seq_len = seq_len; p.next_len = next_len;
+    p.path = path; p.n_commit = n_commit; p.seq_len = seq_len; p.next_len = next_len; p.n_candidates = n_candidates;
     p.B = dims->batch; p.T = T; p.M = M; p.Hkv = dims->n_kv_heads; p.max_blocks = dims->max_blocks;
     p.n_cols = n_cols; p.local_col = local_col;
     prefer_max_shared_carveout(commit_kv_kernel);
@@ -151,7 +157,7 @@ extern "C" int oasis_commit_kv(const oasis_dims_t *dims, const void *tree_kv, in
                                int32_t local_col, void *hbm_pool, void *host_kv, int32_t *next_len, void *stream)
 {
     return oasis::launch_commit(dims, 1, &tree_kv, n_tree, path, max_path, n_commit, seq_len, &block_table, &slot_tbl, &blk_tbl,
-                                n_cols, local_col, &hbm_pool, &host_kv, next_len, (cudaStream_t)stream, "oasis_commit_kv");
+                                n_cols, local_col, &hbm_pool, &host_kv, nullptr, next_len, (cudaStream_t)stream, "oasis_commit_kv");
 }
 
 extern "C" int oasis_commit_kv_layers(const oasis_dims_t *dims, int32_t n_layers, const void *const *tree_kvs, int32_t n_tree,
@@ -161,6 +167,17 @@ extern "C" int oasis_commit_kv_layers(const oasis_dims_t *dims, int32_t n_layers
                                       void *const *host_kvs, int32_t *next_len, void *stream)
 {
     return oasis::launch_commit(dims, n_layers, tree_kvs, n_tree, path, max_path, n_commit, seq_len, block_tables, slot_tbls,
-                                blk_tbls, n_cols, local_col, hbm_pools, host_kvs, next_len, (cudaStream_t)stream,
+                                blk_tbls, n_cols, local_col, hbm_pools, host_kvs, nullptr, next_len, (cudaStream_t)stream,
                                 "oasis_commit_kv_layers");
+}
+
+extern "C" int oasis_commit_kv_layers_after_select(const oasis_dims_t *dims, int32_t n_layers, const void *const *tree_kvs, int32_t n_tree,
+                                                   const int32_t *path, int32_t max_path, const int32_t *n_commit, const int32_t *seq_len,
+                                                   const int32_t *const *block_tables, const int32_t *const *slot_tbls,
+                                                   int32_t *const *blk_tbls, int32_t n_cols, int32_t local_col, void *const *hbm_pools,
+                                                   void *const *host_kvs, const int32_t *n_candidates, int32_t *next_len, void *stream)
+{
+    return oasis::launch_commit(dims, n_layers, tree_kvs, n_tree, path, max_path, n_commit, seq_len, block_tables, slot_tbls,
+                                blk_tbls, n_cols, local_col, hbm_pools, host_kvs, n_candidates, next_len, (cudaStream_t)stream,
+                                "oasis_commit_kv_layers_after_select");
 }

@@ -22,7 +22,7 @@ namespace {
 // The entry points of the library that the binding has loaded (`bind`).
 decltype(&oasis_tree_attn) g_tree_attn = nullptr;
 decltype(&oasis_verify_tree) g_verify_tree = nullptr;
-decltype(&oasis_commit_kv_layers) g_commit_kv_layers = nullptr;
+decltype(&oasis_commit_kv_layers_after_select) g_commit_kv_layers = nullptr;
 
 struct Refused {
     PyObject *type;
@@ -282,12 +282,12 @@ PyObject *verify_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// commit_kv_layers(plan, path, n_commit, seq_len, next_len, stream), plan = (device, dims, n_layers, tree_kvs, T, block_tables,
+// commit_kv_layers(plan, path, n_commit, seq_len, next_len, stream, n_candidates), plan = (device, dims, n_layers, tree_kvs, T, block_tables,
 // slot_tbls, blk_tbls, n_cols, local_col, pools, host_kvs): numbers and the addresses of arrays that the caller holds
 PyObject *commit_kv_layers(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
-        takes(n, 6);
+        takes(n, 7);
         if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 12) refuse(PyExc_TypeError, "plan: expected a CommitPlan's tuple");
         const auto item = [&](int i) { return PyTuple_GET_ITEM(a[0], i); };
         const int device = c10::cuda::current_device();
@@ -301,6 +301,7 @@ PyObject *commit_kv_layers(PyObject *, PyObject *const *a, Py_ssize_t n)
         const auto *n_commit = (const int32_t *)dense(a[2], at::kInt, {B}, "n_commit", device);
         const auto *len = (const int32_t *)dense(a[3], at::kInt, {B}, "seq_len", device);
         auto *next = (int32_t *)dense_or_null(a[4], at::kInt, {B}, "next_len", device);
+        const auto *candidates = (const int32_t *)dense_or_null(a[6], at::kInt, {B}, "n_candidates", device);
         const int32_t layers = narrow(integer(item(2)), "n_layers"), T = narrow(integer(item(4)), "n_tree"), m = narrow(M, "max_path");
         const int32_t cols = narrow(integer(item(8)), "n_cols"), local = narrow(integer(item(9)), "local_col");
         const auto *kv = address<const void *const *>(item(3));
@@ -309,7 +310,7 @@ PyObject *commit_kv_layers(PyObject *, PyObject *const *a, Py_ssize_t n)
         const auto *pools = address<void *const *>(item(10)), *hosts = address<void *const *>(item(11));
         void *stream = stream_of(a[5], device);
         return status([&] {
-            return g_commit_kv_layers(dims, layers, kv, T, path, m, n_commit, len, tables, slots, blks, cols, local, pools, hosts, next, stream);
+            return g_commit_kv_layers(dims, layers, kv, T, path, m, n_commit, len, tables, slots, blks, cols, local, pools, hosts, candidates, next, stream);
         });
     });
 }

@@ -490,12 +490,15 @@ class DecodeEngine:
 
     def commit(self, plan, path, n_commit, seq_len, next_len=None):
         """After a step with draft trees: the kept path of every request goes into the local windows and full-KV pools of
-        all layers (on the foreground stream, after the current stream's work so far, which produced the path)."""
+        all layers (on the foreground stream, after the current stream's work so far, which produced the path).  A request
+        with n_commit 0 keeps nothing of the step; its local blocks that the step's selection could choose leave the local window."""
         if not self.tree:
             raise ValueError("commit goes with engines built with tree=True")
         self.main.wait_event(self._event(torch.cuda.current_stream(self.device)))
         with torch.cuda.stream(self.main):
-            oasis.commit_kv_layers(plan, path, n_commit, seq_len, next_len=next_len)
+            if self.score_done[0] is not None:
+                self.main.wait_event(self.score_done[0])         # it writes n_cand, alike for all layers
+            oasis.commit_kv_layers(plan, path, n_commit, seq_len, next_len=next_len, n_candidates=self.layers[0].n_cand)
             self.launches += 1
             self.commit_done = self._event(self.main)
         torch.cuda.current_stream(self.device).wait_event(self.commit_done)

@@ -196,3 +196,52 @@ def test_padding_nodes_do_not_choose_the_working_set(L, fill):
 def test_padding_nodes_do_not_choose_the_working_set_in_a_graph(L):
     want, got = selections(0.0, False), selections(math.nan, True)
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+# ---- requests that keep nothing ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("nodes", [0, 5], ids=["sits out", "thrown away"])
+@pytest.mark.parametrize("graph", [False, True], ids=["eager", "graph"])
+def test_a_request_that_keeps_nothing_for_a_step(L, nodes, graph):
+    """Request 0 commits across a block's border, keeps nothing for one or two steps, and goes on: block 2 is then in the working
+    set once, as a selected block or in its local column."""
+    loop = Loop([45, 60], 2, 8, 2, 6, 2, 16, 16, 16, seed=4)
+    loop.step([6, 6], graph=graph)
+    loop.commit([6, 6])                                   # 45 -> 51: blocks 2 and 3 are local now
+    for _ in range(2):
+        loop.step([nodes, 6], graph=graph)
+        loop.check_dense([0, 1] if nodes else [1])
+        loop.commit([0, 6])
+        loop.check_no_block_twice()
+    for _ in range(2):
+        loop.step([6, 3], graph=graph)
+        loop.check_dense([0, 1])
+        loop.commit([4, 2])
+        loop.check_no_block_twice()
+
+
+def test_local_blocks_that_may_have_been_selected(L):
+    """Rows of nine requests with the local blocks (even, odd) and candidates given: only a request that keeps nothing gives a
+    column up, and only one whose block is below its number of candidates."""
+    cols = [(4, 5), (4, 5), (4, 5), (4, 5), (-1, 5), (4, -1), (4, 5), (6, 5), (-9, -9)]
+    cand, keep = [5, 4, 6, 0, 6, 6, 6, 6, 50], [0, 0, -2, 0, 0, 0, 2, 0, 0]
+    want = [(-1, 5), (4, 5), (-1, -1), (4, 5), (-1, -1), (-1, -1), (6, 5), (6, -1), (-9, -9)]
+    B, Hkv, n_cols, layers = 9, 3, 6, 2
+    dims = L.Dims(B, Hkv, Hkv, 16)
+    z = lambda *shape, dt=torch.bfloat16: torch.zeros(shape, dtype=dt, device="cuda")  # noqa: E731
+    blk = [torch.tensor(cols, dtype=torch.int32, device="cuda")[:, None].expand(B, Hkv, 2).repeat(1, 1, 3).contiguous() for _ in range(layers)]
+    before = [t.clone() for t in blk]
+    plan = L.CommitPlan(dims, [z(B, 2, Hkv, 2, 128)] * layers, [z(B, 16, dt=torch.int32)] * layers, [z(B, Hkv, n_cols, dt=torch.int32) - 1] * layers,
+                        blk, 4, [z(4, 2, 16, 128)] * layers)
+    args, nxt = (plan, i32([[0, 1]] * B), i32(keep), i32([95] * B)), i32([0] * B)
+    L.commit_kv_layers(*args, next_len=nxt, n_candidates=i32(cand))
+    for a, was in zip(blk, before):
+        assert a[:, :, :4].equal(was[:, :, :4]) and a[:, :, 4:].tolist() == [[list(w)] * Hkv for w in want]
+        a.copy_(was)
+    assert nxt.tolist() == [95 + max(n, 0) for n in keep]
+    L.commit_kv_layers(*args)                             # no selection was made: those requests' columns stay
+    for a, was in zip(blk, before):
+        assert a[:6].equal(was[:6]) and a[7:].equal(was[7:])
+    with pytest.raises(L.OasisError, match="share memory"):
+        L.commit_kv_layers(*args, next_len=nxt, n_candidates=nxt)
+    with pytest.raises(TypeError):
+        L.commit_kv_layers(*args, n_candidates=nxt.long())
