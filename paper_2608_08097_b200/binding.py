@@ -443,11 +443,10 @@ def _calls():
 
 
 def _cdims(dims):
-    """Address of the dims' C struct, which is made once per Dims object (it is immutable) and lives as long."""
+    """Address of the dims' C struct, which is made once per Dims object (it is immutable) and lives as long: the struct that
+    comes first stays, whichever thread made it, because another call may already be using it."""
     c = dims.__dict__.get("_c")
-    if c is None:
-        c = dims.__dict__["_c"] = dims.c()
-    return ctypes.addressof(c)
+    return ctypes.addressof(dims.__dict__.setdefault("_c", dims.c()) if c is None else c)
 
 
 def _handle(stream):

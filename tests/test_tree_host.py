@@ -28,3 +28,25 @@ def test_refusals_of_the_tree_scoring(L):
     for bad in (dict(dims=L.Dims(2, 258, 2, 64)), dict(dims=L.Dims(1 << 12, 32, 8, 1 << 17)), dict(dims=L.Dims(2, 32, 8, 64, head_dim=64))):
         assert call(**bad) == 2, bad
     assert call(dims=L.Dims(0, 32, 8, 64), q=None) == 0
+
+
+def test_a_dims_struct_is_made_once_whatever_the_threads_do(L, monkeypatch):
+    """A second thread makes the struct while the first one is making it: both have to end with the same one, and the one whose
+    address was handed out has to live on."""
+    import threading
+    d, inner, made = L.Dims(2, 32, 8, 64), [], []
+    real = L.Dims.c
+
+    def slow(self):
+        made.append(real(self))
+        if len(made) == 1:
+            t = threading.Thread(target=lambda: inner.append(L._cdims(d)))
+            t.start()
+            t.join()
+            return made[0]
+        return made[-1]
+
+    monkeypatch.setattr(L.Dims, "c", slow)
+    outer = L._cdims(d)
+    assert len(inner) == 1 and inner[0] == outer == L._cdims(d)
+    assert ctypes.cast(outer, ctypes.POINTER(L._Dims)).contents.n_q_heads == 32
