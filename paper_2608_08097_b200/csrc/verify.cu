@@ -209,7 +209,7 @@ struct Control {
     Dist d;
     double ma, mb;
     // kept by warp 0 from one decision about a node to the next
-    double z, away;                    // sum of all weights; weight of the tried tokens
+    double z, away;                    // sum of the weights when it was last measured; weight of the tokens tried since
     unsigned long long left;           // children not tried yet
     int exact, have_mass, need;        // z is the fp64 sum; s_mass fits the distribution; what the mass pass is for
     // the search
@@ -589,8 +589,9 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                     } else {
                         double mass = 0.0;
                         for (int r = 0; r < C; ++r) mass += __longlong_as_double((long long)got[r].a);
-                        if (need == kExact) {
-                            z = mass + away;
+                        if (need == kExact) {                                       // of what is left: tried tokens have left the row
+                            z = mass;
+                            away = 0.0;
                             exact = true;
                         } else {
                             have_mass = need == kFinal || mass > 0.0;               // (else nothing is left: p stays as it was)
@@ -629,6 +630,9 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                         if (!exact && fabs(u * (z - away) - wc) <= kFuzzy * z) { need = kExact; break; }
                         if (u * (z - away) < wc) { child = i; break; }
                         away += wc;
+                        // Where a rejection leaves less than 2^-10 of the measured sum, z - away has lost more than ten of its bits:
+                        // what is left is measured again (random numbers close to 1; four tokens in a row of 2^-24 each lost them all).
+                        if (z - away < 0x1p-10 * z) exact = false;
                         tried |= 1ull << i;
                         left &= left - 1;
                     }
