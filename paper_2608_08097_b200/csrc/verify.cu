@@ -29,10 +29,14 @@
 namespace oasis {
 
 constexpr int kVerMaxCluster = 8;
-// The fp32 sum of exponentials is off by less than 2e-3 of itself: m c2 is rounded (2^-12, a common factor), a term of
-// weight 2^-x has a relative error below (1.5 x + 4) 2^-23, and a lane adds at most 2^22 / 512 / 4 = 2048 pairs to an
-// accumulator one after the other (2048 * 2^-24) -- 4e-4 together at the largest vocabulary; the careful loop, one
-// accumulator for up to 8192 terms, is off by 5e-4.
+// The fp32 sum of exponentials is off by less than 3e-4 of itself, and 2e-3 is taken for it:
+//   m c2, below 4096, is rounded once per lane and chunk (2^-12 in the exponent)                                1.7e-4
+//   a term of weight 2^-x has a relative error below (1.5 x + 4) 2^-23; x is below 20 on the weighted average     4e-6
+//   a lane adds the terms of a chunk, 17 vectors at most (blocks of 512 threads; 16 with 256), to two accumulators
+//   (34 additions each; the careful loop 136 to one)                                                             8e-6
+//   then chunk after chunk, each a rescaling by an exponential (2^-22) and an addition: 257 chunks at most
+//   (2^22 fp32 logits, one block of 256 threads)                                                                8e-5
+//   and twelve such steps over the lanes, warps and thread blocks                                                4e-6
 constexpr double kFuzzy = 2e-3;
 
 struct VerifyParams {
@@ -180,8 +184,9 @@ __device__ const ExpTable g_exp_table = ExpTable();
 
 // exp((l - m) / temperature) in fp64, to about 1e-13 of itself.  With y = (l - m) c and n = y rounded to a whole number,
 //   2^(y / 64) = 2^floor(n / 64) * T[n mod 64] * exp(z),  z = (y - n) ln 2 / 64,  |z| <= 0.0055,
-// and four terms of the series for exp(z) - 1 leave 4e-14.  Kept to 33 bits: sums of equal weights are then exact, so that
-// a random number that falls on a border between equal logits is decided as in exact arithmetic.  This is the pass over
+// and four terms of the series for exp(z) - 1 leave 4e-14; y's own rounding adds up to 6e-14 at weights of 2^-360.  All bits are
+// kept: where a draft row nearly agrees with the target their difference is a 2^-25 or less of either, and cut to 33 bits (which
+// this was once, for sums of equal weights to be exact) it chose another token in 2 of 512 draws.  This is the pass over
 // 152,000 logits that the last node of every walk needs; exp() takes 2.5 times as long (19.7 against 7.8 cycles per 32
 // logits and SM, with a table of 1,024 steps that had bank conflicts).
 __device__ __forceinline__ double weight(float l, const Dist &d, const double *table)       // table: this lane's copy
@@ -194,7 +199,7 @@ __device__ __forceinline__ double weight(float l, const Dist &d, const double *t
     const double f = table[(n & (kExpSteps - 1)) * kExpCopies];
     const double e = fma(r, fma(r, fma(r, kStep * kStep * kStep * kStep / 24, kStep * kStep * kStep / 6), kStep * kStep / 2), kStep);
     const double w = fma(f * r, e, f);
-    const double scaled = __hiloint2double(__double2hiint(w) + ((n & ~(kExpSteps - 1)) << 14), __double2loint(w) & 0xfff00000);
+    const double scaled = __hiloint2double(__double2hiint(w) + ((n & ~(kExpSteps - 1)) << 14), __double2loint(w));
     return l > d.l_min ? scaled : 0.0;                     // (also for NaN and -infinity)
 }
 

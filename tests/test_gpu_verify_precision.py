@@ -48,3 +48,22 @@ def test_the_last_tokens_after_rejections_that_took_nearly_everything(L):
     got, ref = verify(L, torch.tensor(x, device="cuda"), tokens, parent, u, 1.0)
     assert (ref[0][:, 1] == 4).all()
     assert all(np.array_equal(g, r) for g, r in zip(got, ref)), (got[0][:, 1], got[2] - ref[2])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_a_draft_that_differs_from_the_target_in_the_last_bits(L, dtype):
+    """The draft is the target rounded to fp32, all but the drafted token, which is rejected: the next token is drawn from the
+    differences, about 2^-25 of either.  (A weight that is off by e moves the border between two tokens by e 2^25 or so of a
+    token's share: 1e-13 by 3e-6 of it, once in 1e5 draws; 2e-10 by more than a hundredth.)"""
+    rng = np.random.default_rng(1)
+    N, V = 512, 2000
+    x = torch.tensor(rng.standard_normal((N, 2, V)), device="cuda").to(dtype)
+    p = torch.softmax(x.double() / 0.9000000357627869, -1)                # (the temperature as fp32 holds it)
+    q = p.float()
+    tokens, parent = rng.integers(0, V, (N, 2)).astype(np.int32), np.tile([-1, 0], (N, 1)).astype(np.int32)
+    q[torch.arange(N), 0, torch.tensor(tokens[:, 1].astype(np.int64))] = 0.9
+    u = rng.random((N, 2)).astype(np.float32)
+    u[:, 1] = 1 - 2.0 ** -24
+    got, ref = verify(L, x, tokens, parent, u, 0.9, q)
+    assert (ref[1] == 1).all()
+    assert all(np.array_equal(g, r) for g, r in zip(got, ref)), int((got[2] != ref[2]).sum())
