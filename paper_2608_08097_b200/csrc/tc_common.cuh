@@ -186,8 +186,16 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+// The driver's encoder of tensor maps, which needs the calling thread to have a context: a thread that has made no runtime call but
+// this library's first one gets the current device's here.
 inline EncodeTiledFn encode_tiled_fn()
 {
+    static thread_local bool has_context = false;
+    if (!has_context) {
+        int dev = 0;
+        has_context = cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess;
+        if (!has_context) cudaGetLastError();
+    }
     static EncodeTiledFn fn = nullptr;
     static bool tried = false;
     if (!tried) {
