@@ -50,3 +50,41 @@ def test_a_dims_struct_is_made_once_whatever_the_threads_do(L, monkeypatch):
     outer = L._cdims(d)
     assert len(inner) == 1 and inner[0] == outer == L._cdims(d)
     assert ctypes.cast(outer, ctypes.POINTER(L._Dims)).contents.n_q_heads == 32
+
+
+HARNESS = r"""
+#include <cuda_runtime.h>
+#include <chrono>
+#include <cstdio>
+#include <thread>
+static cudaError_t slow_entry_point(const char *, void **ptr, unsigned long long, cudaDriverEntryPointQueryResult *q)
+{
+    std::this_thread::sleep_for(std::chrono::milliseconds(300));
+    *ptr = (void *)0x1000;
+    *q = cudaDriverEntryPointSuccess;
+    return cudaSuccess;
+}
+#define cudaGetDriverEntryPoint slow_entry_point
+#include "common.cuh"
+#include "tc_common.cuh"
+int main()
+{
+    bool got[4];
+    std::thread t[4];
+    for (int i = 0; i < 4; ++i) t[i] = std::thread([&, i] { got[i] = oasis::encode_tiled_fn() != nullptr; });
+    for (auto &x : t) x.join();
+    std::printf("%d %d %d %d\n", got[0], got[1], got[2], got[3]);
+}
+"""
+
+
+def test_threads_that_ask_for_the_drivers_encoder_together(L, tmp_path):
+    """The driver's answer takes a while: no thread may go on without it."""
+    import os
+    import subprocess
+    from paper_2608_08097_b200 import build
+    (tmp_path / "first.cu").write_text(HARNESS)
+    exe = str(tmp_path / "first")
+    subprocess.run([build.NVCC, *build.ARCH, "-std=c++17", "-I" + build.CSRC, "-o", exe, str(tmp_path / "first.cu"),
+                    os.path.join(build.OBJ, "api.o")], check=True, capture_output=True)
+    assert subprocess.run([exe], capture_output=True, text=True, timeout=60).stdout.split() == ["1"] * 4
