@@ -1,5 +1,5 @@
 """Builds the CUDA library (csrc/*.cu -> liboasis.so, in-tree) for sm_100a, and the Python calls of the draft-tree
-operators (csrc/py_call.cpp -> _call.so, host code only).
+operators (csrc/py_call.cpp -> _call.so, host code only; left out where torch is not installed).
 
 nvcc cross-compiles without a GPU.  Objects are rebuilt only when their source (or a
 header) is newer; `python -m paper_2608_08097_b200.build --force` rebuilds everything,
@@ -9,6 +9,7 @@ device array is range-checked on the device; see include/oasis.h).
 """
 import concurrent.futures
 import glob
+import importlib.metadata
 import importlib.util
 import os
 import subprocess
@@ -43,9 +44,25 @@ def _compile(src, verbose, obj_dir=OBJ, defines=()):
     return obj, r.stderr
 
 
+def _call_tag():
+    """What _call.so is tied to beside its sources: the interpreter's and torch's binary interfaces.  None: no torch here."""
+    if importlib.util.find_spec("torch") is None:
+        return None
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:                  # a source tree on the path
+        version = "of no version"
+    return "%s torch %s" % (sysconfig.get_config_var("SOABI"), version)
+
+
 def _build_call(force=False):
+    tag, tag_file = _call_tag(), os.path.join(OBJ, "_call.tag")
+    if tag is None:                                                  # the C library alone: there are no tensors to check
+        return
     src = os.path.join(CSRC, "py_call.cpp")
-    if not force and os.path.exists(CALL) and os.path.getmtime(CALL) >= max(os.path.getmtime(src), os.path.getmtime(os.path.join(HERE, "..", "include", "oasis.h"))):
+    built_for = open(tag_file).read() if os.path.exists(tag_file) else ""
+    if (not force and built_for == tag and os.path.exists(CALL)
+            and os.path.getmtime(CALL) >= max(os.path.getmtime(src), os.path.getmtime(os.path.join(HERE, "..", "include", "oasis.h")))):
         return
     torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     cuda = os.path.dirname(os.path.dirname(NVCC))
@@ -57,10 +74,12 @@ def _build_call(force=False):
     if r.returncode != 0:
         raise RuntimeError("g++ failed for %s:\n%s\n%s" % (src, r.stdout, r.stderr))
     os.replace(part, CALL)
+    os.makedirs(OBJ, exist_ok=True)
+    with open(tag_file, "w") as f:
+        f.write(tag)
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
-    _build_call(force)
     obj_dir, lib = (OBJ_CHECKED, LIB_CHECKED) if checked else (OBJ, LIB)
     defines = ("-DOASIS_BOUNDS_CHECK",) if checked else ()
     os.makedirs(obj_dir, exist_ok=True)
@@ -83,6 +102,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
+    _build_call(force)
     return lib
 
 

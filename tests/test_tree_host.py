@@ -88,3 +88,27 @@ def test_threads_that_ask_for_the_drivers_encoder_together(L, tmp_path):
     subprocess.run([build.NVCC, *build.ARCH, "-std=c++17", "-I" + build.CSRC, "-o", exe, str(tmp_path / "first.cu"),
                     os.path.join(build.OBJ, "api.o")], check=True, capture_output=True)
     assert subprocess.run([exe], capture_output=True, text=True, timeout=60).stdout.split() == ["1"] * 4
+
+
+def test_the_c_library_builds_without_torch(L, monkeypatch, tmp_path):
+    import importlib.util
+    from paper_2608_08097_b200 import build
+    real = importlib.util.find_spec
+    monkeypatch.setattr(build, "CALL", str(tmp_path / "_call.so"))      # (not built yet)
+    monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: None if name == "torch" else real(name, *a))
+    assert build.build() == build.LIB and not (tmp_path / "_call.so").exists()
+
+
+def test_the_python_calls_are_built_again_for_another_torch(L, monkeypatch):
+    from paper_2608_08097_b200 import build
+    ran = []
+
+    class Failed:
+        returncode, stdout, stderr = 1, "", "(not run)"
+
+    monkeypatch.setattr(build.subprocess, "run", lambda cmd, **kw: ran.append(cmd) or Failed)
+    assert build.build() == build.LIB and not ran                    # up to date: nothing is run
+    monkeypatch.setattr(build.importlib.metadata, "version", lambda name: "99.0")
+    with pytest.raises(RuntimeError, match="g.. failed"):
+        build.build()
+    assert len(ran) == 1 and any("py_call.cpp" in x for x in ran[0])
