@@ -54,7 +54,6 @@ __host__ __device__ constexpr int tr_smem(int mma_m, bool pair)
 static_assert(kTrPlain + 4 * kAtMaxStages <= 512 && tr_smem(128, false) <= 232448 && tr_smem(128, true) <= 232448, "shared memory of a thread block");
 
 struct TreeAttnParams {
-    const uint8_t *q;
     const int32_t *slot_tbl, *blk_tbl, *seq_len, *parent, *n_nodes;
     uint8_t *out;
     float *lse;
@@ -143,8 +142,6 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
     const int c1 = min(c0 + p.cols_per_split, p.n_cols);
     const int32_t *slot_row = p.slot_tbl + (long long)bh * p.n_cols;
     const int32_t *blk_row = p.blk_tbl + (long long)bh * p.n_cols;
-    // a launch behind this one (the merge of the splits, or the next attention) may bring its thread blocks onto the SMs
-    // already, and this one may have been brought so: what earlier launches wrote is read from here on
     if (tid == 0) {
         for (int s = 0; s < kAtMaxStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
         for (int a = 0; a < kAtSBufs; ++a) { mbar_init(bar_s_full(a), 1); mbar_init(bar_p_full(a), 4); }
@@ -152,8 +149,11 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap pool_map, const __grid_c
         *s_count = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // This launch may have been brought onto the SMs before the previous one ended: what that wrote is read from here on.  Only then
+    // may a launch behind this one (the merge of the splits, the next attention) be brought in the same way: it may read, without
+    // a wait of its own, what launches before this one wrote (the scoring of oasis_attn_and_score does).
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == 0 && c0 < c1) window_request(smem_u32(win), lane, blk_row, slot_row, c0 + lane, c1);     // (needs no length)
     // every first load is on its way before the first is used: lengths, this thread's column, the parents (warp 2)
     const int n_nodes_raw = p.n_nodes[b], L = p.seq_len[b];
@@ -764,7 +764,7 @@ extern "C" int oasis_tree_attn(const oasis_dims_t *dims, const void *q, int32_t 
     if (cr != CUDA_SUCCESS) return fail(OASIS_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed (%d)", who, (int)cr);
 
     TreeAttnParams p = {};
-    p.q = (const uint8_t *)q; p.slot_tbl = slot_tbl; p.blk_tbl = blk_tbl; p.seq_len = seq_len; p.parent = parent;
+    p.slot_tbl = slot_tbl; p.blk_tbl = blk_tbl; p.seq_len = seq_len; p.parent = parent;
     p.n_nodes = n_nodes; p.out = (uint8_t *)out; p.lse = lse; p.err = error_word();
     p.scale_log2 = scale * kAtLog2e;
     p.T = n_tree; p.Hq = dims->n_q_heads; p.Hkv = dims->n_kv_heads; p.G = p.Hq / p.Hkv; p.n_cols = n_cols; p.R = n_tree * p.G;

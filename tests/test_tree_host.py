@@ -112,3 +112,16 @@ def test_the_python_calls_are_built_again_for_another_torch(L, monkeypatch):
     with pytest.raises(RuntimeError, match="g.. failed"):
         build.build()
     assert len(ran) == 1 and any("py_call.cpp" in x for x in ran[0])
+
+
+def test_the_attention_lets_a_successor_start_only_after_its_own_wait(L):
+    """oasis_attn_and_score reads its scoring inputs without a wait: a launch between it and their producer separates the two
+    only if it lets a successor start after it has waited for the producer itself."""
+    import os
+    import re
+    from paper_2608_08097_b200 import build
+    text = open(os.path.join(build.CSRC, "tree_attn.cu")).read()
+    kernel = text[text.index("tree_attn_tc_kernel(const"):text.index("tree_combine_kernel(const")]
+    assert re.findall(r"griddepcontrol\.(\w+)", kernel) == ["wait", "launch_dependents"]
+    for name in ("verify.cu", "commit.cu"):                          # these never let a successor start early
+        assert re.findall(r"griddepcontrol\.(\w+)", open(os.path.join(build.CSRC, name)).read()) == ["wait"]
