@@ -512,7 +512,10 @@ class DecodeEngine:
         """Captures consecutive steps -- a list of (args, kwargs) of `step` -- into one CUDA graph on the
         foreground stream and returns it.  Inside the graph the steps overlap as far as their per-layer
         dependencies allow; `graph.replay()` must be issued on that stream, and a replay completes only when
-        all streams' work of its last step has completed."""
+        all streams' work of its last step has completed.  Steps with draft trees are captured one at a time: `commit` follows
+        each of them."""
+        if self.tree and len(steps) > 1:
+            raise ValueError("steps with draft trees are captured one at a time: a commit follows each of them")
         torch.cuda.synchronize(self.device)
         self._reset_events()
         before = self.launches

@@ -125,3 +125,12 @@ def test_the_attention_lets_a_successor_start_only_after_its_own_wait(L):
     assert re.findall(r"griddepcontrol\.(\w+)", kernel) == ["wait", "launch_dependents"]
     for name in ("verify.cu", "commit.cu"):                          # these never let a successor start early
         assert re.findall(r"griddepcontrol\.(\w+)", open(os.path.join(build.CSRC, name)).read()) == ["wait"]
+
+
+def test_steps_with_trees_are_captured_one_at_a_time():
+    """No commit can lie between the steps of one graph."""
+    from paper_2608_08097_b200 import pipeline
+    eng = pipeline.DecodeEngine.__new__(pipeline.DecodeEngine)
+    eng.tree = True
+    with pytest.raises(ValueError, match="commit"):
+        eng.capture_steps([((), {}), ((), {})])
