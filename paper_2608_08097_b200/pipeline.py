@@ -484,22 +484,32 @@ class DecodeEngine:
                 pending, readies = [], []
 
     def commit_plan(self, tree_kvs):
-        """The handle of `commit` for these per-layer tree buffers [B][T][Hkv][2][128] (the `new_kv` of the steps)."""
-        return oasis.CommitPlan(self.layers[0].dims, list(tree_kvs), self.table, [L.slot_tbl for L in self.layers], self.resident,
-                                self.k, [L.pool for L in self.layers], self.kv)
+        """The handle of `commit` for these per-layer tree buffers [B][T][Hkv][2][128] (the `new_kv` of the steps): a
+        CommitPlan, or a list of them, one for every oasis.MAX_APPEND_LAYERS layers."""
+        def plan(l0, l1):
+            layers = self.layers[l0:l1]
+            return oasis.CommitPlan(layers[0].dims, list(tree_kvs[l0:l1]), self.table[l0:l1], [L.slot_tbl for L in layers],
+                                    self.resident[l0:l1], self.k, [L.pool for L in layers], self.kv[l0:l1])
+
+        if len(tree_kvs) != self.n_layers:
+            raise ValueError("tree_kvs: %d tensors for %d layers" % (len(tree_kvs), self.n_layers))
+        plans = [plan(l0, l0 + oasis.MAX_APPEND_LAYERS) for l0 in range(0, self.n_layers, oasis.MAX_APPEND_LAYERS)]
+        return plans[0] if len(plans) == 1 else plans
 
     def commit(self, plan, path, n_commit, seq_len, next_len=None):
-        """After a step with draft trees: the kept path of every request goes into the local windows and full-KV pools of
-        all layers (on the foreground stream, after the current stream's work so far, which produced the path).  A request
-        with n_commit 0 keeps nothing of the step; its local blocks that the step's selection could choose leave the local window."""
+        """After a step with draft trees: the kept path of every request ([B][max_path], at most 16 nodes) goes into the local
+        windows and full-KV pools of all layers (on the foreground stream, after the current stream's work so far, which produced
+        the path).  A request with n_commit 0 keeps nothing of the step; its local blocks that the step's selection could choose
+        leave the local window."""
         if not self.tree:
             raise ValueError("commit goes with engines built with tree=True")
         self.main.wait_event(self._event(torch.cuda.current_stream(self.device)))
         with torch.cuda.stream(self.main):
             if self.score_done[0] is not None:
                 self.main.wait_event(self.score_done[0])         # it writes n_cand, alike for all layers
-            oasis.commit_kv_layers(plan, path, n_commit, seq_len, next_len=next_len, n_candidates=self.layers[0].n_cand)
-            self.launches += 1
+            for one in [plan] if isinstance(plan, oasis.CommitPlan) else plan:
+                oasis.commit_kv_layers(one, path, n_commit, seq_len, next_len=next_len, n_candidates=self.layers[0].n_cand)
+                self.launches += 1
             self.commit_done = self._event(self.main)
         torch.cuda.current_stream(self.device).wait_event(self.commit_done)
 

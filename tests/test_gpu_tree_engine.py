@@ -245,3 +245,14 @@ def test_local_blocks_that_may_have_been_selected(L):
         L.commit_kv_layers(*args, next_len=nxt, n_candidates=nxt)
     with pytest.raises(TypeError):
         L.commit_kv_layers(*args, n_candidates=nxt.long())
+
+
+def test_more_layers_than_one_commit_takes(L):
+    loop = Loop([30], 1, 2, 1, 3, 66, 8, 6, 6, seed=6)
+    for keep in (3, 2, 1):
+        loop.step([3])
+        loop.check_dense([0])
+        loop.commit([keep])
+        loop.check_no_block_twice()
+    with pytest.raises(ValueError, match="66 layers"):
+        loop.eng.commit_plan(loop.tree_kv[:65])
