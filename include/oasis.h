@@ -429,7 +429,8 @@ typedef enum { OASIS_F32 = 0, OASIS_BF16 = 1, OASIS_F16 = 2 } oasis_dtype_t;
  * then: the lowest index at which the running sum of p exceeds uniforms[b][0] (greedy: the largest logit's index).
  *   logits      element (b, x, v) at logits[b * logits_batch_stride + x * logits_row_stride + v], of type logits_type
  *               (oasis_dtype_t); strides in elements, row stride >= vocab; any alignment of its type.  -infinity leaves
- *               a token out, and so does NaN; +infinity shares all of p among the tokens that have it.
+ *               a token out, and so do NaN and, when sampling, a logit 600 temperatures or more below the row's largest (a
+ *               share of e^-600 of that token's); +infinity shares all of p among the tokens that have it.
  *   tokens      [B][n_tree] int32: the nodes' tokens (node 0's is not read); one outside [0, vocab) is never kept
  *   uniforms    [B][n_tree] fp32 random numbers, taken into [0, 1 - 2^-24]
  *   temperature [B] fp32

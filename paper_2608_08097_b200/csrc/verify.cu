@@ -38,6 +38,9 @@ constexpr int kVerMaxCluster = 8;
 //   (2^22 fp32 logits, one block of 256 threads)                                                                8e-5
 //   and twelve such steps over the lanes, warps and thread blocks                                                4e-6
 constexpr double kFuzzy = 2e-3;
+// A weight reaches down to e^-600 = 1e-260: it, its share after a rejection that left only such tokens (times 1e260) and what
+// further rejections cancel of that stay within the range of a double.
+constexpr float kReach = 600.f;
 
 struct VerifyParams {
     const void *logits;
@@ -152,7 +155,7 @@ struct __align__(16) Pair { uint64_t a, b; };
 // What the target's distribution at the current node has become: a token's share is
 //   max(a * w - b * q, 0)   with w = exp((logit - m) / temperature); rejected tokens without a draft row are left out
 struct Dist {
-    float l_min;                       // logits up to here have weight 0: 250 temperatures below m, and everything but m at tiny ones
+    float l_min;                       // logits up to here have weight 0: kReach temperatures below m, and everything but m at tiny ones
     double m, c;                       // c = 64 log2(e) / temperature
     double a, b;
     const float *q;                    // the draft's row, or NULL
@@ -184,7 +187,7 @@ __device__ const ExpTable g_exp_table = ExpTable();
 
 // exp((l - m) / temperature) in fp64, to about 1e-13 of itself.  With y = (l - m) c and n = y rounded to a whole number,
 //   2^(y / 64) = 2^floor(n / 64) * T[n mod 64] * exp(z),  z = (y - n) ln 2 / 64,  |z| <= 0.0055,
-// and four terms of the series for exp(z) - 1 leave 4e-14; y's own rounding adds up to 6e-14 at weights of 2^-360.  All bits are
+// and four terms of the series for exp(z) - 1 leave 4e-14; y's own rounding adds up to 1.3e-13 at the smallest weights.  All bits are
 // kept: where a draft row nearly agrees with the target their difference is a 2^-25 or less of either, and cut to 33 bits (which
 // this was once, for sums of equal weights to be exact) it chose another token in 2 of 512 draws.  This is the pass over
 // 152,000 logits that the last node of every walk needs; exp() takes 2.5 times as long (19.7 against 7.8 cycles per 32
@@ -580,7 +583,7 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                         }
                         const float at = infinite ? 0.f : top;
                         d.m = (double)at;
-                        d.l_min = fminf(at - 250.f * temp, nextafterf(at, -CUDART_INF_F));
+                        d.l_min = fminf(at - kReach * temp, nextafterf(at, -CUDART_INF_F));
                         d.q = q_row;
                         d.a = 1.0;
                         d.b = 0.0;

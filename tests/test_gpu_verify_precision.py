@@ -67,3 +67,27 @@ def test_a_draft_that_differs_from_the_target_in_the_last_bits(L, dtype):
     got, ref = verify(L, x, tokens, parent, u, 0.9, q)
     assert (ref[1] == 1).all()
     assert all(np.array_equal(g, r) for g, r in zip(got, ref)), int((got[2] != ref[2]).sum())
+
+
+@pytest.mark.parametrize("draft", [False, True], ids=["fixed", "drawn"])
+def test_tokens_far_below_the_likeliest(L, draft):
+    """Shares from e^-240 to e^-590 of the largest still count: a random number of 0 keeps such a child, and where the draft
+    takes all of the likely token, the unlikely ones share what is left."""
+    rng = np.random.default_rng(2)
+    N, V = 96, 40
+    x = np.full((N, 2, V), -np.inf, np.float32)
+    tokens, parent, u = np.zeros((N, 2), np.int32), np.tile([-1, 0], (N, 1)).astype(np.int32), np.zeros((N, 2), np.float32)
+    q = np.zeros((N, 2, V), np.float32)
+    for i in range(N):
+        t = rng.choice(V, 6, replace=False)
+        x[i, :, t[0]] = 7.0
+        x[i, :, t[1:]] = (7.0 - 0.5 * rng.uniform(240 + 3 * i, 245 + 3 * i, (5, 1)))      # (240 to 530 temperatures of 0.5 below)
+        q[i, :, t[0]] = 1.0
+        tokens[i, 1] = t[1 + i % 5]
+        if draft:                                         # rejected: it has a share of the draft, and none of the target's
+            tokens[i, 1] = rng.choice(np.setdiff1d(np.arange(V), t))
+            q[i, :, tokens[i, 1]] = 0.25
+            u[i] = rng.random(2)
+    got, ref = verify(L, torch.tensor(x, device="cuda"), tokens, parent, u, 0.5, torch.tensor(q, device="cuda") if draft else None)
+    assert (ref[1] == (1 if draft else 2)).all()
+    assert all(np.array_equal(g, r) for g, r in zip(got, ref)), int((got[2] != ref[2]).sum())
