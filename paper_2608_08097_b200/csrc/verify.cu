@@ -152,13 +152,15 @@ __device__ __forceinline__ void send(const void *place, uint32_t bar, uint32_t r
 
 struct __align__(16) Pair { uint64_t a, b; };
 
-// What the target's distribution at the current node has become: a token's share is
-//   max(a * w - b * q, 0)   with w = exp((logit - m) / temperature); rejected tokens without a draft row are left out
+// The target's distribution at the current node: a token's weight is w = exp((logit - m) / temperature).  Rejected tokens leave
+// the row; under a draft row q, k rejections leave a token with r_k, where r_0 = w and r_j = max(s_{j-1} r_{j-1} - q, 0), s_j being one
+// over the sum of all r_j, and with the share s_k r_k.  (Folded into one product a w - b q, what is 0 after one rejection came
+// back out of the rounding of large a and b after the next.)
 struct Dist {
     float l_min;                       // logits up to here have weight 0: kReach temperatures below m, and everything but m at tiny ones
     double m, c;                       // c = 64 log2(e) / temperature
-    double a, b;
     const float *q;                    // the draft's row, or NULL
+    int k;                             // rejections against it so far
 };
 
 // 2^(j / 64), made at compile time from square roots (Newton's iteration) of two: the binary digits of j pick the factors.
@@ -209,13 +211,14 @@ __device__ __forceinline__ double weight(float l, const Dist &d, const double *t
 __device__ __forceinline__ double shfl_d(double v, int lane) { return __shfl_sync(0xffffffffu, v, lane); }
 
 // What warp 0 decides and the other warps carry out.
-enum { kGo = 0, kMass = 1, kSearch = 2, kEnd = 3 };        // on to a child | a mass pass under (ma, mb) | find the next token | done
+enum { kGo = 0, kMass = 1, kSearch = 2, kEnd = 3 };        // on to a child | a mass pass | find the next token | done
 struct Control {
     int cmd, cur, ahead;               // ahead: the likeliest node after cur, or -1
     int infinite;                      // some logit of the row is +infinity
     unsigned long long tried;          // rejected children (without a draft row)
     Dist d;
-    double ma, mb;
+    double s[OASIS_MAX_TREE];          // s_0 .. s_k
+    int pass;                          // the mass pass sums r_pass
     // kept by warp 0 from one decision about a node to the next
     double z, away;                    // sum of the weights when it was last measured; weight of the tokens tried since
     unsigned long long left;           // children not tried yet
@@ -225,7 +228,16 @@ struct Control {
     int in_warp, take_last;            // (in_warp -1: another thread block has it)
 };
 
-// One chunk of a warp's vectors under (ma, mb): the mass of every vector goes to my_sum, the lane's sum is returned.  Tokens
+// r_k, k > 0, of a token with weight w and draft share q.
+__device__ __forceinline__ double left_of(double w, double q, int k, double s0, const Control &ctl)
+{
+    double r = fmax(s0 * w - q, 0.0);
+#pragma unroll 1
+    for (int j = 1; j < k; ++j) r = fmax(ctl.s[j] * r - q, 0.0);
+    return r;
+}
+
+// One chunk of a warp's vectors: the sum of r_pass of every vector goes to my_sum, the lane's sum is returned.  Tokens
 // that were tried leave the row by turning their logits into -infinity.
 template <typename LT>
 __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row, int vc, int ve, int lane, bool reload, uint4 *my_row,
@@ -239,13 +251,14 @@ __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row
         if (token >= 0 && token < row.V && v >= vc && v < ve && ((v - vc) & 31) == lane) leave_out<LT>(my_row + (v - vc - lane), e % N);
     }
     const Dist d = ctl.d;
-    const double ma = ctl.ma, mb = ctl.mb;
+    const int pass = ctl.pass;
+    const double s0 = ctl.s[0];
     const double *const my_table = table + (lane & (kExpCopies - 1));
     double sum = 0.0;
-    if (d.q && mb == 0.0)                                          // a pass under the draft's row may follow: on its way to L2
+    if (d.q && pass == 0)                                          // a pass under the draft's row may follow: on its way to L2
         for (int i = max(row.first(vc), 0) + lane * 32; i < min(row.first(ve), row.V); i += 32 * 32)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(d.q + i));
-    if (mb == 0.0 && !ctl.infinite) {
+    if (pass == 0 && !ctl.infinite) {
 #pragma unroll 1
         for (int v = vc + lane; v < ve; v += 32) {
             const uint4 w = my_row[v - vc - lane];
@@ -266,10 +279,10 @@ __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const int i = row.first(v) + k;
-                f[k] = mb != 0.0 && v < ve && i >= 0 && i < row.V ? d.q[i] : 0.f;
+                f[k] = pass > 0 && v < ve && i >= 0 && i < row.V ? d.q[i] : 0.f;
             }
         };
-        const bool plain = !ctl.infinite;
+        const bool plain = !ctl.infinite && pass == 1;              // (the others are rare)
         fetch(vc + lane, q);
 #pragma unroll 1
         for (int v = vc + lane; v < ve; v += 32) {
@@ -279,14 +292,14 @@ __device__ __noinline__ double chunk_mass(const Control &ctl, const Row<LT> &row
             if (plain) {
 #pragma unroll
                 for (int k = 0; k < N; ++k)                        // (outside the row the logit is -infinity)
-                    part += fmax(ma * weight(Logit<LT>::get(w, k), d, my_table) - mb * (double)q[k], 0.0);
+                    part += fmax(s0 * weight(Logit<LT>::get(w, k), d, my_table) - (double)q[k], 0.0);
             } else {
 #pragma unroll 1
                 for (int k = 0; k < N; ++k) {
                     const float l = Logit<LT>::one(reinterpret_cast<const LT *>(my_row + (v - vc - lane)) + k);
                     const double f = weight(!ctl.infinite ? l : l == CUDART_INF_F ? 0.f : -CUDART_INF_F, d, my_table);
                     const int i = row.first(v) + k;
-                    part += mb == 0.0 ? f : i >= 0 && i < row.V ? fmax(ma * f - mb * (double)d.q[i], 0.0) : 0.0;
+                    part += pass == 0 ? f : i >= 0 && i < row.V ? left_of(f, (double)d.q[i], pass, s0, ctl) : 0.0;
                 }
             }
 #pragma unroll
@@ -585,8 +598,7 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                         d.m = (double)at;
                         d.l_min = fminf(at - kReach * temp, nextafterf(at, -CUDART_INF_F));
                         d.q = q_row;
-                        d.a = 1.0;
-                        d.b = 0.0;
+                        d.k = 0;
                         z = (double)s;
                         away = 0.0;
                         left = (unsigned long long)kids1 << 32 | kids0;
@@ -605,8 +617,9 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                             have_mass = need == kFinal || mass > 0.0;               // (else nothing is left: p stays as it was)
                             if (have_mass) total = mass;
                             if (need == kRest && have_mass) {
-                                d.a = ctl.ma / mass;
-                                d.b = ctl.mb / mass;
+                                d.k = ctl.pass;
+                                if (lane == 0) ctl.s[d.k] = 1.0 / mass;
+                                __syncwarp();
                             }
                         }
                         if (have_mass && need == kExact) have_mass = false;         // (s_mass was used for something else)
@@ -624,11 +637,11 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                         if (q_row) {
                             const double q = (double)__shfl_sync(0xffffffffu, i < 32 ? kq0 : kq1, i & 31);
                             const double uq = u * q;
-                            if (d.b == 0.0 && !exact && fabs(uq * z - wc) <= kFuzzy * (uq * z + wc)) { need = kExact; break; }
-                            const double share = d.b == 0.0 ? wc / z : fmax(d.a * wc - d.b * q, 0.0);
+                            if (d.k == 0 && !exact && fabs(uq * z - wc) <= kFuzzy * (uq * z + wc)) { need = kExact; break; }
+                            const double share = d.k == 0 ? wc / z : ctl.s[d.k] * left_of(wc, q, d.k, ctl.s[0], ctl);
                             if (uq < share) { child = i; break; }
                             if (!exact) { need = kExact; break; }
-                            if (d.b == 0.0) d.a = 1.0 / z;
+                            if (d.k == 0 && lane == 0) ctl.s[0] = 1.0 / z;
                             left &= left - 1;
                             need = kRest;
                             break;
@@ -681,8 +694,7 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                     }
                     if (lane == 0) {
                         if (cmd == kMass) {
-                            ctl.ma = need == kExact ? 1.0 : d.a;
-                            ctl.mb = need == kExact ? 0.0 : need == kRest ? d.b + 1.0 : d.b;
+                            ctl.pass = need == kExact ? 0 : need == kRest ? d.k + 1 : d.k;
                         }
                         ctl.d = d;
                         ctl.z = z;
@@ -709,7 +721,7 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
             __syncthreads();
             if (ctl.cmd != kMass) break;
 
-            // ---- a mass pass: the share of every vector under (ma, mb) to my_sum, of the warp's part to s_mass
+            // ---- a mass pass: the sum of every vector's r_pass to my_sum, of the warp's part to s_mass
             double sum = 0.0;
             for (int ch = 0; ch < n_chunks; ++ch) {
                 const int vc = v0 + cap * ch, ve = min(vc + cap, v1);
@@ -772,7 +784,7 @@ verify_tree_kernel(const VerifyParams p, const int C, const int cap)
                         if (out) continue;
                         const float l = Logit<LT>::one(row_ptr + i);
                         double f = weight(!ctl.infinite ? l : l == CUDART_INF_F ? 0.f : -CUDART_INF_F, ctl.d, s_table);
-                        if (ctl.mb != 0.0) f = fmax(ctl.ma * f - ctl.mb * (double)q_row[i], 0.0);
+                        if (ctl.pass > 0) f = left_of(f, (double)q_row[i], ctl.pass, ctl.s[0], ctl);
                         if (!(f > 0.0)) continue;
                         next = i;                                  // (the last positive one so far)
                         acc += f;

@@ -91,3 +91,23 @@ def test_tokens_far_below_the_likeliest(L, draft):
     got, ref = verify(L, torch.tensor(x, device="cuda"), tokens, parent, u, 0.5, torch.tensor(q, device="cuda") if draft else None)
     assert (ref[1] == (1 if draft else 2)).all()
     assert all(np.array_equal(g, r) for g, r in zip(got, ref)), int((got[2] != ref[2]).sum())
+
+
+def test_several_rejections_that_leave_only_tokens_the_draft_has_not(L):
+    """The draft takes all of the likely token and more than the target has of the second; five tokens at e^-60 to e^-300 are
+    left after the first rejection, and share everything after the others too."""
+    rng = np.random.default_rng(3)
+    N, T, V = 128, 5, 40
+    x, q = np.full((N, T, V), -np.inf, np.float32), np.zeros((N, T, V), np.float32)
+    tokens, parent = np.zeros((N, T), np.int32), np.tile([-1, 0, 0, 0, 0], (N, 1)).astype(np.int32)
+    for i in range(N):
+        t = rng.choice(V, 7, replace=False)
+        x[i, :, t[0]], q[i, :, t[0]] = 0.0, 1.0
+        x[i, :, t[1]], q[i, :, t[1]] = -rng.uniform(35.0, 37.0), 1e-10
+        x[i, :, t[2:]] = -(60.0 + 240.0 * i / N) - rng.uniform(0.0, 2.0, (5, 1))
+        tokens[i, 1:] = rng.choice(np.setdiff1d(np.arange(V), t), 4, replace=False)
+    u = rng.random((N, T)).astype(np.float32)
+    for dtype in (torch.float32, torch.bfloat16):
+        got, ref = verify(L, torch.tensor(x, device="cuda").to(dtype), tokens, parent, u, 1.0, torch.tensor(q, device="cuda"))
+        assert (ref[1] == 1).all()
+        assert all(np.array_equal(g, r) for g, r in zip(got, ref)), int((got[2] != ref[2]).sum())
