@@ -379,7 +379,8 @@ int oasis_append_kv_layers(const oasis_dims_t *dims, int32_t n_layers, const voi
  * Tree attention: node t of request b attends to the history in the working set, i.e. the tokens i of every column c
  * with blk_tbl[b][h][c] = j >= 0 and j * 16 + i < seq_len[b] (seq_len [B] int32: tokens in the cache), to its
  * ancestors in the tree and to itself.
- *   out = softmax(scale * q K^T) V, bf16 tensor-core products with fp32 accumulation and fp32 softmax statistics.
+ *   out = softmax(scale * q K^T) V, bf16 tensor-core products with fp32 accumulation and fp32 softmax statistics; the
+ * softmax weights are rounded to bf16 for their product with V.
  *   q, out      [B][n_tree][Hq][128] bf16
  *   tree_kv, parent, n_nodes as above; hbm_pool, slot_tbl, blk_tbl, n_cols as in oasis_sparse_attn
  *   scale       finite and above zero
@@ -438,7 +439,7 @@ typedef enum { OASIS_F32 = 0, OASIS_BF16 = 1, OASIS_F16 = 2 } oasis_dtype_t;
  *   path        [B][max_path] int32: the nodes of the walk, node 0 first, then -1
  *   n_commit    [B] int32: how many they are; 0 for a request without nodes
  *   next_token  [B] int32: -1 for a request without nodes, and where every logit of the last node's row is left out
- * Comparisons and sums that decide are made in 64 bits; the result does not depend on the launch.
+ * Comparisons and sums that decide are made in 64 bits, weights to 1e-13 of themselves; the result does not depend on the launch.
  * 1 <= n_tree <= OASIS_MAX_TREE, 1 <= max_path <= n_tree, 1 <= vocab <= OASIS_MAX_VOCAB.
  */
 #define OASIS_MAX_VOCAB 4194304

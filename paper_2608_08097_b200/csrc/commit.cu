@@ -5,7 +5,8 @@
 // length, the count, the path and the two blocks' places are read once per warp, in two rounds of loads (lane i holds path
 // entry i; lanes 0 and 1 the places of the even and the odd block), then up to eight rows are in flight at a time.
 // Traffic per layer: 512 B read and 2 x 512 B written per (request, kept token, head).  A warp per row, which read all of that
-// for each of them, took 9.2 us for 32 layers of 16 requests x 8 heads x 4 tokens (28 MB); this 6.0 us (0.71 of the copy rate).  The launch may
+// for each of them, took 9.2 us for 32 layers of 16 requests x 8 heads x 4 tokens (28 MB); this 6.0 us (0.71 of the copy rate) with the
+// full-KV pool in HBM.  Into pinned host memory the link bounds it: 190 us, 49 GB/s (a copy takes 57).  The launch may
 // overlap the end of the previous kernel, for which every warp waits before its first load (8.3 -> 6.0 us a call, launched one
 // by one); letting its own successor start early costs more than it gains (7.2 instead of 6.4 us for 549 thread blocks).
 #include "common.cuh"

@@ -18,11 +18,16 @@
 //     size, neighbouring thread blocks that read the same entries at the same time, so that all but one come from L2.
 //   - Splits of a row merge inside a thread-block cluster where a cluster reaches far enough, else in a second launch.
 // Algorithmic traffic: 8 KiB per (request, KV head, visible column), 512 B per (node, KV head), plus Q, O and lse.
+// Precision: logits, the running maximum and sum and the accumulators are fp32.  The softmax weights go to P V as bf16 (half a
+// step, 2^-8 of a weight), because both operands of one tcgen05.mma kind::f16 have the same type and V is bf16; the sum that
+// divides them is of the unrounded ones.  Against 64 bits outputs are off by 0.2 % of their norm, 0.17 % with fp32 weights.
 // What bounds it (32 query and 8 KV heads, per call in a replayed graph): HBM for long lists, 86.4 us at 6.2 TB/s for 2
 // requests x 4,098 columns; HBM and some 7 us of launch, first loads, epilogue and merge for 16 requests x 130 columns
-// under 16 nodes, 28.2 us (4.9 TB/s); the tensor pipe and the softmax between its MMAs under 64 nodes, 42.8 us: an MMA of
-// 64 key columns takes as long as one of 128, and tiles of 128 keys, whose logits fit into the tensor memory only once
-// beside the accumulators, take 47.4 us.
+// under 16 nodes, 28.1 us (4.9 TB/s); under 64 nodes, 42.7 us, the softmax and the products between which a tile goes back and
+// forth: of its 2,050 cycles the exponential unit is busy for 1,024 (two softmax warps per scheduler, 64 ex2 each at 8 cycles) and
+// the tensor core for 1,280.  That is sixteen products of 128 x 64 x 16 with both operands in shared memory, 48 cycles each (32
+// of arithmetic; reading the operands' 6 KiB takes 48), and eight of 128 x 128 x 16 at 64.  Tiles of 128 keys, whose logits fit
+// into the tensor memory only once beside the accumulators, take 47.4 us.
 #include <cuda.h>
 #include <math_constants.h>
 

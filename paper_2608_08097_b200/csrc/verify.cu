@@ -16,8 +16,8 @@
 // All sums have a fixed order, so a result does not depend on timing.
 // What bounds it: the latency of the serial steps, not bytes.  16 requests, 64-node trees, 151,936 bf16 logits: 28.1 us, of
 // which (cycles) start 4,500, each node 9,000 (copy 2,000, fp32 pass 2,900, exchange 1,300, decision 2,700), the fp64 pass
-// 9,800, the search 1,700.  One request, greedy, 32,000 logits: 7.9 us.  16 requests, chains of 5 with draft distributions,
-// 128,256 fp32 logits: 39.7 us.  128 requests, 6 nodes, 50,257 fp16 logits: 31.2 us.  (In a graph.  The launch may overlap the
+// 9,800, the search 1,700.  One request, greedy, 32,000 logits: 7.7 us.  16 requests, chains of 5 with draft distributions,
+// 128,256 fp32 logits: 40.4 us.  128 requests, 6 nodes, 50,257 fp16 logits: 30.6 us.  (In a graph.  The launch may overlap the
 // end of the previous kernel, which it waits for before it reads any input: that saves 1.5 to 2.4 us a call where calls are
 // launched one by one.)  No launch_dependents here: it gains 0.5 to 1 us for one request and for 128 and costs the chains 3 us,
 // whose successors' thread blocks then take the places beside theirs.

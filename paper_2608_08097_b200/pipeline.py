@@ -132,6 +132,8 @@ class DecodeEngine:
     fused (default: whenever the library takes the shapes): a layer's attention and its scoring run
     as one launch on the foreground stream (`oasis_attn_and_score`); the summary updates of all
     layers are then issued at the start of the step on the prediction stream.
+    tree (append engines): the drafts of a step form trees (`step(..., tree=(parent, n_nodes))`); the nodes' keys and values stay
+    in the caller's tree buffer, and `commit` writes the kept path's after the step.  Steps are captured one per graph.
     transfer_streams: consecutive layers' gathers alternate between this many transfer streams (useful
     when the pool is in host memory: one gather's requests are in flight while the previous one's last
     ones come back).

@@ -198,6 +198,20 @@ def test_padding_nodes_do_not_choose_the_working_set_in_a_graph(L):
     assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+def test_priming_reads_no_padding_node(L):
+    """The first working set, chosen by `prime` from queries whose padding rows hold NaN, equals that from clean ones."""
+    nodes, got = [4, 1, 2], []
+    for fill in (0.0, math.nan):
+        loop = Loop([300, 200, 330], 3, 8, 2, 4, 2, 32, 5, 5, seed=8)
+        q = [loop.randn(3, 4, 8, 128) for _ in range(2)]
+        for t in q:
+            for b, n in enumerate(nodes):
+                t[b, n:] = fill
+        loop.eng.prime(q, loop.seq // 16, loop.seq, n_nodes=i32(nodes))
+        got.append([t.clone() for t in (*loop.eng.resident, *[x.sel for x in loop.eng.layers])])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 # ---- requests that keep nothing ------------------------------------------------------------------------------------
 @pytest.mark.parametrize("nodes", [0, 5], ids=["sits out", "thrown away"])
 @pytest.mark.parametrize("graph", [False, True], ids=["eager", "graph"])
