@@ -382,7 +382,8 @@ class DecodeEngine:
         tree=True): (parent, n_nodes) of the step's draft trees; new_kv then holds the nodes' keys and values, and
         `commit` follows the step.  The next working set is predicted from a request's drafts (its first 128 // group of
         them; node 0 where it has none); rows of padding nodes take no part, and a request without nodes selects nothing: its
-        working set stays."""
+        working set stays.  The engine's streams do not wait for the caller's: the inputs are complete, or `main` and `pred` have
+        been made to wait for them."""
         ms, n = self.main, self.n_layers
         if self.tree != (tree is not None):
             raise ValueError("tree must be given exactly when the engine was built with tree=True")

@@ -33,13 +33,13 @@ def f64(t):
 class Loop:
     """An engine over random histories; `hist` is the truth, one [tokens][Hkv][2][128] tensor per layer and request."""
 
-    def __init__(self, lens, B, Hq, Hkv, T, layers, mb, k, cap, seed):
+    def __init__(self, lens, B, Hq, Hkv, T, layers, mb, k, cap, seed, **options):
         from paper_2608_08097_b200 import pipeline
         self.g, self.rng = torch.Generator(device="cuda"), np.random.default_rng(seed)
         self.g.manual_seed(seed)
         self.B, self.Hq, self.Hkv, self.T, self.layers, self.k = B, Hq, Hkv, T, layers, k
         self.lens = list(lens)
-        self.eng = pipeline.DecodeEngine(B, Hq, Hkv, mb, k, T, layers, mode="delta", cap=cap, append=True, tree=True)
+        self.eng = pipeline.DecodeEngine(B, Hq, Hkv, mb, k, T, layers, mode="delta", cap=cap, append=True, tree=True, **options)
         self.hist = [[self.randn(n, Hkv, 2, 128) for n in lens] for _ in range(layers)]
         for l in range(layers):
             kv = torch.zeros((B * mb, Hkv, 2, 16, 128), dtype=torch.bfloat16)
@@ -270,3 +270,44 @@ def test_more_layers_than_one_commit_takes(L):
         loop.check_no_block_twice()
     with pytest.raises(ValueError, match="66 layers"):
         loop.eng.commit_plan(loop.tree_kv[:65])
+
+
+@pytest.mark.parametrize("options", [{}, dict(transfer_group=2, wait_group=1, transfer_streams=2), dict(transfer_kind="bulk", wait_group=2, plan_stream="side")],
+                         ids=["default", "grouped", "bulk"])
+def test_a_loop_without_host_synchronisation(L, options):
+    """Six steps whose order rests on streams and events alone give the bits of the same steps made one by one."""
+    def run(sync):
+        torch.cuda.synchronize()
+        g = torch.Generator(device="cuda")
+        g.manual_seed(9)
+        B, T, layers, mb, k = 3, 7, 3, 32, 6
+        loop = Loop([200, 310, 45], B, 8, 2, T, layers, mb, k, k, seed=9, **options)
+        eng, now = loop.eng, torch.cuda.current_stream()
+        parent, path = i32([[-1, 0, 1, 2, 3, 4, 5]] * B), i32([list(range(T))] * B)
+        counts = [i32(n) for n in ([7, 3, 0], [1, 7, 5], [7, 7, 7], [0, 4, 7], [7, 1, 2], [7, 7, 7])]
+        keeps = [i32(n) for n in ([6, 2, 0], [1, 7, 0], [3, 5, 7], [0, 4, 6], [7, 0, 2], [1, 2, 3])]
+        seq, before, got = loop.seq, loop.seq // 16, []
+        for s, (nodes, keep) in enumerate(zip(counts, keeps)):
+            q = [torch.randn((B, T, 8, 128), generator=g, device="cuda").to(torch.bfloat16) for _ in range(layers)]
+            kv = [torch.randn((B, T, 2, 2, 128), generator=g, device="cuda").to(torch.bfloat16) for _ in range(layers)]
+            full, nxt = seq // 16, torch.empty_like(seq)
+            if sync:
+                torch.cuda.synchronize()
+            for st in (eng.main, eng.pred):
+                st.wait_stream(now)
+            eng.step(q, seq, before, full - before, full, seq, step_stamp=s + 1, new_kv=kv, sel_log=loop.sel, tree=(parent, nodes))
+            eng.join()
+            now.wait_stream(eng.main)
+            if sync:
+                torch.cuda.synchronize()
+            got += [x.clone() for x in loop.sel]
+            got += [torch.where((torch.arange(T, device="cuda") < nodes[:, None])[..., None, None], x.out, 0) for x in eng.layers]
+            eng.commit(eng.commit_plan(kv), path, keep, seq, next_len=nxt)
+            got += [x.clone() for x in eng.resident]
+            seq, before = nxt, full
+        torch.cuda.synchronize()
+        return got + [x.cpu() for x in eng.kv]
+
+    want = run(True)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(want, run(False)))
