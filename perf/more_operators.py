@@ -76,7 +76,7 @@ def draw(rng):
         group, kv = rng.choice([1, 2, 3, 4, 5, 8, 16]), rng.choice([1, 2, 3, 4, 8])
         c = dict(op="attn", batch=_log(rng, 1, 48), q_heads=group * kv, kv_heads=kv, tokens=rng.choice([1, 1, rng.randint(1, min(16, 128 // group))]),
                  context=_log(rng, 1, 131072), budget=_log(rng, 4, 8192), ragged=rng.random() < 0.7)
-        while work(c)["flops"] > 1e10 or work(c)["bytes"] > 300e6 or c["batch"] * kv * min(c["budget"], c["context"] // BLK + 1) > 131072:
+        while work(c)["flops"] > 1e10 or work(c)["bytes"] > 300e6 or c["batch"] * kv * c["budget"] > 131072:
             c["batch" if c["batch"] > 1 else "budget"] //= 2
         return c
     group, kv = rng.choice([1, 2, 4, 5, 8]), rng.choice([1, 2, 4, 8])
