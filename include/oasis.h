@@ -238,7 +238,7 @@ size_t oasis_attn_workspace_bytes(const oasis_dims_t *dims, int32_t n_q_tokens,
  * are read, and scores written, while that previous launch may still be running, and the launch after this
  * one may start as soon as this one has begun.  So the previous launch on `stream` must neither produce
  * those inputs nor still use `scores` (an oasis_attn_and_score of another layer is the intended
- * predecessor; it, oasis_sparse_attn, oasis_tree_attn and their merge launches are the launches of this library that let
+ * predecessor; it, oasis_sparse_attn, oasis_tree_attn, oasis_packed_attn and their merge launches are the launches of this library that let
  * a successor start early); separate such producers and consumers from this call by an event on another
  * stream or by another launch in between.  Everything the attention phase touches (q,
  * hbm_pool, the tables, out, lse, workspace) is ordered as usual.
@@ -487,6 +487,116 @@ int oasis_commit_kv_layers_after_select(const oasis_dims_t *dims, int32_t n_laye
                                         const int32_t *const *slot_tbls, int32_t *const *blk_tbls, int32_t n_cols,
                                         int32_t local_col, void *const *hbm_pools, void *const *host_kvs,
                                         const int32_t *n_candidates, int32_t *next_len, void *stream);
+
+/*
+ * A cache in 4 bits (no counterpart in the paper, whose cache is bf16; its step is bound by the host link and its attention by
+ * HBM, and a packed entry is 2,304 bytes on both instead of 8,192).  The packed entry of one (block, KV head):
+ *   [0, 1024)      key codes: dims 32c .. 32c + 31 of token i in 16 bytes at 256 c + 16 i
+ *   [1024, 2048)   value codes: the 16 tokens of dim d in 8 bytes at 1024 + 8 d
+ *   [2048, 2176)   key scales: one byte for dims 16g .. 16g + 15 of token i at 2048 + 8 i + g
+ *   [2176, 2304)   value scales: one byte for the 16 tokens of dim d at 2176 + d
+ * Eight codes are a little-endian 32-bit word: code 2p in bits 4p .. 4p + 3, code 2p + 1 in bits 16 + 4p .. 16 + 4p + 3.
+ * A code c with the scale byte b stands for (c - 8) * s, s = (1 + (b & 7) / 8) * 2^((b >> 3) - 20): exact in bf16.
+ * Packing a group of 16 values x with the largest magnitude a: s is a / 7 rounded to four significant bits (ties to even) and
+ * taken into [2^-20, 3840]; c - 8 is the whole number within +-7 nearest to x / s (halfway: the one nearer to zero).  NaN packs
+ * as zero, infinity as the group's largest value.  Every comparison is exact: the result does not depend on the launch.
+ * A packed full-KV pool is [n_phys_blocks][n_kv_heads] such entries, a packed working-set pool [n_slots] of them.  Only whole
+ * blocks are packed; the block that still grows stays in the bf16 local window.
+ */
+#define OASIS_PACKED_BYTES 2304
+
+/*
+ * Packs blocks j = first_block[b] .. first_block[b] + n_blocks[b] - 1 (those in [0, max_blocks)) of every request and KV head:
+ * entry (src_table[b][j], h) of kv_pool -> packed entry (block_table[b][j], h).
+ *   kv_pool      full-KV pool of bf16 entries (device memory, or mapped pinned host memory)
+ *   src_table, block_table   [B][max_blocks] int32 (device); may be the same
+ *   packed       packed full-KV pool (device memory, or mapped pinned host memory), 16-byte aligned
+ *   summaries    [B][Hkv][max_blocks][2][128] bf16 or NULL: the blocks' summaries as oasis_build_summaries makes them, from
+ *                the bf16 keys
+ *   max_new_blocks   host-side upper bound of n_blocks[b]; sizes the launch (blocks past it are not packed)
+ */
+int oasis_pack_blocks(const oasis_dims_t *dims, const void *kv_pool, const int32_t *src_table, const int32_t *first_block,
+                      const int32_t *n_blocks, int32_t max_new_blocks, void *packed, const int32_t *block_table,
+                      void *summaries, void *stream);
+
+/*
+ * The same for several layers at once, from the local window: block j's source is entry slot_tbl[b][h][local_col + (j & 1)] of
+ * hbm_pool (a negative slot: skipped).  For a block that has just filled up, before a later one takes its column.
+ *   hbm_pools, slot_tbls, packed, block_tables   host arrays of n_layers <= OASIS_MAX_APPEND_LAYERS device pointers (packed: or
+ *                mapped pinned host memory);  summaries: such an array, whose members may be NULL, or NULL
+ *   slot_tbls[l] [B][Hkv][n_cols] int32 (device), local_col + 2 <= n_cols;  max_new_blocks <= 2
+ */
+int oasis_pack_local_layers(const oasis_dims_t *dims, int32_t n_layers, const void *const *hbm_pools,
+                            const int32_t *const *slot_tbls, int32_t n_cols, int32_t local_col, const int32_t *first_block,
+                            const int32_t *n_blocks, int32_t max_new_blocks, void *const *packed,
+                            const int32_t *const *block_tables, void *const *summaries, void *stream);
+
+/* The dense -> sparse hand-over into a packed pool: oasis_offload_blocks with packed entries (whole blocks only). */
+int oasis_offload_blocks_packed(const oasis_dims_t *dims, const void *dense_k, const void *dense_v, const int32_t *gpu_table,
+                                const int32_t *block_table, const int32_t *first_block, const int32_t *n_blocks,
+                                int32_t max_new_blocks, void *packed, void *summaries, void *stream);
+
+/* out[i] = packed entry idx[i] as a bf16 entry [2][16][128], for i < n; idx[i] < 0: skipped.  idx [n] int64 (device). */
+int oasis_unpack_blocks(const void *packed, const int64_t *idx, int32_t n, void *out, void *stream);
+
+/* Step 3 for packed entries: oasis_stage_blocks_layers with 2,304-byte entries (same arguments and rules). */
+int oasis_stage_packed_layers(int32_t n_layers, const void *const *host_packed, const int64_t *const *idx,
+                              const int32_t *const *slots, int32_t n, void *const *packed_pools, int32_t max_ctas,
+                              void *stream);
+
+/*
+ * Step 4 over a packed working set: columns c < local_col of blk_tbl name packed entries (slot_tbl[b][h][c] of packed_pool), the
+ * others, at most OASIS_MAX_LOCAL_COLS, bf16 entries (slot_tbl[b][h][c] of hbm_pool: the local window).  Query token t of request
+ * b sits at position seq_len[b] + t; the keys are the tokens i of every column with blk_tbl[b][h][c] = j >= 0 and position
+ * j * 16 + i <= seq_len[b] + t.
+ *   out = softmax(scale * q K^T) V over the values that the entries stand for, bf16 tensor-core products with fp32 accumulation
+ * and fp32 softmax statistics; the softmax weights are rounded to bf16 for their product with V.
+ *   q, out       [B][n_q_tokens][Hq][128] bf16;  n_q_tokens * (Hq/Hkv) may not exceed 128
+ *   slot_tbl, blk_tbl   [B][Hkv][n_cols] int32 (device)
+ *   packed_pool  may be NULL if local_col is 0, hbm_pool if local_col is n_cols
+ *   scale        finite and above zero
+ *   lse          optional [B][n_q_tokens][Hq] fp32: natural-log sum of exponentials
+ *   workspace    device scratch of at least oasis_packed_attn_workspace_bytes() bytes, 16-byte aligned; contents undefined before
+ *                and after; may be NULL when that function returns 0.  Calls that may run at the same time (other streams,
+ *                captured graphs that are replayed together) need a workspace each.
+ * A query row that sees no key yields zeros (lse = -inf).  Positions that no token of the request sees may hold anything,
+ * infinities and NaN included; every visible row of a bf16 entry must be finite (a packed entry always is).
+ * A launch of this call lets the next launch of the stream start early (see oasis_attn_and_score).
+ */
+#define OASIS_MAX_LOCAL_COLS 8
+int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_t n_q_tokens, const void *packed_pool,
+                      const void *hbm_pool, const int32_t *slot_tbl, const int32_t *blk_tbl, int32_t n_cols,
+                      int32_t local_col, const int32_t *seq_len, float scale, void *out, float *lse, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/* Scratch bytes oasis_packed_attn needs for these shapes on the current device. */
+size_t oasis_packed_attn_workspace_bytes(const oasis_dims_t *dims, int32_t n_q_tokens, int32_t n_cols, int32_t local_col);
+
+/*
+ * Rotary positions (no counterpart in the paper, which takes rotated queries and keys as given): from the rows of a fused
+ * projection to what the attention and the KV append read.  Row (b, t) holds the Hq query heads, then the Hkv key heads, then the
+ * Hkv value heads, 128 elements each.  With a = position * freqs[i], i < rot_dim / 2, every pair (x, x') of a query or key head
+ * becomes factor * (x cos a - x' sin a), factor * (x' cos a + x sin a); the pairs are
+ *   interleaved = 0   dims i and i + rot_dim / 2        interleaved = 1   dims 2i and 2i + 1
+ * Dims from rot_dim on and the values are copied.  Angles are reduced in 64 bits; products and sums are fp32, rounded once to bf16.
+ *   qkv          element (b, t, a, x) at qkv[b * qkv_batch_stride + t * qkv_token_stride + a * 128 + x], of type qkv_type
+ *                (oasis_dtype_t); strides in elements, multiples of 8, at least (Hq + 2 Hkv) * 128 (not looked at where there is
+ *                one request or one token); 16-byte aligned
+ *   positions    [B][n_tokens] int32, or NULL: position seq_len[b] + t, or, with parent (as for oasis_tree_attn), seq_len[b] +
+ *                the number of t's ancestors
+ *   seq_len      [B] int32, may be NULL with positions
+ *   parent       [B][n_tokens] int32 or NULL; goes with n_nodes, without positions, n_tokens <= OASIS_MAX_TREE
+ *   n_nodes      [B] int32 or NULL: rows t >= n_nodes[b] of q and kv are left as they were
+ *   freqs        [rot_dim / 2] fp64 (device), in radians per position
+ *   rot_dim      even, 2 to 128
+ *   q            [B][n_tokens][Hq][128] bf16;  kv [B][n_tokens][Hkv][2][128] bf16, key row then value row (new_kv of
+ *                oasis_append_kv, tree_kv of oasis_tree_attn).  They may not share memory with qkv.
+ * Of dims the batch and the head counts are used.
+ */
+int oasis_rotate_qkv(const oasis_dims_t *dims, const void *qkv, int32_t qkv_type, int64_t qkv_batch_stride,
+                     int64_t qkv_token_stride, int32_t n_tokens, const int32_t *positions, const int32_t *seq_len,
+                     const int32_t *parent, const int32_t *n_nodes, const double *freqs, int32_t rot_dim,
+                     int32_t interleaved, float factor, void *q, void *kv, void *stream);
 
 /*
  * Head-union block set (Sec. 4.4.1, partial transfer: per layer the per-head selected sets are

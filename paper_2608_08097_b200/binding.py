@@ -27,7 +27,9 @@ SYMBOLS = ("oasis_build_summaries", "oasis_score_blocks", "oasis_select_topk",
            "oasis_local_window", "oasis_append_kv", "oasis_append_kv_layers", "oasis_stage_blocks_layers", "oasis_stage_blocks_bulk",
            "oasis_set_extents", "oasis_bounds_checked",
            "oasis_score_tree", "oasis_tree_attn", "oasis_tree_attn_workspace_bytes", "oasis_verify_tree", "oasis_commit_kv", "oasis_commit_kv_layers",
-           "oasis_commit_kv_layers_after_select")
+           "oasis_commit_kv_layers_after_select",
+           "oasis_pack_blocks", "oasis_pack_local_layers", "oasis_offload_blocks_packed", "oasis_unpack_blocks", "oasis_stage_packed_layers",
+           "oasis_packed_attn", "oasis_packed_attn_workspace_bytes", "oasis_rotate_qkv")
 
 
 class OasisError(RuntimeError):
@@ -126,6 +128,18 @@ def lib():
         L.oasis_commit_kv_layers.restype = ctypes.c_int
         L.oasis_commit_kv_layers_after_select.argtypes = [dp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
         L.oasis_commit_kv_layers_after_select.restype = ctypes.c_int
+        L.oasis_pack_blocks.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+        L.oasis_pack_local_layers.argtypes = [dp, i32, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
+        L.oasis_offload_blocks_packed.argtypes = [dp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.oasis_unpack_blocks.argtypes = [vp, vp, i32, vp, vp]
+        L.oasis_stage_packed_layers.argtypes = [i32, vp, vp, vp, i32, vp, i32, vp]
+        L.oasis_packed_attn.argtypes = [dp, vp, i32, vp, vp, vp, vp, i32, i32, vp, f32, vp, vp, vp, sz, vp]
+        L.oasis_rotate_qkv.argtypes = [dp, vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        for name in ("oasis_pack_blocks", "oasis_pack_local_layers", "oasis_offload_blocks_packed", "oasis_unpack_blocks",
+                     "oasis_stage_packed_layers", "oasis_packed_attn", "oasis_rotate_qkv"):
+            getattr(L, name).restype = ctypes.c_int
+        L.oasis_packed_attn_workspace_bytes.argtypes = [dp, i32, i32, i32]
+        L.oasis_packed_attn_workspace_bytes.restype = sz
         L.oasis_set_error_word.argtypes = [vp]
         L.oasis_set_error_word.restype = ctypes.c_int
         L.oasis_last_error.restype = ctypes.c_char_p
@@ -429,7 +443,8 @@ _call = None
 
 
 def _calls():
-    """The native calls of the draft-tree operators (tensor checks and the call of the C ABI), bound to the loaded library."""
+    """The native calls of the draft-tree operators, the packed cache and the rotary positions (tensor checks and the call of
+    the C ABI), bound to the loaded library."""
     global _call
     if _call is None:
         L = lib()
@@ -437,7 +452,9 @@ def _calls():
             from . import _call as native
         except ImportError as e:
             raise OasisError("_call.so cannot be loaded: build it with `python -m paper_2608_08097_b200.build` (%s)" % e) from e
-        native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.oasis_tree_attn, L.oasis_verify_tree, L.oasis_commit_kv_layers_after_select)))
+        native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.oasis_tree_attn, L.oasis_verify_tree, L.oasis_commit_kv_layers_after_select, L.oasis_pack_blocks, L.oasis_unpack_blocks,
+            L.oasis_packed_attn, L.oasis_rotate_qkv)))
         _call = native
     return _call
 
@@ -545,3 +562,108 @@ def commit_kv(dims, tree_kv, path, n_commit, seq_len, block_table, slot_tbl, blk
     """commit_kv_layers for one layer."""
     commit_kv_layers(CommitPlan(dims, [tree_kv], [block_table], [slot_tbl], [blk_tbl], local_col, [hbm_pool], [host_kv]),
                      path, n_commit, seq_len, next_len=next_len, stream=stream)
+
+
+# ---- a cache in 4 bits: packing, gather, attention --------------------------------------------------------------------
+PACKED_BYTES = 2304
+
+
+def pack_blocks(dims, kv_pool, src_table, first_block, n_blocks, max_new_blocks, packed, block_table, summaries=None, stream=None):
+    """Packs blocks first_block[b] .. first_block[b] + n_blocks[b] - 1 of every request: entry (src_table[b][j], h) of kv_pool ->
+    packed entry (block_table[b][j], h).  packed: uint8 [...][2304], device or pinned host memory; summaries
+    [B][Hkv][max_blocks][2][128]: also the blocks' minima and maxima, of the bf16 keys."""
+    rc = (_call or _calls()).pack_blocks(_cdims(dims), kv_pool, src_table, first_block, n_blocks, max_new_blocks, packed, block_table,
+                                         summaries, None if stream is None else _handle(stream))
+    if rc:
+        _check(rc, "oasis_pack_blocks")
+
+
+def unpack_blocks(packed, idx, out, stream=None):
+    """out[i] = packed entry idx[i] as a bf16 entry (idx < 0: left as it was); idx [n] int64, out [n][2][16][128]."""
+    rc = (_call or _calls()).unpack_blocks(packed, idx, out, None if stream is None else _handle(stream))
+    if rc:
+        _check(rc, "oasis_unpack_blocks")
+
+
+def _layer_list(tensors, kind, shape, name):
+    """An array of the addresses of one tensor per layer (kinds as in the native `addresses`)."""
+    got = _calls().addresses(list(tensors), kind, shape, name)
+    return (ctypes.c_void_p * max(len(tensors), 1)).from_buffer_copy(got.ljust(8, b"\0"))
+
+
+def pack_local_layers(dims, hbm_pools, slot_tbls, local_col, first_block, n_blocks, max_new_blocks, packed, block_tables, summaries=None,
+                      stream=None):
+    """Packs blocks that have just filled up from the local windows of several layers: lists with one tensor per layer (summaries:
+    None, or a list in which a layer may be None).  max_new_blocks is at most 2."""
+    n = len(hbm_pools)
+    summaries = [None] * n if summaries is None else list(summaries)
+    if not all(len(x) == n for x in (slot_tbls, packed, block_tables, summaries)):
+        raise ValueError("one tensor per layer is needed in every list")
+    if not 1 <= n <= MAX_APPEND_LAYERS:
+        raise ValueError("%d layers outside [1, %d]" % (n, MAX_APPEND_LAYERS))
+    B, Hkv, mb, n_cols = dims.batch, dims.n_kv_heads, dims.max_blocks, int(slot_tbls[0].shape[-1])
+    lists = (_layer_list(hbm_pools, 2, (), "hbm_pools"), _layer_list(slot_tbls, 1, (B, Hkv, n_cols), "slot_tbls"),
+             _layer_list(packed, 4, (), "packed"), _layer_list(block_tables, 1, (B, mb), "block_tables"),
+             _layer_list(summaries, 6, (B, Hkv, mb, 2, 128), "summaries"))
+    ends = [_layer_list([t], 1, (B,), name)[0] for t, name in ((first_block, "first_block"), (n_blocks, "n_blocks"))]
+    d = dims.c()
+    _check(lib().oasis_pack_local_layers(ctypes.byref(d), n, lists[0], lists[1], n_cols, int(local_col), ends[0], ends[1],
+                                         int(max_new_blocks), lists[2], lists[3], lists[4], _stream(stream)), "oasis_pack_local_layers")
+
+
+def offload_blocks_packed(dims, dense_k, dense_v, gpu_table, block_table, first_block, n_blocks, max_new_blocks, packed, summaries=None,
+                          stream=None):
+    """The dense -> sparse hand-over into a packed pool: dense_k / dense_v [P_gpu][Hkv][16][128] -> packed entries (and the blocks'
+    summaries when given)."""
+    B, Hkv, mb = dims.batch, dims.n_kv_heads, dims.max_blocks
+    if tuple(dense_k.shape[1:]) != (Hkv, 16, 128) or dense_v.shape != dense_k.shape:
+        raise ValueError("dense_k and dense_v: expected shape [P][%d][16][128], got %s and %s" % (Hkv, tuple(dense_k.shape), tuple(dense_v.shape)))
+    one = lambda t, kind, shape, name: _layer_list([t], kind, shape, name)[0]
+    d = dims.c()
+    _check(lib().oasis_offload_blocks_packed(
+        ctypes.byref(d), one(dense_k, 0, tuple(dense_k.shape), "dense_k"), one(dense_v, 0, tuple(dense_v.shape), "dense_v"),
+        one(gpu_table, 1, (B, mb), "gpu_table"), one(block_table, 1, (B, mb), "block_table"), one(first_block, 1, (B,), "first_block"),
+        one(n_blocks, 1, (B,), "n_blocks"), int(max_new_blocks), one(packed, 4, (), "packed"),
+        one(summaries, 6, (B, Hkv, mb, 2, 128), "summaries"), _stream(stream)), "oasis_offload_blocks_packed")
+
+
+def stage_packed_layers(host_packed, idx, slots, n, packed_pools, max_ctas=0, stream=None):
+    """stage_blocks_layers for packed entries: host_packed[l] entries idx[l] -> packed_pools[l] slots slots[l], lists of length n."""
+    nl = len(host_packed)
+    if not all(len(x) == nl for x in (idx, slots, packed_pools)):
+        raise ValueError("one tensor per layer is needed in every list")
+    for t in (*idx, *slots):
+        if t.numel() < n:
+            raise ValueError("the lists must have n = %d elements, got %d" % (n, t.numel()))
+    arr = ctypes.c_void_p * max(nl, 1)
+    mk = lambda ts, dt, nm: arr(*[_ptr(t, dt, nm).value for t in ts])
+    _check(lib().oasis_stage_packed_layers(
+        nl, _layer_list(host_packed, 4, (), "host_packed"), mk(idx, torch.int64, "idx"), mk(slots, torch.int32, "slots"), int(n),
+        _layer_list(packed_pools, 4, (), "packed_pools"), int(max_ctas), _stream(stream)), "oasis_stage_packed_layers")
+
+
+def packed_attn_workspace_bytes(dims, n_q_tokens, n_cols, local_col) -> int:
+    d = dims.c()
+    return int(lib().oasis_packed_attn_workspace_bytes(ctypes.byref(d), int(n_q_tokens), int(n_cols), int(local_col)))
+
+
+def packed_attn(dims, q, packed_pool, hbm_pool, slot_tbl, blk_tbl, local_col, seq_len, scale, out, lse=None, workspace=None, stream=None):
+    """Attention over a packed working set: columns below local_col of blk_tbl name packed entries (slots of packed_pool, uint8
+    [...][2304]), the others (at most 8) bf16 entries (slots of hbm_pool, the local window).  q, out [B][T][Hq][128]; query
+    token t sees positions up to seq_len[b] + t.  `workspace`: packed_attn_workspace_bytes() bytes where that is not zero."""
+    rc = (_call or _calls()).packed_attn(_cdims(dims), q, packed_pool, hbm_pool, slot_tbl, blk_tbl, local_col, seq_len, scale, out, lse,
+                                         workspace, None if stream is None else _handle(stream))
+    if rc:
+        _check(rc, "oasis_packed_attn")
+
+
+# ---- rotary positions -------------------------------------------------------------------------------------------------
+def rotate_qkv(dims, qkv, table, q, kv, positions=None, seq_len=None, parent=None, n_nodes=None, stream=None):
+    """Rotates a fused projection's rows: qkv [B][T][(Hq + 2 Hkv) * 128] (fp32, bf16 or fp16; rows dense, any row and batch
+    stride that is a multiple of 8) -> q [B][T][Hq][128] and kv [B][T][Hkv][2][128] (bf16), with the frequencies of `table`, a
+    rotary.RotaryTable.  Positions: positions [B][T] int32, or seq_len[b] + t, or, with parent [B][T] (and n_nodes), seq_len[b] +
+    the depth of node t.  Rows t >= n_nodes[b] are left as they were."""
+    rc = (_call or _calls()).rotate_qkv(_cdims(dims), qkv, table.freqs, table.rot_dim, table.interleaved, table.factor, q, kv, positions,
+                                        seq_len, parent, n_nodes, None if stream is None else _handle(stream))
+    if rc:
+        _check(rc, "oasis_rotate_qkv")

@@ -77,6 +77,53 @@ stage_blocks_layers_kernel(const __grid_constant__ StageLayers ly, int n, const 
     }
 }
 
+// Packed entries (2,304 bytes = 144 16-byte units): a warp takes four list positions at a time, so that 9 KiB are in flight
+// like the 8 KiB of a bf16 entry.  Of every entry a lane moves four units; the last sixteen units of two entries fill a fifth
+// warp-wide load.  Algorithmic traffic: 2,304 B over the host link and 2,304 B written per request.
+__global__ void __launch_bounds__(kStageWarps * 32)
+stage_packed_layers_kernel(const __grid_constant__ StageLayers ly, int n, const Bounds bd)
+{
+    const int l = blockIdx.y, lane = threadIdx.x & 31;
+    const long long warps_total = (long long)gridDim.x * kStageWarps;
+    for (long long i0 = ((long long)blockIdx.x * kStageWarps + (threadIdx.x >> 5)) * 4; i0 < n; i0 += warps_total * 4) {
+        long long from = -1;                                // lane k < 4: the entry and the slot of list position i0 + k
+        int to = 0;
+        if (lane < 4 && i0 + lane < n) {
+            from = ly.idx[l][i0 + lane];
+            to = ly.slots[l][i0 + lane];
+            if (from >= 0 && (!in_range(from, bd.n_entries, bd, kErrHostEntry) || !in_range(to, bd.n_slots, bd, kErrSlot))) from = -1;
+        }
+        uint4 v[18];
+        const uint8_t *src[4];
+        uint8_t *dst[4];
+        bool ok[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const long long f = __shfl_sync(0xffffffffu, from, k);
+            ok[k] = f >= 0;
+            src[k] = ly.host_kv[l] + (ok[k] ? f : 0) * OASIS_PACKED_BYTES;
+            dst[k] = ly.pool[l] + (long long)__shfl_sync(0xffffffffu, to, k) * OASIS_PACKED_BYTES;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (ok[k]) v[4 * k + c] = ld_stream_v4(src[k] + c * 512 + lane * 16);
+        }
+        const bool second = lane >= 16;
+        const int tail = 2048 + (lane & 15) * 16;
+#pragma unroll
+        for (int k = 0; k < 4; k += 2)
+            if (second ? ok[k + 1] : ok[k]) v[16 + k / 2] = ld_stream_v4((second ? src[k + 1] : src[k]) + tail);
+        asm volatile("" ::: "memory");                      // keeps the stores behind all loads
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (ok[k]) *reinterpret_cast<uint4 *>(dst[k] + c * 512 + lane * 16) = v[4 * k + c];
+#pragma unroll
+        for (int k = 0; k < 4; k += 2)
+            if (second ? ok[k + 1] : ok[k]) *reinterpret_cast<uint4 *>((second ? dst[k + 1] : dst[k]) + tail) = v[16 + k / 2];
+    }
+}
+
 // The several-layers gather through the copy unit: one thread per CTA moves its share of the list as 8 KiB bulk
 // copies, CPU pool -> shared memory -> working-set pool, one buffer per CTA; no warp spends an instruction on the
 // bytes, and the CTA (32 threads, 8 KiB of shared memory) fits on an SM beside the fused attention + scoring CTA.
@@ -167,6 +214,38 @@ extern "C" int oasis_stage_blocks_layers(int32_t n_layers, const void *const *ho
     if (grid > max_ctas) grid = max_ctas;
     prefer_max_shared_carveout(stage_blocks_layers_kernel);
     stage_blocks_layers_kernel<<<dim3((unsigned)grid, (unsigned)n_layers), kStageWarps * 32, 0, (cudaStream_t)stream>>>(ly, n, bounds());
+    return check_launch(who);
+}
+
+extern "C" int oasis_stage_packed_layers(int32_t n_layers, const void *const *host_packed, const int64_t *const *idx,
+                                         const int32_t *const *slots, int32_t n, void *const *packed_pools,
+                                         int32_t max_ctas_arg, void *stream)
+{
+    using namespace oasis;
+    const char *who = "oasis_stage_packed_layers";
+    if (n < 0) return fail(OASIS_ERR_INVALID_ARG, "%s: n %d < 0", who, n);
+    if (n_layers < 0 || n_layers > OASIS_MAX_STAGE_LAYERS)
+        return fail(OASIS_ERR_INVALID_ARG, "%s: n_layers %d outside [0, %d]", who, n_layers, OASIS_MAX_STAGE_LAYERS);
+    if (max_ctas_arg < 0) return fail(OASIS_ERR_INVALID_ARG, "%s: max_ctas %d < 0", who, max_ctas_arg);
+    if (n == 0 || n_layers == 0) return OASIS_OK;
+    if (!host_packed || !idx || !slots || !packed_pools) return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
+    StageLayers ly = {};
+    for (int l = 0; l < n_layers; ++l) {
+        if (!host_packed[l] || !idx[l] || !slots[l] || !packed_pools[l])
+            return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer for layer %d", who, l);
+        if (!aligned16(host_packed[l]) || !aligned16(packed_pools[l]))
+            return fail(OASIS_ERR_INVALID_ARG, "%s: host_packed and packed_pools must be 16-byte aligned (layer %d)", who, l);
+        ly.host_kv[l] = (const uint8_t *)host_packed[l];
+        ly.idx[l] = (const long long *)idx[l];
+        ly.slots[l] = slots[l];
+        ly.pool[l] = (uint8_t *)packed_pools[l];
+    }
+    int max_ctas = (max_ctas_arg > 0 ? max_ctas_arg : kStageDefaultCtas) / n_layers;
+    if (max_ctas < 1) max_ctas = 1;
+    int grid = (int)((n + 4ll * kStageWarps - 1) / (4 * kStageWarps));
+    if (grid > max_ctas) grid = max_ctas;
+    prefer_max_shared_carveout(stage_packed_layers_kernel);
+    stage_packed_layers_kernel<<<dim3((unsigned)grid, (unsigned)n_layers), kStageWarps * 32, 0, (cudaStream_t)stream>>>(ly, n, bounds());
     return check_launch(who);
 }
 
