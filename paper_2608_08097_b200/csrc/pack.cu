@@ -184,9 +184,11 @@ unpack_blocks_kernel(const uint8_t *__restrict__ packed, const long long *__rest
     for (int i = 0; i < 8; ++i) {
         const int token = odd + 2 * i;
         const uint32_t w = *reinterpret_cast<const uint32_t *>(sm + (chunk >> 2) * 256 + token * 16 + (chunk & 3) * 4);
-        uint32_t s2, c2, o[4];
-        scale_pair(sm[kPackedKScale + token * 8 + (chunk >> 1)] * 0x00010001u, s2, c2);
-        dequant_word(w, s2, c2, o);
+        const float sc = scale_value(sm[kPackedKScale + token * 8 + (chunk >> 1)]);
+        uint32_t o[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            o[p] = pack_bf16x2((float)((int)((w >> (4 * p)) & 15u) - 8) * sc, (float)((int)((w >> (16 + 4 * p)) & 15u) - 8) * sc);
         *reinterpret_cast<uint4 *>(dst + i * 512) = make_uint4(o[0], o[1], o[2], o[3]);
     }
     // values: this lane's dims, both words of each; token 2 i + odd of word i >> 2 is in place i & 3 of its half of the word

@@ -9,9 +9,7 @@
 // for s = (1 + (b & 7) / 8) * 2^((b >> 3) - 20): a sign-less float of five exponent and three fraction bits, no zero.
 //
 // Why these: both products of the attention run over bf16 operands.  |c - 8| <= 8 has four significant bits and s has four, so
-// (c - 8) * s is exact in bf16 and the attention adds no rounding of its own to the quantisation.  c enters a register as the
-// bf16 number 128 + c (0x4300 | c) and leaves it by one fused multiply-add, (128 + c) * s - 136 s, whose every term is exact: 136 s
-// is 17 (8 + m) * 2^k, at most 255.  Whole numbers at equal distances lose less than 4-bit floats on groups as small as 16: 8.6 %
+// (c - 8) * s is exact in bf16 and the attention adds no rounding of its own to the quantisation.  Whole numbers at equal distances lose less than 4-bit floats on groups as small as 16: 8.6 %
 // of the norm of normally distributed values.  The groups follow the attention's operands: a thread that prepares keys owns a
 // token, one that prepares values a dim, and each of its sixteen values share a scale.
 #pragma once
@@ -41,20 +39,36 @@ __device__ __forceinline__ uint32_t code_bits(float x, float inv)
     return __float_as_uint(fminf(fmaxf(x * inv, -7.0f), 7.0f) + 12582920.0f) & 15u;
 }
 
-// Eight codes of a word as four bf16 pairs times a scale: s2 = (s, s), c2 = (-136 s, -136 s).
-__device__ __forceinline__ void dequant_word(uint32_t w, uint32_t s2, uint32_t c2, uint32_t (&out)[4])
+// Eight codes of a word as four bf16 pairs (c - 8) * s * 2^-kDequantShift.  A whole number n < 256 in the low bits of a bf16 is
+// n * 2^-133 (subnormal up to 127, and the first binade has the same spacing): so a nibble in bits 0 .. 3 needs no more than a mask
+// to be c * 2^-133, one in bits 4 .. 7 c * 2^-129, and one shift serves the other two pairs.  A fused multiply-add takes the power of
+// two, the scale and the 8 away; the shift keeps its factor below 2^128.
+constexpr int kDequantShift = 20;
+struct DequantScale {
+    uint32_t lo, hi, minus;                            // (x, x) for s 2^(133 - shift), s 2^(129 - shift), -8 s 2^-shift
+};
+// `twice`: the scale byte in both halves (0x00bb00bb).
+__device__ __forceinline__ DequantScale dequant_scale(uint32_t twice)
 {
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const uint32_t pair = ((w >> (4 * p)) & 0x000f000fu) | 0x43004300u;
-        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(out[p]) : "r"(pair), "r"(s2), "r"(c2));
-    }
+    DequantScale d;
+    d.lo = twice * 16u + 0x00010001u * ((127u - kScaleBias + 133u - kDequantShift) << 7);
+    d.hi = twice * 16u + 0x00010001u * ((127u - kScaleBias + 129u - kDequantShift) << 7);
+    d.minus = twice * 16u + 0x00010001u * (0x8000u | ((127u - kScaleBias + 3u - kDequantShift) << 7));
+    return d;
 }
-// (s, s) and (-136 s, -136 s) of the byte twice in a register (0x00bb00bb).
-__device__ __forceinline__ void scale_pair(uint32_t twice, uint32_t &s2, uint32_t &c2)
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c)
 {
-    s2 = twice * 16u + 0x00010001u * ((127u - kScaleBias) << 7);
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(c2) : "r"(s2), "r"(0xc308c308u));       // bf16 -136 = 0xc308
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ void dequant_word(uint32_t w, const DequantScale &d, uint32_t *out)
+{
+    const uint32_t v = w >> 8;
+    out[0] = fma_bf16x2(w & 0x000f000fu, d.lo, d.minus);
+    out[1] = fma_bf16x2(w & 0x00f000f0u, d.hi, d.minus);
+    out[2] = fma_bf16x2(v & 0x000f000fu, d.lo, d.minus);
+    out[3] = fma_bf16x2(v & 0x00f000f0u, d.hi, d.minus);
 }
 
 }  // namespace oasis

@@ -1,24 +1,25 @@
 // Attention over a working set held in 4 bits (packed.cuh), with the local window in bf16, on the 5th-generation tensor cores.
 //
-// Work item = (request, KV head, row group, split of the columns), one thread block of 128 threads.  Tiles of eight 16-token blocks.
+// Work item = (request, KV head, row group, split of the columns), one thread block.  Tiles of eight 16-token blocks.
 // Other than in the bf16 kernels the keys and values, which have to pass through registers anyway, are the A operands in tensor
 // memory, and the query rows the columns:
 //   S[token][row] = K Q^T    thread = token: 64 B of codes become the token's 128 bf16 dims, 64 columns of its tensor-memory lane
 //   O[dim][row]  += V^T P    thread = dim: 8 B of codes per block become the dim's 16 tokens, 8 columns of its lane
 // Q (K-major) and P (row-major by token) are the B operands in shared memory.  So 4-bit data crosses shared memory once, bf16 data
 // never (as bf16 tiles in shared memory they would be written and read there, 2.5 times the time that HBM takes to bring them).
-// A row's logits lie across the threads: the reference maximum that its weights are taken against is shared and raised only when a
-// logit exceeds it by 2^8, which one vote per tile finds out; the rows' sums are kept per thread and added up at the end.
-// One tile after the other in a thread block: wait for its entries, keys, K Q^T, (meanwhile) values, softmax, V^T P (meanwhile the
-// next keys).  Four thread blocks per SM (two with more than 32 rows) overlap each other's waits.
-// Entries come as bulk copies, one per block, a ring of two to four tiles ahead.  Columns that no row sees are left out when the
-// column list of the split is read (compacted in order: the result does not depend on the launch).  The local columns, at most one
-// tile, are the first tile of split 0, read straight from global memory while the ring fills.
-// Rows: up to 64 per thread block (16, 32 or 64 columns of the products); more are cut into row groups.
+// A row's logits lie across the threads: the reference maximum that its weights are taken against is shared, comes from the first
+// tile, and is raised only when a logit exceeds it by 2^32 (weights, sums and accumulators have fp32's range, so that only their
+// overflow matters), which one vote per tile finds out; the rows' sums are kept per thread and added up at the end.
+// Roles: four warps unpack keys (thread = token) and then take the softmax of the tile before, four unpack values (thread = dim),
+// one issues the products, one requests entries (bulk copies, one per block, a ring of four or five tiles).  Two thread blocks per
+// SM fill each other's waits.  With more than 32 rows the value warps take half of the softmax's columns.
+// Columns that no row sees are left out when the column list of the split is read (compacted in order: the result does not depend
+// on the launch).  The local columns, at most one tile, are the first tile of split 0, read straight from global memory while the
+// ring fills.  Rows: up to 64 per thread block (16, 32 or 64 columns of the products); more are cut into row groups.
 // Splits of a row merge inside a thread-block cluster where eight reach, else through the workspace and a second launch.
-// Precision: (c - 8) s is exact in bf16; logits, maxima, sums and accumulators are fp32; the weights go to V^T P as bf16 (half a
-// step, 2^-8 of a weight), because both operands of one tcgen05.mma kind::f16 have the same type; the sum that divides them is of
-// the unrounded ones.
+// Precision: the unpacked keys and values are exact, 2^-20 of what they stand for (the power of two returns in the logits' scale and
+// in the output's); logits, maxima, sums and accumulators are fp32; the weights go to V^T P as bf16 (half a step, 2^-8 of a weight),
+// because both operands of one tcgen05.mma kind::f16 have the same type; the sum that divides them is of the unrounded ones.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -30,19 +31,23 @@ namespace oasis {
 constexpr int kPaTileCols = 8, kPaTileKeys = kPaTileCols * kBlock;       // 128 tokens: the rows of one MMA
 constexpr int kPaStageBytes = kPaTileCols * kPackedBytes;                // 18 KiB
 constexpr int kPaListCols = 256;                                         // columns of a split at most
-constexpr int kPaThreads = 128;
+constexpr int kPaThreads = 320;                                          // key warps 0-3, value warps 4-7, products 8, copies 9
 constexpr int kPaMaxCluster = 8;
-__host__ __device__ constexpr int pa_blocks(int n) { return n <= 32 ? 4 : 2; }              // thread blocks per SM
-__host__ __device__ constexpr int pa_stages(int n) { return n <= 32 ? 2 : 4; }
-__host__ __device__ constexpr int pa_tmem_cols(int n) { return n <= 32 ? 128 : 256; }       // K, V: 64 (shared up to 32 rows); S, O: n each
+constexpr int kPaBlocks = 2;                                             // thread blocks per SM
+constexpr int kPaTmemCols = 256;                                         // K 64 | V 64 | S (two buffers up to 32 rows) | O
+constexpr float kPaRaise = 32.f;                                         // (log2) how far a logit may exceed its row's reference
+__host__ __device__ constexpr int pa_stages(int n) { return n <= 32 ? 5 : 4; }
+__host__ __device__ constexpr int pa_s_bufs(int n) { return n <= 32 ? 2 : 1; }
 // Shared memory: Q [dim half][n rows][128 B] | P [128 tokens][2 n B] | ring | column list | statistics and barriers.
-constexpr int kPaMisc = 1536;
+constexpr int kPaMisc = 1024;
 __host__ __device__ constexpr int pa_smem(int n)
 {
-    return 1024 + n * kRowBytes + kPaTileKeys * 2 * n + pa_stages(n) * kPaStageBytes + kPaListCols * 8 + (n <= 32 ? 768 : kPaMisc);
+    return 1024 + n * kRowBytes + kPaTileKeys * 2 * n + pa_stages(n) * kPaStageBytes + kPaListCols * 8 + kPaMisc;
 }
-static_assert((pa_smem(16) + 1024) * 4 <= 233472 && (pa_smem(32) + 1024) * 4 <= 233472 && (pa_smem(64) + 1024) * 2 <= 233472, "thread blocks per SM");
-static_assert(pa_stages(32) * kPaStageBytes >= 32 * kHeadDim * 4 && pa_stages(64) * kPaStageBytes >= 64 * kHeadDim * 4, "the accumulator fits into the ring");
+static_assert((pa_smem(16) + 1024) * kPaBlocks <= 233472 && (pa_smem(32) + 1024) * kPaBlocks <= 233472 && (pa_smem(64) + 1024) * kPaBlocks <= 233472,
+              "thread blocks per SM");
+static_assert(128 + 3 * 32 <= kPaTmemCols && 128 + 2 * 64 <= kPaTmemCols, "tensor memory of a thread block");
+static_assert(pa_stages(64) * kPaStageBytes >= 64 * kHeadDim * 4, "the accumulator fits into the ring");
 
 struct PackedAttnParams {
     const uint8_t *q, *packed, *local;
@@ -52,7 +57,7 @@ struct PackedAttnParams {
     float *part_o;      // [items][rows per group][128] fp32, normalised (runs through the workspace only)
     float *part_lse;    // [items][rows per group]      log2 domain
     int32_t *err;
-    float scale_log2;
+    float scale_log2;   // of bf16 keys; of unpacked ones: times 2^kDequantShift
     int T, Hq, Hkv, G, n_cols, local_col, R, n_splits, tiles_per_split, n_groups, group_rows;
     Bounds bd;
 };
@@ -107,13 +112,33 @@ __device__ __forceinline__ uint32_t pa_p_chunk(int token, int c)         // byte
     return (uint32_t)(token * 2 * N + ((c ^ x) << 4));
 }
 
+// Named barrier 1 over the softmax threads, returning the OR of their predicates; and the plain barrier 2.
+template <int THREADS>
+__device__ __forceinline__ bool pa_any(bool pred)
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "bar.red.or.pred q, 1, %2, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r) : "r"((uint32_t)pred), "n"(THREADS) : "memory");
+    return r != 0;
+}
+template <int THREADS>
+__device__ __forceinline__ void pa_sync()
+{
+    asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
+}
+
 // N: columns of the products (query rows, padded).
 template <int N, bool CLUSTER>
-__global__ void __launch_bounds__(kPaThreads, pa_blocks(N))
+__global__ void __launch_bounds__(kPaThreads, kPaBlocks)
 packed_attn_kernel(const PackedAttnParams p)
 {
-    constexpr int STAGES = pa_stages(N);
-    constexpr bool SHARED_KV = N <= 32;                     // keys and values take turns in the same 64 columns of tensor memory
+    constexpr int STAGES = pa_stages(N), SBUFS = pa_s_bufs(N);
+    constexpr int NC = N <= 32 ? N : 32;                    // softmax columns of a thread
+    constexpr int SOFT = N <= 32 ? 128 : 256;               // softmax threads
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -123,12 +148,14 @@ packed_attn_kernel(const PackedAttnParams p)
     float *const neg_m = reinterpret_cast<float *>(list + kPaListCols);                     // [N] minus the rows' reference maxima
     float *const l_sm = neg_m + N;                                                          // [N]; while a maximum is raised: factors
     uint64_t *const bars = reinterpret_cast<uint64_t *>(l_sm + N);
-    int2 *const s_local = reinterpret_cast<int2 *>(bars + STAGES + 2);                      // [8] the local columns
+    int2 *const s_local = reinterpret_cast<int2 *>(bars + 2 * STAGES + 6);                  // [8] the local columns
     int *const s_cnt = reinterpret_cast<int *>(s_local + kPaTileCols);                      // [8]
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(s_cnt + 8);
-    volatile int *const dead = reinterpret_cast<int *>(tmem_slot + 1);
-    const uint32_t bar0 = smem_u32(bars), bar_s = bar0 + 8u * STAGES, bar_o = bar_s + 8u;
+    const uint32_t bar0 = smem_u32(bars), bar_k = bar0 + 16u * STAGES, bar_v = bar_k + 8u, bar_p = bar_k + 16u, bar_o = bar_k + 24u;
     auto bar_full = [&](int s) { return bar0 + 8u * s; };
+    auto bar_empty = [&](int s) { return bar0 + 8u * (STAGES + s); };
+    auto bar_s = [&](int k) { return bar_k + 32u + 8u * (k % SBUFS); };                    // of tile k
+    auto par_s = [&](int k) { return (uint32_t)((k / SBUFS) & 1); };
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int grp = CLUSTER ? (blockIdx.x / p.n_splits) % p.n_groups : blockIdx.x % p.n_groups;
@@ -136,14 +163,19 @@ packed_attn_kernel(const PackedAttnParams p)
     const int bh = blockIdx.x / (p.n_groups * p.n_splits);
     const int b = bh / p.Hkv, h = bh % p.Hkv;
     const int row0 = grp * p.group_rows, rows = min(p.group_rows, p.R - row0);
-    if (warp == 0) {
+    if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)pa_tmem_cols(N)) : "memory");
+                     ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)kPaTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (tid == 0) {
-        for (int s = 0; s < STAGES + 2; ++s) mbar_init(bar0 + 8u * s, 1);
-        *dead = 0;
+        for (int s = 0; s < STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 8); }
+        mbar_init(bar_k, 4);
+        mbar_init(bar_v, 4);
+        mbar_init(bar_p, SOFT / 32);
+        mbar_init(bar_o, 1);
+        mbar_init(bar_s(0), 1);
+        if (SBUFS > 1) mbar_init(bar_s(1), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < N) neg_m[tid] = CUDART_INF_F;
@@ -152,23 +184,18 @@ packed_attn_kernel(const PackedAttnParams p)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- the split's columns ------------------------------------------------------------------------------------
-    // Tiles of a row: the local columns (if any), then eight packed columns each.
+    // Tiles of a row: the local columns (if any), then eight packed columns each.  Thread k < 256 holds the split's column k.
     const int has_local = p.n_cols > p.local_col;
     const int t0 = split * p.tiles_per_split, t1 = t0 + p.tiles_per_split;
     const int c0 = max(t0 - has_local, 0) * kPaTileCols, c1 = min((t1 - has_local) * kPaTileCols, p.local_col);
     const int32_t *blk_row = p.blk_tbl + (long long)bh * p.n_cols, *slot_row = p.slot_tbl + (long long)bh * p.n_cols;
     const long long L = p.seq_len[b], last = L + p.T - 1;               // last position that a row sees
-    int2 col[2];
-    unsigned got[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int c = c0 + tid + 128 * k;
-        col[k] = make_int2(-1, -1);
-        if (c < c1) col[k] = make_int2(blk_row[c], slot_row[c]);
+    int2 col = make_int2(-1, -1);
+    if (warp < 8) {
+        if (c0 + tid < c1) col = make_int2(blk_row[c0 + tid], slot_row[c0 + tid]);
+    } else if (warp == 8 && lane < kPaTileCols && has_local && t0 == 0 && p.local_col + lane < p.n_cols) {
+        col = make_int2(blk_row[p.local_col + lane], slot_row[p.local_col + lane]);
     }
-    int2 near = make_int2(-1, -1);
-    if (tid < kPaTileCols && has_local && t0 == 0 && p.local_col + tid < p.n_cols)
-        near = make_int2(blk_row[p.local_col + tid], slot_row[p.local_col + tid]);
     // Q: 16 bytes (chunk c of row r) at a time; rows past the group's are zero
 #pragma unroll 4
     for (int i = tid; i < N * 16; i += kPaThreads) {
@@ -181,289 +208,330 @@ packed_attn_kernel(const PackedAttnParams p)
         *reinterpret_cast<uint4 *>(base_ptr + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        bool ok = col[k].x >= 0 && (long long)col[k].x * kBlock <= last;
-        if (kBoundsCheck && ok) ok = in_range(col[k].y, p.bd.n_slots, p.bd, kErrSlot);
-        got[k] = __ballot_sync(0xffffffffu, ok);
-        if (lane == 0) s_cnt[k * 4 + warp] = __popc(got[k]);
-    }
-    if (warp == 0) {
-        bool ok = near.x >= 0 && (long long)near.x * kBlock <= last;
-        if (kBoundsCheck && ok) ok = in_range(near.y, p.bd.n_slots, p.bd, kErrSlot);
-        if (lane < kPaTileCols) s_local[lane] = ok ? near : make_int2(-1, -1);
-    }
+    bool seen = col.x >= 0 && (long long)col.x * kBlock <= last;
+    if (kBoundsCheck && seen) seen = in_range(col.y, p.bd.n_slots, p.bd, kErrSlot);
+    const unsigned got = __ballot_sync(0xffffffffu, seen);
+    if (warp < 8 && lane == 0) s_cnt[warp] = __popc(got);
+    if (warp == 8 && lane < kPaTileCols) s_local[lane] = seen ? col : make_int2(-1, -1);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     int count = 0;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w == warp && ((got[k] >> lane) & 1u)) list[count + __popc(got[k] & ((1u << lane) - 1u))] = col[k];
-            count += s_cnt[k * 4 + w];
-        }
+    for (int w = 0; w < 8; ++w) {
+        if (w == warp && seen) list[count + __popc(got & ((1u << lane) - 1u))] = col;
+        count += s_cnt[w];
+    }
     int do_local = 0;
 #pragma unroll
     for (int k = 0; k < kPaTileCols; ++k) do_local |= s_local[k].x >= 0;
     const int packed_tiles = (count + kPaTileCols - 1) / kPaTileCols, n_tiles = do_local + packed_tiles;
-    const uint32_t tmem = *tmem_slot, lane_base = (uint32_t)(warp * 32) << 16;
-    const uint32_t t_k = tmem, t_v = tmem + (SHARED_KV ? 0 : 64), t_s = t_v + 64, t_o = t_s + N;
+    const uint32_t tmem = *tmem_slot, t_k = tmem, t_v = tmem + 64, t_s = tmem + 128, t_o = t_s + SBUFS * N;
     __syncthreads();                                                     // the list is complete
 
-    // Warp 0, lanes 0..7: one entry each of packed tile `pi` into its stage.
-    auto request = [&](int pi) {
-        const int n = min(kPaTileCols, count - pi * kPaTileCols), s = pi % STAGES;
-        if (lane == 0) mbar_arrive_expect_tx(bar_full(s), (uint32_t)(n * kPackedBytes));
-        __syncwarp();
-        if (lane < n)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                         ::"r"(smem_u32(ring) + (uint32_t)(s * kPaStageBytes + lane * kPackedBytes)),
-                           "l"(p.packed + (long long)list[pi * kPaTileCols + lane].y * kPackedBytes), "r"((uint32_t)kPackedBytes),
-                           "r"(bar_full(s)) : "memory");
-        __syncwarp();
-    };
-    if (warp == 0)
-        for (int pi = 0; pi < min(STAGES, packed_tiles); ++pi) request(pi);
-
-    float l[N];
-#pragma unroll
-    for (int n = 0; n < N; ++n) l[n] = 0.f;
-    const int kb = 2 * warp + (lane >> 4), tok = lane & 15;             // this thread's block of the tile and token, for the keys
-    int issued = min(STAGES, packed_tiles), done_tiles = 0;
+    float *const o_sm = reinterpret_cast<float *>(ring);                 // [N][128], after the last tile
+    float *const l_part = reinterpret_cast<float *>(p_ptr);              // [4][N], after the last tile
+    bool alive = true;
+    if (warp == 9) {
+        // ---------------------------------------------------------------- copies
+        int s = 0, pi = 0;
+        uint32_t ph = 1;
 #pragma unroll 1
-    for (int i = 0; i < n_tiles; ++i) {
-        const bool loc = do_local && i == 0;
-        const int pi = i - do_local, s = pi % STAGES;
-        const uint8_t *const stage = ring + s * kPaStageBytes;
-        const int2 mine = loc ? s_local[kb] : pi * kPaTileCols + kb < count ? list[pi * kPaTileCols + kb] : make_int2(-1, -1);
-        // the first column (query row) that sees this thread's token
-        const long long ahead = (long long)mine.x * kBlock + tok - L;
-        const int n_min = mine.x < 0 || ahead >= p.T ? N : ahead <= 0 ? 0 : min(max((int)ahead * p.G - row0, 0), N);
-        // ---- keys
-        uint32_t r[64];
-        if (loc) {
-#pragma unroll
-            for (int e = 0; e < 64; ++e) r[e] = 0;
-            if (n_min < N) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(p.local + (long long)mine.y * kEntryBytes + tok * kRowBytes);
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const uint4 v = src[c];
-                    r[4 * c] = v.x; r[4 * c + 1] = v.y; r[4 * c + 2] = v.z; r[4 * c + 3] = v.w;
-                }
-            }
-        } else {
-            if (!mbar_wait(bar_full(s), (pi / STAGES) & 1, p.err, 81)) *dead = 1;
-            const uint8_t *ent = stage + kb * kPackedBytes;
-            const uint2 sc = *reinterpret_cast<const uint2 *>(ent + kPackedKScale + tok * 8);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(ent + c * 256 + tok * 16);
-                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int byte = 2 * c + g;
-                    uint32_t s2, c2;
-                    scale_pair(__byte_perm(byte < 4 ? sc.x : sc.y, 0u, 0x4040 | (byte & 3) | ((byte & 3) << 8)), s2, c2);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint32_t o[4];
-                        dequant_word(ww[2 * g + e], s2, c2, o);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) r[16 * c + 8 * g + 4 * e + k] = o[k];
-                    }
-                }
-            }
+        for (; pi < packed_tiles; ++pi) {
+            if (pi >= STAGES) alive = mbar_wait_warp(bar_empty(s), ph, p.err, 81);
+            if (!alive) break;
+            const int n = min(kPaTileCols, count - pi * kPaTileCols);
+            if (lane == 0) mbar_arrive_expect_tx(bar_full(s), (uint32_t)(n * kPackedBytes));
+            __syncwarp();
+            if (lane < n)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                             ::"r"(smem_u32(ring) + (uint32_t)(s * kPaStageBytes + lane * kPackedBytes)),
+                               "l"(p.packed + (long long)list[pi * kPaTileCols + lane].y * kPackedBytes), "r"((uint32_t)kPackedBytes),
+                               "r"(bar_full(s)) : "memory");
+            ring_advance(s, ph, 1, STAGES);
         }
-        // V^T P of the previous tile has read its values and weights, and O is complete up to it
-        if (i > 0 && !mbar_wait(bar_o, (i - 1) & 1, p.err, 82)) *dead = 1;
-        tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tc_st16(t_k + lane_base + c * 16, *reinterpret_cast<const uint32_t(*)[16]>(r + 16 * c));
-        tc_wait_st();
-        tc_fence_before();
-        __syncthreads();
-        if (*dead) break;
-        if (warp == 0) {
+        if (!alive)                                                      // nobody leaves while copies are on their way
+            for (int k = max(0, pi - STAGES); k < pi; ++k) mbar_wait_warp(bar_full(k % STAGES), (k / STAGES) & 1, p.err, 82);
+    } else if (warp == 8) {
+        // ---------------------------------------------------------------- products (the whole warp, converged)
+        const uint64_t q_desc = smem_desc_sw128(base), p_desc = pa_p_desc<N>(base + N * kRowBytes);
+        auto keys = [&](int i) {
+            alive = alive && mbar_wait_warp(bar_k, i & 1, p.err, 83);
+            if (!alive) return;
             tc_fence_after();
-            const uint64_t q_desc = smem_desc_sw128(base);
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                tc_mma_bf16_ts(t_s, t_k + 8 * k, q_desc + (uint64_t)(((k >> 2) * (N * 128) + (k & 3) * 32) >> 4), pa_idesc(N, false), k ? 1u : 0u);
-            tc_commit(bar_s);
-        }
-        // ---- values: thread = dim
-        if (loc) {
-#pragma unroll
-            for (int k = 0; k < kPaTileCols; ++k) {
-                const int2 e = s_local[k];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) r[8 * k + j] = 0;
-                if (e.x >= 0) {                                          // (tokens past the last visible one may hold anything)
-                    const uint16_t *src = reinterpret_cast<const uint16_t *>(p.local + (long long)e.y * kEntryBytes + kPartBytes) + tid;
-                    const int n = (int)min((long long)kBlock, last - (long long)e.x * kBlock + 1);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t lo = 2 * j < n ? src[2 * j * kHeadDim] : 0u, hi = 2 * j + 1 < n ? src[(2 * j + 1) * kHeadDim] : 0u;
-                        r[8 * k + j] = lo | hi << 16;
-                    }
-                }
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kPaTileCols; ++k) {
-                const uint8_t *ent = stage + k * kPackedBytes;
-                const uint2 w = *reinterpret_cast<const uint2 *>(ent + kPackedV + tid * 8);
-                uint32_t s2, c2, o[4];
-                scale_pair(ent[kPackedVScale + tid] * 0x00010001u, s2, c2);
-                dequant_word(w.x, s2, c2, o);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) r[8 * k + j] = o[j];
-                dequant_word(w.y, s2, c2, o);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) r[8 * k + 4 + j] = o[j];
-            }
-        }
-        if (!mbar_wait(bar_s, i & 1, p.err, 83)) *dead = 1;
-        tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tc_st16(t_v + lane_base + c * 16, *reinterpret_cast<const uint32_t(*)[16]>(r + 16 * c));
-        // ---- softmax: thread = token, one logit per query row
-        float x[N];
-        {
-            uint32_t v[N / 16][16];
-#pragma unroll
-            for (int c = 0; c < N / 16; ++c) tc_ld16_nowait(t_s + lane_base + c * 16, v[c]);
-            tc_wait_ld();
-#pragma unroll
-            for (int n = 0; n < N; ++n) x[n] = __uint_as_float(v[n >> 4][n & 15]);
-        }
-        tc_wait_st();
-        const bool masked = __any_sync(0xffffffffu, n_min > 0);
-        if (masked) {
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-                if (n < n_min) x[n] = -CUDART_INF_F;
-        }
-        float top = -CUDART_INF_F;
-#pragma unroll
-        for (int n = 0; n < N; n += 4) {
-            const float4 m = *reinterpret_cast<const float4 *>(neg_m + n);
-            top = max3(top, fmaf(x[n], p.scale_log2, m.x), fmaf(x[n + 1], p.scale_log2, m.y));
-            top = max3(top, fmaf(x[n + 2], p.scale_log2, m.z), fmaf(x[n + 3], p.scale_log2, m.w));
-        }
-        const int raise = __syncthreads_or(top > 8.f);                   // (also: every thread has read the stage)
-        if (*dead) break;
-        if (!loc) ++done_tiles;
-        if (!loc && warp == 0 && pi + STAGES < packed_tiles) request(pi + STAGES);
-        if (!loc && pi + STAGES < packed_tiles) ++issued;
-        if (raise) {
-            int *const w_max = reinterpret_cast<int *>(p_ptr);           // [4][N]: P is written later
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int m = __reduce_max_sync(0xffffffffu, ordered(x[n]));
-                if (lane == 0) w_max[warp * N + n] = m;
-            }
-            __syncthreads();
-            if (tid < N) {
-                const float m_old = -neg_m[tid];
-                const float mx = unordered(max(max(w_max[tid], w_max[N + tid]), max(w_max[2 * N + tid], w_max[3 * N + tid]))) * p.scale_log2;
-                const float m_new = fmaxf(m_old, mx);
-                neg_m[tid] = -m_new;
-                l_sm[tid] = m_new == -CUDART_INF_F ? 1.f : fast_exp2(m_old - m_new);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int n = 0; n < N; ++n) l[n] *= l_sm[n];
-            if (i > 0) {
-#pragma unroll
-                for (int c = 0; c < N / 16; ++c) {
-                    uint32_t v[16];
-                    tc_ld16(t_o + lane_base + c * 16, v);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * l_sm[c * 16 + e]);
-                    tc_st16(t_o + lane_base + c * 16, v);
-                }
-                tc_wait_st();
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < N / 8; ++c) {
-            float e[8];
-#pragma unroll
-            for (int k = 0; k < 8; k += 4) {
-                const float4 m = *reinterpret_cast<const float4 *>(neg_m + 8 * c + k);
-                const float mm[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-                for (int u = 0; u < 4; ++u) e[k + u] = fast_exp2(fmaf(x[8 * c + k + u], p.scale_log2, mm[u]));
-            }
-            if (masked) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (8 * c + k < n_min) e[k] = 0.f;
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) l[8 * c + k] += e[k];
-            *reinterpret_cast<uint4 *>(p_ptr + pa_p_chunk<N>(tid, c)) =
-                make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7]));
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        tc_fence_before();
-        __syncthreads();
-        if (warp == 0) {
+                tc_mma_bf16_ts(t_s + (i % SBUFS) * N, t_k + 8 * k, q_desc + (uint64_t)(((k >> 2) * (N * 128) + (k & 3) * 32) >> 4), pa_idesc(N, false),
+                               k ? 1u : 0u);
+            tc_commit(bar_s(i));
+        };
+        auto values = [&](int i) {
+            alive = alive && mbar_wait_warp(bar_v, i & 1, p.err, 84) && mbar_wait_warp(bar_p, i & 1, p.err, 85);
+            if (!alive) return;
             tc_fence_after();
-            const uint64_t p_desc = pa_p_desc<N>(base + N * kRowBytes);
 #pragma unroll
             for (int k = 0; k < kPaTileCols; ++k)
                 tc_mma_bf16_ts(t_o, t_v + 8 * k, p_desc + (uint64_t)((k * 32 * N) >> 4), pa_idesc(N, true), (i > 0 || k) ? 1u : 0u);
             tc_commit(bar_o);
+        };
+#pragma unroll 1
+        for (int i = 0; i < n_tiles && alive; ++i) {
+            if (SBUFS == 1 && i > 0) values(i - 1);                      // (one S buffer: its tile has to be read first)
+            keys(i);
+            if (SBUFS > 1 && i > 0) values(i - 1);
         }
-    }
-    // ---- epilogue -------------------------------------------------------------------------------------------------
-    if (n_tiles > 0 && !*dead && !mbar_wait(bar_o, (n_tiles - 1) & 1, p.err, 84)) *dead = 1;
-    if (*dead) {                                                         // nobody leaves while copies are on their way
-        if (tid == 0)
-            for (int pi = done_tiles; pi < issued; ++pi) mbar_wait(bar_full(pi % STAGES), (pi / STAGES) & 1, p.err, 85);
-    }
-    tc_fence_after();
-    float *const o_sm = reinterpret_cast<float *>(ring);                 // [N][128]
-    float *const l_part = reinterpret_cast<float *>(p_ptr);              // [4][N]
-    __syncthreads();                                                     // (waits over, P and the ring idle)
-    if (n_tiles > 0) {
+        if (n_tiles > 0) values(n_tiles - 1);
+    } else {
+        // ---------------------------------------------------------------- unpacking and softmax
+        const int side = warp >> 2, me = tid & 127;                      // 0: keys, 1: values; token or dim
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        const int kb = me >> 4, tok = me & 15;
+        const int n0 = side * NC;                                        // first softmax column of this thread
+        float l[NC];
 #pragma unroll
-        for (int c = 0; c < N / 16; ++c) {
-            uint32_t v[16];
-            tc_ld16(t_o + lane_base + c * 16, v);
+        for (int n = 0; n < NC; ++n) l[n] = 0.f;
+
+        auto softmax = [&](int i) {                                      // of tile i, whose logits are there
+            const bool loc = do_local && i == 0;
+            const int pi = i - do_local;
+            const int blk = loc ? s_local[kb].x : pi * kPaTileCols + kb < count ? list[pi * kPaTileCols + kb].x : -1;
+            // the first query row that sees this thread's token
+            const long long ahead = (long long)blk * kBlock + tok - L;
+            const int n_min = (blk < 0 || ahead >= p.T ? N : ahead <= 0 ? 0 : min(max((int)ahead * p.G - row0, 0), N)) - n0;
+            const float scale = loc ? p.scale_log2 : p.scale_log2 * (float)(1 << kDequantShift);
+            const uint32_t t_mine = t_s + (i % SBUFS) * N + n0 + lane_base;
+            float x[16];                                                 // sixteen columns at a time (32: read a second time for the weights)
+            bool masked = __any_sync(0xffffffffu, n_min > 0);
+            auto logits = [&](int c) {
+                uint32_t v[16];
+                tc_ld16(t_mine + c * 16, v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o_sm[(c * 16 + e) * kHeadDim + tid] = __uint_as_float(v[e]);
-        }
-    }
-    // the threads' sums of a row: half of the values change hands in every round, so that lane k ends with rows k, k + 32, ..
+                for (int n = 0; n < 16; ++n) x[n] = __uint_as_float(v[n]);
+                if (masked) {
 #pragma unroll
-    for (int w = N / 2, bit = 16; bit >= 1; bit >>= 1) {
-        const bool up = lane & bit;
-        if (w >= 1) {
-#pragma unroll
-            for (int k = 0; k < N / 2; ++k)
-                if (k < w) {
-                    const float give = up ? l[k] : l[k + w], keep = up ? l[k + w] : l[k];
-                    l[k] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
+                    for (int n = 0; n < 16; ++n)
+                        if (c * 16 + n < n_min) x[n] = -CUDART_INF_F;
                 }
-            w >>= 1;
-        } else {
-            l[0] += __shfl_xor_sync(0xffffffffu, l[0], bit);
+            };
+            float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+            for (int c = 0; c < NC / 16; ++c) {
+                logits(c);
+#pragma unroll
+                for (int n = 0; n < 16; n += 8) {
+                    const float4 m = *reinterpret_cast<const float4 *>(neg_m + n0 + c * 16 + n), w = *reinterpret_cast<const float4 *>(neg_m + n0 + c * 16 + n + 4);
+                    m4[0] = max3(m4[0], fmaf(x[n], scale, m.x), fmaf(x[n + 4], scale, w.x));
+                    m4[1] = max3(m4[1], fmaf(x[n + 1], scale, m.y), fmaf(x[n + 5], scale, w.y));
+                    m4[2] = max3(m4[2], fmaf(x[n + 2], scale, m.z), fmaf(x[n + 6], scale, w.z));
+                    m4[3] = max3(m4[3], fmaf(x[n + 3], scale, m.w), fmaf(x[n + 7], scale, w.w));
+                }
+            }
+            const bool raise = pa_any<SOFT>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) > kPaRaise);
+            // V^T P of the tile before has read its weights, and O is complete up to it
+            if (i > 0) alive = alive && mbar_wait(bar_o, (i - 1) & 1, p.err, 86);
+            if (raise) {
+                int *const w_max = reinterpret_cast<int *>(p_ptr);       // [4][N]: P is written later
+#pragma unroll
+                for (int c = 0; c < NC / 16; ++c) {
+                    if (NC > 16) logits(c);
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) {
+                        const int m = __reduce_max_sync(0xffffffffu, ordered(x[n]));
+                        if (lane == 0) w_max[(warp & 3) * N + n0 + c * 16 + n] = m;
+                    }
+                }
+                pa_sync<SOFT>();
+                if (tid < N) {
+                    const float m_old = -neg_m[tid];
+                    const float mx = unordered(max(max(w_max[tid], w_max[N + tid]), max(w_max[2 * N + tid], w_max[3 * N + tid]))) * scale;
+                    const float m_new = fmaxf(m_old, mx);
+                    neg_m[tid] = -m_new;
+                    l_sm[tid] = m_new == -CUDART_INF_F ? 1.f : fast_exp2(m_old - m_new);
+                }
+                pa_sync<SOFT>();
+#pragma unroll
+                for (int n = 0; n < NC; ++n) l[n] *= l_sm[n0 + n];
+                if (i > 0) {
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < NC / 16; ++c) {
+                        uint32_t v[16];
+                        tc_ld16(t_o + n0 + lane_base + c * 16, v);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * l_sm[n0 + c * 16 + e]);
+                        tc_st16(t_o + n0 + lane_base + c * 16, v);
+                    }
+                    tc_wait_st();
+                }
+            }
+            const float unit = loc ? 1.f / (float)(1 << kDequantShift) : 1.f;      // the accumulator's unit is 2^-kDequantShift
+#pragma unroll
+            for (int c = 0; c < NC / 8; ++c) {
+                if (NC > 16 && c % 2 == 0) logits(c / 2);
+                float e[8];
+#pragma unroll
+                for (int k = 0; k < 8; k += 4) {
+                    const float4 m = *reinterpret_cast<const float4 *>(neg_m + n0 + 8 * c + k);
+                    const float mm[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) e[k + u] = fast_exp2(fmaf(x[8 * (c % 2) + k + u], scale, mm[u]));
+                }
+                if (masked) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (8 * c + k < n_min) e[k] = 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) l[8 * c + k] += e[k];
+                if (loc) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) e[k] *= unit;
+                }
+                *reinterpret_cast<uint4 *>(p_ptr + pa_p_chunk<N>(me, n0 / 8 + c)) =
+                    make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7]));
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_p);
+        };
+
+        int s = 0;
+        uint32_t ph = 0;
+#pragma unroll 1
+        for (int i = 0; i <= n_tiles; ++i) {                             // (a wait that gave up: no more waits, but every barrier)
+            const bool loc = do_local && i == 0;
+            if (!loc && i < n_tiles) alive = alive && mbar_wait(bar_full(s), ph, p.err, 87);
+            const uint8_t *const stage = ring + s * kPaStageBytes;
+            if (side == 0) {
+                // keys: K Q^T of the tile before has read its operand (and its logits are there)
+                if (i > 0) alive = alive && mbar_wait(bar_s(i - 1), par_s(i - 1), p.err, 88);
+                tc_fence_after();
+                if (i == n_tiles) {
+                } else if (loc) {
+                    const int2 e = s_local[kb];
+                    const bool any = e.x >= 0 && (long long)e.x * kBlock + tok <= last;     // (others may hold anything)
+                    const uint4 *src = reinterpret_cast<const uint4 *>(p.local + (long long)(any ? e.y : 0) * kEntryBytes + tok * kRowBytes);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t r[16];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint4 v = any ? src[4 * c + k] : make_uint4(0, 0, 0, 0);
+                            r[4 * k] = v.x; r[4 * k + 1] = v.y; r[4 * k + 2] = v.z; r[4 * k + 3] = v.w;
+                        }
+                        tc_st16(t_k + lane_base + c * 16, r);
+                    }
+                } else {
+                    const uint8_t *ent = stage + kb * kPackedBytes;
+                    const uint2 sc = *reinterpret_cast<const uint2 *>(ent + kPackedKScale + tok * 8);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint4 w = *reinterpret_cast<const uint4 *>(ent + c * 256 + tok * 16);
+                        uint32_t r[16];
+                        const DequantScale d0 = dequant_scale(__byte_perm(c < 2 ? sc.x : sc.y, 0u, c & 1 ? 0x4242 : 0x4040));
+                        const DequantScale d1 = dequant_scale(__byte_perm(c < 2 ? sc.x : sc.y, 0u, c & 1 ? 0x4343 : 0x4141));
+                        dequant_word(w.x, d0, r);
+                        dequant_word(w.y, d0, r + 4);
+                        dequant_word(w.z, d1, r + 8);
+                        dequant_word(w.w, d1, r + 12);
+                        tc_st16(t_k + lane_base + c * 16, r);
+                    }
+                }
+            } else {
+                // values: V^T P of the tile before has read its operand
+                if (i > 0) alive = alive && mbar_wait(bar_o, (i - 1) & 1, p.err, 89);
+                tc_fence_after();
+                if (i == n_tiles) {
+                } else if (loc) {
+#pragma unroll
+                    for (int k2 = 0; k2 < kPaTileCols; k2 += 2) {
+                        uint32_t r[16];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int2 e = s_local[k2 + u];
+                            const uint16_t *src = reinterpret_cast<const uint16_t *>(p.local + (long long)(e.x >= 0 ? e.y : 0) * kEntryBytes + kPartBytes) + me;
+                            // tokens past the last visible one may hold anything
+                            const int n = e.x >= 0 ? (int)min((long long)kBlock, last - (long long)e.x * kBlock + 1) : 0;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const uint32_t lo = 2 * j < n ? src[2 * j * kHeadDim] : 0u, hi = 2 * j + 1 < n ? src[(2 * j + 1) * kHeadDim] : 0u;
+                                r[8 * u + j] = lo | hi << 16;
+                            }
+                        }
+                        tc_st16(t_v + lane_base + k2 * 8, r);
+                    }
+                } else {
+#pragma unroll
+                    for (int k2 = 0; k2 < kPaTileCols; k2 += 2) {
+                        uint32_t r[16];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const uint8_t *ent = stage + (k2 + u) * kPackedBytes;
+                            const uint2 w = *reinterpret_cast<const uint2 *>(ent + kPackedV + me * 8);
+                            const DequantScale d = dequant_scale(ent[kPackedVScale + me] * 0x00010001u);
+                            dequant_word(w.x, d, r + 8 * u);
+                            dequant_word(w.y, d, r + 8 * u + 4);
+                        }
+                        tc_st16(t_v + lane_base + k2 * 8, r);
+                    }
+                }
+            }
+            if (i < n_tiles) {
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(side == 0 ? bar_k : bar_v);
+                    if (!loc) mbar_arrive(bar_empty(s));
+                }
+                if (!loc) ring_advance(s, ph, 1, STAGES);
+            }
+            // the key warps' softmax is one tile behind their unpacking, the value warps' (their columns) level with it
+            const int tile = side == 0 ? i - 1 : SOFT == 256 && i < n_tiles ? i : -1;
+            if (tile < 0) continue;
+            if (side == 1) {
+                alive = alive && mbar_wait(bar_s(i), par_s(i), p.err, 90);
+                tc_fence_after();
+            }
+            softmax(tile);
+        }
+        if (n_tiles > 0 && side == 0) alive = alive && mbar_wait(bar_o, (n_tiles - 1) & 1, p.err, 92);
+        tc_fence_after();
+        // ---- the split's result: accumulators and sums to shared memory (the ring and P are idle)
+        if (n_tiles > 0 && alive) {
+#pragma unroll
+            for (int c = 0; c < N / 16; ++c) {
+                if (N > 16 ? (c & 1) != side : side != 0) continue;      // the two sides take turns
+                uint32_t v[16];
+                tc_ld16(t_o + lane_base + c * 16, v);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o_sm[(c * 16 + e) * kHeadDim + me] = __uint_as_float(v[e]) * (float)(1 << kDequantShift);
+            }
+        }
+        if (SOFT == 256 || side == 0) {
+            // the threads' sums of a row: half of the values change hands in every round, so that lane k ends with row k (or k / 2)
+            int w = NC / 2;
+#pragma unroll
+            for (int bit = 16; bit >= 1; bit >>= 1) {
+                const bool up = lane & bit;
+                if (w >= 1) {
+#pragma unroll
+                    for (int k = 0; k < NC / 2; ++k)
+                        if (k < w) {
+                            const float give = up ? l[k] : l[k + w], keep = up ? l[k + w] : l[k];
+                            l[k] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
+                        }
+                    w >>= 1;
+                } else {
+                    l[0] += __shfl_xor_sync(0xffffffffu, l[0], bit);
+                }
+            }
+            if (NC == 32) l_part[(warp & 3) * N + n0 + lane] = l[0];
+            else if (!(lane & 1)) l_part[(warp & 3) * N + (lane >> 1)] = l[0];
         }
     }
-    // lane's row: bit 16 chose the half of N, bit 8 the quarter, ..
-    if (N >= 32) {
-#pragma unroll
-        for (int k = 0; k < N / 32; ++k) l_part[warp * N + (N / 32) * lane + k] = l[k];
-    } else if (!(lane & 1)) {
-        l_part[warp * N + (lane >> 1)] = l[0];
-    }
-    __syncthreads();
+    alive = __syncthreads_and(alive);
     if (tid < N) l_sm[tid] = n_tiles > 0 ? l_part[tid] + l_part[N + tid] + l_part[2 * N + tid] + l_part[3 * N + tid] : 0.f;
     if constexpr (CLUSTER) {
         __syncwarp();
@@ -472,9 +540,9 @@ packed_attn_kernel(const PackedAttnParams p)
     } else {
         __syncthreads();
     }
-    if (!*dead) {
+    if (alive && warp < 8) {
         // one warp per row; in a cluster, block `split` takes rows split, split + n_splits, ..
-        const int first = CLUSTER ? split + p.n_splits * warp : warp, step = CLUSTER ? 4 * p.n_splits : 4, parts = CLUSTER ? p.n_splits : 1;
+        const int first = CLUSTER ? split + p.n_splits * warp : warp, step = CLUSTER ? 8 * p.n_splits : 8, parts = CLUSTER ? p.n_splits : 1;
 #pragma unroll 1
         for (int r = first; r < rows; r += step) {
             float m = -CUDART_INF_F, den = 0.f;
@@ -533,8 +601,8 @@ packed_attn_kernel(const PackedAttnParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 0)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)pa_tmem_cols(N)) : "memory");
+    if (warp == 8)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kPaTmemCols) : "memory");
 }
 
 // Merges the splits of one query row: out = sum_s w_s o_s / sum_s w_s with w_s = 2^(lse_s - max lse).  One warp per row, four output
@@ -604,7 +672,7 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
     const long long items = (long long)dims->batch * dims->n_kv_heads * pl.n_groups;
     const int tiles = (local_col + kPaTileCols - 1) / kPaTileCols + (n_cols > local_col ? 1 : 0);
     // all thread blocks resident at once as far as the tiles can be split
-    long long s = items > 0 ? (long long)sm_count() * pa_blocks(pl.n) / items : 1;
+    long long s = items > 0 ? (long long)sm_count() * kPaBlocks / items : 1;
     if (s > tiles) s = tiles;
     if (s < 1) s = 1;
     const int most = kPaListCols / kPaTileCols;                          // tiles whose columns a thread block can list
