@@ -10,9 +10,9 @@
 // A row's logits lie across the threads: the reference maximum that its weights are taken against is shared, comes from the first
 // tile, and is raised only when a logit exceeds it by 2^32 (weights, sums and accumulators have fp32's range, so that only their
 // overflow matters), which one vote per tile finds out; the rows' sums are kept per thread and added up at the end.
-// Roles: four warps unpack keys (thread = token) and then take the softmax of the tile before, four unpack values (thread = dim),
-// one issues the products, one requests entries (bulk copies, one per block, a ring of four or five tiles).  Two thread blocks per
-// SM fill each other's waits.  With more than 32 rows the value warps take half of the softmax's columns.
+// Roles: four warps unpack keys (thread = token), four values (thread = dim), four (eight with more than 32 rows) take the softmax
+// (thread = token), one issues the products, one requests entries (bulk copies, one per block, a ring of five or eight tiles).  With
+// up to 32 rows two thread blocks share an SM, with more one has two K and V buffers in tensor memory.
 // Columns that no row sees are left out when the column list of the split is read (compacted in order: the result does not depend
 // on the launch).  The local columns, at most one tile, are the first tile of split 0, read straight from global memory while the
 // ring fills.  Rows: up to 64 per thread block (16, 32 or 64 columns of the products); more are cut into row groups.
@@ -30,23 +30,28 @@ namespace oasis {
 
 constexpr int kPaTileCols = 8, kPaTileKeys = kPaTileCols * kBlock;       // 128 tokens: the rows of one MMA
 constexpr int kPaStageBytes = kPaTileCols * kPackedBytes;                // 18 KiB
-constexpr int kPaListCols = 256;                                         // columns of a split at most
-constexpr int kPaThreads = 320;                                          // key warps 0-3, value warps 4-7, products 8, copies 9
+constexpr int kPaListCols = 768;                                         // columns of a split at most
 constexpr int kPaMaxCluster = 8;
-constexpr int kPaBlocks = 2;                                             // thread blocks per SM
-constexpr int kPaTmemCols = 256;                                         // K 64 | V 64 | S (two buffers up to 32 rows) | O
 constexpr float kPaRaise = 32.f;                                         // (log2) how far a logit may exceed its row's reference
-__host__ __device__ constexpr int pa_stages(int n) { return n <= 32 ? 5 : 4; }
-__host__ __device__ constexpr int pa_s_bufs(int n) { return n <= 32 ? 2 : 1; }
+// Warps: 0-3 keys, 4-7 values, then four per 32 columns for the softmax, one for the products, one for the copies.
+__host__ __device__ constexpr int pa_soft(int n) { return n <= 32 ? 128 : 256; }            // softmax threads
+__host__ __device__ constexpr int pa_threads(int n) { return 256 + pa_soft(n) + 64; }
+__host__ __device__ constexpr int pa_blocks(int n) { return n <= 32 ? 2 : 1; }              // thread blocks per SM
+__host__ __device__ constexpr int pa_stages(int n) { return n <= 32 ? 4 : 8; }
+__host__ __device__ constexpr int pa_k_bufs(int n) { return n <= 32 ? 1 : 2; }              // K and V operands in tensor memory
+__host__ __device__ constexpr int pa_v_bufs(int n) { return n == 32 ? 1 : 2; }
+__host__ __device__ constexpr int pa_tmem_used(int n) { return 64 * (pa_k_bufs(n) + pa_v_bufs(n)) + 3 * n; }     // K | V | two S | O
+__host__ __device__ constexpr int pa_tmem_cols(int n) { return n <= 32 ? 256 : 512; }
 // Shared memory: Q [dim half][n rows][128 B] | P [128 tokens][2 n B] | ring | column list | statistics and barriers.
 constexpr int kPaMisc = 1024;
 __host__ __device__ constexpr int pa_smem(int n)
 {
     return 1024 + n * kRowBytes + kPaTileKeys * 2 * n + pa_stages(n) * kPaStageBytes + kPaListCols * 8 + kPaMisc;
 }
-static_assert((pa_smem(16) + 1024) * kPaBlocks <= 233472 && (pa_smem(32) + 1024) * kPaBlocks <= 233472 && (pa_smem(64) + 1024) * kPaBlocks <= 233472,
+static_assert((pa_smem(16) + 1024) * pa_blocks(16) <= 233472 && (pa_smem(32) + 1024) * pa_blocks(32) <= 233472 && (pa_smem(64) + 1024) * pa_blocks(64) <= 233472,
               "thread blocks per SM");
-static_assert(128 + 3 * 32 <= kPaTmemCols && 128 + 2 * 64 <= kPaTmemCols, "tensor memory of a thread block");
+static_assert(pa_tmem_used(16) <= pa_tmem_cols(16) && pa_tmem_used(32) <= pa_tmem_cols(32) && pa_tmem_used(64) <= pa_tmem_cols(64), "tensor memory");
+static_assert(pa_tmem_cols(32) * pa_blocks(32) <= 512 && pa_tmem_cols(64) * pa_blocks(64) <= 512, "tensor memory of an SM");
 static_assert(pa_stages(64) * kPaStageBytes >= 64 * kHeadDim * 4, "the accumulator fits into the ring");
 
 struct PackedAttnParams {
@@ -133,12 +138,13 @@ __device__ __forceinline__ void pa_sync()
 
 // N: columns of the products (query rows, padded).
 template <int N, bool CLUSTER>
-__global__ void __launch_bounds__(kPaThreads, kPaBlocks)
+__global__ void __launch_bounds__(pa_threads(N), pa_blocks(N))
 packed_attn_kernel(const PackedAttnParams p)
 {
-    constexpr int STAGES = pa_stages(N), SBUFS = pa_s_bufs(N);
+    constexpr int STAGES = pa_stages(N), KB = pa_k_bufs(N), VB = pa_v_bufs(N), THREADS = pa_threads(N);
     constexpr int NC = N <= 32 ? N : 32;                    // softmax columns of a thread
-    constexpr int SOFT = N <= 32 ? 128 : 256;               // softmax threads
+    constexpr int SOFT = pa_soft(N);                        // softmax threads
+    constexpr int SOFT0 = 8, MMA = SOFT0 + SOFT / 32, COPY = MMA + 1;      // first softmax warp, the others
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -148,14 +154,19 @@ packed_attn_kernel(const PackedAttnParams p)
     float *const neg_m = reinterpret_cast<float *>(list + kPaListCols);                     // [N] minus the rows' reference maxima
     float *const l_sm = neg_m + N;                                                          // [N]; while a maximum is raised: factors
     uint64_t *const bars = reinterpret_cast<uint64_t *>(l_sm + N);
-    int2 *const s_local = reinterpret_cast<int2 *>(bars + 2 * STAGES + 6);                  // [8] the local columns
-    int *const s_cnt = reinterpret_cast<int *>(s_local + kPaTileCols);                      // [8]
-    uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(s_cnt + 8);
-    const uint32_t bar0 = smem_u32(bars), bar_k = bar0 + 16u * STAGES, bar_v = bar_k + 8u, bar_p = bar_k + 16u, bar_o = bar_k + 24u;
+    int2 *const s_local = reinterpret_cast<int2 *>(bars + 2 * STAGES + 10);                  // [8] the local columns
+    int *const s_cnt = reinterpret_cast<int *>(s_local + kPaTileCols);                      // [columns / 32]
+    uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(s_cnt + kPaListCols / 32);
+    const uint32_t bar0 = smem_u32(bars), bar1 = bar0 + 16u * STAGES, bar_p = bar1 + 64u;
     auto bar_full = [&](int s) { return bar0 + 8u * s; };
     auto bar_empty = [&](int s) { return bar0 + 8u * (STAGES + s); };
-    auto bar_s = [&](int k) { return bar_k + 32u + 8u * (k % SBUFS); };                    // of tile k
-    auto par_s = [&](int k) { return (uint32_t)((k / SBUFS) & 1); };
+    auto bar_k = [&](int i) { return bar1 + 8u * (i % KB); };           // keys, values of tile i unpacked
+    auto bar_v = [&](int i) { return bar1 + 16u + 8u * (i % VB); };
+    auto bar_s = [&](int i) { return bar1 + 32u + 8u * (i & 1); };      // logits of tile i there
+    auto bar_o = [&](int i) { return bar1 + 48u + 8u * (i & 1); };      // accumulators complete up to tile i
+    auto par_k = [&](int i) { return (uint32_t)((i / KB) & 1); };
+    auto par_v = [&](int i) { return (uint32_t)((i / VB) & 1); };
+    auto par_2 = [&](int i) { return (uint32_t)((i >> 1) & 1); };
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int grp = CLUSTER ? (blockIdx.x / p.n_splits) % p.n_groups : blockIdx.x % p.n_groups;
@@ -163,19 +174,20 @@ packed_attn_kernel(const PackedAttnParams p)
     const int bh = blockIdx.x / (p.n_groups * p.n_splits);
     const int b = bh / p.Hkv, h = bh % p.Hkv;
     const int row0 = grp * p.group_rows, rows = min(p.group_rows, p.R - row0);
-    if (warp == 8) {
+    if (warp == MMA) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)kPaTmemCols) : "memory");
+                     ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)pa_tmem_cols(N)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 8); }
-        mbar_init(bar_k, 4);
-        mbar_init(bar_v, 4);
+        for (int k = 0; k < 2; ++k) {
+            mbar_init(bar1 + 8u * k, 4);
+            mbar_init(bar1 + 16u + 8u * k, 4);
+            mbar_init(bar_s(k), 1);
+            mbar_init(bar_o(k), 1);
+        }
         mbar_init(bar_p, SOFT / 32);
-        mbar_init(bar_o, 1);
-        mbar_init(bar_s(0), 1);
-        if (SBUFS > 1) mbar_init(bar_s(1), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < N) neg_m[tid] = CUDART_INF_F;
@@ -184,21 +196,24 @@ packed_attn_kernel(const PackedAttnParams p)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- the split's columns ------------------------------------------------------------------------------------
-    // Tiles of a row: the local columns (if any), then eight packed columns each.  Thread k < 256 holds the split's column k.
+    // Tiles of a row: the local columns (if any), then eight packed columns each.  Thread k < 256 holds the split's columns k, k + 256, ..
     const int has_local = p.n_cols > p.local_col;
     const int t0 = split * p.tiles_per_split, t1 = t0 + p.tiles_per_split;
     const int c0 = max(t0 - has_local, 0) * kPaTileCols, c1 = min((t1 - has_local) * kPaTileCols, p.local_col);
     const int32_t *blk_row = p.blk_tbl + (long long)bh * p.n_cols, *slot_row = p.slot_tbl + (long long)bh * p.n_cols;
     const long long L = p.seq_len[b], last = L + p.T - 1;               // last position that a row sees
-    int2 col = make_int2(-1, -1);
-    if (warp < 8) {
-        if (c0 + tid < c1) col = make_int2(blk_row[c0 + tid], slot_row[c0 + tid]);
-    } else if (warp == 8 && lane < kPaTileCols && has_local && t0 == 0 && p.local_col + lane < p.n_cols) {
-        col = make_int2(blk_row[p.local_col + lane], slot_row[p.local_col + lane]);
+    int2 col[kPaListCols / 256];
+#pragma unroll
+    for (int k = 0; k < kPaListCols / 256; ++k) {
+        const int c = c0 + tid + 256 * k;
+        col[k] = make_int2(-1, -1);
+        if (warp < 8 && c < c1) col[k] = make_int2(blk_row[c], slot_row[c]);
     }
+    if (warp == MMA && lane < kPaTileCols && has_local && t0 == 0 && p.local_col + lane < p.n_cols)
+        col[0] = make_int2(blk_row[p.local_col + lane], slot_row[p.local_col + lane]);
     // Q: 16 bytes (chunk c of row r) at a time; rows past the group's are zero
 #pragma unroll 4
-    for (int i = tid; i < N * 16; i += kPaThreads) {
+    for (int i = tid; i < N * 16; i += THREADS) {
         const int r = i >> 4, c = i & 15;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (r < rows) {
@@ -208,31 +223,41 @@ packed_attn_kernel(const PackedAttnParams p)
         *reinterpret_cast<uint4 *>(base_ptr + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    bool seen = col.x >= 0 && (long long)col.x * kBlock <= last;
-    if (kBoundsCheck && seen) seen = in_range(col.y, p.bd.n_slots, p.bd, kErrSlot);
-    const unsigned got = __ballot_sync(0xffffffffu, seen);
-    if (warp < 8 && lane == 0) s_cnt[warp] = __popc(got);
-    if (warp == 8 && lane < kPaTileCols) s_local[lane] = seen ? col : make_int2(-1, -1);
+    bool seen[kPaListCols / 256], late = false;
+    unsigned got[kPaListCols / 256];
+#pragma unroll
+    for (int k = 0; k < kPaListCols / 256; ++k) {
+        seen[k] = col[k].x >= 0 && (long long)col[k].x * kBlock <= last;
+        if (kBoundsCheck && seen[k]) seen[k] = in_range(col[k].y, p.bd.n_slots, p.bd, kErrSlot);
+        late |= warp < 8 && seen[k] && (long long)col[k].x * kBlock + kBlock - 1 > L;        // some token of it not every row sees
+        got[k] = __ballot_sync(0xffffffffu, seen[k]);
+        if (warp < 8 && lane == 0) s_cnt[8 * k + warp] = __popc(got[k]);
+    }
+    if (warp == MMA && lane < kPaTileCols) s_local[lane] = seen[0] ? col[0] : make_int2(-1, -1);
     tc_fence_before();
-    __syncthreads();
+    late = __syncthreads_or(late);
     tc_fence_after();
     int count = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        if (w == warp && seen) list[count + __popc(got & ((1u << lane) - 1u))] = col;
-        count += s_cnt[w];
-    }
+    for (int k = 0; k < kPaListCols / 256; ++k)
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            if (w == warp && seen[k]) list[count + __popc(got[k] & ((1u << lane) - 1u))] = col[k];
+            count += s_cnt[8 * k + w];
+        }
     int do_local = 0;
 #pragma unroll
     for (int k = 0; k < kPaTileCols; ++k) do_local |= s_local[k].x >= 0;
     const int packed_tiles = (count + kPaTileCols - 1) / kPaTileCols, n_tiles = do_local + packed_tiles;
-    const uint32_t tmem = *tmem_slot, t_k = tmem, t_v = tmem + 64, t_s = tmem + 128, t_o = t_s + SBUFS * N;
+    const uint32_t tmem = *tmem_slot, t_s = tmem + 64 * (KB + VB), t_o = t_s + 2 * N;
+    auto t_k = [&](int i) { return tmem + 64u * (uint32_t)(i % KB); };
+    auto t_v = [&](int i) { return tmem + 64u * (uint32_t)(KB + i % VB); };
     __syncthreads();                                                     // the list is complete
 
     float *const o_sm = reinterpret_cast<float *>(ring);                 // [N][128], after the last tile
     float *const l_part = reinterpret_cast<float *>(p_ptr);              // [4][N], after the last tile
     bool alive = true;
-    if (warp == 9) {
+    if (warp == COPY) {
         // ---------------------------------------------------------------- copies
         int s = 0, pi = 0;
         uint32_t ph = 1;
@@ -252,57 +277,148 @@ packed_attn_kernel(const PackedAttnParams p)
         }
         if (!alive)                                                      // nobody leaves while copies are on their way
             for (int k = max(0, pi - STAGES); k < pi; ++k) mbar_wait_warp(bar_full(k % STAGES), (k / STAGES) & 1, p.err, 82);
-    } else if (warp == 8) {
+    } else if (warp == MMA) {
         // ---------------------------------------------------------------- products (the whole warp, converged)
         const uint64_t q_desc = smem_desc_sw128(base), p_desc = pa_p_desc<N>(base + N * kRowBytes);
-        auto keys = [&](int i) {
-            alive = alive && mbar_wait_warp(bar_k, i & 1, p.err, 83);
-            if (!alive) return;
-            tc_fence_after();
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                tc_mma_bf16_ts(t_s + (i % SBUFS) * N, t_k + 8 * k, q_desc + (uint64_t)(((k >> 2) * (N * 128) + (k & 3) * 32) >> 4), pa_idesc(N, false),
-                               k ? 1u : 0u);
-            tc_commit(bar_s(i));
-        };
         auto values = [&](int i) {
-            alive = alive && mbar_wait_warp(bar_v, i & 1, p.err, 84) && mbar_wait_warp(bar_p, i & 1, p.err, 85);
+            alive = alive && mbar_wait_warp(bar_v(i), par_v(i), p.err, 84) && mbar_wait_warp(bar_p, i & 1, p.err, 85);
             if (!alive) return;
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < kPaTileCols; ++k)
-                tc_mma_bf16_ts(t_o, t_v + 8 * k, p_desc + (uint64_t)((k * 32 * N) >> 4), pa_idesc(N, true), (i > 0 || k) ? 1u : 0u);
-            tc_commit(bar_o);
+                tc_mma_bf16_ts(t_o, t_v(i) + 8 * k, p_desc + (uint64_t)((k * 32 * N) >> 4), pa_idesc(N, true), (i > 0 || k) ? 1u : 0u);
+            tc_commit(bar_o(i));
         };
 #pragma unroll 1
         for (int i = 0; i < n_tiles && alive; ++i) {
-            if (SBUFS == 1 && i > 0) values(i - 1);                      // (one S buffer: its tile has to be read first)
-            keys(i);
-            if (SBUFS > 1 && i > 0) values(i - 1);
+            alive = mbar_wait_warp(bar_k(i), par_k(i), p.err, 83);
+            // (two S buffers: the softmax has read tile i - 2's when its weights came, before V^T P of that tile)
+            if (!alive) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                tc_mma_bf16_ts(t_s + (i & 1) * N, t_k(i) + 8 * k, q_desc + (uint64_t)(((k >> 2) * (N * 128) + (k & 3) * 32) >> 4), pa_idesc(N, false),
+                               k ? 1u : 0u);
+            tc_commit(bar_s(i));
+            if (i > 0) values(i - 1);
         }
         if (n_tiles > 0) values(n_tiles - 1);
+    } else if (warp < SOFT0) {
+        // ---------------------------------------------------------------- unpacking: thread = token (keys) or dim (values)
+        const int me = tid & 127, kb = me >> 4, tok = me & 15;
+        const bool keys = warp < 4;
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        int s = 0;
+        uint32_t ph = 0;
+#pragma unroll 1
+        for (int i = 0; i < n_tiles; ++i) {                              // (a wait that gave up: no more waits)
+            const bool loc = do_local && i == 0;
+            if (!loc) alive = alive && mbar_wait_warp(bar_full(s), ph, p.err, 87);
+            const uint8_t *const stage = ring + s * kPaStageBytes;
+            // the product that read this buffer's last tile is over
+            if (keys && i >= KB) alive = alive && mbar_wait_warp(bar_s(i - KB), par_2(i - KB), p.err, 88);
+            if (!keys && i >= VB) alive = alive && mbar_wait_warp(bar_o(i - VB), par_2(i - VB), p.err, 89);
+            tc_fence_after();
+            const uint32_t dst = (keys ? t_k(i) : t_v(i)) + lane_base;
+            if (loc && keys) {
+                const int2 e = s_local[kb];
+                const bool any = e.x >= 0 && (long long)e.x * kBlock + tok <= last;         // (others may hold anything)
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.local + (long long)(any ? e.y : 0) * kEntryBytes + tok * kRowBytes);
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t r[16];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint4 v = any ? src[4 * c + k] : make_uint4(0, 0, 0, 0);
+                        r[4 * k] = v.x; r[4 * k + 1] = v.y; r[4 * k + 2] = v.z; r[4 * k + 3] = v.w;
+                    }
+                    tc_st16(dst + c * 16, r);
+                }
+            } else if (loc) {
+#pragma unroll 1
+                for (int k2 = 0; k2 < kPaTileCols; k2 += 2) {
+                    uint32_t r[16];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int2 e = s_local[k2 + u];
+                        const uint16_t *src = reinterpret_cast<const uint16_t *>(p.local + (long long)(e.x >= 0 ? e.y : 0) * kEntryBytes + kPartBytes) + me;
+                        // tokens past the last visible one may hold anything
+                        const int n = e.x >= 0 ? (int)min((long long)kBlock, last - (long long)e.x * kBlock + 1) : 0;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint32_t lo = 2 * j < n ? src[2 * j * kHeadDim] : 0u, hi = 2 * j + 1 < n ? src[(2 * j + 1) * kHeadDim] : 0u;
+                            r[8 * u + j] = lo | hi << 16;
+                        }
+                    }
+                    tc_st16(dst + k2 * 8, r);
+                }
+            } else if (keys) {
+                const uint8_t *ent = stage + kb * kPackedBytes;
+#pragma unroll 2
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(ent + c * 256 + tok * 16);
+                    const uint32_t sc = *reinterpret_cast<const uint16_t *>(ent + kPackedKScale + tok * 8 + c * 2);
+                    uint32_t r[16];
+                    const DequantScale d0 = dequant_scale(__byte_perm(sc, 0u, 0x4040));
+                    const DequantScale d1 = dequant_scale(__byte_perm(sc, 0u, 0x4141));
+                    dequant_word(w.x, d0, r);
+                    dequant_word(w.y, d0, r + 4);
+                    dequant_word(w.z, d1, r + 8);
+                    dequant_word(w.w, d1, r + 12);
+                    tc_st16(dst + c * 16, r);
+                }
+            } else {
+#pragma unroll 2
+                for (int k2 = 0; k2 < kPaTileCols; k2 += 2) {
+                    uint32_t r[16];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint8_t *ent = stage + (k2 + u) * kPackedBytes;
+                        const uint2 w = *reinterpret_cast<const uint2 *>(ent + kPackedV + me * 8);
+                        const DequantScale d = dequant_scale(ent[kPackedVScale + me] * 0x00010001u);
+                        dequant_word(w.x, d, r + 8 * u);
+                        dequant_word(w.y, d, r + 8 * u + 4);
+                    }
+                    tc_st16(dst + k2 * 8, r);
+                }
+            }
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(keys ? bar_k(i) : bar_v(i));
+                if (!loc) mbar_arrive(bar_empty(s));
+            }
+            if (!loc) ring_advance(s, ph, 1, STAGES);
+        }
     } else {
-        // ---------------------------------------------------------------- unpacking and softmax
-        const int side = warp >> 2, me = tid & 127;                      // 0: keys, 1: values; token or dim
+        // ---------------------------------------------------------------- softmax: thread = token, one logit per query row
+        const int me = (tid - 32 * SOFT0) & 127, n0 = (warp - SOFT0) / 4 * NC;        // token of the tile, first column
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const int kb = me >> 4, tok = me & 15;
-        const int n0 = side * NC;                                        // first softmax column of this thread
-        float l[NC];
+        uint64_t l2[NC / 2];                                             // sums of the weights, two columns each
 #pragma unroll
-        for (int n = 0; n < NC; ++n) l[n] = 0.f;
-
-        auto softmax = [&](int i) {                                      // of tile i, whose logits are there
+        for (int n = 0; n < NC / 2; ++n) l2[n] = 0;
+#pragma unroll 1
+        for (int i = 0; i < n_tiles; ++i) {                              // (a wait that gave up: no more waits, but every barrier)
             const bool loc = do_local && i == 0;
-            const int pi = i - do_local;
-            const int blk = loc ? s_local[kb].x : pi * kPaTileCols + kb < count ? list[pi * kPaTileCols + kb].x : -1;
-            // the first query row that sees this thread's token
-            const long long ahead = (long long)blk * kBlock + tok - L;
-            const int n_min = (blk < 0 || ahead >= p.T ? N : ahead <= 0 ? 0 : min(max((int)ahead * p.G - row0, 0), N)) - n0;
+            int n_min = 0;                                               // the first query row that sees this thread's token
+            bool masked = false;
+            if (late || loc || i == n_tiles - 1) {                       // (elsewhere eight blocks that every row sees whole)
+                const int at = (i - do_local) * kPaTileCols + kb;
+                const int blk = loc ? s_local[kb].x : at < count ? list[at].x : -1;
+                const long long ahead = (long long)blk * kBlock + tok - L;
+                n_min = (blk < 0 || ahead >= p.T ? N : ahead <= 0 ? 0 : min(max((int)ahead * p.G - row0, 0), N)) - n0;
+                masked = __any_sync(0xffffffffu, n_min > 0);
+            }
             const float scale = loc ? p.scale_log2 : p.scale_log2 * (float)(1 << kDequantShift);
-            const uint32_t t_mine = t_s + (i % SBUFS) * N + n0 + lane_base;
-            float x[16];                                                 // sixteen columns at a time (32: read a second time for the weights)
-            bool masked = __any_sync(0xffffffffu, n_min > 0);
-            auto logits = [&](int c) {
+            const uint32_t t_mine = t_s + (i & 1) * N + n0 + lane_base;
+            alive = alive && mbar_wait_warp(bar_s(i), par_2(i), p.err, 90);
+            tc_fence_after();
+            // sixteen columns at a time, as (logit - reference) in log2 units (32: read a second time for the weights)
+            float x[16];
+            const uint64_t scale2 = f32x2(scale, scale);
+            auto read = [&](int c) {
                 uint32_t v[16];
                 tc_ld16(t_mine + c * 16, v);
 #pragma unroll
@@ -313,27 +429,33 @@ packed_attn_kernel(const PackedAttnParams p)
                         if (c * 16 + n < n_min) x[n] = -CUDART_INF_F;
                 }
             };
+            auto relative = [&](int c) {
+#pragma unroll
+                for (int n = 0; n < 16; n += 4) {
+                    const float4 m = *reinterpret_cast<const float4 *>(neg_m + n0 + c * 16 + n);
+                    f32x2_split(fma_f32x2(f32x2(x[n], x[n + 1]), scale2, f32x2(m.x, m.y)), x[n], x[n + 1]);
+                    f32x2_split(fma_f32x2(f32x2(x[n + 2], x[n + 3]), scale2, f32x2(m.z, m.w)), x[n + 2], x[n + 3]);
+                }
+            };
             float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
             for (int c = 0; c < NC / 16; ++c) {
-                logits(c);
+                read(c);
+                relative(c);
 #pragma unroll
-                for (int n = 0; n < 16; n += 8) {
-                    const float4 m = *reinterpret_cast<const float4 *>(neg_m + n0 + c * 16 + n), w = *reinterpret_cast<const float4 *>(neg_m + n0 + c * 16 + n + 4);
-                    m4[0] = max3(m4[0], fmaf(x[n], scale, m.x), fmaf(x[n + 4], scale, w.x));
-                    m4[1] = max3(m4[1], fmaf(x[n + 1], scale, m.y), fmaf(x[n + 5], scale, w.y));
-                    m4[2] = max3(m4[2], fmaf(x[n + 2], scale, m.z), fmaf(x[n + 6], scale, w.z));
-                    m4[3] = max3(m4[3], fmaf(x[n + 3], scale, m.w), fmaf(x[n + 7], scale, w.w));
+                for (int n = 0; n < 4; ++n) {
+                    m4[n] = max3(m4[n], x[n], x[n + 4]);
+                    m4[n] = max3(m4[n], x[n + 8], x[n + 12]);
                 }
             }
             const bool raise = pa_any<SOFT>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) > kPaRaise);
             // V^T P of the tile before has read its weights, and O is complete up to it
-            if (i > 0) alive = alive && mbar_wait(bar_o, (i - 1) & 1, p.err, 86);
+            if (i > 0) alive = alive && mbar_wait_warp(bar_o(i - 1), par_2(i - 1), p.err, 86);
             if (raise) {
                 int *const w_max = reinterpret_cast<int *>(p_ptr);       // [4][N]: P is written later
 #pragma unroll
                 for (int c = 0; c < NC / 16; ++c) {
-                    if (NC > 16) logits(c);
+                    read(c);
 #pragma unroll
                     for (int n = 0; n < 16; ++n) {
                         const int m = __reduce_max_sync(0xffffffffu, ordered(x[n]));
@@ -341,16 +463,17 @@ packed_attn_kernel(const PackedAttnParams p)
                     }
                 }
                 pa_sync<SOFT>();
-                if (tid < N) {
-                    const float m_old = -neg_m[tid];
-                    const float mx = unordered(max(max(w_max[tid], w_max[N + tid]), max(w_max[2 * N + tid], w_max[3 * N + tid]))) * scale;
+                const int n = tid - 32 * SOFT0;
+                if (n < N) {
+                    const float m_old = -neg_m[n];
+                    const float mx = unordered(max(max(w_max[n], w_max[N + n]), max(w_max[2 * N + n], w_max[3 * N + n]))) * scale;
                     const float m_new = fmaxf(m_old, mx);
-                    neg_m[tid] = -m_new;
-                    l_sm[tid] = m_new == -CUDART_INF_F ? 1.f : fast_exp2(m_old - m_new);
+                    neg_m[n] = -m_new;
+                    l_sm[n] = m_new == -CUDART_INF_F ? 1.f : fast_exp2(m_old - m_new);
                 }
                 pa_sync<SOFT>();
 #pragma unroll
-                for (int n = 0; n < NC; ++n) l[n] *= l_sm[n0 + n];
+                for (int k = 0; k < NC / 2; ++k) l2[k] = fma_f32x2(l2[k], f32x2(l_sm[n0 + 2 * k], l_sm[n0 + 2 * k + 1]), 0);
                 if (i > 0) {
                     tc_fence_after();
 #pragma unroll
@@ -363,173 +486,72 @@ packed_attn_kernel(const PackedAttnParams p)
                     }
                     tc_wait_st();
                 }
-            }
-            const float unit = loc ? 1.f / (float)(1 << kDequantShift) : 1.f;      // the accumulator's unit is 2^-kDequantShift
-#pragma unroll
-            for (int c = 0; c < NC / 8; ++c) {
-                if (NC > 16 && c % 2 == 0) logits(c / 2);
-                float e[8];
-#pragma unroll
-                for (int k = 0; k < 8; k += 4) {
-                    const float4 m = *reinterpret_cast<const float4 *>(neg_m + n0 + 8 * c + k);
-                    const float mm[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) e[k + u] = fast_exp2(fmaf(x[8 * (c % 2) + k + u], scale, mm[u]));
+                if (NC == 16) {
+                    read(0);
+                    relative(0);
                 }
+            }
+#pragma unroll
+            for (int c = 0; c < NC / 16; ++c) {
+                if (NC > 16) read(c);
+                if (NC > 16) relative(c);
+#pragma unroll
+                for (int n = 0; n < 16; ++n) x[n] = fast_exp2(x[n]);
                 if (masked) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (8 * c + k < n_min) e[k] = 0.f;
+                    for (int n = 0; n < 16; ++n)
+                        if (c * 16 + n < n_min) x[n] = 0.f;
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) l[8 * c + k] += e[k];
-                if (loc) {
+                for (int n = 0; n < 8; ++n) l2[c * 8 + n] = add_f32x2(l2[c * 8 + n], f32x2(x[2 * n], x[2 * n + 1]));
+                if (loc) {                                               // the accumulator's unit is 2^-kDequantShift
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) e[k] *= unit;
+                    for (int n = 0; n < 16; ++n) x[n] *= 1.f / (float)(1 << kDequantShift);
                 }
-                *reinterpret_cast<uint4 *>(p_ptr + pa_p_chunk<N>(me, n0 / 8 + c)) =
-                    make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7]));
+#pragma unroll
+                for (int k = 0; k < 16; k += 8)
+                    *reinterpret_cast<uint4 *>(p_ptr + pa_p_chunk<N>(me, (n0 + c * 16 + k) / 8)) =
+                        make_uint4(pack_bf16x2(x[k], x[k + 1]), pack_bf16x2(x[k + 2], x[k + 3]), pack_bf16x2(x[k + 4], x[k + 5]), pack_bf16x2(x[k + 6], x[k + 7]));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_p);
-        };
-
-        int s = 0;
-        uint32_t ph = 0;
-#pragma unroll 1
-        for (int i = 0; i <= n_tiles; ++i) {                             // (a wait that gave up: no more waits, but every barrier)
-            const bool loc = do_local && i == 0;
-            if (!loc && i < n_tiles) alive = alive && mbar_wait(bar_full(s), ph, p.err, 87);
-            const uint8_t *const stage = ring + s * kPaStageBytes;
-            if (side == 0) {
-                // keys: K Q^T of the tile before has read its operand (and its logits are there)
-                if (i > 0) alive = alive && mbar_wait(bar_s(i - 1), par_s(i - 1), p.err, 88);
-                tc_fence_after();
-                if (i == n_tiles) {
-                } else if (loc) {
-                    const int2 e = s_local[kb];
-                    const bool any = e.x >= 0 && (long long)e.x * kBlock + tok <= last;     // (others may hold anything)
-                    const uint4 *src = reinterpret_cast<const uint4 *>(p.local + (long long)(any ? e.y : 0) * kEntryBytes + tok * kRowBytes);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t r[16];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint4 v = any ? src[4 * c + k] : make_uint4(0, 0, 0, 0);
-                            r[4 * k] = v.x; r[4 * k + 1] = v.y; r[4 * k + 2] = v.z; r[4 * k + 3] = v.w;
-                        }
-                        tc_st16(t_k + lane_base + c * 16, r);
-                    }
-                } else {
-                    const uint8_t *ent = stage + kb * kPackedBytes;
-                    const uint2 sc = *reinterpret_cast<const uint2 *>(ent + kPackedKScale + tok * 8);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint4 w = *reinterpret_cast<const uint4 *>(ent + c * 256 + tok * 16);
-                        uint32_t r[16];
-                        const DequantScale d0 = dequant_scale(__byte_perm(c < 2 ? sc.x : sc.y, 0u, c & 1 ? 0x4242 : 0x4040));
-                        const DequantScale d1 = dequant_scale(__byte_perm(c < 2 ? sc.x : sc.y, 0u, c & 1 ? 0x4343 : 0x4141));
-                        dequant_word(w.x, d0, r);
-                        dequant_word(w.y, d0, r + 4);
-                        dequant_word(w.z, d1, r + 8);
-                        dequant_word(w.w, d1, r + 12);
-                        tc_st16(t_k + lane_base + c * 16, r);
-                    }
-                }
-            } else {
-                // values: V^T P of the tile before has read its operand
-                if (i > 0) alive = alive && mbar_wait(bar_o, (i - 1) & 1, p.err, 89);
-                tc_fence_after();
-                if (i == n_tiles) {
-                } else if (loc) {
-#pragma unroll
-                    for (int k2 = 0; k2 < kPaTileCols; k2 += 2) {
-                        uint32_t r[16];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int2 e = s_local[k2 + u];
-                            const uint16_t *src = reinterpret_cast<const uint16_t *>(p.local + (long long)(e.x >= 0 ? e.y : 0) * kEntryBytes + kPartBytes) + me;
-                            // tokens past the last visible one may hold anything
-                            const int n = e.x >= 0 ? (int)min((long long)kBlock, last - (long long)e.x * kBlock + 1) : 0;
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const uint32_t lo = 2 * j < n ? src[2 * j * kHeadDim] : 0u, hi = 2 * j + 1 < n ? src[(2 * j + 1) * kHeadDim] : 0u;
-                                r[8 * u + j] = lo | hi << 16;
-                            }
-                        }
-                        tc_st16(t_v + lane_base + k2 * 8, r);
-                    }
-                } else {
-#pragma unroll
-                    for (int k2 = 0; k2 < kPaTileCols; k2 += 2) {
-                        uint32_t r[16];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const uint8_t *ent = stage + (k2 + u) * kPackedBytes;
-                            const uint2 w = *reinterpret_cast<const uint2 *>(ent + kPackedV + me * 8);
-                            const DequantScale d = dequant_scale(ent[kPackedVScale + me] * 0x00010001u);
-                            dequant_word(w.x, d, r + 8 * u);
-                            dequant_word(w.y, d, r + 8 * u + 4);
-                        }
-                        tc_st16(t_v + lane_base + k2 * 8, r);
-                    }
-                }
-            }
-            if (i < n_tiles) {
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(side == 0 ? bar_k : bar_v);
-                    if (!loc) mbar_arrive(bar_empty(s));
-                }
-                if (!loc) ring_advance(s, ph, 1, STAGES);
-            }
-            // the key warps' softmax is one tile behind their unpacking, the value warps' (their columns) level with it
-            const int tile = side == 0 ? i - 1 : SOFT == 256 && i < n_tiles ? i : -1;
-            if (tile < 0) continue;
-            if (side == 1) {
-                alive = alive && mbar_wait(bar_s(i), par_s(i), p.err, 90);
-                tc_fence_after();
-            }
-            softmax(tile);
         }
-        if (n_tiles > 0 && side == 0) alive = alive && mbar_wait(bar_o, (n_tiles - 1) & 1, p.err, 92);
+        if (n_tiles > 0) alive = alive && mbar_wait_warp(bar_o(n_tiles - 1), par_2(n_tiles - 1), p.err, 92);
         tc_fence_after();
         // ---- the split's result: accumulators and sums to shared memory (the ring and P are idle)
         if (n_tiles > 0 && alive) {
 #pragma unroll
-            for (int c = 0; c < N / 16; ++c) {
-                if (N > 16 ? (c & 1) != side : side != 0) continue;      // the two sides take turns
+            for (int c = 0; c < NC / 16; ++c) {
                 uint32_t v[16];
-                tc_ld16(t_o + lane_base + c * 16, v);
+                tc_ld16(t_o + n0 + lane_base + c * 16, v);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o_sm[(c * 16 + e) * kHeadDim + me] = __uint_as_float(v[e]) * (float)(1 << kDequantShift);
+                for (int e = 0; e < 16; ++e) o_sm[(n0 + c * 16 + e) * kHeadDim + me] = __uint_as_float(v[e]) * (float)(1 << kDequantShift);
             }
         }
-        if (SOFT == 256 || side == 0) {
-            // the threads' sums of a row: half of the values change hands in every round, so that lane k ends with row k (or k / 2)
-            int w = NC / 2;
+        // the threads' sums of a row: half of the values change hands in every round, so that lane k ends with row k (or k / 2)
+        float l[NC];
 #pragma unroll
-            for (int bit = 16; bit >= 1; bit >>= 1) {
-                const bool up = lane & bit;
-                if (w >= 1) {
+        for (int n = 0; n < NC / 2; ++n) f32x2_split(l2[n], l[2 * n], l[2 * n + 1]);
+        int w = NC / 2;
 #pragma unroll
-                    for (int k = 0; k < NC / 2; ++k)
-                        if (k < w) {
-                            const float give = up ? l[k] : l[k + w], keep = up ? l[k + w] : l[k];
-                            l[k] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
-                        }
-                    w >>= 1;
-                } else {
-                    l[0] += __shfl_xor_sync(0xffffffffu, l[0], bit);
-                }
+        for (int bit = 16; bit >= 1; bit >>= 1) {
+            const bool up = lane & bit;
+            if (w >= 1) {
+#pragma unroll
+                for (int k = 0; k < NC / 2; ++k)
+                    if (k < w) {
+                        const float give = up ? l[k] : l[k + w], keep = up ? l[k + w] : l[k];
+                        l[k] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
+                    }
+                w >>= 1;
+            } else {
+                l[0] += __shfl_xor_sync(0xffffffffu, l[0], bit);
             }
-            if (NC == 32) l_part[(warp & 3) * N + n0 + lane] = l[0];
-            else if (!(lane & 1)) l_part[(warp & 3) * N + (lane >> 1)] = l[0];
         }
+        if (NC == 32) l_part[(warp & 3) * N + n0 + lane] = l[0];
+        else if (!(lane & 1)) l_part[(warp & 3) * N + (lane >> 1)] = l[0];
     }
     alive = __syncthreads_and(alive);
     if (tid < N) l_sm[tid] = n_tiles > 0 ? l_part[tid] + l_part[N + tid] + l_part[2 * N + tid] + l_part[3 * N + tid] : 0.f;
@@ -540,9 +562,9 @@ packed_attn_kernel(const PackedAttnParams p)
     } else {
         __syncthreads();
     }
-    if (alive && warp < 8) {
+    if (alive && warp < MMA) {
         // one warp per row; in a cluster, block `split` takes rows split, split + n_splits, ..
-        const int first = CLUSTER ? split + p.n_splits * warp : warp, step = CLUSTER ? 8 * p.n_splits : 8, parts = CLUSTER ? p.n_splits : 1;
+        const int first = CLUSTER ? split + p.n_splits * warp : warp, step = CLUSTER ? MMA * p.n_splits : MMA, parts = CLUSTER ? p.n_splits : 1;
 #pragma unroll 1
         for (int r = first; r < rows; r += step) {
             float m = -CUDART_INF_F, den = 0.f;
@@ -601,8 +623,8 @@ packed_attn_kernel(const PackedAttnParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 8)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kPaTmemCols) : "memory");
+    if (warp == MMA)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)pa_tmem_cols(N)) : "memory");
 }
 
 // Merges the splits of one query row: out = sum_s w_s o_s / sum_s w_s with w_s = 2^(lse_s - max lse).  One warp per row, four output
@@ -672,7 +694,7 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
     const long long items = (long long)dims->batch * dims->n_kv_heads * pl.n_groups;
     const int tiles = (local_col + kPaTileCols - 1) / kPaTileCols + (n_cols > local_col ? 1 : 0);
     // all thread blocks resident at once as far as the tiles can be split
-    long long s = items > 0 ? (long long)sm_count() * kPaBlocks / items : 1;
+    long long s = items > 0 ? (long long)sm_count() * pa_blocks(pl.n) / items : 1;
     if (s > tiles) s = tiles;
     if (s < 1) s = 1;
     const int most = kPaListCols / kPaTileCols;                          // tiles whose columns a thread block can list
@@ -751,7 +773,6 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
     attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)pl.items);
-    cfg.blockDim = dim3(kPaThreads);
     cfg.stream = (cudaStream_t)stream;
     cfg.attrs = attr;
     cfg.numAttrs = pl.in_cluster ? 2 : 1;
@@ -764,6 +785,7 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
     } while (0)
 #define OASIS_PACKED_LAUNCH(N)                                                                                                \
     do {                                                                                                                      \
+        cfg.blockDim = dim3(pa_threads(N));                                                                                   \
         cfg.dynamicSmemBytes = pa_smem(N);                                                                                    \
         if (pl.in_cluster) OASIS_PACKED_LAUNCH_AS(N, true);                                                                   \
         else OASIS_PACKED_LAUNCH_AS(N, false);                                                                                \
