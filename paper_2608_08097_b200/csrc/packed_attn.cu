@@ -136,6 +136,79 @@ __device__ __forceinline__ void pa_sync()
     asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }
 
+// The end of a thread block's work: its rows' accumulators (o_sm, PITCH floats a row), reference maxima (neg_m, negated, log2) and
+// sums (l_sm) become outputs, or the split's part of them.  `warps` warps take a row each; in a cluster, block `split` takes rows split,
+// split + n_splits, .. of all its blocks.  Called by the whole thread block.
+template <bool CLUSTER, int PITCH>
+__device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive, int warp, int warps, int lane, int split, int rows, int row0, int b, int h,
+                                          const float *o_sm, const float *neg_m, const float *l_sm)
+{
+    if constexpr (CLUSTER) {
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        __syncthreads();
+    }
+    if (alive && warp < warps) {
+        const int first = CLUSTER ? split + p.n_splits * warp : warp, step = CLUSTER ? warps * p.n_splits : warps, parts = CLUSTER ? p.n_splits : 1;
+#pragma unroll 1
+        for (int r = first; r < rows; r += step) {
+            float m = -CUDART_INF_F, den = 0.f;
+            float4 f[CLUSTER ? kPaMaxCluster : 1];
+            if constexpr (CLUSTER) {
+#pragma unroll
+                for (int k = 0; k < kPaMaxCluster; ++k)
+                    if (k < parts) f[k] = pa_ld_cluster4(pa_at_rank(o_sm + r * PITCH + lane * 4, (uint32_t)k));
+                if (lane < parts) {
+                    m = -pa_ld_cluster(pa_at_rank(neg_m + r, (uint32_t)lane));
+                    den = pa_ld_cluster(pa_at_rank(l_sm + r, (uint32_t)lane));
+                }
+            } else {
+                f[0] = *reinterpret_cast<const float4 *>(o_sm + r * PITCH + lane * 4);
+                if (lane == 0) {
+                    m = -neg_m[r];
+                    den = l_sm[r];
+                }
+            }
+            const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(m)));
+            float w = m == -CUDART_INF_F ? 0.f : fast_exp2(m - top);
+            den *= w;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+            den = __shfl_sync(0xffffffffu, den, 0);
+            w *= den > 0.f ? 1.f / den : 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < (CLUSTER ? kPaMaxCluster : 1); ++k) {
+                const float wk = __shfl_sync(0xffffffffu, w, k);
+                if (k < parts && wk != 0.f) {                            // (a part that saw no key has not written its accumulator)
+                    acc.x = fmaf(wk, f[k].x, acc.x);
+                    acc.y = fmaf(wk, f[k].y, acc.y);
+                    acc.z = fmaf(wk, f[k].z, acc.z);
+                    acc.w = fmaf(wk, f[k].w, acc.w);
+                }
+            }
+            const float lse2 = den > 0.f ? top + log2f(den) : den == 0.f ? -CUDART_INF_F : den;
+            if (CLUSTER || p.n_splits == 1) {
+                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+                const long long o = ((long long)b * p.T + tq) * p.Hq + a;
+                reinterpret_cast<uint2 *>(p.out + o * kRowBytes)[lane] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+                if (p.lse && lane == 0) p.lse[o] = lse2 * kAtLn2;
+            } else {
+                const long long o = (long long)blockIdx.x * p.group_rows + r;
+                reinterpret_cast<float4 *>(p.part_o + o * kHeadDim)[lane] = acc;
+                if (lane == 0) p.part_lse[o] = lse2;
+            }
+        }
+    }
+    if constexpr (CLUSTER) {
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");       // nobody leaves while its shared memory is read
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+}
+
 // N: columns of the products (query rows, padded).
 template <int N, bool CLUSTER>
 __global__ void __launch_bounds__(pa_threads(N), pa_blocks(N))
@@ -555,76 +628,380 @@ packed_attn_kernel(const PackedAttnParams p)
     }
     alive = __syncthreads_and(alive);
     if (tid < N) l_sm[tid] = n_tiles > 0 ? l_part[tid] + l_part[N + tid] + l_part[2 * N + tid] + l_part[3 * N + tid] : 0.f;
-    if constexpr (CLUSTER) {
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    } else {
-        __syncthreads();
-    }
-    if (alive && warp < MMA) {
-        // one warp per row; in a cluster, block `split` takes rows split, split + n_splits, ..
-        const int first = CLUSTER ? split + p.n_splits * warp : warp, step = CLUSTER ? MMA * p.n_splits : MMA, parts = CLUSTER ? p.n_splits : 1;
-#pragma unroll 1
-        for (int r = first; r < rows; r += step) {
-            float m = -CUDART_INF_F, den = 0.f;
-            float4 f[CLUSTER ? kPaMaxCluster : 1];
-            if constexpr (CLUSTER) {
-#pragma unroll
-                for (int k = 0; k < kPaMaxCluster; ++k)
-                    if (k < parts) f[k] = pa_ld_cluster4(pa_at_rank(o_sm + r * kHeadDim + lane * 4, (uint32_t)k));
-                if (lane < parts) {
-                    m = -pa_ld_cluster(pa_at_rank(neg_m + r, (uint32_t)lane));
-                    den = pa_ld_cluster(pa_at_rank(l_sm + r, (uint32_t)lane));
-                }
-            } else {
-                f[0] = *reinterpret_cast<const float4 *>(o_sm + r * kHeadDim + lane * 4);
-                if (lane == 0) {
-                    m = -neg_m[r];
-                    den = l_sm[r];
-                }
-            }
-            const float top = unordered(__reduce_max_sync(0xffffffffu, ordered(m)));
-            float w = m == -CUDART_INF_F ? 0.f : fast_exp2(m - top);
-            den *= w;
-#pragma unroll
-            for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-            den = __shfl_sync(0xffffffffu, den, 0);
-            w *= den > 0.f ? 1.f / den : 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < (CLUSTER ? kPaMaxCluster : 1); ++k) {
-                const float wk = __shfl_sync(0xffffffffu, w, k);
-                if (k < parts && wk != 0.f) {                            // (a part that saw no key has not written its accumulator)
-                    acc.x = fmaf(wk, f[k].x, acc.x);
-                    acc.y = fmaf(wk, f[k].y, acc.y);
-                    acc.z = fmaf(wk, f[k].z, acc.z);
-                    acc.w = fmaf(wk, f[k].w, acc.w);
-                }
-            }
-            const float lse2 = den > 0.f ? top + log2f(den) : den == 0.f ? -CUDART_INF_F : den;
-            if (CLUSTER || p.n_splits == 1) {
-                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
-                const long long o = ((long long)b * p.T + tq) * p.Hq + a;
-                reinterpret_cast<uint2 *>(p.out + o * kRowBytes)[lane] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-                if (p.lse && lane == 0) p.lse[o] = lse2 * kAtLn2;
-            } else {
-                const long long o = (long long)blockIdx.x * p.group_rows + r;
-                reinterpret_cast<float4 *>(p.part_o + o * kHeadDim)[lane] = acc;
-                if (lane == 0) p.part_lse[o] = lse2;
-            }
-        }
-    }
-    if constexpr (CLUSTER) {
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");       // nobody leaves while its shared memory is read
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
+    pa_finish<CLUSTER, kHeadDim>(p, alive, warp, MMA, lane, split, rows, row0, b, h, o_sm, neg_m, l_sm);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == MMA)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)pa_tmem_cols(N)) : "memory");
+}
+
+// ---- up to 32 query rows: every warp by itself ----------------------------------------------------------------------------
+// With few rows the products are small and what a tile costs above is mostly its way through five roles and their barriers (about
+// 500 of 1,000 instructions a scheduler spends per 128 tokens, and 2,200 cycles of latency).  Here a warp takes 32 tokens (two
+// blocks) through unpacking, softmax and products alone, with warp-wide products of 16 rows x 8 tokens (or dims) x 16: no barrier
+// but the arrival of its own copies.  The layout of the entries fits the products' operands, because the order of a contraction is
+// free: in S = Q K^T lane (g, t) = (lane / 4, lane % 4) brings 32 dims, chunk t, of one token; in O += P V it brings eight tokens, a
+// 32-bit word, of one dim; and the columns of S are dealt so that the weights a lane has computed are those its word of V needs:
+//   product j of four, column n = 2 t + e  <->  token 8 (t & 1) + 2 j + e of block t >> 1.
+// MT: products of 16 query rows.
+constexpr int kPfThreads = 128, kPfWarps = 4;
+constexpr int kPfUnitBytes = 2 * kPackedBytes;
+constexpr int kPfPitch = kHeadDim + 4;
+__host__ __device__ constexpr int pf_blocks(int mt) { return mt == 1 ? 3 : 2; }             // thread blocks per SM
+__host__ __device__ constexpr int pf_stages(int mt) { return mt == 1 ? 3 : 4; }             // units of a warp in flight
+// Shared memory: Q fragments | rings | column list | statistics and barriers.
+__host__ __device__ constexpr int pf_smem(int mt)
+{
+    return 128 + mt * 4096 + kPfWarps * pf_stages(mt) * kPfUnitBytes + kPaListCols * 8 + 1536;
+}
+static_assert((pf_smem(1) + 1024) * pf_blocks(1) <= 233472 && (pf_smem(2) + 1024) * pf_blocks(2) <= 233472, "thread blocks per SM");
+static_assert(pf_stages(1) * kPfUnitBytes >= 16 * kPfPitch * 4 && pf_stages(2) * kPfUnitBytes >= 32 * kPfPitch * 4, "a warp's accumulator fits into its ring");
+
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
+
+template <int MT, bool CLUSTER>
+__global__ void __launch_bounds__(kPfThreads, pf_blocks(MT))
+packed_attn_few_kernel(const PackedAttnParams p)
+{
+    constexpr int STAGES = pf_stages(MT), ROWS = 16 * MT;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *const base_ptr = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+    uint4 *const q_frag = reinterpret_cast<uint4 *>(base_ptr);                              // [MT][8 steps][32 lanes]
+    uint8_t *const rings = base_ptr + MT * 4096;
+    int2 *const list = reinterpret_cast<int2 *>(rings + kPfWarps * STAGES * kPfUnitBytes);   // (block, slot)
+    float *const neg_m = reinterpret_cast<float *>(list + kPaListCols);                       // [warps][ROWS], then [ROWS] of the block
+    float *const l_sm = neg_m + kPfWarps * ROWS;
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(l_sm + kPfWarps * ROWS);              // [warps][STAGES]
+    int2 *const s_local = reinterpret_cast<int2 *>(bars + kPfWarps * STAGES);                 // [8]
+    int *const s_cnt = reinterpret_cast<int *>(s_local + kPaTileCols);                        // [columns / 32]
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int split = CLUSTER ? blockIdx.x % p.n_splits : blockIdx.x % p.n_splits;
+    const int bh = blockIdx.x / p.n_splits;
+    const int b = bh / p.Hkv, h = bh % p.Hkv;
+    const int rows = p.R;
+    const uint32_t bar0 = smem_u32(bars + warp * STAGES);
+    uint8_t *const ring = rings + warp * STAGES * kPfUnitBytes;
+    if (lane == 0) {
+        for (int s = 0; s < STAGES; ++s) mbar_init(bar0 + 8u * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    // This launch may have been brought onto the SMs before the previous one ended: what that wrote is read from here on.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- the split's columns, as in packed_attn_kernel -----------------------------------------------------------
+    constexpr int PER = kPaListCols / kPfThreads;
+    const int has_local = p.n_cols > p.local_col;
+    const int t0 = split * p.tiles_per_split, t1 = t0 + p.tiles_per_split;
+    const int c0 = max(t0 - has_local, 0) * kPaTileCols, c1 = min((t1 - has_local) * kPaTileCols, p.local_col);
+    const int32_t *blk_row = p.blk_tbl + (long long)bh * p.n_cols, *slot_row = p.slot_tbl + (long long)bh * p.n_cols;
+    const long long L = p.seq_len[b], last = L + p.T - 1;               // last position that a row sees
+    int2 col[PER], near = make_int2(-1, -1);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = c0 + tid + kPfThreads * k;
+        col[k] = make_int2(-1, -1);
+        if (c < c1) col[k] = make_int2(blk_row[c], slot_row[c]);
+    }
+    if (tid < kPaTileCols && has_local && t0 == 0 && p.local_col + tid < p.n_cols)
+        near = make_int2(blk_row[p.local_col + tid], slot_row[p.local_col + tid]);
+    // Q as the lanes of a product hold it: step k, lane (g, t): dims 32 t + 4 k .. + 3 of rows g and g + 8
+    for (int i = tid; i < MT * 256; i += kPfThreads) {
+        const int lt = i & 31, k = (i >> 5) & 7, r = (i >> 8) * 16 + (lt >> 2);
+        uint2 v[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = r + 8 * e;
+            v[e] = make_uint2(0, 0);
+            if (row < rows) {
+                const int tq = row / p.G, a = h * p.G + row % p.G;
+                v[e] = *reinterpret_cast<const uint2 *>(p.q + (((long long)b * p.T + tq) * p.Hq + a) * kRowBytes + (32 * (lt & 3) + 4 * k) * 2);
+            }
+        }
+        q_frag[i] = make_uint4(v[0].x, v[1].x, v[0].y, v[1].y);
+    }
+    bool seen[PER], late = false;
+    unsigned got[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        seen[k] = col[k].x >= 0 && (long long)col[k].x * kBlock <= last;
+        if (kBoundsCheck && seen[k]) seen[k] = in_range(col[k].y, p.bd.n_slots, p.bd, kErrSlot);
+        late |= seen[k] && (long long)col[k].x * kBlock + kBlock - 1 > L;                    // some token of it not every row sees
+        got[k] = __ballot_sync(0xffffffffu, seen[k]);
+        if (lane == 0) s_cnt[4 * k + warp] = __popc(got[k]);
+    }
+    if (warp == 0) {
+        bool ok = near.x >= 0 && (long long)near.x * kBlock <= last;
+        if (kBoundsCheck && ok) ok = in_range(near.y, p.bd.n_slots, p.bd, kErrSlot);
+        if (lane < kPaTileCols) s_local[lane] = ok ? near : make_int2(-1, -1);
+    }
+    late = __syncthreads_or(late);
+    int count = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+#pragma unroll
+        for (int w = 0; w < kPfWarps; ++w) {
+            if (w == warp && seen[k]) list[count + __popc(got[k] & ((1u << lane) - 1u))] = col[k];
+            count += s_cnt[4 * k + w];
+        }
+    __syncthreads();                                                     // the list is complete
+
+    // Lanes 0 and 1: the entries of the warp's unit k (units warp, warp + 4, ..) into its stage.
+    const int n_units = (count + 1) / 2, mine = n_units > warp ? (n_units - warp + kPfWarps - 1) / kPfWarps : 0;
+    auto request = [&](int k, int s) {
+        const int at = 2 * (warp + kPfWarps * k), n = min(2, count - at);
+        if (lane == 0) mbar_arrive_expect_tx(bar0 + 8u * s, (uint32_t)(n * kPackedBytes));
+        __syncwarp();
+        if (lane < n)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(smem_u32(ring) + (uint32_t)(s * kPfUnitBytes + lane * kPackedBytes)),
+                           "l"(p.packed + (long long)list[at + lane].y * kPackedBytes), "r"((uint32_t)kPackedBytes), "r"(bar0 + 8u * s) : "memory");
+    };
+#pragma unroll 1
+    for (int k = 0; k < min(STAGES, mine); ++k) request(k, k);
+
+    float o[MT][16][4], m_neg[MT][2], l[MT][2];                          // accumulators; rows g and g + 8 of each product
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[mt][j][e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { m_neg[mt][e] = CUDART_INF_F; l[mt][e] = 0.f; }
+    }
+    float s[MT][4][4];                                                   // logits of a unit
+    uint4 pw[MT][2];                                                     // weights of a unit, as the operand of P V
+    // From logits to weights.  blk: this lane's block (that of its two columns of every product); `mask`: some token may be hidden.
+    auto softmax = [&](int blk, bool mask, float scale, float unit) {
+        if (mask) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const long long ahead = (long long)blk * kBlock + 8 * (t & 1) + 2 * j + e - L;
+                    const int n_min = blk < 0 || ahead >= p.T ? ROWS : ahead <= 0 ? 0 : (int)min(ahead * p.G, (long long)ROWS);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        if (16 * mt + g < n_min) s[mt][j][e] = -CUDART_INF_F;
+                        if (16 * mt + g + 8 < n_min) s[mt][j][2 + e] = -CUDART_INF_F;
+                    }
+                }
+        }
+        float top = -CUDART_INF_F;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                top = max3(top, fmaf(s[mt][j][0], scale, m_neg[mt][0]), fmaf(s[mt][j][1], scale, m_neg[mt][0]));
+                top = max3(top, fmaf(s[mt][j][2], scale, m_neg[mt][1]), fmaf(s[mt][j][3], scale, m_neg[mt][1]));
+            }
+        if (__any_sync(0xffffffffu, top > kPaRaise)) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = -CUDART_INF_F;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) mx = max3(mx, s[mt][j][2 * e], s[mt][j][2 * e + 1]);
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    const float m_new = fmaxf(-m_neg[mt][e], mx * scale);
+                    const float f = m_new == -CUDART_INF_F ? 1.f : fast_exp2(-m_neg[mt][e] - m_new);
+                    m_neg[mt][e] = -m_new;
+                    l[mt][e] *= f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) { o[mt][j][2 * e] *= f; o[mt][j][2 * e + 1] *= f; }
+                }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            uint32_t w[4][2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float a = fast_exp2(fmaf(s[mt][j][2 * e], scale, m_neg[mt][e])), c = fast_exp2(fmaf(s[mt][j][2 * e + 1], scale, m_neg[mt][e]));
+                    if (mask) {
+                        if (s[mt][j][2 * e] == -CUDART_INF_F) a = 0.f;
+                        if (s[mt][j][2 * e + 1] == -CUDART_INF_F) c = 0.f;
+                    }
+                    l[mt][e] += a + c;
+                    w[j][e] = pack_bf16x2(a * unit, c * unit);
+                }
+            pw[mt][0] = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
+            pw[mt][1] = make_uint4(w[2][0], w[2][1], w[3][0], w[3][1]);
+        }
+    };
+    auto clear = [&]() {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[mt][j][e] = 0.f;
+    };
+    const int kblk = g >> 2, ktok = 8 * ((g >> 1) & 1) + (g & 1);        // keys: token ktok + 2 j of block kblk for product j
+
+    // ---- the local columns: unit k of two blocks is warp 3 - k's, straight from global memory
+    const int2 la = s_local[2 * (3 - warp)], lb = s_local[2 * (3 - warp) + 1];
+    if (la.x >= 0 || lb.x >= 0) {
+        clear();
+        const int2 kl = kblk ? lb : la, vl = t >> 1 ? lb : la;
+#pragma unroll 1
+        for (int k = 0; k < 8; ++k) {                                    // step k: dims 32 t + 4 k .. + 3
+            uint2 w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int tok = ktok + 2 * j;
+                w[j] = make_uint2(0, 0);
+                if (kl.x >= 0 && (long long)kl.x * kBlock + tok <= last)                    // (others may hold anything)
+                    w[j] = *reinterpret_cast<const uint2 *>(p.local + (long long)kl.y * kEntryBytes + tok * kRowBytes + (32 * t + 4 * k) * 2);
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const uint4 a = q_frag[(mt * 8 + k) * 32 + lane];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma_16x8x16(s[mt][j], a, w[j].x, w[j].y);
+            }
+        }
+        softmax(vl.x, true, p.scale_log2, 1.f / (float)(1 << kDequantShift));
+        const uint16_t *src = reinterpret_cast<const uint16_t *>(p.local + (long long)(vl.x >= 0 ? vl.y : 0) * kEntryBytes + kPartBytes) + 8 * (t & 1) * kHeadDim + g;
+        const int n = vl.x >= 0 ? (int)min(8ll, max(0ll, last - ((long long)vl.x * kBlock + 8 * (t & 1)) + 1)) : 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {                                   // dims 8 j + g
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t lo = 2 * k < n ? src[2 * k * kHeadDim + 8 * j] : 0u, hi = 2 * k + 1 < n ? src[(2 * k + 1) * kHeadDim + 8 * j] : 0u;
+                w[k] = lo | hi << 16;
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                mma_16x8x16(o[mt][j], pw[mt][0], w[0], w[1]);
+                mma_16x8x16(o[mt][j], pw[mt][1], w[2], w[3]);
+            }
+        }
+    }
+
+    // ---- the packed columns
+    bool alive = true;
+    int st = 0, k = 0;
+    uint32_t ph = 0;
+    const float scale = p.scale_log2 * (float)(1 << kDequantShift);
+#pragma unroll 1
+    for (; k < mine; ++k) {
+        alive = __all_sync(0xffffffffu, mbar_wait(bar0 + 8u * st, ph, p.err, 93));
+        if (!alive) break;
+        const uint8_t *const stage = ring + st * kPfUnitBytes;
+        clear();
+        {
+            const uint8_t *const ent = stage + kblk * kPackedBytes;
+            uint4 w[4];
+            uint32_t sc[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[j] = *reinterpret_cast<const uint4 *>(ent + 256 * t + 16 * (ktok + 2 * j));
+                sc[j] = *reinterpret_cast<const uint16_t *>(ent + kPackedKScale + 8 * (ktok + 2 * j) + 2 * t);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                DequantScale d[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[j] = dequant_scale(__byte_perm(sc[j], 0u, half ? 0x4141 : 0x4040));
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    uint32_t v[4][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) dequant_word(half ? (q ? w[j].w : w[j].z) : (q ? w[j].y : w[j].x), d[j], v[j]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            const uint4 a = q_frag[(mt * 8 + half * 4 + q * 2 + u) * 32 + lane];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) mma_16x8x16(s[mt][j], a, v[j][2 * u], v[j][2 * u + 1]);
+                        }
+                }
+            }
+        }
+        const int at = 2 * (warp + kPfWarps * k) + (t >> 1);
+        const bool mask = late || 2 * (warp + kPfWarps * k) + 2 > count;
+        softmax(mask ? (at < count ? list[at].x : -1) : 0, mask, scale, 1.f);
+        {
+            const uint8_t *const ent = stage + (t >> 1) * kPackedBytes;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {                               // dims 8 j + g
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(ent + kPackedV + 8 * (8 * j + g) + 4 * (t & 1));
+                const DequantScale d = dequant_scale(ent[kPackedVScale + 8 * j + g] * 0x00010001u);
+                uint32_t v[4];
+                dequant_word(w, d, v);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    mma_16x8x16(o[mt][j], pw[mt][0], v[0], v[1]);
+                    mma_16x8x16(o[mt][j], pw[mt][1], v[2], v[3]);
+                }
+            }
+        }
+        __syncwarp();                                                    // the stage has been read
+        if (k + STAGES < mine) request(k + STAGES, st);
+        ring_advance(st, ph, 1, STAGES);
+    }
+    if (!alive)                                                          // nobody leaves while copies are on their way
+        for (int j = 1; j < STAGES && k + j < mine; ++j) mbar_wait(bar0 + 8u * ((k + j) % STAGES), ((k + j) / STAGES) & 1, p.err, 94);
+    // ---- the warps' results come together
+    float *const o_mine = reinterpret_cast<float *>(ring);               // [ROWS][kPfPitch]
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float sum = l[mt][e];
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            const int r = 16 * mt + 8 * e + g;
+            if (t == 0) {
+                neg_m[warp * ROWS + r] = m_neg[mt][e];
+                l_sm[warp * ROWS + r] = sum;
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                *reinterpret_cast<float2 *>(o_mine + r * kPfPitch + 8 * j + 2 * t) = make_float2(o[mt][j][2 * e], o[mt][j][2 * e + 1]);
+        }
+    }
+    alive = __syncthreads_and(alive);
+    float *const o_sm = reinterpret_cast<float *>(rings);
+    constexpr int kPart = STAGES * kPfUnitBytes / 4;                     // floats between the warps' accumulators
+#pragma unroll 1
+    for (int r = warp; r < rows; r += kPfWarps) {
+        float m[kPfWarps], top = -CUDART_INF_F, den = 0.f;
+#pragma unroll
+        for (int w = 0; w < kPfWarps; ++w) {
+            m[w] = -neg_m[w * ROWS + r];
+            top = fmaxf(top, m[w]);
+        }
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kPfWarps; ++w) {
+            const float f = m[w] == -CUDART_INF_F ? 0.f : fast_exp2(m[w] - top);
+            const float4 v = *reinterpret_cast<const float4 *>(o_sm + w * kPart + r * kPfPitch + lane * 4);
+            den = fmaf(f, l_sm[w * ROWS + r], den);
+            acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+        }
+        const float k20 = (float)(1 << kDequantShift);
+        *reinterpret_cast<float4 *>(o_sm + r * kPfPitch + lane * 4) = make_float4(acc.x * k20, acc.y * k20, acc.z * k20, acc.w * k20);
+        __syncwarp();
+        if (lane == 0) {                                                 // (the row's places of warp 0, which only this warp reads)
+            neg_m[r] = -top;
+            l_sm[r] = den;
+        }
+    }
+    pa_finish<CLUSTER, kPfPitch>(p, alive, warp, kPfWarps, lane, split, rows, 0, b, h, o_sm, neg_m, l_sm);
 }
 
 // Merges the splits of one query row: out = sum_s w_s o_s / sum_s w_s with w_s = 2^(lse_s - max lse).  One warp per row, four output
@@ -691,10 +1068,11 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
     pl.n_groups = (R + 63) / 64;
     pl.group_rows = (R + pl.n_groups - 1) / pl.n_groups;
     pl.n = pl.group_rows <= 16 ? 16 : pl.group_rows <= 32 ? 32 : 64;
+    const int blocks = pl.n == 64 ? pa_blocks(64) : pf_blocks(pl.n / 16);
     const long long items = (long long)dims->batch * dims->n_kv_heads * pl.n_groups;
     const int tiles = (local_col + kPaTileCols - 1) / kPaTileCols + (n_cols > local_col ? 1 : 0);
     // all thread blocks resident at once as far as the tiles can be split
-    long long s = items > 0 ? (long long)sm_count() * pa_blocks(pl.n) / items : 1;
+    long long s = items > 0 ? (long long)sm_count() * blocks / items : 1;
     if (s > tiles) s = tiles;
     if (s < 1) s = 1;
     const int most = kPaListCols / kPaTileCols;                          // tiles whose columns a thread block can list
@@ -777,22 +1155,22 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
     cfg.attrs = attr;
     cfg.numAttrs = pl.in_cluster ? 2 : 1;
     cudaError_t e;
-#define OASIS_PACKED_LAUNCH_AS(N, X)                                                                                          \
+#define OASIS_PACKED_LAUNCH_AS(...)                                                                                           \
     do {                                                                                                                      \
-        e = allow_dynamic_shared(reinterpret_cast<const void *>(packed_attn_kernel<N, X>), pa_smem(N));                       \
-        if (e == cudaSuccess) prefer_max_shared_carveout(packed_attn_kernel<N, X>);                                           \
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, packed_attn_kernel<N, X>, p);                                      \
+        e = allow_dynamic_shared(reinterpret_cast<const void *>(__VA_ARGS__), (int)cfg.dynamicSmemBytes);                     \
+        if (e == cudaSuccess) prefer_max_shared_carveout(__VA_ARGS__);                                                        \
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, __VA_ARGS__, p);                                                   \
     } while (0)
-#define OASIS_PACKED_LAUNCH(N)                                                                                                \
+#define OASIS_PACKED_LAUNCH(KERNEL, N, THREADS, SMEM)                                                                         \
     do {                                                                                                                      \
-        cfg.blockDim = dim3(pa_threads(N));                                                                                   \
-        cfg.dynamicSmemBytes = pa_smem(N);                                                                                    \
-        if (pl.in_cluster) OASIS_PACKED_LAUNCH_AS(N, true);                                                                   \
-        else OASIS_PACKED_LAUNCH_AS(N, false);                                                                                \
+        cfg.blockDim = dim3(THREADS);                                                                                         \
+        cfg.dynamicSmemBytes = SMEM;                                                                                          \
+        if (pl.in_cluster) OASIS_PACKED_LAUNCH_AS(KERNEL<N, true>);                                                           \
+        else OASIS_PACKED_LAUNCH_AS(KERNEL<N, false>);                                                                        \
     } while (0)
-    if (pl.n == 16) OASIS_PACKED_LAUNCH(16);
-    else if (pl.n == 32) OASIS_PACKED_LAUNCH(32);
-    else OASIS_PACKED_LAUNCH(64);
+    if (pl.n == 16) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 1, kPfThreads, pf_smem(1));
+    else if (pl.n == 32) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 2, kPfThreads, pf_smem(2));
+    else OASIS_PACKED_LAUNCH(packed_attn_kernel, 64, pa_threads(64), pa_smem(64));
 #undef OASIS_PACKED_LAUNCH
 #undef OASIS_PACKED_LAUNCH_AS
     if (e != cudaSuccess) {
