@@ -639,40 +639,49 @@ packed_attn_kernel(const PackedAttnParams p)
 // ---- up to 32 query rows: every warp by itself ----------------------------------------------------------------------------
 // With few rows the products are small and what a tile costs above is mostly its way through five roles and their barriers (about
 // 500 of 1,000 instructions a scheduler spends per 128 tokens, and 2,200 cycles of latency).  Here a warp takes 32 tokens (two
-// blocks) through unpacking, softmax and products alone, with warp-wide products of 16 rows x 8 tokens (or dims) x 16: no barrier
-// but the arrival of its own copies.  The layout of the entries fits the products' operands, because the order of a contraction is
-// free: in S = Q K^T lane (g, t) = (lane / 4, lane % 4) brings 32 dims, chunk t, of one token; in O += P V it brings eight tokens, a
-// 32-bit word, of one dim; and the columns of S are dealt so that the weights a lane has computed are those its word of V needs:
-//   product j of four, column n = 2 t + e  <->  token 8 (t & 1) + 2 j + e of block t >> 1.
-// MT: products of 16 query rows.
+// blocks) through unpacking, softmax and products alone, with warp-wide products of 16 tokens (or dims) x 8 query rows x 16: no
+// barrier but the arrival of its own copies.  The layout of the entries fits the products' operands, because the order of a
+// contraction is free.  With lane = (g, t) = (lane / 4, lane % 4):
+//   S^T = K Q^T   the lane brings 32 dims, chunk t, of token 8 (t' & 1) + 2 j + e of block t' >> 1, g = 2 t' + e, for j = 0 .. 3
+//   O^T += V^T P^T   the lane brings a 32-bit word, tokens 8 (t & 1) .. + 7 of block t >> 1, of dims 16 m + g and + 8
+// so that the weights, transposed 8 x 8 (one instruction), are in the order of the words: tokens 2 j and 2 j + 1 of word t.
+// NT: products of 8 query rows.
 constexpr int kPfThreads = 128, kPfWarps = 4;
 constexpr int kPfUnitBytes = 2 * kPackedBytes;
 constexpr int kPfPitch = kHeadDim + 4;
-__host__ __device__ constexpr int pf_blocks(int mt) { return mt == 1 ? 3 : 2; }             // thread blocks per SM
-__host__ __device__ constexpr int pf_stages(int mt) { return mt == 1 ? 3 : 4; }             // units of a warp in flight
+__host__ __device__ constexpr int pf_blocks(int nt) { return nt == 1 ? 4 : nt == 2 ? 3 : 2; }       // thread blocks per SM
+__host__ __device__ constexpr int pf_stages(int nt) { return nt == 1 ? 2 : nt == 2 ? 3 : 4; }       // units of a warp in flight
 // Shared memory: Q fragments | rings | column list | statistics and barriers.
-__host__ __device__ constexpr int pf_smem(int mt)
+__host__ __device__ constexpr int pf_smem(int nt)
 {
-    return 128 + mt * 4096 + kPfWarps * pf_stages(mt) * kPfUnitBytes + kPaListCols * 8 + 1536;
+    return 128 + nt * 2048 + kPfWarps * pf_stages(nt) * kPfUnitBytes + kPaListCols * 8 + 1536;
 }
-static_assert((pf_smem(1) + 1024) * pf_blocks(1) <= 233472 && (pf_smem(2) + 1024) * pf_blocks(2) <= 233472, "thread blocks per SM");
-static_assert(pf_stages(1) * kPfUnitBytes >= 16 * kPfPitch * 4 && pf_stages(2) * kPfUnitBytes >= 32 * kPfPitch * 4, "a warp's accumulator fits into its ring");
+static_assert((pf_smem(1) + 1024) * pf_blocks(1) <= 233472 && (pf_smem(2) + 1024) * pf_blocks(2) <= 233472 && (pf_smem(3) + 1024) * pf_blocks(3) <= 233472 &&
+              (pf_smem(4) + 1024) * pf_blocks(4) <= 233472, "thread blocks per SM");
+static_assert(pf_stages(1) * kPfUnitBytes >= 8 * kPfPitch * 4 && pf_stages(2) * kPfUnitBytes >= 16 * kPfPitch * 4 &&
+              pf_stages(4) * kPfUnitBytes >= 32 * kPfPitch * 4, "a warp's accumulator fits into its ring");
 
-__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 
-template <int MT, bool CLUSTER>
-__global__ void __launch_bounds__(kPfThreads, pf_blocks(MT))
+template <int NT, bool CLUSTER>
+__global__ void __launch_bounds__(kPfThreads, pf_blocks(NT))
 packed_attn_few_kernel(const PackedAttnParams p)
 {
-    constexpr int STAGES = pf_stages(MT), ROWS = 16 * MT;
+    constexpr int STAGES = pf_stages(NT), ROWS = 8 * NT;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const base_ptr = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
-    uint4 *const q_frag = reinterpret_cast<uint4 *>(base_ptr);                              // [MT][8 steps][32 lanes]
-    uint8_t *const rings = base_ptr + MT * 4096;
+    uint4 *const q_frag = reinterpret_cast<uint4 *>(base_ptr);                              // [NT][4 pairs of steps][32 lanes]
+    uint8_t *const rings = base_ptr + NT * 2048;
     int2 *const list = reinterpret_cast<int2 *>(rings + kPfWarps * STAGES * kPfUnitBytes);   // (block, slot)
     float *const neg_m = reinterpret_cast<float *>(list + kPaListCols);                       // [warps][ROWS], then [ROWS] of the block
     float *const l_sm = neg_m + kPfWarps * ROWS;
@@ -681,7 +690,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
     int *const s_cnt = reinterpret_cast<int *>(s_local + kPaTileCols);                        // [columns / 32]
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int split = CLUSTER ? blockIdx.x % p.n_splits : blockIdx.x % p.n_splits;
+    const int split = blockIdx.x % p.n_splits;
     const int bh = blockIdx.x / p.n_splits;
     const int b = bh / p.Hkv, h = bh % p.Hkv;
     const int rows = p.R;
@@ -711,20 +720,15 @@ packed_attn_few_kernel(const PackedAttnParams p)
     }
     if (tid < kPaTileCols && has_local && t0 == 0 && p.local_col + tid < p.n_cols)
         near = make_int2(blk_row[p.local_col + tid], slot_row[p.local_col + tid]);
-    // Q as the lanes of a product hold it: step k, lane (g, t): dims 32 t + 4 k .. + 3 of rows g and g + 8
-    for (int i = tid; i < MT * 256; i += kPfThreads) {
-        const int lt = i & 31, k = (i >> 5) & 7, r = (i >> 8) * 16 + (lt >> 2);
-        uint2 v[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int row = r + 8 * e;
-            v[e] = make_uint2(0, 0);
-            if (row < rows) {
-                const int tq = row / p.G, a = h * p.G + row % p.G;
-                v[e] = *reinterpret_cast<const uint2 *>(p.q + (((long long)b * p.T + tq) * p.Hq + a) * kRowBytes + (32 * (lt & 3) + 4 * k) * 2);
-            }
+    // Q as the lanes of a product hold it: pair k of steps, lane (g, t): dims 32 t + 8 k .. + 7 of row g
+    for (int i = tid; i < NT * 128; i += kPfThreads) {
+        const int lt = i & 31, k = (i >> 5) & 3, row = (i >> 7) * 8 + (lt >> 2);
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < rows) {
+            const int tq = row / p.G, a = h * p.G + row % p.G;
+            v = *reinterpret_cast<const uint4 *>(p.q + (((long long)b * p.T + tq) * p.Hq + a) * kRowBytes + (32 * (lt & 3) + 8 * k) * 2);
         }
-        q_frag[i] = make_uint4(v[0].x, v[1].x, v[0].y, v[1].y);
+        q_frag[i] = v;
     }
     bool seen[PER], late = false;
     unsigned got[PER];
@@ -766,88 +770,85 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll 1
     for (int k = 0; k < min(STAGES, mine); ++k) request(k, k);
 
-    float o[MT][16][4], m_neg[MT][2], l[MT][2];                          // accumulators; rows g and g + 8 of each product
+    float o[NT][8][4], m_neg[NT][2], l[NT][2];                           // accumulators: dims 16 m + g, + 8; rows 8 nt + 2 t, + 1
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
+        for (int m = 0; m < 8; ++m)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[mt][j][e] = 0.f;
+            for (int e = 0; e < 4; ++e) o[nt][m][e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) { m_neg[mt][e] = CUDART_INF_F; l[mt][e] = 0.f; }
+        for (int e = 0; e < 2; ++e) { m_neg[nt][e] = CUDART_INF_F; l[nt][e] = 0.f; }
     }
-    float s[MT][4][4];                                                   // logits of a unit
-    uint4 pw[MT][2];                                                     // weights of a unit, as the operand of P V
-    // From logits to weights.  blk: this lane's block (that of its two columns of every product); `mask`: some token may be hidden.
+    float s[NT][4][2];                                                   // logits of a unit: token j of this lane, rows 2 t and 2 t + 1
+    uint32_t pw[NT][4];                                                  // weights of a unit, as the operand of V^T P^T
+    const int kblk = g >> 2, ktok = 8 * ((g >> 1) & 1) + (g & 1);        // keys: token ktok + 2 j of block kblk
+    // From logits to weights.  blk: the block of this lane's tokens; `mask`: some token may be hidden.
     auto softmax = [&](int blk, bool mask, float scale, float unit) {
         if (mask) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j) {
+                const long long ahead = (long long)blk * kBlock + ktok + 2 * j - L;
+                const int n_min = blk < 0 || ahead >= p.T ? ROWS : ahead <= 0 ? 0 : (int)min(ahead * p.G, (long long)ROWS);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const long long ahead = (long long)blk * kBlock + 8 * (t & 1) + 2 * j + e - L;
-                    const int n_min = blk < 0 || ahead >= p.T ? ROWS : ahead <= 0 ? 0 : (int)min(ahead * p.G, (long long)ROWS);
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        if (16 * mt + g < n_min) s[mt][j][e] = -CUDART_INF_F;
-                        if (16 * mt + g + 8 < n_min) s[mt][j][2 + e] = -CUDART_INF_F;
-                    }
-                }
+                    for (int e = 0; e < 2; ++e)
+                        if (8 * nt + 2 * t + e < n_min) s[nt][j][e] = -CUDART_INF_F;
+            }
         }
         float top = -CUDART_INF_F;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                top = max3(top, fmaf(s[mt][j][0], scale, m_neg[mt][0]), fmaf(s[mt][j][1], scale, m_neg[mt][0]));
-                top = max3(top, fmaf(s[mt][j][2], scale, m_neg[mt][1]), fmaf(s[mt][j][3], scale, m_neg[mt][1]));
-            }
+            for (int j = 0; j < 4; ++j)
+                top = max3(top, fmaf(s[nt][j][0], scale, m_neg[nt][0]), fmaf(s[nt][j][1], scale, m_neg[nt][1]));
         if (__any_sync(0xffffffffu, top > kPaRaise)) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = -CUDART_INF_F;
+                    float mx = fmaxf(fmaxf(s[nt][0][e], s[nt][1][e]), fmaxf(s[nt][2][e], s[nt][3][e]));
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) mx = max3(mx, s[mt][j][2 * e], s[mt][j][2 * e + 1]);
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                    const float m_new = fmaxf(-m_neg[mt][e], mx * scale);
-                    const float f = m_new == -CUDART_INF_F ? 1.f : fast_exp2(-m_neg[mt][e] - m_new);
-                    m_neg[mt][e] = -m_new;
-                    l[mt][e] *= f;
+                    for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                    const float m_new = fmaxf(-m_neg[nt][e], mx * scale);
+                    const float f = m_new == -CUDART_INF_F ? 1.f : fast_exp2(-m_neg[nt][e] - m_new);
+                    m_neg[nt][e] = -m_new;
+                    l[nt][e] *= f;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) { o[mt][j][2 * e] *= f; o[mt][j][2 * e + 1] *= f; }
+                    for (int m = 0; m < 8; ++m) { o[nt][m][e] *= f; o[nt][m][2 + e] *= f; }
                 }
         }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            uint32_t w[4][2];
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float a = fast_exp2(fmaf(s[mt][j][2 * e], scale, m_neg[mt][e])), c = fast_exp2(fmaf(s[mt][j][2 * e + 1], scale, m_neg[mt][e]));
-                    if (mask) {
-                        if (s[mt][j][2 * e] == -CUDART_INF_F) a = 0.f;
-                        if (s[mt][j][2 * e + 1] == -CUDART_INF_F) c = 0.f;
-                    }
-                    l[mt][e] += a + c;
-                    w[j][e] = pack_bf16x2(a * unit, c * unit);
+            for (int j = 0; j < 4; ++j) {
+                float a = fast_exp2(fmaf(s[nt][j][0], scale, m_neg[nt][0])), c = fast_exp2(fmaf(s[nt][j][1], scale, m_neg[nt][1]));
+                if (mask) {
+                    if (s[nt][j][0] == -CUDART_INF_F) a = 0.f;
+                    if (s[nt][j][1] == -CUDART_INF_F) c = 0.f;
                 }
-            pw[mt][0] = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
-            pw[mt][1] = make_uint4(w[2][0], w[2][1], w[3][0], w[3][1]);
-        }
+                l[nt][0] += a;
+                l[nt][1] += c;
+                pw[nt][j] = transpose_8x8(pack_bf16x2(a * unit, c * unit));
+            }
     };
+    // S^T of four tokens per lane: tokens 0, 1 are rows g, g + 8 of the first product, 2, 3 of the second.
+    float acc[NT][2][4];
     auto clear = [&]() {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[nt][0][e] = acc[nt][1][e] = 0.f;
+    };
+    auto logits = [&]() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[mt][j][e] = 0.f;
+                for (int e = 0; e < 2; ++e) s[nt][j][e] = acc[nt][j >> 1][2 * (j & 1) + e];
     };
-    const int kblk = g >> 2, ktok = 8 * ((g >> 1) & 1) + (g & 1);        // keys: token ktok + 2 j of block kblk for product j
 
     // ---- the local columns: unit k of two blocks is warp 3 - k's, straight from global memory
     const int2 la = s_local[2 * (3 - warp)], lb = s_local[2 * (3 - warp) + 1];
@@ -855,37 +856,43 @@ packed_attn_few_kernel(const PackedAttnParams p)
         clear();
         const int2 kl = kblk ? lb : la, vl = t >> 1 ? lb : la;
 #pragma unroll 1
-        for (int k = 0; k < 8; ++k) {                                    // step k: dims 32 t + 4 k .. + 3
-            uint2 w[4];
+        for (int k = 0; k < 4; ++k) {                                    // dims 32 t + 8 k .. + 7
+            uint4 w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int tok = ktok + 2 * j;
-                w[j] = make_uint2(0, 0);
+                w[j] = make_uint4(0, 0, 0, 0);
                 if (kl.x >= 0 && (long long)kl.x * kBlock + tok <= last)                    // (others may hold anything)
-                    w[j] = *reinterpret_cast<const uint2 *>(p.local + (long long)kl.y * kEntryBytes + tok * kRowBytes + (32 * t + 4 * k) * 2);
+                    w[j] = *reinterpret_cast<const uint4 *>(p.local + (long long)kl.y * kEntryBytes + tok * kRowBytes + (32 * t + 8 * k) * 2);
             }
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const uint4 a = q_frag[(mt * 8 + k) * 32 + lane];
+            for (int nt = 0; nt < NT; ++nt) {
+                const uint4 q = q_frag[(nt * 4 + k) * 32 + lane];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) mma_16x8x16(s[mt][j], a, w[j].x, w[j].y);
+                for (int m = 0; m < 2; ++m) {
+                    mma_16x8x16(acc[nt][m], w[2 * m].x, w[2 * m + 1].x, w[2 * m].y, w[2 * m + 1].y, q.x, q.y);
+                    mma_16x8x16(acc[nt][m], w[2 * m].z, w[2 * m + 1].z, w[2 * m].w, w[2 * m + 1].w, q.z, q.w);
+                }
             }
         }
-        softmax(vl.x, true, p.scale_log2, 1.f / (float)(1 << kDequantShift));
+        logits();
+        softmax(kl.x, true, p.scale_log2, 1.f / (float)(1 << kDequantShift));
         const uint16_t *src = reinterpret_cast<const uint16_t *>(p.local + (long long)(vl.x >= 0 ? vl.y : 0) * kEntryBytes + kPartBytes) + 8 * (t & 1) * kHeadDim + g;
         const int n = vl.x >= 0 ? (int)min(8ll, max(0ll, last - ((long long)vl.x * kBlock + 8 * (t & 1)) + 1)) : 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {                                   // dims 8 j + g
-            uint32_t w[4];
+        for (int m = 0; m < 8; ++m) {                                    // dims 16 m + g, + 8
+            uint32_t w[2][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t lo = 2 * k < n ? src[2 * k * kHeadDim + 8 * j] : 0u, hi = 2 * k + 1 < n ? src[(2 * k + 1) * kHeadDim + 8 * j] : 0u;
-                w[k] = lo | hi << 16;
-            }
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                mma_16x8x16(o[mt][j], pw[mt][0], w[0], w[1]);
-                mma_16x8x16(o[mt][j], pw[mt][1], w[2], w[3]);
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t lo = 2 * k < n ? src[2 * k * kHeadDim + 16 * m + 8 * u] : 0u, hi = 2 * k + 1 < n ? src[(2 * k + 1) * kHeadDim + 16 * m + 8 * u] : 0u;
+                    w[u][k] = lo | hi << 16;
+                }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                mma_16x8x16(o[nt][m], w[0][0], w[1][0], w[0][1], w[1][1], pw[nt][0], pw[nt][1]);
+                mma_16x8x16(o[nt][m], w[0][2], w[1][2], w[0][3], w[1][3], pw[nt][2], pw[nt][3]);
             }
         }
     }
@@ -916,36 +923,41 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) d[j] = dequant_scale(__byte_perm(sc[j], 0u, half ? 0x4141 : 0x4040));
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int u = 0; u < 2; ++u) {
                     uint32_t v[4][4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) dequant_word(half ? (q ? w[j].w : w[j].z) : (q ? w[j].y : w[j].x), d[j], v[j]);
+                    for (int j = 0; j < 4; ++j) dequant_word(half ? (u ? w[j].w : w[j].z) : (u ? w[j].y : w[j].x), d[j], v[j]);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint4 q = q_frag[(nt * 4 + half * 2 + u) * 32 + lane];
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            const uint4 a = q_frag[(mt * 8 + half * 4 + q * 2 + u) * 32 + lane];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) mma_16x8x16(s[mt][j], a, v[j][2 * u], v[j][2 * u + 1]);
+                        for (int m = 0; m < 2; ++m) {
+                            mma_16x8x16(acc[nt][m], v[2 * m][0], v[2 * m + 1][0], v[2 * m][1], v[2 * m + 1][1], q.x, q.y);
+                            mma_16x8x16(acc[nt][m], v[2 * m][2], v[2 * m + 1][2], v[2 * m][3], v[2 * m + 1][3], q.z, q.w);
                         }
+                    }
                 }
             }
         }
-        const int at = 2 * (warp + kPfWarps * k) + (t >> 1);
+        const int at = 2 * (warp + kPfWarps * k) + kblk;
         const bool mask = late || 2 * (warp + kPfWarps * k) + 2 > count;
+        logits();
         softmax(mask ? (at < count ? list[at].x : -1) : 0, mask, scale, 1.f);
         {
             const uint8_t *const ent = stage + (t >> 1) * kPackedBytes;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {                               // dims 8 j + g
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(ent + kPackedV + 8 * (8 * j + g) + 4 * (t & 1));
-                const DequantScale d = dequant_scale(ent[kPackedVScale + 8 * j + g] * 0x00010001u);
-                uint32_t v[4];
-                dequant_word(w, d, v);
+            for (int m = 0; m < 8; ++m) {                                // dims 16 m + g, + 8
+                uint32_t v[2][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    mma_16x8x16(o[mt][j], pw[mt][0], v[0], v[1]);
-                    mma_16x8x16(o[mt][j], pw[mt][1], v[2], v[3]);
+                for (int u = 0; u < 2; ++u) {
+                    const int dim = 16 * m + 8 * u + g;
+                    const uint32_t w = *reinterpret_cast<const uint32_t *>(ent + kPackedV + 8 * dim + 4 * (t & 1));
+                    dequant_word(w, dequant_scale(ent[kPackedVScale + dim] * 0x00010001u), v[u]);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mma_16x8x16(o[nt][m], v[0][0], v[1][0], v[0][1], v[1][1], pw[nt][0], pw[nt][1]);
+                    mma_16x8x16(o[nt][m], v[0][2], v[1][2], v[0][3], v[1][3], pw[nt][2], pw[nt][3]);
                 }
             }
         }
@@ -958,20 +970,22 @@ packed_attn_few_kernel(const PackedAttnParams p)
     // ---- the warps' results come together
     float *const o_mine = reinterpret_cast<float *>(ring);               // [ROWS][kPfPitch]
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            float sum = l[mt][e];
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            const int r = 16 * mt + 8 * e + g;
-            if (t == 0) {
-                neg_m[warp * ROWS + r] = m_neg[mt][e];
+            float sum = l[nt][e];
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            const int r = 8 * nt + 2 * t + e;
+            if (g == 0) {
+                neg_m[warp * ROWS + r] = m_neg[nt][e];
                 l_sm[warp * ROWS + r] = sum;
             }
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                *reinterpret_cast<float2 *>(o_mine + r * kPfPitch + 8 * j + 2 * t) = make_float2(o[mt][j][2 * e], o[mt][j][2 * e + 1]);
+            for (int m = 0; m < 8; ++m) {
+                o_mine[r * kPfPitch + 16 * m + g] = o[nt][m][e];
+                o_mine[r * kPfPitch + 16 * m + g + 8] = o[nt][m][2 + e];
+            }
         }
     }
     alive = __syncthreads_and(alive);
@@ -1067,8 +1081,8 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
     const int R = T * (dims->n_q_heads / dims->n_kv_heads);
     pl.n_groups = (R + 63) / 64;
     pl.group_rows = (R + pl.n_groups - 1) / pl.n_groups;
-    pl.n = pl.group_rows <= 16 ? 16 : pl.group_rows <= 32 ? 32 : 64;
-    const int blocks = pl.n == 64 ? pa_blocks(64) : pf_blocks(pl.n / 16);
+    pl.n = pl.group_rows <= 32 ? (pl.group_rows + 7) / 8 * 8 : 64;
+    const int blocks = pl.n == 64 ? pa_blocks(64) : pf_blocks(pl.n / 8);
     const long long items = (long long)dims->batch * dims->n_kv_heads * pl.n_groups;
     const int tiles = (local_col + kPaTileCols - 1) / kPaTileCols + (n_cols > local_col ? 1 : 0);
     // all thread blocks resident at once as far as the tiles can be split
@@ -1168,8 +1182,10 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
         if (pl.in_cluster) OASIS_PACKED_LAUNCH_AS(KERNEL<N, true>);                                                           \
         else OASIS_PACKED_LAUNCH_AS(KERNEL<N, false>);                                                                        \
     } while (0)
-    if (pl.n == 16) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 1, kPfThreads, pf_smem(1));
-    else if (pl.n == 32) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 2, kPfThreads, pf_smem(2));
+    if (pl.n == 8) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 1, kPfThreads, pf_smem(1));
+    else if (pl.n == 16) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 2, kPfThreads, pf_smem(2));
+    else if (pl.n == 24) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 3, kPfThreads, pf_smem(3));
+    else if (pl.n == 32) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 4, kPfThreads, pf_smem(4));
     else OASIS_PACKED_LAUNCH(packed_attn_kernel, 64, pa_threads(64), pa_smem(64));
 #undef OASIS_PACKED_LAUNCH
 #undef OASIS_PACKED_LAUNCH_AS
