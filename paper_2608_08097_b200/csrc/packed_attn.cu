@@ -30,40 +30,38 @@ namespace oasis {
 
 constexpr int kPaTileCols = 8, kPaTileKeys = kPaTileCols * kBlock;       // 128 tokens: the rows of one MMA
 constexpr int kPaStageBytes = kPaTileCols * kPackedBytes;                // 18 KiB
-constexpr int kPaListCols = 768;                                         // columns of a split at most
 constexpr int kPaMaxCluster = 8;
 constexpr float kPaRaise = 32.f;                                         // (log2) how far a logit may exceed its row's reference
-// Warps: 0-3 keys, 4-7 values, then four per 32 columns for the softmax, one for the products, one for the copies.
-__host__ __device__ constexpr int pa_soft(int n) { return n <= 32 ? 128 : 256; }            // softmax threads
+// packed_attn_kernel, n = 64, 96 or 128 columns.  Warps: 0-3 keys, 4-7 values, then four per 32 columns for the softmax, one for the
+// products, one for the copies.
+constexpr int kPaListCols = 2048;                                        // columns of a split at most
+__host__ __device__ constexpr int pa_soft(int n) { return 4 * n; }                          // softmax threads
 __host__ __device__ constexpr int pa_threads(int n) { return 256 + pa_soft(n) + 64; }
-__host__ __device__ constexpr int pa_blocks(int n) { return n <= 32 ? 2 : 1; }              // thread blocks per SM
-__host__ __device__ constexpr int pa_stages(int n) { return n <= 32 ? 4 : 8; }
-__host__ __device__ constexpr int pa_k_bufs(int n) { return n <= 32 ? 1 : 2; }              // K and V operands in tensor memory
-__host__ __device__ constexpr int pa_v_bufs(int n) { return n == 32 ? 1 : 2; }
+__host__ __device__ constexpr int pa_stages(int n) { return n == 64 ? 7 : 5; }
+__host__ __device__ constexpr int pa_k_bufs(int n) { return n == 64 ? 2 : 1; }              // K and V operands in tensor memory
+__host__ __device__ constexpr int pa_v_bufs(int n) { return n == 128 ? 1 : 2; }
 __host__ __device__ constexpr int pa_tmem_used(int n) { return 64 * (pa_k_bufs(n) + pa_v_bufs(n)) + 3 * n; }     // K | V | two S | O
-__host__ __device__ constexpr int pa_tmem_cols(int n) { return n <= 32 ? 256 : 512; }
-// Shared memory: Q [dim half][n rows][128 B] | P [128 tokens][2 n B] | ring | column list | statistics and barriers.
-constexpr int kPaMisc = 1024;
+constexpr int kPaTmemCols = 512;
+// Shared memory: Q [dim half][n rows][128 B] | P [64 columns][128 tokens][128 B] | ring | column list | statistics and barriers.
+__host__ __device__ constexpr int pa_p_bytes(int n) { return (n + 63) / 64 * kPaTileKeys * 128; }
 __host__ __device__ constexpr int pa_smem(int n)
 {
-    return 1024 + n * kRowBytes + kPaTileKeys * 2 * n + pa_stages(n) * kPaStageBytes + kPaListCols * 8 + kPaMisc;
+    return 1024 + n * kRowBytes + pa_p_bytes(n) + pa_stages(n) * kPaStageBytes + kPaListCols * 8 + 2048;
 }
-static_assert((pa_smem(16) + 1024) * pa_blocks(16) <= 233472 && (pa_smem(32) + 1024) * pa_blocks(32) <= 233472 && (pa_smem(64) + 1024) * pa_blocks(64) <= 233472,
-              "thread blocks per SM");
-static_assert(pa_tmem_used(16) <= pa_tmem_cols(16) && pa_tmem_used(32) <= pa_tmem_cols(32) && pa_tmem_used(64) <= pa_tmem_cols(64), "tensor memory");
-static_assert(pa_tmem_cols(32) * pa_blocks(32) <= 512 && pa_tmem_cols(64) * pa_blocks(64) <= 512, "tensor memory of an SM");
-static_assert(pa_stages(64) * kPaStageBytes >= 64 * kHeadDim * 4, "the accumulator fits into the ring");
+static_assert(pa_smem(64) <= 232448 && pa_smem(96) <= 232448 && pa_smem(128) <= 232448, "shared memory of a thread block");
+static_assert(pa_tmem_used(64) <= kPaTmemCols && pa_tmem_used(96) <= kPaTmemCols && pa_tmem_used(128) <= kPaTmemCols, "tensor memory");
+static_assert(pa_stages(128) * kPaStageBytes >= 128 * kHeadDim * 4, "the accumulator fits into the ring");
 
 struct PackedAttnParams {
     const uint8_t *q, *packed, *local;
     const int32_t *slot_tbl, *blk_tbl, *seq_len;
     uint8_t *out;
     float *lse;
-    float *part_o;      // [items][rows per group][128] fp32, normalised (runs through the workspace only)
-    float *part_lse;    // [items][rows per group]      log2 domain
+    float *part_o;      // [items][rows][128] fp32, normalised (runs through the workspace only)
+    float *part_lse;    // [items][rows]      log2 domain
     int32_t *err;
     float scale_log2;   // of bf16 keys; of unpacked ones: times 2^kDequantShift
-    int T, Hq, Hkv, G, n_cols, local_col, R, n_splits, tiles_per_split, n_groups, group_rows;
+    int T, Hq, Hkv, G, n_cols, local_col, R, n_splits, tiles_per_split;
     Bounds bd;
 };
 
@@ -98,23 +96,10 @@ __device__ __forceinline__ uint32_t pa_idesc(int n, bool b_mn_major)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-// P: rows = tokens of 2 N bytes, swizzled over as many bytes (16 rows: 32, 32 rows: 64, 64 rows: 128), groups of eight tokens.
-template <int N>
-__device__ __forceinline__ uint64_t pa_p_desc(uint32_t addr)
+// P: rows = tokens of 128 bytes (64 columns), 128-byte swizzle, groups of eight tokens; the next 64 columns 128 rows further.
+__device__ __forceinline__ uint32_t pa_p_chunk(int token, int c)         // byte offset of columns 8 c .. 8 c + 7 of a token
 {
-    uint64_t d = 0;
-    d |= (uint64_t)((addr & 0x3ffffu) >> 4);
-    d |= (uint64_t)1 << 16;                                              // (one atom holds all columns)
-    d |= (uint64_t)((16 * N) >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)(N == 64 ? 2 : N == 32 ? 4 : 6) << 61;
-    return d;
-}
-template <int N>
-__device__ __forceinline__ uint32_t pa_p_chunk(int token, int c)         // byte offset of columns 8 c .. 8 c + 7 of a token's row
-{
-    const int x = N == 64 ? token & 7 : N == 32 ? (token >> 1) & 3 : (token >> 2) & 1;
-    return (uint32_t)(token * 2 * N + ((c ^ x) << 4));
+    return (uint32_t)((c >> 3) * (kPaTileKeys * 128) + token * 128 + (((c ^ token) & 7) << 4));
 }
 
 // Named barrier 1 over the softmax threads, returning the OR of their predicates; and the plain barrier 2.
@@ -140,7 +125,7 @@ __device__ __forceinline__ void pa_sync()
 // sums (l_sm) become outputs, or the split's part of them.  `warps` warps take a row each; in a cluster, block `split` takes rows split,
 // split + n_splits, .. of all its blocks.  Called by the whole thread block.
 template <bool CLUSTER, int PITCH>
-__device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive, int warp, int warps, int lane, int split, int rows, int row0, int b, int h,
+__device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive, int warp, int warps, int lane, int split, int rows, int b, int h,
                                           const float *o_sm, const float *neg_m, const float *l_sm)
 {
     if constexpr (CLUSTER) {
@@ -191,12 +176,12 @@ __device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive,
             }
             const float lse2 = den > 0.f ? top + log2f(den) : den == 0.f ? -CUDART_INF_F : den;
             if (CLUSTER || p.n_splits == 1) {
-                const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+                const int tq = r / p.G, a = h * p.G + r % p.G;
                 const long long o = ((long long)b * p.T + tq) * p.Hq + a;
                 reinterpret_cast<uint2 *>(p.out + o * kRowBytes)[lane] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
                 if (p.lse && lane == 0) p.lse[o] = lse2 * kAtLn2;
             } else {
-                const long long o = (long long)blockIdx.x * p.group_rows + r;
+                const long long o = (long long)blockIdx.x * p.R + r;
                 reinterpret_cast<float4 *>(p.part_o + o * kHeadDim)[lane] = acc;
                 if (lane == 0) p.part_lse[o] = lse2;
             }
@@ -211,18 +196,18 @@ __device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive,
 
 // N: columns of the products (query rows, padded).
 template <int N, bool CLUSTER>
-__global__ void __launch_bounds__(pa_threads(N), pa_blocks(N))
+__global__ void __launch_bounds__(pa_threads(N), 1)
 packed_attn_kernel(const PackedAttnParams p)
 {
     constexpr int STAGES = pa_stages(N), KB = pa_k_bufs(N), VB = pa_v_bufs(N), THREADS = pa_threads(N);
-    constexpr int NC = N <= 32 ? N : 32;                    // softmax columns of a thread
+    constexpr int NC = 32;                                  // softmax columns of a thread
     constexpr int SOFT = pa_soft(N);                        // softmax threads
     constexpr int SOFT0 = 8, MMA = SOFT0 + SOFT / 32, COPY = MMA + 1;      // first softmax warp, the others
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     uint8_t *const p_ptr = base_ptr + N * kRowBytes;
-    uint8_t *const ring = p_ptr + kPaTileKeys * 2 * N;
+    uint8_t *const ring = p_ptr + pa_p_bytes(N);
     int2 *const list = reinterpret_cast<int2 *>(ring + STAGES * kPaStageBytes);           // (block, slot)
     float *const neg_m = reinterpret_cast<float *>(list + kPaListCols);                     // [N] minus the rows' reference maxima
     float *const l_sm = neg_m + N;                                                          // [N]; while a maximum is raised: factors
@@ -242,14 +227,11 @@ packed_attn_kernel(const PackedAttnParams p)
     auto par_2 = [&](int i) { return (uint32_t)((i >> 1) & 1); };
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int grp = CLUSTER ? (blockIdx.x / p.n_splits) % p.n_groups : blockIdx.x % p.n_groups;
-    const int split = CLUSTER ? blockIdx.x % p.n_splits : (blockIdx.x / p.n_groups) % p.n_splits;
-    const int bh = blockIdx.x / (p.n_groups * p.n_splits);
-    const int b = bh / p.Hkv, h = bh % p.Hkv;
-    const int row0 = grp * p.group_rows, rows = min(p.group_rows, p.R - row0);
+    const int split = blockIdx.x % p.n_splits, bh = blockIdx.x / p.n_splits;
+    const int b = bh / p.Hkv, h = bh % p.Hkv, rows = p.R;
     if (warp == MMA) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)pa_tmem_cols(N)) : "memory");
+                     ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)kPaTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (tid == 0) {
@@ -290,7 +272,7 @@ packed_attn_kernel(const PackedAttnParams p)
         const int r = i >> 4, c = i & 15;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (r < rows) {
-            const int tq = (row0 + r) / p.G, a = h * p.G + (row0 + r) % p.G;
+            const int tq = r / p.G, a = h * p.G + r % p.G;
             v = *reinterpret_cast<const uint4 *>(p.q + (((long long)b * p.T + tq) * p.Hq + a) * kRowBytes + c * 16);
         }
         *reinterpret_cast<uint4 *>(base_ptr + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
@@ -352,14 +334,14 @@ packed_attn_kernel(const PackedAttnParams p)
             for (int k = max(0, pi - STAGES); k < pi; ++k) mbar_wait_warp(bar_full(k % STAGES), (k / STAGES) & 1, p.err, 82);
     } else if (warp == MMA) {
         // ---------------------------------------------------------------- products (the whole warp, converged)
-        const uint64_t q_desc = smem_desc_sw128(base), p_desc = pa_p_desc<N>(base + N * kRowBytes);
+        const uint64_t q_desc = smem_desc_sw128(base), p_desc = smem_desc_sw128_mn(base + N * kRowBytes, kPaTileKeys * 128, 1024);
         auto values = [&](int i) {
             alive = alive && mbar_wait_warp(bar_v(i), par_v(i), p.err, 84) && mbar_wait_warp(bar_p, i & 1, p.err, 85);
             if (!alive) return;
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < kPaTileCols; ++k)
-                tc_mma_bf16_ts(t_o, t_v(i) + 8 * k, p_desc + (uint64_t)((k * 32 * N) >> 4), pa_idesc(N, true), (i > 0 || k) ? 1u : 0u);
+                tc_mma_bf16_ts(t_o, t_v(i) + 8 * k, p_desc + (uint64_t)((k * 2048) >> 4), pa_idesc(N, true), (i > 0 || k) ? 1u : 0u);
             tc_commit(bar_o(i));
         };
 #pragma unroll 1
@@ -481,14 +463,14 @@ packed_attn_kernel(const PackedAttnParams p)
                 const int at = (i - do_local) * kPaTileCols + kb;
                 const int blk = loc ? s_local[kb].x : at < count ? list[at].x : -1;
                 const long long ahead = (long long)blk * kBlock + tok - L;
-                n_min = (blk < 0 || ahead >= p.T ? N : ahead <= 0 ? 0 : min(max((int)ahead * p.G - row0, 0), N)) - n0;
+                n_min = (blk < 0 || ahead >= p.T ? N : ahead <= 0 ? 0 : min((int)ahead * p.G, N)) - n0;
                 masked = __any_sync(0xffffffffu, n_min > 0);
             }
             const float scale = loc ? p.scale_log2 : p.scale_log2 * (float)(1 << kDequantShift);
             const uint32_t t_mine = t_s + (i & 1) * N + n0 + lane_base;
             alive = alive && mbar_wait_warp(bar_s(i), par_2(i), p.err, 90);
             tc_fence_after();
-            // sixteen columns at a time, as (logit - reference) in log2 units (32: read a second time for the weights)
+            // sixteen columns at a time, as (logit - reference) in log2 units; read a second time for the weights
             float x[16];
             const uint64_t scale2 = f32x2(scale, scale);
             auto read = [&](int c) {
@@ -559,15 +541,11 @@ packed_attn_kernel(const PackedAttnParams p)
                     }
                     tc_wait_st();
                 }
-                if (NC == 16) {
-                    read(0);
-                    relative(0);
-                }
             }
 #pragma unroll
             for (int c = 0; c < NC / 16; ++c) {
-                if (NC > 16) read(c);
-                if (NC > 16) relative(c);
+                read(c);
+                relative(c);
 #pragma unroll
                 for (int n = 0; n < 16; ++n) x[n] = fast_exp2(x[n]);
                 if (masked) {
@@ -583,7 +561,7 @@ packed_attn_kernel(const PackedAttnParams p)
                 }
 #pragma unroll
                 for (int k = 0; k < 16; k += 8)
-                    *reinterpret_cast<uint4 *>(p_ptr + pa_p_chunk<N>(me, (n0 + c * 16 + k) / 8)) =
+                    *reinterpret_cast<uint4 *>(p_ptr + pa_p_chunk(me, (n0 + c * 16 + k) / 8)) =
                         make_uint4(pack_bf16x2(x[k], x[k + 1]), pack_bf16x2(x[k + 2], x[k + 3]), pack_bf16x2(x[k + 4], x[k + 5]), pack_bf16x2(x[k + 6], x[k + 7]));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -603,37 +581,30 @@ packed_attn_kernel(const PackedAttnParams p)
                 for (int e = 0; e < 16; ++e) o_sm[(n0 + c * 16 + e) * kHeadDim + me] = __uint_as_float(v[e]) * (float)(1 << kDequantShift);
             }
         }
-        // the threads' sums of a row: half of the values change hands in every round, so that lane k ends with row k (or k / 2)
+        // the threads' sums of a row: half of the values change hands in every round, so that lane k ends with row k
         float l[NC];
 #pragma unroll
         for (int n = 0; n < NC / 2; ++n) f32x2_split(l2[n], l[2 * n], l[2 * n + 1]);
-        int w = NC / 2;
 #pragma unroll
-        for (int bit = 16; bit >= 1; bit >>= 1) {
-            const bool up = lane & bit;
-            if (w >= 1) {
+        for (int w = NC / 2; w >= 1; w >>= 1) {                          // (lane bit w picks the half)
+            const bool up = lane & w;
 #pragma unroll
-                for (int k = 0; k < NC / 2; ++k)
-                    if (k < w) {
-                        const float give = up ? l[k] : l[k + w], keep = up ? l[k + w] : l[k];
-                        l[k] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
-                    }
-                w >>= 1;
-            } else {
-                l[0] += __shfl_xor_sync(0xffffffffu, l[0], bit);
-            }
+            for (int k = 0; k < NC / 2; ++k)
+                if (k < w) {
+                    const float give = up ? l[k] : l[k + w], keep = up ? l[k + w] : l[k];
+                    l[k] = keep + __shfl_xor_sync(0xffffffffu, give, w);
+                }
         }
-        if (NC == 32) l_part[(warp & 3) * N + n0 + lane] = l[0];
-        else if (!(lane & 1)) l_part[(warp & 3) * N + (lane >> 1)] = l[0];
+        l_part[(warp & 3) * N + n0 + lane] = l[0];
     }
     alive = __syncthreads_and(alive);
     if (tid < N) l_sm[tid] = n_tiles > 0 ? l_part[tid] + l_part[N + tid] + l_part[2 * N + tid] + l_part[3 * N + tid] : 0.f;
-    pa_finish<CLUSTER, kHeadDim>(p, alive, warp, MMA, lane, split, rows, row0, b, h, o_sm, neg_m, l_sm);
+    pa_finish<CLUSTER, kHeadDim>(p, alive, warp, MMA, lane, split, rows, b, h, o_sm, neg_m, l_sm);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == MMA)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)pa_tmem_cols(N)) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kPaTmemCols) : "memory");
 }
 
 // ---- up to 32 query rows: every warp by itself ----------------------------------------------------------------------------
@@ -647,6 +618,7 @@ packed_attn_kernel(const PackedAttnParams p)
 // so that the weights, transposed 8 x 8 (one instruction), are in the order of the words: tokens 2 j and 2 j + 1 of word t.
 // NT: products of 8 query rows.
 constexpr int kPfThreads = 128, kPfWarps = 4;
+constexpr int kPfListCols = 768;                                         // columns of a split at most
 constexpr int kPfUnitBytes = 2 * kPackedBytes;
 constexpr int kPfPitch = kHeadDim + 4;
 __host__ __device__ constexpr int pf_blocks(int nt) { return nt == 1 ? 4 : nt == 2 ? 3 : 2; }       // thread blocks per SM
@@ -654,7 +626,7 @@ __host__ __device__ constexpr int pf_stages(int nt) { return nt == 1 ? 2 : nt ==
 // Shared memory: Q fragments | rings | column list | statistics and barriers.
 __host__ __device__ constexpr int pf_smem(int nt)
 {
-    return 128 + nt * 2048 + kPfWarps * pf_stages(nt) * kPfUnitBytes + kPaListCols * 8 + 1536;
+    return 128 + nt * 2048 + kPfWarps * pf_stages(nt) * kPfUnitBytes + kPfListCols * 8 + 1536;
 }
 static_assert((pf_smem(1) + 1024) * pf_blocks(1) <= 233472 && (pf_smem(2) + 1024) * pf_blocks(2) <= 233472 && (pf_smem(3) + 1024) * pf_blocks(3) <= 233472 &&
               (pf_smem(4) + 1024) * pf_blocks(4) <= 233472, "thread blocks per SM");
@@ -683,17 +655,15 @@ packed_attn_few_kernel(const PackedAttnParams p)
     uint4 *const q_frag = reinterpret_cast<uint4 *>(base_ptr);                              // [NT][4 pairs of steps][32 lanes]
     uint8_t *const rings = base_ptr + NT * 2048;
     int2 *const list = reinterpret_cast<int2 *>(rings + kPfWarps * STAGES * kPfUnitBytes);   // (block, slot)
-    float *const neg_m = reinterpret_cast<float *>(list + kPaListCols);                       // [warps][ROWS], then [ROWS] of the block
+    float *const neg_m = reinterpret_cast<float *>(list + kPfListCols);                       // [warps][ROWS], then [ROWS] of the block
     float *const l_sm = neg_m + kPfWarps * ROWS;
     uint64_t *const bars = reinterpret_cast<uint64_t *>(l_sm + kPfWarps * ROWS);              // [warps][STAGES]
     int2 *const s_local = reinterpret_cast<int2 *>(bars + kPfWarps * STAGES);                 // [8]
     int *const s_cnt = reinterpret_cast<int *>(s_local + kPaTileCols);                        // [columns / 32]
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int split = blockIdx.x % p.n_splits;
-    const int bh = blockIdx.x / p.n_splits;
-    const int b = bh / p.Hkv, h = bh % p.Hkv;
-    const int rows = p.R;
+    const int split = blockIdx.x % p.n_splits, bh = blockIdx.x / p.n_splits;
+    const int b = bh / p.Hkv, h = bh % p.Hkv, rows = p.R;
     const uint32_t bar0 = smem_u32(bars + warp * STAGES);
     uint8_t *const ring = rings + warp * STAGES * kPfUnitBytes;
     if (lane == 0) {
@@ -705,7 +675,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- the split's columns, as in packed_attn_kernel -----------------------------------------------------------
-    constexpr int PER = kPaListCols / kPfThreads;
+    constexpr int PER = kPfListCols / kPfThreads;
     const int has_local = p.n_cols > p.local_col;
     const int t0 = split * p.tiles_per_split, t1 = t0 + p.tiles_per_split;
     const int c0 = max(t0 - has_local, 0) * kPaTileCols, c1 = min((t1 - has_local) * kPaTileCols, p.local_col);
@@ -789,7 +759,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const long long ahead = (long long)blk * kBlock + ktok + 2 * j - L;
-                const int n_min = blk < 0 || ahead >= p.T ? ROWS : ahead <= 0 ? 0 : (int)min(ahead * p.G, (long long)ROWS);
+                const int n_min = blk < 0 || ahead >= p.T ? ROWS : ahead <= 0 ? 0 : min((int)ahead * p.G, ROWS);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -1015,7 +985,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
             l_sm[r] = den;
         }
     }
-    pa_finish<CLUSTER, kPfPitch>(p, alive, warp, kPfWarps, lane, split, rows, 0, b, h, o_sm, neg_m, l_sm);
+    pa_finish<CLUSTER, kPfPitch>(p, alive, warp, kPfWarps, lane, split, rows, b, h, o_sm, neg_m, l_sm);
 }
 
 // Merges the splits of one query row: out = sum_s w_s o_s / sum_s w_s with w_s = 2^(lse_s - max lse).  One warp per row, four output
@@ -1030,9 +1000,7 @@ packed_combine_kernel(const PackedAttnParams p, int total)
     const int row = wi % p.R, bh = wi / p.R;
     const int b = bh / p.Hkv, h = bh % p.Hkv;
     const int tq = row / p.G, a = h * p.G + row % p.G;
-    const int grp = row / p.group_rows, r = row % p.group_rows;
-    const long long prow0 = ((long long)bh * p.n_splits * p.n_groups + grp) * p.group_rows + r;     // partial row of split 0
-    const long long pstride = (long long)p.n_groups * p.group_rows;
+    const long long prow0 = (long long)bh * p.n_splits * p.R + row, pstride = p.R;      // partial row of split 0, from split to split
     float mx = -CUDART_INF_F;
     for (int s = lane; s < p.n_splits; s += 32) mx = fmaxf(mx, p.part_lse[prow0 + s * pstride]);
 #pragma unroll
@@ -1069,7 +1037,7 @@ packed_combine_kernel(const PackedAttnParams p, int total)
 
 // ---- host side -----------------------------------------------------------------------------------------
 struct PackedPlan {
-    int n_groups, group_rows, n, n_splits, tiles_per_split;
+    int rows, n, n_splits, tiles_per_split;         // query rows per KV head; columns of the products
     bool in_cluster;
     long long items;
     size_t workspace;
@@ -1079,24 +1047,47 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
 {
     PackedPlan pl;
     const int R = T * (dims->n_q_heads / dims->n_kv_heads);
-    pl.n_groups = (R + 63) / 64;
-    pl.group_rows = (R + pl.n_groups - 1) / pl.n_groups;
-    pl.n = pl.group_rows <= 32 ? (pl.group_rows + 7) / 8 * 8 : 64;
-    const int blocks = pl.n == 64 ? pa_blocks(64) : pf_blocks(pl.n / 8);
-    const long long items = (long long)dims->batch * dims->n_kv_heads * pl.n_groups;
+    pl.rows = R;
+    pl.n = R <= 32 ? (R + 7) / 8 * 8 : R <= 64 ? 64 : R <= 96 ? 96 : 128;
+    const bool few = pl.n <= 32;
+    const long long items = (long long)dims->batch * dims->n_kv_heads;
     const int tiles = (local_col + kPaTileCols - 1) / kPaTileCols + (n_cols > local_col ? 1 : 0);
-    // all thread blocks resident at once as far as the tiles can be split
-    long long s = items > 0 ? (long long)sm_count() * blocks / items : 1;
-    if (s > tiles) s = tiles;
-    if (s < 1) s = 1;
-    const int most = kPaListCols / kPaTileCols;                          // tiles whose columns a thread block can list
-    if ((tiles + s - 1) / s > most) s = (tiles + most - 1) / most;
-    pl.in_cluster = s <= kPaMaxCluster;
+    const int most = (few ? kPfListCols : kPaListCols) / kPaTileCols;    // tiles whose columns a thread block can list
+    const int least = (tiles + most - 1) / most, blocks = few ? pf_blocks(pl.n / 8) : 1, sms = sm_count();
+    // The number of splits with the smallest estimate, in the time that a thread block alone on an SM takes for a tile: 3 for its
+    // first loads and its end, then its tiles, slower by 0.7 for every thread block beyond the first that shares the SM; a wave of them
+    // after the other; 0.5 for a merge in a cluster, 2.5 through the workspace.  Candidates: what a cluster holds, and what fills the
+    // SMs with one, two, .. thread blocks.  Measured against it, in a graph, one token, 32 query and 8 KV heads (splits: us):
+    //   16 requests x 130 columns  1: 20.7  2: 17.3  3: 18.9  4: 17.3  6: 22.9      40 requests  1: 40.8  2: 39.3  3: 35.7  4: 44.1
+    //    1 request  x 130 columns  4: 9.0  6: 7.3  8: 7.3  18: 8.3         2 x 4,098 columns  8: 85.9  18: 45.7  27: 42.7  37: 44.6
+    const float share = few ? 0.7f : 1.f;
+    long long best = 0;
+    float best_cost = 0.f;
+    auto consider = [&](long long s) {
+        s = s > tiles ? tiles : s;
+        s = s < least ? least : s;
+        s = s < 1 ? 1 : s;
+        const long long per = (tiles + s - 1) / s;
+        if (per > 0) s = (tiles + per - 1) / per;                        // (no split without a tile)
+        const long long on_sm = (items * s + sms - 1) / sms, waves = (on_sm + blocks - 1) / blocks, rest = on_sm - (waves - 1) * blocks;
+        auto wave = [&](long long n) { return 3.f + (float)per * (share * (float)n > 1.f ? share * (float)n : 1.f); };
+        const float cost = (float)(waves - 1) * wave(blocks) + wave(rest) + (s == 1 ? 0.f : s <= kPaMaxCluster ? 0.5f : 2.5f);
+        if (best == 0 || cost < best_cost) {
+            best = s;
+            best_cost = cost;
+        }
+    };
+    if (items > 0) {
+        for (int s = 1; s <= kPaMaxCluster; ++s)
+            if (few || s == 1 || clusters_at_once(s) >= items) consider(s);      // (one thread block per SM: all clusters at once)
+        for (int k = 1; k <= blocks; ++k) consider((long long)sms * k / items);
+    }
+    const long long s = best > 0 ? best : 1;
     pl.tiles_per_split = (int)((tiles + s - 1) / s);
-    pl.n_splits = (tiles + pl.tiles_per_split - 1) / pl.tiles_per_split;
-    if (pl.n_splits == 1) pl.in_cluster = false;
+    pl.n_splits = pl.tiles_per_split > 0 ? (tiles + pl.tiles_per_split - 1) / pl.tiles_per_split : 1;
+    pl.in_cluster = pl.n_splits > 1 && pl.n_splits <= kPaMaxCluster && (few || clusters_at_once(pl.n_splits) >= items);
     pl.items = items * pl.n_splits;
-    pl.workspace = pl.n_splits > 1 && !pl.in_cluster ? (size_t)pl.items * pl.group_rows * (kHeadDim + 1) * sizeof(float) : 0;
+    pl.workspace = pl.n_splits > 1 && !pl.in_cluster ? (size_t)pl.items * pl.rows * (kHeadDim + 1) * sizeof(float) : 0;
     return pl;
 }
 
@@ -1143,18 +1134,18 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
         if (!aligned16(workspace)) return fail(OASIS_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
     }
     const long long total = (long long)dims->batch * dims->n_q_heads * n_q_tokens;
-    if (pl.items * pl.group_rows > 0x7fffffffLL || total > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: grid too large", who);
+    if (pl.items * pl.rows > 0x7fffffffLL || total > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: grid too large", who);
 
     PackedAttnParams p = {};
     p.q = (const uint8_t *)q; p.packed = (const uint8_t *)packed_pool; p.local = (const uint8_t *)hbm_pool;
     p.slot_tbl = slot_tbl; p.blk_tbl = blk_tbl; p.seq_len = seq_len; p.out = (uint8_t *)out; p.lse = lse; p.err = error_word();
     p.scale_log2 = scale * kAtLog2e;
     p.T = n_q_tokens; p.Hq = dims->n_q_heads; p.Hkv = dims->n_kv_heads; p.G = p.Hq / p.Hkv; p.n_cols = n_cols; p.local_col = local_col;
-    p.R = p.T * p.G; p.n_splits = pl.n_splits; p.tiles_per_split = pl.tiles_per_split; p.n_groups = pl.n_groups; p.group_rows = pl.group_rows;
+    p.R = p.T * p.G; p.n_splits = pl.n_splits; p.tiles_per_split = pl.tiles_per_split;
     p.bd = bounds();
     if (pl.workspace > 0) {
         p.part_o = (float *)workspace;
-        p.part_lse = p.part_o + (size_t)pl.items * pl.group_rows * kHeadDim;
+        p.part_lse = p.part_o + (size_t)pl.items * pl.rows * kHeadDim;
     }
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1186,7 +1177,9 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
     else if (pl.n == 16) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 2, kPfThreads, pf_smem(2));
     else if (pl.n == 24) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 3, kPfThreads, pf_smem(3));
     else if (pl.n == 32) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 4, kPfThreads, pf_smem(4));
-    else OASIS_PACKED_LAUNCH(packed_attn_kernel, 64, pa_threads(64), pa_smem(64));
+    else if (pl.n == 64) OASIS_PACKED_LAUNCH(packed_attn_kernel, 64, pa_threads(64), pa_smem(64));
+    else if (pl.n == 96) OASIS_PACKED_LAUNCH(packed_attn_kernel, 96, pa_threads(96), pa_smem(96));
+    else OASIS_PACKED_LAUNCH(packed_attn_kernel, 128, pa_threads(128), pa_smem(128));
 #undef OASIS_PACKED_LAUNCH
 #undef OASIS_PACKED_LAUNCH_AS
     if (e != cudaSuccess) {
