@@ -1059,6 +1059,7 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
     // after the other; 0.5 for a merge in a cluster, 2.5 through the workspace.  Candidates: what a cluster holds, and what fills the
     // SMs with one, two, .. thread blocks.  Measured against it, in a graph, one token, 32 query and 8 KV heads (splits: us):
     //   16 requests x 130 columns  1: 20.7  2: 17.3  3: 18.9  4: 17.3  6: 22.9      40 requests  1: 40.8  2: 39.3  3: 35.7  4: 44.1
+    // 16 requests x 130 columns, 4 tokens (three thread blocks per SM)  1: 25.9  2: 26.1  3: 20.9  4: 33.1
     //    1 request  x 130 columns  4: 9.0  6: 7.3  8: 7.3  18: 8.3         2 x 4,098 columns  8: 85.9  18: 45.7  27: 42.7  37: 44.6
     const float share = few ? 0.7f : 1.f;
     long long best = 0;
@@ -1069,7 +1070,9 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
         s = s < 1 ? 1 : s;
         const long long per = (tiles + s - 1) / s;
         if (per > 0) s = (tiles + per - 1) / per;                        // (no split without a tile)
-        const long long on_sm = (items * s + sms - 1) / sms, waves = (on_sm + blocks - 1) / blocks, rest = on_sm - (waves - 1) * blocks;
+        const long long on_sm = (items * s + sms - 1) / sms, waves = (on_sm + blocks - 1) / blocks;
+        long long rest = on_sm - (waves - 1) * blocks;
+        if (blocks % 2 && rest < blocks && s > 1 && s % 2 == 0) ++rest;      // (three places per SM: pairs of a cluster fill them unevenly)
         auto wave = [&](long long n) { return 3.f + (float)per * (share * (float)n > 1.f ? share * (float)n : 1.f); };
         const float cost = (float)(waves - 1) * wave(blocks) + wave(rest) + (s == 1 ? 0.f : s <= kPaMaxCluster ? 0.5f : 2.5f);
         if (best == 0 || cost < best_cost) {

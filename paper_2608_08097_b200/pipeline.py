@@ -19,14 +19,23 @@ class DecodeLayer:
 
     Fetch-all layout: row (b, h) owns the k + 2 consecutive pool slots
     (b * Hkv + h) * (k + 2) + c, column c holding the block sel[b][h][c].
+
+    kv_bits=4: the first k columns of a row are packed entries, slots (b * Hkv + h) * k + c of `pool` (uint8 [...][2304]); the
+    last two, the local window, stay bf16 entries of `local`, slot (2 b + r) * Hkv + h for column k + r.
     """
 
     def __init__(self, batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, device="cuda",
-                 want_lse=False, out=None, tree=False):
+                 want_lse=False, out=None, tree=False, kv_bits=16):
         self.B, self.Hq, self.Hkv, self.mb = batch, n_q_heads, n_kv_heads, max_blocks
         self.k, self.T = k, n_q_tokens
         self.cols = k + 2
         self.tree = bool(tree)
+        if kv_bits not in (4, 16):
+            raise ValueError("kv_bits must be 16 or 4")
+        self.packed = kv_bits == 4
+        if self.packed and self.tree:
+            raise ValueError("draft trees go with a bf16 working set")
+        self.slot_stride = k if self.packed else self.cols
         self.dims = oasis.Dims(batch, n_q_heads, n_kv_heads, max_blocks)
         self.device = torch.device(device)
         dev = self.device
@@ -36,16 +45,33 @@ class DecodeLayer:
         self.sel = torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int32, device=dev)
         self.stage_idx = torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int64, device=dev)
         self.stage_slots = torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int32, device=dev)
-        self.pool = torch.zeros((rows * self.cols, 2, 16, 128), dtype=torch.bfloat16, device=dev)
-        self.slot_tbl = torch.arange(rows * self.cols, dtype=torch.int32, device=dev).view(batch, n_kv_heads, self.cols)
+        if self.packed:
+            self.pool = torch.zeros((rows * k, oasis.PACKED_BYTES), dtype=torch.uint8, device=dev)
+            self.local = torch.zeros((rows * 2, 2, 16, 128), dtype=torch.bfloat16, device=dev)
+            near = torch.arange(rows * 2, dtype=torch.int32, device=dev).view(batch, 2, n_kv_heads).transpose(1, 2)
+            self.slot_tbl = torch.cat([torch.arange(rows * k, dtype=torch.int32, device=dev).view(batch, n_kv_heads, k), near], 2).contiguous()
+        else:
+            self.pool = torch.zeros((rows * self.cols, 2, 16, 128), dtype=torch.bfloat16, device=dev)
+            self.slot_tbl = torch.arange(rows * self.cols, dtype=torch.int32, device=dev).view(batch, n_kv_heads, self.cols)
         self.out = torch.empty((batch, n_q_tokens, n_q_heads, 128), dtype=torch.bfloat16, device=dev) if out is None else out
         self.lse = torch.empty((batch, n_q_tokens, n_q_heads), dtype=torch.float32, device=dev) if want_lse else None
-        ws = (oasis.tree_attn_workspace_bytes if tree else oasis.attn_workspace_bytes)(self.dims, n_q_tokens, self.cols)
+        if self.packed:
+            ws = oasis.packed_attn_workspace_bytes(self.dims, n_q_tokens, self.cols, k)
+        else:
+            ws = (oasis.tree_attn_workspace_bytes if tree else oasis.attn_workspace_bytes)(self.dims, n_q_tokens, self.cols)
+        self.splits = ws > 0                             # the attention has a second launch, which merges split rows
         self.workspace = torch.empty((max(ws, 16),), dtype=torch.uint8, device=dev)
         self.scale = 1.0 / math.sqrt(128.0)
         if self.tree:
             self.all_nodes = torch.full((batch,), n_q_tokens, dtype=torch.int32, device=dev)
             self.n_cand = torch.zeros((batch,), dtype=torch.int32, device=dev)     # blocks that the latest selection was made among
+
+    # in front of the step: a projection's rows become the step's queries and its new keys and values
+    def rotate(self, qkv, table, q, kv, seq_len, stream=None, parent=None, n_nodes=None):
+        """qkv [B][T][(Hq + 2 Hkv) * 128] -> q [B][T][Hq][128] and kv [B][T][Hkv][2][128] (`step`'s new_kv), rotated with the
+        frequencies of `table` (a rotary.RotaryTable) at positions seq_len[b] + t, or, with parent and n_nodes, seq_len[b] + the
+        depth of node t."""
+        oasis.rotate_qkv(self.dims, qkv, table, q, kv, seq_len=seq_len, parent=parent, n_nodes=n_nodes, stream=stream)
 
     # step 0
     def build_summaries(self, kv_pool, block_table, first_block, n_blocks, max_new_blocks, stream=None):
@@ -83,6 +109,11 @@ class DecodeLayer:
 
     # step 4
     def attend(self, q, seq_len, blk_tbl=None, slot_tbl=None, stream=None):
+        if self.packed:
+            oasis.packed_attn(self.dims, q, self.pool, self.local, self.slot_tbl if slot_tbl is None else slot_tbl,
+                              self.sel if blk_tbl is None else blk_tbl, self.k, seq_len, self.scale, self.out, lse=self.lse,
+                              workspace=self.workspace, stream=stream)
+            return self.out
         oasis.sparse_attn(self.dims, q, self.T, self.pool, self.slot_tbl if slot_tbl is None else slot_tbl,
                           self.sel if blk_tbl is None else blk_tbl, self.cols, seq_len, self.scale,
                           self.out, lse=self.lse, workspace=self.workspace, stream=stream)
@@ -134,6 +165,9 @@ class DecodeEngine:
     layers are then issued at the start of the step on the prediction stream.
     tree (append engines): the drafts of a step form trees (`step(..., tree=(parent, n_nodes))`); the nodes' keys and values stay
     in the caller's tree buffer, and `commit` writes the kept path's after the step.  Steps are captured one per graph.
+    kv_bits=4 (append engines): the full-KV pool and the working set hold packed entries of 2,304 bytes, the local window stays
+    bf16.  A block is packed, and summarised from its bf16 keys, in the step that fills it (`oasis_pack_local_layers`); the pool is
+    filled by `handover`, which also loads the partially filled block.  Attention (`oasis_packed_attn`) and scoring are two launches.
     transfer_streams: consecutive layers' gathers alternate between this many transfer streams (useful
     when the pool is in host memory: one gather's requests are in flight while the previous one's last
     ones come back).
@@ -152,13 +186,18 @@ class DecodeEngine:
     def __init__(self, batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, n_layers,
                  device="cuda", mode="fetch_all", cap=None, fused=None, transfer_streams=1, wait_group=8,
                  append=False, transfer_group=1, plan_stream="own", n_commit=1, transfer_ctas=0, transfer_kind="warp",
-                 tree=False):
+                 tree=False, kv_bits=16):
         assert mode in ("fetch_all", "delta")
         assert not append or mode == "delta", "the KV append goes with delta selection"
         if tree and not (append and n_q_tokens >= 2):
             raise ValueError("draft trees need the KV append (delta mode) and room for two nodes or more")
         if tree and fused:
             raise ValueError("the fused launch takes chains of drafts")
+        if kv_bits not in (4, 16):
+            raise ValueError("kv_bits must be 16 or 4")
+        self.packed = kv_bits == 4
+        if self.packed and (not append or tree or fused or transfer_kind != "warp"):
+            raise ValueError("kv_bits=4 goes with the KV append (delta mode) and chains of drafts, unfused, with transfer_kind 'warp'")
         self.tree = bool(tree)
         self.append = bool(append)
         self.transfer_ctas = int(transfer_ctas)  # thread blocks per gather launch (0: the library's default)
@@ -171,7 +210,7 @@ class DecodeEngine:
         # the layers' outputs are slices of one tensor, so that several layers' outputs can leave in one copy
         self.out_all = torch.empty((n_layers, batch, n_q_tokens, n_q_heads, 128), dtype=torch.bfloat16, device=self.device)
         self.layers = [DecodeLayer(batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, device, out=self.out_all[l],
-                                   tree=self.tree)
+                                   tree=self.tree, kv_bits=kv_bits)
                        for l in range(n_layers)]
         self.kv = [None] * n_layers
         self.table = [None] * n_layers
@@ -193,7 +232,7 @@ class DecodeEngine:
         self.cap = cap
         self.wait_group = max(1, int(wait_group))
         self.transfer_group = max(1, min(int(transfer_group), oasis.MAX_STAGE_LAYERS))
-        can_fuse = not self.tree and n_layers > 0 and n_q_tokens > 1 and oasis.attn_and_score_supported(self.layers[0].dims, n_q_tokens, self.layers[0].cols, n_q_tokens - 1)
+        can_fuse = not self.tree and not self.packed and n_layers > 0 and n_q_tokens > 1 and oasis.attn_and_score_supported(self.layers[0].dims, n_q_tokens, self.layers[0].cols, n_q_tokens - 1)
         self.fused = can_fuse if fused is None else (bool(fused) and can_fuse)
         self._reset_events()
         if mode == "delta":
@@ -204,8 +243,10 @@ class DecodeEngine:
             n_req = cap + (0 if append else 2)       # requests per row: the admitted pairs (and the local blocks)
             self.plan_idx = [torch.empty(rows + (n_req,), dtype=torch.int64, device=dev) for _ in range(n_layers)]
             self.plan_slots = [torch.empty(rows + (n_req,), dtype=torch.int32, device=dev) for _ in range(n_layers)]
-        ws_bytes = oasis.tree_attn_workspace_bytes if self.tree else oasis.attn_workspace_bytes
-        self._splits = ws_bytes(self.layers[0].dims, n_q_tokens, k + 2) > 0 if n_layers else False
+        self._splits = self.layers[0].splits if n_layers else False
+        if self.packed:      # the local windows as pages 2 b + (block & 1) of a full-KV pool, for the hand-over of the last block
+            parity = torch.arange(max_blocks, dtype=torch.int32, device=self.device) % 2
+            self.local_table = (2 * torch.arange(batch, dtype=torch.int32, device=self.device)[:, None] + parity).contiguous()
 
     def _reset_events(self):
         """Forgets the previous step's events (everything before has completed)."""
@@ -218,7 +259,7 @@ class DecodeEngine:
         self.commit_done = None              # trees: the latest commit (summaries read what it wrote to the full-KV pool)
 
     def attach(self, layer, kv_src, block_table):
-        """kv_src: the layer's full-KV pool (pinned host memory, or device memory)."""
+        """kv_src: the layer's full-KV pool (pinned host memory, or device memory); packed entries with kv_bits=4."""
         self.kv[layer], self.table[layer] = kv_src, block_table
 
     def blk_tbl(self, layer):
@@ -257,7 +298,8 @@ class DecodeEngine:
                 # the scores buffer is rewritten: the previous step's top-k of this layer must have read it
                 if self.sel_done[l] is not None:
                     ps.wait_event(self.sel_done[l])
-                L.build_summaries(self.kv[l], self.table[l], first_block, n_new, max_new)
+                if not self.packed:                # (packed: summarised when it was packed)
+                    L.build_summaries(self.kv[l], self.table[l], first_block, n_new, max_new)
                 t0 = self._tick(timers, "score", ps)
                 L.score(q, n_full_next, n_nodes=n_nodes)
                 self._tock(timers, "score", t0, ps)
@@ -274,7 +316,7 @@ class DecodeEngine:
             self._tock(timers, "select", t0, qs)
             if sel_log is not None:
                 sel_log.copy_(L.sel, non_blocking=True)  # a record of this step's selection (tests, analysis)
-            self.launches += 3 if own_score else 1      # (summary update, scoring,) top-k
+            self.launches += (2 if self.packed else 3) if own_score else 1      # (summary update, scoring,) top-k
             ev = self._event(qs)
             self.sel_done[l] = ev
         if self.mode == "delta":
@@ -285,7 +327,7 @@ class DecodeEngine:
                 plan_idx = self.plan_idx[l] if plan is None else plan[0]
                 plan_slots = self.plan_slots[l] if plan is None else plan[1]
                 oasis.plan_delta(L.dims, L.sel, self.k, self.table[l], self.resident[l], self.stamp[l],
-                                 L.cols, plan_idx.shape[-1] - n_local, stamp, plan_idx, plan_slots, n_local=n_local,
+                                 L.slot_stride, plan_idx.shape[-1] - n_local, stamp, plan_idx, plan_slots, n_local=n_local,
                                  n_res=self.k)
                 self.launches += 1
                 ev = self._event(self.planq)
@@ -304,7 +346,10 @@ class DecodeEngine:
             else:
                 idx = [self.layers[l].stage_idx for l in ls]
                 slots = [self.layers[l].stage_slots for l in ls]
-            if self.transfer_kind == "bulk":
+            if self.packed:
+                oasis.stage_packed_layers([self.kv[l] for l in ls], idx, slots, idx[0].numel(), [self.layers[l].pool for l in ls],
+                                          max_ctas=self.transfer_ctas)
+            elif self.transfer_kind == "bulk":
                 oasis.stage_blocks_bulk([self.kv[l] for l in ls], idx, slots, idx[0].numel(),
                                         [self.layers[l].pool for l in ls], max_streams=self.transfer_ctas)
             elif len(ls) == 1 and self.transfer_ctas == 0:
@@ -329,17 +374,25 @@ class DecodeEngine:
             n_full = (seq_len // 16).to(torch.int32)
             n_part = ((seq_len + 15) // 16).to(torch.int32) - n_full
             zeros = torch.zeros_like(n_full)
-            oasis.offload_blocks(L.dims, dense_k, dense_v, gpu_table, self.table[layer], zeros, n_full, L.mb,
-                                 self.kv[layer], L.summaries)
-            oasis.offload_blocks(L.dims, dense_k, dense_v, gpu_table, self.table[layer], n_full, n_part, 1,
-                                 self.kv[layer], None)
+            if self.packed:          # whole blocks in 4 bits; the last one, still growing, into the local window
+                oasis.offload_blocks_packed(L.dims, dense_k, dense_v, gpu_table, self.table[layer], zeros, n_full, L.mb,
+                                            self.kv[layer], L.summaries)
+                oasis.offload_blocks(L.dims, dense_k, dense_v, gpu_table, self.local_table, n_full, n_part, 1, L.local, None)
+            else:
+                oasis.offload_blocks(L.dims, dense_k, dense_v, gpu_table, self.table[layer], zeros, n_full, L.mb,
+                                     self.kv[layer], L.summaries)
+                oasis.offload_blocks(L.dims, dense_k, dense_v, gpu_table, self.table[layer], n_full, n_part, 1,
+                                     self.kv[layer], None)
         self.launches += 2
 
     def prime(self, q_list, n_full_next, seq_next, step_stamp=0, summaries_ready=False, n_nodes=None):
         """Before the first step: build every summary (unless the hand-over already did) and run one
         prediction + transfer per layer, as the step before the first one would have done.  With the KV
         append the (partially filled) local block is loaded from the full-KV pool into the local window
-        once, here.  n_nodes (engines built with tree=True): the rows of q_list that are nodes, as in `step`; None: all."""
+        once, here.  n_nodes (engines built with tree=True): the rows of q_list that are nodes, as in `step`; None: all.
+        Engines with kv_bits=4 are primed after `handover`, with summaries_ready=True."""
+        if self.packed and not summaries_ready:
+            raise ValueError("kv_bits=4: the hand-over packs and summarises the blocks; prime with summaries_ready=True")
         B = self.layers[0].B
         zeros = torch.zeros(B, dtype=torch.int32, device=self.device)
         n_build = zeros if summaries_ready else n_full_next
@@ -360,9 +413,13 @@ class DecodeEngine:
                     self.side.wait_event(self.stage_done[l])
                     idx = torch.empty((B, L.Hkv, 2), dtype=torch.int64, device=self.device)
                     slots = torch.empty((B, L.Hkv, 2), dtype=torch.int32, device=self.device)
-                    oasis.local_window(L.dims, seq_next, 1 if self.tree else self.T, self.table[l], self.resident[l], self.k, L.cols, idx, slots)
-                    oasis.stage_blocks(self.kv[l], idx, slots, idx.numel(), L.pool)
-                    self.launches += 2
+                    if self.packed:                    # (its contents came with the hand-over)
+                        oasis.local_window(L.dims, seq_next, self.T, self.table[l], self.resident[l], self.k)
+                        self.launches += 1
+                    else:
+                        oasis.local_window(L.dims, seq_next, 1 if self.tree else self.T, self.table[l], self.resident[l], self.k, L.cols, idx, slots)
+                        oasis.stage_blocks(self.kv[l], idx, slots, idx.numel(), L.pool)
+                        self.launches += 2
             if plan is not None:
                 for st in self.xfer:     # the shared priming plan is reused by the next layer
                     st.synchronize()
@@ -424,9 +481,17 @@ class DecodeEngine:
                             self.pred.wait_event(self.attn_done[l1 - 1])
                         for a0 in range(l0, l1, oasis.MAX_APPEND_LAYERS):
                             a1 = min(a0 + oasis.MAX_APPEND_LAYERS, l1)
-                            oasis.append_kv_layers(self.layers[a0].dims, new_kv[a0:a1], self.n_commit, seq_len, self.table[a0:a1],
-                                                   [L.slot_tbl for L in self.layers[a0:a1]], self.resident[a0:a1], self.k,
-                                                   [L.pool for L in self.layers[a0:a1]], self.kv[a0:a1])
+                            group = self.layers[a0:a1]
+                            slot_tbls = [L.slot_tbl for L in group]
+                            if self.packed:
+                                oasis.append_kv_layers(group[0].dims, new_kv[a0:a1], 0, seq_len, self.table[a0:a1], slot_tbls,
+                                                       self.resident[a0:a1], self.k, [L.local for L in group], [None] * len(group))
+                                oasis.pack_local_layers(group[0].dims, [L.local for L in group], slot_tbls, self.k, first_block, n_new, 1,
+                                                        self.kv[a0:a1], self.table[a0:a1], [L.summaries for L in group])
+                                self.launches += 2
+                                continue
+                            oasis.append_kv_layers(group[0].dims, new_kv[a0:a1], self.n_commit, seq_len, self.table[a0:a1],
+                                                   slot_tbls, self.resident[a0:a1], self.k, [L.pool for L in group], self.kv[a0:a1])
                             self.launches += 1
                     if self.fused:
                         for a0 in range(l0, l1, oasis.MAX_LAYERS):
