@@ -1,13 +1,15 @@
 // Blocks of the KV cache in 4 bits: packing (from entries of a pool, from the local window, from a dense pool's separate key and
 // value blocks) and unpacking.  The format and its arithmetic are in packed.cuh.
 //
-// Packing: one warp per (request, block, KV head).  Sixteen 16-byte loads per lane bring the 8 KiB of keys and values, each
-// warp-wide load two 256-byte token rows: a lane holds the same eight dims of eight tokens, even ones in lanes 0..15 and odd ones
-// in lanes 16..31.  The largest magnitude of a key's group (16 dims of a token) is one exchange with the neighbouring lane away, of
-// a value's group (16 tokens of a dim) seven maxima and one exchange with the other half-warp.  The lane's eight codes of a key
-// are one word.  The entry is put together in shared memory and leaves in 16-byte stores, whole lines, because its place is
-// usually in pinned host memory.  The block's summaries (minimum and maximum of the keys) come from the same registers.
-// Algorithmic traffic: 8,192 B read, 2,304 B (and 512 B of summaries) written per (block, head).
+// Packing: one warp per (request, block, KV head).  Sixteen 16-byte loads per lane bring the 8 KiB of keys and values: a lane holds
+// the same eight dims of eight tokens, 0 .. 7 in lanes 0 .. 15 and 8 .. 15 in lanes 16 .. 31, so that its eight codes of a key are
+// one word, and so are its eight codes of a dim's values.  The largest magnitude of a key's group (16 dims of a token) is one
+// exchange with the neighbouring lane away, of a value's group (16 tokens of a dim) seven maxima and one exchange with the other
+// half-warp.  Divisions are table look-ups by shuffle, a value is rounded by one fused multiply-add, and four codes come together
+// in three integer ones (packed.cuh).  What does not fit into the scales (NaN, infinity, magnitudes above 26,880) is found in the
+// groups' maxima and replaced before.  The entry is put together in shared memory and leaves in 16-byte stores, whole lines,
+// because its place is usually in pinned host memory.  The block's summaries (minimum and maximum of the keys) come from the same
+// registers.  Algorithmic traffic: 8,192 B read, 2,304 B (and 512 B of summaries) written per (block, head).
 #include "packed.cuh"
 
 namespace oasis {
@@ -28,19 +30,30 @@ __device__ __forceinline__ uint32_t bf2_max(uint32_t a, uint32_t b)
 }
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-// NaN counts as zero.
-__device__ __forceinline__ uint32_t without_nan(uint32_t v)
+// NaN counts as zero, what is above the largest value that a scale reaches as that.
+__device__ __forceinline__ uint32_t packable(uint32_t v)
 {
-    const uint32_t lo = (v & 0x7fffu) > 0x7f80u ? 0u : v & 0xffffu, hi = (v & 0x7fff0000u) > 0x7f800000u ? 0u : v & 0xffff0000u;
-    return lo | hi;
+    uint32_t r = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t x = (v >> (16 * e)) & 0xffffu, mag = x & 0x7fffu;
+        r |= (mag > 0x7f80u ? 0u : mag > kPackLargest ? (x & 0x8000u) | kPackLargest : x) << (16 * e);
+    }
+    return r;
 }
-__device__ __forceinline__ bool has_nan(uint32_t v) { return (v & 0x7fffu) > 0x7f80u || (v & 0x7fff0000u) > 0x7f800000u; }
+// Larger of the two halves' magnitudes (bf16 patterns without sign compare like whole numbers; NaN is the largest).
+__device__ __forceinline__ uint32_t bf2_abs_max(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a & 0x7fff7fffu), "r"(b & 0x7fff7fffu));
+    return r;
+}
 
-// keys (k) and values (v) of one block and head, lane -> 16-byte chunk (lane & 15) of token (lane >> 4) + 2 i; `sm`: 2,304 bytes
+// keys (k) and values (v) of one block and head, lane -> 16-byte chunk (lane & 15) of token 8 (lane >> 4) + i; `sm`: 2,304 bytes
 // of this warp, 16-byte aligned; `dst`: the packed entry; `summary` (or NULL): its 512 bytes.
 __device__ __forceinline__ void pack_entry(uint32_t (&k)[8][4], uint32_t (&v)[8][4], uint8_t *sm, uint8_t *dst, uint8_t *summary)
 {
-    const int lane = threadIdx.x & 31, odd = lane >> 4, chunk = lane & 15;
+    const int lane = threadIdx.x & 31, upper = lane >> 4, chunk = lane & 15;
     if (summary) {
         uint32_t lo[4], hi[4];
 #pragma unroll
@@ -55,59 +68,73 @@ __device__ __forceinline__ void pack_entry(uint32_t (&k)[8][4], uint32_t (&v)[8]
             hi[p] = bf2_max(hi[p], __shfl_xor_sync(0xffffffffu, hi[p], 16));
         }
         *reinterpret_cast<uint4 *>(summary + lane * 16) =
-            odd ? make_uint4(hi[0], hi[1], hi[2], hi[3]) : make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            upper ? make_uint4(hi[0], hi[1], hi[2], hi[3]) : make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
-    bool nan = false;
+    uint32_t ka[8], va[8];                                           // the groups' largest magnitudes: of key i, of dim 8 chunk + i
+    auto maxima = [&]() {
+        uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i) {
+            uint32_t a2 = bf2_abs_max(bf2_abs_max(k[i][0], k[i][1]), bf2_abs_max(k[i][2], k[i][3]));
+            a2 = bf2_abs_max(a2, __shfl_xor_sync(0xffffffffu, a2, 1));
+            ka[i] = max(a2 & 0xffffu, a2 >> 16);
+            most = max(most, ka[i]);
+        }
 #pragma unroll
-        for (int p = 0; p < 4; ++p) nan |= has_nan(k[i][p]) | has_nan(v[i][p]);
-    if (__any_sync(0xffffffffu, nan)) {
+        for (int p = 0; p < 4; ++p) {
+            uint32_t a2 = v[0][p] & 0x7fff7fffu;
+#pragma unroll
+            for (int i = 1; i < 8; ++i) a2 = bf2_abs_max(a2, v[i][p]);
+            a2 = bf2_abs_max(a2, __shfl_xor_sync(0xffffffffu, a2, 16));
+            va[2 * p] = a2 & 0xffffu;
+            va[2 * p + 1] = a2 >> 16;
+            most = max(most, max(va[2 * p], va[2 * p + 1]));
+        }
+        return most;
+    };
+    if (__any_sync(0xffffffffu, maxima() > kPackLargest)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                k[i][p] = without_nan(k[i][p]);
-                v[i][p] = without_nan(v[i][p]);
+                k[i][p] = packable(k[i][p]);
+                v[i][p] = packable(v[i][p]);
             }
+        maxima();
     }
+    const uint32_t steps = scale_table();
+    const float inverses = inverse_table();
     // keys: two lanes per group
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        uint32_t a2 = bf2_max(bf2_max(k[i][0] & 0x7fff7fffu, k[i][1] & 0x7fff7fffu), bf2_max(k[i][2] & 0x7fff7fffu, k[i][3] & 0x7fff7fffu));
-        a2 = bf2_max(a2, __shfl_xor_sync(0xffffffffu, a2, 1));
-        const int byte = scale_byte(fmaxf(bf_lo(a2), bf_hi(a2)));
-        const float inv = scale_inverse(byte);
-        uint32_t w = 0;
+        const int byte = scale_byte(ka[i], steps), token = 8 * upper + i;
+        const float inv = scale_inverse(byte, inverses);
+        uint32_t c[8];
 #pragma unroll
-        for (int p = 0; p < 4; ++p) w |= (code_bits(bf_lo(k[i][p]), inv) | code_bits(bf_hi(k[i][p]), inv) << 16) << (4 * p);
-        const int token = odd + 2 * i;
-        *reinterpret_cast<uint32_t *>(sm + (chunk >> 2) * 256 + token * 16 + (chunk & 3) * 4) = w;
+        for (int p = 0; p < 4; ++p) {
+            c[2 * p] = code_bits(bf_lo(k[i][p]), inv);
+            c[2 * p + 1] = code_bits(bf_hi(k[i][p]), inv);
+        }
+        *reinterpret_cast<uint32_t *>(sm + (chunk >> 2) * 256 + token * 16 + (chunk & 3) * 4) =
+            __byte_perm(code_half(c[0], c[2], c[4], c[6]), code_half(c[1], c[3], c[5], c[7]), 0x5410);
         if (!(lane & 1)) sm[kPackedKScale + token * 8 + (chunk >> 1)] = (uint8_t)byte;
     }
-    // values: the lane's eight dims, its tokens in the low (even) or high (odd) halves of the words
+    // values: the lane's eight dims, its eight tokens
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        uint32_t a2 = v[0][p] & 0x7fff7fffu;
+    for (int d = 0; d < 8; ++d) {
+        const int byte = scale_byte(va[d], steps), dim = chunk * 8 + d;
+        const float inv = scale_inverse(byte, inverses);
+        uint32_t c[8];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) a2 = bf2_max(a2, v[i][p] & 0x7fff7fffu);
-        a2 = bf2_max(a2, __shfl_xor_sync(0xffffffffu, a2, 16));
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int dim = chunk * 8 + 2 * p + e;
-            const int byte = scale_byte(e ? bf_hi(a2) : bf_lo(a2));
-            const float inv = scale_inverse(byte);
-            uint32_t half[2] = {0, 0};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) half[i >> 2] |= code_bits(e ? bf_hi(v[i][p]) : bf_lo(v[i][p]), inv) << (4 * (i & 3));
-#pragma unroll
-            for (int w = 0; w < 2; ++w) *reinterpret_cast<uint16_t *>(sm + kPackedV + dim * 8 + w * 4 + odd * 2) = (uint16_t)half[w];
-            if (!odd) sm[kPackedVScale + dim] = (uint8_t)byte;
-        }
+        for (int i = 0; i < 8; ++i) c[i] = code_bits(d & 1 ? bf_hi(v[i][d >> 1]) : bf_lo(v[i][d >> 1]), inv);
+        *reinterpret_cast<uint32_t *>(sm + kPackedV + dim * 8 + upper * 4) =
+            __byte_perm(code_half(c[0], c[2], c[4], c[6]), code_half(c[1], c[3], c[5], c[7]), 0x5410);
+        if (!upper) sm[kPackedVScale + dim] = (uint8_t)byte;
     }
     __syncwarp();
 #pragma unroll
-    for (int i = lane; i < kPackedBytes / 16; i += 32) *reinterpret_cast<uint4 *>(dst + i * 16) = *reinterpret_cast<const uint4 *>(sm + i * 16);
+    for (int i = 0; i < 5; ++i)
+        if (lane + 32 * i < kPackedBytes / 16) *reinterpret_cast<uint4 *>(dst + (lane + 32 * i) * 16) = *reinterpret_cast<const uint4 *>(sm + (lane + 32 * i) * 16);
 }
 
 struct PackLayers {
@@ -132,8 +159,9 @@ pack_blocks_kernel(const __grid_constant__ PackLayers ly, const int32_t *__restr
     const int h = (int)(item % Hkv);
     const int jj = (int)((item / Hkv) % max_new);
     const int b = (int)(item / ((long long)Hkv * max_new));
-    if (jj >= n_blocks[b]) return;
-    const long long j = (long long)first_block[b] + jj;
+    const int n = n_blocks[b];
+    const long long j = (long long)first_block[b] + jj;              // (both on their way at once)
+    if (jj >= n) return;
     if (j < 0 || j >= max_blocks) {
         in_range(j, max_blocks, bd, kErrBlockCount);       // (checked build: reported; always skipped)
         return;
@@ -147,16 +175,17 @@ pack_blocks_kernel(const __grid_constant__ PackLayers ly, const int32_t *__restr
     }
     const long long dst = (long long)ly.block_table[l][(long long)b * max_blocks + j] * Hkv + h;
     if (!in_range(dst, bd.n_entries, bd, kErrHostEntry)) return;
-    const uint8_t *ksrc = ly.k_src[l] + src * src_bytes + lane * 16, *vsrc = ly.v_src[l] + src * src_bytes + lane * 16;
+    const int at = (lane >> 4) * 8 * kRowBytes + (lane & 15) * 16;
+    const uint8_t *ksrc = ly.k_src[l] + src * src_bytes + at, *vsrc = ly.v_src[l] + src * src_bytes + at;
     uint32_t k[8][4], v[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint4 w = ld_stream_v4(ksrc + i * 512);
+        const uint4 w = ld_stream_v4(ksrc + i * kRowBytes);
         k[i][0] = w.x; k[i][1] = w.y; k[i][2] = w.z; k[i][3] = w.w;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint4 w = ld_stream_v4(vsrc + i * 512);
+        const uint4 w = ld_stream_v4(vsrc + i * kRowBytes);
         v[i][0] = w.x; v[i][1] = w.y; v[i][2] = w.z; v[i][3] = w.w;
     }
     pack_entry(k, v, sm[threadIdx.x >> 5], ly.packed[l] + dst * kPackedBytes,
@@ -168,7 +197,7 @@ __global__ void __launch_bounds__(kPackWarps * 32)
 unpack_blocks_kernel(const uint8_t *__restrict__ packed, const long long *__restrict__ idx, int n, uint8_t *__restrict__ out, const Bounds bd)
 {
     __shared__ __align__(16) uint8_t sm_all[kPackWarps][kPackedBytes];
-    const int lane = threadIdx.x & 31, odd = lane >> 4, chunk = lane & 15;
+    const int lane = threadIdx.x & 31, upper = lane >> 4, chunk = lane & 15;
     const long long item = (long long)blockIdx.x * kPackWarps + (threadIdx.x >> 5);
     if (item >= n) return;
     const long long src = idx[item];
@@ -179,42 +208,39 @@ unpack_blocks_kernel(const uint8_t *__restrict__ packed, const long long *__rest
     for (int i = 0; i < 5; ++i)
         if (lane + 32 * i < kPackedBytes / 16) *reinterpret_cast<uint4 *>(sm + (lane + 32 * i) * 16) = ld_stream_v4(from + (lane + 32 * i) * 16);
     __syncwarp();
-    uint8_t *dst = out + item * kEntryBytes + lane * 16;
+    uint8_t *dst = out + item * kEntryBytes + upper * 8 * kRowBytes + chunk * 16;
+    const uint32_t unit = 0x00010001u * ((127u + kDequantShift) << 7);          // (x, x) for 2^kDequantShift
+    auto words = [&](uint32_t w, int byte, uint32_t (&o)[4]) {
+        dequant_word(w, dequant_scale((uint32_t)byte * 0x00010001u), o);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) o[p] = fma_bf16x2(o[p], unit, 0x80008000u);     // (-0 leaves a zero's sign as it is)
+    };
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int token = odd + 2 * i;
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(sm + (chunk >> 2) * 256 + token * 16 + (chunk & 3) * 4);
-        const float sc = scale_value(sm[kPackedKScale + token * 8 + (chunk >> 1)]);
+        const int token = 8 * upper + i;
         uint32_t o[4];
-#pragma unroll
-        for (int p = 0; p < 4; ++p)
-            o[p] = pack_bf16x2((float)((int)((w >> (4 * p)) & 15u) - 8) * sc, (float)((int)((w >> (16 + 4 * p)) & 15u) - 8) * sc);
-        *reinterpret_cast<uint4 *>(dst + i * 512) = make_uint4(o[0], o[1], o[2], o[3]);
+        words(*reinterpret_cast<const uint32_t *>(sm + (chunk >> 2) * 256 + token * 16 + (chunk & 3) * 4), sm[kPackedKScale + token * 8 + (chunk >> 1)], o);
+        *reinterpret_cast<uint4 *>(dst + i * kRowBytes) = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    // values: this lane's dims, both words of each; token 2 i + odd of word i >> 2 is in place i & 3 of its half of the word
-    uint32_t vals[8][4];                                             // [i][pair of dims]
+    // values: this lane's dims, eight tokens of each; then two dims of a token side by side
+    uint32_t vals[8][4];                                             // [token][pair of dims]
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        float s[2];
-        uint32_t w[2][2];
+        uint32_t o[2][4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int dim = chunk * 8 + 2 * p + e;
-            s[e] = scale_value(sm[kPackedVScale + dim]);
-            const uint2 both = *reinterpret_cast<const uint2 *>(sm + kPackedV + dim * 8);
-            w[e][0] = both.x >> (16 * odd);
-            w[e][1] = both.y >> (16 * odd);
+            words(*reinterpret_cast<const uint32_t *>(sm + kPackedV + dim * 8 + upper * 4), sm[kPackedVScale + dim], o[e]);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float lo = (float)((int)((w[0][i >> 2] >> (4 * (i & 3))) & 15u) - 8) * s[0];
-            const float hi = (float)((int)((w[1][i >> 2] >> (4 * (i & 3))) & 15u) - 8) * s[1];
-            vals[i][p] = pack_bf16x2(lo, hi);
+        for (int i = 0; i < 4; ++i) {
+            vals[2 * i][p] = __byte_perm(o[0][i], o[1][i], 0x5410);
+            vals[2 * i + 1][p] = __byte_perm(o[0][i], o[1][i], 0x7632);
         }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        *reinterpret_cast<uint4 *>(dst + kPartBytes + i * 512) = make_uint4(vals[i][0], vals[i][1], vals[i][2], vals[i][3]);
+        *reinterpret_cast<uint4 *>(dst + kPartBytes + i * kRowBytes) = make_uint4(vals[i][0], vals[i][1], vals[i][2], vals[i][3]);
 }
 
 // The checks and the launch that the three packing entry points share.

@@ -21,23 +21,46 @@ constexpr int kPackedBytes = OASIS_PACKED_BYTES;
 constexpr int kPackedV = 1024, kPackedKScale = 2048, kPackedVScale = 2176;
 constexpr int kScaleBias = 20;
 
-// The scale byte of a group whose largest magnitude is `amax` (not NaN): amax / 7, to four significant bits, ties to even.
-// (amax has 8 bits: where the exact quotient is a tie the rounded one is too, elsewhere it is 2^-9 away from one.)
-__device__ __forceinline__ int scale_byte(float amax)
+// The scale byte of a group whose largest magnitude has the bf16 pattern `amax` (at most kPackLargest): amax / 7 to four significant
+// bits, ties to even.  With amax = (128 + M) 2^(E - 134) that is 8 (E - 110) + scale_step(M): M's 128 values are a table that the warp
+// holds in a register, four bytes a lane.
+constexpr uint32_t kPackLargest = 0x46d2;              // 26880 = 7 * 3840, the largest value that the largest scale reaches
+template <uint32_t UNIT>
+__host__ __device__ constexpr uint32_t nearest_even(uint32_t x)        // x / UNIT, ties to even
 {
-    const uint32_t u = __float_as_uint(__fdiv_rn(amax, 7.0f));
-    const int byte = (int)((u + 0x7ffffu + ((u >> 20) & 1u)) >> 20) - ((127 - kScaleBias) << 3);
-    return min(max(byte, 0), 255);
+    return x / UNIT + (2 * (x % UNIT) > UNIT || (2 * (x % UNIT) == UNIT && x / UNIT % 2 == 1) ? 1 : 0);
+}
+__host__ __device__ constexpr uint32_t scale_step(uint32_t m)
+{
+    // (128 + M) / 7 lies in [16, 37): 8 .. 16 units of 2 below 32, 8 or 9 of 4 from there on
+    return m < 96 ? nearest_even<14>(128 + m) - 8 : nearest_even<28>(128 + m);
+}
+static_assert(scale_step(0) == 1 && scale_step(133 - 128) == 2 && scale_step(147 - 128) == 2 && scale_step(96) == 8 && scale_step(238 - 128) == 8, "scale steps");
+__device__ __forceinline__ uint32_t scale_table()      // of this lane
+{
+    const uint32_t m = 4 * (threadIdx.x & 31);
+    return scale_step(m) | scale_step(m + 1) << 8 | scale_step(m + 2) << 16 | scale_step(m + 3) << 24;
+}
+__device__ __forceinline__ int scale_byte(uint32_t amax, uint32_t table)               // by the whole warp
+{
+    const uint32_t m = amax & 127u, four = __shfl_sync(0xffffffffu, table, m >> 2);
+    const int byte = 8 * ((int)(amax >> 7) - 110) + (int)((four >> (8 * (m & 3))) & 255u);
+    return max(byte, 0);
 }
 __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float(((uint32_t)byte << 20) + ((127u - kScaleBias) << 23)); }
-// What `code_bits` multiplies by: 1 / s, a little less.  Products are then below the exact quotient by 2^-21 to 2^-19 of it, so that
+// What a value is multiplied by: 1 / s, 2^-20 of it less.  Products are then below the exact quotient by 2^-21 to 2^-19 of it, so that
 // a value halfway between two multiples of s goes to the smaller one; any other quotient is 2^-9 of itself from a halfway point.
-__device__ __forceinline__ float scale_inverse(int byte) { return __fdiv_rn(1.0f - 0x1p-20f, scale_value(byte)); }
-// c = 8 + the nearest whole number to x / s within +-7, in the low bits (x is not NaN).
-__device__ __forceinline__ uint32_t code_bits(float x, float inv)
+// `table`: lane m < 8 holds that of (8 + m) / 8.
+__device__ __forceinline__ float inverse_table() { return __fdiv_rn(8.0f * (1.0f - 0x1p-20f), (float)(8 + (threadIdx.x & 7))); }
+__device__ __forceinline__ float scale_inverse(int byte, float table)                  // by the whole warp
 {
-    return __float_as_uint(fminf(fmaxf(x * inv, -7.0f), 7.0f) + 12582920.0f) & 15u;
+    return __uint_as_float(__float_as_uint(__shfl_sync(0xffffffffu, table, byte & 7)) + (uint32_t)(kScaleBias - (byte >> 3)) * (1u << 23));
 }
+// The pattern of the float 12582912 + c, c = 8 + the nearest whole number to x / s (one rounding, of the exact x * inv + 12582920);
+// |x| is at most kPackLargest or 7 17/16 s, so c is 1 .. 15.  The patterns' upper 16 bits vanish from sums of 16^k times them.
+__device__ __forceinline__ uint32_t code_bits(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582920.0f)); }
+// Four codes in the lower 16 bits.
+__device__ __forceinline__ uint32_t code_half(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3) { return c0 + 16u * c1 + 256u * c2 + 4096u * c3; }
 
 // Eight codes of a word as four bf16 pairs (c - 8) * s * 2^-kDequantShift.  A whole number n < 256 in the low bits of a bf16 is
 // n * 2^-133 (subnormal up to 127, and the first binade has the same spacing): so a nibble in bits 0 .. 3 needs no more than a mask

@@ -6,8 +6,9 @@
 // values are copied.  Angles: the position times the frequency in turns (frequency / 2 pi), in 64 bits, of which only the fraction
 // of a turn is kept, exactly, before anything is rounded to fp32: a position of a million loses nothing.
 // A thread block takes one or a few tokens: its threads work out their cosines and sines once, into shared memory, and then a
-// half-warp moves a head's row at a time, 8 dims a lane.  With halves the partner's dims come from another lane of the half-warp
-// (or, where the half is no multiple of 8, one by one from the cache).  Every element is read once and written once.
+// half-warp moves a head's row at a time, 8 dims a lane; the first rows are on their way before the angles.  With halves the partner's
+// dims come from another lane of the half-warp, or, where the half is no multiple of 8, through shared memory (a row of fp32, a word
+// of padding after every eight).  Every element is read once and written once.
 // In a draft tree a token's position is seq_len + its depth, which one warp finds by pointer doubling over the parents.
 #include "common.cuh"
 
@@ -28,13 +29,6 @@ struct RotateParams {
     float factor;
 };
 
-template <int TYPE>
-__device__ __forceinline__ float element(const uint8_t *p, long long i)
-{
-    if (TYPE == OASIS_F32) return reinterpret_cast<const float *>(p)[i];
-    if (TYPE == OASIS_BF16) return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(p)[i] << 16);
-    return __half2float(reinterpret_cast<const __half *>(p)[i]);
-}
 // 8 elements in W 32-bit registers as floats.
 template <int TYPE, int W>
 __device__ __forceinline__ void to_floats(const uint32_t (&w)[W], float (&x)[8])
@@ -67,14 +61,34 @@ rotate_qkv_kernel(const RotateParams p)
     constexpr int SIZE = TYPE == OASIS_F32 ? 4 : 2, W = 2 * SIZE;        // registers of 8 elements
     __shared__ __align__(16) float2 turn[kRotMaxTokens][kHeadDim / 2];   // (cos, sin) times the factor
     __shared__ int s_depth[kRotMaxTokens];
+    __shared__ float s_row[MODE == kOddHalves ? kRotWorkers : 1][kRotLanes * 9];
     const int tid = threadIdx.x, lane = tid & 31;
-    const long long n0 = (long long)blockIdx.x * p.tokens_per_block;
-    const int here = (int)min((long long)p.tokens_per_block, p.n_tokens - n0);
+    const uint32_t n0 = blockIdx.x * (uint32_t)p.tokens_per_block, T = (uint32_t)p.T;     // (at most 2^31 tokens)
+    const int here = (int)min((uint32_t)p.tokens_per_block, (uint32_t)p.n_tokens - n0);
+    const int worker = tid / kRotLanes, chunk = tid % kRotLanes, d0 = chunk * 8;
+    const int n_rot = p.Hq + p.Hkv, n_rows = p.Hq + 2 * p.Hkv;
+    uint32_t w[kRotAhead][W];
+    auto load = [&](int k, int a0) {                                     // rows a0, a0 + kRotWorkers, .. of token n0 + k
+        const uint32_t n = n0 + k;
+        const uint8_t *src = p.qkv + ((long long)(n / T) * p.batch_stride + (long long)(n % T) * p.token_stride + d0) * SIZE;
+#pragma unroll
+        for (int u = 0; u < kRotAhead; ++u) {
+            const int a = a0 + u * kRotWorkers;
+            if (a < n_rows) {
+#pragma unroll
+                for (int v = 0; v < W / 4; ++v) {
+                    const uint4 g = ld_stream_v4(src + (long long)a * kHeadDim * SIZE + v * 16);
+                    w[u][4 * v] = g.x; w[u][4 * v + 1] = g.y; w[u][4 * v + 2] = g.z; w[u][4 * v + 3] = g.w;
+                }
+            }
+        }
+    };
+    load(0, worker);
     if (p.parent) {
         // how many ancestors: every node's parent in place of itself, six doublings; a warp per token
         for (int k = tid >> 5; k < here; k += kRotThreads / 32) {
-            const long long n = n0 + k;
-            const int b = (int)(n / p.T), t = (int)(n % p.T);
+            const uint32_t n = n0 + k;
+            const int b = (int)(n / T), t = (int)(n % T);
             int up[2], depth[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -105,8 +119,8 @@ rotate_qkv_kernel(const RotateParams p)
     const int half = p.rot / 2;
     for (int i = tid; i < here * half; i += kRotThreads) {
         const int k = i / half, f = i % half;
-        const long long n = n0 + k;
-        const int b = (int)(n / p.T), t = (int)(n % p.T);
+        const uint32_t n = n0 + k;
+        const int b = (int)(n / T), t = (int)(n % T);
         const double pos = p.positions ? (double)p.positions[n] : (double)p.seq_len[b] + (p.parent ? s_depth[k] : t);
         const double turns = pos * (p.freqs[f] * 0.15915494309189533577);            // 1 / (2 pi)
         float s, c;
@@ -115,15 +129,12 @@ rotate_qkv_kernel(const RotateParams p)
     }
     __syncthreads();
 
-    const int worker = tid / kRotLanes, chunk = tid % kRotLanes, d0 = chunk * 8;
-    const int n_rot = p.Hq + p.Hkv, n_rows = p.Hq + 2 * p.Hkv;
     const bool turned = d0 < p.rot;                                      // some of this lane's dims are rotated
     const unsigned team = 0xffffu << (lane & 16);                        // the half-warp
     for (int k = 0; k < here; ++k) {
-        const long long n = n0 + k;
-        const int b = (int)(n / p.T), t = (int)(n % p.T);
+        const uint32_t n = n0 + k;
+        const int b = (int)(n / T), t = (int)(n % T);
         if (p.n_nodes && t >= p.n_nodes[b]) continue;                    // padding: left as it was
-        const uint8_t *src = p.qkv + ((long long)b * p.batch_stride + (long long)t * p.token_stride) * SIZE;
         float2 cs[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -131,18 +142,7 @@ rotate_qkv_kernel(const RotateParams p)
             cs[e] = d < p.rot ? turn[k][f] : make_float2(1.f, 0.f);
         }
         for (int a0 = worker; a0 < n_rows; a0 += kRotWorkers * kRotAhead) {
-            uint32_t w[kRotAhead][W];
-#pragma unroll
-            for (int u = 0; u < kRotAhead; ++u) {
-                const int a = a0 + u * kRotWorkers;
-                if (a < n_rows) {
-#pragma unroll
-                    for (int v = 0; v < W / 4; ++v) {
-                        const uint4 g = ld_stream_v4(src + ((long long)a * kHeadDim + d0) * SIZE + v * 16);
-                        w[u][4 * v] = g.x; w[u][4 * v + 1] = g.y; w[u][4 * v + 2] = g.z; w[u][4 * v + 3] = g.w;
-                    }
-                }
-            }
+            if (k > 0 || a0 > worker) load(k, a0);
 #pragma unroll
             for (int u = 0; u < kRotAhead; ++u) {
                 const int a = a0 + u * kRotWorkers;
@@ -167,12 +167,17 @@ rotate_qkv_kernel(const RotateParams p)
 #pragma unroll
                             for (int v = 0; v < W; ++v) o[v] = __shfl_sync(team, w[u][v], turned ? (chunk < step ? chunk + step : chunk - step) : chunk, 16);
                             to_floats<TYPE, W>(o, y);
-                        } else if (turned) {
+                        } else {
+                            float *const row = s_row[worker];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) row[chunk * 9 + e] = x[e];
+                            __syncwarp(team);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
-                                const int d = d0 + e;
-                                y[e] = d < p.rot ? element<TYPE>(src, (long long)a * kHeadDim + (d < half ? d + half : d - half)) : 0.f;
+                                const int d = d0 + e, mate = d < half ? d + half : d < p.rot ? d - half : d;
+                                y[e] = row[mate + (mate >> 3)];
                             }
+                            __syncwarp(team);
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
@@ -183,9 +188,9 @@ rotate_qkv_kernel(const RotateParams p)
                     }
                 }
                 uint8_t *dst;
-                if (a < p.Hq) dst = p.q + (n * p.Hq + a) * kRowBytes;
-                else if (a < n_rot) dst = p.kv + ((n * p.Hkv + a - p.Hq) * 2) * kRowBytes;
-                else dst = p.kv + ((n * p.Hkv + a - n_rot) * 2 + 1) * kRowBytes;
+                if (a < p.Hq) dst = p.q + ((long long)n * p.Hq + a) * kRowBytes;
+                else if (a < n_rot) dst = p.kv + (((long long)n * p.Hkv + a - p.Hq) * 2) * kRowBytes;
+                else dst = p.kv + (((long long)n * p.Hkv + a - n_rot) * 2 + 1) * kRowBytes;
                 uint4 o = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
                 if (TYPE == OASIS_BF16 && (a >= n_rot || d0 >= p.rot)) o = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);   // (copied bit by bit)
                 *reinterpret_cast<uint4 *>(dst + d0 * 2) = o;

@@ -418,3 +418,18 @@ def test_refusals(L):
         L.stage_packed_layers([e], [n.long()], [n], 2, [e])
     with pytest.raises(ValueError):
         L.pack_local_layers(d, [kv], [], 0, n, n, 1, [e], [t])
+
+
+def test_the_bounds_check_build_flags_and_skips(L):
+    import json
+    import os
+    import subprocess
+    import sys
+
+    from paper_2608_08097_b200 import build
+    env = dict(os.environ, OASIS_LIB=build.build(checked=True))
+    worker = os.path.join(os.path.dirname(os.path.abspath(__file__)), "packed_checked_worker.py")
+    r = subprocess.run([sys.executable, worker], env=env, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
+    out = json.loads(r.stdout.strip().splitlines()[-1])
+    assert out["ok"] and len(out["flagged"]) == 5
