@@ -1,20 +1,20 @@
 // Blocks of the KV cache in 4 bits: packing (from entries of a pool, from the local window, from a dense pool's separate key and
 // value blocks) and unpacking.  The format and its arithmetic are in packed.cuh.
 //
-// Packing: one warp per (request, block, KV head).  Sixteen 16-byte loads per lane bring the 8 KiB of keys and values: a lane holds
-// the same eight dims of eight tokens, 0 .. 7 in lanes 0 .. 15 and 8 .. 15 in lanes 16 .. 31, so that its eight codes of a key are
-// one word, and so are its eight codes of a dim's values.  The largest magnitude of a key's group (16 dims of a token) is one
-// exchange with the neighbouring lane away, of a value's group (16 tokens of a dim) seven maxima and one exchange with the other
-// half-warp.  Divisions are table look-ups by shuffle, a value is rounded by one fused multiply-add, and four codes come together
-// in three integer ones (packed.cuh).  What does not fit into the scales (NaN, infinity, magnitudes above 26,880) is found in the
-// groups' maxima and replaced before.  The entry is put together in shared memory and leaves in 16-byte stores, whole lines,
-// because its place is usually in pinned host memory.  The block's summaries (minimum and maximum of the keys) come from the same
-// registers.  Algorithmic traffic: 8,192 B read, 2,304 B (and 512 B of summaries) written per (block, head).
+// Packing: two warps per (request, block, KV head), one for the keys and one for the values.  Eight 16-byte loads per lane bring the
+// 4 KiB: a lane holds the same eight dims of eight tokens, 0 .. 7 in lanes 0 .. 15 and 8 .. 15 in lanes 16 .. 31, so that its eight
+// codes of a key are one word, and so are its eight codes of a dim's values.  The largest magnitude of a key's group (16 dims of a
+// token) is one exchange with the neighbouring lane away, of a value's group (16 tokens of a dim) seven maxima and one exchange
+// with the other half-warp.  Divisions are table look-ups by shuffle, a value is rounded by one fused multiply-add, and four codes
+// come together in three integer ones (packed.cuh).  What does not fit into the scales (NaN, infinity, magnitudes above 26,880) is
+// found in the groups' maxima and replaced before.  The part is put together in shared memory and leaves in 16-byte stores, whole
+// lines, because its place is usually in pinned host memory.  The block's summaries (minimum and maximum of the keys) come from
+// the same registers.  Algorithmic traffic: 8,192 B read, 2,304 B (and 512 B of summaries) written per (block, head).
 #include "packed.cuh"
 
 namespace oasis {
 
-constexpr int kPackWarps = 4;
+constexpr int kPackWarps = 4;                               // of a thread block: two entries (unpacking: four)
 
 __device__ __forceinline__ uint32_t bf2_min(uint32_t a, uint32_t b)
 {
@@ -41,120 +41,107 @@ __device__ __forceinline__ uint32_t packable(uint32_t v)
     }
     return r;
 }
-// Larger of the two halves' magnitudes (bf16 patterns without sign compare like whole numbers; NaN is the largest).
-__device__ __forceinline__ uint32_t bf2_abs_max(uint32_t a, uint32_t b)
+// Maximum of two pairs of magnitudes (bf16 patterns without sign; NaN is the largest).
+__device__ __forceinline__ uint32_t bf2_max_nan(uint32_t a, uint32_t b)
 {
     uint32_t r;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a & 0x7fff7fffu), "r"(b & 0x7fff7fffu));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 
-// keys (k) and values (v) of one block and head, lane -> 16-byte chunk (lane & 15) of token 8 (lane >> 4) + i; `sm`: 2,304 bytes
-// of this warp, 16-byte aligned; `dst`: the packed entry; `summary` (or NULL): its 512 bytes.
-__device__ __forceinline__ void pack_entry(uint32_t (&k)[8][4], uint32_t (&v)[8][4], uint8_t *sm, uint8_t *dst, uint8_t *summary)
+// The keys (KEYS) or the values of one block and head, lane -> 16-byte chunk (lane & 15) of token 8 (lane >> 4) + i, into their part
+// of an entry: `sm` holds 1,152 bytes of this warp (codes, then scales), 16-byte aligned; `dst`: the packed entry.
+template <bool KEYS>
+__device__ __forceinline__ void pack_part(uint32_t (&x)[8][4], uint8_t *sm, uint8_t *dst)
 {
     const int lane = threadIdx.x & 31, upper = lane >> 4, chunk = lane & 15;
-    if (summary) {
-        uint32_t lo[4], hi[4];
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            lo[p] = hi[p] = k[0][p];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) {
-                lo[p] = bf2_min(lo[p], k[i][p]);
-                hi[p] = bf2_max(hi[p], k[i][p]);
-            }
-            lo[p] = bf2_min(lo[p], __shfl_xor_sync(0xffffffffu, lo[p], 16));
-            hi[p] = bf2_max(hi[p], __shfl_xor_sync(0xffffffffu, hi[p], 16));
-        }
-        *reinterpret_cast<uint4 *>(summary + lane * 16) =
-            upper ? make_uint4(hi[0], hi[1], hi[2], hi[3]) : make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    }
-    uint32_t ka[8], va[8];                                           // the groups' largest magnitudes: of key i, of dim 8 chunk + i
+    uint32_t most[8];                                                // the groups' largest magnitudes: of token i, or of dim 8 chunk + i
     auto maxima = [&]() {
-        uint32_t most = 0;
+        uint32_t all = 0;
+        if (KEYS) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t a2 = bf2_abs_max(bf2_abs_max(k[i][0], k[i][1]), bf2_abs_max(k[i][2], k[i][3]));
-            a2 = bf2_abs_max(a2, __shfl_xor_sync(0xffffffffu, a2, 1));
-            ka[i] = max(a2 & 0xffffu, a2 >> 16);
-            most = max(most, ka[i]);
+            for (int i = 0; i < 8; ++i) {
+                uint32_t a2 = bf2_max_nan(bf2_max_nan(x[i][0] & 0x7fff7fffu, x[i][1] & 0x7fff7fffu), bf2_max_nan(x[i][2] & 0x7fff7fffu, x[i][3] & 0x7fff7fffu));
+                a2 = bf2_max_nan(a2, __shfl_xor_sync(0xffffffffu, a2, 1));
+                most[i] = max(a2 & 0xffffu, a2 >> 16);
+                all = max(all, most[i]);
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                uint32_t a2 = x[0][p] & 0x7fff7fffu;
+#pragma unroll
+                for (int i = 1; i < 8; ++i) a2 = bf2_max_nan(a2, x[i][p] & 0x7fff7fffu);
+                a2 = bf2_max_nan(a2, __shfl_xor_sync(0xffffffffu, a2, 16));
+                most[2 * p] = a2 & 0xffffu;
+                most[2 * p + 1] = a2 >> 16;
+                all = max(all, max(most[2 * p], most[2 * p + 1]));
+            }
         }
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            uint32_t a2 = v[0][p] & 0x7fff7fffu;
-#pragma unroll
-            for (int i = 1; i < 8; ++i) a2 = bf2_abs_max(a2, v[i][p]);
-            a2 = bf2_abs_max(a2, __shfl_xor_sync(0xffffffffu, a2, 16));
-            va[2 * p] = a2 & 0xffffu;
-            va[2 * p + 1] = a2 >> 16;
-            most = max(most, max(va[2 * p], va[2 * p + 1]));
-        }
-        return most;
+        return all;
     };
     if (__any_sync(0xffffffffu, maxima() > kPackLargest)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                k[i][p] = packable(k[i][p]);
-                v[i][p] = packable(v[i][p]);
-            }
+            for (int p = 0; p < 4; ++p) x[i][p] = packable(x[i][p]);
         maxima();
     }
     const uint32_t steps = scale_table();
     const float inverses = inverse_table();
-    // keys: two lanes per group
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int byte = scale_byte(ka[i], steps), token = 8 * upper + i;
+        const int byte = scale_byte(most[i], steps);
         const float inv = scale_inverse(byte, inverses);
         uint32_t c[8];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            c[2 * p] = code_bits(bf_lo(k[i][p]), inv);
-            c[2 * p + 1] = code_bits(bf_hi(k[i][p]), inv);
+            if (KEYS) {                                              // dims of token 8 upper + i
+                c[2 * p] = code_bits(bf_lo(x[i][p]), inv);
+                c[2 * p + 1] = code_bits(bf_hi(x[i][p]), inv);
+            } else {                                                 // tokens of dim 8 chunk + i
+                c[2 * p] = code_bits(i & 1 ? bf_hi(x[2 * p][i >> 1]) : bf_lo(x[2 * p][i >> 1]), inv);
+                c[2 * p + 1] = code_bits(i & 1 ? bf_hi(x[2 * p + 1][i >> 1]) : bf_lo(x[2 * p + 1][i >> 1]), inv);
+            }
         }
-        *reinterpret_cast<uint32_t *>(sm + (chunk >> 2) * 256 + token * 16 + (chunk & 3) * 4) =
-            __byte_perm(code_half(c[0], c[2], c[4], c[6]), code_half(c[1], c[3], c[5], c[7]), 0x5410);
-        if (!(lane & 1)) sm[kPackedKScale + token * 8 + (chunk >> 1)] = (uint8_t)byte;
-    }
-    // values: the lane's eight dims, its eight tokens
-#pragma unroll
-    for (int d = 0; d < 8; ++d) {
-        const int byte = scale_byte(va[d], steps), dim = chunk * 8 + d;
-        const float inv = scale_inverse(byte, inverses);
-        uint32_t c[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = code_bits(d & 1 ? bf_hi(v[i][d >> 1]) : bf_lo(v[i][d >> 1]), inv);
-        *reinterpret_cast<uint32_t *>(sm + kPackedV + dim * 8 + upper * 4) =
-            __byte_perm(code_half(c[0], c[2], c[4], c[6]), code_half(c[1], c[3], c[5], c[7]), 0x5410);
-        if (!upper) sm[kPackedVScale + dim] = (uint8_t)byte;
+        const uint32_t word = __byte_perm(code_half(c[0], c[2], c[4], c[6]), code_half(c[1], c[3], c[5], c[7]), 0x5410);
+        if (KEYS) {
+            const int token = 8 * upper + i;
+            *reinterpret_cast<uint32_t *>(sm + (chunk >> 2) * 256 + token * 16 + (chunk & 3) * 4) = word;
+            if (!(lane & 1)) sm[1024 + token * 8 + (chunk >> 1)] = (uint8_t)byte;
+        } else {
+            *reinterpret_cast<uint32_t *>(sm + (chunk * 8 + i) * 8 + upper * 4) = word;
+            if (!upper) sm[1024 + chunk * 8 + i] = (uint8_t)byte;
+        }
     }
     __syncwarp();
+    uint8_t *const codes = dst + (KEYS ? 0 : kPackedV);
 #pragma unroll
-    for (int i = 0; i < 5; ++i)
-        if (lane + 32 * i < kPackedBytes / 16) *reinterpret_cast<uint4 *>(dst + (lane + 32 * i) * 16) = *reinterpret_cast<const uint4 *>(sm + (lane + 32 * i) * 16);
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4 *>(codes + (lane + 32 * i) * 16) = *reinterpret_cast<const uint4 *>(sm + (lane + 32 * i) * 16);
+    if (lane < 8) *reinterpret_cast<uint4 *>(dst + (KEYS ? kPackedKScale : kPackedVScale) + lane * 16) = *reinterpret_cast<const uint4 *>(sm + 1024 + lane * 16);
 }
 
+// One layer's buffers, or several's (the parameters of a launch are sent with it: 48 bytes rather than 3 KiB where one will do).
+template <int LAYERS>
 struct PackLayers {
-    const uint8_t *k_src[OASIS_MAX_APPEND_LAYERS];      // entries, or key blocks
-    const uint8_t *v_src[OASIS_MAX_APPEND_LAYERS];
-    const int32_t *src_table[OASIS_MAX_APPEND_LAYERS];  // [B][max_blocks] pages, or [B][Hkv][n_cols] slots
-    const int32_t *block_table[OASIS_MAX_APPEND_LAYERS];
-    uint8_t *packed[OASIS_MAX_APPEND_LAYERS];
-    uint8_t *summaries[OASIS_MAX_APPEND_LAYERS];
+    const uint8_t *k_src[LAYERS];      // entries, or key blocks
+    const uint8_t *v_src[LAYERS];
+    const int32_t *src_table[LAYERS];  // [B][max_blocks] pages, or [B][Hkv][n_cols] slots
+    const int32_t *block_table[LAYERS];
+    uint8_t *packed[LAYERS];
+    uint8_t *summaries[LAYERS];
 };
 
 // SLOTS: the source of block j is the entry of the local column that belongs to j, else of page src_table[b][j].
-template <bool SLOTS>
+template <bool SLOTS, int LAYERS>
 __global__ void __launch_bounds__(kPackWarps * 32)
-pack_blocks_kernel(const __grid_constant__ PackLayers ly, const int32_t *__restrict__ first_block, const int32_t *__restrict__ n_blocks,
+pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t *__restrict__ first_block, const int32_t *__restrict__ n_blocks,
                    int Hkv, int max_blocks, int max_new, int src_bytes, int n_cols, int local_col, long long n_items, const Bounds bd)
 {
-    __shared__ __align__(16) uint8_t sm[kPackWarps][kPackedBytes];
-    const int lane = threadIdx.x & 31, l = blockIdx.y;
-    const long long item = (long long)blockIdx.x * kPackWarps + (threadIdx.x >> 5);
+    __shared__ __align__(16) uint8_t sm[kPackWarps][kPackedBytes / 2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = LAYERS == 1 ? 0 : blockIdx.y;
+    const bool keys = warp < kPackWarps / 2;
+    const long long item = (long long)blockIdx.x * (kPackWarps / 2) + warp % (kPackWarps / 2);
     if (item >= n_items) return;
     const int h = (int)(item % Hkv);
     const int jj = (int)((item / Hkv) % max_new);
@@ -175,21 +162,35 @@ pack_blocks_kernel(const __grid_constant__ PackLayers ly, const int32_t *__restr
     }
     const long long dst = (long long)ly.block_table[l][(long long)b * max_blocks + j] * Hkv + h;
     if (!in_range(dst, bd.n_entries, bd, kErrHostEntry)) return;
-    const int at = (lane >> 4) * 8 * kRowBytes + (lane & 15) * 16;
-    const uint8_t *ksrc = ly.k_src[l] + src * src_bytes + at, *vsrc = ly.v_src[l] + src * src_bytes + at;
-    uint32_t k[8][4], v[8][4];
+    const uint8_t *from = (keys ? ly.k_src[l] : ly.v_src[l]) + src * src_bytes + (lane >> 4) * 8 * kRowBytes + (lane & 15) * 16;
+    uint32_t x[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint4 w = ld_stream_v4(ksrc + i * kRowBytes);
-        k[i][0] = w.x; k[i][1] = w.y; k[i][2] = w.z; k[i][3] = w.w;
+        const uint4 w = ld_stream_v4(from + i * kRowBytes);
+        x[i][0] = w.x; x[i][1] = w.y; x[i][2] = w.z; x[i][3] = w.w;
     }
+    uint8_t *const entry = ly.packed[l] + dst * kPackedBytes;
+    if (!keys) {
+        pack_part<false>(x, sm[warp], entry);
+        return;
+    }
+    if (ly.summaries[l]) {
+        uint32_t lo[4], hi[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint4 w = ld_stream_v4(vsrc + i * kRowBytes);
-        v[i][0] = w.x; v[i][1] = w.y; v[i][2] = w.z; v[i][3] = w.w;
+        for (int p = 0; p < 4; ++p) {
+            lo[p] = hi[p] = x[0][p];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) {
+                lo[p] = bf2_min(lo[p], x[i][p]);
+                hi[p] = bf2_max(hi[p], x[i][p]);
+            }
+            lo[p] = bf2_min(lo[p], __shfl_xor_sync(0xffffffffu, lo[p], 16));
+            hi[p] = bf2_max(hi[p], __shfl_xor_sync(0xffffffffu, hi[p], 16));
+        }
+        uint8_t *const summary = ly.summaries[l] + (((long long)b * Hkv + h) * max_blocks + j) * kSummaryBytes;
+        *reinterpret_cast<uint4 *>(summary + lane * 16) = lane < 16 ? make_uint4(lo[0], lo[1], lo[2], lo[3]) : make_uint4(hi[0], hi[1], hi[2], hi[3]);
     }
-    pack_entry(k, v, sm[threadIdx.x >> 5], ly.packed[l] + dst * kPackedBytes,
-               ly.summaries[l] ? ly.summaries[l] + (((long long)b * Hkv + h) * max_blocks + j) * kSummaryBytes : nullptr);
+    pack_part<true>(x, sm[warp], entry);
 }
 
 // One warp per list position: the packed entry through shared memory, the bf16 entry in sixteen 16-byte stores per lane.
@@ -244,7 +245,8 @@ unpack_blocks_kernel(const uint8_t *__restrict__ packed, const long long *__rest
 }
 
 // The checks and the launch that the three packing entry points share.
-static int launch_pack(const char *who, const oasis_dims_t *dims, int n_layers, const PackLayers &ly, bool slots, const int32_t *first_block,
+template <bool SLOTS, int LAYERS>
+static int launch_pack(const char *who, const oasis_dims_t *dims, int n_layers, const PackLayers<LAYERS> &ly, const int32_t *first_block,
                        const int32_t *n_blocks, int max_new, int src_bytes, int n_cols, int local_col, void *stream)
 {
     if (!first_block || !n_blocks) return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
@@ -258,18 +260,11 @@ static int launch_pack(const char *who, const oasis_dims_t *dims, int n_layers, 
     }
     const long long n_items = (long long)dims->batch * dims->n_kv_heads * max_new;
     if (n_items == 0 || n_layers == 0) return OASIS_OK;
-    const long long grid = (n_items + kPackWarps - 1) / kPackWarps;
+    const long long grid = (n_items + kPackWarps / 2 - 1) / (kPackWarps / 2);
     if (grid > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: too many blocks", who);
-    const dim3 g((unsigned)grid, (unsigned)n_layers);
-    if (slots) {
-        prefer_max_shared_carveout(pack_blocks_kernel<true>);
-        pack_blocks_kernel<true><<<g, kPackWarps * 32, 0, (cudaStream_t)stream>>>(ly, first_block, n_blocks, dims->n_kv_heads, dims->max_blocks,
-                                                                                  max_new, src_bytes, n_cols, local_col, n_items, bounds());
-    } else {
-        prefer_max_shared_carveout(pack_blocks_kernel<false>);
-        pack_blocks_kernel<false><<<g, kPackWarps * 32, 0, (cudaStream_t)stream>>>(ly, first_block, n_blocks, dims->n_kv_heads, dims->max_blocks,
-                                                                                   max_new, src_bytes, n_cols, local_col, n_items, bounds());
-    }
+    prefer_max_shared_carveout(pack_blocks_kernel<SLOTS, LAYERS>);
+    pack_blocks_kernel<SLOTS, LAYERS><<<dim3((unsigned)grid, (unsigned)n_layers), kPackWarps * 32, 0, (cudaStream_t)stream>>>(
+        ly, first_block, n_blocks, dims->n_kv_heads, dims->max_blocks, max_new, src_bytes, n_cols, local_col, n_items, bounds());
     return check_launch(who);
 }
 
@@ -281,14 +276,14 @@ extern "C" int oasis_pack_blocks(const oasis_dims_t *dims, const void *kv_pool, 
 {
     using namespace oasis;
     if (int rc = check_dims(dims)) return rc;
-    PackLayers ly = {};
+    PackLayers<1> ly = {};
     ly.k_src[0] = (const uint8_t *)kv_pool;
     ly.v_src[0] = kv_pool ? (const uint8_t *)kv_pool + kPartBytes : nullptr;
     ly.src_table[0] = src_table;
     ly.block_table[0] = block_table;
     ly.packed[0] = (uint8_t *)packed;
     ly.summaries[0] = (uint8_t *)summaries;
-    return launch_pack("oasis_pack_blocks", dims, 1, ly, false, first_block, n_blocks, max_new_blocks, kEntryBytes, 0, 0, stream);
+    return launch_pack<false>("oasis_pack_blocks", dims, 1, ly, first_block, n_blocks, max_new_blocks, kEntryBytes, 0, 0, stream);
 }
 
 extern "C" int oasis_offload_blocks_packed(const oasis_dims_t *dims, const void *dense_k, const void *dense_v, const int32_t *gpu_table,
@@ -297,14 +292,14 @@ extern "C" int oasis_offload_blocks_packed(const oasis_dims_t *dims, const void 
 {
     using namespace oasis;
     if (int rc = check_dims(dims)) return rc;
-    PackLayers ly = {};
+    PackLayers<1> ly = {};
     ly.k_src[0] = (const uint8_t *)dense_k;
     ly.v_src[0] = (const uint8_t *)dense_v;
     ly.src_table[0] = gpu_table;
     ly.block_table[0] = block_table;
     ly.packed[0] = (uint8_t *)packed;
     ly.summaries[0] = (uint8_t *)summaries;
-    return launch_pack("oasis_offload_blocks_packed", dims, 1, ly, false, first_block, n_blocks, max_new_blocks, kPartBytes, 0, 0, stream);
+    return launch_pack<false>("oasis_offload_blocks_packed", dims, 1, ly, first_block, n_blocks, max_new_blocks, kPartBytes, 0, 0, stream);
 }
 
 extern "C" int oasis_pack_local_layers(const oasis_dims_t *dims, int32_t n_layers, const void *const *hbm_pools,
@@ -323,7 +318,7 @@ extern "C" int oasis_pack_local_layers(const oasis_dims_t *dims, int32_t n_layer
         return fail(OASIS_ERR_INVALID_ARG, "%s: max_new_blocks %d: the local window holds two blocks", who, max_new_blocks);
     if (n_layers == 0) return OASIS_OK;
     if (!hbm_pools || !slot_tbls || !packed || !block_tables) return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
-    PackLayers ly = {};
+    PackLayers<OASIS_MAX_APPEND_LAYERS> ly = {};
     for (int l = 0; l < n_layers; ++l) {
         ly.k_src[l] = (const uint8_t *)hbm_pools[l];
         ly.v_src[l] = hbm_pools[l] ? (const uint8_t *)hbm_pools[l] + kPartBytes : nullptr;
@@ -332,7 +327,7 @@ extern "C" int oasis_pack_local_layers(const oasis_dims_t *dims, int32_t n_layer
         ly.packed[l] = (uint8_t *)packed[l];
         ly.summaries[l] = summaries ? (uint8_t *)summaries[l] : nullptr;
     }
-    return launch_pack(who, dims, n_layers, ly, true, first_block, n_blocks, max_new_blocks, kEntryBytes, n_cols, local_col, stream);
+    return launch_pack<true>(who, dims, n_layers, ly, first_block, n_blocks, max_new_blocks, kEntryBytes, n_cols, local_col, stream);
 }
 
 extern "C" int oasis_unpack_blocks(const void *packed, const int64_t *idx, int32_t n, void *out, void *stream)

@@ -16,7 +16,7 @@ namespace oasis {
 
 constexpr int kRotThreads = 128, kRotLanes = 16, kRotWorkers = kRotThreads / kRotLanes;
 constexpr int kRotMaxTokens = 8;                            // tokens of a thread block at most
-constexpr int kRotAhead = 4;                                // rows of a half-warp in flight
+constexpr int kRotRegs = 24;                                // registers of a lane's rows in flight
 
 struct RotateParams {
     const uint8_t *qkv;
@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(kRotThreads)
 rotate_qkv_kernel(const RotateParams p)
 {
     constexpr int SIZE = TYPE == OASIS_F32 ? 4 : 2, W = 2 * SIZE;        // registers of 8 elements
+    constexpr int AHEAD = kRotRegs / W;                                  // rows of a half-warp in flight
     __shared__ __align__(16) float2 turn[kRotMaxTokens][kHeadDim / 2];   // (cos, sin) times the factor
     __shared__ int s_depth[kRotMaxTokens];
     __shared__ float s_row[MODE == kOddHalves ? kRotWorkers : 1][kRotLanes * 9];
@@ -67,12 +68,12 @@ rotate_qkv_kernel(const RotateParams p)
     const int here = (int)min((uint32_t)p.tokens_per_block, (uint32_t)p.n_tokens - n0);
     const int worker = tid / kRotLanes, chunk = tid % kRotLanes, d0 = chunk * 8;
     const int n_rot = p.Hq + p.Hkv, n_rows = p.Hq + 2 * p.Hkv;
-    uint32_t w[kRotAhead][W];
+    uint32_t w[AHEAD][W];
     auto load = [&](int k, int a0) {                                     // rows a0, a0 + kRotWorkers, .. of token n0 + k
         const uint32_t n = n0 + k;
         const uint8_t *src = p.qkv + ((long long)(n / T) * p.batch_stride + (long long)(n % T) * p.token_stride + d0) * SIZE;
 #pragma unroll
-        for (int u = 0; u < kRotAhead; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const int a = a0 + u * kRotWorkers;
             if (a < n_rows) {
 #pragma unroll
@@ -129,63 +130,54 @@ rotate_qkv_kernel(const RotateParams p)
     }
     __syncthreads();
 
-    const bool turned = d0 < p.rot;                                      // some of this lane's dims are rotated
-    const unsigned team = 0xffffu << (lane & 16);                        // the half-warp
     for (int k = 0; k < here; ++k) {
         const uint32_t n = n0 + k;
         const int b = (int)(n / T), t = (int)(n % T);
         if (p.n_nodes && t >= p.n_nodes[b]) continue;                    // padding: left as it was
-        float2 cs[8];
+        float c[8], s[8];                                                // x cos + (the partner) s, s with the sign of its place
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int d = d0 + e, f = MODE == kSideBySide ? d >> 1 : d < half ? d : d - half;
-            cs[e] = d < p.rot ? turn[k][f] : make_float2(1.f, 0.f);
+            const float2 v = d < p.rot ? turn[k][f] : make_float2(1.f, 0.f);
+            c[e] = v.x;
+            s[e] = (MODE == kSideBySide ? e % 2 == 0 : d < half) ? -v.y : v.y;
         }
-        for (int a0 = worker; a0 < n_rows; a0 += kRotWorkers * kRotAhead) {
+        // the half-warps of a warp go through the rows together (rows a and a + 1)
+        for (int a0 = worker; (a0 & ~1) < n_rows; a0 += kRotWorkers * AHEAD) {
             if (k > 0 || a0 > worker) load(k, a0);
 #pragma unroll
-            for (int u = 0; u < kRotAhead; ++u) {
+            for (int u = 0; u < AHEAD; ++u) {
                 const int a = a0 + u * kRotWorkers;
-                if (a >= n_rows) break;                                  // (the same for the whole half-warp)
+                if ((a & ~1) >= n_rows) break;
                 float x[8];
                 to_floats<TYPE, W>(w[u], x);
-                if (a < n_rot) {
-                    if (MODE == kSideBySide) {
+                float y[8];                                              // the partners
+                if (MODE == kSideBySide) {
 #pragma unroll
-                        for (int e = 0; e < 8; e += 2) {
-                            const float lo = x[e], hi = x[e + 1];
-                            if (d0 + e < p.rot) {
-                                x[e] = lo * cs[e].x - hi * cs[e].y;
-                                x[e + 1] = hi * cs[e].x + lo * cs[e].y;
-                            }
-                        }
-                    } else {
-                        float y[8];                                      // the partners
-                        if (MODE == kHalves) {
-                            const int step = half >> 3;
-                            uint32_t o[W];
+                    for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+                } else if (MODE == kHalves) {
+                    const int step = half >> 3, from = chunk < step ? chunk + step : chunk < 2 * step ? chunk - step : chunk;
+                    uint32_t o[W];
 #pragma unroll
-                            for (int v = 0; v < W; ++v) o[v] = __shfl_sync(team, w[u][v], turned ? (chunk < step ? chunk + step : chunk - step) : chunk, 16);
-                            to_floats<TYPE, W>(o, y);
-                        } else {
-                            float *const row = s_row[worker];
+                    for (int v = 0; v < W; ++v) o[v] = __shfl_sync(0xffffffffu, w[u][v], from, kRotLanes);
+                    to_floats<TYPE, W>(o, y);
+                } else {
+                    float *const row = s_row[worker];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) row[chunk * 9 + e] = x[e];
-                            __syncwarp(team);
+                    for (int e = 0; e < 8; ++e) row[chunk * 9 + e] = x[e];
+                    __syncwarp();
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int d = d0 + e, mate = d < half ? d + half : d < p.rot ? d - half : d;
-                                y[e] = row[mate + (mate >> 3)];
-                            }
-                            __syncwarp(team);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int d = d0 + e;
-                            if (d < half) x[e] = x[e] * cs[e].x - y[e] * cs[e].y;
-                            else if (d < p.rot) x[e] = x[e] * cs[e].x + y[e] * cs[e].y;
-                        }
+                    for (int e = 0; e < 8; ++e) {
+                        const int d = d0 + e, mate = d < half ? d + half : d < p.rot ? d - half : d;
+                        y[e] = row[mate + (mate >> 3)];
                     }
+                    __syncwarp();
+                }
+                if (a >= n_rows) continue;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float r = fmaf(x[e], c[e], y[e] * s[e]);
+                    x[e] = a < n_rot && d0 + e < p.rot ? r : x[e];
                 }
                 uint8_t *dst;
                 if (a < p.Hq) dst = p.q + ((long long)n * p.Hq + a) * kRowBytes;
@@ -235,7 +227,7 @@ extern "C" int oasis_rotate_qkv(const oasis_dims_t *dims, const void *qkv, int32
     // a token per thread block while that leaves SMs without one; else tokens until a half-warp has four rows to move
     const int rows = p.Hq + 2 * p.Hkv;
     long long per = total / (8ll * sm_count());
-    const long long few = (kRotWorkers * kRotAhead + rows - 1) / rows;
+    const long long few = (kRotWorkers * 4 + rows - 1) / rows;
     if (per > few) per = few;
     p.tokens_per_block = (int)(per < 1 ? 1 : per > kRotMaxTokens ? kRotMaxTokens : per);
     const unsigned grid = (unsigned)((total + p.tokens_per_block - 1) / p.tokens_per_block);
