@@ -50,9 +50,10 @@ __device__ __forceinline__ uint32_t bf2_max_nan(uint32_t a, uint32_t b)
 }
 
 // The keys (KEYS) or the values of one block and head, lane -> 16-byte chunk (lane & 15) of token 8 (lane >> 4) + i, into their part
-// of an entry: `sm` holds 1,152 bytes of this warp (codes, then scales), 16-byte aligned; `dst`: the packed entry.
+// of an entry: `steps` and `inverses` are this lane's of the tables, `sm` holds 1,152 bytes of this warp (codes, then scales),
+// 16-byte aligned; `dst`: the packed entry.
 template <bool KEYS>
-__device__ __forceinline__ void pack_part(uint32_t (&x)[8][4], uint8_t *sm, uint8_t *dst)
+__device__ __forceinline__ void pack_part(uint32_t (&x)[8][4], uint32_t steps, float inverses, uint8_t *sm, uint8_t *dst)
 {
     const int lane = threadIdx.x & 31, upper = lane >> 4, chunk = lane & 15;
     uint32_t most[8];                                                // the groups' largest magnitudes: of token i, or of dim 8 chunk + i
@@ -87,8 +88,6 @@ __device__ __forceinline__ void pack_part(uint32_t (&x)[8][4], uint8_t *sm, uint
             for (int p = 0; p < 4; ++p) x[i][p] = packable(x[i][p]);
         maxima();
     }
-    const uint32_t steps = scale_table();
-    const float inverses = inverse_table();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int byte = scale_byte(most[i], steps);
@@ -136,16 +135,17 @@ struct PackLayers {
 template <bool SLOTS, int LAYERS>
 __global__ void __launch_bounds__(kPackWarps * 32)
 pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t *__restrict__ first_block, const int32_t *__restrict__ n_blocks,
-                   int Hkv, int max_blocks, int max_new, int src_bytes, int n_cols, int local_col, long long n_items, const Bounds bd)
+                   int Hkv, int max_blocks, int max_new, int src_bytes, int n_cols, int local_col, uint32_t n_items, const Bounds bd)
 {
     __shared__ __align__(16) uint8_t sm[kPackWarps][kPackedBytes / 2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = LAYERS == 1 ? 0 : blockIdx.y;
     const bool keys = warp < kPackWarps / 2;
-    const long long item = (long long)blockIdx.x * (kPackWarps / 2) + warp % (kPackWarps / 2);
+    const uint32_t item = blockIdx.x * (kPackWarps / 2) + warp % (kPackWarps / 2);
     if (item >= n_items) return;
-    const int h = (int)(item % Hkv);
-    const int jj = (int)((item / Hkv) % max_new);
-    const int b = (int)(item / ((long long)Hkv * max_new));
+    const uint32_t steps = kPackTables.steps[lane];
+    const float inverses = kPackTables.inverses[lane & 7];
+    const uint32_t row = item / (uint32_t)Hkv;
+    const int h = (int)(item % (uint32_t)Hkv), jj = (int)(row % (uint32_t)max_new), b = (int)(row / (uint32_t)max_new);
     const int n = n_blocks[b];
     const long long j = (long long)first_block[b] + jj;              // (both on their way at once)
     if (jj >= n) return;
@@ -171,7 +171,7 @@ pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t 
     }
     uint8_t *const entry = ly.packed[l] + dst * kPackedBytes;
     if (!keys) {
-        pack_part<false>(x, sm[warp], entry);
+        pack_part<false>(x, steps, inverses, sm[warp], entry);
         return;
     }
     if (ly.summaries[l]) {
@@ -190,7 +190,7 @@ pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t 
         uint8_t *const summary = ly.summaries[l] + (((long long)b * Hkv + h) * max_blocks + j) * kSummaryBytes;
         *reinterpret_cast<uint4 *>(summary + lane * 16) = lane < 16 ? make_uint4(lo[0], lo[1], lo[2], lo[3]) : make_uint4(hi[0], hi[1], hi[2], hi[3]);
     }
-    pack_part<true>(x, sm[warp], entry);
+    pack_part<true>(x, steps, inverses, sm[warp], entry);
 }
 
 // One warp per list position: the packed entry through shared memory, the bf16 entry in sixteen 16-byte stores per lane.
@@ -260,11 +260,11 @@ static int launch_pack(const char *who, const oasis_dims_t *dims, int n_layers, 
     }
     const long long n_items = (long long)dims->batch * dims->n_kv_heads * max_new;
     if (n_items == 0 || n_layers == 0) return OASIS_OK;
+    if (n_items > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: too many blocks", who);
     const long long grid = (n_items + kPackWarps / 2 - 1) / (kPackWarps / 2);
-    if (grid > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: too many blocks", who);
     prefer_max_shared_carveout(pack_blocks_kernel<SLOTS, LAYERS>);
     pack_blocks_kernel<SLOTS, LAYERS><<<dim3((unsigned)grid, (unsigned)n_layers), kPackWarps * 32, 0, (cudaStream_t)stream>>>(
-        ly, first_block, n_blocks, dims->n_kv_heads, dims->max_blocks, max_new, src_bytes, n_cols, local_col, n_items, bounds());
+        ly, first_block, n_blocks, dims->n_kv_heads, dims->max_blocks, max_new, src_bytes, n_cols, local_col, (uint32_t)n_items, bounds());
     return check_launch(who);
 }
 

@@ -36,11 +36,19 @@ __host__ __device__ constexpr uint32_t scale_step(uint32_t m)
     return m < 96 ? nearest_even<14>(128 + m) - 8 : nearest_even<28>(128 + m);
 }
 static_assert(scale_step(0) == 1 && scale_step(133 - 128) == 2 && scale_step(147 - 128) == 2 && scale_step(96) == 8 && scale_step(238 - 128) == 8, "scale steps");
-__device__ __forceinline__ uint32_t scale_table()      // of this lane
+struct PackTables {
+    uint32_t steps[32];                                // four scale_step() each
+    float inverses[8];                                 // 2^-20 less than 8 / (8 + m)
+};
+constexpr PackTables pack_tables()
 {
-    const uint32_t m = 4 * (threadIdx.x & 31);
-    return scale_step(m) | scale_step(m + 1) << 8 | scale_step(m + 2) << 16 | scale_step(m + 3) << 24;
+    PackTables t = {};
+    for (uint32_t k = 0; k < 32; ++k)
+        t.steps[k] = scale_step(4 * k) | scale_step(4 * k + 1) << 8 | scale_step(4 * k + 2) << 16 | scale_step(4 * k + 3) << 24;
+    for (int m = 0; m < 8; ++m) t.inverses[m] = 8.0f * (1.0f - 0x1p-20f) / (float)(8 + m);
+    return t;
 }
+static __device__ const PackTables kPackTables = pack_tables();
 __device__ __forceinline__ int scale_byte(uint32_t amax, uint32_t table)               // by the whole warp
 {
     const uint32_t m = amax & 127u, four = __shfl_sync(0xffffffffu, table, m >> 2);
@@ -50,8 +58,7 @@ __device__ __forceinline__ int scale_byte(uint32_t amax, uint32_t table)        
 __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float(((uint32_t)byte << 20) + ((127u - kScaleBias) << 23)); }
 // What a value is multiplied by: 1 / s, 2^-20 of it less.  Products are then below the exact quotient by 2^-21 to 2^-19 of it, so that
 // a value halfway between two multiples of s goes to the smaller one; any other quotient is 2^-9 of itself from a halfway point.
-// `table`: lane m < 8 holds that of (8 + m) / 8.
-__device__ __forceinline__ float inverse_table() { return __fdiv_rn(8.0f * (1.0f - 0x1p-20f), (float)(8 + (threadIdx.x & 7))); }
+// `table`: lane m holds that of (8 + m % 8) / 8.
 __device__ __forceinline__ float scale_inverse(int byte, float table)                  // by the whole warp
 {
     return __uint_as_float(__float_as_uint(__shfl_sync(0xffffffffu, table, byte & 7)) + (uint32_t)(kScaleBias - (byte >> 3)) * (1u << 23));

@@ -16,7 +16,6 @@ namespace oasis {
 
 constexpr int kRotThreads = 128, kRotLanes = 16, kRotWorkers = kRotThreads / kRotLanes;
 constexpr int kRotMaxTokens = 8;                            // tokens of a thread block at most
-constexpr int kRotRegs = 24;                                // registers of a lane's rows in flight
 
 struct RotateParams {
     const uint8_t *qkv;
@@ -59,7 +58,7 @@ __global__ void __launch_bounds__(kRotThreads)
 rotate_qkv_kernel(const RotateParams p)
 {
     constexpr int SIZE = TYPE == OASIS_F32 ? 4 : 2, W = 2 * SIZE;        // registers of 8 elements
-    constexpr int AHEAD = kRotRegs / W;                                  // rows of a half-warp in flight
+    constexpr int AHEAD = TYPE == OASIS_F32 ? 2 : 3;                     // rows of a half-warp in flight
     __shared__ __align__(16) float2 turn[kRotMaxTokens][kHeadDim / 2];   // (cos, sin) times the factor
     __shared__ int s_depth[kRotMaxTokens];
     __shared__ float s_row[MODE == kOddHalves ? kRotWorkers : 1][kRotLanes * 9];
@@ -142,6 +141,8 @@ rotate_qkv_kernel(const RotateParams p)
             c[e] = v.x;
             s[e] = (MODE == kSideBySide ? e % 2 == 0 : d < half) ? -v.y : v.y;
         }
+        uint8_t *const q = p.q + (long long)n * p.Hq * kRowBytes + d0 * 2, *const kv = p.kv + (long long)n * p.Hkv * 2 * kRowBytes + d0 * 2;
+        const bool partly = p.rot % 8 != 0;                              // some lane holds rotated and other dims
         // the half-warps of a warp go through the rows together (rows a and a + 1)
         for (int a0 = worker; (a0 & ~1) < n_rows; a0 += kRotWorkers * AHEAD) {
             if (k > 0 || a0 > worker) load(k, a0);
@@ -151,41 +152,41 @@ rotate_qkv_kernel(const RotateParams p)
                 if ((a & ~1) >= n_rows) break;
                 float x[8];
                 to_floats<TYPE, W>(w[u], x);
-                float y[8];                                              // the partners
-                if (MODE == kSideBySide) {
+                uint4 o = TYPE == OASIS_BF16 ? make_uint4(w[u][0], w[u][1], w[u][2], w[u][3])          // (copied bit by bit)
+                                             : make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+                if ((a & ~1) < n_rot) {
+                    float y[8];                                          // the partners
+                    if (MODE == kSideBySide) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
-                } else if (MODE == kHalves) {
-                    const int step = half >> 3, from = chunk < step ? chunk + step : chunk < 2 * step ? chunk - step : chunk;
-                    uint32_t o[W];
+                        for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+                    } else if (MODE == kHalves) {
+                        const int step = half >> 3, from = chunk < step ? chunk + step : chunk < 2 * step ? chunk - step : chunk;
+                        uint32_t v[W];
 #pragma unroll
-                    for (int v = 0; v < W; ++v) o[v] = __shfl_sync(0xffffffffu, w[u][v], from, kRotLanes);
-                    to_floats<TYPE, W>(o, y);
-                } else {
-                    float *const row = s_row[worker];
+                        for (int i = 0; i < W; ++i) v[i] = __shfl_sync(0xffffffffu, w[u][i], from, kRotLanes);
+                        to_floats<TYPE, W>(v, y);
+                    } else {
+                        float *const row = s_row[worker];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) row[chunk * 9 + e] = x[e];
-                    __syncwarp();
+                        for (int e = 0; e < 8; ++e) row[chunk * 9 + e] = x[e];
+                        __syncwarp();
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int d = d0 + e, mate = d < half ? d + half : d < p.rot ? d - half : d;
+                            y[e] = row[mate + (mate >> 3)];
+                        }
+                        __syncwarp();
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const int d = d0 + e, mate = d < half ? d + half : d < p.rot ? d - half : d;
-                        y[e] = row[mate + (mate >> 3)];
+                        const float r = fmaf(x[e], c[e], y[e] * s[e]);
+                        x[e] = partly && d0 + e >= p.rot ? x[e] : r;
                     }
-                    __syncwarp();
+                    if (a < n_rot && d0 < p.rot)
+                        o = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
                 }
                 if (a >= n_rows) continue;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float r = fmaf(x[e], c[e], y[e] * s[e]);
-                    x[e] = a < n_rot && d0 + e < p.rot ? r : x[e];
-                }
-                uint8_t *dst;
-                if (a < p.Hq) dst = p.q + ((long long)n * p.Hq + a) * kRowBytes;
-                else if (a < n_rot) dst = p.kv + (((long long)n * p.Hkv + a - p.Hq) * 2) * kRowBytes;
-                else dst = p.kv + (((long long)n * p.Hkv + a - n_rot) * 2 + 1) * kRowBytes;
-                uint4 o = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-                if (TYPE == OASIS_BF16 && (a >= n_rot || d0 >= p.rot)) o = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);   // (copied bit by bit)
-                *reinterpret_cast<uint4 *>(dst + d0 * 2) = o;
+                *reinterpret_cast<uint4 *>(a < p.Hq ? q + a * kRowBytes : kv + (a < n_rot ? 2 * (a - p.Hq) : 2 * (a - n_rot) + 1) * kRowBytes) = o;
             }
         }
     }
