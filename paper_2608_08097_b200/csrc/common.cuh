@@ -139,4 +139,21 @@ inline void prefer_max_shared_carveout(K kernel)
     prefer_max_shared_carveout_of(reinterpret_cast<const void *>(kernel));
 }
 
+// Launch of a kernel that waits (griddepcontrol.wait) before it reads or writes anything of the stream's: it may be brought onto the
+// SMs while the launch before it ends, which takes its launch latency out of a chain of small ones.
+template <typename K, typename... A>
+inline cudaError_t launch_waiting(K kernel, dim3 grid, int threads, cudaStream_t stream, const A &...args)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 }  // namespace oasis

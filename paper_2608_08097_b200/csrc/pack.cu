@@ -146,6 +146,7 @@ pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t 
     const float inverses = kPackTables.inverses[lane & 7];
     const uint32_t row = item / (uint32_t)Hkv;
     const int h = (int)(item % (uint32_t)Hkv), jj = (int)(row % (uint32_t)max_new), b = (int)(row / (uint32_t)max_new);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int n = n_blocks[b];
     const long long j = (long long)first_block[b] + jj;              // (both on their way at once)
     if (jj >= n) return;
@@ -201,6 +202,7 @@ unpack_blocks_kernel(const uint8_t *__restrict__ packed, const long long *__rest
     const int lane = threadIdx.x & 31, upper = lane >> 4, chunk = lane & 15;
     const long long item = (long long)blockIdx.x * kPackWarps + (threadIdx.x >> 5);
     if (item >= n) return;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const long long src = idx[item];
     if (src < 0 || !in_range(src, bd.n_entries, bd, kErrHostEntry)) return;
     uint8_t *sm = sm_all[threadIdx.x >> 5];
@@ -263,9 +265,14 @@ static int launch_pack(const char *who, const oasis_dims_t *dims, int n_layers, 
     if (n_items > 0x7fffffffLL) return fail(OASIS_ERR_UNSUPPORTED, "%s: too many blocks", who);
     const long long grid = (n_items + kPackWarps / 2 - 1) / (kPackWarps / 2);
     prefer_max_shared_carveout(pack_blocks_kernel<SLOTS, LAYERS>);
-    pack_blocks_kernel<SLOTS, LAYERS><<<dim3((unsigned)grid, (unsigned)n_layers), kPackWarps * 32, 0, (cudaStream_t)stream>>>(
-        ly, first_block, n_blocks, dims->n_kv_heads, dims->max_blocks, max_new, src_bytes, n_cols, local_col, (uint32_t)n_items, bounds());
-    return check_launch(who);
+    const cudaError_t e = launch_waiting(pack_blocks_kernel<SLOTS, LAYERS>, dim3((unsigned)grid, (unsigned)n_layers), kPackWarps * 32, (cudaStream_t)stream, ly,
+                                         first_block, n_blocks, (int)dims->n_kv_heads, (int)dims->max_blocks, max_new, src_bytes, n_cols, local_col,
+                                         (uint32_t)n_items, bounds());
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return fail(OASIS_ERR_CUDA, "%s: launch: %s", who, cudaGetErrorString(e));
+    }
+    return OASIS_OK;
 }
 
 }  // namespace oasis
@@ -339,7 +346,11 @@ extern "C" int oasis_unpack_blocks(const void *packed, const int64_t *idx, int32
     if (!packed || !idx || !out) return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);
     if (!aligned16(packed) || !aligned16(out)) return fail(OASIS_ERR_INVALID_ARG, "%s: packed and out must be 16-byte aligned", who);
     prefer_max_shared_carveout(unpack_blocks_kernel);
-    unpack_blocks_kernel<<<(n - 1) / kPackWarps + 1, kPackWarps * 32, 0, (cudaStream_t)stream>>>(
-        (const uint8_t *)packed, (const long long *)idx, n, (uint8_t *)out, bounds());
-    return check_launch(who);
+    const cudaError_t e = launch_waiting(unpack_blocks_kernel, dim3((unsigned)((n - 1) / kPackWarps + 1)), kPackWarps * 32, (cudaStream_t)stream,
+                                         (const uint8_t *)packed, (const long long *)idx, (int)n, (uint8_t *)out, bounds());
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return fail(OASIS_ERR_CUDA, "%s: launch: %s", who, cudaGetErrorString(e));
+    }
+    return OASIS_OK;
 }

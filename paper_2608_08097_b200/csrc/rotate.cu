@@ -83,6 +83,7 @@ rotate_qkv_kernel(const RotateParams p)
             }
         }
     };
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     load(0, worker);
     if (p.parent) {
         // how many ancestors: every node's parent in place of itself, six doublings; a warp per token
@@ -233,7 +234,8 @@ extern "C" int oasis_rotate_qkv(const oasis_dims_t *dims, const void *qkv, int32
     p.tokens_per_block = (int)(per < 1 ? 1 : per > kRotMaxTokens ? kRotMaxTokens : per);
     const unsigned grid = (unsigned)((total + p.tokens_per_block - 1) / p.tokens_per_block);
     const int mode = interleaved ? kSideBySide : rot_dim % 16 == 0 ? kHalves : kOddHalves;
-#define OASIS_ROTATE(TY, MO) rotate_qkv_kernel<TY, MO><<<grid, kRotThreads, 0, (cudaStream_t)stream>>>(p)
+    cudaError_t e;
+#define OASIS_ROTATE(TY, MO) e = launch_waiting(rotate_qkv_kernel<TY, MO>, dim3(grid), kRotThreads, (cudaStream_t)stream, p)
 #define OASIS_ROTATE_MODE(TY)                                                                                                 \
     do {                                                                                                                      \
         if (mode == kSideBySide) OASIS_ROTATE(TY, kSideBySide);                                                               \
@@ -245,5 +247,9 @@ extern "C" int oasis_rotate_qkv(const oasis_dims_t *dims, const void *qkv, int32
     else OASIS_ROTATE_MODE(OASIS_F16);
 #undef OASIS_ROTATE_MODE
 #undef OASIS_ROTATE
-    return check_launch(who);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return fail(OASIS_ERR_CUDA, "%s: launch: %s", who, cudaGetErrorString(e));
+    }
+    return OASIS_OK;
 }
