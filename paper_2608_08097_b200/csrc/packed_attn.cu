@@ -507,21 +507,29 @@ packed_attn_kernel(const PackedAttnParams p)
             // V^T P of the tile before has read its weights, and O is complete up to it
             if (i > 0) alive = alive && mbar_wait_warp(bar_o(i - 1), par_2(i - 1), p.err, 86);
             if (raise) {
-                int *const w_max = reinterpret_cast<int *>(p_ptr);       // [4][N]: P is written later
-#pragma unroll
+                // the columns' maxima over the warp's tokens: half of the values change hands in every round
+                float *const w_max = reinterpret_cast<float *>(p_ptr);   // [4][N]: P is written later
+#pragma unroll 1                                                         // (a rare path: unrolled, it costs the loop registers)
                 for (int c = 0; c < NC / 16; ++c) {
                     read(c);
 #pragma unroll
-                    for (int n = 0; n < 16; ++n) {
-                        const int m = __reduce_max_sync(0xffffffffu, ordered(x[n]));
-                        if (lane == 0) w_max[(warp & 3) * N + n0 + c * 16 + n] = m;
+                    for (int w = 8; w >= 1; w >>= 1) {
+                        const bool up = lane & w;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (k < w) {
+                                const float give = up ? x[k] : x[k + w], keep = up ? x[k + w] : x[k];
+                                x[k] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, w));
+                            }
                     }
+                    const float m = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], 16));
+                    if (lane < 16) w_max[(warp & 3) * N + n0 + c * 16 + lane] = m;
                 }
                 pa_sync<SOFT>();
                 const int n = tid - 32 * SOFT0;
                 if (n < N) {
                     const float m_old = -neg_m[n];
-                    const float mx = unordered(max(max(w_max[n], w_max[N + n]), max(w_max[2 * N + n], w_max[3 * N + n]))) * scale;
+                    const float mx = fmaxf(fmaxf(w_max[n], w_max[N + n]), fmaxf(w_max[2 * N + n], w_max[3 * N + n])) * scale;
                     const float m_new = fmaxf(m_old, mx);
                     neg_m[n] = -m_new;
                     l_sm[n] = m_new == -CUDART_INF_F ? 1.f : fast_exp2(m_old - m_new);
@@ -531,7 +539,7 @@ packed_attn_kernel(const PackedAttnParams p)
                 for (int k = 0; k < NC / 2; ++k) l2[k] = fma_f32x2(l2[k], f32x2(l_sm[n0 + 2 * k], l_sm[n0 + 2 * k + 1]), 0);
                 if (i > 0) {
                     tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < NC / 16; ++c) {
                         uint32_t v[16];
                         tc_ld16(t_o + n0 + lane_base + c * 16, v);
