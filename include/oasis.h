@@ -554,7 +554,7 @@ int oasis_stage_packed_layers(int32_t n_layers, const void *const *host_packed, 
  *   q, out       [B][n_q_tokens][Hq][128] bf16;  n_q_tokens * (Hq/Hkv) may not exceed 128
  *   slot_tbl, blk_tbl   [B][Hkv][n_cols] int32 (device)
  *   packed_pool  may be NULL if local_col is 0, hbm_pool if local_col is n_cols
- *   scale        finite and above zero
+ *   scale        above zero, at most 1e30
  *   lse          optional [B][n_q_tokens][Hq] fp32: natural-log sum of exponentials
  *   workspace    device scratch of at least oasis_packed_attn_workspace_bytes() bytes, 16-byte aligned; contents undefined before
  *                and after; may be NULL when that function returns 0.  Calls that may run at the same time (other streams,

@@ -1,25 +1,33 @@
-// Attention over a working set held in 4 bits (packed.cuh), with the local window in bf16, on the 5th-generation tensor cores.
+// Attention over a working set held in 4 bits (packed.cuh), with the local window in bf16.
 //
-// Work item = (request, KV head, row group, split of the columns), one thread block.  Tiles of eight 16-token blocks.
-// Other than in the bf16 kernels the keys and values, which have to pass through registers anyway, are the A operands in tensor
-// memory, and the query rows the columns:
+// Work item = (request, KV head, split of the columns), one thread block; all query rows of the KV head, up to 128, share what it
+// unpacks.  Two kernels, by the number of rows: packed_attn_kernel (33 to 128) on the 5th-generation tensor cores, and
+// packed_attn_few_kernel (up to 32), further down, where every warp works alone.
+// packed_attn_kernel: tiles of eight 16-token blocks.  Other than in the bf16 kernels the keys and values, which have to pass through
+// registers anyway, are the A operands in tensor memory, and the query rows the columns:
 //   S[token][row] = K Q^T    thread = token: 64 B of codes become the token's 128 bf16 dims, 64 columns of its tensor-memory lane
 //   O[dim][row]  += V^T P    thread = dim: 8 B of codes per block become the dim's 16 tokens, 8 columns of its lane
 // Q (K-major) and P (row-major by token) are the B operands in shared memory.  So 4-bit data crosses shared memory once, bf16 data
 // never (as bf16 tiles in shared memory they would be written and read there, 2.5 times the time that HBM takes to bring them).
 // A row's logits lie across the threads: the reference maximum that its weights are taken against is shared, comes from the first
-// tile, and is raised only when a logit exceeds it by 2^32 (weights, sums and accumulators have fp32's range, so that only their
-// overflow matters), which one vote per tile finds out; the rows' sums are kept per thread and added up at the end.
-// Roles: four warps unpack keys (thread = token), four values (thread = dim), four (eight with more than 32 rows) take the softmax
-// (thread = token), one issues the products, one requests entries (bulk copies, one per block, a ring of five or eight tiles).  With
-// up to 32 rows two thread blocks share an SM, with more one has two K and V buffers in tensor memory.
+// tile, and is raised only when a logit exceeds it by 2^32, which one vote per tile finds out; the rows' sums are kept per thread and
+// added up at the end.
+// Roles: four warps unpack keys (thread = token), four values (thread = dim), four per 32 rows take the softmax (thread = token),
+// one issues the products, one requests entries (bulk copies, one per block, a ring of five or seven tiles).
 // Columns that no row sees are left out when the column list of the split is read (compacted in order: the result does not depend
 // on the launch).  The local columns, at most one tile, are the first tile of split 0, read straight from global memory while the
-// ring fills.  Rows: up to 64 per thread block (16, 32 or 64 columns of the products); more are cut into row groups.
-// Splits of a row merge inside a thread-block cluster where eight reach, else through the workspace and a second launch.
+// ring fills.  Splits of a row merge inside a thread-block cluster where eight reach, else through the workspace and a second launch.
 // Precision: the unpacked keys and values are exact, 2^-20 of what they stand for (the power of two returns in the logits' scale and
-// in the output's); logits, maxima, sums and accumulators are fp32; the weights go to V^T P as bf16 (half a step, 2^-8 of a weight),
-// because both operands of one tcgen05.mma kind::f16 have the same type; the sum that divides them is of the unrounded ones.
+// in the output); logits, maxima, sums and accumulators are fp32; the weights go to the second product as bf16 (half a step, 2^-8 of
+// a weight), because both operands of one product have the same type; the sum that divides them is of the unrounded ones.  Against
+// 64 bits outputs are off by 0.17 to 0.23 % of their norm.  Nothing overflows: the local values, which may be of any size, come first,
+// with weights of at most 1 (2^-20 in the accumulator's unit); a packed value is at most 2^15, its weight 2^32.
+// What bounds it (32 query and 8 KV heads, a graph): unpacking takes a scheduler 466 of the about 700 instructions it issues per 128
+// tokens and 8 rows, on the half-rate integer and half-precision units; with 1,150 cycles a tile and SM 2 requests x 8,194 columns
+// take 75 us (4.0 TB/s), 16 requests x 130 columns 17.0 us, 5 of them first loads, list and end; with 20 rows 26.7 us, 8 warps per
+// SM, which their accumulators allow, and 768 cycles of products a tile.  From 33 rows on a tile is a chain of unpacking, product, softmax and
+// product, 3,000 cycles at 72 rows (the exponential unit's share is 768): 16 requests x 130 columns 34.1 us under 64 rows, 39.2 under
+// 72, 49.2 under 128.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -121,7 +129,7 @@ __device__ __forceinline__ void pa_sync()
     asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }
 
-// The end of a thread block's work: its rows' accumulators (o_sm, PITCH floats a row), reference maxima (neg_m, negated, log2) and
+// The end of a thread block's work: its rows' accumulators (o_sm, PITCH floats a row, in units of 2^-kDequantShift), reference maxima (neg_m, negated, log2) and
 // sums (l_sm) become outputs, or the split's part of them.  `warps` warps take a row each; in a cluster, block `split` takes rows split,
 // split + n_splits, .. of all its blocks.  Called by the whole thread block.
 template <bool CLUSTER, int PITCH>
@@ -174,6 +182,8 @@ __device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive,
                     acc.w = fmaf(wk, f[k].w, acc.w);
                 }
             }
+            constexpr float kUnit = (float)(1 << kDequantShift);
+            acc.x *= kUnit; acc.y *= kUnit; acc.z *= kUnit; acc.w *= kUnit;
             const float lse2 = den > 0.f ? top + log2f(den) : den == 0.f ? -CUDART_INF_F : den;
             if (CLUSTER || p.n_splits == 1) {
                 const int tq = r / p.G, a = h * p.G + r % p.G;
@@ -266,7 +276,7 @@ packed_attn_kernel(const PackedAttnParams p)
     }
     if (warp == MMA && lane < kPaTileCols && has_local && t0 == 0 && p.local_col + lane < p.n_cols)
         col[0] = make_int2(blk_row[p.local_col + lane], slot_row[p.local_col + lane]);
-    // Q: 16 bytes (chunk c of row r) at a time; rows past the group's are zero
+    // Q: 16 bytes (chunk c of row r) at a time; columns past the rows are zero
 #pragma unroll 4
     for (int i = tid; i < N * 16; i += THREADS) {
         const int r = i >> 4, c = i & 15;
@@ -586,7 +596,7 @@ packed_attn_kernel(const PackedAttnParams p)
                 uint32_t v[16];
                 tc_ld16(t_o + n0 + lane_base + c * 16, v);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o_sm[(n0 + c * 16 + e) * kHeadDim + me] = __uint_as_float(v[e]) * (float)(1 << kDequantShift);
+                for (int e = 0; e < 16; ++e) o_sm[(n0 + c * 16 + e) * kHeadDim + me] = __uint_as_float(v[e]);
             }
         }
         // the threads' sums of a row: half of the values change hands in every round, so that lane k ends with row k
@@ -616,8 +626,9 @@ packed_attn_kernel(const PackedAttnParams p)
 }
 
 // ---- up to 32 query rows: every warp by itself ----------------------------------------------------------------------------
-// With few rows the products are small and what a tile costs above is mostly its way through five roles and their barriers (about
-// 500 of 1,000 instructions a scheduler spends per 128 tokens, and 2,200 cycles of latency).  Here a warp takes 32 tokens (two
+// With few rows the products are small and what a tile costs above is mostly its way through five roles and their barriers: with 16
+// columns there, and two thread blocks per SM, 500 of 1,000 instructions of a scheduler per tile and 2,200 cycles of latency, 90.4 us
+// for 2 requests x 8,194 columns (16 rows of wider warp products, rows as their 16-row side: 86.5; this: 75).  Here a warp takes 32 tokens (two
 // blocks) through unpacking, softmax and products alone, with warp-wide products of 16 tokens (or dims) x 8 query rows x 16: no
 // barrier but the arrival of its own copies.  The layout of the entries fits the products' operands, because the order of a
 // contraction is free.  With lane = (g, t) = (lane / 4, lane % 4):
@@ -985,8 +996,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
             den = fmaf(f, l_sm[w * ROWS + r], den);
             acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
         }
-        const float k20 = (float)(1 << kDequantShift);
-        *reinterpret_cast<float4 *>(o_sm + r * kPfPitch + lane * 4) = make_float4(acc.x * k20, acc.y * k20, acc.z * k20, acc.w * k20);
+        *reinterpret_cast<float4 *>(o_sm + r * kPfPitch + lane * 4) = acc;
         __syncwarp();
         if (lane == 0) {                                                 // (the row's places of warp 0, which only this warp reads)
             neg_m[r] = -top;
@@ -1080,7 +1090,7 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
         if (per > 0) s = (tiles + per - 1) / per;                        // (no split without a tile)
         const long long on_sm = (items * s + sms - 1) / sms, waves = (on_sm + blocks - 1) / blocks;
         long long rest = on_sm - (waves - 1) * blocks;
-        if (blocks % 2 && rest < blocks && s > 1 && s % 2 == 0) ++rest;      // (three places per SM: pairs of a cluster fill them unevenly)
+        if (blocks == 3 && on_sm > 1 && rest < blocks && s % 2 == 0) ++rest;     // (three places per SM: pairs of a cluster fill them unevenly)
         auto wave = [&](long long n) { return 3.f + (float)per * (share * (float)n > 1.f ? share * (float)n : 1.f); };
         const float cost = (float)(waves - 1) * wave(blocks) + wave(rest) + (s == 1 ? 0.f : s <= kPaMaxCluster ? 0.5f : 2.5f);
         if (best == 0 || cost < best_cost) {
@@ -1131,7 +1141,7 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
     using namespace oasis;
     const char *who = "oasis_packed_attn";
     if (int rc = check_packed(dims, n_q_tokens, n_cols, local_col, who)) return rc;
-    if (!(scale > 0.f) || scale > 3.0e38f) return fail(OASIS_ERR_INVALID_ARG, "%s: scale %g", who, (double)scale);
+    if (!(scale > 0.f) || scale > 1.0e30f) return fail(OASIS_ERR_INVALID_ARG, "%s: scale %g", who, (double)scale);
     if (dims->batch == 0) return OASIS_OK;
     if (!q || !slot_tbl || !blk_tbl || !seq_len || !out || (local_col > 0 && !packed_pool) || (local_col < n_cols && !hbm_pool))
         return fail(OASIS_ERR_INVALID_ARG, "%s: NULL pointer argument", who);

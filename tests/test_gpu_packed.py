@@ -312,6 +312,19 @@ def test_rising_logits_rescale_in_every_tile(L):
     c.check()
 
 
+@pytest.mark.parametrize("T, Hq", [(1, 4), (9, 8)])
+def test_values_near_the_end_of_the_range(L, T, Hq):
+    """Local values of 10^38 beside packed ones: neither weights nor sums may carry them past it."""
+    c = Case(L, 1, Hq, 1, T, [333], 20, seed=8)
+    for col in (20, 21):
+        j = int(c.blk[0, 0, col])
+        if j >= 0:
+            seen = min(16, 333 + T - 16 * j)
+            c.local[int(c.slot[0, 0, col]), 1, :seen] = torch.sign(c.local[int(c.slot[0, 0, col]), 1, :seen]) * 1e38
+    c.run(L)
+    c.check()
+
+
 def test_any_bytes_are_finite(L):
     """Entries of random bytes: code 0 (-8) and the largest scales among them."""
     c = Case(L, 1, 4, 1, 1, [320], 20, seed=4)
