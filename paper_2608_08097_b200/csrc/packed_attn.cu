@@ -823,12 +823,15 @@ packed_attn_few_kernel(const PackedAttnParams p)
             }
     };
     // S^T of four tokens per lane: tokens 0, 1 are rows g, g + 8 of the first product, 2, 3 of the second.
-    float acc[NT][2][4];
+    constexpr int KS = NT == 1 ? 2 : 1;                                  // two accumulators where there are few products: shorter chains
+    float acc[KS][NT][2][4];
     auto clear = [&]() {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[nt][0][e] = acc[nt][1][e] = 0.f;
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][nt][0][e] = acc[i][nt][1][e] = 0.f;
     };
     auto logits = [&]() {
 #pragma unroll
@@ -836,7 +839,11 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) s[nt][j][e] = acc[nt][j >> 1][2 * (j & 1) + e];
+                for (int e = 0; e < 2; ++e) {
+                    s[nt][j][e] = acc[0][nt][j >> 1][2 * (j & 1) + e];
+#pragma unroll
+                    for (int i = 1; i < KS; ++i) s[nt][j][e] += acc[i][nt][j >> 1][2 * (j & 1) + e];
+                }
     };
 
     // ---- the local columns: unit k of two blocks is warp 3 - k's, straight from global memory
@@ -859,8 +866,8 @@ packed_attn_few_kernel(const PackedAttnParams p)
                 const uint4 q = q_frag[(nt * 4 + k) * 32 + lane];
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    mma_16x8x16(acc[nt][m], w[2 * m].x, w[2 * m + 1].x, w[2 * m].y, w[2 * m + 1].y, q.x, q.y);
-                    mma_16x8x16(acc[nt][m], w[2 * m].z, w[2 * m + 1].z, w[2 * m].w, w[2 * m + 1].w, q.z, q.w);
+                    mma_16x8x16(acc[0][nt][m], w[2 * m].x, w[2 * m + 1].x, w[2 * m].y, w[2 * m + 1].y, q.x, q.y);
+                    mma_16x8x16(acc[0][nt][m], w[2 * m].z, w[2 * m + 1].z, w[2 * m].w, w[2 * m + 1].w, q.z, q.w);
                 }
             }
         }
@@ -920,10 +927,9 @@ packed_attn_few_kernel(const PackedAttnParams p)
                     for (int nt = 0; nt < NT; ++nt) {
                         const uint4 q = q_frag[(nt * 4 + half * 2 + u) * 32 + lane];
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            mma_16x8x16(acc[nt][m], v[2 * m][0], v[2 * m + 1][0], v[2 * m][1], v[2 * m + 1][1], q.x, q.y);
-                            mma_16x8x16(acc[nt][m], v[2 * m][2], v[2 * m + 1][2], v[2 * m][3], v[2 * m + 1][3], q.z, q.w);
-                        }
+                        for (int m = 0; m < 2; ++m) mma_16x8x16(acc[(2 * u) % KS][nt][m], v[2 * m][0], v[2 * m + 1][0], v[2 * m][1], v[2 * m + 1][1], q.x, q.y);
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) mma_16x8x16(acc[(2 * u + 1) % KS][nt][m], v[2 * m][2], v[2 * m + 1][2], v[2 * m][3], v[2 * m + 1][3], q.z, q.w);
                     }
                 }
             }
@@ -935,18 +941,25 @@ packed_attn_few_kernel(const PackedAttnParams p)
         {
             const uint8_t *const ent = stage + (t >> 1) * kPackedBytes;
 #pragma unroll
-            for (int m = 0; m < 8; ++m) {                                // dims 16 m + g, + 8
-                uint32_t v[2][4];
+            for (int m2 = 0; m2 < 8; m2 += 2) {                          // dims 16 m + g, + 8
+                uint32_t v[2][2][4];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int dim = 16 * m + 8 * u + g;
-                    const uint32_t w = *reinterpret_cast<const uint32_t *>(ent + kPackedV + 8 * dim + 4 * (t & 1));
-                    dequant_word(w, dequant_scale(ent[kPackedVScale + dim] * 0x00010001u), v[u]);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int dim = 16 * (m2 + i) + 8 * u + g;
+                        const uint32_t w = *reinterpret_cast<const uint32_t *>(ent + kPackedV + 8 * dim + 4 * (t & 1));
+                        dequant_word(w, dequant_scale(ent[kPackedVScale + dim] * 0x00010001u), v[i][u]);
+                    }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) mma_16x8x16(o[nt][m2 + i], v[i][0][0], v[i][1][0], v[i][0][1], v[i][1][1], pw[nt][0], pw[nt][1]);
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    mma_16x8x16(o[nt][m], v[0][0], v[1][0], v[0][1], v[1][1], pw[nt][0], pw[nt][1]);
-                    mma_16x8x16(o[nt][m], v[0][2], v[1][2], v[0][3], v[1][3], pw[nt][2], pw[nt][3]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) mma_16x8x16(o[nt][m2 + i], v[i][0][2], v[i][1][2], v[i][0][3], v[i][1][3], pw[nt][2], pw[nt][3]);
                 }
             }
         }
