@@ -23,11 +23,11 @@
 // 64 bits outputs are off by 0.17 to 0.23 % of their norm.  Nothing overflows: the local values, which may be of any size, come first,
 // with weights of at most 1 (2^-20 in the accumulator's unit); a packed value is at most 2^15, its weight 2^32.
 // What bounds it (32 query and 8 KV heads, a graph): unpacking takes a scheduler 466 of the about 700 instructions it issues per 128
-// tokens and 8 rows, on the half-rate integer and half-precision units; with 1,150 cycles a tile and SM 2 requests x 8,194 columns
-// take 75 us (4.0 TB/s), 16 requests x 130 columns 17.0 us, 5 of them first loads, list and end; with 20 rows 26.7 us, 8 warps per
-// SM, which their accumulators allow, and 768 cycles of products a tile.  From 33 rows on a tile is a chain of unpacking, product, softmax and
-// product, 3,000 cycles at 72 rows (the exponential unit's share is 768): 16 requests x 130 columns 34.1 us under 64 rows, 39.2 under
-// 72, 49.2 under 128.
+// tokens and 8 rows, on the half-rate integer and half-precision units; with 1,100 cycles a tile and SM 2 requests x 8,194 columns
+// take 71.3 us (4.2 TB/s), 16 requests x 130 columns 16.6 us, 5 of them first loads, list and end; with 20 rows 26.4 us, 8 warps per
+// SM, which their accumulators allow, and 768 cycles of products a tile.  From 33 rows on a tile is a chain of unpacking, product,
+// softmax and product, 3,000 cycles at 72 rows (the exponential unit's share is 768): 16 requests x 130 columns 34.2 us under 64
+// rows, 39.0 under 72, 49.4 under 128.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -628,14 +628,16 @@ packed_attn_kernel(const PackedAttnParams p)
 // ---- up to 32 query rows: every warp by itself ----------------------------------------------------------------------------
 // With few rows the products are small and what a tile costs above is mostly its way through five roles and their barriers: with 16
 // columns there, and two thread blocks per SM, 500 of 1,000 instructions of a scheduler per tile and 2,200 cycles of latency, 90.4 us
-// for 2 requests x 8,194 columns (16 rows of wider warp products, rows as their 16-row side: 86.5; this: 75).  Here a warp takes 32 tokens (two
+// for 2 requests x 8,194 columns (16 rows of wider warp products, rows as their 16-row side: 86.5; this: 71.3).  Here a warp takes 32 tokens (two
 // blocks) through unpacking, softmax and products alone, with warp-wide products of 16 tokens (or dims) x 8 query rows x 16: no
 // barrier but the arrival of its own copies.  The layout of the entries fits the products' operands, because the order of a
 // contraction is free.  With lane = (g, t) = (lane / 4, lane % 4):
 //   S^T = K Q^T   the lane brings 32 dims, chunk t, of token 8 (t' & 1) + 2 j + e of block t' >> 1, g = 2 t' + e, for j = 0 .. 3
 //   O^T += V^T P^T   the lane brings a 32-bit word, tokens 8 (t & 1) .. + 7 of block t >> 1, of dims 16 m + g and + 8
 // so that the weights, transposed 8 x 8 (one instruction), are in the order of the words: tokens 2 j and 2 j + 1 of word t.
-// NT: products of 8 query rows.
+// Consecutive products go to different accumulators, and with 8 rows the logits have two sets: 75.5 us with one chain after the other.
+// NT: products of 8 query rows.  Against it at the change-over, 2 requests x 4,098 columns: 32 rows 83.8 us here, 33 to 64 there 87;
+// 40 rows in two thread blocks of 20 here 119.
 constexpr int kPfThreads = 128, kPfWarps = 4;
 constexpr int kPfListCols = 768;                                         // columns of a split at most
 constexpr int kPfUnitBytes = 2 * kPackedBytes;
@@ -1089,9 +1091,10 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
     // first loads and its end, then its tiles, slower by 0.7 for every thread block beyond the first that shares the SM; a wave of them
     // after the other; 0.5 for a merge in a cluster, 2.5 through the workspace.  Candidates: what a cluster holds, and what fills the
     // SMs with one, two, .. thread blocks.  Measured against it, in a graph, one token, 32 query and 8 KV heads (splits: us):
-    //   16 requests x 130 columns  1: 20.7  2: 17.3  3: 18.9  4: 17.3  6: 22.9      40 requests  1: 40.8  2: 39.3  3: 35.7  4: 44.1
-    // 16 requests x 130 columns, 4 tokens (three thread blocks per SM)  1: 25.9  2: 26.1  3: 20.9  4: 33.1
-    //    1 request  x 130 columns  4: 9.0  6: 7.3  8: 7.3  18: 8.3         2 x 4,098 columns  8: 85.9  18: 45.7  27: 42.7  37: 44.6
+    //   16 requests x 130 columns  1: 19.5  2: 16.7  3: 18.3  4: 17.0  6: 22.2      40 requests  1: 38.6  2: 37.4  3: 34.3  4: 42.1
+    //   1 request x 130 columns  1: 17.5  4: 8.8  6: 7.2  8: 7.1  9: 9.2            2 x 4,098 columns  8: 81.1  18: 44.5  27: 42.7  37: 43.1
+    //   16 requests x 130 columns, 4 tokens (three thread blocks per SM)  1: 26.2  2: 26.0  3: 20.8  4: 33.1
+    //   5 tokens (two)  1: 30.6  2: 26.4  3: 38.2     72 rows (one)  1: 39.0  2: 59.5
     const float share = few ? 0.7f : 1.f;
     long long best = 0;
     float best_cost = 0.f;

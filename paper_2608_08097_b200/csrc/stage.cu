@@ -80,6 +80,8 @@ stage_blocks_layers_kernel(const __grid_constant__ StageLayers ly, int n, const 
 // Packed entries (2,304 bytes = 144 16-byte units): a warp takes four list positions at a time, so that 9 KiB are in flight
 // like the 8 KiB of a bf16 entry.  Of every entry a lane moves four units; the last sixteen units of two entries fill a fifth
 // warp-wide load.  Algorithmic traffic: 2,304 B over the host link and 2,304 B written per request.
+// Measured from pinned memory, four layers of 6,144 entries: 51.0 GB/s, what the bf16 gather reaches (51.3), so 22.1 entries a
+// microsecond instead of 6.3; 768 entries of one layer 43 us (130).
 __global__ void __launch_bounds__(kStageWarps * 32)
 stage_packed_layers_kernel(const __grid_constant__ StageLayers ly, int n, const Bounds bd)
 {
