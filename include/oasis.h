@@ -509,8 +509,9 @@ int oasis_commit_kv_layers_after_select(const oasis_dims_t *dims, int32_t n_laye
  * Packs blocks j = first_block[b] .. first_block[b] + n_blocks[b] - 1 (those in [0, max_blocks)) of every request and KV head:
  * entry (src_table[b][j], h) of kv_pool -> packed entry (block_table[b][j], h).
  *   kv_pool      full-KV pool of bf16 entries (device memory, or mapped pinned host memory)
- *   src_table, block_table   [B][max_blocks] int32 (device); may be the same
- *   packed       packed full-KV pool (device memory, or mapped pinned host memory), 16-byte aligned
+ *   src_table, block_table   [B][max_blocks] int32 (device); may be the same.  No page of block_table is named twice among the
+ *                blocks that are packed (a page of src_table may be)
+ *   packed       packed full-KV pool (device memory, or mapped pinned host memory), 16-byte aligned; apart from kv_pool
  *   summaries    [B][Hkv][max_blocks][2][128] bf16 or NULL: the blocks' summaries as oasis_build_summaries makes them, from
  *                the bf16 keys
  *   max_new_blocks   host-side upper bound of n_blocks[b]; sizes the launch (blocks past it are not packed)
@@ -560,7 +561,8 @@ int oasis_stage_packed_layers(int32_t n_layers, const void *const *host_packed, 
  *                and after; may be NULL when that function returns 0.  Calls that may run at the same time (other streams,
  *                captured graphs that are replayed together) need a workspace each.
  * A query row that sees no key yields zeros (lse = -inf).  Positions that no token of the request sees may hold anything,
- * infinities and NaN included; every visible row of a bf16 entry must be finite (a packed entry always is).
+ * infinities and NaN included; every visible row of a bf16 entry must be finite (a packed entry always is), and so must the
+ * logits be in fp32.
  * A launch of this call lets the next launch of the stream start early (see oasis_attn_and_score).
  */
 #define OASIS_MAX_LOCAL_COLS 8

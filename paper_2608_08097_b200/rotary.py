@@ -10,6 +10,9 @@ import torch
 def _yarn(rot_dim, base, factor, trained, beta_fast=32.0, beta_slow=1.0, attention_factor=None):
     """Frequencies that turn less than beta_slow times over the trained positions are divided by `factor`, those that turn more than
     beta_fast times stay, with a linear ramp over the dims between; cos and sin grow by 0.1 ln(factor) + 1."""
+    if not beta_fast > beta_slow > 0:
+        raise ValueError("scaling 'yarn': beta_fast above beta_slow above zero")
+
     def dim_of(turns):
         return rot_dim * math.log(trained / (turns * 2 * math.pi)) / (2 * math.log(base))
 
@@ -24,6 +27,8 @@ def _yarn(rot_dim, base, factor, trained, beta_fast=32.0, beta_slow=1.0, attenti
 def _bands(rot_dim, base, factor, trained, low_freq_factor=1.0, high_freq_factor=4.0):
     """Wavelengths longer than trained / low_freq_factor are stretched by `factor`, those shorter than trained / high_freq_factor
     stay, and between them the two are blended."""
+    if not high_freq_factor > low_freq_factor > 0:
+        raise ValueError("scaling 'bands': high_freq_factor above low_freq_factor above zero")
     f = _plain(rot_dim, base)
     turns = trained * f / (2 * math.pi)                          # over the trained positions
     blend = ((turns - low_freq_factor) / (high_freq_factor - low_freq_factor)).clamp(0, 1)

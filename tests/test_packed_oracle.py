@@ -128,6 +128,14 @@ def test_frequency_tables():
             RotaryTable(device="cpu", **bad)
 
 
+def test_frequency_bands_must_be_in_order():
+    from paper_2608_08097_b200.rotary import RotaryTable
+    for kw in (dict(kind="bands", low_freq_factor=4.0, high_freq_factor=4.0), dict(kind="bands", low_freq_factor=0.0), dict(kind="bands", high_freq_factor=0.5),
+               dict(kind="yarn", beta_fast=1.0), dict(kind="yarn", beta_slow=0.0), dict(kind="yarn", beta_fast=float("nan"))):
+        with pytest.raises(ValueError):
+            RotaryTable(64, scaling=dict(kw, factor=4.0, trained=8192), device="cpu")
+
+
 def test_the_c_abi_refuses_without_a_gpu(L):
     lib, null, one, odd = L.lib(), ctypes.c_void_p(0), ctypes.c_void_p(4096), ctypes.c_void_p(4104)
     d = ctypes.byref(L.Dims(2, 32, 8, 64).c())
