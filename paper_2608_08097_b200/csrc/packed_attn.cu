@@ -129,9 +129,9 @@ __device__ __forceinline__ void pa_sync()
     asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }
 
-// The end of a thread block's work: its rows' accumulators (o_sm, PITCH floats a row, in units of 2^-kDequantShift), reference maxima (neg_m, negated, log2) and
-// sums (l_sm) become outputs, or the split's part of them.  `warps` warps take a row each; in a cluster, block `split` takes rows split,
-// split + n_splits, .. of all its blocks.  Called by the whole thread block.
+// The end of a thread block's work: its rows' accumulators (o_sm, PITCH floats a row, in units of 2^-kDequantShift), reference maxima
+// (neg_m, negated, log2) and sums (l_sm) become outputs, or the split's part of them.  `warps` warps take a row each; in a cluster,
+// block `split` takes rows split, split + n_splits, .. of all its blocks.  Called by the whole thread block.
 template <bool CLUSTER, int PITCH>
 __device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive, int warp, int warps, int lane, int split, int rows, int b, int h,
                                           const float *o_sm, const float *neg_m, const float *l_sm)
@@ -170,7 +170,7 @@ __device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive,
 #pragma unroll
             for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
             den = __shfl_sync(0xffffffffu, den, 0);
-            w *= den > 0.f ? 1.f / den : 0.f;
+            w *= den == 0.f ? 0.f : 1.f / den;                           // (a query with NaN: NaN)
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < (CLUSTER ? kPaMaxCluster : 1); ++k) {
@@ -184,7 +184,7 @@ __device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive,
             }
             constexpr float kUnit = (float)(1 << kDequantShift);
             acc.x *= kUnit; acc.y *= kUnit; acc.z *= kUnit; acc.w *= kUnit;
-            const float lse2 = den > 0.f ? top + log2f(den) : den == 0.f ? -CUDART_INF_F : den;
+            const float lse2 = den == 0.f ? -CUDART_INF_F : top + log2f(den);
             if (CLUSTER || p.n_splits == 1) {
                 const int tq = r / p.G, a = h * p.G + r % p.G;
                 const long long o = ((long long)b * p.T + tq) * p.Hq + a;
@@ -1035,12 +1035,18 @@ packed_combine_kernel(const PackedAttnParams p, int total)
     const int tq = row / p.G, a = h * p.G + row % p.G;
     const long long prow0 = (long long)bh * p.n_splits * p.R + row, pstride = p.R;      // partial row of split 0, from split to split
     float mx = -CUDART_INF_F;
-    for (int s = lane; s < p.n_splits; s += 32) mx = fmaxf(mx, p.part_lse[prow0 + s * pstride]);
+    bool nan = false;
+    for (int s = lane; s < p.n_splits; s += 32) {
+        const float v = p.part_lse[prow0 + s * pstride];
+        mx = fmaxf(mx, v);
+        nan |= v != v;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float den = 0.f;
-    if (mx > -CUDART_INF_F) {
+    if (__any_sync(0xffffffffu, nan)) mx = CUDART_NAN_F;
+    if (mx != -CUDART_INF_F) {
 #pragma unroll 1
         for (int s0 = 0; s0 < p.n_splits; s0 += 8) {
             float w[8];
@@ -1060,7 +1066,7 @@ packed_combine_kernel(const PackedAttnParams p, int total)
             }
         }
     }
-    const bool any = den > 0.f;
+    const bool any = den != 0.f;
     const float inv = any ? 1.f / den : 0.f;
     const long long orow = ((long long)b * p.T + tq) * p.Hq + a;
     reinterpret_cast<uint2 *>(p.out + orow * kRowBytes)[lane] =

@@ -383,6 +383,20 @@ def test_results_do_not_depend_on_the_run_stream_or_graph(L, B, T, budget):
         c.check()
 
 
+@pytest.mark.parametrize("B, T, Hq, lens, budget", [(2, 1, 8, [40, 700], 12), (2, 3, 8, [900, 900], 130), (1, 9, 16, [900], 56), (1, 1, 8, [9600], 600), (1, 20, 8, [40000], 2500)])
+def test_a_query_that_is_no_number_stays_alone(L, B, T, Hq, lens, budget):
+    """NaN in one query row: its output and sum are NaN, every other row is what it was."""
+    c = Case(L, B, Hq, 2, T, lens, budget, seed=T)
+    c.run(L)
+    want, want_lse = c.out.clone(), c.lse.clone()
+    c.q[B - 1, T - 1, 3, 77] = float("nan")
+    c.fresh()
+    c.run(L)
+    assert bool(c.out[B - 1, T - 1, 3].isnan().all()) and bool(c.lse[B - 1, T - 1, 3].isnan())
+    c.out[B - 1, T - 1, 3], c.lse[B - 1, T - 1, 3] = want[B - 1, T - 1, 3], want_lse[B - 1, T - 1, 3]
+    assert torch.equal(c.out, want) and torch.equal(c.lse, want_lse)
+
+
 def test_back_to_back_calls_share_a_workspace_in_order(L):
     a, b = Case(L, 1, 8, 2, 1, [9600], 600, seed=1), Case(L, 1, 8, 2, 1, [9000], 600, seed=2)
     assert a.need == b.need > 0
