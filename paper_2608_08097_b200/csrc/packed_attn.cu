@@ -18,9 +18,14 @@
 // on the launch).  The local columns, at most one tile, are the first tile of split 0, read straight from global memory while the
 // ring fills.  Splits of a row merge inside a thread-block cluster where eight reach, else through the workspace and a second launch.
 // Precision: the unpacked keys and values are exact, 2^-20 of what they stand for (the power of two returns in the logits' scale and
-// in the output); logits, maxima, sums and accumulators are fp32; the weights go to the second product as bf16 (half a step, 2^-8 of
-// a weight), because both operands of one product have the same type; the sum that divides them is of the unrounded ones.  Against
-// 64 bits outputs are off by 0.17 to 0.23 % of their norm.  Nothing overflows: the local values, which may be of any size, come first,
+// in the output); logits, maxima, sums and accumulators are fp32; both operands of a product have one type, so the weights go to the
+// second product in bf16.  Rounded once (half a step, 2^-8 of a weight) they would put an output that one key decides off by up to 2.3
+// times as much as its own rounding to bf16 does: the reference lags behind the maximum, so that key's weight is rounded like any other.
+// packed_attn_kernel multiplies them as two terms (2^-17; 27.9 -> 30.8 us for 72 rows, ragged; a reference within 2^3 of the maximum,
+// whose raises cost more: 34.3); packed_attn_few_kernel takes them once, sums them as rounded by a product with ones, and scales its
+// accumulators by the ratio of the two sums, so that the error of a key that decides cancels (71.3 -> 73.2 us for 2 requests x 8,194
+// columns).  Against 64 bits outputs are off by at most 1.21 times what the rounding of the output alone costs (0.17 % of their norm)
+// over 90 drawn shapes, 1.00 times from 33 rows on.  Nothing overflows: the local values, which may be of any size, come first,
 // with weights of at most 1 (2^-20 in the accumulator's unit); a packed value is at most 2^15, its weight 2^32.
 // What bounds it (32 query and 8 KV heads, a graph): unpacking takes a scheduler 466 of the about 700 instructions it issues per 128
 // tokens and 8 rows, on the half-rate integer and half-precision units; with 1,100 cycles a tile and SM 2 requests x 8,194 columns
@@ -50,11 +55,11 @@ __host__ __device__ constexpr int pa_k_bufs(int n) { return n == 64 ? 2 : 1; }  
 __host__ __device__ constexpr int pa_v_bufs(int n) { return n == 128 ? 1 : 2; }
 __host__ __device__ constexpr int pa_tmem_used(int n) { return 64 * (pa_k_bufs(n) + pa_v_bufs(n)) + 3 * n; }     // K | V | two S | O
 constexpr int kPaTmemCols = 512;
-// Shared memory: Q [dim half][n rows][128 B] | P [64 columns][128 tokens][128 B] | ring | column list | statistics and barriers.
+// Shared memory: Q [dim half][n rows][128 B] | two terms of P [64 columns][128 tokens][128 B] | ring | column list | statistics and barriers.
 __host__ __device__ constexpr int pa_p_bytes(int n) { return (n + 63) / 64 * kPaTileKeys * 128; }
 __host__ __device__ constexpr int pa_smem(int n)
 {
-    return 1024 + n * kRowBytes + pa_p_bytes(n) + pa_stages(n) * kPaStageBytes + kPaListCols * 8 + 2048;
+    return 1024 + n * kRowBytes + 2 * pa_p_bytes(n) + pa_stages(n) * kPaStageBytes + kPaListCols * 8 + 2048;
 }
 static_assert(pa_smem(64) <= 232448 && pa_smem(96) <= 232448 && pa_smem(128) <= 232448, "shared memory of a thread block");
 static_assert(pa_tmem_used(64) <= kPaTmemCols && pa_tmem_used(96) <= kPaTmemCols && pa_tmem_used(128) <= kPaTmemCols, "tensor memory");
@@ -217,7 +222,7 @@ packed_attn_kernel(const PackedAttnParams p)
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     uint8_t *const p_ptr = base_ptr + N * kRowBytes;
-    uint8_t *const ring = p_ptr + pa_p_bytes(N);
+    uint8_t *const ring = p_ptr + 2 * pa_p_bytes(N);
     int2 *const list = reinterpret_cast<int2 *>(ring + STAGES * kPaStageBytes);           // (block, slot)
     float *const neg_m = reinterpret_cast<float *>(list + kPaListCols);                     // [N] minus the rows' reference maxima
     float *const l_sm = neg_m + N;                                                          // [N]; while a maximum is raised: factors
@@ -352,6 +357,9 @@ packed_attn_kernel(const PackedAttnParams p)
 #pragma unroll
             for (int k = 0; k < kPaTileCols; ++k)
                 tc_mma_bf16_ts(t_o, t_v(i) + 8 * k, p_desc + (uint64_t)((k * 2048) >> 4), pa_idesc(N, true), (i > 0 || k) ? 1u : 0u);
+#pragma unroll
+            for (int k = 0; k < kPaTileCols; ++k)
+                tc_mma_bf16_ts(t_o, t_v(i) + 8 * k, p_desc + (uint64_t)((pa_p_bytes(N) + k * 2048) >> 4), pa_idesc(N, true), 1u);
             tc_commit(bar_o(i));
         };
 #pragma unroll 1
@@ -578,9 +586,18 @@ packed_attn_kernel(const PackedAttnParams p)
                     for (int n = 0; n < 16; ++n) x[n] *= 1.f / (float)(1 << kDequantShift);
                 }
 #pragma unroll
-                for (int k = 0; k < 16; k += 8)
-                    *reinterpret_cast<uint4 *>(p_ptr + pa_p_chunk(me, (n0 + c * 16 + k) / 8)) =
-                        make_uint4(pack_bf16x2(x[k], x[k + 1]), pack_bf16x2(x[k + 2], x[k + 3]), pack_bf16x2(x[k + 4], x[k + 5]), pack_bf16x2(x[k + 6], x[k + 7]));
+                for (int k = 0; k < 16; k += 8) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const float a = x[k + 2 * u], c = x[k + 2 * u + 1];
+                        hi[u] = pack_bf16x2(a, c);
+                        lo[u] = pack_bf16x2(a - __uint_as_float(hi[u] << 16), c - __uint_as_float(hi[u] & 0xffff0000u));
+                    }
+                    const uint32_t at = pa_p_chunk(me, (n0 + c * 16 + k) / 8);
+                    *reinterpret_cast<uint4 *>(p_ptr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4 *>(p_ptr + pa_p_bytes(N) + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_fence_before();
@@ -771,6 +788,9 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll
         for (int e = 0; e < 2; ++e) { m_neg[nt][e] = CUDART_INF_F; l[nt][e] = 0.f; }
     }
+    float lw[NT][4];                                                     // sums of the rounded weights (elements 0 and 1)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) lw[nt][0] = lw[nt][1] = lw[nt][2] = lw[nt][3] = 0.f;
     float s[NT][4][2];                                                   // logits of a unit: token j of this lane, rows 2 t and 2 t + 1
     uint32_t pw[NT][4];                                                  // weights of a unit, as the operand of V^T P^T
     const int kblk = g >> 2, ktok = 8 * ((g >> 1) & 1) + (g & 1);        // keys: token ktok + 2 j of block kblk
@@ -806,6 +826,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
                     const float f = m_new == -CUDART_INF_F ? 1.f : fast_exp2(-m_neg[nt][e] - m_new);
                     m_neg[nt][e] = -m_new;
                     l[nt][e] *= f;
+                    lw[nt][e] *= f;
 #pragma unroll
                     for (int m = 0; m < 8; ++m) { o[nt][m][e] *= f; o[nt][m][2 + e] *= f; }
                 }
@@ -823,6 +844,14 @@ packed_attn_few_kernel(const PackedAttnParams p)
                 l[nt][1] += c;
                 pw[nt][j] = transpose_8x8(pack_bf16x2(a * unit, c * unit));
             }
+    };
+    // One more row of V^T, of ones: the sums of the weights as the product takes them.
+    auto count_weights = [&](uint32_t one) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            mma_16x8x16(lw[nt], one, one, one, one, pw[nt][0], pw[nt][1]);
+            mma_16x8x16(lw[nt], one, one, one, one, pw[nt][2], pw[nt][3]);
+        }
     };
     // S^T of four tokens per lane: tokens 0, 1 are rows g, g + 8 of the first product, 2, 3 of the second.
     constexpr int KS = NT == 1 ? 2 : 1;                                  // two accumulators where there are few products: shorter chains
@@ -875,6 +904,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
         }
         logits();
         softmax(kl.x, true, p.scale_log2, 1.f / (float)(1 << kDequantShift));
+        count_weights(0x00010001u * ((127u + kDequantShift) << 7));
         const uint16_t *src = reinterpret_cast<const uint16_t *>(p.local + (long long)(vl.x >= 0 ? vl.y : 0) * kEntryBytes + kPartBytes) + 8 * (t & 1) * kHeadDim + g;
         const int n = vl.x >= 0 ? (int)min(8ll, max(0ll, last - ((long long)vl.x * kBlock + 8 * (t & 1)) + 1)) : 0;
 #pragma unroll
@@ -940,6 +970,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
         const bool mask = late || 2 * (warp + kPfWarps * k) + 2 > count;
         logits();
         softmax(mask ? (at < count ? list[at].x : -1) : 0, mask, scale, 1.f);
+        count_weights(0x3f803f80u);
         {
             const uint8_t *const ent = stage + (t >> 1) * kPackedBytes;
 #pragma unroll
@@ -981,14 +1012,15 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
             const int r = 8 * nt + 2 * t + e;
+            const float fit = lw[nt][e] == 0.f ? 1.f : sum / lw[nt][e];  // (the accumulators are of rounded weights)
             if (g == 0) {
                 neg_m[warp * ROWS + r] = m_neg[nt][e];
                 l_sm[warp * ROWS + r] = sum;
             }
 #pragma unroll
             for (int m = 0; m < 8; ++m) {
-                o_mine[r * kPfPitch + 16 * m + g] = o[nt][m][e];
-                o_mine[r * kPfPitch + 16 * m + g + 8] = o[nt][m][2 + e];
+                o_mine[r * kPfPitch + 16 * m + g] = o[nt][m][e] * fit;
+                o_mine[r * kPfPitch + 16 * m + g + 8] = o[nt][m][2 + e] * fit;
             }
         }
     }
