@@ -1012,7 +1012,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
             const int r = 8 * nt + 2 * t + e;
-            const float fit = lw[nt][e] == 0.f ? 1.f : sum / lw[nt][e];  // (the accumulators are of rounded weights)
+            const float fit = lw[nt][e] == 0.f ? 1.f : __fdividef(sum, lw[nt][e]);  // (the accumulators are of rounded weights)
             if (g == 0) {
                 neg_m[warp * ROWS + r] = m_neg[nt][e];
                 l_sm[warp * ROWS + r] = sum;

@@ -388,17 +388,22 @@ def test_a_key_that_decides_the_output(L, T, Hq):
     """All queries of a head look for one late key, so its value is the output: off by half a step of bf16, not by its weight's rounding.
     (The weight is no power of two: the reference comes from earlier keys.)"""
     c = Case(L, 2, Hq, 2, T, [1999, 1500], 124, seed=Hq + T)
+    key = np.zeros((2, 2, 128))
     for b in range(2):
         for h in range(2):
             at = max(j for j in range(c.budget) if 0 <= c.blk[b, h, j] and 16 * c.blk[b, h, j] + 15 <= c.lens[b])
             entry = torch.zeros(1, 2, 16, 128, dtype=torch.bfloat16, device="cuda")
             L.unpack_blocks(c.packed, torch.tensor([int(c.slot[b, h, at])], device="cuda"), entry)
-            rows = torch.linspace(2.0, 2.6, T * Hq // 2, device="cuda").view(T, Hq // 2, 1)
+            key[b, h] = f64(entry[0, 0, 5 + b])
+            rows = torch.linspace(1.5, 1.9, T * Hq // 2, device="cuda").view(T, Hq // 2, 1)
             c.q[b, :, h * Hq // 2:(h + 1) * Hq // 2] = (rows * entry[0, 0, 5 + b].float()).to(torch.bfloat16)
     c.run(L)
     out, lse, _, _ = op.attn(f64(c.q), c.packed.cpu().numpy(), np.nan_to_num(f64(c.local), nan=0.0, posinf=0.0, neginf=0.0), c.slot, c.blk, c.budget, c.lens, SCALE)
-    # half a step is 2^-8 of the value; what the other keys and fp32 add is below 2^-16 of a value (at most about 4)
-    assert np.all(np.abs(f64(c.out) - out) <= 2.0 ** -8 * np.abs(out) + 2.0 ** -14)
+    others = 1 - np.exp(SCALE * np.einsum("bthd,bhd->bth", f64(c.q), np.repeat(key, Hq // 2, axis=1)) - lse)       # their share of the weights
+    assert others.max() < 0.01
+    # half a step is 2^-8 of the value; a weight that is 2^-8 off moves the output by that times the others' share of the difference of
+    # two values (at most about 10); fp32 adds 2^-20 of a value
+    assert np.all(np.abs(f64(c.out) - out) <= 2.0 ** -8 * np.abs(out) + (2.0 ** -8 * 10 * others + 2.0 ** -17)[..., None])
     assert np.all(np.abs(f64(c.lse) - lse) <= 1e-5 * (1 + np.abs(lse)))
 
 
