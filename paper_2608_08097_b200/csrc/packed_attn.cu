@@ -23,16 +23,16 @@
 // times as much as its own rounding to bf16 does: the reference lags behind the maximum, so that key's weight is rounded like any other.
 // packed_attn_kernel multiplies them as two terms (2^-17; 27.9 -> 30.8 us for 72 rows, ragged; a reference within 2^3 of the maximum,
 // whose raises cost more: 34.3); packed_attn_few_kernel takes them once, sums them as rounded by a product with ones, and scales its
-// accumulators by the ratio of the two sums, so that the error of a key that decides cancels (71.3 -> 73.2 us for 2 requests x 8,194
+// accumulators by the ratio of the two sums, so that the error of a key that decides cancels (71.3 -> 72.9 us for 2 requests x 8,194
 // columns).  Against 64 bits outputs are off by at most 1.21 times what the rounding of the output alone costs (0.17 % of their norm)
 // over 90 drawn shapes, 1.00 times from 33 rows on.  Nothing overflows: the local values, which may be of any size, come first,
 // with weights of at most 1 (2^-20 in the accumulator's unit); a packed value is at most 2^15, its weight 2^32.
 // What bounds it (32 query and 8 KV heads, a graph): unpacking takes a scheduler 466 of the about 700 instructions it issues per 128
 // tokens and 8 rows, on the half-rate integer and half-precision units; with 1,100 cycles a tile and SM 2 requests x 8,194 columns
-// take 71.3 us (4.2 TB/s), 16 requests x 130 columns 16.6 us, 5 of them first loads, list and end; with 20 rows 26.4 us, 8 warps per
-// SM, which their accumulators allow, and 768 cycles of products a tile.  From 33 rows on a tile is a chain of unpacking, product,
-// softmax and product, 3,000 cycles at 72 rows (the exponential unit's share is 768): 16 requests x 130 columns 34.2 us under 64
-// rows, 39.0 under 72, 49.4 under 128.
+// take 72.9 us (4.1 TB/s), 16 requests x 130 columns 17.0 us, 5 of them first loads, list and end; with 20 rows 27.4 us, 8 warps per
+// SM, which their accumulators allow, and 800 cycles of products a tile.  From 33 rows on half of a tile's time is its way through
+// copies, unpacking, products and softmax and their barriers (3,500 cycles at 72 rows, of which the exponential unit is busy for 768):
+// 16 requests x 130 columns 37.1 us under 64 rows, 44.6 under 72, 56.2 under 128.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -645,16 +645,17 @@ packed_attn_kernel(const PackedAttnParams p)
 // ---- up to 32 query rows: every warp by itself ----------------------------------------------------------------------------
 // With few rows the products are small and what a tile costs above is mostly its way through five roles and their barriers: with 16
 // columns there, and two thread blocks per SM, 500 of 1,000 instructions of a scheduler per tile and 2,200 cycles of latency, 90.4 us
-// for 2 requests x 8,194 columns (16 rows of wider warp products, rows as their 16-row side: 86.5; this: 71.3).  Here a warp takes 32 tokens (two
+// for 2 requests x 8,194 columns (16 rows of wider warp products, rows as their 16-row side: 86.5; this: 72.9).  Here a warp takes 32 tokens (two
 // blocks) through unpacking, softmax and products alone, with warp-wide products of 16 tokens (or dims) x 8 query rows x 16: no
 // barrier but the arrival of its own copies.  The layout of the entries fits the products' operands, because the order of a
 // contraction is free.  With lane = (g, t) = (lane / 4, lane % 4):
 //   S^T = K Q^T   the lane brings 32 dims, chunk t, of token 8 (t' & 1) + 2 j + e of block t' >> 1, g = 2 t' + e, for j = 0 .. 3
 //   O^T += V^T P^T   the lane brings a 32-bit word, tokens 8 (t & 1) .. + 7 of block t >> 1, of dims 16 m + g and + 8
 // so that the weights, transposed 8 x 8 (one instruction), are in the order of the words: tokens 2 j and 2 j + 1 of word t.
-// Consecutive products go to different accumulators, and with 8 rows the logits have two sets: 75.5 us with one chain after the other.
-// NT: products of 8 query rows.  Against it at the change-over, 2 requests x 4,098 columns: 32 rows 83.8 us here, 33 to 64 there 87;
-// 40 rows in two thread blocks of 20 here 119.
+// Consecutive products go to different accumulators, and with 8 rows the logits have two sets (75.5 -> 71.3 us
+// before the weights were summed as rounded).
+// NT: products of 8 query rows.  Against it at the change-over, 2 requests x 4,098 columns: 32 rows 87.8 us here, 33 to 64 there 97;
+// 40 rows in two thread blocks of 20 here 119, there 83 (both with weights rounded once).
 constexpr int kPfThreads = 128, kPfWarps = 4;
 constexpr int kPfListCols = 768;                                         // columns of a split at most
 constexpr int kPfUnitBytes = 2 * kPackedBytes;
@@ -1129,10 +1130,10 @@ static PackedPlan packed_plan(const oasis_dims_t *dims, int T, int n_cols, int l
     // first loads and its end, then its tiles, slower by 0.7 for every thread block beyond the first that shares the SM; a wave of them
     // after the other; 0.5 for a merge in a cluster, 2.5 through the workspace.  Candidates: what a cluster holds, and what fills the
     // SMs with one, two, .. thread blocks.  Measured against it, in a graph, one token, 32 query and 8 KV heads (splits: us):
-    //   16 requests x 130 columns  1: 19.5  2: 16.7  3: 18.3  4: 17.0  6: 22.2      40 requests  1: 38.6  2: 37.4  3: 34.3  4: 42.1
-    //   1 request x 130 columns  1: 17.5  4: 8.8  6: 7.2  8: 7.1  9: 9.2            2 x 4,098 columns  8: 81.1  18: 44.5  27: 42.7  37: 43.1
-    //   16 requests x 130 columns, 4 tokens (three thread blocks per SM)  1: 26.2  2: 26.0  3: 20.8  4: 33.1
-    //   5 tokens (two)  1: 30.6  2: 26.4  3: 38.2     72 rows (one)  1: 39.0  2: 59.5
+    //   16 requests x 130 columns  1: 20.2  2: 17.2  3: 19.0  4: 17.5  6: 23.0      40 requests  1: 39.4  2: 38.7  3: 35.7  4: 43.3
+    //   1 request x 130 columns  1: 18.3  4: 9.0  6: 7.4  8: 7.4  9: 9.2            2 x 4,098 columns  8: 83.2  18: 46.1  27: 43.4  37: 44.6
+    //   16 requests x 130 columns, 4 tokens (three thread blocks per SM)  1: 26.8  2: 27.1  3: 22.0  4: 34.1
+    //   5 tokens (two)  1: 31.9  2: 27.4  3: 39.5     72 rows (one)  1: 44.6  2: 65.6
     const float share = few ? 0.7f : 1.f;
     long long best = 0;
     float best_cost = 0.f;
