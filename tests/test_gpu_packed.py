@@ -102,6 +102,26 @@ def test_packing_is_bounded_by_the_block_array_and_by_max_new_blocks(L):
             assert np.array_equal(got[j], op.pack(f64(pool[j, 0])))
 
 
+def test_far_entries_and_pages_read_twice(L):
+    """Entries whose offsets pass 32 bits, in both pools; one source page packed to two places, one packed entry read back twice."""
+    n, m = (1 << 32) // 8192 + 7, (1 << 32) // 2304 + 9
+    few = odd_entries(gen(2), 6)
+    pool = torch.empty((n, 1, 2, 16, 128), dtype=torch.bfloat16, device="cuda")
+    packed = torch.empty((m, 2304), dtype=torch.uint8, device="cuda")
+    pool[n - 6:, 0] = few
+    L.pack_blocks(L.Dims(1, 1, 1, 4), pool, i32([[n - 1, n - 3, n - 3, n - 5]]), i32([0]), i32([4]), 4, packed, i32([[m - 1, m - 4, 2, 0]]))
+    out = torch.zeros((4, 2, 16, 128), dtype=torch.bfloat16, device="cuda")
+    L.unpack_blocks(packed, torch.tensor([m - 1, m - 4, m - 4, 2], device="cuda"), out)
+    want = [op.pack(f64(few[k])) for k in (5, 3, 3, 1)]
+    for at, w in zip((m - 1, m - 4, 2, 0), want):
+        assert np.array_equal(packed[at].cpu().numpy(), w)
+    got = out.view(torch.int16)
+    assert torch.equal(got[1], got[2]) and torch.equal(got[1], got[3])
+    again = torch.zeros((4, 2304), dtype=torch.uint8, device="cuda")
+    L.pack_blocks(L.Dims(1, 1, 1, 4), out.view(4, 1, 2, 16, 128), i32([[0, 1, 2, 3]]), i32([0]), i32([4]), 4, again, i32([[0, 1, 2, 3]]))
+    assert [np.array_equal(op.unpack(again[k].cpu().numpy()), f64(out[k])) for k in range(4)] == [True] * 4
+
+
 @pytest.mark.parametrize("layers", [1, 3])
 def test_pack_local_takes_the_column_of_the_blocks_parity(L, layers):
     B, Hkv, cols, col, mb, g, rng = 3, 2, 7, 4, 12, gen(9), np.random.default_rng(9)
@@ -419,6 +439,34 @@ def test_a_query_that_is_no_number_stays_alone(L, B, T, Hq, lens, budget):
     assert bool(c.out[B - 1, T - 1, 3].isnan().all()) and bool(c.lse[B - 1, T - 1, 3].isnan())
     c.out[B - 1, T - 1, 3], c.lse[B - 1, T - 1, 3] = want[B - 1, T - 1, 3], want_lse[B - 1, T - 1, 3]
     assert torch.equal(c.out, want) and torch.equal(c.lse, want_lse)
+
+
+@pytest.mark.parametrize("shapes", [((1, 1, 1200), (16, 1, 130)), ((4, 9, 300), (2, 5, 600))])
+def test_two_calls_at_once(L, shapes):
+    """On two streams, and as two graphs that are replayed together, each with its own workspace."""
+    cases = [Case(L, B, 16, 2, T, [budget * 16] * B, budget, seed=budget) for B, T, budget in shapes]
+    streams, graphs, want = [torch.cuda.Stream() for _ in cases], [], []
+    for c in cases:
+        c.run(L)
+        c.check()
+        want.append((c.out.clone(), c.lse.clone()))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(4):
+                c.run(L)
+        graphs.append(g)
+    for replay in (False, True):
+        for c in cases:
+            c.out.fill_(7.0)
+            c.lse.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for c, s, g in zip(cases, streams, graphs):
+                with torch.cuda.stream(s):
+                    g.replay() if replay else c.run(L)
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            assert torch.equal(c.out, w[0]) and torch.equal(c.lse, w[1])
 
 
 def test_back_to_back_calls_share_a_workspace_in_order(L):
