@@ -59,12 +59,27 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 // ---- device helpers -----------------------------------------------------------------
 
+// 16 bytes that are read once.  This form takes the read-only path, which asks that nothing writes the bytes while the kernel is
+// resident: only for kernels that start when the launch before them has ended.
 __device__ __forceinline__ uint4 ld_stream_v4(const void *p)
 {
     uint4 v;
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                  : "l"(p));
+    return v;
+}
+
+// The same through the coherent path, for kernels that wait (griddepcontrol.wait) and may be on the SMs while the launch before them
+// still writes what they read.  (Their pointers are not __restrict__ for the same reason: it allows read-only loads as well, and lets
+// them move above the wait.)
+__device__ __forceinline__ uint4 ld_once_v4(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p)
+                 : "memory");
     return v;
 }
 

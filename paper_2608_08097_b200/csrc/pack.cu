@@ -137,7 +137,7 @@ struct PackLayers {
 // SLOTS: the source of block j is the entry of the local column that belongs to j, else of page src_table[b][j].
 template <bool SLOTS, int LAYERS>
 __global__ void __launch_bounds__(kPackWarps * 32)
-pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t *__restrict__ first_block, const int32_t *__restrict__ n_blocks,
+pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t *first_block, const int32_t *n_blocks,
                    int Hkv, int max_blocks, int max_new, int src_bytes, int n_cols, int local_col, uint32_t n_items, const Bounds bd)
 {
     __shared__ __align__(16) uint8_t sm[kPackWarps][kPackedBytes / 2];
@@ -170,7 +170,7 @@ pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t 
     uint32_t x[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint4 w = ld_stream_v4(from + i * kRowBytes);
+        const uint4 w = ld_once_v4(from + i * kRowBytes);
         x[i][0] = w.x; x[i][1] = w.y; x[i][2] = w.z; x[i][3] = w.w;
     }
     uint8_t *const entry = ly.packed[l] + dst * kPackedBytes;
@@ -199,7 +199,7 @@ pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t 
 
 // One warp per list position: the packed entry through shared memory, the bf16 entry in sixteen 16-byte stores per lane.
 __global__ void __launch_bounds__(kPackWarps * 32)
-unpack_blocks_kernel(const uint8_t *__restrict__ packed, const long long *__restrict__ idx, int n, uint8_t *__restrict__ out, const Bounds bd)
+unpack_blocks_kernel(const uint8_t *packed, const long long *idx, int n, uint8_t *out, const Bounds bd)
 {
     __shared__ __align__(16) uint8_t sm_all[kPackWarps][kPackedBytes];
     const int lane = threadIdx.x & 31, upper = lane >> 4, chunk = lane & 15;
@@ -212,7 +212,7 @@ unpack_blocks_kernel(const uint8_t *__restrict__ packed, const long long *__rest
     const uint8_t *from = packed + src * kPackedBytes;
 #pragma unroll
     for (int i = 0; i < 5; ++i)
-        if (lane + 32 * i < kPackedBytes / 16) *reinterpret_cast<uint4 *>(sm + (lane + 32 * i) * 16) = ld_stream_v4(from + (lane + 32 * i) * 16);
+        if (lane + 32 * i < kPackedBytes / 16) *reinterpret_cast<uint4 *>(sm + (lane + 32 * i) * 16) = ld_once_v4(from + (lane + 32 * i) * 16);
     __syncwarp();
     uint8_t *dst = out + item * kEntryBytes + upper * 8 * kRowBytes + chunk * 16;
     const uint32_t unit = 0x00010001u * ((127u + kDequantShift) << 7);          // (x, x) for 2^kDequantShift

@@ -80,7 +80,7 @@ rotate_qkv_kernel(const RotateParams p)
             if (a < n_rows) {
 #pragma unroll
                 for (int v = 0; v < W / 4; ++v) {
-                    const uint4 g = ld_stream_v4(src + (long long)a * kHeadDim * SIZE + v * 16);
+                    const uint4 g = ld_once_v4(src + (long long)a * kHeadDim * SIZE + v * 16);
                     w[u][4 * v] = g.x; w[u][4 * v + 1] = g.y; w[u][4 * v + 2] = g.z; w[u][4 * v + 3] = g.w;
                 }
             }
