@@ -1060,6 +1060,7 @@ __global__ void __launch_bounds__(256)
 packed_combine_kernel(const PackedAttnParams p, int total)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (behind the wait: the splits' launch is over for the next one too)
     const int lane = threadIdx.x & 31;
     const int wi = 8 * blockIdx.x + (threadIdx.x >> 5);
     if (wi >= total) return;

@@ -37,3 +37,18 @@ def test_a_kernel_that_waits_reads_nothing_through_the_read_only_path(file, name
     assert "__restrict__" not in signature
     for closed in ("ld_stream_v4", "__ldg", "ld.global.nc", "__restrict__"):
         assert closed not in body, (file, name, closed)
+
+
+@pytest.mark.parametrize("file", ["attn.cu", "attn_tc.cu", "layer_tc.cu", "tree_attn.cu", "packed_attn.cu"])
+def test_attention_launches_let_a_successor_start_early(file):
+    """As the header says of them and of their merge launches (oasis_attn_and_score)."""
+    found = [k for k in kernels() if k[0] == file]
+    assert found
+    for _, name, _, body in found:
+        assert "griddepcontrol.launch_dependents" in body, name
+
+
+def test_a_merge_of_splits_waits_before_it_lets_the_next_launch_start():
+    """What follows packed_combine_kernel may read before it waits: the splits' launch must be over by then."""
+    body = next(k[3] for k in kernels() if k[1] == "packed_combine_kernel")
+    assert body.index("griddepcontrol.wait") < body.index("griddepcontrol.launch_dependents")
