@@ -486,9 +486,7 @@ class DecodeEngine:
                             if self.packed:
                                 oasis.append_kv_layers(group[0].dims, new_kv[a0:a1], 0, seq_len, self.table[a0:a1], slot_tbls,
                                                        self.resident[a0:a1], self.k, [L.local for L in group], [None] * len(group))
-                                oasis.pack_local_layers(group[0].dims, [L.local for L in group], slot_tbls, self.k, first_block, n_new, 1,
-                                                        self.kv[a0:a1], self.table[a0:a1], [L.summaries for L in group])
-                                self.launches += 2
+                                self.launches += 1
                                 continue
                             oasis.append_kv_layers(group[0].dims, new_kv[a0:a1], self.n_commit, seq_len, self.table[a0:a1],
                                                    slot_tbls, self.resident[a0:a1], self.k, [L.pool for L in group], self.kv[a0:a1])
@@ -500,6 +498,13 @@ class DecodeEngine:
                                                          n_new, 1, [L.summaries for L in self.layers[a0:a1]])
                             self.launches += 1
                     head_ready[l0] = self._event(self.pred)
+                if self.packed:      # behind the event: the attention reads the local window, only the scoring what is written here
+                    for a0 in range(0, n, oasis.MAX_APPEND_LAYERS):
+                        group = self.layers[a0:a0 + oasis.MAX_APPEND_LAYERS]
+                        a1 = a0 + len(group)
+                        oasis.pack_local_layers(group[0].dims, [L.local for L in group], [L.slot_tbl for L in group], self.k, first_block,
+                                                n_new, 1, self.kv[a0:a1], self.table[a0:a1], [L.summaries for L in group])
+                        self.launches += 1
         pending, readies = [], []
         for l in range(n):
             L = self.layers[l]

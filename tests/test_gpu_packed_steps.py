@@ -1,0 +1,57 @@
+"""GPU tests of the engine over packed blocks beyond its smallest shape: many query rows, splits through the workspace, several steps
+in one graph, queries and outputs in pinned memory, and the order of a step's launches."""
+import pytest
+import torch
+
+from tests.packed_loop import Loop
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_08097_b200 import build
+    build.build()
+    from paper_2608_08097_b200 import binding, pipeline
+    binding.lib()
+    return binding, pipeline
+
+
+SMALL = dict(B=2, Hq=8, Hkv=2, T=3, K=6, max_blocks=16, layers=3, seq0=[100, 77], steps=8, cap=2)
+
+
+def test_the_attention_does_not_wait_for_the_packing(oracle, gpu, monkeypatch):
+    """It reads the local window; what is packed goes to the pool, over the host link as a rule, and only scoring and gathers need it."""
+    binding, pipeline = gpu
+    loop, log = Loop(oracle, pipeline, **dict(SMALL, wait_group=2)), []
+    eng, event, pack, wait = loop.eng, pipeline.DecodeEngine._event, binding.pack_local_layers, torch.cuda.Stream.wait_event
+
+    def logged_event(stream):
+        ev = event(stream)
+        log.append(("event", stream, ev))
+        return ev
+
+    def logged_pack(*a, **k):
+        log.append(("pack", torch.cuda.current_stream(), None))
+        return pack(*a, **k)
+
+    def logged_wait(stream, ev):
+        log.append(("wait", stream, ev))
+        return wait(stream, ev)
+    monkeypatch.setattr(eng, "_event", logged_event)
+    monkeypatch.setattr(binding, "pack_local_layers", logged_pack)
+    monkeypatch.setattr(torch.cuda.Stream, "wait_event", logged_wait)
+    loop.sel_log = {}
+    args, kw = loop.call(0)
+    eng.step(*args, **kw)
+    eng.join()
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    packs = [k for k, e in enumerate(log) if e[0] == "pack"]
+    assert packs and all(log[k][1] == eng.pred for k in packs)
+    from_pred = {id(e[2]): k for k, e in enumerate(log) if e[0] == "event" and e[1] == eng.pred}
+    last = max(k for k, e in enumerate(log) if e[0] == "event" and e[1] == eng.main)                 # the last attention's
+    waits = [from_pred[id(e[2])] for k, e in enumerate(log[:last]) if e[0] == "wait" and e[1] == eng.main and id(e[2]) in from_pred]
+    assert len(waits) == 2 and max(waits) < min(packs)               # one per group of layers
