@@ -163,6 +163,7 @@ pack_blocks_kernel(const __grid_constant__ PackLayers<LAYERS> ly, const int32_t 
         if (src < 0 || !in_range(src, bd.n_slots, bd, kErrSlot)) return;
     } else {
         src = (long long)ly.src_table[l][(long long)b * max_blocks + j] * Hkv + h;
+        if (src_bytes == kEntryBytes && !in_range(src, bd.n_entries, bd, kErrHostEntry)) return;     // (a dense pool's extent is not declared)
     }
     const long long dst = (long long)ly.block_table[l][(long long)b * max_blocks + j] * Hkv + h;
     if (!in_range(dst, bd.n_entries, bd, kErrHostEntry)) return;
