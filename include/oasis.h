@@ -633,7 +633,8 @@ int oasis_set_error_word(int32_t *device_word);
  * 202 slot, 203 block id, 204 block count) and the access is skipped -- the request is dropped, the column is
  * treated as missing, the count is clamped; nothing traps or asserts.  The attention's tensor map then also
  * declares the pool's real extent.  oasis_set_extents declares the two extents (process-wide, like the error
- * word; 0 = unknown = unchecked); in the regular build it is accepted and has no effect.
+ * word; 0 = unknown = unchecked); in the regular build it is accepted and has no effect.  A packed working set has two pools (packed
+ * entries and the local window): n_slots is then the larger one's.
  * oasis_bounds_checked() tells which build is loaded (1 = checked).
  */
 int oasis_set_extents(int64_t n_host_entries, int64_t n_slots);

@@ -21,7 +21,8 @@ class DecodeLayer:
     (b * Hkv + h) * (k + 2) + c, column c holding the block sel[b][h][c].
 
     kv_bits=4: the first k columns of a row are packed entries, slots (b * Hkv + h) * k + c of `pool` (uint8 [...][2304]); the
-    last two, the local window, stay bf16 entries of `local`, slot (2 b + r) * Hkv + h for column k + r.
+    last two, the local window, stay bf16 entries of `local`, slot (2 b + r) * Hkv + h for column k + r.  Such a layer is filled by a
+    transfer plan (`plan_delta`, `stage_packed_layers`): `select` makes no gather list, and `stage` is refused.
     """
 
     def __init__(self, batch, n_q_heads, n_kv_heads, max_blocks, k, n_q_tokens, device="cuda",
@@ -43,8 +44,9 @@ class DecodeLayer:
         self.summaries = torch.zeros((batch, n_kv_heads, max_blocks, 2, 128), dtype=torch.bfloat16, device=dev)
         self.scores = torch.empty((batch, n_kv_heads, max_blocks), dtype=torch.float32, device=dev)
         self.sel = torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int32, device=dev)
-        self.stage_idx = torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int64, device=dev)
-        self.stage_slots = torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int32, device=dev)
+        # the gather list that goes with the fetch-all layout
+        self.stage_idx = None if self.packed else torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int64, device=dev)
+        self.stage_slots = None if self.packed else torch.empty((batch, n_kv_heads, self.cols), dtype=torch.int32, device=dev)
         if self.packed:
             self.pool = torch.zeros((rows * k, oasis.PACKED_BYTES), dtype=torch.uint8, device=dev)
             self.local = torch.zeros((rows * 2, 2, 16, 128), dtype=torch.bfloat16, device=dev)
@@ -99,11 +101,13 @@ class DecodeLayer:
     def select(self, n_full, seq_len, block_table, stream=None, sel=None):
         oasis.select_topk(self.dims, self.scores, n_full, seq_len, self.T, self.k, block_table,
                           self.sel if sel is None else sel,
-                          self.stage_idx if sel is None else None,
+                          self.stage_idx if sel is None else None,           # (packed layers have no list)
                           self.stage_slots if sel is None else None, stream=stream)
 
     # step 3
     def stage(self, host_kv, stream=None):
+        if self.packed:
+            raise ValueError("kv_bits=4: entries are gathered by a transfer plan (plan_delta, stage_packed_layers)")
         oasis.stage_blocks(host_kv, self.stage_idx, self.stage_slots, self.stage_idx.numel(), self.pool,
                            stream=stream)
 

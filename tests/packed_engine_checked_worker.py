@@ -10,7 +10,9 @@ import torch
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 sys.path.insert(0, ROOT)
 
-from paper_2608_08097_b200 import binding  # noqa: E402
+from oracle import oracle  # noqa: E402
+from paper_2608_08097_b200 import binding, pipeline  # noqa: E402
+from tests.packed_loop import Loop  # noqa: E402
 
 HOST_ENTRY = 201
 word = torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -46,8 +48,23 @@ def source_pages():
     return got
 
 
+def engine(K, **shape):
+    """A loop over packed blocks against the oracle with the real extents declared: no check may fire."""
+    B, Hkv, blocks = 2, 2, 16
+    binding.set_extents(B * blocks * Hkv, B * Hkv * max(K, 2))
+    loop = Loop(oracle, pipeline, B=B, Hq=8, Hkv=Hkv, K=K, max_blocks=blocks, layers=2, seq0=[100, 77], steps=7, cap=1, **shape)
+    assert loop.eng.layers[0].pool.shape[0] == B * Hkv * K and loop.eng.layers[0].local.shape[0] == B * Hkv * 2
+    assert take_code() == 0, "a check fired on valid indices"
+    loop.run()
+    code = take_code()
+    binding.set_extents(0, 0)
+    return code
+
+
 assert binding.bounds_checked()
 binding.set_error_word(word)
 every = [0, 1, 2, 3, 4, 5]
 assert source_pages() == [(0, every), (0, every), (HOST_ENTRY, [0, 1, 4, 5]), (0, every)]
+oracle.lib()
+assert [engine(6, T=3), engine(1, T=2), engine(4, T=9, host=True)] == [0, 0, 0]
 print(json.dumps({"ok": True}))

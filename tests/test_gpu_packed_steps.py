@@ -55,3 +55,16 @@ def test_the_attention_does_not_wait_for_the_packing(oracle, gpu, monkeypatch):
     last = max(k for k, e in enumerate(log) if e[0] == "event" and e[1] == eng.main)                 # the last attention's
     waits = [from_pred[id(e[2])] for k, e in enumerate(log[:last]) if e[0] == "wait" and e[1] == eng.main and id(e[2]) in from_pred]
     assert len(waits) == 2 and max(waits) < min(packs)               # one per group of layers
+
+
+def test_a_packed_layer_has_no_gather_list(gpu):
+    """The slots of the top-k's list are those of a bf16 layer, k + 2 to a row."""
+    _, pipeline = gpu
+    lay = pipeline.DecodeLayer(1, 4, 1, 8, 2, 2, kv_bits=4)
+    assert lay.stage_idx is None and lay.stage_slots is None
+    lay.scores.copy_(torch.arange(8.0).view(1, 1, 8))
+    n, length, table = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([6], [100], [list(range(8))]))
+    lay.select(n, length, table)
+    assert lay.sel.flatten().tolist() == [5, 4, 6, -1]
+    with pytest.raises(ValueError, match="transfer plan"):
+        lay.stage(torch.zeros((8, 1, 2304), dtype=torch.uint8, device="cuda"))
