@@ -172,6 +172,8 @@ class DecodeEngine:
     kv_bits=4 (append engines): the full-KV pool and the working set hold packed entries of 2,304 bytes, the local window stays
     bf16.  A block is packed, and summarised from its bf16 keys, in the step that fills it (`oasis_pack_local_layers`); the pool is
     filled by `handover`, which also loads the partially filled block.  Attention (`oasis_packed_attn`) and scoring are two launches.
+    Only whole blocks reach the pool, whatever n_commit is: a step's first_block and n_new have to name the blocks that its first n_commit
+    tokens fill (later steps write over the local window).
     transfer_streams: consecutive layers' gathers alternate between this many transfer streams (useful
     when the pool is in host memory: one gather's requests are in flight while the previous one's last
     ones come back).
@@ -202,6 +204,8 @@ class DecodeEngine:
         self.packed = kv_bits == 4
         if self.packed and (not append or tree or fused or transfer_kind != "warp"):
             raise ValueError("kv_bits=4 goes with the KV append (delta mode) and chains of drafts, unfused, with transfer_kind 'warp'")
+        if self.packed and not 1 <= int(n_commit) <= n_q_tokens:
+            raise ValueError("kv_bits=4: n_commit %d outside [1, %d]" % (n_commit, n_q_tokens))
         self.tree = bool(tree)
         self.append = bool(append)
         self.transfer_ctas = int(transfer_ctas)  # thread blocks per gather launch (0: the library's default)

@@ -68,3 +68,17 @@ def test_a_packed_layer_has_no_gather_list(gpu):
     assert lay.sel.flatten().tolist() == [5, 4, 6, -1]
     with pytest.raises(ValueError, match="transfer plan"):
         lay.stage(torch.zeros((8, 1, 2304), dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("n_commit, T", [(3, 3), (2, 5), (16, 16)])
+def test_steps_that_commit_several_tokens(oracle, gpu, n_commit, T):
+    """A step adds n_commit tokens; the block that they fill is packed in that step."""
+    _, pipeline = gpu
+    Loop(oracle, pipeline, **dict(SMALL, T=T, layers=2, steps=6, n_commit=n_commit)).run(chunk=2)
+
+
+@pytest.mark.parametrize("n_commit", [0, 4, -1])
+def test_a_packed_engine_refuses_counts_that_no_step_has(gpu, n_commit):
+    _, pipeline = gpu
+    with pytest.raises(ValueError, match="n_commit"):
+        pipeline.DecodeEngine(1, 4, 1, 8, 2, 3, 1, mode="delta", cap=2, append=True, kv_bits=4, n_commit=n_commit)
