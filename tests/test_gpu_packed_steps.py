@@ -82,3 +82,34 @@ def test_a_packed_engine_refuses_counts_that_no_step_has(gpu, n_commit):
     _, pipeline = gpu
     with pytest.raises(ValueError, match="n_commit"):
         pipeline.DecodeEngine(1, 4, 1, 8, 2, 3, 1, mode="delta", cap=2, append=True, kv_bits=4, n_commit=n_commit)
+
+
+@pytest.mark.parametrize("shape", [
+    dict(B=2, Hq=16, Hkv=2, T=9, K=12, max_blocks=40, layers=2, seq0=[500, 333], steps=5, cap=3),             # 72 query rows: tensor memory
+    dict(B=1, Hq=4, Hkv=2, T=10, K=24, max_blocks=40, layers=1, seq0=[600], steps=4, cap=24),                 # 20 rows, splits in a cluster
+    dict(B=1, Hq=2, Hkv=1, T=4, K=230, max_blocks=260, layers=1, seq0=[250 * 16 + 14], steps=4, cap=20),      # splits through the workspace
+    dict(B=1, Hq=8, Hkv=1, T=8, K=230, max_blocks=260, layers=1, seq0=[250 * 16 + 14], steps=3, cap=20),      # the same with 64 rows
+])
+def test_rows_and_splits(oracle, gpu, shape):
+    _, pipeline = gpu
+    loop = Loop(oracle, pipeline, host=True, **shape)
+    assert loop.eng.layers[0].splits == (shape["K"] == 230)
+    loop.run(chunk=2)
+
+
+@pytest.mark.parametrize("graph, e2e, chunk, group, streams", [
+    (True, "stacked", 4, 2, 1), (True, "layers", 3, 1, 2), (False, "stacked", 4, 2, 2), (False, "layers", 8, 1, 1), (False, None, 8, 2, 2), (True, None, 1, 3, 1)])
+def test_several_steps_and_pinned_queries_and_outputs(oracle, gpu, graph, e2e, chunk, group, streams):
+    """No synchronisation between the steps of a chunk; blocks fill up and are gathered within it."""
+    _, pipeline = gpu
+    loop = Loop(oracle, pipeline, host=True, wait_group=group, transfer_group=group, transfer_streams=streams, **dict(SMALL, seq0=[109, 77], steps=9))
+    loop.run(chunk=chunk, graph=graph, e2e=e2e)
+
+
+def test_launches_are_counted(oracle, gpu):
+    """Two launches for the appends and packs of a step, five per layer (attention, scoring, top-k, plan, gather)."""
+    _, pipeline = gpu
+    loop = Loop(oracle, pipeline, **dict(SMALL, steps=1, wait_group=3))
+    before = loop.eng.launches
+    loop.run()
+    assert loop.eng.launches - before == 2 + 5 * 3
