@@ -635,10 +635,9 @@ def stage_packed_layers(host_packed, idx, slots, n, packed_pools, max_ctas=0, st
     for t in (*idx, *slots):
         if t.numel() < n:
             raise ValueError("the lists must have n = %d elements, got %d" % (n, t.numel()))
-    arr = ctypes.c_void_p * max(nl, 1)
-    mk = lambda ts, dt, nm: arr(*[_ptr(t, dt, nm).value for t in ts])
+    lists = lambda ts, kind, name: (ctypes.c_void_p * max(nl, 1))(*[_layer_list([t], kind, tuple(t.shape), name)[0] for t in ts])
     _check(lib().oasis_stage_packed_layers(
-        nl, _layer_list(host_packed, 4, (), "host_packed"), mk(idx, torch.int64, "idx"), mk(slots, torch.int32, "slots"), int(n),
+        nl, _layer_list(host_packed, 4, (), "host_packed"), lists(idx, 5, "idx"), lists(slots, 1, "slots"), int(n),
         _layer_list(packed_pools, 4, (), "packed_pools"), int(max_ctas), _stream(stream)), "oasis_stage_packed_layers")
 
 

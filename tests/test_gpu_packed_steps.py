@@ -113,3 +113,16 @@ def test_launches_are_counted(oracle, gpu):
     before = loop.eng.launches
     loop.run()
     assert loop.eng.launches - before == 2 + 5 * 3
+
+
+def test_the_gather_refuses_lists_in_host_memory(gpu):
+    """Its kernel reads them on the device."""
+    binding, _ = gpu
+    packed, pool = (torch.zeros((4, 2304), dtype=torch.uint8, device="cuda") for _ in range(2))
+    idx, slots = torch.tensor([1, 2], device="cuda"), torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    for i, s, e in ((idx.cpu(), slots, ValueError), (idx, slots.cpu(), ValueError), (idx.cpu().pin_memory(), slots, ValueError), (idx.int(), slots, TypeError),
+                    (idx, slots.long(), TypeError), (idx.repeat(2)[::2], slots, ValueError), (idx[:1], slots, ValueError)):
+        with pytest.raises(e):
+            binding.stage_packed_layers([packed], [i], [s], 2, [pool])
+    binding.stage_packed_layers([packed], [idx], [slots], 2, [pool])
+    binding.stage_packed_layers([], [], [], 0, [])
