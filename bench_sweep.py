@@ -1,6 +1,6 @@
 """Secondary measurements of the sparse-decode path on one B200 (not part of the `bench.py` contract).
 
-    python bench_sweep.py [--what c5,stage,shapes]
+    python bench_sweep.py [--what c5,stage,shapes,packed]
 
 Kernels alone (the whole step, every configuration and the fetch-ratio sweep are `bench.py --config / --sweep-ratios`).
 Prints one JSON line per section:
@@ -11,6 +11,9 @@ Prints one JSON line per section:
   shapes  the kernels alone at the shapes of configs[0] to configs[3] (one layer, random
           summaries and pools): scoring, top-k, attention, and the fused attention + scoring launch where
           it takes the shape, each against the measured copy peak.
+  packed  (not run by default) entries in 4 bits beside bf16 ones: the attention kernels on the same rows and columns, the hand-over
+          into a pinned pool, and the whole step of the reasoning-style decode (bench.py's default workload) by DecodeEngine with
+          kv_bits 16 and 4, with the pool in pinned memory and in HBM (--layers: fewer layers than that workload's).
 Inputs are synthetic (the generators of `synth`); nothing here touches the CPU oracle.
 """
 import argparse
@@ -210,10 +213,128 @@ def section_shapes(args, dev, hbm_peak):
                       "hbm_peak_GBps": hbm_peak, "rows": rows}))
 
 
+def attention_pair(dev, seed, batch, Hq, Hkv, T, K):
+    """us of packed_attn, sparse_attn and tree_attn (None where it does not take the rows) for one list of K whole blocks and the
+    local window, in a graph over more working sets than L2 holds."""
+    from paper_2608_08097_b200 import binding, pipeline
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    randn = lambda *s: torch.randn(s, device=dev, generator=g).to(torch.bfloat16)
+    q, seq = randn(batch, T, Hq, 128), torch.full((batch,), 16 * K, dtype=torch.int32, device=dev)
+    sel = torch.arange(K + 2, dtype=torch.int32, device=dev).repeat(batch, Hkv, 1)
+    sel[..., K + 1:] = K + 1 if T > 16 else -1
+    n_ent, got = batch * Hkv * K, []
+    one = torch.arange(n_ent, dtype=torch.int32, device=dev).view(1, -1)
+    n, zero = torch.full((1,), n_ent, dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    par = (torch.arange(T, dtype=torch.int32, device=dev) - 1).repeat(batch, 1).contiguous()
+    nodes, tree_kv = torch.full((batch,), T, dtype=torch.int32, device=dev), randn(batch, T, Hkv, 2, 128)
+    for kind in ("packed", "bf16", "tree"):
+        if kind == "tree" and T > binding.MAX_TREE:
+            got.append(None)
+            continue
+        size = n_ent * (2304 if kind == "packed" else 8192)
+        n_rot = max(2, min(16, -(-300_000_000 // size)))
+        Ls = []
+        for _ in range(n_rot):
+            L = pipeline.DecodeLayer(batch, Hq, Hkv, K + 16, K, T, dev, tree=kind == "tree", kv_bits=4 if kind == "packed" else 16)
+            if kind == "packed":
+                kv = randn(n_ent, 2, 16, 128)
+                binding.pack_blocks(binding.Dims(1, 1, 1, n_ent), kv, one, zero, n, n_ent, L.pool, one)
+                L.local.copy_(randn(*L.local.shape))
+            else:
+                L.pool.copy_(randn(*L.pool.shape))
+            L.sel.copy_(sel)
+            Ls.append(L)
+        torch.cuda.synchronize()
+        if kind == "tree":
+            us = graph_time(lambda i: Ls[i].attend_tree(q, tree_kv, par, nodes, seq), n_rot)
+        else:
+            us = graph_time(lambda i: Ls[i].attend(q, seq), n_rot)
+        got.append(round(us, 1))
+        del Ls
+        torch.cuda.empty_cache()
+    return got
+
+
+def section_packed(args, dev, hbm_peak):
+    """Entries in 4 bits beside bf16 ones: attention kernels, hand-over, the engine's step."""
+    from paper_2608_08097_b200 import binding, synth
+    kernels = []
+    for batch, Hq, Hkv, T, K in ((1, 32, 8, 1, 16), (16, 32, 8, 1, 128), (16, 32, 8, 5, 128), (16, 32, 8, 8, 128), (16, 32, 8, 16, 128),
+                                 (16, 32, 4, 9, 128), (16, 32, 8, 32, 128), (2, 32, 8, 1, 4096), (2, 32, 8, 5, 4096), (2, 32, 8, 16, 4096),
+                                 (2, 32, 8, 1, 8192)):
+        p, b, t = attention_pair(dev, args.seed, batch, Hq, Hkv, T, K)
+        kernels.append({"batch": batch, "q_heads": Hq, "kv_heads": Hkv, "tokens": T, "rows": T * Hq // Hkv, "columns": K + 2,
+                        "packed_us": p, "bf16_us": b, "bf16_tree_us": t})
+    # the hand-over of 16,384 dense blocks of 8 heads (1 GiB of bf16) into a packed pool
+    Bq, Hkv, mb = 8, 8, 2048
+    dims = binding.Dims(Bq, 32, Hkv, mb)
+    dk, dv = (torch.randn((Bq * mb, Hkv, 16, 128), device=dev).to(torch.bfloat16) for _ in range(2))
+    tbl = torch.arange(Bq * mb, dtype=torch.int32, device=dev).view(Bq, mb)
+    summ = torch.empty((Bq, Hkv, mb, 2, 128), dtype=torch.bfloat16, device=dev)
+    first, n = torch.zeros(Bq, dtype=torch.int32, device=dev), torch.full((Bq,), mb, dtype=torch.int32, device=dev)
+    hand_over = {}
+    for where in ("pinned", "hbm"):
+        pool = torch.empty((Bq * mb, Hkv, 2304), dtype=torch.uint8, device="cpu" if where == "pinned" else dev, pin_memory=where == "pinned")
+        us = graph_time(lambda i: binding.offload_blocks_packed(dims, dk, dv, tbl, tbl, first, n, mb, pool, summ), 1, iters=2, warm=1)
+        hand_over[where] = {"us": round(us, 1), "GBps_written": round(Bq * mb * Hkv * 2304 / us / 1e3, 2), "GBps_read": round(Bq * mb * Hkv * 8192 / us / 1e3, 1)}
+        del pool
+    del dk, dv, summ
+    torch.cuda.empty_cache()
+
+    # the step of the reasoning-style decode
+    opt = argparse.Namespace(config=1, layers=args.layers, batch=None, context=None, seed=args.seed, group=0, wait_group=0, transfer_group=0,
+                             transfer_kind="", again=2, steps=20, warmup=5, fetch_ratio=0.05)
+    cfg, _ = B.workload(opt)
+    bench = B.Bench(opt, cfg, dev, 0)
+    bench.h2d_peak, bench.hbm_peak = B.time_pinned_h2d(dev), hbm_peak
+    bench.generate(want_mirror=False, want_host=True)
+    w, cap = B.Work(bench, cfg.k_blocks, cfg.n_draft), B.cap_of(opt.fetch_ratio, cfg.k_blocks)
+    steps = []
+
+    def timed(eng, bits, where, group):
+        ms, clocks, _, _ = bench.timed(eng, w, 1, opt.warmup, opt.steps)
+        steps.append({"kv_bits": bits, "pool": where, "fused": eng.fused, "layers_per_gather": group, "ms_per_step": round(ms, 4),
+                      "ms_per_step_again": list(bench.again_ms), "us_per_layer": round(ms * 1e3 / cfg.layers, 1),
+                      "MB_gathered_per_layer": round(B.admitted_entries(eng) * (2304 if bits == 4 else 8192) / 1e6, 2),
+                      "sm_mhz": clocks["sm_mhz"], "reasons": clocks["reasons"]})
+    for where in ("pinned", "hbm"):
+        pools = bench.host_kv if where == "pinned" else [kv.to(dev) for kv in bench.host_kv]
+        eng = bench.engine(w, pools, cap)
+        timed(eng, 16, where, eng.transfer_group)
+        del eng, pools
+        torch.cuda.empty_cache()
+    n = cfg.layers
+    P, Hkv = bench.host_kv[0].shape[:2]
+    for where in ("pinned", "hbm"):
+        pools = [torch.empty((P, Hkv, 2304), dtype=torch.uint8, pin_memory=True) if where == "pinned" else
+                 torch.empty((P, Hkv, 2304), dtype=torch.uint8, device=dev) for _ in range(n)]
+        ratio = bench.link_ratio(w, cap) * 2304 / 8192
+        group = B.pick_transfer_group(ratio, n, bench.compute_us(w)) if where == "pinned" else 1
+        eng = bench.pipeline.DecodeEngine(cfg.batch, cfg.n_q_heads, Hkv, cfg.max_blocks, w.k, w.T, n, dev, mode="delta", cap=cap, append=True,
+                                          wait_group=bench.wait_group(), transfer_group=group, kv_bits=4)
+        for l in range(n):
+            eng.attach(l, pools[l], bench.tables[l])
+            kv = bench.host_kv[l].to(dev)
+            dense = kv[:, :, 0].contiguous(), kv[:, :, 1].contiguous()
+            eng.handover(l, *dense, bench.tables[l], bench.seq_dev[0].contiguous())
+            torch.cuda.synchronize()
+            del kv, dense
+        eng.prime([w.q_dev[l][0] for l in range(n)], bench.first_dev[0].contiguous(), bench.seq_dev[0].contiguous(), summaries_ready=True)
+        timed(eng, 4, where, group)
+        del eng, pools
+        torch.cuda.empty_cache()
+    print(json.dumps({"section": "packed", "workload": "kernels: one list of whole blocks and the local window, graph replay over working sets "
+                      "that L2 does not hold; steps: reasoning-style decode (batch %d, context %d, %d layers, %d tokens a step, budget %d blocks, at most %d new "
+                      "blocks per row), %d steps in one graph" % (cfg.batch, cfg.context, n, w.T, w.k, cap, opt.steps),
+                      "hbm_peak_GBps": hbm_peak, "pinned_h2d_peak_GBps": round(bench.h2d_peak, 2), "attention": kernels, "hand_over": hand_over, "steps": steps}))
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--seed", type=int, default=0)
     ap.add_argument("--what", default="c5,stage,shapes")
+    ap.add_argument("--layers", type=int, default=None, help="layers of the packed section's steps (default: the workload's)")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         raise SystemExit("bench_sweep.py needs a CUDA device: the product path has no CPU fallback")
@@ -223,7 +344,7 @@ def main():
     build.build()
     hbm_peak, _ = B.measured_peaks()
     for what in args.what.split(","):
-        {"c5": section_c5, "stage": section_stage, "shapes": section_shapes}[what](args, dev, hbm_peak)
+        {"c5": section_c5, "stage": section_stage, "shapes": section_shapes, "packed": section_packed}[what](args, dev, hbm_peak)
         torch.cuda.empty_cache()
 
 
