@@ -551,8 +551,8 @@ int oasis_stage_packed_layers(int32_t n_layers, const void *const *host_packed, 
  * b sits at position seq_len[b] + t; the keys are the tokens i of every column with blk_tbl[b][h][c] = j >= 0 and position
  * j * 16 + i <= seq_len[b] + t.
  *   out = softmax(scale * q K^T) V over the values that the entries stand for, bf16 tensor-core products with fp32 accumulation
- * and fp32 softmax statistics.  The softmax weights meet V in bf16: rounded once and divided by the sum of the rounded ones up to 32
- * query rows per KV head, as the sum of two bf16 terms above.
+ * and fp32 softmax statistics.  The softmax weights meet V in bf16: as the sum of two bf16 terms up to 4 query rows per KV head and
+ * above 32, rounded once and divided by the sum of the rounded ones between.
  *   q, out       [B][n_q_tokens][Hq][128] bf16;  n_q_tokens * (Hq/Hkv) may not exceed 128
  *   slot_tbl, blk_tbl   [B][Hkv][n_cols] int32 (device)
  *   packed_pool  may be NULL if local_col is 0, hbm_pool if local_col is n_cols

@@ -22,11 +22,15 @@
 // second product in bf16.  Rounded once (half a step, 2^-8 of a weight) they would put an output that one key decides off by up to 2.3
 // times as much as its own rounding to bf16 does: the reference lags behind the maximum, so that key's weight is rounded like any other.
 // packed_attn_kernel multiplies them as two terms (2^-17; 27.9 -> 30.8 us for 72 rows, ragged; a reference within 2^3 of the maximum,
-// whose raises cost more: 34.3); packed_attn_few_kernel takes them once, sums them as rounded by a product with ones, and scales its
-// accumulators by the ratio of the two sums, so that the error of a key that decides cancels (71.3 -> 72.9 us for 2 requests x 8,194
-// columns).  Against 64 bits outputs are off by at most 1.21 times what the rounding of the output alone costs (0.17 % of their norm)
-// over 90 drawn shapes, 1.00 times from 33 rows on.  Nothing overflows: the local values, which may be of any size, come first,
-// with weights of at most 1 (2^-20 in the accumulator's unit); a packed value is at most 2^15, its weight 2^32.
+// whose raises cost more: 34.3).  packed_attn_few_kernel has the second term in the half of a product that up to four rows leave empty:
+// 1.00 times the error of the output's own rounding (0.17 % of its norm, against 64 bits), as above 32 rows, where weights rounded once
+// had up to 1.65 times as much in a single row (1,500 drawn ones), for 17.0 -> 16.8 us (16 single tokens) and 72.5 -> 73.2 (2 requests x
+// 8,194 columns).  From 5 to 32 rows it takes them once, sums them as rounded by a product with ones, and scales its accumulators by the
+// ratio of the two sums, so that the error of a key that decides cancels: 1.05 times on average, 1.26 at most over 4,200 drawn cases of
+// one KV head.  A second term by products of its own costs there (one term: two) 16 requests x 130 columns, 20 rows 27.4: 30.7 us;
+// 2 x 4,098 columns, 8 rows 45.8: 49.1, 16 rows 57.7: 65.0, 20 rows 71.6: 83.5, 32 rows 87.2: 102.1; the bf16 attention rounds its
+// weights once too.  Nothing overflows: the local values, which may be of any size, come first, with weights of at most 1 (2^-20 in the
+// accumulator's unit); a packed value is at most 2^15, its weight 2^32.
 // What bounds it (32 query and 8 KV heads, a graph): unpacking takes a scheduler 466 of the about 700 instructions it issues per 128
 // tokens and 8 rows, on the half-rate integer and half-precision units; with 1,100 cycles a tile and SM 2 requests x 8,194 columns
 // take 72.9 us (4.1 TB/s), 16 requests x 130 columns 17.0 us, 5 of them first loads, list and end; with 20 rows 27.4 us, 8 warps per
@@ -645,7 +649,7 @@ packed_attn_kernel(const PackedAttnParams p)
 // ---- up to 32 query rows: every warp by itself ----------------------------------------------------------------------------
 // With few rows the products are small and what a tile costs above is mostly its way through five roles and their barriers: with 16
 // columns there, and two thread blocks per SM, 500 of 1,000 instructions of a scheduler per tile and 2,200 cycles of latency, 90.4 us
-// for 2 requests x 8,194 columns (16 rows of wider warp products, rows as their 16-row side: 86.5; this: 72.9).  Here a warp takes 32 tokens (two
+// for 2 requests x 8,194 columns (16 rows of wider warp products, rows as their 16-row side: 86.5; this: 73.2).  Here a warp takes 32 tokens (two
 // blocks) through unpacking, softmax and products alone, with warp-wide products of 16 tokens (or dims) x 8 query rows x 16: no
 // barrier but the arrival of its own copies.  The layout of the entries fits the products' operands, because the order of a
 // contraction is free.  With lane = (g, t) = (lane / 4, lane % 4):
@@ -684,10 +688,13 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
     return r;
 }
 
-template <int NT, bool CLUSTER>
+// TWO (up to four rows): rows 4 .. 7 of the product repeat rows 0 .. 3, and their weights are what the first four's lose in rounding to
+// bf16, so that the weights are two terms for no more products.
+template <int NT, bool TWO, bool CLUSTER>
 __global__ void __launch_bounds__(kPfThreads, pf_blocks(NT))
 packed_attn_few_kernel(const PackedAttnParams p)
 {
+    static_assert(!TWO || NT == 1, "two terms side by side in one product of eight rows");
     constexpr int STAGES = pf_stages(NT), ROWS = 8 * NT;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const base_ptr = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
@@ -731,7 +738,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
         near = make_int2(blk_row[p.local_col + tid], slot_row[p.local_col + tid]);
     // Q as the lanes of a product hold it: pair k of steps, lane (g, t): dims 32 t + 8 k .. + 7 of row g
     for (int i = tid; i < NT * 128; i += kPfThreads) {
-        const int lt = i & 31, k = (i >> 5) & 3, row = (i >> 7) * 8 + (lt >> 2);
+        const int lt = i & 31, k = (i >> 5) & 3, row = TWO ? (lt >> 2) & 3 : (i >> 7) * 8 + (lt >> 2);
         uint4 v = make_uint4(0, 0, 0, 0);
         if (row < rows) {
             const int tq = row / p.G, a = h * p.G + row % p.G;
@@ -794,6 +801,8 @@ packed_attn_few_kernel(const PackedAttnParams p)
     for (int nt = 0; nt < NT; ++nt) lw[nt][0] = lw[nt][1] = lw[nt][2] = lw[nt][3] = 0.f;
     float s[NT][4][2];                                                   // logits of a unit: token j of this lane, rows 2 t and 2 t + 1
     uint32_t pw[NT][4];                                                  // weights of a unit, as the operand of V^T P^T
+    const int row0 = TWO ? 2 * (t & 1) : 2 * t;                          // this lane's query rows 8 nt + row0, + 1
+    const float less = TWO && t >= 2 ? 1.f : 0.f;                        // the weights' second term
     const int kblk = g >> 2, ktok = 8 * ((g >> 1) & 1) + (g & 1);        // keys: token ktok + 2 j of block kblk
     // From logits to weights.  blk: the block of this lane's tokens; `mask`: some token may be hidden.
     auto softmax = [&](int blk, bool mask, float scale, float unit) {
@@ -806,7 +815,7 @@ packed_attn_few_kernel(const PackedAttnParams p)
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        if (8 * nt + 2 * t + e < n_min) s[nt][j][e] = -CUDART_INF_F;
+                        if (8 * nt + row0 + e < n_min) s[nt][j][e] = -CUDART_INF_F;
             }
         }
         float top = -CUDART_INF_F;
@@ -843,11 +852,16 @@ packed_attn_few_kernel(const PackedAttnParams p)
                 }
                 l[nt][0] += a;
                 l[nt][1] += c;
-                pw[nt][j] = transpose_8x8(pack_bf16x2(a * unit, c * unit));
+                a *= unit;
+                c *= unit;
+                uint32_t w = pack_bf16x2(a, c);
+                if (TWO) w = pack_bf16x2(fmaf(-less, __uint_as_float(w << 16), a), fmaf(-less, __uint_as_float(w & 0xffff0000u), c));
+                pw[nt][j] = transpose_8x8(w);
             }
     };
     // One more row of V^T, of ones: the sums of the weights as the product takes them.
     auto count_weights = [&](uint32_t one) {
+        if (TWO) return;                                                 // (two terms: nothing to make good)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             mma_16x8x16(lw[nt], one, one, one, one, pw[nt][0], pw[nt][1]);
@@ -1013,15 +1027,20 @@ packed_attn_few_kernel(const PackedAttnParams p)
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
             const int r = 8 * nt + 2 * t + e;
-            const float fit = lw[nt][e] == 0.f ? 1.f : __fdividef(sum, lw[nt][e]);  // (the accumulators are of rounded weights)
+            const float fit = TWO || lw[nt][e] == 0.f ? 1.f : __fdividef(sum, lw[nt][e]);  // (the accumulators are of rounded weights)
             if (g == 0) {
                 neg_m[warp * ROWS + r] = m_neg[nt][e];
                 l_sm[warp * ROWS + r] = sum;
             }
 #pragma unroll
             for (int m = 0; m < 8; ++m) {
-                o_mine[r * kPfPitch + 16 * m + g] = o[nt][m][e] * fit;
-                o_mine[r * kPfPitch + 16 * m + g + 8] = o[nt][m][2 + e] * fit;
+                float lo = o[nt][m][e], hi = o[nt][m][2 + e];
+                if (TWO) {                                               // both terms, in either row
+                    lo += __shfl_xor_sync(0xffffffffu, lo, 2);
+                    hi += __shfl_xor_sync(0xffffffffu, hi, 2);
+                }
+                o_mine[r * kPfPitch + 16 * m + g] = lo * fit;
+                o_mine[r * kPfPitch + 16 * m + g + 8] = hi * fit;
             }
         }
     }
@@ -1243,20 +1262,21 @@ extern "C" int oasis_packed_attn(const oasis_dims_t *dims, const void *q, int32_
         if (e == cudaSuccess) prefer_max_shared_carveout(__VA_ARGS__);                                                        \
         if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, __VA_ARGS__, p);                                                   \
     } while (0)
-#define OASIS_PACKED_LAUNCH(KERNEL, N, THREADS, SMEM)                                                                         \
+#define OASIS_PACKED_LAUNCH(THREADS, SMEM, KERNEL, ...)                                                                       \
     do {                                                                                                                      \
         cfg.blockDim = dim3(THREADS);                                                                                         \
         cfg.dynamicSmemBytes = SMEM;                                                                                          \
-        if (pl.in_cluster) OASIS_PACKED_LAUNCH_AS(KERNEL<N, true>);                                                           \
-        else OASIS_PACKED_LAUNCH_AS(KERNEL<N, false>);                                                                        \
+        if (pl.in_cluster) OASIS_PACKED_LAUNCH_AS(KERNEL<__VA_ARGS__, true>);                                                 \
+        else OASIS_PACKED_LAUNCH_AS(KERNEL<__VA_ARGS__, false>);                                                              \
     } while (0)
-    if (pl.n == 8) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 1, kPfThreads, pf_smem(1));
-    else if (pl.n == 16) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 2, kPfThreads, pf_smem(2));
-    else if (pl.n == 24) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 3, kPfThreads, pf_smem(3));
-    else if (pl.n == 32) OASIS_PACKED_LAUNCH(packed_attn_few_kernel, 4, kPfThreads, pf_smem(4));
-    else if (pl.n == 64) OASIS_PACKED_LAUNCH(packed_attn_kernel, 64, pa_threads(64), pa_smem(64));
-    else if (pl.n == 96) OASIS_PACKED_LAUNCH(packed_attn_kernel, 96, pa_threads(96), pa_smem(96));
-    else OASIS_PACKED_LAUNCH(packed_attn_kernel, 128, pa_threads(128), pa_smem(128));
+    if (pl.rows <= 4) OASIS_PACKED_LAUNCH(kPfThreads, pf_smem(1), packed_attn_few_kernel, 1, true);
+    else if (pl.n == 8) OASIS_PACKED_LAUNCH(kPfThreads, pf_smem(1), packed_attn_few_kernel, 1, false);
+    else if (pl.n == 16) OASIS_PACKED_LAUNCH(kPfThreads, pf_smem(2), packed_attn_few_kernel, 2, false);
+    else if (pl.n == 24) OASIS_PACKED_LAUNCH(kPfThreads, pf_smem(3), packed_attn_few_kernel, 3, false);
+    else if (pl.n == 32) OASIS_PACKED_LAUNCH(kPfThreads, pf_smem(4), packed_attn_few_kernel, 4, false);
+    else if (pl.n == 64) OASIS_PACKED_LAUNCH(pa_threads(64), pa_smem(64), packed_attn_kernel, 64);
+    else if (pl.n == 96) OASIS_PACKED_LAUNCH(pa_threads(96), pa_smem(96), packed_attn_kernel, 96);
+    else OASIS_PACKED_LAUNCH(pa_threads(128), pa_smem(128), packed_attn_kernel, 128);
 #undef OASIS_PACKED_LAUNCH
 #undef OASIS_PACKED_LAUNCH_AS
     if (e != cudaSuccess) {
