@@ -10,8 +10,10 @@
 // found in the groups' maxima and replaced before.  The part is put together in shared memory and leaves in 16-byte stores, whole
 // lines, because its place is usually in pinned host memory.  The block's summaries (minimum and maximum of the keys) come from
 // the same registers.  Algorithmic traffic: 8,192 B read, 2,304 B (and 512 B of summaries) written per (block, head).
-// Measured in device memory, 16,384 entries (a request of 32 K tokens, 8 heads): packing 39.3 us, 4.6 TB/s, the issue slots 52 % and
-// the integer units 47 % busy; into pinned host memory the link bounds it.  Unpacking 28.6 us, 6.0 TB/s, near what a copy reaches.
+// Measured in device memory, 16,384 entries (a request of 32 K tokens, 8 heads): packing 39.3 us, 4.6 TB/s.  No unit is full there
+// (issue slots 52 %, integer 47 %, HBM 43 %): a warp loads once, computes once and stores once, and 24 warps per SM (80 registers) do
+// not cover it.  The hand-over of 131,072 dense entries (1 GiB): 280 us into device memory, 5.73 ms into pinned host memory, where the
+// link bounds it (52.7 GB/s).  Unpacking 28.6 us, 6.0 TB/s, near what a copy reaches.
 // (Both with one warp per entry, divisions and two roundings: 115 us.)  One block of one head: 4.0 us, two dependent launches.
 #include "packed.cuh"
 

@@ -31,12 +31,14 @@
 // 2 x 4,098 columns, 8 rows 45.8: 49.1, 16 rows 57.7: 65.0, 20 rows 71.6: 83.5, 32 rows 87.2: 102.1; the bf16 attention rounds its
 // weights once too.  Nothing overflows: the local values, which may be of any size, come first, with weights of at most 1 (2^-20 in the
 // accumulator's unit); a packed value is at most 2^15, its weight 2^32.
-// What bounds it (32 query and 8 KV heads, a graph): unpacking takes a scheduler 466 of the about 700 instructions it issues per 128
-// tokens and 8 rows, on the half-rate integer and half-precision units; with 1,100 cycles a tile and SM 2 requests x 8,194 columns
-// take 72.9 us (4.1 TB/s), 16 requests x 130 columns 17.0 us, 5 of them first loads, list and end; with 20 rows 27.4 us, 8 warps per
-// SM, which their accumulators allow, and 800 cycles of products a tile.  From 33 rows on half of a tile's time is its way through
+// What bounds it (32 query and 8 KV heads, a graph): up to 8 rows a warp's chain of loads, unpacking, products and softmax at 16 warps per
+// SM: no unit is full (issue slots 54 %, integer 43 %, HBM 44 %), and unpacking is 466 of the about 700 instructions that a scheduler
+// issues per 128 tokens and 8 rows.  With 1,100 cycles a tile and SM 2 requests x 8,194 columns take 73.2 us (4.1 TB/s; the bf16 kernel
+// 171), 16 requests x 130 columns 16.8, 5 of them first loads, list and end (26.4); with 20 rows 27.4, 8 warps per SM, which their
+// accumulators allow, and 800 cycles of products a tile (27.2).  From 33 rows on half of a tile's time is its way through
 // copies, unpacking, products and softmax and their barriers (3,500 cycles at 72 rows, of which the exponential unit is busy for 768):
-// 16 requests x 130 columns 37.1 us under 64 rows, 44.6 under 72, 56.2 under 128.
+// 16 requests x 130 columns 36.4 us under 64 rows, 44.6 under 72, 55.4 under 128; the bf16 kernel, which copies and does not unpack, takes
+// 27.5 under 32 rows (here 33.4), 28.1 under 64 and 29.4 under 128, and 94.6 for 2 requests x 4,098 columns under 64 (here 98.4).
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -213,7 +215,7 @@ __device__ __forceinline__ void pa_finish(const PackedAttnParams &p, bool alive,
     }
 }
 
-// N: columns of the products (query rows, padded).
+// N: columns of the products (query rows, padded).  With 128 (72 registers a thread) 16 to 20 bytes are spilled, with 96 four.
 template <int N, bool CLUSTER>
 __global__ void __launch_bounds__(pa_threads(N), 1)
 packed_attn_kernel(const PackedAttnParams p)
@@ -659,7 +661,8 @@ packed_attn_kernel(const PackedAttnParams p)
 // Consecutive products go to different accumulators, and with 8 rows the logits have two sets (75.5 -> 71.3 us
 // before the weights were summed as rounded).
 // NT: products of 8 query rows.  Against it at the change-over, 2 requests x 4,098 columns: 32 rows 87.8 us here, 33 to 64 there 97;
-// 40 rows in two thread blocks of 20 here 119, there 83 (both with weights rounded once).
+// 40 rows in two thread blocks of 20 here 119, there 83 (both with weights rounded once).  25 to 32 rows spill 36 bytes at 255 registers, 9 to 16
+// rows four at 168, 5 to 8 rows in a cluster twelve at 128.
 constexpr int kPfThreads = 128, kPfWarps = 4;
 constexpr int kPfListCols = 768;                                         // columns of a split at most
 constexpr int kPfUnitBytes = 2 * kPackedBytes;
